@@ -58,7 +58,7 @@ enum {
   TGNN_EBOUNDS = -7    /* a device-side index check failed (reported through tgnn_status) */
 };
 
-enum { TGNN_F32 = 0, TGNN_BF16 = 1 };
+enum { TGNN_F32 = 0, TGNN_BF16 = 1, TGNN_F16 = 2 }; /* TGNN_F16: rows of the history operators only */
 
 /* math_mode: how the dense projections are computed.  Gates, softmax, loss, the
  * time encoding and Adam are always fp32. */
@@ -516,6 +516,61 @@ TGNN_API int tgnn_pack_rows(const float* memory, const double* last_update, int6
                             int64_t err_size);
 TGNN_API int tgnn_unpack_rows(float* memory, double* last_update, int64_t num_nodes, int d, const int32_t* nodes, int n,
                               const float* packed, int32_t* status, void* stream, char* err_host, int64_t err_size);
+
+/* ---- histories: sampling with sinks, a row cache in 4 or 8 bits, attention over it, slot attention ----
+ * The serving side of temporal attention, and its training side with a learned time bias.  With a bias by buckets of the time
+ * difference in place of an encoding inside the keys, a key and a value depend on their entry alone: they can be computed
+ * when the event arrives, kept in few bits beside the T-CSR, and read by every later root.
+ * Stateless, device pointers (except *_host), work enqueued on `stream` of the current device, nothing allocated; errors as above.
+ * status: device int32, NOT zeroed by these calls; 4 is recorded for an index outside its table (what then happens stands with each
+ * call; nothing is read or written out of range).
+ *
+ * History of a root (node, time): the entries of the node's T-CSR slice with ts < time, oldest first; `first` is the place of the
+ * slice's first entry, `len` their number.  With window w and s sinks a root sees the last w of them and the first s of the rest.
+ *
+ * tgnn_sample_window: first_out:int64[n], len_out:int32[n] of every root, and its slots, [n, window + sinks] each: the window, most recent
+ *   first, then the sinks, oldest first; cnt_out:int32[n] = slots in use, unused ones hold nbr = eid = -1, ts = 0.  Any output may be
+ *   NULL (nbr, eid are not read then).  A node outside [0, num_nodes) or a slice outside [0, num_entries) sees nothing (status 4).
+ *   window + sinks is 1 at least, and 65536 at most where slots are asked for.  Times are compared as fp64; NaN sees nothing. */
+TGNN_API int tgnn_sample_window(const int64_t* indptr, const int32_t* nbr, const int32_t* eid, const double* ts, int64_t num_nodes,
+                                int64_t num_entries, const int32_t* nodes, const double* times, int64_t n, int window, int sinks,
+                                int32_t* nbr_out, int32_t* eid_out, double* ts_out, int32_t* cnt_out, int64_t* first_out,
+                                int32_t* len_out, int32_t* status, void* stream, char* err_host, int64_t err_size);
+
+/* Row cache.  A row is `heads` groups of `dim` values (1 to 128).  A group is held as codes of 4 or 8 bits and one scale:
+ *   amax = max |x|; L = 7 or 127; scale = fp32(amax / L) rounded up to bf16; r = fp32(1 / scale);
+ *   code = the integer nearest to x * r, ties to even; the value read back is code * scale.
+ *   A group with amax < 2^-100 is held as zeros; one with an infinity or a NaN reads back as NaN, all of it.
+ * Row p has its codes at codes + p * code_stride (heads x tgnn_cache_code_bytes(dim, bits) bytes: a head's values in order, low bits
+ * first, each code + 8 or + 128, padded to 32, 64 or 128 values), its scales at scales + p * scale_stride (bf16[heads]) and its time
+ * (fp64) at times + p * time_stride; times may be NULL.  Strides in bytes, below 2^31: codes and code_stride multiples of 16, scales
+ * of 2, times of 8.  Separate arrays and records of one buffer are both described this way. */
+typedef struct tgnn_cache {
+  void* codes;
+  void* scales;
+  void* times;
+  int64_t rows;
+  int64_t code_stride;
+  int64_t scale_stride;
+  int64_t time_stride;
+  int32_t heads;
+  int32_t dim;
+  int32_t bits;
+  int32_t reserved;
+} tgnn_cache;
+TGNN_API int64_t tgnn_cache_code_bytes(int dim, int bits); /* of one head in a row: 16 to 128; -1 if out of range */
+
+/* tgnn_cache_write: cache row dst[i] = quantised rows[src[i]], i < n;   tgnn_cache_read: rows[dst[i]] = values of cache row src[i].
+ *   rows: num_rows rows of heads * dim values of `dtype` (TGNN_F32, TGNN_BF16, TGNN_F16), row_stride values apart; src, dst: indices of
+ *   index_bits (32 or 64) bits, NULL = i.  times: fp64[num_rows] moved along with the rows (write: from it, read: into it), or NULL.
+ *   dst must name distinct rows (one that is named twice is left with parts of several).  src outside its table: zeros are written
+ *   (codes, scale and time); dst outside: that row is skipped; status 4 for both.  n * heads is below 2^31. */
+TGNN_API int tgnn_cache_write(const tgnn_cache* cache_host, const void* rows, int dtype, int64_t num_rows, int64_t row_stride,
+                              const void* src, const void* dst, int index_bits, int64_t n, const double* times, int32_t* status,
+                              void* stream, char* err_host, int64_t err_size);
+TGNN_API int tgnn_cache_read(const tgnn_cache* cache_host, void* rows, int dtype, int64_t num_rows, int64_t row_stride,
+                             const void* src, const void* dst, int index_bits, int64_t n, double* times, int32_t* status,
+                             void* stream, char* err_host, int64_t err_size);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(_HERE, "libtgnn_b200.so")
 
 TGNN_OK, TGNN_EINVAL, TGNN_ESHAPE, TGNN_ECAPACITY, TGNN_ESTATE, TGNN_ECUDA, TGNN_ETIMEOUT, TGNN_EBOUNDS = (
     0, -1, -2, -3, -4, -5, -6, -7)
-TGNN_F32, TGNN_BF16 = 0, 1
+TGNN_F32, TGNN_BF16, TGNN_F16 = 0, 1, 2
 TGNN_MATH_FP32, TGNN_MATH_TF32, TGNN_MATH_TF32_FAST, TGNN_MATH_F16X3 = 0, 1, 2, 3
 
 PARAM_NAMES = ("time_w", "time_b", "gru_w_i", "gru_w_h", "gru_b_i", "gru_b_h", "w_q", "b_q", "w_k", "w_v",
@@ -37,7 +37,8 @@ EXPORTS = ("tgnn_create", "tgnn_destroy", "tgnn_last_error", "tgnn_param_count",
            "tgnn_controller_end_batch", "tgnn_controller_state", "tgnn_backward_scan_scratch", "tgnn_backward_scan",
            "tgnn_build_mixed", "tgnn_set_grad_sync", "tgnn_grad_buffer", "tgnn_apply_gradient", "tgnn_refresh_plan",
            "tgnn_pack_rows", "tgnn_unpack_rows", "tgnn_debug_get_embeddings", "tgnn_debug_gemm_split",
-           "tgnn_clear_status", "tgnn_order_streams")
+           "tgnn_clear_status", "tgnn_order_streams", "tgnn_sample_window", "tgnn_cache_code_bytes", "tgnn_cache_write",
+           "tgnn_cache_read")
 TGNN_STATIC_MAX_NODES = 65536
 
 
@@ -47,6 +48,12 @@ class TgnnConfig(C.Structure):
                 ("max_roots", C.c_int32), ("math_mode", C.c_int32),
                 ("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("model", C.c_int32), ("embed_aux", C.c_int32)]
+
+
+class TgnnCache(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("times", C.c_void_p), ("rows", C.c_int64),
+                ("code_stride", C.c_int64), ("scale_stride", C.c_int64), ("time_stride", C.c_int64),
+                ("heads", C.c_int32), ("dim", C.c_int32), ("bits", C.c_int32), ("reserved", C.c_int32)]
 
 
 class TgnnError(RuntimeError):
@@ -120,6 +127,12 @@ def load_library():
         lib.tgnn_refresh_plan.argtypes = [vp, vp, i64, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, i64]
         lib.tgnn_pack_rows.argtypes = [vp, vp, i64, i32, vp, i32, vp, vp, vp, vp, i64]
         lib.tgnn_unpack_rows.argtypes = [vp, vp, i64, i32, vp, i32, vp, vp, vp, vp, i64]
+        f32, cp = C.c_float, C.POINTER(TgnnCache)
+        lib.tgnn_sample_window.argtypes = [vp] * 4 + [i64, i64, vp, vp, i64, i32, i32] + [vp] * 9 + [i64]
+        lib.tgnn_cache_code_bytes.argtypes = [i32, i32]
+        lib.tgnn_cache_code_bytes.restype = i64
+        for fn in (lib.tgnn_cache_write, lib.tgnn_cache_read):
+            fn.argtypes = [cp, vp, i32, i64, i64, vp, vp, i32, i64, vp, vp, vp, vp, i64]
         _lib = lib
     return _lib
 
@@ -269,6 +282,137 @@ def pack_rows(memory, last_update, nodes, packed, status) -> int:
 def unpack_rows(memory, last_update, nodes, packed, status) -> int:
     """tgnn_unpack_rows: the state of nodes[i] becomes packed[i]."""
     return _rows(load_library().tgnn_unpack_rows, memory, last_update, nodes, packed, status)
+
+
+# ---- histories: sampling with sinks, row cache, attention over it, slot attention ----
+_ROW_TYPES = {torch.float32: TGNN_F32, torch.bfloat16: TGNN_BF16, torch.float16: TGNN_F16}
+
+
+def _stateless(fn, device, *args) -> int:
+    """Calls a stateless entry point on the current stream of the tensors' device; raises with its message."""
+    err = C.create_string_buffer(512)
+    here = torch.cuda.current_device()
+    if device.index == here:                      # the usual case, without the device switch
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(here), C.addressof(err), len(err))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _stream(), C.addressof(err), len(err))
+    if rc != TGNN_OK:
+        raise TgnnError(rc, err.value.decode())
+    return rc
+
+
+def _row_type(t: torch.Tensor, name: str) -> int:
+    if not t.is_cuda or t.dtype not in _ROW_TYPES:
+        raise TypeError(f"{name}: expected a CUDA tensor of float32, bfloat16 or float16, got {t.dtype} on {t.device}")
+    return _ROW_TYPES[t.dtype]
+
+
+def _same(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+    """Device pointer of a dense tensor of the type and device of `like` and the given shape."""
+    if t.dtype != like.dtype or t.device != like.device or t.shape != shape or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}, "
+                        f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _vec(t: Optional[torch.Tensor], dt: str, device, n, name: str, at_least: bool = False):
+    """Device pointer of a contiguous tensor of n elements (or at least n) on `device`; None -> NULL."""
+    if t is None:
+        return None
+    p = _dp(t, dt, name)
+    if t.device != device or (t.numel() < n if at_least else t.numel() != n):
+        raise TypeError(f"{name}: expected {'at least ' if at_least else ''}{n} elements on {device}, got {t.numel()} on {t.device}")
+    return p
+
+
+class RowCache:
+    """Rows of `heads` groups of `dim` values held in 4 or 8 bits, with a scale per group and (times) an fp64 time per row.
+
+    Separate arrays by default; with record=True one byte tensor `data` [rows, record_bytes] whose rows hold codes, time and
+    scales, so that a slice of rows can be sent as it is.  All rows are zeros at first."""
+
+    def __init__(self, rows: int, heads: int, dim: int, bits: int, times: bool = True, device="cuda", record: bool = False):
+        gb = load_library().tgnn_cache_code_bytes(dim, bits)
+        if gb < 0 or rows < 0 or not 1 <= heads <= 1024:
+            raise TgnnError(TGNN_EINVAL, f"RowCache: {rows} rows of {heads} heads of {dim} values in {bits} bits")
+        self.rows, self.heads, self.dim, self.bits = rows, heads, dim, bits
+        dev = torch.device(device)
+        if dev.type != "cuda":
+            raise TypeError(f"RowCache: expected a CUDA device, got {dev}")
+        if record:
+            at_time = heads * gb
+            at_scale = at_time + (8 if times else 0)
+            self.record_bytes = (at_scale + 2 * heads + 15) // 16 * 16
+            self.codes = self.scales = self.times = None
+            self.data = torch.zeros((rows, self.record_bytes), dtype=torch.uint8, device=dev)
+            self.device = self.data.device
+            p, r = self.data.data_ptr(), self.record_bytes
+            self.c = TgnnCache(p, p + at_scale, p + at_time if times else None, rows, r, r, r, heads, dim, bits, 0)
+        else:
+            self.data = None
+            self.codes = torch.zeros((rows, heads, gb), dtype=torch.uint8, device=dev)
+            self.scales = torch.zeros((rows, heads), dtype=torch.bfloat16, device=dev)
+            self.times = torch.zeros(rows, dtype=torch.float64, device=dev) if times else None
+            self.device = self.codes.device
+            self.c = TgnnCache(self.codes.data_ptr(), self.scales.data_ptr(), self.times.data_ptr() if times else None, rows,
+                               heads * gb, 2 * heads, 8, heads, dim, bits, 0)
+
+
+def _rows_of(cache: RowCache, rows: torch.Tensor):
+    """(type, number of rows, row stride) of [N, heads, dim] or [N, heads * dim] rows, dense within a row."""
+    dt = _row_type(rows, "rows")
+    width = cache.heads * cache.dim
+    inner = (cache.heads, cache.dim) if rows.dim() == 3 else (width,)
+    if rows.device != cache.device or tuple(rows.shape[1:]) != inner:
+        raise TypeError(f"rows: expected {cache.heads} x {cache.dim} values on {cache.device}, got {tuple(rows.shape)} on {rows.device}")
+    if rows.is_contiguous():
+        return dt, rows.shape[0], width
+    if rows.shape[0] > 1 and rows.stride(0) < width or not rows[0].is_contiguous():
+        raise TypeError(f"rows: a row's values must lie side by side and rows apart, got strides {rows.stride()}")
+    return dt, rows.shape[0], rows.stride(0)
+
+
+def _cache_move(fn, cache: RowCache, rows, status, src, dst, times, n) -> int:
+    dt, num, stride = _rows_of(cache, rows)
+    bits = 64
+    for t, name in ((src, "src"), (dst, "dst")):
+        if t is not None:
+            if t.dtype not in (torch.int32, torch.int64) or t.device != cache.device or not t.is_contiguous():
+                raise TypeError(f"{name}: expected a contiguous int32 or int64 tensor on {cache.device}")
+            bits = 32 if t.dtype == torch.int32 else 64
+    if src is not None and dst is not None and (src.dtype != dst.dtype or src.numel() != dst.numel()):
+        raise TypeError("src and dst: expected the same type and number of indices")
+    return _stateless(fn, cache.device, C.byref(cache.c), rows.data_ptr(), dt, num, stride, None if src is None else src.data_ptr(),
+                      None if dst is None else dst.data_ptr(), bits, n, _vec(times, "f64", cache.device, num, "times"),
+                      _vec(status, "i32", cache.device, 1, "status"))
+
+
+def cache_write(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
+    """tgnn_cache_write: cache row dst[i] = quantised rows[src[i]] (None: i), with times[src[i]]; as many rows as there are indices,
+    or as there are rows."""
+    n = src.numel() if src is not None else dst.numel() if dst is not None else rows.shape[0]
+    return _cache_move(load_library().tgnn_cache_write, cache, rows, status, src, dst, times, n)
+
+
+def cache_read(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
+    """tgnn_cache_read: rows[dst[i]] = values of cache row src[i] (None: i), times[dst[i]] = its time; as many rows as there are
+    indices, or as the cache holds."""
+    n = src.numel() if src is not None else dst.numel() if dst is not None else cache.rows
+    return _cache_move(load_library().tgnn_cache_read, cache, rows, status, src, dst, times, n)
+
+
+def sample_window(indptr, nbr, eid, ts, nodes, times, window: int, sinks: int, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out,
+                  status) -> int:
+    """tgnn_sample_window: history (first, len) and slots (window, then sinks) of every root; any output may be None, and nbr, eid
+    where their slots are."""
+    dev, n, P, S = ts.device, nodes.numel(), ts.numel(), window + sinks
+    return _stateless(
+        load_library().tgnn_sample_window, dev, _vec(indptr, "i64", dev, 1, "indptr", at_least=True), _vec(nbr, "i32", dev, P, "nbr"),
+        _vec(eid, "i32", dev, P, "eid"), _dp(ts, "f64", "ts"), indptr.numel() - 1, P, _vec(nodes, "i32", dev, n, "nodes"),
+        _vec(times, "f64", dev, n, "times"), n, window, sinks, _vec(nbr_out, "i32", dev, n * S, "nbr_out"),
+        _vec(eid_out, "i32", dev, n * S, "eid_out"), _vec(ts_out, "f64", dev, n * S, "ts_out"), _vec(cnt_out, "i32", dev, n, "cnt_out"),
+        _vec(first_out, "i64", dev, n, "first_out"), _vec(len_out, "i32", dev, n, "len_out"), _vec(status, "i32", dev, 1, "status"))
 
 
 class Controller:

@@ -1,0 +1,94 @@
+// Sampling of a history with a window and sinks: for every root the place of its node's first entry, the number of entries
+// strictly earlier than the root's time, and (where asked for) the slots: the most recent `window` of them, then the first
+// `sinks` of what the window leaves out.
+//
+// One warp per root.  The lower bound is found by a 32-way search, as for the most-recent-k search: the lanes probe 32 spread
+// positions with independent loads and a ballot picks the sub-range, so a slice of 2*10^7 entries costs 5 dependent loads.  The
+// slots of the window lie side by side in the T-CSR; the lanes copy 32 of them at a time.  Small batches are bound by the chain of
+// dependent loads (root, slice, search, slots), large ones by the slots' bytes.
+#include "tgnn_history.cuh"
+
+using namespace tgnn_history;
+
+namespace {
+
+__global__ void __launch_bounds__(256) sample_window_kernel(const int64_t* __restrict__ indptr, const int32_t* __restrict__ g_nbr,
+                                                            const int32_t* __restrict__ g_eid, const double* __restrict__ g_ts,
+                                                            int64_t N, int64_t P, const int32_t* __restrict__ nodes,
+                                                            const double* __restrict__ times, int n, int window, int sinks,
+                                                            int32_t* __restrict__ nbr_out, int32_t* __restrict__ eid_out,
+                                                            double* __restrict__ ts_out, int32_t* __restrict__ cnt_out,
+                                                            int64_t* __restrict__ first_out, int32_t* __restrict__ len_out,
+                                                            int32_t* status) {
+  const int lane = threadIdx.x & 31;
+  const int64_t root = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
+  if (root >= n) return;
+  const int node = nodes[root];
+  const double t = times[root];
+  int64_t base = 0, lo = 0, hi = 0;
+  const bool known = node >= 0 && node < N;
+  if (known) {
+    base = lo = indptr[node];
+    hi = indptr[node + 1];
+  }
+  // a node outside the graph, or a slice outside the entries: reported, nothing visible
+  if (!known || base < 0 || hi < base || hi > P || hi - base > 0x7fffffff) {
+    if (lane == 0) atomicMax(status, 4);
+    base = lo = hi = 0;
+  }
+  while (hi - lo > 32) {
+    const int64_t len = hi - lo;
+    const int64_t idx = lo + ((int64_t)(lane + 1) * len) / 33;            // in [lo, hi), non-decreasing in lane
+    const int c = __popc(__ballot_sync(FULL, g_ts[idx] < t));
+    const int64_t idx_hi = __shfl_sync(FULL, idx, c < 32 ? c : 31);       // first probe with ts >= t
+    const int64_t idx_lo = __shfl_sync(FULL, idx, c > 0 ? c - 1 : 0);     // last probe with ts < t
+    if (c < 32) hi = idx_hi;
+    if (c > 0) lo = idx_lo + 1;
+  }
+  lo += __popc(__ballot_sync(FULL, lane < hi - lo && g_ts[lo + lane] < t));
+  const int len = (int)(lo - base);
+  const int nw = min(len, window), ns = min(len - nw, sinks), slots = window + sinks;
+  if (lane == 0) {
+    if (first_out) first_out[root] = base;
+    if (len_out) len_out[root] = len;
+    if (cnt_out) cnt_out[root] = nw + ns;
+  }
+  if (!nbr_out && !eid_out && !ts_out) return;
+  const int64_t row = root * slots;
+  for (int j = lane; j < slots; j += 32) {
+    const bool in = j < nw + ns;
+    const int64_t e = j < nw ? base + len - 1 - j : base + (j - nw);
+    if (nbr_out) nbr_out[row + j] = in ? __ldg(g_nbr + e) : -1;
+    if (eid_out) eid_out[row + j] = in ? __ldg(g_eid + e) : -1;
+    if (ts_out) ts_out[row + j] = in ? __ldg(g_ts + e) : 0.0;
+  }
+}
+
+}  // namespace
+
+extern "C" int tgnn_sample_window(const int64_t* indptr, const int32_t* nbr, const int32_t* eid, const double* ts, int64_t num_nodes,
+                                  int64_t num_entries, const int32_t* nodes, const double* times, int64_t n, int window, int sinks,
+                                  int32_t* nbr_out, int32_t* eid_out, double* ts_out, int32_t* cnt_out, int64_t* first_out,
+                                  int32_t* len_out, int32_t* status, void* stream, char* err_host, int64_t err_size) {
+  const char* who = "tgnn_sample_window";
+  if (n < 0 || num_nodes < 0 || num_entries < 0 || window < 0 || sinks < 0 || (int64_t)window + sinks < 1)
+    return fail(err_host, err_size, TGNN_EINVAL, "%s: size out of range (window and sinks hold one slot at least)", who);
+  if (n > 0x7fffffff) return fail(err_host, err_size, TGNN_ECAPACITY, "%s: n beyond int32", who);
+  if ((nbr_out || eid_out || ts_out) && (int64_t)window + sinks > 65536)
+    return fail(err_host, err_size, TGNN_ECAPACITY, "%s: more than 65536 slots", who);
+  if (!status || (n > 0 && (!nodes || !times || (num_nodes > 0 && !indptr) || (num_entries > 0 && !ts))))
+    return fail(err_host, err_size, TGNN_EINVAL, "%s: null pointer", who);
+  if (num_entries > 0 && ((nbr_out && !nbr) || (eid_out && !eid)))
+    return fail(err_host, err_size, TGNN_EINVAL, "%s: slots of an array that is not given", who);
+  if ((((uintptr_t)indptr | (uintptr_t)ts | (uintptr_t)times | (uintptr_t)ts_out | (uintptr_t)first_out) & 7) ||
+      (((uintptr_t)nbr | (uintptr_t)eid | (uintptr_t)nodes | (uintptr_t)nbr_out | (uintptr_t)eid_out | (uintptr_t)cnt_out |
+        (uintptr_t)len_out | (uintptr_t)status) & 3))
+    return fail(err_host, err_size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", who);
+  if (n == 0) return TGNN_OK;
+  const unsigned grid = (unsigned)((n + 7) / 8);
+  sample_window_kernel<<<grid, 256, 0, (cudaStream_t)stream>>>(indptr, nbr, eid, ts, num_nodes, num_entries, nodes, times, (int)n, window,
+                                                              sinks, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out, status);
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return fail(err_host, err_size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(e));
+  return TGNN_OK;
+}

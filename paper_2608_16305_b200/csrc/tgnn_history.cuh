@@ -1,0 +1,134 @@
+// What the history operators share (row cache, attention over it, slot attention): error texts, row types, the time
+// buckets and the view of a row cache.
+#pragma once
+#include <cstdarg>
+#include <cstdio>
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/tgnn.h"
+
+namespace tgnn_history {
+
+constexpr unsigned FULL = 0xffffffffu;
+constexpr int kMaxBuckets = 128;
+constexpr float kLog2e = 1.4426950408889634f;
+
+inline int fail(char* err, int64_t size, int code, const char* fmt, ...) {
+  if (err && size > 0) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(err, (size_t)size, fmt, ap);
+    va_end(ap);
+  }
+  return code;
+}
+
+inline int elem_bytes(int dtype) { return dtype == TGNN_F32 ? 4 : 2; }
+inline bool known_dtype(int dtype) { return dtype == TGNN_F32 || dtype == TGNN_BF16 || dtype == TGNN_F16; }
+
+// Values that a head's codes are padded to: the readers' tiles of 32, 64 or 128.
+inline int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
+
+// Multiprocessors of the current device (asked for once per device; the answer cannot change).
+inline int num_sms() {
+  static int cached[64] = {};
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 148;
+  if (dev >= 0 && dev < 64 && cached[dev]) return cached[dev];
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
+  if (dev >= 0 && dev < 64) cached[dev] = n;
+  return n;
+}
+
+template <typename T>
+__device__ __forceinline__ float to_float(T x);
+template <>
+__device__ __forceinline__ float to_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <>
+__device__ __forceinline__ float to_float<__half>(__half x) { return __half2float(x); }
+// One rounding to the row type, to nearest even.
+template <typename T>
+__device__ __forceinline__ T from_float(float x);
+template <>
+__device__ __forceinline__ float from_float<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+
+// Words of VB bytes.
+template <int VB>
+struct Vec;
+template <>
+struct Vec<16> { typedef uint4 type; };
+template <>
+struct Vec<8> { typedef uint2 type; };
+template <>
+struct Vec<4> { typedef uint32_t type; };
+template <>
+struct Vec<2> { typedef uint16_t type; };
+
+// 2^x, relative error 2^-22; results below 2^-126 are 0.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Bucket of a time difference: how many of the n ascending bounds are <= dt.  The comparisons are in fp64, so a difference
+// on a bound lands where the definition says; NaN is above no bound.  Halving: ceil(log2(n + 1)) dependent loads.
+__device__ __forceinline__ int bucket_of(const double* bounds, int n, double dt) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (bounds[mid] <= dt) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// A row cache as the kernels see it (tgnn_cache with the codes' size).
+struct CacheView {
+  uint8_t* codes;
+  uint8_t* scales;
+  uint8_t* times;
+  int64_t rows, code_stride, scale_stride, time_stride;
+  int heads, dim, bits, code_bytes;      // code_bytes: of one head in a row
+};
+
+// Checks a cache description and fills its view; the entry point's name goes into the message.
+inline int check_cache(const char* who, const char* which, const tgnn_cache* c, CacheView* v, char* err, int64_t size) {
+  if (!c) return fail(err, size, TGNN_EINVAL, "%s: %s is null", who, which);
+  if (c->bits != 4 && c->bits != 8) return fail(err, size, TGNN_EINVAL, "%s: %s has %d bits (4 or 8)", who, which, c->bits);
+  if (c->dim < 1 || c->dim > 128 || c->heads < 1 || c->heads > 1024 || c->rows < 0)
+    return fail(err, size, TGNN_EINVAL, "%s: %s: size out of range (dim 1 to 128, heads 1 to 1024)", who, which);
+  const int gb = padded_dim(c->dim) * c->bits / 8;
+  if (c->rows > 0 && (!c->codes || !c->scales)) return fail(err, size, TGNN_EINVAL, "%s: %s: null pointer", who, which);
+  if (((uintptr_t)c->codes & 15) || (c->code_stride & 15) || ((uintptr_t)c->scales & 1) || (c->scale_stride & 1) ||
+      ((uintptr_t)c->times & 7) || (c->times && (c->time_stride & 7)))
+    return fail(err, size, TGNN_EINVAL, "%s: %s: codes must be 16-byte, scales 2-byte and times 8-byte aligned, strides too", who, which);
+  if (c->code_stride < (int64_t)c->heads * gb || c->scale_stride < 2 * (int64_t)c->heads || (c->times && c->time_stride < 8))
+    return fail(err, size, TGNN_EINVAL, "%s: %s: stride shorter than a row", who, which);
+  if (c->code_stride > 0x7fffffff || c->scale_stride > 0x7fffffff || (c->times && c->time_stride > 0x7fffffff))
+    return fail(err, size, TGNN_ECAPACITY, "%s: %s: stride beyond int32", who, which);
+  v->codes = (uint8_t*)c->codes;
+  v->scales = (uint8_t*)c->scales;
+  v->times = (uint8_t*)c->times;
+  v->rows = c->rows;
+  v->code_stride = c->code_stride;
+  v->scale_stride = c->scale_stride;
+  v->time_stride = c->time_stride;
+  v->heads = c->heads;
+  v->dim = c->dim;
+  v->bits = c->bits;
+  v->code_bytes = gb;
+  return TGNN_OK;
+}
+
+}  // namespace tgnn_history
