@@ -538,7 +538,7 @@ TGNN_API int tgnn_sample_window(const int64_t* indptr, const int32_t* nbr, const
                                 int32_t* len_out, int32_t* status, void* stream, char* err_host, int64_t err_size);
 
 /* Row cache.  A row is `heads` groups of `dim` values (1 to 128).  A group is held as codes of 4 or 8 bits and one scale:
- *   amax = max |x|; L = 7 or 127; scale = fp32(amax / L) rounded up to bf16; r = fp32(1 / scale);
+ *   amax = max |x|; L = 7 or 127; scale = fp32(amax * fp32(1 / L)) rounded up to bf16; r = fp32(1 / scale);
  *   code = the integer nearest to x * r, ties to even; the value read back is code * scale.
  *   A group with amax < 2^-100 is held as zeros; one with an infinity or a NaN reads back as NaN, all of it.
  * Row p has its codes at codes + p * code_stride (heads x tgnn_cache_code_bytes(dim, bits) bytes: a head's values in order, low bits
@@ -571,6 +571,22 @@ TGNN_API int tgnn_cache_write(const tgnn_cache* cache_host, const void* rows, in
 TGNN_API int tgnn_cache_read(const tgnn_cache* cache_host, void* rows, int dtype, int64_t num_rows, int64_t row_stride,
                              const void* src, const void* dst, int index_bits, int64_t n, double* times, int32_t* status,
                              void* stream, char* err_host, int64_t err_size);
+
+/* tgnn_cached_attend: attention of one query per root and head over the root's history, keys and values in row caches.
+ *   out[i, h] = sum_j a_j v_j over the entries j that root i sees (rows first[i] + j of the caches),
+ *   a = softmax_j(scale * q[i, h] . k_j + bias[h, bucket(times[i] - ts[first[i] + j])]),
+ *   bucket(dt) = number of bounds <= dt.  Query head h reads cached head h / (heads / kv_heads).
+ *   q, out: [n, heads, dim] of `dtype`, dense (out may not alias q); k, v: caches with the same rows, heads, dim and bits;
+ *   first:int64[n], len:int32[n] as from tgnn_sample_window; bias: fp32[heads, num_buckets] or NULL; with a bias bounds:
+ *   fp64[num_buckets - 1] ascending, times: fp64[n] and ts: fp64[k.rows] are needed (num_buckets 1 to 128).  window >= 0, sinks >= 0,
+ *   not both 0.  max_len: no root's len is above it, or 0 if unknown (it chooses the launch; results hold for any len).
+ *   A root that sees nothing, or whose logits are all -infinity, gets zeros; entries that it does not see do not touch its result.
+ *   A history outside the cache (first < 0, len < 0, first + len > rows) sees nothing, status 4.
+ *   n * kv_heads * ceil(heads / kv_heads / 8) is below 2^28.  Sums in an order fixed by the sizes and the device. */
+TGNN_API int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_host, const tgnn_cache* v_host, int64_t n, int heads,
+                                const int64_t* first, const int32_t* len, const float* bias, int num_buckets, const double* bounds,
+                                const double* times, const double* ts, int window, int sinks, int max_len, float scale, void* out,
+                                int32_t* status, void* stream, char* err_host, int64_t err_size);
 
 #ifdef __cplusplus
 }

@@ -41,7 +41,7 @@ def quantise(x, bits):
     with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
         amax = np.abs(x).max(-1)
         bad = ~np.isfinite(x).all(-1)
-        s = bf16_up((np.where(bad, 0.0, amax).astype(np.float32) / np.float32(7 if bits == 4 else 127)).astype(np.float32))
+        s = bf16_up((np.where(bad, 0.0, amax).astype(np.float32) * (np.float32(1) / np.float32(7 if bits == 4 else 127))).astype(np.float32))
         s = np.where(amax < 2.0 ** -100, np.float32(0), s).astype(np.float32)
         r = np.where(s > 0, np.float32(1) / s, np.float32(0)).astype(np.float32)
         codes = np.rint(np.where(bad[..., None], 0.0, x) * r[..., None].astype(np.float64))

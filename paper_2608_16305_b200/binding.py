@@ -38,7 +38,7 @@ EXPORTS = ("tgnn_create", "tgnn_destroy", "tgnn_last_error", "tgnn_param_count",
            "tgnn_build_mixed", "tgnn_set_grad_sync", "tgnn_grad_buffer", "tgnn_apply_gradient", "tgnn_refresh_plan",
            "tgnn_pack_rows", "tgnn_unpack_rows", "tgnn_debug_get_embeddings", "tgnn_debug_gemm_split",
            "tgnn_clear_status", "tgnn_order_streams", "tgnn_sample_window", "tgnn_cache_code_bytes", "tgnn_cache_write",
-           "tgnn_cache_read")
+           "tgnn_cache_read", "tgnn_cached_attend")
 TGNN_STATIC_MAX_NODES = 65536
 
 
@@ -133,6 +133,7 @@ def load_library():
         lib.tgnn_cache_code_bytes.restype = i64
         for fn in (lib.tgnn_cache_write, lib.tgnn_cache_read):
             fn.argtypes = [cp, vp, i32, i64, i64, vp, vp, i32, i64, vp, vp, vp, vp, i64]
+        lib.tgnn_cached_attend.argtypes = [vp, i32, cp, cp, i64, i32, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, i64]
         _lib = lib
     return _lib
 
@@ -413,6 +414,34 @@ def sample_window(indptr, nbr, eid, ts, nodes, times, window: int, sinks: int, n
         _vec(times, "f64", dev, n, "times"), n, window, sinks, _vec(nbr_out, "i32", dev, n * S, "nbr_out"),
         _vec(eid_out, "i32", dev, n * S, "eid_out"), _vec(ts_out, "f64", dev, n * S, "ts_out"), _vec(cnt_out, "i32", dev, n, "cnt_out"),
         _vec(first_out, "i64", dev, n, "first_out"), _vec(len_out, "i32", dev, n, "len_out"), _vec(status, "i32", dev, 1, "status"))
+
+
+def _bias_args(bias, bounds, times, ts, heads: int, n: int, entries: int, dev):
+    """Pointers of a time bias [heads, buckets] with bounds [buckets - 1], root times [n] and entry times."""
+    if bias is None:
+        return None, 0, None, None, None
+    if bias.dim() != 2 or bias.shape[0] != heads:
+        raise TypeError(f"bias: expected [heads = {heads}, buckets], got {tuple(bias.shape)}")
+    nb = bias.shape[1]
+    if times is None or ts is None or (bounds is None and nb > 1):
+        raise TypeError("a bias needs bounds, times and ts")
+    return (_vec(bias, "f32", dev, heads * nb, "bias"), nb, _vec(bounds, "f64", dev, nb - 1, "bounds"),
+            _vec(times, "f64", dev, n, "times"), _vec(ts, "f64", dev, entries, "ts", at_least=True))
+
+
+def cached_attend(q, k: RowCache, v: RowCache, first, length, window: int, sinks: int, out, status, bias=None, bounds=None, times=None,
+                  ts=None, max_len: int = 0, scale: Optional[float] = None) -> int:
+    """tgnn_cached_attend: q [n, heads, dim] over the window and sinks of the histories (first, length) in the caches.
+    scale defaults to 1 / sqrt(dim)."""
+    dt, dev = _row_type(q, "q"), q.device
+    if q.dim() != 3 or q.shape[2] != k.dim or k.device != dev or v.device != dev:
+        raise TypeError(f"q: expected [n, heads, dim = {k.dim}] on the caches' device, got {tuple(q.shape)} on {dev}")
+    n, heads, dim = q.shape
+    return _stateless(
+        load_library().tgnn_cached_attend, dev, _same(q, q, q.shape, "q"), dt, C.byref(k.c), C.byref(v.c), n, heads,
+        _vec(first, "i64", dev, n, "first"), _vec(length, "i32", dev, n, "length"),
+        *_bias_args(bias, bounds, times, ts, heads, n, k.rows, dev), window, sinks, max_len, dim ** -0.5 if scale is None else scale,
+        _same(out, q, q.shape, "out"), _vec(status, "i32", dev, 1, "status"))
 
 
 class Controller:

@@ -1,8 +1,8 @@
 // Row cache in 4 or 8 bits: rows are quantised as they are written and read back as the values their codes stand for.
 // A group is one head of one row (dim values):
-//     amax = max |x|,  L = 7 or 127,  scale = fp32(amax / L) rounded up to bf16,  r = fp32(1 / scale),
+//     amax = max |x|,  L = 7 or 127,  scale = fp32(amax * fp32(1 / L)) rounded up to bf16,  r = fp32(1 / scale),
 //     code = the integer nearest to the exact product x * r (ties to even),  value = code * scale.
-// The scale is rounded up so that |x * r| never passes L by more than the rounding of r, and no code needs clamping.  It is held
+// The scale is rounded up so that |x * r| never passes L by more than fp32's roundings, and no code needs clamping.  It is held
 // in 16 bits, as bf16, for its fp32 range: more of its bits would be lost on codes of 8 bits or less, and 2 bytes beside 16 to 128
 // of codes cost 2 to 12 % where fp32 would cost 3 to 25 %.  A group below 2^-100 is held as zeros (scale 0) so that 1 / scale
 // stays in range; a group with an infinity or a NaN has scale NaN and reads back as NaN, all of it, instead of as wrong numbers.
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const CacheView c,
     for (int j = 0; j < 8; ++j) amax = max_nan(amax, fabsf(v[u][j]));
     for (int o = lanes >> 1; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, o));
     const bool bad = !(amax <= 3.4028234e38f);
-    float s = __uint_as_float((__float_as_uint(__fdiv_rn(amax, BITS == 4 ? 7.f : 127.f)) + 0xffffu) & 0xffff0000u);
+    float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
     if (amax < 7.8886091e-31f) s = 0.f;                                   // 2^-100
     const float r = s > 0.f ? __frcp_rn(s) : 0.f;
     uint32_t w[BITS == 4 ? 1 : 2];

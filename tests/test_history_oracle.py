@@ -34,7 +34,7 @@ def test_quantiser_closed_forms(bits):
     # half a step from the value, and the bf16 scale at most 2^-7 above amax / L
     assert (np.abs(oh.dequantise(codes, s) - x) <= s[:, None] * (0.5 + 1e-5)).all()
     amax = np.abs(x).max(1)
-    assert (s * L >= amax * (1 - 2.0 ** -23)).all() and (s * L <= amax * (1 + 2.0 ** -7) * (1 + 2.0 ** -22)).all()
+    assert (s * L >= amax * (1 - 2.0 ** -22)).all() and (s * L <= amax * (1 + 2.0 ** -7) * (1 + 2.0 ** -22)).all()
 
 
 def test_bf16_up_is_the_next_number_above():

@@ -86,3 +86,18 @@ def test_binding_refuses_tensors_of_the_wrong_kind(lib):
     x = torch.zeros(4)
     with pytest.raises(TypeError):
         B.sample_window(x.long(), None, None, x.double(), x.int(), x.double(), 2, 1, None, None, None, None, None, None, x.int())
+
+
+@pytest.mark.parametrize("bad", [dict(q=None), dict(out=None), dict(first=None), dict(len=None), dict(status=None), dict(dtype=7), dict(n=-1),
+                                 dict(n=1 << 28), dict(heads=0), dict(heads=3), dict(heads=2048), dict(nb=0), dict(nb=129), dict(bounds=None),
+                                 dict(times=None), dict(ts=None), dict(window=-1), dict(sinks=-1), dict(window=0, sinks=0),
+                                 dict(max_len=-1), dict(q=PTR + 2), dict(out=PTR + 2), dict(first=PTR + 4), dict(len=PTR + 2),
+                                 dict(bias=PTR + 2), dict(ts=PTR + 4), dict(v=dict(bits=8, code_stride=128)), dict(v=dict(rows=9)),
+                                 dict(v=dict(dim=49)), dict(v=dict(heads=1)), dict(v=dict(codes=None)), dict(v=dict(codes=PTR + 8))], ids=str)
+def test_cached_attend(lib, bad):
+    a = dict(q=PTR, dtype=B.TGNN_F32, k={}, v={}, n=3, heads=4, first=PTR, len=PTR, bias=PTR, nb=8, bounds=PTR, times=PTR, ts=PTR, window=4,
+             sinks=2, max_len=0, scale=1.0, out=PTR, status=PTR)
+    a.update(bad)
+    a["k"], a["v"] = C.byref(_cache(**a["k"])), C.byref(_cache(**a["v"]))
+    rc, msg = _call(lib.tgnn_cached_attend, *a.values())
+    assert rc in (B.TGNN_EINVAL, B.TGNN_ECAPACITY, B.TGNN_ESHAPE) and "tgnn_cached_attend" in msg, (rc, msg)
