@@ -588,6 +588,25 @@ TGNN_API int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_ho
                                 const double* times, const double* ts, int window, int sinks, int max_len, float scale, void* out,
                                 int32_t* status, void* stream, char* err_host, int64_t err_size);
 
+/* tgnn_slot_attend: the same attention over sampled slots, for training: keys and values are rows of their own per (root, slot).
+ *   q, out: [n, heads, dim], k, v: [n, slots, kv_heads, dim], all of `dtype`, dense; cnt:int32[n]: a root's first cnt slots count (cnt
+ *   below 0 or above slots is taken as 0 or slots); bias, bounds, times as above, ts: fp64[n, slots].
+ * tgnn_slot_attend_backward: its gradients dq, dk, dv (of `dtype`) and dbias (fp32[heads, num_buckets], NULL where bias is) from
+ *   dout, recomputing the weights; needs nothing kept from the forward pass.  Slots beyond cnt get zero gradients.  All outputs are
+ *   overwritten, summed in an order fixed by the sizes and the device: the same call gives the same bits.
+ *   scratch: fp32[tgnn_slot_attend_scratch(n, heads, num_buckets)], 8-byte aligned, needed with dbias; it belongs to the call until the
+ *   call's work has ended (calls that may overlap, two captured graphs among them, need one each); contents undefined after.
+ *   heads * dim up to 2048, heads to 256, dim to 128, heads * num_buckets to 16384; slots 1 to 65536.  No output may alias an input. */
+TGNN_API int tgnn_slot_attend(const void* q, const void* k, const void* v, int dtype, int64_t n, int slots, int heads, int kv_heads, int dim,
+                              const int32_t* cnt, const float* bias, int num_buckets, const double* bounds, const double* times,
+                              const double* ts, float scale, void* out, void* stream, char* err_host, int64_t err_size);
+TGNN_API int64_t tgnn_slot_attend_scratch(int64_t n, int heads, int num_buckets);
+TGNN_API int tgnn_slot_attend_backward(const void* q, const void* k, const void* v, int dtype, int64_t n, int slots, int heads,
+                                       int kv_heads, int dim, const int32_t* cnt, const float* bias, int num_buckets,
+                                       const double* bounds, const double* times, const double* ts, float scale, const void* dout,
+                                       void* dq, void* dk, void* dv, float* dbias, float* scratch, void* stream, char* err_host,
+                                       int64_t err_size);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,7 @@ EXPORTS = ("tgnn_create", "tgnn_destroy", "tgnn_last_error", "tgnn_param_count",
            "tgnn_build_mixed", "tgnn_set_grad_sync", "tgnn_grad_buffer", "tgnn_apply_gradient", "tgnn_refresh_plan",
            "tgnn_pack_rows", "tgnn_unpack_rows", "tgnn_debug_get_embeddings", "tgnn_debug_gemm_split",
            "tgnn_clear_status", "tgnn_order_streams", "tgnn_sample_window", "tgnn_cache_code_bytes", "tgnn_cache_write",
-           "tgnn_cache_read", "tgnn_cached_attend")
+           "tgnn_cache_read", "tgnn_cached_attend", "tgnn_slot_attend", "tgnn_slot_attend_scratch", "tgnn_slot_attend_backward")
 TGNN_STATIC_MAX_NODES = 65536
 
 
@@ -134,6 +134,11 @@ def load_library():
         for fn in (lib.tgnn_cache_write, lib.tgnn_cache_read):
             fn.argtypes = [cp, vp, i32, i64, i64, vp, vp, i32, i64, vp, vp, vp, vp, i64]
         lib.tgnn_cached_attend.argtypes = [vp, i32, cp, cp, i64, i32, vp, vp, vp, i32, vp, vp, vp, i32, i32, i32, f32, vp, vp, vp, vp, i64]
+        slot = [vp, vp, vp, i32, i64, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, f32]
+        lib.tgnn_slot_attend.argtypes = slot + [vp, vp, vp, i64]
+        lib.tgnn_slot_attend_scratch.argtypes = [i64, i32, i32]
+        lib.tgnn_slot_attend_scratch.restype = i64
+        lib.tgnn_slot_attend_backward.argtypes = slot + [vp] * 8 + [i64]
         _lib = lib
     return _lib
 
@@ -442,6 +447,45 @@ def cached_attend(q, k: RowCache, v: RowCache, first, length, window: int, sinks
         _vec(first, "i64", dev, n, "first"), _vec(length, "i32", dev, n, "length"),
         *_bias_args(bias, bounds, times, ts, heads, n, k.rows, dev), window, sinks, max_len, dim ** -0.5 if scale is None else scale,
         _same(out, q, q.shape, "out"), _vec(status, "i32", dev, 1, "status"))
+
+
+def _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale):
+    dt, dev = _row_type(q, "q"), q.device
+    if q.dim() != 3 or k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[2]:
+        raise TypeError(f"expected q [n, heads, dim] and k [n, slots, kv_heads, dim], got {tuple(q.shape)} and {tuple(k.shape)}")
+    n, heads, dim = q.shape
+    slots, kv = k.shape[1], k.shape[2]
+    return [_same(q, q, q.shape, "q"), _same(k, q, k.shape, "k"), _same(v, q, k.shape, "v"), dt, n, slots, heads, kv, dim,
+            _vec(cnt, "i32", dev, n, "cnt"), *_bias_args(bias, bounds, times, ts, heads, n, n * slots, dev),
+            dim ** -0.5 if scale is None else scale]
+
+
+def slot_attend(q, k, v, cnt, out, bias=None, bounds=None, times=None, ts=None, scale: Optional[float] = None) -> int:
+    """tgnn_slot_attend: q [n, heads, dim] over the first cnt of k, v [n, slots, kv_heads, dim].  scale defaults to 1 / sqrt(dim)."""
+    a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
+    return _stateless(load_library().tgnn_slot_attend, q.device, *a, _same(out, q, q.shape, "out"))
+
+
+def slot_attend_scratch(n: int, heads: int, num_buckets: int) -> int:
+    """fp32 elements tgnn_slot_attend_backward needs as scratch."""
+    size = load_library().tgnn_slot_attend_scratch(n, heads, num_buckets)
+    if size < 0:
+        raise TgnnError(TGNN_EINVAL, "tgnn_slot_attend_scratch: size out of range")
+    return size
+
+
+def slot_attend_backward(q, k, v, cnt, dout, dq, dk, dv, bias=None, bounds=None, times=None, ts=None, dbias=None, scratch=None,
+                         scale: Optional[float] = None) -> int:
+    """tgnn_slot_attend_backward: gradients of slot_attend for dout, all overwritten."""
+    a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
+    n, heads, dev = q.shape[0], q.shape[1], q.device
+    nb = a[11]
+    if (bias is None) != (dbias is None) or (dbias is not None and scratch is None):
+        raise TypeError("dbias and scratch belong to a bias")
+    return _stateless(
+        load_library().tgnn_slot_attend_backward, dev, *a, _same(dout, q, q.shape, "dout"), _same(dq, q, q.shape, "dq"),
+        _same(dk, q, k.shape, "dk"), _same(dv, q, k.shape, "dv"), _vec(dbias, "f32", dev, heads * nb, "dbias"),
+        None if dbias is None else _vec(scratch, "f32", dev, slot_attend_scratch(n, heads, nb), "scratch", at_least=True))
 
 
 class Controller:

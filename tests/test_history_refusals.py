@@ -101,3 +101,34 @@ def test_cached_attend(lib, bad):
     a["k"], a["v"] = C.byref(_cache(**a["k"])), C.byref(_cache(**a["v"]))
     rc, msg = _call(lib.tgnn_cached_attend, *a.values())
     assert rc in (B.TGNN_EINVAL, B.TGNN_ECAPACITY, B.TGNN_ESHAPE) and "tgnn_cached_attend" in msg, (rc, msg)
+
+
+SLOT = dict(q=PTR, k=PTR, v=PTR, dtype=B.TGNN_F32, n=3, slots=5, heads=4, kv=2, dim=50, cnt=PTR, bias=PTR, nb=8, bounds=PTR, times=PTR, ts=PTR, scale=1.0)
+BAD_SLOTS = [dict(q=None), dict(k=None), dict(v=None), dict(cnt=None), dict(dtype=5), dict(n=-1), dict(n=1 << 31), dict(slots=0), dict(slots=65537),
+             dict(heads=0), dict(heads=3), dict(heads=512, kv=1, dim=1), dict(kv=0), dict(dim=0), dict(dim=129), dict(heads=32, dim=128), dict(nb=0),
+             dict(nb=129), dict(heads=256, kv=2, dim=8, nb=100), dict(bounds=None), dict(times=None), dict(ts=None), dict(q=PTR + 2), dict(k=PTR + 2),
+             dict(cnt=PTR + 2), dict(bias=PTR + 2), dict(bounds=PTR + 4), dict(ts=PTR + 4)]
+
+
+@pytest.mark.parametrize("bad", BAD_SLOTS, ids=str)
+def test_slot_attend(lib, bad):
+    a = dict(SLOT, **bad)
+    for fn, rest in ((lib.tgnn_slot_attend, [PTR]), (lib.tgnn_slot_attend_backward, [PTR] * 6)):
+        rc, msg = _call(fn, *a.values(), *rest)
+        assert rc in (B.TGNN_EINVAL, B.TGNN_ECAPACITY) and "tgnn_slot_attend" in msg, (rc, msg)
+
+
+@pytest.mark.parametrize("i,value", [(0, None), (1, None), (2, None), (3, None), (4, None), (5, None), (0, PTR + 1), (2, PTR + 2), (4, PTR + 2), (5, PTR + 4)])
+def test_slot_attend_outputs(lib, i, value):
+    rest = [PTR] * 6
+    rest[i] = value
+    assert _call(lib.tgnn_slot_attend_backward, *SLOT.values(), *rest)[0] == B.TGNN_EINVAL
+    if i == 0:
+        assert _call(lib.tgnn_slot_attend, *SLOT.values(), value)[0] == B.TGNN_EINVAL
+    assert _call(lib.tgnn_slot_attend_backward, *dict(SLOT, bias=None).values(), *[PTR] * 6)[0] == B.TGNN_EINVAL      # dbias without a bias
+
+
+def test_slot_attend_scratch(lib):
+    size = lib.tgnn_slot_attend_scratch
+    assert size(0, 2, 8) == 0 and size(10, 2, 8) == 320 and size(10 ** 6, 2, 8) == size(1024, 2, 8) and size(5, 2, 0) == 0
+    assert [size(*a) for a in ((-1, 2, 8), (1, 0, 8), (1, 257, 8), (1, 2, 129), (1, 2, -1))] == [-1] * 5
