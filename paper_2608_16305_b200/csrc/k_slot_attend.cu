@@ -8,14 +8,17 @@
 //
 // Keys and values are rows of their own per (root, slot): every byte of k and v is used once (forward) or for one root's gradients
 // (backward), so both passes are bound by HBM: k and v in, and for the backward pass dk and dv out.  Tensor cores have nothing to
-// gain on one query per row.  The backward pass recomputes the weights, which costs no traffic while a root's rows stay in
-// shared memory, and needs nothing of the forward pass.
+// gain on one query per row.  The backward pass recomputes the weights and needs nothing of the forward pass.
 //
-// A warp takes one root after another.  The rows of a root lie side by side; they are staged in the warp's own shared memory by
-// asynchronous copies in chunks of slots, the next chunk (of this root or the next) while one is worked on, so that two chunks
-// per warp are in flight or in use.  Roots with more slots than a chunk are walked twice by the backward pass: maximum, sum
-// and delta first, gradients then.  All sums are fp32; those of the bias, which run over the whole batch, fp64: each warp
-// keeps a table of its own and a second kernel adds the blocks' tables in a fixed order, so no atomics decide on a result.
+// A warp takes a root.  The values of one (slot, cached head) lie side by side; P lanes hold such a segment, NV words of VB bytes each,
+// so that a warp loads 32 / P segments at once straight into registers, four deep for k and v.  A dot product is then VB / size
+// multiplications and log2(P) shuffles.  Forward, every group of P lanes runs a softmax of its own over its slots (maximum, sum and
+// output in registers; the groups of a head are merged at the end), so nothing is written between k and the output.  Backward,
+// logits and dp go to shared memory for the root's slots, weights and dz are formed there, and a second walk over k (which lies
+// in L1 or L2 by then) sums dq while dk and dv are written.  Roots with more slots than a warp's shared memory holds are taken in
+// chunks: maximum, sum and delta over all of them first, gradients then.
+// All sums are fp32; those of the bias, which run over the whole batch, fp64: each warp keeps a table of its own and a second
+// kernel adds the blocks' tables in a fixed order, so no atomics decide on a result.
 // Logits stay in natural units: a bias of the type's lowest value is then still finite.
 #include "tgnn_history.cuh"
 
@@ -42,134 +45,206 @@ struct SlotArgs {
   float scale;
 };
 
-// A warp's shared memory, all parts multiples of 16 bytes: two stages of (K chunk, V chunk), then floats:
-// query [H * dim], output or dq [H * dim], (backward: dout [H * dim]), z [H * chunk], (backward: dp [H * chunk]),
-// per head m, l, corr, delta; bucket [chunk]; (backward with bias: table [H * buckets] fp64)
-__host__ __device__ inline int up16(int x) { return (x + 15) & ~15; }
+// A warp's shared memory, all parts multiples of 16 bytes: bucket [chunk] (bytes); backward: z and dp [chunk * H], per head m, 1 / l
+// and delta, dq [H * dim] where there are several chunks, and with a bias the table [H * buckets] in fp64.
 struct Layout {
-  int row, stage, q, o, g, z, dp, head, bucket, table, total;
+  int z, dp, head, dq, table, total;
 };
-__host__ __device__ inline Layout layout(int heads, int kv_heads, int dim, int chunk, int elem, bool backward, int table) {
+__host__ __device__ inline int up16(int x) { return (x + 15) & ~15; }
+__host__ __device__ inline Layout layout(int heads, int dim, int chunk, bool several, bool backward, int table) {
   Layout l;
-  l.row = kv_heads * dim * elem;
-  l.stage = up16(l.row * chunk);
-  int at = 4 * l.stage;
-  const int vec = up16(heads * dim * 4), hc = up16(heads * chunk * 4);
-  l.q = at; at += vec;
-  l.o = at; at += vec;
-  l.g = at; at += backward ? vec : 0;
-  l.z = at; at += hc;
-  l.dp = at; at += backward ? hc : 0;
-  l.head = at; at += up16(heads * 16);
-  l.bucket = at; at += up16(chunk * 4);
+  int at = up16(chunk);
+  l.z = at; at += backward ? up16(heads * chunk * 4) : 0;
+  l.dp = at; at += backward ? up16(heads * chunk * 4) : 0;
+  l.head = at; at += backward ? up16(heads * 16) : 0;
+  l.dq = at; at += backward && several ? up16(heads * dim * 4) : 0;
   l.table = at; at += up16(table * 8);
   l.total = at;
   return l;
 }
 
-template <int VB>
-__device__ __forceinline__ void copy_async(uint8_t* dst, const uint8_t* src) {
-  if constexpr (VB >= 4) {
-    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
-    if constexpr (VB == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
-    else if constexpr (VB == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(d), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(d), "l"(src) : "memory");
-  } else {
-    *reinterpret_cast<uint16_t*>(dst) = __ldg(reinterpret_cast<const uint16_t*>(src));
+// NV words of VB bytes of a segment, as they are in memory and as fp32.  Word i of lane `part` starts at value (i * P + part) * VE.
+template <typename T, int VB, int P, int NV>
+struct Seg {
+  static constexpr int VE = VB / (int)sizeof(T), N = NV * VE;
+  typedef typename Vec<VB>::type W;
+  W w[NV];
+  __device__ __forceinline__ void load(const T* p, int part, int dim, bool on) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      w[i] = W();
+      if (on && (i * P + part) * VE < dim) w[i] = __ldg(reinterpret_cast<const W*>(p) + i * P + part);
+    }
   }
+  __device__ __forceinline__ float at(int j) const {           // j: compile-time after unrolling
+    if constexpr (sizeof(T) == 4) {
+      return reinterpret_cast<const float*>(w)[j];
+    } else if constexpr (VB == 2) {
+      return to_float<T>(reinterpret_cast<const T*>(w)[j]);
+    } else {
+      const uint32_t x = reinterpret_cast<const uint32_t*>(w)[j >> 1];
+      if constexpr (sizeof(T) == 2 && is_bf16()) return __uint_as_float((j & 1) ? x & 0xffff0000u : x << 16);
+      else return to_float<T>(reinterpret_cast<const T*>(&x)[j & 1]);
+    }
+  }
+  static __device__ constexpr bool is_bf16();
+  static __device__ __forceinline__ void store(T* p, int part, int dim, const float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      union { W w; T e[VE]; } u;
+#pragma unroll
+      for (int e = 0; e < VE; ++e) u.e[e] = from_float<T>(x[i * VE + e]);
+      if ((i * P + part) * VE < dim) reinterpret_cast<W*>(p)[i * P + part] = u.w;
+    }
+  }
+};
+template <typename T>
+struct IsBf16 { static constexpr bool value = false; };
+template <>
+struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
+template <typename T, int VB, int P, int NV>
+__device__ constexpr bool Seg<T, VB, P, NV>::is_bf16() { return IsBf16<T>::value; }
+
+template <int P>
+__device__ __forceinline__ float sum_p(float x) {              // over the lanes of a segment
+#pragma unroll
+  for (int o = 1; o < P; o <<= 1) x += __shfl_xor_sync(FULL, x, o);
+  return x;
 }
 
-// E neighbouring values as fp32
-template <typename T, int E>
-__device__ __forceinline__ void load_e(const T* p, float (&x)[E]) {
-  if constexpr (E == 1) {
-    x[0] = to_float<T>(*p);
-  } else if constexpr (sizeof(T) == 4) {
-    const float2 f = *reinterpret_cast<const float2*>(p);
-    x[0] = f.x;
-    x[1] = f.y;
-  } else {
-    union { uint32_t w; T e[2]; } u;
-    u.w = *reinterpret_cast<const uint32_t*>(p);
-    x[0] = to_float<T>(u.e[0]);
-    x[1] = to_float<T>(u.e[1]);
-  }
-}
-template <typename T, int E>
-__device__ __forceinline__ void store_e(T* p, const float (&x)[E]) {
-  if constexpr (E == 1) {
-    *p = from_float<T>(x[0]);
-  } else if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
-  } else {
-    union { uint32_t w; T e[2]; } u;
-    u.e[0] = from_float<T>(x[0]);
-    u.e[1] = from_float<T>(x[1]);
-    *reinterpret_cast<uint32_t*>(p) = u.w;
-  }
-}
+constexpr int UN = 4;                                          // segments of k and of v in flight per lane
 
-// What a warp works on: chunk `c` of root `r`, in sweep 0 (maximum, sum, delta) or 1 (gradients; backward passes over several
-// chunks only).  A root without slots is one empty chunk.
-struct Item {
-  int64_t r;
-  int c, sweep, cnt;
+// Which segments a lane takes: 32 / P of them at a time, KC neighbouring cached heads of RPI neighbouring slots.
+template <int P>
+struct Lanes {
+  int part, kc, KC, row, RPI;
+  __device__ __forceinline__ Lanes(int lane, int kv_heads) {
+    constexpr int NG = 32 / P;
+    part = lane & (P - 1);
+    KC = min(NG, kv_heads & -kv_heads);                        // powers of two
+    RPI = NG / KC;
+    kc = (lane / P) & (KC - 1);
+    row = (lane / P) / KC;
+  }
 };
 
-// One root's slots against one vector per head: out[h * chunk + s] = x[h] . rows[s][h / group], s < ns.
-// A lane takes a (slot, head) pair, or a part of one where there are fewer pairs than lanes.  Lanes start at different columns, so that
-// rows a multiple of 128 bytes long do not meet in one bank.
-template <typename T, int E>
-__device__ __forceinline__ void dots(const SlotArgs& a, const T* rows, const float* x, float* out, int ns, int lane) {
-  const int pairs = ns * a.heads, row = a.kv_heads * a.dim, steps = a.dim / E;
-  int lg = 0;                                                  // 2^lg lanes per pair
-  while (lg < 3 && (pairs << (lg + 1)) <= 32) ++lg;
-  const int part = lane & ((1 << lg) - 1), per = 32 >> lg;
-  for (int p0 = 0; p0 < pairs; p0 += per) {
-    const int p = p0 + (lane >> lg);
-    float acc = 0.f;
-    int h = 0, s = 0;
-    if (p < pairs) {
-      s = p / a.heads;
-      h = p - s * a.heads;
-      const T* kr = rows + s * row + (h / a.group) * a.dim;
-      const float* xr = x + h * a.dim;
-      const int mine = (steps - part + (1 << lg) - 1) >> lg;   // steps part, part + 2^lg, ...
-      if (mine > 0) {
-        int i = (lane >> lg) % mine;
-        for (int j = 0; j < mine; ++j) {
-          const int e = (part + (i << lg)) * E;
-          float kx[E], xx[E];
-          load_e<T, E>(kr + e, kx);
-          load_e<float, E>(xr + e, xx);
-#pragma unroll
-          for (int q = 0; q < E; ++q) acc = fmaf(kx[q], xx[q], acc);
-          if (++i == mine) i = 0;
-        }
-      }
-    }
-    for (int o = 1; o < (1 << lg); o <<= 1) acc += __shfl_xor_sync(FULL, acc, o);
-    if (p < pairs && part == 0) out[h * a.chunk + s] = acc;
-  }
+__device__ __forceinline__ void fill_buckets(const SlotArgs& a, const double* s_bounds, uint8_t* bucket, int64_t r, int s0, int s1, int lane) {
+  if (!a.bias) return;
+  const double t = a.times[r];
+  for (int s = s0 + lane; s < s1; s += 32) bucket[s - s0] = (uint8_t)bucket_of(s_bounds, a.buckets - 1, t - __ldg(a.ts + r * a.slots + s));
 }
 
-template <typename T, int VB, int E, bool BACKWARD>
-__global__ void __launch_bounds__(32 * MAX_WARPS) slot_attend_kernel(const SlotArgs a) {
+template <typename T, int VB, int P, int NV>
+__global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const SlotArgs a) {
+  using S = Seg<T, VB, P, NV>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  const int H = a.heads, D = a.dim, HD = H * D, ROW = a.kv_heads * D;
-  const bool table = BACKWARD && a.partial != nullptr;
-  const Layout L = layout(H, a.kv_heads, D, a.chunk, (int)sizeof(T), BACKWARD, table ? H * a.buckets : 0);
+  uint8_t* bucket = smem + (size_t)wid * a.warp_bytes;
+  if (a.bias) {
+    for (int i = threadIdx.x; i < a.buckets - 1; i += blockDim.x) s_bounds[i] = a.bounds[i];
+    __syncthreads();
+  }
+  const Lanes<P> me(lane, a.kv_heads);
+  const int D = a.dim, ROW = a.kv_heads * D;
+  const int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  if (r >= a.n) return;
+  const int cnt = min(max(a.cnt[r], 0), a.slots);
+  const bool several = cnt > a.chunk;
+  if (!several) fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
+  __syncwarp();
+  const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
+  const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
+  for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
+    const int kv = kv0 + me.kc;
+    for (int g = 0; g < a.group; ++g) {
+      const int h = kv * a.group + g;
+      S q;
+      q.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
+      const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
+      float m = -INFINITY, l = 0.f, acc[S::N];
+#pragma unroll
+      for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
+      for (int c0 = 0; c0 < cnt; c0 += a.chunk) {
+        const int c1 = min(cnt, c0 + a.chunk);
+        if (several) {
+          __syncwarp();
+          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
+          __syncwarp();
+        }
+        for (int s0 = c0; s0 < c1; s0 += UN * me.RPI) {
+          S k[UN], v[UN];
+          float z[UN];
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            const int s = s0 + u * me.RPI + me.row;
+            k[u].load(kr + (int64_t)s * ROW + kv * D, me.part, D, s < c1);
+          }
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            const int s = s0 + u * me.RPI + me.row;
+            v[u].load(vr + (int64_t)s * ROW + kv * D, me.part, D, s < c1);
+          }
+          float top = m;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            const int s = s0 + u * me.RPI + me.row;
+            float x = 0.f;
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) x = fmaf(k[u].at(j), q.at(j), x);
+            x = sum_p<P>(x) * a.scale;
+            if (bias && s < c1) x += __ldg(bias + bucket[s - c0]);
+            z[u] = s < c1 ? x : -INFINITY;
+            top = fmaxf(top, z[u]);
+          }
+          const float base = top == -INFINITY ? 0.f : top;     // nothing but -infinity: weights are 0
+          const float corr = exp2_fast((m - base) * kLog2e);   // m = -infinity: 0
+          m = top;
+          l *= corr;
+#pragma unroll
+          for (int j = 0; j < S::N; ++j) acc[j] *= corr;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            const float p = exp2_fast((z[u] - base) * kLog2e);
+            l += p;
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) acc[j] = fmaf(p, v[u].at(j), acc[j]);
+          }
+        }
+      }
+      // the groups of lanes that shared a head's slots
+      for (int o = P * me.KC; o < 32; o <<= 1) {
+        const float om = __shfl_xor_sync(FULL, m, o), top = fmaxf(m, om);
+        const float base = top == -INFINITY ? 0.f : top;
+        const float f = exp2_fast((m - base) * kLog2e), of = exp2_fast((om - base) * kLog2e);
+        m = top;
+        l = l * f + __shfl_xor_sync(FULL, l, o) * of;
+#pragma unroll
+        for (int j = 0; j < S::N; ++j) acc[j] = acc[j] * f + __shfl_xor_sync(FULL, acc[j], o) * of;
+      }
+      const float f = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+      for (int j = 0; j < S::N; ++j) acc[j] *= f;
+      if (me.row == 0) S::store(reinterpret_cast<T*>(a.out) + (r * a.heads + h) * D, me.part, D, acc);
+    }
+  }
+}
+
+template <typename T, int VB, int P, int NV>
+__global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const SlotArgs a) {
+  using S = Seg<T, VB, P, NV>;
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ double s_bounds[kMaxBuckets];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  const int H = a.heads, D = a.dim, ROW = a.kv_heads * D;
+  const bool table = a.partial != nullptr;
+  const Layout L = layout(H, D, a.chunk, a.chunk < a.slots, true, table ? H * a.buckets : 0);
   uint8_t* my = smem + (size_t)wid * a.warp_bytes;
-  float* q = reinterpret_cast<float*>(my + L.q);
-  float* o = reinterpret_cast<float*>(my + L.o);
-  float* g = reinterpret_cast<float*>(my + L.g);
-  float* z = reinterpret_cast<float*>(my + L.z);
-  float* dp = reinterpret_cast<float*>(my + L.dp);
-  float* s_m = reinterpret_cast<float*>(my + L.head);
-  float *s_l = s_m + H, *s_c = s_m + 2 * H, *s_d = s_m + 3 * H;
-  int* bucket = reinterpret_cast<int*>(my + L.bucket);
+  uint8_t* bucket = my;
+  float* z = reinterpret_cast<float*>(my + L.z);               // [slot][head]: logits, then weights
+  float* dp = reinterpret_cast<float*>(my + L.dp);             // [slot][head]: do . v, then dz
+  float *s_m = reinterpret_cast<float*>(my + L.head), *s_l = s_m + H, *s_d = s_m + 2 * H;
+  float* s_dq = reinterpret_cast<float*>(my + L.dq);
   double* tab = reinterpret_cast<double*>(my + L.table);
   if (a.bias) {
     for (int i = threadIdx.x; i < a.buckets - 1; i += blockDim.x) s_bounds[i] = a.bounds[i];
@@ -178,242 +253,213 @@ __global__ void __launch_bounds__(32 * MAX_WARPS) slot_attend_kernel(const SlotA
     for (int i = lane; i < H * a.buckets; i += 32) tab[i] = 0.0;
   }
   __syncthreads();
-
-  const int64_t stride = (int64_t)gridDim.x * a.warps;
-  auto count = [&](int64_t r) { return r < a.n ? min(max(a.cnt[r], 0), a.slots) : 0; };
-  int64_t next_r = (int64_t)blockIdx.x * a.warps + wid;        // the root behind the item's
-  int next_cnt = count(next_r);
-  auto advance = [&](Item it) {
-    const int chunks = it.cnt > 0 ? (it.cnt + a.chunk - 1) / a.chunk : 1;
-    if (++it.c < chunks) return it;
-    it.c = 0;
-    if (BACKWARD && it.sweep == 0 && chunks > 1) { it.sweep = 1; return it; }
-    it.sweep = 0;
-    it.r = next_r;
-    it.cnt = next_cnt;
-    next_r += stride;
-    next_cnt = count(next_r);
-    return it;
-  };
-  auto stage = [&](const Item& it, int buf) {
-    if (it.r < a.n) {
-      const int s0 = it.c * a.chunk, ns = min(a.chunk, it.cnt - s0);
-      const int64_t at = (it.r * a.slots + s0) * ROW * (int64_t)sizeof(T);
-      const uint8_t* kp = reinterpret_cast<const uint8_t*>(a.k) + at;
-      const uint8_t* vp = reinterpret_cast<const uint8_t*>(a.v) + at;
-      uint8_t* ks = my + 2 * buf * L.stage;
-      uint8_t* vs = ks + L.stage;
-      const int bytes = max(ns, 0) * L.row;                    // a last word may reach into the root's next slot, never beyond its rows
-      for (int i = lane * VB; i < bytes; i += 32 * VB) copy_async<VB>(ks + i, kp + i);
-      for (int i = lane * VB; i < bytes; i += 32 * VB) copy_async<VB>(vs + i, vp + i);
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-
-  Item cur;
-  cur.r = next_r;
-  cur.cnt = next_cnt;
-  cur.c = cur.sweep = 0;
-  next_r += stride;
-  next_cnt = count(next_r);
-  int buf = 0;
-  stage(cur, 0);
-  while (cur.r < a.n) {
-    const Item nxt = advance(cur);
-    stage(nxt, buf ^ 1);
-    const int64_t r = cur.r;
-    const int s0 = cur.c * a.chunk, ns = max(min(a.chunk, cur.cnt - s0), 0);
-    const int chunks = cur.cnt > 0 ? (cur.cnt + a.chunk - 1) / a.chunk : 1;
-    const bool last = cur.c == chunks - 1;
-    if (cur.c == 0 && cur.sweep == 0) {                        // a new root
-      const T* qg = reinterpret_cast<const T*>(a.q) + r * HD;
-      for (int i = lane * E; i < HD; i += 32 * E) {
-        float x[E];
-        load_e<T, E>(qg + i, x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) { q[i + e] = x[e]; o[i + e] = 0.f; }
-      }
-      if (BACKWARD) {
-        const T* gg = reinterpret_cast<const T*>(a.dout) + r * HD;
-        for (int i = lane * E; i < HD; i += 32 * E) {
-          float x[E];
-          load_e<T, E>(gg + i, x);
-#pragma unroll
-          for (int e = 0; e < E; ++e) g[i + e] = x[e];
-        }
-      }
-      for (int h = lane; h < H; h += 32) { s_m[h] = -INFINITY; s_l[h] = 0.f; s_d[h] = 0.f; }
-    }
-    if (a.bias) {
-      const double t = a.times[r];
-      for (int s = lane; s < ns; s += 32) bucket[s] = bucket_of(s_bounds, a.buckets - 1, t - __ldg(a.ts + r * a.slots + s0 + s));
-    }
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
-    __syncwarp();
-    const T* ks = reinterpret_cast<const T*>(my + 2 * buf * L.stage);
-    const T* vs = reinterpret_cast<const T*>(my + 2 * buf * L.stage + L.stage);
-    dots<T, E>(a, ks, q, z, ns, lane);
-    if (BACKWARD) dots<T, E>(a, vs, g, dp, ns, lane);
+  const Lanes<P> me(lane, a.kv_heads);
+  for (int64_t r = (int64_t)blockIdx.x * a.warps + wid; r < a.n; r += (int64_t)gridDim.x * a.warps) {
+    const int cnt = min(max(a.cnt[r], 0), a.slots);
+    const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
+    const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
+    T* dkr = reinterpret_cast<T*>(a.dk) + r * a.slots * ROW;
+    T* dvr = reinterpret_cast<T*>(a.dv) + r * a.slots * ROW;
+    const T* qr = reinterpret_cast<const T*>(a.q) + r * H * D;
+    const T* gr = reinterpret_cast<const T*>(a.dout) + r * H * D;
+    T* dqr = reinterpret_cast<T*>(a.dq) + r * H * D;
+    const bool several = cnt > a.chunk;
+    for (int h = lane; h < H; h += 32) { s_m[h] = -INFINITY; s_l[h] = s_d[h] = 0.f; }
     __syncwarp();
 
-    // softmax of the chunk: 2^lg lanes per head, 32 / 2^lg heads at a time
-    {
-      int lg = 5;
-      while (lg > 0 && (H << lg) > 32) --lg;
-      const int per = 32 >> lg, part = lane & ((1 << lg) - 1);
-      for (int h0 = 0; h0 < H; h0 += per) {
-        const int h = h0 + (lane >> lg);
-        const bool in = h < H;
-        float* zh = z + h * a.chunk;
-        float top = in ? s_m[h] : -INFINITY;
-        const float was = top;
-        if (in) {
-          for (int s = part; s < ns; s += 1 << lg) {
-            float x = zh[s] * a.scale;
-            if (a.bias) x += __ldg(a.bias + h * a.buckets + bucket[s]);
-            zh[s] = x;
-            top = fmaxf(top, x);
+    for (int sweep = 0; sweep < (several ? 2 : 1); ++sweep) {
+      for (int c0 = 0; c0 == 0 || c0 < cnt; c0 += a.chunk) {
+        const int ns = min(cnt - c0, a.chunk);
+        fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane);
+        __syncwarp();
+        // logits and dp of the chunk
+        for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
+          const int kv = kv0 + me.kc;
+          for (int g = 0; g < a.group; ++g) {
+            const int h = kv * a.group + g;
+            S q, go;
+            q.load(qr + h * D, me.part, D, true);
+            go.load(gr + h * D, me.part, D, true);
+            const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
+            for (int s0 = 0; s0 < ns; s0 += UN * me.RPI) {
+              S k[UN], v[UN];
+#pragma unroll
+              for (int u = 0; u < UN; ++u) {
+                const int s = s0 + u * me.RPI + me.row;
+                k[u].load(kr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
+              }
+#pragma unroll
+              for (int u = 0; u < UN; ++u) {
+                const int s = s0 + u * me.RPI + me.row;
+                v[u].load(vr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
+              }
+#pragma unroll
+              for (int u = 0; u < UN; ++u) {
+                const int s = s0 + u * me.RPI + me.row;
+                float x = 0.f, y = 0.f;
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) {
+                  x = fmaf(k[u].at(j), q.at(j), x);
+                  y = fmaf(v[u].at(j), go.at(j), y);
+                }
+                x = sum_p<P>(x);
+                y = sum_p<P>(y);
+                if (me.part == 0 && s < ns) {
+                  x *= a.scale;
+                  if (bias) x += __ldg(bias + bucket[s]);
+                  z[s * H + h] = x;
+                  dp[s * H + h] = y;
+                }
+              }
+            }
           }
         }
-        if (cur.sweep == 0) {
-          for (int w = 1; w < (1 << lg); w <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, w));
-        }
-        const float base = top == -INFINITY ? 0.f : top;       // nothing but -infinity: weights are 0
-        float sum = 0.f, del = 0.f;
-        const float inv = in && cur.sweep ? s_c[h] : 1.f;
-        if (in) {
-          for (int s = part; s < ns; s += 1 << lg) {
-            const float p = exp2_fast((zh[s] - base) * kLog2e) * inv;
-            zh[s] = p;
-            sum += p;
-            if (BACKWARD) del = fmaf(p, dp[h * a.chunk + s], del);
-          }
-        }
-        if (cur.sweep == 0) {
-          for (int w = 1; w < (1 << lg); w <<= 1) {
-            sum += __shfl_xor_sync(FULL, sum, w);
-            if (BACKWARD) del += __shfl_xor_sync(FULL, del, w);
+        __syncwarp();
+        if (sweep == 0) {
+          // maximum, sum and delta: 2^lg lanes per head, 32 / 2^lg heads at a time
+          int lg = 5;
+          while (lg > 0 && (H << lg) > 32) --lg;
+          const int per = 32 >> lg, part = lane & ((1 << lg) - 1);
+          for (int h0 = 0; h0 < H; h0 += per) {
+            const int h = h0 + (lane >> lg);
+            const bool in = h < H;
+            const float was = in ? s_m[h] : -INFINITY;
+            float top = was;
+            for (int s = part; in && s < ns; s += 1 << lg) top = fmaxf(top, z[s * H + h]);
+            for (int w = 1; w < (1 << lg); w <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, w));
+            const float base = top == -INFINITY ? 0.f : top;   // nothing but -infinity: weights are 0
+            float sum = 0.f, del = 0.f;
+            for (int s = part; in && s < ns; s += 1 << lg) {
+              const float p = exp2_fast((z[s * H + h] - base) * kLog2e);
+              if (!several) z[s * H + h] = p;
+              sum += p;
+              del = fmaf(p, dp[s * H + h], del);
+            }
+            for (int w = 1; w < (1 << lg); w <<= 1) {
+              sum += __shfl_xor_sync(FULL, sum, w);
+              del += __shfl_xor_sync(FULL, del, w);
+            }
+            __syncwarp();
+            if (in && part == 0) {
+              const float corr = exp2_fast((was - base) * kLog2e);        // was = -infinity: 0
+              sum = fmaf(s_l[h], corr, sum);
+              del = fmaf(s_d[h], corr, del);
+              if (c0 + a.chunk >= cnt) {                       // the last chunk: 1 / l and delta
+                sum = sum == 0.f ? 0.f : 1.f / sum;
+                del *= sum;
+              }
+              s_m[h] = top;
+              s_l[h] = sum;
+              s_d[h] = del;
+            }
           }
           __syncwarp();
-          if (in && part == 0) {
-            const float corr = exp2_fast((was - base) * kLog2e);          // was = -infinity: 0
-            const float l = fmaf(s_l[h], corr, sum);
-            s_m[h] = top;
-            s_l[h] = l;
-            if (BACKWARD) {
-              const float d = fmaf(s_d[h], corr, del);
-              const float il = l == 0.f ? 0.f : 1.f / l;
-              s_d[h] = last ? d * il : d;
-              s_c[h] = il;                                     // the weights' factor, final at the last chunk
-            } else {
-              s_c[h] = corr;
+          if (several) continue;
+        }
+        // weights and dz
+        for (int i = lane; i < ns * H; i += 32) {
+          const int h = i % H;
+          float p = z[i];
+          if (several) {
+            const float m = s_m[h];
+            p = exp2_fast((p - (m == -INFINITY ? 0.f : m)) * kLog2e);
+          }
+          p *= s_l[h];
+          z[i] = p;
+          dp[i] = p * (dp[i] - s_d[h]);
+        }
+        __syncwarp();
+        if (table) {
+          // a lane per head, so that no two lanes add to one bucket; slots of one bucket mostly lie side by side
+          for (int h = lane; h < H; h += 32) {
+            double sum = 0.0;
+            int b = ns > 0 ? bucket[0] : 0;
+            for (int s = 0; s < ns; ++s) {
+              const int nb = bucket[s];
+              if (nb != b) {
+                tab[h * a.buckets + b] += sum;
+                sum = 0.0;
+                b = nb;
+              }
+              sum += (double)dp[s * H + h];
+            }
+            tab[h * a.buckets + b] += sum;
+          }
+        }
+        const bool final_chunk = c0 + a.chunk >= cnt;
+        for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
+          const int kv = kv0 + me.kc;
+          for (int g = 0; g < a.group; ++g) {
+            const int h = kv * a.group + g;
+            float acc[S::N];
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
+            for (int s0 = 0; s0 < ns; s0 += UN * me.RPI) {
+              S k[UN];
+#pragma unroll
+              for (int u = 0; u < UN; ++u) {
+                const int s = s0 + u * me.RPI + me.row;
+                k[u].load(kr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
+              }
+#pragma unroll
+              for (int u = 0; u < UN; ++u) {
+                const int s = s0 + u * me.RPI + me.row;
+                const float w = s < ns ? dp[s * H + h] : 0.f;
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) acc[j] = fmaf(w, k[u].at(j), acc[j]);
+              }
+            }
+            for (int o = P * me.KC; o < 32; o <<= 1) {
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) acc[j] += __shfl_xor_sync(FULL, acc[j], o);
+            }
+            if (several && me.row == 0) {                      // carried from chunk to chunk
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) {
+                const int e = ((j / S::VE) * P + me.part) * S::VE + j % S::VE;
+                if (e < D) {
+                  if (c0 > 0) acc[j] += s_dq[h * D + e];
+                  if (!final_chunk) s_dq[h * D + e] = acc[j];
+                }
+              }
+            }
+            if (final_chunk && me.row == 0) {
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) acc[j] *= a.scale;
+              S::store(dqr + h * D, me.part, D, acc);
             }
           }
-        }
-      }
-    }
-    __syncwarp();
-
-    if (!BACKWARD) {
-      // o = o * corr + sum_s p_s v_s
-      T* og = reinterpret_cast<T*>(a.out) + r * HD;
-      for (int i = lane * E; i < HD; i += 32 * E) {
-        const int h = i / D, col = (h / a.group) * D + (i - h * D);
-        const float corr = s_c[h];
-        const float* p = z + h * a.chunk;
-        float acc[E];
+          S q, go;
+          q.load(qr + kv * a.group * D, me.part, D, true);
+          go.load(gr + kv * a.group * D, me.part, D, true);
+          const int end = final_chunk ? a.slots - c0 : ns;     // behind the last slot that counts: zeros
+          for (int s = me.row; s < end; s += me.RPI) {
+            float xk[S::N], xv[S::N];
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = o[i + e] * corr;
-        for (int s = 0; s < ns; ++s) {
-          float x[E];
-          load_e<T, E>(vs + s * ROW + col, x);
-          const float w = p[s];
+            for (int j = 0; j < S::N; ++j) xk[j] = xv[j] = 0.f;
+            if (s < ns) {
+              for (int g = 0; g < a.group; ++g) {
+                const int h = kv * a.group + g;
+                if (a.group > 1) {
+                  q.load(qr + h * D, me.part, D, true);
+                  go.load(gr + h * D, me.part, D, true);
+                }
+                const float wz = dp[s * H + h] * a.scale, wp = z[s * H + h];
 #pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] = fmaf(w, x[e], acc[e]);
-        }
-        if (last) {
-          const float l = s_l[h], f = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] *= f;
-          store_e<T, E>(og + i, acc);
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[i + e] = acc[e];
-        }
-      }
-    } else if (chunks == 1 || cur.sweep == 1) {
-      // weights and dz of the chunk; the bias's sums: a lane per head, so that no two lanes add to one bucket
-      const bool single = cur.sweep == 0;
-      for (int i = lane; i < ns * H; i += 32) {
-        const int s = i / H, h = i - s * H;
-        const float p = single ? z[h * a.chunk + s] * s_c[h] : z[h * a.chunk + s];
-        z[h * a.chunk + s] = p;
-        dp[h * a.chunk + s] = p * (dp[h * a.chunk + s] - s_d[h]);
-      }
-      __syncwarp();
-      if (table) {
-        for (int h = lane; h < H; h += 32) {
-          for (int s = 0; s < ns; ++s) tab[h * a.buckets + bucket[s]] += (double)dp[h * a.chunk + s];
-        }
-      }
-      const int64_t row0 = (r * a.slots + s0) * (int64_t)ROW;
-      T* dkg = reinterpret_cast<T*>(a.dk) + row0;
-      T* dvg = reinterpret_cast<T*>(a.dv) + row0;
-      T* dqg = reinterpret_cast<T*>(a.dq) + r * HD;
-      for (int i = lane * E; i < HD; i += 32 * E) {
-        const int h = i / D, col = (h / a.group) * D + (i - h * D);
-        const float* dz = dp + h * a.chunk;
-        float acc[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = o[i + e];
-        for (int s = 0; s < ns; ++s) {
-          float x[E];
-          load_e<T, E>(ks + s * ROW + col, x);
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] = fmaf(dz[s], x[e], acc[e]);
-        }
-        if (last) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) acc[e] *= a.scale;
-          store_e<T, E>(dqg + i, acc);
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[i + e] = acc[e];
-        }
-      }
-      for (int i = lane * E; i < ROW; i += 32 * E) {
-        const int kv = i / D, h0 = kv * a.group, col = i - kv * D;
-        for (int s = 0; s < ns; ++s) {
-          float xk[E], xv[E];
-#pragma unroll
-          for (int e = 0; e < E; ++e) xk[e] = xv[e] = 0.f;
-          for (int h = h0; h < h0 + a.group; ++h) {
-            const float dz = dp[h * a.chunk + s] * a.scale, p = z[h * a.chunk + s];
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              xk[e] = fmaf(dz, q[h * D + col + e], xk[e]);
-              xv[e] = fmaf(p, g[h * D + col + e], xv[e]);
+                for (int j = 0; j < S::N; ++j) {
+                  xk[j] = fmaf(wz, q.at(j), xk[j]);
+                  xv[j] = fmaf(wp, go.at(j), xv[j]);
+                }
+              }
             }
-          }
-          store_e<T, E>(dkg + (int64_t)s * ROW + i, xk);
-          store_e<T, E>(dvg + (int64_t)s * ROW + i, xv);
-        }
-        if (last) {                                            // slots that do not count
-          float zero[E];
-#pragma unroll
-          for (int e = 0; e < E; ++e) zero[e] = 0.f;
-          for (int s = ns; s < a.slots - s0; ++s) {
-            store_e<T, E>(dkg + (int64_t)s * ROW + i, zero);
-            store_e<T, E>(dvg + (int64_t)s * ROW + i, zero);
+            S::store(dkr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, xk);
+            S::store(dvr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, xv);
           }
         }
+        __syncwarp();                                          // before the next chunk or root overwrites what was read
       }
     }
-    __syncwarp();                                              // the stage may be filled again
-    cur = nxt;
-    buf ^= 1;
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
   if (table) {
     __syncthreads();
     for (int i = threadIdx.x; i < H * a.buckets; i += blockDim.x) {
@@ -434,68 +480,62 @@ __global__ void __launch_bounds__(256) bias_sum_kernel(const double* __restrict_
   if (lane == 0) dbias[i] = (float)sum;
 }
 
-template <typename T, int VB, int E, bool BACKWARD>
+template <bool BACKWARD, typename T, int VB, int P, int NV>
 cudaError_t launch_kernel(const SlotArgs& a, int blocks, cudaStream_t s) {
+  const auto kernel = BACKWARD ? slot_backward_kernel<T, VB, P, NV> : slot_forward_kernel<T, VB, P, NV>;
   const int bytes = a.warps * a.warp_bytes;
-  // more dynamic shared memory than 48 KB has to be asked for, per device; asking again costs less than a microsecond
-  const cudaError_t e = cudaFuncSetAttribute(slot_attend_kernel<T, VB, E, BACKWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e != cudaSuccess) return e;
-  slot_attend_kernel<T, VB, E, BACKWARD><<<blocks, 32 * a.warps, bytes, s>>>(a);
+  if (bytes > 46 * 1024) {          // more than a kernel has without asking for it (per device; asking again costs little)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+  }
+  kernel<<<blocks, 32 * a.warps, bytes, s>>>(a);
   return cudaGetLastError();
 }
 
-// Chunks are copied in words of 16, 8, 4 or 2 bytes: the widest on which k, v, a root's rows and a chunk's rows all start.  Even
-// head sizes are worked on two values at a time.
-template <typename T, bool BACKWARD>
+// Words of 16 bytes where every head of every row starts on one: 4 to 32 lanes per segment.  Pairs of values (heads of 50) and
+// single values (odd heads, odd bases) take a whole warp per segment.
+template <bool BACKWARD, typename T>
 cudaError_t launch_type(const SlotArgs& a, int blocks, cudaStream_t s) {
-  const int64_t row = (int64_t)a.kv_heads * a.dim * (int64_t)sizeof(T);
-  uint64_t at = (uint64_t)(uintptr_t)a.k | (uint64_t)(uintptr_t)a.v | (uint64_t)(row * a.slots);
-  if (a.chunk < a.slots) at |= (uint64_t)(row * a.chunk);
-  const bool even = a.dim % 2 == 0 &&
-                    ((((uintptr_t)a.q | (uintptr_t)a.out | (uintptr_t)a.dout | (uintptr_t)a.dq | (uintptr_t)a.dk | (uintptr_t)a.dv) &
-                      (2 * sizeof(T) - 1)) == 0);
-  if (even) {
-    if ((at & 15) == 0) return launch_kernel<T, 16, 2, BACKWARD>(a, blocks, s);
-    if ((at & 7) == 0) return launch_kernel<T, 8, 2, BACKWARD>(a, blocks, s);
-    if ((at & 3) == 0) return launch_kernel<T, 4, 2, BACKWARD>(a, blocks, s);
-    return launch_kernel<T, (int)sizeof(T), 2, BACKWARD>(a, blocks, s);
+  constexpr int V16 = 16 / (int)sizeof(T);
+  const uint64_t at = (uint64_t)(uintptr_t)a.k | (uint64_t)(uintptr_t)a.v | (uint64_t)(uintptr_t)a.q | (uint64_t)(uintptr_t)a.out |
+                      (uint64_t)(uintptr_t)a.dout | (uint64_t)(uintptr_t)a.dq | (uint64_t)(uintptr_t)a.dk | (uint64_t)(uintptr_t)a.dv |
+                      (uint64_t)(a.dim * (int)sizeof(T));
+  if ((at & 15) == 0) {
+    const int words = a.dim / V16;
+    if (words <= 4) return launch_kernel<BACKWARD, T, 16, 4, 1>(a, blocks, s);
+    if (words <= 8) return launch_kernel<BACKWARD, T, 16, 8, 1>(a, blocks, s);
+    if (words <= 16) return launch_kernel<BACKWARD, T, 16, 16, 1>(a, blocks, s);
+    if constexpr (sizeof(T) == 4) return launch_kernel<BACKWARD, T, 16, 32, 1>(a, blocks, s);
   }
-  if ((at & 15) == 0) return launch_kernel<T, 16, 1, BACKWARD>(a, blocks, s);
-  if ((at & 3) == 0) return launch_kernel<T, 4, 1, BACKWARD>(a, blocks, s);
-  return launch_kernel<T, (int)sizeof(T), 1, BACKWARD>(a, blocks, s);
+  if ((at & (2 * sizeof(T) - 1)) == 0) {
+    if (a.dim <= 64) return launch_kernel<BACKWARD, T, 2 * (int)sizeof(T), 32, 1>(a, blocks, s);
+    return launch_kernel<BACKWARD, T, 2 * (int)sizeof(T), 32, 2>(a, blocks, s);
+  }
+  return launch_kernel<BACKWARD, T, (int)sizeof(T), 32, 4>(a, blocks, s);
 }
 
 constexpr int SMEM_BLOCK = 200 * 1024;     // of an SM's 227 KB, beside the bounds and what the system keeps
-constexpr int WANT_WARP = 24 * 1024;
 
-// Slots of a chunk and warps of a block: chunks as large as WANT_WARP allows for a warp, all slots if they fit; multiples of 4 slots
-// otherwise, which keeps chunks on word boundaries.  false: not even one slot fits.
-bool plan(SlotArgs* a, int elem, bool backward) {
+// Slots of a chunk and warps of a block.  Forward a slot takes a byte: chunks of 4096.  Backward logits and dp of a chunk take
+// 8 * heads bytes a slot: 12 KB of them, so that 16 warps have room on an SM.  false: a warp's share exceeds shared memory.
+bool plan(SlotArgs* a, bool backward) {
   const int table = backward && a->partial ? a->heads * a->buckets : 0;
-  auto bytes = [&](int chunk) { return layout(a->heads, a->kv_heads, a->dim, chunk, elem, backward, table).total; };
-  const int fixed = bytes(1), per = bytes(9) - fixed;           // of 8 slots
-  int chunk = a->slots < 2048 ? a->slots : 2048;
-  if (bytes(chunk) > WANT_WARP) {
-    const int fit = fixed < WANT_WARP ? 1 + (WANT_WARP - fixed) * 8 / (per > 0 ? per : 1) : 1;
-    chunk = fit < chunk ? fit : chunk;
-    chunk = chunk >= 4 ? chunk & ~3 : chunk;
-    while (chunk > 1 && bytes(chunk) > SMEM_BLOCK) chunk = chunk > 4 ? (chunk - 1) & ~3 : chunk - 1;
-  }
+  int chunk = backward ? 12 * 1024 / (8 * a->heads) : 4096;
+  if (chunk > a->slots) chunk = a->slots;
   a->chunk = chunk;
-  a->warp_bytes = bytes(chunk);
-  int w = SMEM_BLOCK / a->warp_bytes;
-  const int64_t per_sm = (a->n + num_sms() - 1) / num_sms();    // few roots: over all SMs
-  if (w > MAX_WARPS) w = MAX_WARPS;
-  if (w > per_sm) w = (int)per_sm;
+  a->warp_bytes = layout(a->heads, a->dim, chunk, chunk < a->slots, backward, table).total;
+  int w = MAX_WARPS;
+  while (w > 1 && (w * a->warp_bytes > SMEM_BLOCK / 2 || w * (int64_t)num_sms() > a->n)) w >>= 1;   // two blocks to an SM; few roots: over all SMs
   a->warps = w;
-  return w >= 1;
+  return w * a->warp_bytes <= SMEM_BLOCK;
 }
 
-int grid_of(const SlotArgs& a) {
+int grid_of(const SlotArgs& a, bool backward) {
   const int64_t want = (a.n + a.warps - 1) / a.warps;
+  if (!backward) return (int)want;
   int resident = (int)((220 * 1024) / ((int64_t)a.warps * a.warp_bytes + 2048));
   if (resident < 1) resident = 1;
-  if (resident > 64 / a.warps) resident = 64 / a.warps;
+  if (resident > 16 / a.warps) resident = 16 / a.warps;
   int64_t most = (int64_t)num_sms() * resident;
   if (most > MAX_BLOCKS) most = MAX_BLOCKS;
   return (int)(want < most ? want : most);
@@ -532,13 +572,13 @@ int run(const char* who, SlotArgs& a, int dtype, const void* out_like, float* db
   }
   a.group = a.heads / a.kv_heads;
   a.partial = dbias ? reinterpret_cast<double*>(scratch) : nullptr;
-  if (!plan(&a, elem, BACKWARD))
-    return fail(err, size, TGNN_ECAPACITY, "%s: one slot of %d heads of %d with %d buckets exceeds shared memory", who, a.heads, a.dim, a.buckets);
-  const int blocks = grid_of(a);
+  if (!plan(&a, BACKWARD))
+    return fail(err, size, TGNN_ECAPACITY, "%s: %d heads with %d buckets exceed shared memory", who, a.heads, a.buckets);
+  const int blocks = grid_of(a, BACKWARD);
   cudaError_t e;
-  if (dtype == TGNN_F32) e = launch_type<float, BACKWARD>(a, blocks, s);
-  else if (dtype == TGNN_BF16) e = launch_type<__nv_bfloat16, BACKWARD>(a, blocks, s);
-  else e = launch_type<__half, BACKWARD>(a, blocks, s);
+  if (dtype == TGNN_F32) e = launch_type<BACKWARD, float>(a, blocks, s);
+  else if (dtype == TGNN_BF16) e = launch_type<BACKWARD, __nv_bfloat16>(a, blocks, s);
+  else e = launch_type<BACKWARD, __half>(a, blocks, s);
   if (e == cudaSuccess && BACKWARD && a.partial) {
     const int entries = a.heads * a.buckets;
     bias_sum_kernel<<<(entries + 7) / 8, 256, 0, s>>>(a.partial, blocks, entries, dbias);
