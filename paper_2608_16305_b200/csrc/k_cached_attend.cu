@@ -6,19 +6,21 @@
 // (Logits stay in natural units, and log2(e) goes into the difference: a bias of the type's lowest value is then still finite.)
 //
 // Both products run on the tensor cores (m16n8k16, fp16 operands, fp32 sums) although a root has a single query: what they save is not
-// the multiplications but the conversion of every code to fp32 and the sums across lanes.  The codes go in as they are, as fp16
-// integers (exact), and the scales are applied to the other side: ks_j to the finished logits, vs_j to the weights.  The other operand
-// is kept to fp32's accuracy by splitting it in two fp16 terms (x = hi + lo / 2048, 22 bits): a tile has 16 rows, the terms of 8
-// query heads that share a cached head take all of them (hi in rows 0-7, lo in rows 8-15), so the split costs nothing.  Both terms of
-// a row end up in one thread.  fp16's range is no limit: a query is divided by a power of two at its largest value, and
-// weights w_j = p_j vs_j are divided by a running bound sc of w.  The output is held in units of sc at maximum m; when a weight
-// passes sc it is rescaled.
+// the multiplications but the conversion of every code to fp32 and the sums across lanes.  Codes are the 16-row operand (16 keys,
+// or 16 columns of the values), queries and weights the 8 columns: two for each of four query heads that share a cached head.
+// Those two hold a number x as hi + lo / 2048 in fp16 (22 bits), and both products of a head end up in one thread.
+// Codes go in as fp16 integers (exact), centred: their bits under the exponent of 1024 minus 1024 and the stored offset.  (Under a zero
+// exponent a mask alone would unpack them, but the tensor core lines products up by their nominal exponents, and sums of such
+// numbers came out at 2^-17.)  Scales are applied to the other side: ks_j to the finished logits, vs_j to the weights.  fp16's range is
+// no limit: a query is divided by a power of two at its largest value, and weights w_j = p_j vs_j are divided by a running bound
+// sc of w.  The output is held in units of sc at maximum m;
+// when a weight passes sc it is rescaled.
 //
 // The sum over dim may be taken in any order, so a lane reads neighbouring words of a key's codes with one wide load and the query
-// is laid out to match; likewise for the values' columns.  tcgen05's 128-row tiles would be filled to 1/16 by one root's
-// heads, and roots see different rows.
+// is laid out to match; likewise for the values' columns.  tcgen05's tiles have 128 rows that share one operand; here every root
+// brings rows of its own, 20 to a few hundred, and each with its own mask.
 //
-// Work: a unit is a root, a cached head and up to 8 of its query heads.  Units are handled by a warp, by a block of 4 warps
+// Work: a unit is a root, a cached head and up to 4 of its query heads (8 where more share it).  Units are handled by a warp, by a block of 4 warps
 // or by a cluster of 2 to 8 blocks whose partial results meet in distributed shared memory (no workspace, no atomics, sums in
 // a fixed order); the launch takes more warps per unit while the units alone would leave SMs idle and each warp still has a few
 // tiles to walk.
@@ -34,7 +36,6 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int WARPS = 4;
-constexpr int GH = 8;                     // query heads of a unit
 constexpr float kLo = 2048.f;             // lo terms are held times 2^11, clear of fp16's subnormals
 
 struct AttendArgs {
@@ -45,7 +46,8 @@ struct AttendArgs {
   int k_code_stride, v_code_stride, k_scale_stride, v_scale_stride;
   int64_t rows;
   uint32_t units;
-  int heads, kv_heads, group, passes, dim;    // group = heads / kv_heads, passes = ceil(group / 8)
+  int heads, kv_heads, group, passes, dim;    // group = heads / kv_heads, passes = ceil(group / heads of a unit)
+  int take;                                   // units of a warp: 1, or all of a root (passes * kv_heads)
   const int64_t* first;
   const int32_t* len;
   const float* bias;
@@ -53,6 +55,7 @@ struct AttendArgs {
   int buckets, window, sinks;
   float scale;
   int32_t* status;
+  bool pairs;                                 // q and out may be read and written two values at a time
 };
 
 __device__ __forceinline__ uint32_t h2u(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
@@ -76,12 +79,14 @@ __device__ __forceinline__ void nibbles(uint32_t t, uint32_t (&out)[4]) {
   out[2] = h2u(__hsub2(u2h(and_or(t, 0x000f000fu, 0x64006400u)), one));
   out[3] = h2u(__hfma2(u2h(and_or(t, 0x00f000f0u, 0x64006400u)), sixteenth, off));
 }
+// Two bytes under the exponent of 1024, minus 1024 and their offset of 128.
+__device__ __forceinline__ uint32_t centre(uint32_t x) { return h2u(__hsub2(u2h(x), u2h(0x64806480u))); }
 
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
 // x0, x1 as fp16 pairs hi and lo with x = hi + lo / 2048
@@ -129,209 +134,324 @@ __device__ __forceinline__ Words<(B + 3) / 4> load_piece(const uint8_t* p) {
   }
 }
 
-__device__ __forceinline__ float load_q(const void* q, int dtype, int64_t i) {
-  if (dtype == TGNN_F32) return __ldg(reinterpret_cast<const float*>(q) + i);
-  if (dtype == TGNN_BF16) return __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[i]);
-  return __half2float(reinterpret_cast<const __half*>(q)[i]);
+// N values of a query row from column e0 on, as fp32 (0 beyond dim): in pairs where every row starts on one.
+template <int N>
+__device__ __forceinline__ void load_query(const AttendArgs& a, int64_t base, int e0, bool on, float (&x)[N]) {
+  if (a.pairs) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const bool in = on && e0 + i < a.dim;
+      float2 f = make_float2(0.f, 0.f);
+      if (a.dtype == TGNN_F32) {
+        if (in) f = __ldg(reinterpret_cast<const float2*>(reinterpret_cast<const float*>(a.q) + base + e0 + i));
+      } else {
+        uint32_t w = 0;
+        if (in) w = __ldg(reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint16_t*>(a.q) + base + e0 + i));
+        if (a.dtype == TGNN_BF16) f = make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        else f = __half22float2(u2h(w));
+      }
+      x[i] = f.x;
+      x[i + 1] = f.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] = 0.f;
+      if (on && e0 + i < a.dim) {
+        if (a.dtype == TGNN_F32) x[i] = __ldg(reinterpret_cast<const float*>(a.q) + base + e0 + i);
+        else if (a.dtype == TGNN_BF16) x[i] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.q)[base + e0 + i]);
+        else x[i] = __half2float(reinterpret_cast<const __half*>(a.q)[base + e0 + i]);
+      }
+    }
+  }
 }
-__device__ __forceinline__ void store_out(void* o, int dtype, int64_t i, float x) {
-  if (dtype == TGNN_F32) reinterpret_cast<float*>(o)[i] = x;
-  else if (dtype == TGNN_BF16) reinterpret_cast<__nv_bfloat16*>(o)[i] = __float2bfloat16_rn(x);
-  else reinterpret_cast<__half*>(o)[i] = __float2half_rn(x);
+__device__ __forceinline__ void store_out(const AttendArgs& a, int64_t i, float x) {
+  if (a.dtype == TGNN_F32) reinterpret_cast<float*>(a.out)[i] = x;
+  else if (a.dtype == TGNN_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(x);
+  else reinterpret_cast<__half*>(a.out)[i] = __float2half_rn(x);
+}
+// Columns e and e + 1 of an output row: e is even, the row a pair's multiple long.
+__device__ __forceinline__ void store_pair(const AttendArgs& a, int64_t i, float x, float y) {
+  if (a.dtype == TGNN_F32) {
+    *reinterpret_cast<float2*>(reinterpret_cast<float*>(a.out) + i) = make_float2(x, y);
+  } else if (a.dtype == TGNN_BF16) {
+    *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(a.out) + i) = __floats2bfloat162_rn(x, y);
+  } else {
+    *reinterpret_cast<__half2*>(reinterpret_cast<__half*>(a.out) + i) = __floats2half2_rn(x, y);
+  }
 }
 
-// Keys that a warp takes at a time: 32, or 16 where 32 rows of codes would not fit into registers.
+// Keys that a warp takes at a time: 32, or 16 where 32 rows of codes would take too many registers.
 template <int BITS, int DP>
 struct Tile {
-  static constexpr int TK = (BITS == 8 && DP == 128) ? 16 : 32;
-  static constexpr int NT = TK / 8;                 // key tiles of 8 columns
+  static constexpr int TK = BITS * DP >= 1024 ? 16 : 32;
+  static constexpr int NT = TK / 8;                 // keys per lane group: kw[j] is key 8 j + lane / 4
   static constexpr int KW = DP * BITS / 128;        // words of a key that a lane reads (a quarter of the row)
   static constexpr int VD = DP / 8;                 // columns of a value that a lane reads
   static constexpr int VB = VD * BITS / 8;          // bytes of them: 2 to 16
 };
 
-// One warp's walk over tiles w, w + workers, ... of the unit's visible entries.  Results: o[VD][4] in units of sc, m, l, sc; the rows
-// of a lane are the hi and lo terms of head `lane / 4` of the unit, its columns [2 c VD, 2 c VD + 2 VD) with c = lane % 4.
+// A root's visible entries: u < ns are the sinks, the others lie `skip` further on; first is the place of entry 0.
+struct Seen {
+  int64_t first;
+  int n, ns, skip;
+  double t;
+};
+
+// Codes, scales and times of one tile, on their way in registers.  Lane (g, c) = (lane / 4, lane % 4) holds quarter c of keys
+// 8 j + g, piece g of the values of keys 16 t + 2 c + {0, 1, 8, 9}, and the scales and time of key lane.
 template <int BITS, int DP>
+struct Rows {
+  using T = Tile<BITS, DP>;
+  Words<T::KW> kw[T::NT];
+  Words<(T::VB + 3) / 4> vw[T::TK / 4];
+  uint32_t scales;
+  double ts;
+
+  __device__ __forceinline__ void load(const AttendArgs& a, const Seen& seen, int kv, int tile) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3, u0 = tile * T::TK;
+    const uint8_t* kp = a.k_codes + seen.first * a.k_code_stride + kv * (DP * BITS / 8) + c * (DP * BITS / 32);
+    const uint8_t* vp = a.v_codes + seen.first * a.v_code_stride + kv * (DP * BITS / 8) + g * T::VB;
+    int e;
+    if (u0 >= seen.ns && u0 + T::TK <= seen.n) {                     // neighbouring rows
+      const int e0 = u0 + seen.skip;
+      e = e0 + (lane & (T::TK - 1));
+      kp += (int64_t)(e0 + g) * a.k_code_stride;
+      vp += (int64_t)(e0 + 2 * c) * a.v_code_stride;
+#pragma unroll
+      for (int j = 0; j < T::NT; ++j) {
+        kw[j] = load_words<T::KW>(kp);
+        kp += 8 * (int64_t)a.k_code_stride;
+      }
+#pragma unroll
+      for (int i = 0; i < T::TK / 4; i += 2) {
+        vw[i] = load_piece<T::VB>(vp);
+        vw[i + 1] = load_piece<T::VB>(vp + a.v_code_stride);
+        vp += 8 * (int64_t)a.v_code_stride;
+      }
+    } else {
+      // beyond the last entry: the last (its weight is set to 0)
+      auto entry = [&](int u) { u = min(u, seen.n - 1); return u < seen.ns ? u : u + seen.skip; };
+      e = entry(u0 + (lane & (T::TK - 1)));
+#pragma unroll
+      for (int j = 0; j < T::NT; ++j) kw[j] = load_words<T::KW>(kp + (int64_t)entry(u0 + 8 * j + g) * a.k_code_stride);
+#pragma unroll
+      for (int i = 0; i < T::TK / 4; ++i)
+        vw[i] = load_piece<T::VB>(vp + (int64_t)entry(u0 + 8 * (i >> 1) + 2 * c + (i & 1)) * a.v_code_stride);
+    }
+    const int64_t place = seen.first + e;
+    scales = __ldg(reinterpret_cast<const uint16_t*>(a.k_scales + place * a.k_scale_stride + 2 * kv)) |
+             (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v_scales + place * a.v_scale_stride + 2 * kv)) << 16;
+    ts = a.bias ? __ldg(a.ts + place) : 0.0;
+  }
+};
+
+// A unit's running sums over the tiles that one warp walks, for 4 NH heads.  Lane (g, c) has head c of every four: its logits at keys
+// 16 b + g and 16 b + g + 8, its output columns g VD + i at o[i / 2][.][2 (i & 1) + {hi, lo}] in units of sc, its sum l over the
+// lane's own keys until finish().
+template <int BITS, int DP, int NH>
 struct Walk {
   using T = Tile<BITS, DP>;
-  float o[T::VD][4];
-  float m, l, sc;
+  static constexpr int KS = DP / 16, MT = T::VD / 2;
+  float o[MT][NH][4];
+  float m[NH], l[NH], sc[NH], qfac[NH];
+  uint32_t qb[NH][KS][2];
 
-  __device__ __forceinline__ void run(const AttendArgs& a, const double* s_bounds, int64_t root, int kv, int head0, int64_t first, int lo,
-                                      int ns, int n, int worker, int workers) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    constexpr int KS = DP / 16;
-    m = -INFINITY;
-    l = 0.f;
-    sc = 0.f;
+  __device__ __forceinline__ void none() {
 #pragma unroll
-    for (int i = 0; i < T::VD; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    const int tiles = (n + T::TK - 1) / T::TK;
-    if (worker >= tiles) return;
-    const bool mine = head0 + g < (kv + 1) * a.group;               // a query head of this unit
+    for (int x = 0; x < NH; ++x) {
+      m[x] = -INFINITY;
+      l[x] = sc[x] = 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[i][x][0] = o[i][x][1] = o[i][x][2] = o[i][x][3] = 0.f;
+    }
+  }
 
-    // the query: a lane holds columns [c * DP / 4, (c + 1) * DP / 4) of head g, divided by a power of two
-    uint32_t qa[KS][4];
-    float qfac;
-    {
-      float x[DP / 4];
-      const int64_t base = (root * a.heads + head0 + g) * a.dim;
+  // The query: lane (g, c) holds columns [c DP / 4, (c + 1) DP / 4) of head g / 2 of every four, the hi terms where g is even, lo
+  // where it is odd, divided by a power of two.
+  __device__ __forceinline__ void begin(const AttendArgs& a, int64_t root, int head0, int nh) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    none();
+#pragma unroll
+    for (int x = 0; x < NH; ++x) {
+      const int h = 4 * x + (g >> 1);
+      float q[DP / 4];
+      load_query<DP / 4>(a, (root * a.heads + head0 + h) * a.dim, c * (DP / 4), h < nh, q);
       float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < DP / 4; ++i) {
-        const int e = c * (DP / 4) + i;
-        x[i] = mine && e < a.dim ? load_q(a.q, a.dtype, base + e) : 0.f;
-        top = fmaxf(top, fabsf(x[i]));
-      }
+      for (int i = 0; i < DP / 4; ++i) top = fmaxf(top, fabsf(q[i]));
       top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
       top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
       // 2^e <= top < 2^(e + 1): scaled queries lie below 2 (infinities and NaN stay what they are)
       const int e = min(max((int)(__float_as_uint(top) >> 23), 2), 252);
       const float down = __uint_as_float((uint32_t)(254 - e) << 23);
-      qfac = a.scale * __uint_as_float((uint32_t)e << 23);
+      qfac[x] = a.scale * __uint_as_float((uint32_t)__shfl_sync(FULL, e, 8 * c) << 23);       // to the lanes of the head's logits
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         // BITS 4: the columns of a step in the order in which nibbles() pairs them
         const int b = BITS == 4 ? 8 * (s >> 1) + 2 * (s & 1) : 4 * s;
         const int i1 = BITS == 4 ? b + 4 : b + 1, i2 = BITS == 4 ? b + 1 : b + 2, i3 = BITS == 4 ? b + 5 : b + 3;
-        split2(x[b] * down, x[i1] * down, &qa[s][0], &qa[s][1]);
-        split2(x[i2] * down, x[i3] * down, &qa[s][2], &qa[s][3]);
+        uint32_t hi, lo;
+        split2(q[b] * down, q[i1] * down, &hi, &lo);
+        qb[x][s][0] = (g & 1) ? lo : hi;
+        split2(q[i2] * down, q[i3] * down, &hi, &lo);
+        qb[x][s][1] = (g & 1) ? lo : hi;
       }
     }
+  }
 
-    const double t_root = a.bias ? a.times[root] : 0.0;
-    const uint8_t* kp = a.k_codes + first * a.k_code_stride + kv * (DP * BITS / 8) + c * (DP * BITS / 32);
-    const uint8_t* vp = a.v_codes + first * a.v_code_stride + kv * (DP * BITS / 8) + g * T::VB;
-    const uint8_t* ksp = a.k_scales + first * a.k_scale_stride + 2 * kv;
-    const uint8_t* vsp = a.v_scales + first * a.v_scale_stride + 2 * kv;
-    const float* bias = a.bias ? a.bias + (int64_t)min(head0 + g, a.heads - 1) * a.buckets : nullptr;
-    const int skip = lo - ns;
-    // entry of the u-th visible one; beyond the last: the last (its weight is set to 0)
-    auto entry = [&](int u) { u = min(u, n - 1); return u < ns ? u : u + skip; };
-
-    for (int tile = worker; tile < tiles; tile += workers) {
-      const int u0 = tile * T::TK;
-      Words<T::KW> kw[T::NT];
-      Words<(T::VB + 3) / 4> vw[T::TK / 4];
+  __device__ __forceinline__ void tile(const AttendArgs& a, const double* s_bounds, const float* bias, const Seen& seen, const Rows<BITS, DP>& in,
+                                       int u0, int nh) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    const int bucket = bias ? bucket_of(s_bounds, a.buckets - 1, seen.t - in.ts) : 0;
+    // logits: s[x][j] of head 4 x + c at key 8 j + g
+    float s[NH][T::NT];
 #pragma unroll
-      for (int j = 0; j < T::NT; ++j) kw[j] = load_words<T::KW>(kp + (int64_t)entry(u0 + 8 * j + g) * a.k_code_stride);
-      uint32_t scales;
-      int bucket = 0;
-      {
-        const int e = entry(u0 + (lane & (T::TK - 1)));
-        scales = __ldg(reinterpret_cast<const uint16_t*>(ksp + (int64_t)e * a.k_scale_stride)) |
-                 (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(vsp + (int64_t)e * a.v_scale_stride)) << 16;
-        if (bias) bucket = bucket_of(s_bounds, a.buckets - 1, t_root - __ldg(a.ts + first + e));
-      }
+    for (int b = 0; b < T::NT / 2; ++b) {
+      float acc[NH][4];
 #pragma unroll
-      for (int i = 0; i < T::TK / 4; ++i)            // pieces 4 t + {0, 1, 2, 3}: keys 16 t + 2 c + {0, 1, 8, 9}
-        vw[i] = load_piece<T::VB>(vp + (int64_t)entry(u0 + 16 * (i >> 2) + 2 * c + (i & 1) + 8 * ((i >> 1) & 1)) * a.v_code_stride);
-
-      // logits
-      float s[T::NT][2];
+      for (int x = 0; x < NH; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
 #pragma unroll
-      for (int j = 0; j < T::NT; ++j) {
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < T::KW; ++w) {
+        const uint32_t k0 = in.kw[2 * b].w[w], k1 = in.kw[2 * b + 1].w[w];
+        if constexpr (BITS == 4) {
+          uint32_t p[4], q[4];
+          nibbles(k0, p);
+          nibbles(k1, q);
 #pragma unroll
-        for (int w = 0; w < T::KW; ++w) {
-          if constexpr (BITS == 4) {
-            uint32_t b[4];
-            nibbles(kw[j].w[w], b);
-            mma(acc, qa[2 * w], b[0], b[1]);
-            mma(acc, qa[2 * w + 1], b[2], b[3]);
-          } else {
-            const __half2 off = u2h(0x64806480u);    // 1152: a byte under the exponent of 1024, minus the offset of 128
-            const uint32_t b0 = h2u(__hsub2(u2h(__byte_perm(kw[j].w[w], 0x64646464u, 0x4140)), off));
-            const uint32_t b1 = h2u(__hsub2(u2h(__byte_perm(kw[j].w[w], 0x64646464u, 0x4342)), off));
-            mma(acc, qa[w], b0, b1);
+          for (int x = 0; x < NH; ++x) {
+            mma(acc[x], p[0], q[0], p[1], q[1], qb[x][2 * w][0], qb[x][2 * w][1]);
+            mma(acc[x], p[2], q[2], p[3], q[3], qb[x][2 * w + 1][0], qb[x][2 * w + 1][1]);
           }
+        } else {
+          const uint32_t p0 = centre(__byte_perm(k0, 0x64646464u, 0x4140)), p1 = centre(__byte_perm(k0, 0x64646464u, 0x4342));
+          const uint32_t q0 = centre(__byte_perm(k1, 0x64646464u, 0x4140)), q1 = centre(__byte_perm(k1, 0x64646464u, 0x4342));
+#pragma unroll
+          for (int x = 0; x < NH; ++x) mma(acc[x], p0, q0, p1, q1, qb[x][w][0], qb[x][w][1]);
         }
-        s[j][0] = fmaf(acc[2], 1.f / kLo, acc[0]);
-        s[j][1] = fmaf(acc[3], 1.f / kLo, acc[1]);
       }
-      float vs[T::NT][2], top = m;
+#pragma unroll
+      for (int x = 0; x < NH; ++x) {
+        s[x][2 * b] = fmaf(acc[x][1], 1.f / kLo, acc[x][0]);
+        s[x][2 * b + 1] = fmaf(acc[x][3], 1.f / kLo, acc[x][2]);
+      }
+    }
+    float vs[T::NT], top[NH];
+#pragma unroll
+    for (int x = 0; x < NH; ++x) top[x] = m[x];
+#pragma unroll
+    for (int j = 0; j < T::NT; ++j) {
+      const int key = 8 * j + g;
+      const uint32_t two = __shfl_sync(FULL, in.scales, key);
+      const float ks = __uint_as_float(two << 16);
+      vs[j] = __uint_as_float(two & 0xffff0000u);
+      const int at = bias ? __shfl_sync(FULL, bucket, key) : 0;
+#pragma unroll
+      for (int x = 0; x < NH; ++x) {
+        float z = s[x][j] * (qfac[x] * ks);
+        if (bias) z += __ldg(bias + min(4 * x + c, nh - 1) * a.buckets + at);
+        s[x][j] = u0 + key < seen.n ? z : -INFINITY;
+        top[x] = fmaxf(top[x], s[x][j]);
+      }
+    }
+    float wmax[NH];
+#pragma unroll
+    for (int x = 0; x < NH; ++x) {
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(FULL, top[x], w));
+      const float base = top[x] == -INFINITY ? 0.f : top[x];         // nothing but -infinity so far: weights are 0
+      const float corr = exp2_fast((m[x] - base) * kLog2e);          // m = -infinity: 0
+      m[x] = top[x];
+      float sum = 0.f;
+      wmax[x] = 0.f;
 #pragma unroll
       for (int j = 0; j < T::NT; ++j) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int key = 8 * j + 2 * c + e;
-          const uint32_t two = __shfl_sync(FULL, scales, key);
-          vs[j][e] = __uint_as_float(two & 0xffff0000u);
-          float x = s[j][e] * (qfac * __uint_as_float(two << 16));
-          if (bias) x += __ldg(bias + __shfl_sync(FULL, bucket, key));
-          s[j][e] = u0 + key < n ? x : -INFINITY;
-          top = fmaxf(top, s[j][e]);
-        }
+        const float p = exp2_fast((s[x][j] - base) * kLog2e);
+        sum += p;
+        s[x][j] = u0 + 8 * j + g < seen.n ? p * vs[j] : 0.f;
+        wmax[x] = fmaxf(wmax[x], s[x][j]);
       }
-      top = fmaxf(top, __shfl_xor_sync(FULL, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(FULL, top, 2));
-      const float base = top == -INFINITY ? 0.f : top;               // nothing but -infinity so far: weights are 0
-      const float corr = exp2_fast((m - base) * kLog2e);                  // m = -infinity: 0
-      m = top;
-      float wmax = 0.f, sum = 0.f;
+      l[x] = fmaf(l[x], corr, sum);
+      sc[x] *= corr;                                                 // a larger maximum shrinks the unit of the sums, not the sums
 #pragma unroll
-      for (int j = 0; j < T::NT; ++j) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float p = exp2_fast((s[j][e] - base) * kLog2e);
-          sum += p;
-          const float w = u0 + 8 * j + 2 * c + e < n ? p * vs[j][e] : 0.f;
-          s[j][e] = w;
-          wmax = fmaxf(wmax, w);
-        }
-      }
-      l = fmaf(l, corr, sum);
-      wmax = fmaxf(wmax, __shfl_xor_sync(FULL, wmax, 1));
-      wmax = fmaxf(wmax, __shfl_xor_sync(FULL, wmax, 2));
-      // a larger maximum m shrinks the unit of the sums, not the sums; they are rescaled where a weight passes the unit
-      const float old = sc * corr;
-      const float need = __uint_as_float(min(max((__float_as_uint(wmax) >> 23) + 1u, 2u), 252u) << 23);   // 2^e > wmax
-      const bool grow = need > old;
-      sc = grow ? need : old;
-      const float inv = __frcp_rn(sc);
+      for (int w = 4; w < 32; w <<= 1) wmax[x] = fmaxf(wmax[x], __shfl_xor_sync(FULL, wmax[x], w));
+      const float need = __uint_as_float(min(max((__float_as_uint(wmax[x]) >> 23) + 1u, 2u), 252u) << 23);   // 2^e > wmax
+      const bool grow = need > sc[x];
+      const float old = sc[x];
+      sc[x] = grow ? need : old;
+      const float inv = __frcp_rn(sc[x]);
       if (__any_sync(FULL, grow)) {
         const float f = grow ? old * inv : 1.f;
 #pragma unroll
-        for (int i = 0; i < T::VD; ++i) { o[i][0] *= f; o[i][1] *= f; o[i][2] *= f; o[i][3] *= f; }
+        for (int i = 0; i < MT; ++i) { o[i][x][0] *= f; o[i][x][1] *= f; o[i][x][2] *= f; o[i][x][3] *= f; }
       }
-      // output: 16 keys at a time
 #pragma unroll
-      for (int t = 0; t < T::TK / 16; ++t) {
-        uint32_t pa[4];
-        split2(s[2 * t][0] * inv, s[2 * t][1] * inv, &pa[0], &pa[1]);
-        split2(s[2 * t + 1][0] * inv, s[2 * t + 1][1] * inv, &pa[2], &pa[3]);
-        const auto &v0 = vw[4 * t], &v1 = vw[4 * t + 1], &v2 = vw[4 * t + 2], &v3 = vw[4 * t + 3];
-        if constexpr (BITS == 4) {
+      for (int j = 0; j < T::NT; ++j) s[x][j] *= inv;
+    }
+    // output: 16 keys at a time.  The weights go from (key, head) lanes to (column, key) lanes: column g is head g / 2, hi or lo.
+    const int from = 8 * c + (g >> 1);
 #pragma unroll
-          for (int h = 0; h < T::VD / 4; ++h) {                      // four columns of two keys share a word
-            uint32_t b0[4], b1[4];
-            nibbles(__byte_perm(v0.w[h >> 1], v1.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), b0);
-            nibbles(__byte_perm(v2.w[h >> 1], v3.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), b1);
+    for (int t = 0; t < T::TK / 16; ++t) {
+      uint32_t pb[NH][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) mma(o[4 * h + j], pa, b0[j], b1[j]);
+      for (int x = 0; x < NH; ++x) {
+        uint32_t hi, lo;
+        split2(s[x][2 * t], s[x][2 * t + 1], &hi, &lo);
+        const uint32_t ha = __shfl_sync(FULL, hi, from), hb = __shfl_sync(FULL, hi, from + 4);
+        const uint32_t la = __shfl_sync(FULL, lo, from), lb = __shfl_sync(FULL, lo, from + 4);
+        const uint32_t wa = (g & 1) ? la : ha, wb = (g & 1) ? lb : hb;
+        pb[x][0] = __byte_perm(wa, wb, 0x5410);                      // keys 2 c, 2 c + 1
+        pb[x][1] = __byte_perm(wa, wb, 0x7632);                      // keys 2 c + 8, 2 c + 9
+      }
+      const auto &v0 = in.vw[4 * t], &v1 = in.vw[4 * t + 1], &v2 = in.vw[4 * t + 2], &v3 = in.vw[4 * t + 3];
+      if constexpr (BITS == 4) {
+#pragma unroll
+        for (int h = 0; h < T::VD / 4; ++h) {                        // four columns of two keys share a word
+          uint32_t p[4], q[4];
+          nibbles(__byte_perm(v0.w[h >> 1], v1.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), p);
+          nibbles(__byte_perm(v2.w[h >> 1], v3.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), q);
+#pragma unroll
+          for (int x = 0; x < NH; ++x) {
+            mma(o[2 * h][x], p[0], p[1], q[0], q[1], pb[x][0], pb[x][1]);
+            mma(o[2 * h + 1][x], p[2], p[3], q[2], q[3], pb[x][0], pb[x][1]);
           }
-        } else {
-          const __half2 off = u2h(0x64806480u);
+        }
+      } else {
 #pragma unroll
-          for (int i = 0; i < T::VD; ++i) {
-            const uint32_t sel = (uint32_t)(i & 3) | (uint32_t)(4 + (i & 3)) << 8;     // byte i of both words, to bytes 0 and 2
-            const uint32_t x0 = __byte_perm(v0.w[i >> 2], v1.w[i >> 2], sel), x1 = __byte_perm(v2.w[i >> 2], v3.w[i >> 2], sel);
-            mma(o[i], pa, h2u(__hsub2(u2h(and_or(x0, 0x00ff00ffu, 0x64006400u)), off)),
-                h2u(__hsub2(u2h(and_or(x1, 0x00ff00ffu, 0x64006400u)), off)));
+        for (int i = 0; i < T::VD; i += 2) {
+          uint32_t p[2], q[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t sel = (uint32_t)((i + e) & 3) | (uint32_t)(4 + ((i + e) & 3)) << 8;     // byte i + e of both, to bytes 0 and 2
+            p[e] = centre(and_or(__byte_perm(v0.w[i >> 2], v1.w[i >> 2], sel), 0x00ff00ffu, 0x64006400u));
+            q[e] = centre(and_or(__byte_perm(v2.w[i >> 2], v3.w[i >> 2], sel), 0x00ff00ffu, 0x64006400u));
           }
+#pragma unroll
+          for (int x = 0; x < NH; ++x) mma(o[i / 2][x], p[0], p[1], q[0], q[1], pb[x][0], pb[x][1]);
         }
       }
     }
-    l += __shfl_xor_sync(FULL, l, 1);
-    l += __shfl_xor_sync(FULL, l, 2);
+  }
+
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int x = 0; x < NH; ++x) {
+#pragma unroll
+      for (int w = 4; w < 32; w <<= 1) l[x] += __shfl_xor_sync(FULL, l[x], w);
+    }
+  }
+  // output column g VD + i of head 4 x + c, in units of sc
+  __device__ __forceinline__ float value(int x, int i) const {
+    return fmaf(o[i >> 1][x][2 * (i & 1) + 1], 1.f / kLo, o[i >> 1][x][2 * (i & 1)]);
   }
 };
 
-// BY_BLOCK false: a warp per unit.  true: all warps of a cluster (of one block or more) work on one unit.
-template <int BITS, int DP, bool BY_BLOCK>
-__global__ void __launch_bounds__(32 * WARPS) cached_attend_kernel(const AttendArgs a) {
+// BY_BLOCK false: a warp per `take` neighbouring units (all of a root, or one).  true: all warps of a cluster (of one block or more)
+// work on one unit.
+template <int BITS, int DP, int NH, bool BY_BLOCK>
+__global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 128 ? 3 : 5) cached_attend_kernel(const AttendArgs a) {
   using T = Tile<BITS, DP>;
+  constexpr int GH = 4 * NH;                                        // query heads of a unit
   __shared__ double s_bounds[kMaxBuckets];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   if (a.bias) {
@@ -343,46 +463,75 @@ __global__ void __launch_bounds__(32 * WARPS) cached_attend_kernel(const AttendA
     ranks = (int)cg::this_cluster().num_blocks();
     rank = (int)cg::this_cluster().block_rank();
   }
-  const uint32_t unit = BY_BLOCK ? blockIdx.x / (uint32_t)ranks : blockIdx.x * WARPS + wid;
-  if (unit >= a.units) return;                                      // (by warp: no barrier follows; by block: the grid fits)
-  const uint32_t pass = unit % (uint32_t)a.passes, rest = unit / (uint32_t)a.passes;
-  const int kv = (int)(rest % (uint32_t)a.kv_heads);
-  const int64_t root = rest / (uint32_t)a.kv_heads;
-  const int head0 = kv * a.group + (int)pass * GH;
-  const int nh = min(GH, (kv + 1) * a.group - head0);
-  const int64_t first = a.first[root];
+  const uint32_t unit0 = BY_BLOCK ? blockIdx.x / (uint32_t)ranks : (blockIdx.x * WARPS + wid) * (uint32_t)a.take;
+  if (unit0 >= a.units) return;                                     // (by warp: no barrier follows; by block: the grid fits)
+  const int per_root = a.passes * a.kv_heads;
+  const int64_t root = unit0 / (uint32_t)per_root;
+  const int sub = (int)(unit0 - (uint32_t)root * (uint32_t)per_root);   // unit of the root: cached head, and which of its query heads
+  Seen seen;
+  seen.first = a.first[root];
   int len = a.len[root];
-  if (first < 0 || len < 0 || first > a.rows - len) {
+  seen.t = a.bias ? a.times[root] : 0.0;
+  if (seen.first < 0 || len < 0 || seen.first > a.rows - len) {
     if (lane == 0) atomicMax(a.status, 4);
     len = 0;
   }
   const int lo = len > a.window ? len - a.window : 0;
-  const int ns = min(a.sinks, lo);
-  const int n = len - lo + ns;
-  Walk<BITS, DP> w;
-  w.run(a, s_bounds, root, kv, head0, first, lo, ns, n, BY_BLOCK ? rank * WARPS + wid : 0, BY_BLOCK ? ranks * WARPS : 1);
-
-  if constexpr (!BY_BLOCK) {
-    const float f = w.l == 0.f ? 0.f : w.sc / w.l;                   // nothing seen, or nothing but -infinity: zeros
-    const int64_t base = (root * a.heads + head0 + g) * a.dim;
-    if (g < nh) {
+  seen.ns = min(a.sinks, lo);
+  seen.n = len - lo + seen.ns;
+  seen.skip = lo - seen.ns;
+  const int tiles = (seen.n + T::TK - 1) / T::TK;
+  const int worker = BY_BLOCK ? rank * WARPS + wid : 0, workers = BY_BLOCK ? ranks * WARPS : 1;
+  Walk<BITS, DP, NH> w;
+  int kv = sub / a.passes, pass = sub - kv * a.passes;
+  for (int left = BY_BLOCK ? 1 : a.take; left > 0; --left) {
+    const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
+    const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : nullptr;
+    if (worker < tiles) {
+      Rows<BITS, DP> rows;
+      rows.load(a, seen, kv, worker);                               // on their way while the query is prepared
+      w.begin(a, root, head0, nh);
+      for (int tile = worker;;) {
+        w.tile(a, s_bounds, bias, seen, rows, tile * T::TK, nh);
+        tile += workers;
+        if (tile >= tiles) break;
+        rows.load(a, seen, kv, tile);
+      }
+      w.finish();
+    } else {
+      w.none();
+    }
+    if constexpr (!BY_BLOCK) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int x = 0; x < NH; ++x) {
+        const int h = 4 * x + c;
+        const float f = w.l[x] == 0.f ? 0.f : w.sc[x] / w.l[x];      // nothing seen, or nothing but -infinity: zeros
+        const int64_t base = (root * a.heads + head0 + h) * a.dim;
+        if (h < nh) {
 #pragma unroll
-        for (int i = 0; i < T::VD; ++i) {
-          const int e = (2 * c + h) * T::VD + i;
-          if (e < a.dim) store_out(a.out, a.dtype, base + e, fmaf(w.o[i][2 + h], 1.f / kLo, w.o[i][h]) * f);
+          for (int i = 0; i < T::VD; i += 2) {
+            const int e = g * T::VD + i;
+            if (a.pairs) {
+              if (e < a.dim) store_pair(a, base + e, w.value(x, i) * f, w.value(x, i + 1) * f);
+            } else {
+              if (e < a.dim) store_out(a, base + e, w.value(x, i) * f);
+              if (e + 1 < a.dim) store_out(a, base + e + 1, w.value(x, i + 1) * f);
+            }
+          }
         }
       }
+      if (++pass == a.passes) { pass = 0; ++kv; }                    // the unit behind
     }
-  } else {
+  }
+  if constexpr (BY_BLOCK) {
+    const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
     __shared__ float s_o[WARPS][GH][DP + 4], s_m[WARPS][GH], s_l[WARPS][GH], b_m[GH], b_l[GH];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int x = 0; x < NH; ++x) {
 #pragma unroll
-      for (int i = 0; i < T::VD; ++i) s_o[wid][g][(2 * c + h) * T::VD + i] = fmaf(w.o[i][2 + h], 1.f / kLo, w.o[i][h]) * w.sc;
+      for (int i = 0; i < T::VD; ++i) s_o[wid][4 * x + c][g * T::VD + i] = w.value(x, i) * w.sc[x];
+      if (g == 0) { s_m[wid][4 * x + c] = w.m[x]; s_l[wid][4 * x + c] = w.l[x]; }
     }
-    if (c == 0) { s_m[wid][g] = w.m; s_l[wid][g] = w.l; }
     __syncthreads();
     // the block's sums, at the block's maximum
     for (int i = threadIdx.x; i < nh * DP; i += 32 * WARPS) {
@@ -399,7 +548,7 @@ __global__ void __launch_bounds__(32 * WARPS) cached_attend_kernel(const AttendA
         l = fmaf(s_l[x][h], f, l);
       }
       if (ranks == 1) {
-        if (e < a.dim) store_out(a.out, a.dtype, (root * a.heads + head0 + h) * a.dim + e, l == 0.f ? 0.f : o / l);
+        if (e < a.dim) store_out(a, (root * a.heads + head0 + h) * a.dim + e, l == 0.f ? 0.f : o / l);
       } else {
         s_o[0][h][e] = o;                                            // this thread alone reads and writes column e of head h
         if (e == 0) { b_m[h] = top; b_l[h] = l; }
@@ -421,31 +570,33 @@ __global__ void __launch_bounds__(32 * WARPS) cached_attend_kernel(const AttendA
         o = fmaf(*cl.map_shared_rank(&s_o[0][h][e], r), f, o);
         l = fmaf(*cl.map_shared_rank(&b_l[h], r), f, l);
       }
-      store_out(a.out, a.dtype, (root * a.heads + head0 + h) * a.dim + e, l == 0.f ? 0.f : o / l);
+      store_out(a, (root * a.heads + head0 + h) * a.dim + e, l == 0.f ? 0.f : o / l);
     }
     cl.sync();                                                       // no block leaves while its memory is read
   }
 }
 
 // Warps on one unit: by warp, unless the units leave most of the machine's warps without work and a unit has more tiles than
-// a warp should walk alone.
+// a warp should walk alone.  By warp, a warp takes all units of a root where the roots alone fill the machine.
 struct Shape {
   bool by_block;
-  int ranks;
+  int ranks, take;
 };
-Shape choose(int64_t units, int64_t tiles) {
-  Shape s = {false, 1};
+Shape choose(int64_t roots, int per_root, int64_t tiles) {
+  const int64_t units = roots * per_root;
   const int64_t machine = (int64_t)num_sms() * 12;                   // warps that are resident together
+  Shape s = {false, 1, roots >= machine ? per_root : 1};
   if (tiles <= 2 || units >= 2 * machine) return s;
   s.by_block = true;
   while (s.ranks < 8 && units * WARPS * s.ranks * 2 <= machine && tiles >= 2 * WARPS * s.ranks * 2) s.ranks *= 2;
   return s;
 }
 
-template <int BITS, int DP>
+template <int BITS, int DP, int NH>
 cudaError_t launch(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
   if (!sh.by_block) {
-    cached_attend_kernel<BITS, DP, false><<<(a.units + WARPS - 1) / WARPS, 32 * WARPS, 0, s>>>(a);
+    const unsigned per = (unsigned)(WARPS * a.take);
+    cached_attend_kernel<BITS, DP, NH, false><<<(a.units + per - 1) / per, 32 * WARPS, 0, s>>>(a);
     return cudaGetLastError();
   }
   cudaLaunchConfig_t cfg = {};
@@ -458,15 +609,20 @@ cudaError_t launch(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, cached_attend_kernel<BITS, DP, true>, a);
+  return cudaLaunchKernelEx(&cfg, cached_attend_kernel<BITS, DP, NH, true>, a);
+}
+
+template <int BITS, int DP>
+cudaError_t launch_heads(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
+  return a.group > 4 ? launch<BITS, DP, 2>(a, sh, s) : launch<BITS, DP, 1>(a, sh, s);
 }
 
 template <int BITS>
 cudaError_t launch_dim(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
   switch (padded_dim(a.dim)) {
-    case 32: return launch<BITS, 32>(a, sh, s);
-    case 64: return launch<BITS, 64>(a, sh, s);
-    default: return launch<BITS, 128>(a, sh, s);
+    case 32: return launch_heads<BITS, 32>(a, sh, s);
+    case 64: return launch_heads<BITS, 64>(a, sh, s);
+    default: return launch_heads<BITS, 128>(a, sh, s);
   }
 }
 
@@ -499,7 +655,7 @@ extern "C" int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_
     return fail(err_host, err_size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", who);
   AttendArgs a = {};
   a.group = heads / k.heads;
-  a.passes = (a.group + GH - 1) / GH;
+  a.passes = a.group > 4 ? (a.group + 7) / 8 : 1;
   if (n > 0x0fffffff / ((int64_t)k.heads * a.passes)) return fail(err_host, err_size, TGNN_ECAPACITY, "%s: n * heads above 2^28", who);
   if (n == 0) return TGNN_OK;
   a.q = q;
@@ -532,8 +688,10 @@ extern "C" int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_
   int64_t see = (int64_t)window + sinks;
   if (max_len > 0 && max_len < see) see = max_len;
   if (k.rows < see) see = k.rows;
-  const int tk = k.bits == 8 && padded_dim(k.dim) == 128 ? 16 : 32;
-  const Shape sh = choose(a.units, (see + tk - 1) / tk);
+  const int tk = k.bits * padded_dim(k.dim) >= 1024 ? 16 : 32;
+  const Shape sh = choose(n, k.heads * a.passes, (see + tk - 1) / tk);
+  a.take = sh.take;
+  a.pairs = k.dim % 2 == 0 && (((uintptr_t)q | (uintptr_t)out) & (2 * es + 1)) == 0;
   const cudaError_t e = k.bits == 4 ? launch_dim<4>(a, sh, (cudaStream_t)stream) : launch_dim<8>(a, sh, (cudaStream_t)stream);
   if (e != cudaSuccess) {
     cudaGetLastError();
