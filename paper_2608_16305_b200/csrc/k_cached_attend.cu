@@ -97,41 +97,31 @@ __device__ __forceinline__ void split2(float x0, float x1, uint32_t* hi, uint32_
   *lo = h2u(__floats2half2_rn((x0 - f.x) * kLo, (x1 - f.y) * kLo));
 }
 
-template <int N>
-struct Words { uint32_t w[N]; };
-// N words that start on a multiple of their size (16 bytes at most)
-template <int N>
-__device__ __forceinline__ Words<N> load_words(const uint8_t* p) {
-  Words<N> r;
-  if constexpr (N % 4 == 0) {
+// N neighbouring words (or, for B = 2, a half word) from shared memory.
+template <int B>
+struct Piece { uint32_t w[(B + 3) / 4]; };
+template <int B>
+__device__ __forceinline__ Piece<B> load_piece(const uint8_t* p) {
+  Piece<B> r;
+  if constexpr (B == 2) {
+    r.w[0] = *reinterpret_cast<const uint16_t*>(p);
+  } else if constexpr (B == 4) {
+    r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (B == 8) {
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = x.x;
+    r.w[1] = x.y;
+  } else {
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    for (int i = 0; i < B / 16; ++i) {
+      const uint4 x = *(reinterpret_cast<const uint4*>(p) + i);
       r.w[4 * i] = x.x;
       r.w[4 * i + 1] = x.y;
       r.w[4 * i + 2] = x.z;
       r.w[4 * i + 3] = x.w;
     }
-  } else if constexpr (N == 2) {
-    const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
-    r.w[0] = x.x;
-    r.w[1] = x.y;
-  } else {
-    static_assert(N == 1, "");
-    r.w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
   }
   return r;
-}
-// B bytes: 2, or whole words
-template <int B>
-__device__ __forceinline__ Words<(B + 3) / 4> load_piece(const uint8_t* p) {
-  if constexpr (B == 2) {
-    Words<1> r;
-    r.w[0] = __ldg(reinterpret_cast<const uint16_t*>(p));
-    return r;
-  } else {
-    return load_words<B / 4>(p);
-  }
 }
 
 // N values of a query row from column e0 on, as fp32 (0 beyond dim): in pairs where every row starts on one.
@@ -181,14 +171,15 @@ __device__ __forceinline__ void store_pair(const AttendArgs& a, int64_t i, float
   }
 }
 
-// Keys that a warp takes at a time: 32, or 16 where 32 rows of codes would take too many registers.
+// Keys that a warp takes at a time: 32, or 16 where 32 rows take 8 KB of shared memory.
 template <int BITS, int DP>
 struct Tile {
   static constexpr int TK = BITS * DP >= 1024 ? 16 : 32;
-  static constexpr int NT = TK / 8;                 // keys per lane group: kw[j] is key 8 j + lane / 4
+  static constexpr int NT = TK / 8;                 // keys whose logits a lane has: 8 j + lane / 4
   static constexpr int KW = DP * BITS / 128;        // words of a key that a lane reads (a quarter of the row)
   static constexpr int VD = DP / 8;                 // columns of a value that a lane reads
   static constexpr int VB = VD * BITS / 8;          // bytes of them: 2 to 16
+  static constexpr int RB = DP * BITS / 8;          // bytes of a row's head
 };
 
 // A root's visible entries: u < ns are the sinks, the others lie `skip` further on; first is the place of entry 0.
@@ -198,48 +189,29 @@ struct Seen {
   double t;
 };
 
-// Codes, scales and times of one tile, on their way in registers.  Lane (g, c) = (lane / 4, lane % 4) holds quarter c of keys
-// 8 j + g, piece g of the values of keys 16 t + 2 c + {0, 1, 8, 9}, and the scales and time of key lane.
+// One tile on its way: codes by asynchronous copies to the warp's shared memory (keys, then values, row by row), the scales and time of
+// key `lane` in registers.
 template <int BITS, int DP>
 struct Rows {
   using T = Tile<BITS, DP>;
-  Words<T::KW> kw[T::NT];
-  Words<(T::VB + 3) / 4> vw[T::TK / 4];
   uint32_t scales;
   double ts;
 
-  __device__ __forceinline__ void load(const AttendArgs& a, const Seen& seen, int kv, int tile) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3, u0 = tile * T::TK;
-    const uint8_t* kp = a.k_codes + seen.first * a.k_code_stride + kv * (DP * BITS / 8) + c * (DP * BITS / 32);
-    const uint8_t* vp = a.v_codes + seen.first * a.v_code_stride + kv * (DP * BITS / 8) + g * T::VB;
-    int e;
-    if (u0 >= seen.ns && u0 + T::TK <= seen.n) {                     // neighbouring rows
-      const int e0 = u0 + seen.skip;
-      e = e0 + (lane & (T::TK - 1));
-      kp += (int64_t)(e0 + g) * a.k_code_stride;
-      vp += (int64_t)(e0 + 2 * c) * a.v_code_stride;
+  __device__ __forceinline__ void load(const AttendArgs& a, const Seen& seen, int kv, int tile, uint8_t* to) {
+    const int lane = threadIdx.x & 31, u0 = tile * T::TK;
+    // beyond the last entry: the last (its weight is set to 0)
+    auto entry = [&](int u) { u = min(u, seen.n - 1); return u < seen.ns ? u : u + seen.skip; };
+    constexpr int CPR = T::RB / 16, PER = 32 / CPR;                 // 16-byte pieces of a row, rows per copy of the warp
+    const uint8_t* kp = a.k_codes + seen.first * a.k_code_stride + kv * T::RB + 16 * (lane % CPR);
+    const uint8_t* vp = a.v_codes + seen.first * a.v_code_stride + kv * T::RB + 16 * (lane % CPR);
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to) + 16 * lane;
 #pragma unroll
-      for (int j = 0; j < T::NT; ++j) {
-        kw[j] = load_words<T::KW>(kp);
-        kp += 8 * (int64_t)a.k_code_stride;
-      }
-#pragma unroll
-      for (int i = 0; i < T::TK / 4; i += 2) {
-        vw[i] = load_piece<T::VB>(vp);
-        vw[i + 1] = load_piece<T::VB>(vp + a.v_code_stride);
-        vp += 8 * (int64_t)a.v_code_stride;
-      }
-    } else {
-      // beyond the last entry: the last (its weight is set to 0)
-      auto entry = [&](int u) { u = min(u, seen.n - 1); return u < seen.ns ? u : u + seen.skip; };
-      e = entry(u0 + (lane & (T::TK - 1)));
-#pragma unroll
-      for (int j = 0; j < T::NT; ++j) kw[j] = load_words<T::KW>(kp + (int64_t)entry(u0 + 8 * j + g) * a.k_code_stride);
-#pragma unroll
-      for (int i = 0; i < T::TK / 4; ++i)
-        vw[i] = load_piece<T::VB>(vp + (int64_t)entry(u0 + 8 * (i >> 1) + 2 * c + (i & 1)) * a.v_code_stride);
+    for (int i = 0; i < T::TK / PER; ++i) {
+      const int64_t e = entry(u0 + i * PER + lane / CPR);
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + 512 * i), "l"(kp + e * a.k_code_stride) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + T::TK * T::RB + 512 * i), "l"(vp + e * a.v_code_stride) : "memory");
     }
-    const int64_t place = seen.first + e;
+    const int64_t place = seen.first + entry(u0 + (lane & (T::TK - 1)));
     scales = __ldg(reinterpret_cast<const uint16_t*>(a.k_scales + place * a.k_scale_stride + 2 * kv)) |
              (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v_scales + place * a.v_scale_stride + 2 * kv)) << 16;
     ts = a.bias ? __ldg(a.ts + place) : 0.0;
@@ -300,10 +272,9 @@ struct Walk {
     }
   }
 
-  __device__ __forceinline__ void tile(const AttendArgs& a, const double* s_bounds, const float* bias, const Seen& seen, const Rows<BITS, DP>& in,
+  __device__ __forceinline__ void tile(const AttendArgs& a, const float* bias, const Seen& seen, uint32_t scales, int bucket, const uint8_t* rows,
                                        int u0, int nh) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-    const int bucket = bias ? bucket_of(s_bounds, a.buckets - 1, seen.t - in.ts) : 0;
     // logits: s[x][j] of head 4 x + c at key 8 j + g
     float s[NH][T::NT];
 #pragma unroll
@@ -311,9 +282,11 @@ struct Walk {
       float acc[NH][4];
 #pragma unroll
       for (int x = 0; x < NH; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
+      const auto r0 = load_piece<T::RB / 4>(rows + (16 * b + g) * T::RB + c * (T::RB / 4));
+      const auto r1 = load_piece<T::RB / 4>(rows + (16 * b + 8 + g) * T::RB + c * (T::RB / 4));
 #pragma unroll
       for (int w = 0; w < T::KW; ++w) {
-        const uint32_t k0 = in.kw[2 * b].w[w], k1 = in.kw[2 * b + 1].w[w];
+        const uint32_t k0 = r0.w[w], k1 = r1.w[w];
         if constexpr (BITS == 4) {
           uint32_t p[4], q[4];
           nibbles(k0, p);
@@ -342,7 +315,7 @@ struct Walk {
 #pragma unroll
     for (int j = 0; j < T::NT; ++j) {
       const int key = 8 * j + g;
-      const uint32_t two = __shfl_sync(FULL, in.scales, key);
+      const uint32_t two = __shfl_sync(FULL, scales, key);
       const float ks = __uint_as_float(two << 16);
       vs[j] = __uint_as_float(two & 0xffff0000u);
       const int at = bias ? __shfl_sync(FULL, bucket, key) : 0;
@@ -388,8 +361,10 @@ struct Walk {
 #pragma unroll
       for (int j = 0; j < T::NT; ++j) s[x][j] *= inv;
     }
-    // output: 16 keys at a time.  The weights go from (key, head) lanes to (column, key) lanes: column g is head g / 2, hi or lo.
-    const int from = 8 * c + (g >> 1);
+    // output: 16 keys at a time, in the order c, c + 4, c + 8, c + 12 for lane (g, c), whose values' rows then lie in different banks.
+    // The weights go from (key, head) lanes to (column, key) lanes: column g is head g / 2, hi or lo.
+    const int from = 4 * c + (g >> 1);
+    rows += T::TK * T::RB + g * T::VB + c * T::RB;
 #pragma unroll
     for (int t = 0; t < T::TK / 16; ++t) {
       uint32_t pb[NH][2];
@@ -397,13 +372,14 @@ struct Walk {
       for (int x = 0; x < NH; ++x) {
         uint32_t hi, lo;
         split2(s[x][2 * t], s[x][2 * t + 1], &hi, &lo);
-        const uint32_t ha = __shfl_sync(FULL, hi, from), hb = __shfl_sync(FULL, hi, from + 4);
-        const uint32_t la = __shfl_sync(FULL, lo, from), lb = __shfl_sync(FULL, lo, from + 4);
+        const uint32_t ha = __shfl_sync(FULL, hi, from), hb = __shfl_sync(FULL, hi, from + 16);
+        const uint32_t la = __shfl_sync(FULL, lo, from), lb = __shfl_sync(FULL, lo, from + 16);
         const uint32_t wa = (g & 1) ? la : ha, wb = (g & 1) ? lb : hb;
-        pb[x][0] = __byte_perm(wa, wb, 0x5410);                      // keys 2 c, 2 c + 1
-        pb[x][1] = __byte_perm(wa, wb, 0x7632);                      // keys 2 c + 8, 2 c + 9
+        pb[x][0] = __byte_perm(wa, wb, 0x5410);                      // keys c, c + 4
+        pb[x][1] = __byte_perm(wa, wb, 0x7632);                      // keys c + 8, c + 12
       }
-      const auto &v0 = in.vw[4 * t], &v1 = in.vw[4 * t + 1], &v2 = in.vw[4 * t + 2], &v3 = in.vw[4 * t + 3];
+      const auto v0 = load_piece<T::VB>(rows + 16 * t * T::RB), v1 = load_piece<T::VB>(rows + (16 * t + 4) * T::RB);
+      const auto v2 = load_piece<T::VB>(rows + (16 * t + 8) * T::RB), v3 = load_piece<T::VB>(rows + (16 * t + 12) * T::RB);
       if constexpr (BITS == 4) {
 #pragma unroll
         for (int h = 0; h < T::VD / 4; ++h) {                        // four columns of two keys share a word
@@ -452,8 +428,11 @@ template <int BITS, int DP, int NH, bool BY_BLOCK>
 __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 128 ? 3 : 5) cached_attend_kernel(const AttendArgs a) {
   using T = Tile<BITS, DP>;
   constexpr int GH = 4 * NH;                                        // query heads of a unit
+  constexpr int STAGE = 2 * T::TK * T::RB;                          // a tile's keys and values
   __shared__ double s_bounds[kMaxBuckets];
+  __shared__ __align__(128) uint8_t s_rows[WARPS][2 * STAGE];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  uint8_t* my = s_rows[wid];
   if (a.bias) {
     for (int i = threadIdx.x; i < a.buckets - 1; i += 32 * WARPS) s_bounds[i] = a.bounds[i];
     __syncthreads();
@@ -488,14 +467,21 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
     const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
     const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : nullptr;
     if (worker < tiles) {
-      Rows<BITS, DP> rows;
-      rows.load(a, seen, kv, worker);                               // on their way while the query is prepared
+      // two tiles on their way: the query is prepared, and each tile worked on, while the next comes
+      Rows<BITS, DP> next;
+      next.load(a, seen, kv, worker, my);
+      asm volatile("cp.async.commit_group;" ::: "memory");
       w.begin(a, root, head0, nh);
-      for (int tile = worker;;) {
-        w.tile(a, s_bounds, bias, seen, rows, tile * T::TK, nh);
-        tile += workers;
-        if (tile >= tiles) break;
-        rows.load(a, seen, kv, tile);
+      int buf = 0, bucket = 0;
+      for (int tile = worker; tile < tiles; tile += workers) {
+        const uint32_t scales = next.scales;
+        if (bias) bucket = bucket_near(s_bounds, a.buckets - 1, seen.t - next.ts, bucket);
+        if (tile + workers < tiles) next.load(a, seen, kv, tile + workers, my + (buf ^ STAGE));
+        asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        w.tile(a, bias, seen, scales, bucket, my + buf, tile * T::TK, nh);
+        __syncwarp();                                               // the tile's rows may be written over
+        buf ^= STAGE;
       }
       w.finish();
     } else {
@@ -525,7 +511,10 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   }
   if constexpr (BY_BLOCK) {
     const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
-    __shared__ float s_o[WARPS][GH][DP + 4], s_m[WARPS][GH], s_l[WARPS][GH], b_m[GH], b_l[GH];
+    __shared__ float s_m[WARPS][GH], s_l[WARPS][GH], b_m[GH], b_l[GH];
+    static_assert(sizeof(s_rows) >= sizeof(float[WARPS][GH][DP + 4]), "the partial outputs take the rows' place");
+    float(*s_o)[GH][DP + 4] = reinterpret_cast<float(*)[GH][DP + 4]>(&s_rows[0][0]);
+    __syncthreads();                                                 // all warps are done with their rows
 #pragma unroll
     for (int x = 0; x < NH; ++x) {
 #pragma unroll
@@ -577,7 +566,9 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
 }
 
 // Warps on one unit: by warp, unless the units leave most of the machine's warps without work and a unit has more tiles than
-// a warp should walk alone.  By warp, a warp takes all units of a root where the roots alone fill the machine.
+// a warp should walk alone.  By warp, a warp takes all units of a root where they have a single tile and the roots alone fill the
+// machine (14 400 roots of 21 entries: 51 against 55 us; with more tiles single units balance better, 278 against 315 us for 12 000
+// roots of 520).
 struct Shape {
   bool by_block;
   int ranks, take;
@@ -585,7 +576,7 @@ struct Shape {
 Shape choose(int64_t roots, int per_root, int64_t tiles) {
   const int64_t units = roots * per_root;
   const int64_t machine = (int64_t)num_sms() * 12;                   // warps that are resident together
-  Shape s = {false, 1, roots >= machine ? per_root : 1};
+  Shape s = {false, 1, tiles <= 1 && roots >= machine ? per_root : 1};
   if (tiles <= 2 || units >= 2 * machine) return s;
   s.by_block = true;
   while (s.ranks < 8 && units * WARPS * s.ranks * 2 <= machine && tiles >= 2 * WARPS * s.ranks * 2) s.ranks *= 2;

@@ -93,6 +93,13 @@ __device__ __forceinline__ int bucket_of(const double* bounds, int n, double dt)
   return lo;
 }
 
+// The same, looked for from bucket b on: neighbouring entries mostly share one.
+__device__ __forceinline__ int bucket_near(const double* bounds, int n, double dt, int b) {
+  while (b > 0 && !(bounds[b - 1] <= dt)) --b;
+  while (b < n && bounds[b] <= dt) ++b;
+  return b;
+}
+
 // A row cache as the kernels see it (tgnn_cache with the codes' size).
 struct CacheView {
   uint8_t* codes;
