@@ -43,7 +43,7 @@ struct AttendArgs {
   void* out;
   int dtype;
   const uint8_t *k_codes, *v_codes, *k_scales, *v_scales;
-  int k_code_stride, v_code_stride, k_scale_stride, v_scale_stride;
+  uint32_t k_code_stride, v_code_stride, k_scale_stride, v_scale_stride;
   int64_t rows;
   uint32_t units;
   int heads, kv_heads, group, passes, dim;    // group = heads / kv_heads, passes = ceil(group / heads of a unit)
@@ -182,11 +182,17 @@ struct Tile {
   static constexpr int RB = DP * BITS / 8;          // bytes of a row's head
 };
 
-// A root's visible entries: u < ns are the sinks, the others lie `skip` further on; first is the place of entry 0.
+// A root's visible entries: u < ns are the sinks, the others lie `skip` further on.  The pointers are those of entry 0 for the lane's
+// part of a row (codes, of the unit's cached head) and for whole rows (scales of that head, times).
 struct Seen {
-  int64_t first;
   int n, ns, skip;
   double t;
+  const uint8_t *k, *v, *ks, *vs;
+  const double* ts;
+  __device__ __forceinline__ uint32_t entry(int u) const {          // beyond the last entry: the last (its weight is set to 0)
+    u = min(u, n - 1);
+    return (uint32_t)(u < ns ? u : u + skip);
+  }
 };
 
 // One tile on its way: codes by asynchronous copies to the warp's shared memory (keys, then values, row by row), the scales and time of
@@ -197,24 +203,22 @@ struct Rows {
   uint32_t scales;
   double ts;
 
-  __device__ __forceinline__ void load(const AttendArgs& a, const Seen& seen, int kv, int tile, uint8_t* to) {
+  __device__ __forceinline__ void load(const AttendArgs& a, const Seen& seen, int tile, uint32_t to) {
     const int lane = threadIdx.x & 31, u0 = tile * T::TK;
-    // beyond the last entry: the last (its weight is set to 0)
-    auto entry = [&](int u) { u = min(u, seen.n - 1); return u < seen.ns ? u : u + seen.skip; };
     constexpr int CPR = T::RB / 16, PER = 32 / CPR;                 // 16-byte pieces of a row, rows per copy of the warp
-    const uint8_t* kp = a.k_codes + seen.first * a.k_code_stride + kv * T::RB + 16 * (lane % CPR);
-    const uint8_t* vp = a.v_codes + seen.first * a.v_code_stride + kv * T::RB + 16 * (lane % CPR);
-    const uint32_t at = (uint32_t)__cvta_generic_to_shared(to) + 16 * lane;
 #pragma unroll
     for (int i = 0; i < T::TK / PER; ++i) {
-      const int64_t e = entry(u0 + i * PER + lane / CPR);
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + 512 * i), "l"(kp + e * a.k_code_stride) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at + T::TK * T::RB + 512 * i), "l"(vp + e * a.v_code_stride) : "memory");
+      const uint32_t e = seen.entry(u0 + i * PER + lane / CPR);
+      const uint8_t *kp = seen.k + (uint64_t)e * a.k_code_stride, *vp = seen.v + (uint64_t)e * a.v_code_stride;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * i), "l"(kp) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + T::TK * T::RB + 512 * i), "l"(vp) : "memory");
     }
-    const int64_t place = seen.first + entry(u0 + (lane & (T::TK - 1)));
-    scales = __ldg(reinterpret_cast<const uint16_t*>(a.k_scales + place * a.k_scale_stride + 2 * kv)) |
-             (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(a.v_scales + place * a.v_scale_stride + 2 * kv)) << 16;
-    ts = a.bias ? __ldg(a.ts + place) : 0.0;
+    const int u = u0 + (lane & (T::TK - 1));
+    const uint32_t e = seen.entry(u);
+    const uint32_t ks = __ldg(reinterpret_cast<const uint16_t*>(seen.ks + (uint64_t)e * a.k_scale_stride));
+    const uint32_t vs = __ldg(reinterpret_cast<const uint16_t*>(seen.vs + (uint64_t)e * a.v_scale_stride));
+    scales = u < seen.n ? ks | vs << 16 : 0;                        // hidden keys' values weigh nothing
+    if (a.bias) ts = __ldg(seen.ts + e);
   }
 };
 
@@ -341,7 +345,7 @@ struct Walk {
       for (int j = 0; j < T::NT; ++j) {
         const float p = exp2_fast((s[x][j] - base) * kLog2e);
         sum += p;
-        s[x][j] = u0 + 8 * j + g < seen.n ? p * vs[j] : 0.f;
+        s[x][j] = p * vs[j];
         wmax[x] = fmaxf(wmax[x], s[x][j]);
       }
       l[x] = fmaf(l[x], corr, sum);
@@ -429,12 +433,12 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   using T = Tile<BITS, DP>;
   constexpr int GH = 4 * NH;                                        // query heads of a unit
   constexpr int STAGE = 2 * T::TK * T::RB;                          // a tile's keys and values
-  __shared__ double s_bounds[kMaxBuckets];
+  __shared__ double s_bounds[kMaxBuckets + 1];
   __shared__ __align__(128) uint8_t s_rows[WARPS][2 * STAGE];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   uint8_t* my = s_rows[wid];
   if (a.bias) {
-    for (int i = threadIdx.x; i < a.buckets - 1; i += 32 * WARPS) s_bounds[i] = a.bounds[i];
+    stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, 32 * WARPS);
     __syncthreads();
   }
   int ranks = 1, rank = 0;
@@ -448,12 +452,12 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   const int64_t root = unit0 / (uint32_t)per_root;
   const int sub = (int)(unit0 - (uint32_t)root * (uint32_t)per_root);   // unit of the root: cached head, and which of its query heads
   Seen seen;
-  seen.first = a.first[root];
+  int64_t first = a.first[root];
   int len = a.len[root];
   seen.t = a.bias ? a.times[root] : 0.0;
-  if (seen.first < 0 || len < 0 || seen.first > a.rows - len) {
+  if (first < 0 || len < 0 || first > a.rows - len) {
     if (lane == 0) atomicMax(a.status, 4);
-    len = 0;
+    first = len = 0;
   }
   const int lo = len > a.window ? len - a.window : 0;
   seen.ns = min(a.sinks, lo);
@@ -463,20 +467,27 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   const int worker = BY_BLOCK ? rank * WARPS + wid : 0, workers = BY_BLOCK ? ranks * WARPS : 1;
   Walk<BITS, DP, NH> w;
   int kv = sub / a.passes, pass = sub - kv * a.passes;
+  constexpr int CPR = T::RB / 16;
+  seen.k = a.k_codes + first * a.k_code_stride + 16 * (lane % CPR) + kv * T::RB;
+  seen.v = a.v_codes + first * a.v_code_stride + 16 * (lane % CPR) + kv * T::RB;
+  seen.ks = a.k_scales + first * a.k_scale_stride + 2 * kv;
+  seen.vs = a.v_scales + first * a.v_scale_stride + 2 * kv;
+  seen.ts = a.ts + first;
+  const uint32_t to = (uint32_t)__cvta_generic_to_shared(my) + 16 * lane;
   for (int left = BY_BLOCK ? 1 : a.take; left > 0; --left) {
     const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
     const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : nullptr;
     if (worker < tiles) {
       // two tiles on their way: the query is prepared, and each tile worked on, while the next comes
       Rows<BITS, DP> next;
-      next.load(a, seen, kv, worker, my);
+      next.load(a, seen, worker, to);
       asm volatile("cp.async.commit_group;" ::: "memory");
       w.begin(a, root, head0, nh);
       int buf = 0, bucket = 0;
       for (int tile = worker; tile < tiles; tile += workers) {
         const uint32_t scales = next.scales;
         if (bias) bucket = bucket_near(s_bounds, a.buckets - 1, seen.t - next.ts, bucket);
-        if (tile + workers < tiles) next.load(a, seen, kv, tile + workers, my + (buf ^ STAGE));
+        if (tile + workers < tiles) next.load(a, seen, tile + workers, to + (buf ^ STAGE));
         asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
         __syncwarp();
         w.tile(a, bias, seen, scales, bucket, my + buf, tile * T::TK, nh);
@@ -506,7 +517,14 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
           }
         }
       }
-      if (++pass == a.passes) { pass = 0; ++kv; }                    // the unit behind
+      if (++pass == a.passes) {                                      // the unit behind
+        pass = 0;
+        ++kv;
+        seen.k += T::RB;
+        seen.v += T::RB;
+        seen.ks += 2;
+        seen.vs += 2;
+      }
     }
   }
   if constexpr (BY_BLOCK) {
@@ -656,10 +674,10 @@ extern "C" int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_
   a.v_codes = v.codes;
   a.k_scales = k.scales;
   a.v_scales = v.scales;
-  a.k_code_stride = (int)k.code_stride;
-  a.v_code_stride = (int)v.code_stride;
-  a.k_scale_stride = (int)k.scale_stride;
-  a.v_scale_stride = (int)v.scale_stride;
+  a.k_code_stride = (uint32_t)k.code_stride;
+  a.v_code_stride = (uint32_t)v.code_stride;
+  a.k_scale_stride = (uint32_t)k.scale_stride;
+  a.v_scale_stride = (uint32_t)v.scale_stride;
   a.rows = k.rows;
   a.heads = heads;
   a.kv_heads = k.heads;

@@ -138,11 +138,11 @@ template <typename T, int VB, int P, int NV>
 __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ double s_bounds[kMaxBuckets];
+  __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   uint8_t* bucket = smem + (size_t)wid * a.warp_bytes;
   if (a.bias) {
-    for (int i = threadIdx.x; i < a.buckets - 1; i += blockDim.x) s_bounds[i] = a.bounds[i];
+    stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
     __syncthreads();
   }
   const Lanes<P> me(lane, a.kv_heads);
@@ -234,7 +234,7 @@ template <typename T, int VB, int P, int NV>
 __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ double s_bounds[kMaxBuckets];
+  __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int H = a.heads, D = a.dim, ROW = a.kv_heads * D;
   const bool table = a.partial != nullptr;
@@ -246,9 +246,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
   float *s_m = reinterpret_cast<float*>(my + L.head), *s_l = s_m + H, *s_d = s_m + 2 * H;
   float* s_dq = reinterpret_cast<float*>(my + L.dq);
   double* tab = reinterpret_cast<double*>(my + L.table);
-  if (a.bias) {
-    for (int i = threadIdx.x; i < a.buckets - 1; i += blockDim.x) s_bounds[i] = a.bounds[i];
-  }
+  if (a.bias) stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
   if (table) {
     for (int i = lane; i < H * a.buckets; i += 32) tab[i] = 0.0;
   }
@@ -475,7 +473,12 @@ __global__ void __launch_bounds__(256) bias_sum_kernel(const double* __restrict_
   const int i = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
   if (i >= entries) return;
   double sum = 0.0;
-  for (int b = lane; b < blocks; b += 32) sum += partial[(int64_t)b * entries + i];
+#pragma unroll 8
+  for (int j = 0; j < (MAX_BLOCKS + 31) / 32; ++j) {           // a fixed number, so that the loads do not wait for one another
+    const int b = 32 * j + lane;
+    sum += b < blocks ? partial[(int64_t)b * entries + i] : 0.0;
+    if (32 * j + 32 >= blocks) break;
+  }
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
   if (lane == 0) dbias[i] = (float)sum;
 }

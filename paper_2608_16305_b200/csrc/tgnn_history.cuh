@@ -82,21 +82,22 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // Bucket of a time difference: how many of the n ascending bounds are <= dt.  The comparisons are in fp64, so a difference
-// on a bound lands where the definition says; NaN is above no bound.  Halving: ceil(log2(n + 1)) dependent loads.
-__device__ __forceinline__ int bucket_of(const double* bounds, int n, double dt) {
-  int lo = 0, hi = n;
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (bounds[mid] <= dt) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
+// on a bound lands where the definition says; NaN is above no bound.
+// In shared memory the bounds lie behind a -infinity and before +infinities: s[i] is bound i - 1, s[kMaxBuckets] the last.
+__device__ __forceinline__ void stage_bounds(double* s, const double* bounds, int n, int thread, int threads) {
+  for (int i = thread; i <= kMaxBuckets; i += threads) s[i] = i == 0 ? -INFINITY : i <= n ? bounds[i - 1] : INFINITY;
 }
-
-// The same, looked for from bucket b on: neighbouring entries mostly share one.
-__device__ __forceinline__ int bucket_near(const double* bounds, int n, double dt, int b) {
-  while (b > 0 && !(bounds[b - 1] <= dt)) --b;
-  while (b < n && bounds[b] <= dt) ++b;
+// Halving without branches: the largest i <= n with bounds 1 to i <= dt.
+__device__ __forceinline__ int bucket_of(const double* s, int n, double dt) {
+  int b = 0;
+#pragma unroll
+  for (int step = kMaxBuckets / 2; step > 0; step >>= 1)
+    if (s[b + step] <= dt) b += step;
+  return min(b, n);                                            // dt = +infinity passes the padding too
+}
+// The same for all lanes of a warp, where most of them share the bucket b of the last entry that they looked at.
+__device__ __forceinline__ int bucket_near(const double* s, int n, double dt, int b) {
+  if (!__all_sync(FULL, s[b] <= dt && dt < s[b + 1])) b = bucket_of(s, n, dt);
   return b;
 }
 
