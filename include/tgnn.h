@@ -564,7 +564,8 @@ TGNN_API int64_t tgnn_cache_code_bytes(int dim, int bits); /* of one head in a r
  *   rows: num_rows rows of heads * dim values of `dtype` (TGNN_F32, TGNN_BF16, TGNN_F16), row_stride values apart; src, dst: indices of
  *   index_bits (32 or 64) bits, NULL = i.  times: fp64[num_rows] moved along with the rows (write: from it, read: into it), or NULL.
  *   dst must name distinct rows (one that is named twice is left with parts of several).  src outside its table: zeros are written
- *   (codes, scale and time); dst outside: that row is skipped; status 4 for both.  n * heads is below 2^31. */
+ *   (codes, scale and time); dst outside: that row is skipped; status 4 for both.  n * heads is below 2^31, rows and num_rows below 2^32,
+ *   a table row shorter than 2^31 bytes. */
 TGNN_API int tgnn_cache_write(const tgnn_cache* cache_host, const void* rows, int dtype, int64_t num_rows, int64_t row_stride,
                               const void* src, const void* dst, int index_bits, int64_t n, const double* times, int32_t* status,
                               void* stream, char* err_host, int64_t err_size);

@@ -13,7 +13,8 @@
 // Layout: codes [heads][pad * bits / 8 bytes] per row, pad = 32, 64 or 128 values of a head (padding holds code 0), scales bf16 [heads]
 // per row, one fp64 time per row; each with a row stride of its own, so that a row can also be one record of a send buffer.
 //
-// Both kernels are bound by HBM: 8 values per thread, and the rows of four groups in flight per thread.
+// Both kernels are bound by HBM.  A lane takes two pieces of 8 values of a group, half a group apart, so that the neighbouring lanes of
+// a group move whole sectors and the index arithmetic of a row is shared by 16 values; two groups per lane are in flight.
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
@@ -21,11 +22,48 @@ using namespace tgnn_history;
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int U = 4;              // groups per thread, loaded together
+constexpr int U = 2;              // groups per lane, loaded together
 
-__device__ __forceinline__ int64_t index_at(const void* idx, int index64, int64_t i) {
+struct Move {
+  CacheView c;
+  int64_t num_rows;
+  uint32_t row_bytes;             // of a table row to the next
+  const void *src, *dst;
+  int index64;
+  uint32_t groups;
+  uint32_t heads_magic;           // g / heads = (g * magic) >> 32 >> shift for g < 2^31 and more than one head
+  int heads_shift;
+  double* times;
+  int32_t* status;
+  int lg;                         // 2^lg lanes per group: pad / 16
+};
+
+__device__ __forceinline__ int64_t index_at(const void* idx, int index64, uint32_t i) {
   if (!idx) return i;
   return index64 ? __ldg(reinterpret_cast<const long long*>(idx) + i) : (int64_t)__ldg(reinterpret_cast<const int*>(idx) + i);
+}
+
+// Index i of the group and its head; the table row and the cache row, negative where an index lies outside (recorded).
+struct Where {
+  int64_t row, place;
+  int head;
+};
+template <bool WRITE>
+__device__ __forceinline__ Where find(const Move& a, uint32_t g) {
+  Where w = {-1, -1, 0};
+  if (g < a.groups) {
+    const uint32_t i = a.c.heads == 1 ? g : __umulhi(g, a.heads_magic) >> a.heads_shift;
+    w.head = (int)(g - i * (uint32_t)a.c.heads);
+    w.row = index_at(WRITE ? a.src : a.dst, a.index64, i);
+    w.place = index_at(WRITE ? a.dst : a.src, a.index64, i);
+    const bool out_row = (uint64_t)w.row >= (uint64_t)a.num_rows, out_place = (uint64_t)w.place >= (uint64_t)a.c.rows;
+    if (out_row | out_place) {
+      atomicMax(a.status, 4);
+      if (out_row) w.row = -1;
+      if (out_place) w.place = -1;
+    }
+  }
+  return w;
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {      // NaN if either is
@@ -60,177 +98,154 @@ __device__ __forceinline__ void store8(T* row, int e0, int dim, const float (&v)
   }
 }
 
-// A group is handled by 2^lg neighbouring lanes (pad / 8 of them); groups are numbered row by row.
 template <typename T, int VB, int BITS>
-__global__ void __launch_bounds__(THREADS) cache_write_kernel(const CacheView c, const T* __restrict__ rows, int64_t num_rows,
-                                                              int64_t row_stride, const void* __restrict__ src,
-                                                              const void* __restrict__ dst, int index64, uint32_t groups,
-                                                              const double* __restrict__ times, int32_t* status, int lg) {
-  const int lanes = 1 << lg, l = threadIdx.x & (lanes - 1);
-  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> lg);
-  float v[U][8];
-  int64_t place[U];
-  int head[U];
+__global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, const T* __restrict__ rows) {
+  const int lanes = 1 << a.lg, l = threadIdx.x & (lanes - 1);
+  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> a.lg);
+  float v[U][2][8];
+  Where w[U];
   double when[U];
 #pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = find<true>(a, g0 + u * (THREADS >> a.lg));
+#pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t g = g0 + u * (THREADS >> lg);
-    place[u] = -1;
     when[u] = 0.0;
-    int64_t from = -1;
-    head[u] = 0;
-    if (g < groups) {
-      const uint32_t i = g / (uint32_t)c.heads;
-      head[u] = (int)(g - i * (uint32_t)c.heads);
-      from = index_at(src, index64, i);
-      place[u] = index_at(dst, index64, i);
-      if (from < 0 || from >= num_rows) { from = -1; atomicMax(status, 4); }
-      if (place[u] < 0 || place[u] >= c.rows) { place[u] = -1; atomicMax(status, 4); }
-    }
-    if (from >= 0) {
-      load8<T, VB>(rows + from * row_stride + (int64_t)head[u] * c.dim, 8 * l, c.dim, v[u]);
-      if (times && head[u] == 0 && l == 0) when[u] = __ldg(times + from);
+    if (w[u].row >= 0) {
+      const T* row = reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(rows) + (uint64_t)(uint32_t)w[u].row * a.row_bytes) + w[u].head * a.c.dim;
+      load8<T, VB>(row, 8 * l, a.c.dim, v[u][0]);
+      load8<T, VB>(row, 8 * (l + lanes), a.c.dim, v[u][1]);
+      if (a.times && w[u].head == 0 && l == 0) when[u] = __ldg(a.times + w[u].row);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[u][j] = 0.f;
+      for (int j = 0; j < 8; ++j) v[u][0][j] = v[u][1][j] = 0.f;
     }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float amax = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) amax = max_nan(amax, fabsf(v[u][j]));
-    for (int o = lanes >> 1; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, o));
+    for (int j = 0; j < 8; ++j) amax = max_nan(amax, max_nan(fabsf(v[u][0][j]), fabsf(v[u][1][j])));
+    amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 1));
+    if (lanes > 2) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 2));
+    if (lanes > 4) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 4));
     const bool bad = !(amax <= 3.4028234e38f);
     float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
     if (amax < 7.8886091e-31f) s = 0.f;                                   // 2^-100
     const float r = s > 0.f ? __frcp_rn(s) : 0.f;
-    uint32_t w[BITS == 4 ? 1 : 2];
     // float bits of 1.5 * 2^23 + offset + code, added up with shifts; the fixed part of the sum is taken off at the end
     constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
-    constexpr int PER = BITS == 4 ? 8 : 4;
+    constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+    uint32_t code[2][WORDS];
 #pragma unroll
-    for (int q = 0; q < 8 / PER; ++q) {
-      uint32_t acc = 0, fixed = 0;
+    for (int p = 0; p < 2; ++p) {
 #pragma unroll
-      for (int j = PER - 1; j >= 0; --j) {
-        acc = (acc << BITS) + __float_as_uint(fmaf(v[u][q * PER + j], r, kMagic));
-        fixed = (fixed << BITS) + 0x4b400000u;
+      for (int q = 0; q < WORDS; ++q) {
+        uint32_t acc = 0, fixed = 0;
+#pragma unroll
+        for (int j = PER - 1; j >= 0; --j) {
+          acc = (acc << BITS) + __float_as_uint(fmaf(v[u][p][q * PER + j], r, kMagic));
+          fixed = (fixed << BITS) + 0x4b400000u;
+        }
+        code[p][q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
       }
-      w[q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
     }
-    if (place[u] >= 0) {
-      uint8_t* to = c.codes + place[u] * c.code_stride + (int64_t)head[u] * c.code_bytes;
-      if (BITS == 4) reinterpret_cast<uint32_t*>(to)[l] = w[0];
-      else reinterpret_cast<uint2*>(to)[l] = make_uint2(w[0], w[BITS == 4 ? 0 : 1]);
+    if (w[u].place >= 0) {
+      const uint64_t place = (uint32_t)w[u].place;
+      uint8_t* to = a.c.codes + place * (uint32_t)a.c.code_stride + w[u].head * a.c.code_bytes;
+      if constexpr (BITS == 4) {
+        reinterpret_cast<uint32_t*>(to)[l] = code[0][0];
+        reinterpret_cast<uint32_t*>(to)[l + lanes] = code[1][0];
+      } else {
+        reinterpret_cast<uint2*>(to)[l] = make_uint2(code[0][0], code[0][1]);
+        reinterpret_cast<uint2*>(to)[l + lanes] = make_uint2(code[1][0], code[1][1]);
+      }
       if (l == 0) {
         const uint16_t bits = bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
-        *reinterpret_cast<uint16_t*>(c.scales + place[u] * c.scale_stride + 2 * head[u]) = bits;
-        if (times && c.times && head[u] == 0) *reinterpret_cast<double*>(c.times + place[u] * c.time_stride) = when[u];
+        *reinterpret_cast<uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride + 2 * w[u].head) = bits;
+        if (a.times && w[u].head == 0) *reinterpret_cast<double*>(a.c.times + place * (uint32_t)a.c.time_stride) = when[u];
       }
     }
   }
 }
 
 template <typename T, int VB, int BITS>
-__global__ void __launch_bounds__(THREADS) cache_read_kernel(const CacheView c, T* __restrict__ rows, int64_t num_rows,
-                                                             int64_t row_stride, const void* __restrict__ src,
-                                                             const void* __restrict__ dst, int index64, uint32_t groups,
-                                                             double* __restrict__ times, int32_t* status, int lg) {
-  const int lanes = 1 << lg, l = threadIdx.x & (lanes - 1);
-  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> lg);
-  uint32_t w[U][2];
-  uint16_t sb[U];
+__global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __restrict__ rows) {
+  const int lanes = 1 << a.lg, l = threadIdx.x & (lanes - 1);
+  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> a.lg);
+  constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+  Where w[U];
+  uint32_t code[U][2][WORDS];
+  uint32_t sb[U];
   double when[U];
-  int64_t to[U];
-  int head[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) w[u] = find<false>(a, g0 + u * (THREADS >> a.lg));
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t g = g0 + u * (THREADS >> lg);
-    to[u] = -1;
-    head[u] = 0;
     sb[u] = 0;
     when[u] = 0.0;
-    w[u][0] = w[u][1] = 0;
-    if (g < groups) {
-      const uint32_t i = g / (uint32_t)c.heads;
-      head[u] = (int)(g - i * (uint32_t)c.heads);
-      const int64_t place = index_at(src, index64, i);
-      to[u] = index_at(dst, index64, i);
-      if (to[u] < 0 || to[u] >= num_rows) { to[u] = -1; atomicMax(status, 4); }
-      if (place < 0 || place >= c.rows) {
-        atomicMax(status, 4);                                             // reads as zeros
+#pragma unroll
+    for (int q = 0; q < WORDS; ++q) code[u][0][q] = code[u][1][q] = 0;     // an index outside reads as zeros: scale 0
+    if (w[u].place >= 0) {
+      const uint64_t place = (uint32_t)w[u].place;
+      const uint8_t* from = a.c.codes + place * (uint32_t)a.c.code_stride + w[u].head * a.c.code_bytes;
+      if constexpr (BITS == 4) {
+        code[u][0][0] = __ldg(reinterpret_cast<const uint32_t*>(from) + l);
+        code[u][1][0] = __ldg(reinterpret_cast<const uint32_t*>(from) + l + lanes);
       } else {
-        const uint8_t* from = c.codes + place * c.code_stride + (int64_t)head[u] * c.code_bytes;
-        if (BITS == 4) {
-          w[u][0] = __ldg(reinterpret_cast<const uint32_t*>(from) + l);
-        } else {
-          const uint2 p = __ldg(reinterpret_cast<const uint2*>(from) + l);
-          w[u][0] = p.x;
-          w[u][1] = p.y;
-        }
-        sb[u] = __ldg(reinterpret_cast<const uint16_t*>(c.scales + place * c.scale_stride + 2 * head[u]));
-        if (times && c.times && head[u] == 0 && l == 0) when[u] = __ldg(reinterpret_cast<const double*>(c.times + place * c.time_stride));
+        const uint2 p = __ldg(reinterpret_cast<const uint2*>(from) + l), q = __ldg(reinterpret_cast<const uint2*>(from) + l + lanes);
+        code[u][0][0] = p.x;
+        code[u][0][1] = p.y;
+        code[u][1][0] = q.x;
+        code[u][1][1] = q.y;
       }
+      sb[u] = __ldg(reinterpret_cast<const uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride + 2 * w[u].head));
+      if (a.times && w[u].head == 0 && l == 0) when[u] = __ldg(reinterpret_cast<const double*>(a.c.times + place * (uint32_t)a.c.time_stride));
     }
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    if (to[u] >= 0) {
-      const float s = __uint_as_float((uint32_t)sb[u] << 16);
-      float v[8];
-      // a code under fp32's exponent for 2^23 reads as 2^23 + offset + code
+    if (w[u].row >= 0) {
+      const float s = __uint_as_float(sb[u] << 16);
+      T* row = reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(rows) + (uint64_t)(uint32_t)w[u].row * a.row_bytes) + w[u].head * a.c.dim;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t code = BITS == 4 ? (w[u][0] >> (4 * j)) & 0xfu : (w[u][j >> 2] >> (8 * (j & 3))) & 0xffu;
-        v[j] = (__uint_as_float(0x4b000000u | code) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
+      for (int p = 0; p < 2; ++p) {
+        float v[8];
+        // a code under fp32's exponent for 2^23 reads as 2^23 + offset + code
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t x = (code[u][p][j / PER] >> (BITS * (j % PER))) & (BITS == 4 ? 0xfu : 0xffu);
+          v[j] = (__uint_as_float(0x4b000000u | x) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
+        }
+        store8<T, VB>(row, 8 * (l + p * lanes), a.c.dim, v);
       }
-      store8<T, VB>(rows + to[u] * row_stride + (int64_t)head[u] * c.dim, 8 * l, c.dim, v);
-      if (times && c.times && head[u] == 0 && l == 0) times[to[u]] = when[u];
+      if (a.times && w[u].head == 0 && l == 0) a.times[w[u].row] = when[u];
     }
   }
 }
 
-struct Args {
-  CacheView c;
-  void* rows;
-  int64_t num_rows, row_stride;
-  const void *src, *dst;
-  int index64;
-  uint32_t groups;
-  double* times;
-  int32_t* status;
-  int lg;
-  cudaStream_t s;
-};
-
 template <bool WRITE, typename T, int VB, int BITS>
-void launch(const Args& a) {
+void launch(const Move& a, void* rows, cudaStream_t s) {
   const uint64_t threads = (uint64_t)a.groups << a.lg;
   const unsigned grid = (unsigned)((threads + THREADS * U - 1) / (THREADS * U));
-  if (WRITE)
-    cache_write_kernel<T, VB, BITS><<<grid, THREADS, 0, a.s>>>(a.c, (const T*)a.rows, a.num_rows, a.row_stride, a.src, a.dst,
-                                                               a.index64, a.groups, a.times, a.status, a.lg);
-  else
-    cache_read_kernel<T, VB, BITS><<<grid, THREADS, 0, a.s>>>(a.c, (T*)a.rows, a.num_rows, a.row_stride, a.src, a.dst, a.index64,
-                                                              a.groups, a.times, a.status, a.lg);
+  if (WRITE) cache_write_kernel<T, VB, BITS><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
+  else cache_read_kernel<T, VB, BITS><<<grid, THREADS, 0, s>>>(a, (T*)rows);
 }
 
 // Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8 (heads of 50 in fp32), 4 (heads of 50
 // in 16 bits) or single values.
 template <bool WRITE, typename T, int BITS>
-void launch_aligned(const Args& a) {
-  const uint64_t at = (uint64_t)(uintptr_t)a.rows | (uint64_t)(a.row_stride * (int64_t)sizeof(T)) | (uint64_t)(a.c.dim * (int)sizeof(T));
-  if ((at & 15) == 0) launch<WRITE, T, 16, BITS>(a);
-  else if (sizeof(T) == 4 && (at & 7) == 0) launch<WRITE, T, 8, BITS>(a);
-  else if ((at & 3) == 0) launch<WRITE, T, 4, BITS>(a);
-  else launch<WRITE, T, sizeof(T), BITS>(a);
+void launch_aligned(const Move& a, void* rows, cudaStream_t s) {
+  const uint64_t at = (uint64_t)(uintptr_t)rows | (uint64_t)a.row_bytes | (uint64_t)(a.c.dim * (int)sizeof(T));
+  if ((at & 15) == 0) launch<WRITE, T, 16, BITS>(a, rows, s);
+  else if (sizeof(T) == 4 && (at & 7) == 0) launch<WRITE, T, 8, BITS>(a, rows, s);
+  else if ((at & 3) == 0) launch<WRITE, T, 4, BITS>(a, rows, s);
+  else launch<WRITE, T, sizeof(T), BITS>(a, rows, s);
 }
 
 template <bool WRITE>
 int run(const char* who, const tgnn_cache* cache, void* rows, int dtype, int64_t num_rows, int64_t row_stride, const void* src,
         const void* dst, int index_bits, int64_t n, double* times, int32_t* status, void* stream, char* err, int64_t size) {
-  Args a;
+  Move a = {};
   const int rc = check_cache(who, "cache", cache, &a.c, err, size);
   if (rc) return rc;
   if (!known_dtype(dtype)) return fail(err, size, TGNN_EINVAL, "%s: unknown row type %d", who, dtype);
@@ -239,6 +254,8 @@ int run(const char* who, const tgnn_cache* cache, void* rows, int dtype, int64_t
   if (num_rows < 0 || n < 0 || row_stride < (int64_t)a.c.heads * a.c.dim)
     return fail(err, size, TGNN_EINVAL, "%s: size out of range (a row holds heads * dim values)", who);
   if (n > 0x7fffffff / a.c.heads) return fail(err, size, TGNN_ECAPACITY, "%s: n * heads beyond int32", who);
+  if (num_rows > 0xffffffffll || a.c.rows > 0xffffffffll || row_stride > 0x7fffffff / elem_bytes(dtype))
+    return fail(err, size, TGNN_ECAPACITY, "%s: 2^32 rows and more, or a row stride of 2^31 bytes and more", who);
   if (!status || (n > 0 && num_rows > 0 && !rows)) return fail(err, size, TGNN_EINVAL, "%s: null pointer", who);
   if (times && n > 0 && !a.c.times) return fail(err, size, TGNN_EINVAL, "%s: times given, but the cache holds none", who);
   const int idx = index_bits == 64 ? 7 : 3;
@@ -246,22 +263,26 @@ int run(const char* who, const tgnn_cache* cache, void* rows, int dtype, int64_t
       ((uintptr_t)status & 3))
     return fail(err, size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", who);
   if (n == 0) return TGNN_OK;
-  a.rows = rows;
   a.num_rows = num_rows;
-  a.row_stride = row_stride;
+  a.row_bytes = (uint32_t)(row_stride * elem_bytes(dtype));
   a.src = src;
   a.dst = dst;
   a.index64 = index_bits == 64;
   a.groups = (uint32_t)(n * a.c.heads);
+  // division by heads > 1: with 2^b >= heads > 2^(b - 1), magic = ceil(2^(31 + b) / heads) is exact below 2^31
+  int b = 1;
+  while ((1 << b) < a.c.heads) ++b;
+  a.heads_magic = a.c.heads == 1 ? 0 : (uint32_t)(((1ull << (31 + b)) + a.c.heads - 1) / a.c.heads);
+  a.heads_shift = b - 1;
   a.times = times;
   a.status = status;
-  a.s = (cudaStream_t)stream;
   const int pad = padded_dim(a.c.dim);
-  a.lg = pad == 32 ? 2 : pad == 64 ? 3 : 4;
+  a.lg = pad == 32 ? 1 : pad == 64 ? 2 : 3;
   const bool four = a.c.bits == 4;
-  if (dtype == TGNN_F32) four ? launch_aligned<WRITE, float, 4>(a) : launch_aligned<WRITE, float, 8>(a);
-  else if (dtype == TGNN_BF16) four ? launch_aligned<WRITE, __nv_bfloat16, 4>(a) : launch_aligned<WRITE, __nv_bfloat16, 8>(a);
-  else four ? launch_aligned<WRITE, __half, 4>(a) : launch_aligned<WRITE, __half, 8>(a);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (dtype == TGNN_F32) four ? launch_aligned<WRITE, float, 4>(a, rows, s) : launch_aligned<WRITE, float, 8>(a, rows, s);
+  else if (dtype == TGNN_BF16) four ? launch_aligned<WRITE, __nv_bfloat16, 4>(a, rows, s) : launch_aligned<WRITE, __nv_bfloat16, 8>(a, rows, s);
+  else four ? launch_aligned<WRITE, __half, 4>(a, rows, s) : launch_aligned<WRITE, __half, 8>(a, rows, s);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail(err, size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(e));
   return TGNN_OK;

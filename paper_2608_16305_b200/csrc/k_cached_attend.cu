@@ -58,6 +58,8 @@ struct AttendArgs {
   bool pairs;                                 // q and out may be read and written two values at a time
 };
 
+__device__ const float no_bias = 0.f;         // read where there is no bias (buckets = 0: by every head)
+
 __device__ __forceinline__ uint32_t h2u(__half2 x) { return *reinterpret_cast<uint32_t*>(&x); }
 __device__ __forceinline__ __half2 u2h(uint32_t x) { return *reinterpret_cast<__half2*>(&x); }
 
@@ -322,11 +324,10 @@ struct Walk {
       const uint32_t two = __shfl_sync(FULL, scales, key);
       const float ks = __uint_as_float(two << 16);
       vs[j] = __uint_as_float(two & 0xffff0000u);
-      const int at = bias ? __shfl_sync(FULL, bucket, key) : 0;
+      const int at = __shfl_sync(FULL, bucket, key);
 #pragma unroll
       for (int x = 0; x < NH; ++x) {
-        float z = s[x][j] * (qfac[x] * ks);
-        if (bias) z += __ldg(bias + min(4 * x + c, nh - 1) * a.buckets + at);
+        const float z = fmaf(s[x][j], qfac[x] * ks, __ldg(bias + min(4 * x + c, nh - 1) * a.buckets + at));
         s[x][j] = u0 + key < seen.n ? z : -INFINITY;
         top[x] = fmaxf(top[x], s[x][j]);
       }
@@ -356,7 +357,7 @@ struct Walk {
       const bool grow = need > sc[x];
       const float old = sc[x];
       sc[x] = grow ? need : old;
-      const float inv = __frcp_rn(sc[x]);
+      const float inv = rcp_fast(sc[x]);
       if (__any_sync(FULL, grow)) {
         const float f = grow ? old * inv : 1.f;
 #pragma unroll
@@ -476,17 +477,17 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   const uint32_t to = (uint32_t)__cvta_generic_to_shared(my) + 16 * lane;
   for (int left = BY_BLOCK ? 1 : a.take; left > 0; --left) {
     const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
-    const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : nullptr;
+    const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : &no_bias;
     if (worker < tiles) {
       // two tiles on their way: the query is prepared, and each tile worked on, while the next comes
       Rows<BITS, DP> next;
       next.load(a, seen, worker, to);
       asm volatile("cp.async.commit_group;" ::: "memory");
       w.begin(a, root, head0, nh);
-      int buf = 0, bucket = 0;
+      int buf = 0, bucket = 0;                                      // (without a bias: bucket 0 of none)
       for (int tile = worker; tile < tiles; tile += workers) {
         const uint32_t scales = next.scales;
-        if (bias) bucket = bucket_near(s_bounds, a.buckets - 1, seen.t - next.ts, bucket);
+        if (a.bias) bucket = bucket_near(s_bounds, a.buckets - 1, seen.t - next.ts, bucket);
         if (tile + workers < tiles) next.load(a, seen, tile + workers, to + (buf ^ STAGE));
         asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 1;" ::: "memory");
         __syncwarp();
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
 #pragma unroll
       for (int x = 0; x < NH; ++x) {
         const int h = 4 * x + c;
-        const float f = w.l[x] == 0.f ? 0.f : w.sc[x] / w.l[x];      // nothing seen, or nothing but -infinity: zeros
+        const float f = w.l[x] == 0.f ? 0.f : w.sc[x] * rcp_fast(w.l[x]);      // nothing seen, or nothing but -infinity: zeros
         const int64_t base = (root * a.heads + head0 + h) * a.dim;
         if (h < nh) {
 #pragma unroll
@@ -689,7 +690,7 @@ extern "C" int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_
   a.bounds = bounds;
   a.times = times;
   a.ts = ts;
-  a.buckets = num_buckets;
+  a.buckets = bias ? num_buckets : 0;
   a.window = window;
   a.sinks = sinks;
   a.scale = scale;

@@ -81,6 +81,13 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+// 1 / x, relative error 2^-23, for normal x (and NaN).
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // Bucket of a time difference: how many of the n ascending bounds are <= dt.  The comparisons are in fp64, so a difference
 // on a bound lands where the definition says; NaN is above no bound.
 // In shared memory the bounds lie behind a -infinity and before +infinities: s[i] is bound i - 1, s[kMaxBuckets] the last.

@@ -42,7 +42,7 @@ def test_cache_descriptions(lib, bad):
 
 @pytest.mark.parametrize("bad", [dict(rows=None), dict(dtype=3), dict(dtype=-1), dict(num=-1), dict(stride=99), dict(src=PTR + 4),
                                  dict(dst=PTR + 4), dict(bits=16), dict(n=-1), dict(n=1 << 30), dict(times=PTR + 4), dict(status=None),
-                                 dict(rows=PTR + 2), dict(status=PTR + 2)], ids=str)
+                                 dict(rows=PTR + 2), dict(status=PTR + 2), dict(num=1 << 32), dict(stride=1 << 29)], ids=str)
 def test_cache_moves(lib, bad):
     a = dict(cache=C.byref(_cache()), rows=PTR, dtype=B.TGNN_F32, num=10, stride=100, src=PTR, dst=PTR, bits=64, n=5, times=PTR, status=PTR)
     a.update(bad)
