@@ -27,7 +27,7 @@ using namespace tgnn_history;
 namespace {
 
 constexpr int MAX_BLOCKS = 1024;
-constexpr int MAX_WARPS = 8;
+constexpr int MAX_WARPS = 4;
 
 struct SlotArgs {
   const void *q, *k, *v, *dout;
@@ -87,6 +87,10 @@ struct Seg {
       else return to_float<T>(reinterpret_cast<const T*>(&x)[j & 1]);
     }
   }
+  __device__ __forceinline__ void floats(float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = at(j);
+  }
   static __device__ constexpr bool is_bf16();
   static __device__ __forceinline__ void store(T* p, int part, int dim, const float (&x)[N]) {
 #pragma unroll
@@ -105,12 +109,43 @@ struct IsBf16<__nv_bfloat16> { static constexpr bool value = true; };
 template <typename T, int VB, int P, int NV>
 __device__ constexpr bool Seg<T, VB, P, NV>::is_bf16() { return IsBf16<T>::value; }
 
-template <int P>
-__device__ __forceinline__ float sum_p(float x) {              // over the lanes of a segment
+// Sums of N values each over the P lanes of a segment, several at a time: a lane hands half of its values to its partner and
+// goes on with the other half, so that 8 values take 9 shuffles over 32 lanes instead of 40.  What a lane ends up with is the sum
+// of value Reduced::id (and the next ones, where P < N); lanes whose Reduced::first is not set hold copies.
+template <int P, int N>
+struct Reduced {
+  int id;
+  bool first;
+  __device__ __forceinline__ explicit Reduced(int lane) {
+    id = 0;
+    int n = N;
 #pragma unroll
-  for (int o = 1; o < P; o <<= 1) x += __shfl_xor_sync(FULL, x, o);
-  return x;
-}
+    for (int o = P / 2; o > 0 && n > 1; o >>= 1) {
+      n >>= 1;
+      id += (lane & o) ? n : 0;
+    }
+    first = (lane & (P > N ? P / N - 1 : 0)) == 0;
+  }
+  static __device__ __forceinline__ void run(float (&v)[N], int lane) {
+    int n = N;
+#pragma unroll
+    for (int o = P / 2; o > 0; o >>= 1) {
+      if (n > 1) {
+        n >>= 1;
+        const bool up = (lane & o) != 0;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          if (i < n) {
+            const float give = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
+            v[i] = keep + __shfl_xor_sync(FULL, give, o);
+          }
+        }
+      } else {
+        v[0] += __shfl_xor_sync(FULL, v[0], o);
+      }
+    }
+  }
+};
 
 constexpr int UN = 4;                                          // segments of k and of v in flight per lane
 
@@ -135,7 +170,7 @@ __device__ __forceinline__ void fill_buckets(const SlotArgs& a, const double* s_
 }
 
 template <typename T, int VB, int P, int NV>
-__global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const SlotArgs a) {
+__global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
@@ -159,8 +194,12 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const S
     const int kv = kv0 + me.kc;
     for (int g = 0; g < a.group; ++g) {
       const int h = kv * a.group + g;
-      S q;
-      q.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
+      float q[S::N];
+      {
+        S raw;
+        raw.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
+        raw.floats(q);
+      }
       const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
       float m = -INFINITY, l = 0.f, acc[S::N];
 #pragma unroll
@@ -172,29 +211,43 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const S
           fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
           __syncwarp();
         }
-        for (int s0 = c0; s0 < c1; s0 += UN * me.RPI) {
+        const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
+        const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
+        for (int s0 = c0 + me.row; s0 - me.row < c1; s0 += UN * me.RPI) {
           S k[UN], v[UN];
+#pragma unroll
+          for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < c1);
+#pragma unroll
+          for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < c1);
+          kp += UN * me.RPI * ROW;
+          vp += UN * me.RPI * ROW;
           float z[UN];
 #pragma unroll
           for (int u = 0; u < UN; ++u) {
-            const int s = s0 + u * me.RPI + me.row;
-            k[u].load(kr + (int64_t)s * ROW + kv * D, me.part, D, s < c1);
-          }
+            z[u] = 0.f;
 #pragma unroll
-          for (int u = 0; u < UN; ++u) {
-            const int s = s0 + u * me.RPI + me.row;
-            v[u].load(vr + (int64_t)s * ROW + kv * D, me.part, D, s < c1);
+            for (int j = 0; j < S::N; ++j) z[u] = fmaf(k[u].at(j), q[j], z[u]);
+          }
+          if constexpr (P >= 16) {
+            // the sums of four slots together, then back to all lanes of the segment
+            Reduced<P, UN>::run(z, lane);
+            const float mine = z[0];
+#pragma unroll
+            for (int u = 0; u < UN; ++u) z[u] = __shfl_sync(FULL, mine, (lane & ~(P - 1)) | ((u & 2) ? P / 2 : 0) | ((u & 1) ? P / 4 : 0));
+          } else {
+#pragma unroll
+            for (int u = 0; u < UN; ++u) {
+#pragma unroll
+              for (int o = 1; o < P; o <<= 1) z[u] += __shfl_xor_sync(FULL, z[u], o);
+            }
           }
           float top = m;
 #pragma unroll
           for (int u = 0; u < UN; ++u) {
-            const int s = s0 + u * me.RPI + me.row;
-            float x = 0.f;
-#pragma unroll
-            for (int j = 0; j < S::N; ++j) x = fmaf(k[u].at(j), q.at(j), x);
-            x = sum_p<P>(x) * a.scale;
-            if (bias && s < c1) x += __ldg(bias + bucket[s - c0]);
-            z[u] = s < c1 ? x : -INFINITY;
+            const int s = s0 + u * me.RPI;
+            z[u] *= a.scale;
+            if (bias && s < c1) z[u] += __ldg(bias + bucket[s - c0]);
+            if (s >= c1) z[u] = -INFINITY;
             top = fmaxf(top, z[u]);
           }
           const float base = top == -INFINITY ? 0.f : top;     // nothing but -infinity: weights are 0
@@ -231,7 +284,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_forward_kernel(const S
 }
 
 template <typename T, int VB, int P, int NV>
-__global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const SlotArgs a) {
+__global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
@@ -252,6 +305,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
   }
   __syncthreads();
   const Lanes<P> me(lane, a.kv_heads);
+  const Reduced<P, 2 * UN> sums(lane);
+  const int h_first = lane % H, h_step = 32 % H;               // head of entry lane + 32 i of a [slot][head] array, by steps
   for (int64_t r = (int64_t)blockIdx.x * a.warps + wid; r < a.n; r += (int64_t)gridDim.x * a.warps) {
     const int cnt = min(max(a.cnt[r], 0), a.slots);
     const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
@@ -275,38 +330,49 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
           const int kv = kv0 + me.kc;
           for (int g = 0; g < a.group; ++g) {
             const int h = kv * a.group + g;
-            S q, go;
-            q.load(qr + h * D, me.part, D, true);
-            go.load(gr + h * D, me.part, D, true);
+            float q[S::N], go[S::N];
+            {
+              S raw;
+              raw.load(qr + h * D, me.part, D, true);
+              raw.floats(q);
+              raw.load(gr + h * D, me.part, D, true);
+              raw.floats(go);
+            }
             const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
-            for (int s0 = 0; s0 < ns; s0 += UN * me.RPI) {
+            const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
+            const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
+            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
               S k[UN], v[UN];
 #pragma unroll
-              for (int u = 0; u < UN; ++u) {
-                const int s = s0 + u * me.RPI + me.row;
-                k[u].load(kr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
-              }
+              for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
+#pragma unroll
+              for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
+              kp += UN * me.RPI * ROW;
+              vp += UN * me.RPI * ROW;
+              float x[2 * UN];                                 // q . k of the four slots, then do . v
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
-                const int s = s0 + u * me.RPI + me.row;
-                v[u].load(vr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
-              }
-#pragma unroll
-              for (int u = 0; u < UN; ++u) {
-                const int s = s0 + u * me.RPI + me.row;
-                float x = 0.f, y = 0.f;
+                x[u] = x[UN + u] = 0.f;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) {
-                  x = fmaf(k[u].at(j), q.at(j), x);
-                  y = fmaf(v[u].at(j), go.at(j), y);
+                  x[u] = fmaf(k[u].at(j), q[j], x[u]);
+                  x[UN + u] = fmaf(v[u].at(j), go[j], x[UN + u]);
                 }
-                x = sum_p<P>(x);
-                y = sum_p<P>(y);
-                if (me.part == 0 && s < ns) {
-                  x *= a.scale;
-                  if (bias) x += __ldg(bias + bucket[s]);
-                  z[s * H + h] = x;
-                  dp[s * H + h] = y;
+              }
+              Reduced<P, 2 * UN>::run(x, lane);
+              if (sums.first) {
+#pragma unroll
+                for (int i = 0; i < (2 * UN > P ? 2 * UN / P : 1); ++i) {
+                  const int s = s0 + ((sums.id + i) & (UN - 1)) * me.RPI;
+                  if (s < ns) {
+                    if (sums.id + i < UN) {
+                      float y = x[i] * a.scale;
+                      if (bias) y += __ldg(bias + bucket[s]);
+                      z[s * H + h] = y;
+                    } else {
+                      dp[s * H + h] = x[i];
+                    }
+                  }
                 }
               }
             }
@@ -355,8 +421,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
           if (several) continue;
         }
         // weights and dz
-        for (int i = lane; i < ns * H; i += 32) {
-          const int h = i % H;
+        for (int i = lane, h = h_first; i < ns * H; i += 32) {
           float p = z[i];
           if (several) {
             const float m = s_m[h];
@@ -365,6 +430,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
           p *= s_l[h];
           z[i] = p;
           dp[i] = p * (dp[i] - s_d[h]);
+          h += h_step;
+          if (h >= H) h -= H;
         }
         __syncwarp();
         if (table) {
@@ -392,20 +459,20 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
             float acc[S::N];
 #pragma unroll
             for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
-            for (int s0 = 0; s0 < ns; s0 += UN * me.RPI) {
+            const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
+            const float* wz = dp + me.row * H + h;
+            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
               S k[UN];
 #pragma unroll
-              for (int u = 0; u < UN; ++u) {
-                const int s = s0 + u * me.RPI + me.row;
-                k[u].load(kr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, s < ns);
-              }
+              for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
+              kp += UN * me.RPI * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
-                const int s = s0 + u * me.RPI + me.row;
-                const float w = s < ns ? dp[s * H + h] : 0.f;
+                const float w = s0 + u * me.RPI < ns ? wz[u * me.RPI * H] : 0.f;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) acc[j] = fmaf(w, k[u].at(j), acc[j]);
               }
+              wz += UN * me.RPI * H;
             }
             for (int o = P * me.KC; o < 32; o <<= 1) {
 #pragma unroll
@@ -427,31 +494,69 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 2) slot_backward_kernel(const 
               S::store(dqr + h * D, me.part, D, acc);
             }
           }
-          S q, go;
-          q.load(qr + kv * a.group * D, me.part, D, true);
-          go.load(gr + kv * a.group * D, me.part, D, true);
-          const int end = final_chunk ? a.slots - c0 : ns;     // behind the last slot that counts: zeros
-          for (int s = me.row; s < end; s += me.RPI) {
-            float xk[S::N], xv[S::N];
+          T* dkp = dkr + (int64_t)(c0 + me.row) * ROW + kv * D;
+          T* dvp = dvr + (int64_t)(c0 + me.row) * ROW + kv * D;
+          int s = me.row;
+          if (a.group == 1) {
+            float q[S::N], go[S::N];
+            {
+              S raw;
+              raw.load(qr + kv * D, me.part, D, true);
+              raw.floats(q);
+              raw.load(gr + kv * D, me.part, D, true);
+              raw.floats(go);
+            }
 #pragma unroll
-            for (int j = 0; j < S::N; ++j) xk[j] = xv[j] = 0.f;
-            if (s < ns) {
-              for (int g = 0; g < a.group; ++g) {
-                const int h = kv * a.group + g;
-                if (a.group > 1) {
-                  q.load(qr + h * D, me.part, D, true);
-                  go.load(gr + h * D, me.part, D, true);
-                }
-                const float wz = dp[s * H + h] * a.scale, wp = z[s * H + h];
+            for (int j = 0; j < S::N; ++j) q[j] *= a.scale;
+            const float *wz = dp + s * H + kv, *wp = z + s * H + kv;
+#pragma unroll 2
+            for (; s < ns; s += me.RPI) {
+              float xk[S::N], xv[S::N];
+              const float y = *wz, p = *wp;
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) {
+                xk[j] = y * q[j];
+                xv[j] = p * go[j];
+              }
+              S::store(dkp, me.part, D, xk);
+              S::store(dvp, me.part, D, xv);
+              dkp += me.RPI * ROW;
+              dvp += me.RPI * ROW;
+              wz += me.RPI * H;
+              wp += me.RPI * H;
+            }
+          } else {
+            for (; s < ns; s += me.RPI) {
+              float xk[S::N], xv[S::N];
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) xk[j] = xv[j] = 0.f;
+              for (int h = kv * a.group; h < (kv + 1) * a.group; ++h) {
+                S q, go;
+                q.load(qr + h * D, me.part, D, true);
+                go.load(gr + h * D, me.part, D, true);
+                const float y = dp[s * H + h] * a.scale, p = z[s * H + h];
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) {
-                  xk[j] = fmaf(wz, q.at(j), xk[j]);
-                  xv[j] = fmaf(wp, go.at(j), xv[j]);
+                  xk[j] = fmaf(y, q.at(j), xk[j]);
+                  xv[j] = fmaf(p, go.at(j), xv[j]);
                 }
               }
+              S::store(dkp, me.part, D, xk);
+              S::store(dvp, me.part, D, xv);
+              dkp += me.RPI * ROW;
+              dvp += me.RPI * ROW;
             }
-            S::store(dkr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, xk);
-            S::store(dvr + (int64_t)(c0 + s) * ROW + kv * D, me.part, D, xv);
+          }
+          if (final_chunk) {                                   // behind the last slot that counts: zeros
+            float zero[S::N];
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) zero[j] = 0.f;
+            for (; s < a.slots - c0; s += me.RPI) {
+              S::store(dkp, me.part, D, zero);
+              S::store(dvp, me.part, D, zero);
+              dkp += me.RPI * ROW;
+              dvp += me.RPI * ROW;
+            }
           }
         }
         __syncwarp();                                          // before the next chunk or root overwrites what was read
@@ -528,7 +633,7 @@ bool plan(SlotArgs* a, bool backward) {
   a->chunk = chunk;
   a->warp_bytes = layout(a->heads, a->dim, chunk, chunk < a->slots, backward, table).total;
   int w = MAX_WARPS;
-  while (w > 1 && (w * a->warp_bytes > SMEM_BLOCK / 2 || w * (int64_t)num_sms() > a->n)) w >>= 1;   // two blocks to an SM; few roots: over all SMs
+  while (w > 1 && (w * a->warp_bytes > SMEM_BLOCK / 4 || w * (int64_t)num_sms() > a->n)) w >>= 1;   // four blocks to an SM; few roots: over all SMs
   a->warps = w;
   return w * a->warp_bytes <= SMEM_BLOCK;
 }
