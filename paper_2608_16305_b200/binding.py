@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import threading
 from typing import Dict, Optional
 
 import numpy as np
@@ -294,42 +295,51 @@ def unpack_rows(memory, last_update, nodes, packed, status) -> int:
 _ROW_TYPES = {torch.float32: TGNN_F32, torch.bfloat16: TGNN_BF16, torch.float16: TGNN_F16}
 
 
-def _stateless(fn, device, *args) -> int:
-    """Calls a stateless entry point on the current stream of the tensors' device; raises with its message."""
-    err = C.create_string_buffer(512)
-    here = torch.cuda.current_device()
-    if device.index == here:                      # the usual case, without the device switch
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(here), C.addressof(err), len(err))
+_I32, _I64, _F32, _F64 = torch.int32, torch.int64, torch.float32, torch.float64
+_errors = threading.local()
+
+
+def _stateless(fn, dev: int, *args) -> int:
+    """Calls a stateless entry point on the current stream of device `dev`, its tensors' device; raises with its message."""
+    err = getattr(_errors, "buf", None)
+    if err is None:
+        err = _errors.buf = C.create_string_buffer(512)
+        _errors.addr = C.addressof(err)
+    if torch._C._cuda_getDevice() == dev:         # the usual case, without the device switch
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev), _errors.addr, 512)
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, _stream(), C.addressof(err), len(err))
+        with torch.cuda.device(dev):
+            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev), _errors.addr, 512)
     if rc != TGNN_OK:
         raise TgnnError(rc, err.value.decode())
     return rc
 
 
 def _row_type(t: torch.Tensor, name: str) -> int:
-    if not t.is_cuda or t.dtype not in _ROW_TYPES:
+    dt = _ROW_TYPES.get(t.dtype)
+    if dt is None or t.get_device() < 0:
         raise TypeError(f"{name}: expected a CUDA tensor of float32, bfloat16 or float16, got {t.dtype} on {t.device}")
-    return _ROW_TYPES[t.dtype]
+    return dt
 
 
-def _same(t: torch.Tensor, like: torch.Tensor, shape, name: str):
+def _same(t: torch.Tensor, like: torch.Tensor, dev: int, shape, name: str):
     """Device pointer of a dense tensor of the type and device of `like` and the given shape."""
-    if t.dtype != like.dtype or t.device != like.device or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not like.dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
         raise TypeError(f"{name}: expected a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}, "
                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()
 
 
-def _vec(t: Optional[torch.Tensor], dt: str, device, n, name: str, at_least: bool = False):
-    """Device pointer of a contiguous tensor of n elements (or at least n) on `device`; None -> NULL."""
+def _vec(t: Optional[torch.Tensor], dt: torch.dtype, dev: int, n: int, name: str, at_least: bool = False):
+    """Device pointer of a contiguous tensor of n elements (or at least n) on device `dev`; None -> NULL."""
     if t is None:
         return None
-    p = _dp(t, dt, name)
-    if t.device != device or (t.numel() < n if at_least else t.numel() != n):
-        raise TypeError(f"{name}: expected {'at least ' if at_least else ''}{n} elements on {device}, got {t.numel()} on {t.device}")
-    return p
+    if t.dtype is dt and t.get_device() == dev and t.is_contiguous():
+        m = t.numel()
+        if m == n or (at_least and m > n):
+            return t.data_ptr()
+    raise TypeError(f"{name}: expected a contiguous {dt} tensor of {'at least ' if at_least else ''}{n} elements on CUDA device {dev}, "
+                    f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class RowCache:
@@ -346,13 +356,13 @@ class RowCache:
         dev = torch.device(device)
         if dev.type != "cuda":
             raise TypeError(f"RowCache: expected a CUDA device, got {dev}")
+        self.device = dev = torch.device("cuda", torch.cuda.current_device() if dev.index is None else dev.index)
         if record:
             at_time = heads * gb
             at_scale = at_time + (8 if times else 0)
             self.record_bytes = (at_scale + 2 * heads + 15) // 16 * 16
             self.codes = self.scales = self.times = None
             self.data = torch.zeros((rows, self.record_bytes), dtype=torch.uint8, device=dev)
-            self.device = self.data.device
             p, r = self.data.data_ptr(), self.record_bytes
             self.c = TgnnCache(p, p + at_scale, p + at_time if times else None, rows, r, r, r, heads, dim, bits, 0)
         else:
@@ -360,65 +370,73 @@ class RowCache:
             self.codes = torch.zeros((rows, heads, gb), dtype=torch.uint8, device=dev)
             self.scales = torch.zeros((rows, heads), dtype=torch.bfloat16, device=dev)
             self.times = torch.zeros(rows, dtype=torch.float64, device=dev) if times else None
-            self.device = self.codes.device
             self.c = TgnnCache(self.codes.data_ptr(), self.scales.data_ptr(), self.times.data_ptr() if times else None, rows,
                                heads * gb, 2 * heads, 8, heads, dim, bits, 0)
+        self.ref = C.byref(self.c)
 
 
 def _rows_of(cache: RowCache, rows: torch.Tensor):
     """(type, number of rows, row stride) of [N, heads, dim] or [N, heads * dim] rows, dense within a row."""
     dt = _row_type(rows, "rows")
-    width = cache.heads * cache.dim
-    inner = (cache.heads, cache.dim) if rows.dim() == 3 else (width,)
-    if rows.device != cache.device or tuple(rows.shape[1:]) != inner:
-        raise TypeError(f"rows: expected {cache.heads} x {cache.dim} values on {cache.device}, got {tuple(rows.shape)} on {rows.device}")
+    shape, width = rows.shape, cache.heads * cache.dim
+    if rows.get_device() != cache.device.index or not (len(shape) == 2 and shape[1] == width or
+                                                       len(shape) == 3 and shape[1] == cache.heads and shape[2] == cache.dim):
+        raise TypeError(f"rows: expected {cache.heads} x {cache.dim} values on {cache.device}, got {tuple(shape)} on {rows.device}")
     if rows.is_contiguous():
-        return dt, rows.shape[0], width
-    if rows.shape[0] > 1 and rows.stride(0) < width or not rows[0].is_contiguous():
+        return dt, shape[0], width
+    if shape[0] > 1 and rows.stride(0) < width or not rows[0].is_contiguous():
         raise TypeError(f"rows: a row's values must lie side by side and rows apart, got strides {rows.stride()}")
-    return dt, rows.shape[0], rows.stride(0)
+    return dt, shape[0], rows.stride(0)
+
+
+def _index(t, dev: int, name: str):
+    """(device pointer, elements, bits) of a list of row numbers; None -> NULL."""
+    if t is None:
+        return None, None, None
+    bits = 64 if t.dtype is _I64 else 32 if t.dtype is _I32 else 0
+    if not bits or t.get_device() != dev or not t.is_contiguous():
+        raise TypeError(f"{name}: expected a contiguous int32 or int64 tensor on CUDA device {dev}, got {t.dtype} on {t.device}")
+    return t.data_ptr(), t.numel(), bits
 
 
 def _cache_move(fn, cache: RowCache, rows, status, src, dst, times, n) -> int:
+    dev = cache.device.index
     dt, num, stride = _rows_of(cache, rows)
-    bits = 64
-    for t, name in ((src, "src"), (dst, "dst")):
-        if t is not None:
-            if t.dtype not in (torch.int32, torch.int64) or t.device != cache.device or not t.is_contiguous():
-                raise TypeError(f"{name}: expected a contiguous int32 or int64 tensor on {cache.device}")
-            bits = 32 if t.dtype == torch.int32 else 64
-    if src is not None and dst is not None and (src.dtype != dst.dtype or src.numel() != dst.numel()):
+    ps, ns, bs = _index(src, dev, "src")
+    pd, nd, bd = _index(dst, dev, "dst")
+    if ns is not None and nd is not None and (ns != nd or bs != bd):
         raise TypeError("src and dst: expected the same type and number of indices")
-    return _stateless(fn, cache.device, C.byref(cache.c), rows.data_ptr(), dt, num, stride, None if src is None else src.data_ptr(),
-                      None if dst is None else dst.data_ptr(), bits, n, _vec(times, "f64", cache.device, num, "times"),
-                      _vec(status, "i32", cache.device, 1, "status"))
+    n = ns if ns is not None else nd if nd is not None else n
+    return _stateless(fn, dev, cache.ref, rows.data_ptr(), dt, num, stride, ps, pd, bs or bd or 64, n,
+                      _vec(times, _F64, dev, num, "times"), _vec(status, _I32, dev, 1, "status"))
 
 
 def cache_write(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
     """tgnn_cache_write: cache row dst[i] = quantised rows[src[i]] (None: i), with times[src[i]]; as many rows as there are indices,
     or as there are rows."""
-    n = src.numel() if src is not None else dst.numel() if dst is not None else rows.shape[0]
-    return _cache_move(load_library().tgnn_cache_write, cache, rows, status, src, dst, times, n)
+    return _cache_move(load_library().tgnn_cache_write, cache, rows, status, src, dst, times, rows.shape[0])
 
 
 def cache_read(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
     """tgnn_cache_read: rows[dst[i]] = values of cache row src[i] (None: i), times[dst[i]] = its time; as many rows as there are
     indices, or as the cache holds."""
-    n = src.numel() if src is not None else dst.numel() if dst is not None else cache.rows
-    return _cache_move(load_library().tgnn_cache_read, cache, rows, status, src, dst, times, n)
+    return _cache_move(load_library().tgnn_cache_read, cache, rows, status, src, dst, times, cache.rows)
 
 
 def sample_window(indptr, nbr, eid, ts, nodes, times, window: int, sinks: int, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out,
                   status) -> int:
     """tgnn_sample_window: history (first, len) and slots (window, then sinks) of every root; any output may be None, and nbr, eid
     where their slots are."""
-    dev, n, P, S = ts.device, nodes.numel(), ts.numel(), window + sinks
+    dev, n, P = ts.get_device(), nodes.numel(), ts.numel()
+    S = n * (window + sinks)
+    if dev < 0:
+        raise TypeError(f"ts: expected a CUDA tensor, got {ts.device}")
     return _stateless(
-        load_library().tgnn_sample_window, dev, _vec(indptr, "i64", dev, 1, "indptr", at_least=True), _vec(nbr, "i32", dev, P, "nbr"),
-        _vec(eid, "i32", dev, P, "eid"), _dp(ts, "f64", "ts"), indptr.numel() - 1, P, _vec(nodes, "i32", dev, n, "nodes"),
-        _vec(times, "f64", dev, n, "times"), n, window, sinks, _vec(nbr_out, "i32", dev, n * S, "nbr_out"),
-        _vec(eid_out, "i32", dev, n * S, "eid_out"), _vec(ts_out, "f64", dev, n * S, "ts_out"), _vec(cnt_out, "i32", dev, n, "cnt_out"),
-        _vec(first_out, "i64", dev, n, "first_out"), _vec(len_out, "i32", dev, n, "len_out"), _vec(status, "i32", dev, 1, "status"))
+        load_library().tgnn_sample_window, dev, _vec(indptr, _I64, dev, 1, "indptr", True), _vec(nbr, _I32, dev, P, "nbr"),
+        _vec(eid, _I32, dev, P, "eid"), _vec(ts, _F64, dev, P, "ts"), indptr.numel() - 1, P, _vec(nodes, _I32, dev, n, "nodes"),
+        _vec(times, _F64, dev, n, "times"), n, window, sinks, _vec(nbr_out, _I32, dev, S, "nbr_out"),
+        _vec(eid_out, _I32, dev, S, "eid_out"), _vec(ts_out, _F64, dev, S, "ts_out"), _vec(cnt_out, _I32, dev, n, "cnt_out"),
+        _vec(first_out, _I64, dev, n, "first_out"), _vec(len_out, _I32, dev, n, "len_out"), _vec(status, _I32, dev, 1, "status"))
 
 
 def _bias_args(bias, bounds, times, ts, heads: int, n: int, entries: int, dev):
@@ -430,40 +448,40 @@ def _bias_args(bias, bounds, times, ts, heads: int, n: int, entries: int, dev):
     nb = bias.shape[1]
     if times is None or ts is None or (bounds is None and nb > 1):
         raise TypeError("a bias needs bounds, times and ts")
-    return (_vec(bias, "f32", dev, heads * nb, "bias"), nb, _vec(bounds, "f64", dev, nb - 1, "bounds"),
-            _vec(times, "f64", dev, n, "times"), _vec(ts, "f64", dev, entries, "ts", at_least=True))
+    return (_vec(bias, _F32, dev, heads * nb, "bias"), nb, _vec(bounds, _F64, dev, nb - 1, "bounds"),
+            _vec(times, _F64, dev, n, "times"), _vec(ts, _F64, dev, entries, "ts", True))
 
 
 def cached_attend(q, k: RowCache, v: RowCache, first, length, window: int, sinks: int, out, status, bias=None, bounds=None, times=None,
                   ts=None, max_len: int = 0, scale: Optional[float] = None) -> int:
     """tgnn_cached_attend: q [n, heads, dim] over the window and sinks of the histories (first, length) in the caches.
     scale defaults to 1 / sqrt(dim)."""
-    dt, dev = _row_type(q, "q"), q.device
-    if q.dim() != 3 or q.shape[2] != k.dim or k.device != dev or v.device != dev:
-        raise TypeError(f"q: expected [n, heads, dim = {k.dim}] on the caches' device, got {tuple(q.shape)} on {dev}")
-    n, heads, dim = q.shape
+    dt, dev, shape = _row_type(q, "q"), q.get_device(), q.shape
+    if len(shape) != 3 or shape[2] != k.dim or k.device.index != dev or v.device.index != dev:
+        raise TypeError(f"q: expected [n, heads, dim = {k.dim}] on the caches' device, got {tuple(shape)} on {q.device}")
+    n, heads, dim = shape
     return _stateless(
-        load_library().tgnn_cached_attend, dev, _same(q, q, q.shape, "q"), dt, C.byref(k.c), C.byref(v.c), n, heads,
-        _vec(first, "i64", dev, n, "first"), _vec(length, "i32", dev, n, "length"),
+        load_library().tgnn_cached_attend, dev, _same(q, q, dev, shape, "q"), dt, k.ref, v.ref, n, heads,
+        _vec(first, _I64, dev, n, "first"), _vec(length, _I32, dev, n, "length"),
         *_bias_args(bias, bounds, times, ts, heads, n, k.rows, dev), window, sinks, max_len, dim ** -0.5 if scale is None else scale,
-        _same(out, q, q.shape, "out"), _vec(status, "i32", dev, 1, "status"))
+        _same(out, q, dev, shape, "out"), _vec(status, _I32, dev, 1, "status"))
 
 
 def _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale):
-    dt, dev = _row_type(q, "q"), q.device
-    if q.dim() != 3 or k.dim() != 4 or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[2]:
-        raise TypeError(f"expected q [n, heads, dim] and k [n, slots, kv_heads, dim], got {tuple(q.shape)} and {tuple(k.shape)}")
-    n, heads, dim = q.shape
-    slots, kv = k.shape[1], k.shape[2]
-    return [_same(q, q, q.shape, "q"), _same(k, q, k.shape, "k"), _same(v, q, k.shape, "v"), dt, n, slots, heads, kv, dim,
-            _vec(cnt, "i32", dev, n, "cnt"), *_bias_args(bias, bounds, times, ts, heads, n, n * slots, dev),
-            dim ** -0.5 if scale is None else scale]
+    dt, dev, shape, rows = _row_type(q, "q"), q.get_device(), q.shape, k.shape
+    if len(shape) != 3 or len(rows) != 4 or rows[0] != shape[0] or rows[3] != shape[2]:
+        raise TypeError(f"expected q [n, heads, dim] and k [n, slots, kv_heads, dim], got {tuple(shape)} and {tuple(rows)}")
+    n, heads, dim = shape
+    return dev, shape, rows, (
+        _same(q, q, dev, shape, "q"), _same(k, q, dev, rows, "k"), _same(v, q, dev, rows, "v"), dt, n, rows[1], heads, rows[2], dim,
+        _vec(cnt, _I32, dev, n, "cnt"), *_bias_args(bias, bounds, times, ts, heads, n, n * rows[1], dev),
+        dim ** -0.5 if scale is None else scale)
 
 
 def slot_attend(q, k, v, cnt, out, bias=None, bounds=None, times=None, ts=None, scale: Optional[float] = None) -> int:
     """tgnn_slot_attend: q [n, heads, dim] over the first cnt of k, v [n, slots, kv_heads, dim].  scale defaults to 1 / sqrt(dim)."""
-    a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
-    return _stateless(load_library().tgnn_slot_attend, q.device, *a, _same(out, q, q.shape, "out"))
+    dev, shape, _, a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
+    return _stateless(load_library().tgnn_slot_attend, dev, *a, _same(out, q, dev, shape, "out"))
 
 
 def slot_attend_scratch(n: int, heads: int, num_buckets: int) -> int:
@@ -477,15 +495,14 @@ def slot_attend_scratch(n: int, heads: int, num_buckets: int) -> int:
 def slot_attend_backward(q, k, v, cnt, dout, dq, dk, dv, bias=None, bounds=None, times=None, ts=None, dbias=None, scratch=None,
                          scale: Optional[float] = None) -> int:
     """tgnn_slot_attend_backward: gradients of slot_attend for dout, all overwritten."""
-    a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
-    n, heads, dev = q.shape[0], q.shape[1], q.device
-    nb = a[11]
+    dev, shape, rows, a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
     if (bias is None) != (dbias is None) or (dbias is not None and scratch is None):
         raise TypeError("dbias and scratch belong to a bias")
+    nb = a[11]
     return _stateless(
-        load_library().tgnn_slot_attend_backward, dev, *a, _same(dout, q, q.shape, "dout"), _same(dq, q, q.shape, "dq"),
-        _same(dk, q, k.shape, "dk"), _same(dv, q, k.shape, "dv"), _vec(dbias, "f32", dev, heads * nb, "dbias"),
-        None if dbias is None else _vec(scratch, "f32", dev, slot_attend_scratch(n, heads, nb), "scratch", at_least=True))
+        load_library().tgnn_slot_attend_backward, dev, *a, _same(dout, q, dev, shape, "dout"), _same(dq, q, dev, shape, "dq"),
+        _same(dk, q, dev, rows, "dk"), _same(dv, q, dev, rows, "dv"), _vec(dbias, _F32, dev, shape[1] * nb, "dbias"),
+        None if dbias is None else _vec(scratch, _F32, dev, slot_attend_scratch(shape[0], shape[1], nb), "scratch", True))
 
 
 class Controller:

@@ -307,8 +307,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
   const Lanes<P> me(lane, a.kv_heads);
   const Reduced<P, 2 * UN> sums(lane);
   const int h_first = lane % H, h_step = 32 % H;               // head of entry lane + 32 i of a [slot][head] array, by steps
-  for (int64_t r = (int64_t)blockIdx.x * a.warps + wid; r < a.n; r += (int64_t)gridDim.x * a.warps) {
-    const int cnt = min(max(a.cnt[r], 0), a.slots);
+  const int64_t stride = (int64_t)gridDim.x * a.warps;
+  auto count = [&](int64_t r) { return r < a.n ? min(max(a.cnt[r], 0), a.slots) : 0; };
+  int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  int cnt = count(r), next_cnt = count(r + stride);
+  for (; r < a.n; r += stride, cnt = next_cnt, next_cnt = count(r + stride)) {
     const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
     const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
     T* dkr = reinterpret_cast<T*>(a.dk) + r * a.slots * ROW;
