@@ -5,6 +5,7 @@ library's kernels do everything that touches the model state:
 
     offline   tgnn_backward_scan (N_sync flags)  ->  tgnn_refresh_plan (who sends what, per window)
     boundary  tgnn_pack_rows -> all_to_all_single -> tgnn_unpack_rows         (only when S_r = 1)
+              or, in 8 or 4 bits, tgnn_cache_write -> all_to_all_single -> tgnn_cache_read
     step      step with the gradient left in the context's buffer -> all_reduce -> tgnn_apply_gradient
 
 Received rows land in this GPU's own memory before any kernel reads them.  The row movers are
@@ -101,6 +102,43 @@ class BoundaryRefresh:
         self.rows_sent += self.pack(q, memory, last_update)
         self.exchange(q)
         self.rows_received += self.unpack(q, memory, last_update)
+
+
+class QuantisedRefresh(BoundaryRefresh):
+    """The same refresh with the rows in 8 or 4 bits on the wire: a record holds a row's codes, its scales (one per group of at most
+    128 values) and its last-update time, which stays exact.  For d = 100 a record takes 144 (8 bits) or 80 (4 bits) bytes instead of
+    408.  A received row is within half a step, amax / 127 or amax / 7 of its group, of the owner's."""
+
+    def __init__(self, plan: RefreshPlan, d: int, bits: int = 8, group=None, cache: Callable = B.RowCache, write: Callable = B.cache_write,
+                 read: Callable = B.cache_read):
+        self.plan, self.d, self.group, self.bits = plan, d, group, bits
+        self._write, self._read = write, read
+        heads = next(h for h in range(1, d + 1) if d % h == 0 and d // h <= 128)
+        dev = plan.recv_nodes.device
+        self.send = cache(plan.cap, heads, d // heads, bits, device=dev, record=True)
+        self.recv = cache(plan.cap, heads, d // heads, bits, device=dev, record=True)
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self.rows_sent = self.rows_received = 0
+
+    def pack(self, q: int, memory: torch.Tensor, last_update: torch.Tensor) -> int:
+        ns = int(self.plan.send_off[q, -1])
+        if ns:
+            self._write(self.send, memory, self.status, src=self.plan.send_nodes[q, :ns], times=last_update)
+        return ns
+
+    def exchange(self, q: int) -> None:
+        pl = self.plan
+        sc, rc = pl.send_counts(q), pl.recv_counts(q)
+        if pl.P == 1 and sum(sc) == 0 and sum(rc) == 0:
+            return
+        dist.all_to_all_single(self.recv.data[:sum(rc)], self.send.data[:sum(sc)], output_split_sizes=rc, input_split_sizes=sc,
+                               group=self.group)
+
+    def unpack(self, q: int, memory: torch.Tensor, last_update: torch.Tensor) -> int:
+        nr = int(self.plan.recv_off[q, -1])
+        if nr:
+            self._read(self.recv, memory, self.status, dst=self.plan.recv_nodes[q, :nr], times=last_update)
+        return nr
 
 
 def broadcast_decision(sync: int, device, group=None, coordinator: int = 0) -> int:
