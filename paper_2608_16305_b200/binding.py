@@ -1,12 +1,11 @@
 """Thin ctypes binding of libtgnn_b200.so: same names as the C ABI, argument
-marshalling only.  torch is used for device memory and streams; every step of
+marshalling only (the history operators' in C, csrc/marshal.c).  torch is used for device memory and streams; every step of
 the path runs in the library's CUDA kernels.  There is no CPU fallback: loading
 fails loudly when the shared library is missing."""
 from __future__ import annotations
 
 import ctypes as C
 import os
-import threading
 from typing import Dict, Optional
 
 import numpy as np
@@ -64,11 +63,12 @@ class TgnnError(RuntimeError):
 
 
 _lib = None
+_marshal = None
 
 
 def load_library():
-    """Loads the CUDA library; raises if it has not been built."""
-    global _lib
+    """Loads the CUDA library and the marshalling module; raises if they have not been built."""
+    global _lib, _marshal
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_16305_b200.build` "
@@ -140,7 +140,15 @@ def load_library():
         lib.tgnn_slot_attend_scratch.argtypes = [i64, i32, i32]
         lib.tgnn_slot_attend_scratch.restype = i64
         lib.tgnn_slot_attend_backward.argtypes = slot + [vp] * 8 + [i64]
-        _lib = lib
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise RuntimeError(f"the marshalling module is missing or of another interpreter ({e}): build it with `python -m paper_2608_16305_b200.build`")
+        m.init((torch.int32, torch.int64, torch.float32, torch.float64, torch.bfloat16, torch.float16), torch._C._cuda_getDevice,
+               torch._C._cuda_getCurrentRawStream,
+               tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_sample_window, lib.tgnn_cache_write, lib.tgnn_cache_read, lib.tgnn_cached_attend,
+                                                           lib.tgnn_slot_attend, lib.tgnn_slot_attend_scratch, lib.tgnn_slot_attend_backward)))
+        _lib, _marshal = lib, m
     return _lib
 
 
@@ -292,54 +300,19 @@ def unpack_rows(memory, last_update, nodes, packed, status) -> int:
 
 
 # ---- histories: sampling with sinks, row cache, attention over it, slot attention ----
-_ROW_TYPES = {torch.float32: TGNN_F32, torch.bfloat16: TGNN_BF16, torch.float16: TGNN_F16}
-
-
-_I32, _I64, _F32, _F64 = torch.int32, torch.int64, torch.float32, torch.float64
-_errors = threading.local()
-
-
-def _stateless(fn, dev: int, *args) -> int:
-    """Calls a stateless entry point on the current stream of device `dev`, its tensors' device; raises with its message."""
-    err = getattr(_errors, "buf", None)
-    if err is None:
-        err = _errors.buf = C.create_string_buffer(512)
-        _errors.addr = C.addressof(err)
-    if torch._C._cuda_getDevice() == dev:         # the usual case, without the device switch
-        rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev), _errors.addr, 512)
-    else:
-        with torch.cuda.device(dev):
-            rc = fn(*args, torch._C._cuda_getCurrentRawStream(dev), _errors.addr, 512)
-    if rc != TGNN_OK:
-        raise TgnnError(rc, err.value.decode())
-    return rc
-
-
-def _row_type(t: torch.Tensor, name: str) -> int:
-    dt = _ROW_TYPES.get(t.dtype)
-    if dt is None or t.get_device() < 0:
-        raise TypeError(f"{name}: expected a CUDA tensor of float32, bfloat16 or float16, got {t.dtype} on {t.device}")
-    return dt
-
-
-def _same(t: torch.Tensor, like: torch.Tensor, dev: int, shape, name: str):
-    """Device pointer of a dense tensor of the type and device of `like` and the given shape."""
-    if t.dtype is not like.dtype or t.get_device() != dev or t.shape != shape or not t.is_contiguous():
-        raise TypeError(f"{name}: expected a contiguous {like.dtype} tensor of shape {tuple(shape)} on {like.device}, "
-                        f"got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _vec(t: Optional[torch.Tensor], dt: torch.dtype, dev: int, n: int, name: str, at_least: bool = False):
-    """Device pointer of a contiguous tensor of n elements (or at least n) on device `dev`; None -> NULL."""
-    if t is None:
-        return None
-    if t.dtype is dt and t.get_device() == dev and t.is_contiguous():
-        m = t.numel()
-        if m == n or (at_least and m > n):
-            return t.data_ptr()
-    raise TypeError(f"{name}: expected a contiguous {dt} tensor of {'at least ' if at_least else ''}{n} elements on CUDA device {dev}, "
-                    f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+# Tensors are checked in csrc/marshal.c: type, device, contiguity and number of elements, TypeError otherwise.
+def _call(name: str, *args) -> int:
+    """Calls an entry point through the marshalling module, on the current stream of its tensors' device; raises with the library's
+    message."""
+    if _marshal is None:
+        load_library()
+    r = getattr(_marshal, name)(*args)
+    if type(r) is int:                            # the tensors' device is not the current one
+        with torch.cuda.device(r):
+            r = getattr(_marshal, name)(*args)
+    if r is not None:
+        raise TgnnError(*r)
+    return TGNN_OK
 
 
 class RowCache:
@@ -372,116 +345,43 @@ class RowCache:
             self.times = torch.zeros(rows, dtype=torch.float64, device=dev) if times else None
             self.c = TgnnCache(self.codes.data_ptr(), self.scales.data_ptr(), self.times.data_ptr() if times else None, rows,
                                heads * gb, 2 * heads, 8, heads, dim, bits, 0)
-        self.ref = C.byref(self.c)
-
-
-def _rows_of(cache: RowCache, rows: torch.Tensor):
-    """(type, number of rows, row stride) of [N, heads, dim] or [N, heads * dim] rows, dense within a row."""
-    dt = _row_type(rows, "rows")
-    shape, width = rows.shape, cache.heads * cache.dim
-    if rows.get_device() != cache.device.index or not (len(shape) == 2 and shape[1] == width or
-                                                       len(shape) == 3 and shape[1] == cache.heads and shape[2] == cache.dim):
-        raise TypeError(f"rows: expected {cache.heads} x {cache.dim} values on {cache.device}, got {tuple(shape)} on {rows.device}")
-    if rows.is_contiguous():
-        return dt, shape[0], width
-    if shape[0] > 1 and rows.stride(0) < width or not rows[0].is_contiguous():
-        raise TypeError(f"rows: a row's values must lie side by side and rows apart, got strides {rows.stride()}")
-    return dt, shape[0], rows.stride(0)
-
-
-def _index(t, dev: int, name: str):
-    """(device pointer, elements, bits) of a list of row numbers; None -> NULL."""
-    if t is None:
-        return None, None, None
-    bits = 64 if t.dtype is _I64 else 32 if t.dtype is _I32 else 0
-    if not bits or t.get_device() != dev or not t.is_contiguous():
-        raise TypeError(f"{name}: expected a contiguous int32 or int64 tensor on CUDA device {dev}, got {t.dtype} on {t.device}")
-    return t.data_ptr(), t.numel(), bits
-
-
-def _cache_move(fn, cache: RowCache, rows, status, src, dst, times, n) -> int:
-    dev = cache.device.index
-    dt, num, stride = _rows_of(cache, rows)
-    ps, ns, bs = _index(src, dev, "src")
-    pd, nd, bd = _index(dst, dev, "dst")
-    if ns is not None and nd is not None and (ns != nd or bs != bd):
-        raise TypeError("src and dst: expected the same type and number of indices")
-    n = ns if ns is not None else nd if nd is not None else n
-    return _stateless(fn, dev, cache.ref, rows.data_ptr(), dt, num, stride, ps, pd, bs or bd or 64, n,
-                      _vec(times, _F64, dev, num, "times"), _vec(status, _I32, dev, 1, "status"))
+        self.addr = C.addressof(self.c)
 
 
 def cache_write(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
     """tgnn_cache_write: cache row dst[i] = quantised rows[src[i]] (None: i), with times[src[i]]; as many rows as there are indices,
-    or as there are rows."""
-    return _cache_move(load_library().tgnn_cache_write, cache, rows, status, src, dst, times, rows.shape[0])
+    or as there are rows.  rows: [N, heads, dim] or [N, heads * dim], dense within a row; indices int32 or int64."""
+    return _call("cache_move", True, cache.addr, cache.device.index, cache.rows, cache.heads, cache.dim, rows, status, src, dst, times)
 
 
 def cache_read(cache: RowCache, rows, status, src=None, dst=None, times=None) -> int:
     """tgnn_cache_read: rows[dst[i]] = values of cache row src[i] (None: i), times[dst[i]] = its time; as many rows as there are
     indices, or as the cache holds."""
-    return _cache_move(load_library().tgnn_cache_read, cache, rows, status, src, dst, times, cache.rows)
+    return _call("cache_move", False, cache.addr, cache.device.index, cache.rows, cache.heads, cache.dim, rows, status, src, dst, times)
 
 
 def sample_window(indptr, nbr, eid, ts, nodes, times, window: int, sinks: int, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out,
                   status) -> int:
     """tgnn_sample_window: history (first, len) and slots (window, then sinks) of every root; any output may be None, and nbr, eid
     where their slots are."""
-    dev, n, P = ts.get_device(), nodes.numel(), ts.numel()
-    S = n * (window + sinks)
-    if dev < 0:
-        raise TypeError(f"ts: expected a CUDA tensor, got {ts.device}")
-    return _stateless(
-        load_library().tgnn_sample_window, dev, _vec(indptr, _I64, dev, 1, "indptr", True), _vec(nbr, _I32, dev, P, "nbr"),
-        _vec(eid, _I32, dev, P, "eid"), _vec(ts, _F64, dev, P, "ts"), indptr.numel() - 1, P, _vec(nodes, _I32, dev, n, "nodes"),
-        _vec(times, _F64, dev, n, "times"), n, window, sinks, _vec(nbr_out, _I32, dev, S, "nbr_out"),
-        _vec(eid_out, _I32, dev, S, "eid_out"), _vec(ts_out, _F64, dev, S, "ts_out"), _vec(cnt_out, _I32, dev, n, "cnt_out"),
-        _vec(first_out, _I64, dev, n, "first_out"), _vec(len_out, _I32, dev, n, "len_out"), _vec(status, _I32, dev, 1, "status"))
-
-
-def _bias_args(bias, bounds, times, ts, heads: int, n: int, entries: int, dev):
-    """Pointers of a time bias [heads, buckets] with bounds [buckets - 1], root times [n] and entry times."""
-    if bias is None:
-        return None, 0, None, None, None
-    if bias.dim() != 2 or bias.shape[0] != heads:
-        raise TypeError(f"bias: expected [heads = {heads}, buckets], got {tuple(bias.shape)}")
-    nb = bias.shape[1]
-    if times is None or ts is None or (bounds is None and nb > 1):
-        raise TypeError("a bias needs bounds, times and ts")
-    return (_vec(bias, _F32, dev, heads * nb, "bias"), nb, _vec(bounds, _F64, dev, nb - 1, "bounds"),
-            _vec(times, _F64, dev, n, "times"), _vec(ts, _F64, dev, entries, "ts", True))
+    return _call("sample_window", indptr, nbr, eid, ts, nodes, times, window, sinks, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out,
+                 status)
 
 
 def cached_attend(q, k: RowCache, v: RowCache, first, length, window: int, sinks: int, out, status, bias=None, bounds=None, times=None,
                   ts=None, max_len: int = 0, scale: Optional[float] = None) -> int:
-    """tgnn_cached_attend: q [n, heads, dim] over the window and sinks of the histories (first, length) in the caches.
-    scale defaults to 1 / sqrt(dim)."""
-    dt, dev, shape = _row_type(q, "q"), q.get_device(), q.shape
-    if len(shape) != 3 or shape[2] != k.dim or k.device.index != dev or v.device.index != dev:
-        raise TypeError(f"q: expected [n, heads, dim = {k.dim}] on the caches' device, got {tuple(shape)} on {q.device}")
-    n, heads, dim = shape
-    return _stateless(
-        load_library().tgnn_cached_attend, dev, _same(q, q, dev, shape, "q"), dt, k.ref, v.ref, n, heads,
-        _vec(first, _I64, dev, n, "first"), _vec(length, _I32, dev, n, "length"),
-        *_bias_args(bias, bounds, times, ts, heads, n, k.rows, dev), window, sinks, max_len, dim ** -0.5 if scale is None else scale,
-        _same(out, q, dev, shape, "out"), _vec(status, _I32, dev, 1, "status"))
-
-
-def _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale):
-    dt, dev, shape, rows = _row_type(q, "q"), q.get_device(), q.shape, k.shape
-    if len(shape) != 3 or len(rows) != 4 or rows[0] != shape[0] or rows[3] != shape[2]:
-        raise TypeError(f"expected q [n, heads, dim] and k [n, slots, kv_heads, dim], got {tuple(shape)} and {tuple(rows)}")
-    n, heads, dim = shape
-    return dev, shape, rows, (
-        _same(q, q, dev, shape, "q"), _same(k, q, dev, rows, "k"), _same(v, q, dev, rows, "v"), dt, n, rows[1], heads, rows[2], dim,
-        _vec(cnt, _I32, dev, n, "cnt"), *_bias_args(bias, bounds, times, ts, heads, n, n * rows[1], dev),
-        dim ** -0.5 if scale is None else scale)
+    """tgnn_cached_attend: q [n, heads, dim] over the window and sinks of the histories (first, length) in the caches; bias [heads,
+    buckets] with bounds [buckets - 1], root times [n] and entry times.  scale defaults to 1 / sqrt(dim)."""
+    if k.device != v.device:
+        raise TypeError(f"k and v are on different devices, {k.device} and {v.device}")
+    return _call("cached_attend", k.addr, v.addr, k.device.index, k.rows, k.dim, q, first, length, window, sinks, max_len, scale, out, status,
+                 bias, bounds, times, ts)
 
 
 def slot_attend(q, k, v, cnt, out, bias=None, bounds=None, times=None, ts=None, scale: Optional[float] = None) -> int:
-    """tgnn_slot_attend: q [n, heads, dim] over the first cnt of k, v [n, slots, kv_heads, dim].  scale defaults to 1 / sqrt(dim)."""
-    dev, shape, _, a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
-    return _stateless(load_library().tgnn_slot_attend, dev, *a, _same(out, q, dev, shape, "out"))
+    """tgnn_slot_attend: q [n, heads, dim] over the first cnt of k, v [n, slots, kv_heads, dim]; bias as in cached_attend, ts [n, slots].
+    scale defaults to 1 / sqrt(dim)."""
+    return _call("slot_attend", q, k, v, cnt, scale, bias, bounds, times, ts, out)
 
 
 def slot_attend_scratch(n: int, heads: int, num_buckets: int) -> int:
@@ -495,14 +395,7 @@ def slot_attend_scratch(n: int, heads: int, num_buckets: int) -> int:
 def slot_attend_backward(q, k, v, cnt, dout, dq, dk, dv, bias=None, bounds=None, times=None, ts=None, dbias=None, scratch=None,
                          scale: Optional[float] = None) -> int:
     """tgnn_slot_attend_backward: gradients of slot_attend for dout, all overwritten."""
-    dev, shape, rows, a = _slot_args(q, k, v, cnt, bias, bounds, times, ts, scale)
-    if (bias is None) != (dbias is None) or (dbias is not None and scratch is None):
-        raise TypeError("dbias and scratch belong to a bias")
-    nb = a[11]
-    return _stateless(
-        load_library().tgnn_slot_attend_backward, dev, *a, _same(dout, q, dev, shape, "dout"), _same(dq, q, dev, shape, "dq"),
-        _same(dk, q, dev, rows, "dk"), _same(dv, q, dev, rows, "dv"), _vec(dbias, _F32, dev, shape[1] * nb, "dbias"),
-        None if dbias is None else _vec(scratch, _F32, dev, slot_attend_scratch(shape[0], shape[1], nb), "scratch", True))
+    return _call("slot_attend_backward", q, k, v, cnt, scale, bias, bounds, times, ts, dout, dq, dk, dv, dbias, scratch)
 
 
 class Controller:

@@ -132,3 +132,24 @@ def test_slot_attend_scratch(lib):
     size = lib.tgnn_slot_attend_scratch
     assert size(0, 2, 8) == 0 and size(10, 2, 8) == 320 and size(10 ** 6, 2, 8) == size(1024, 2, 8) and size(5, 2, 0) == 0
     assert [size(*a) for a in ((-1, 2, 8), (1, 0, 8), (1, 257, 8), (1, 2, 129), (1, 2, -1))] == [-1] * 5
+
+
+def test_binding_refuses_what_is_no_tensor(lib):
+    t = torch.zeros(3, dtype=torch.int32)
+    for bad in (None, 5, "x", t, t.double(), [1]):
+        with pytest.raises(TypeError):
+            B.sample_window(bad, None, None, bad, bad, bad, 2, 1, None, None, None, None, None, None, t)
+        with pytest.raises(TypeError):
+            B.slot_attend(bad, bad, bad, bad, bad)
+        with pytest.raises(TypeError):
+            B.slot_attend_backward(bad, bad, bad, bad, bad, bad, bad, bad)
+
+    class Cache:                                   # a cache's description without a device
+        c = _cache()
+        addr, rows, heads, dim, bits, device = C.addressof(c), 10, 2, 50, 4, torch.device("cuda", 0)
+    for bad in (None, 5, t, t.float()):
+        for fn in (B.cache_write, B.cache_read):
+            with pytest.raises(TypeError):
+                fn(Cache, bad, t)
+        with pytest.raises(TypeError):
+            B.cached_attend(bad, Cache, Cache, bad, bad, 2, 1, bad, t)
