@@ -13,8 +13,9 @@
 // Layout: codes [heads][pad * bits / 8 bytes] per row, pad = 32, 64 or 128 values of a head (padding holds code 0), scales bf16 [heads]
 // per row, one fp64 time per row; each with a row stride of its own, so that a row can also be one record of a send buffer.
 //
-// Both kernels are bound by HBM.  A lane takes two pieces of 8 values of a group, half a group apart, so that the neighbouring lanes of
-// a group move whole sectors and the index arithmetic of a row is shared by 16 values; two groups per lane are in flight.
+// Both kernels are bound by HBM.  2 to 8 neighbouring lanes take a row, head after head, two heads at a time where there are two.  A lane
+// takes two pieces of 8 values of a head, half a head apart, so that the lanes of a row move whole sectors; the index arithmetic of
+// a row is done once.
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
@@ -22,7 +23,6 @@ using namespace tgnn_history;
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int U = 2;              // groups per lane, loaded together
 
 struct Move {
   CacheView c;
@@ -30,12 +30,10 @@ struct Move {
   uint32_t row_bytes;             // of a table row to the next
   const void *src, *dst;
   int index64;
-  uint32_t groups;
-  uint32_t heads_magic;           // g / heads = (g * magic) >> 32 >> shift for g < 2^31 and more than one head
-  int heads_shift;
+  uint32_t n;
   double* times;
   int32_t* status;
-  int lg;                         // 2^lg lanes per group: pad / 16
+  int lg;                         // 2^lg lanes per row: pad / 16
 };
 
 __device__ __forceinline__ int64_t index_at(const void* idx, int index64, uint32_t i) {
@@ -43,19 +41,16 @@ __device__ __forceinline__ int64_t index_at(const void* idx, int index64, uint32
   return index64 ? __ldg(reinterpret_cast<const long long*>(idx) + i) : (int64_t)__ldg(reinterpret_cast<const int*>(idx) + i);
 }
 
-// Index i of the group and its head; the table row and the cache row, negative where an index lies outside (recorded).
+// The table row and the cache row of list entry i, negative where an index lies outside (recorded) or the list has ended.
 struct Where {
   int64_t row, place;
-  int head;
 };
 template <bool WRITE>
-__device__ __forceinline__ Where find(const Move& a, uint32_t g) {
-  Where w = {-1, -1, 0};
-  if (g < a.groups) {
-    const uint32_t i = a.c.heads == 1 ? g : __umulhi(g, a.heads_magic) >> a.heads_shift;
-    w.head = (int)(g - i * (uint32_t)a.c.heads);
-    w.row = index_at(WRITE ? a.src : a.dst, a.index64, i);
-    w.place = index_at(WRITE ? a.dst : a.src, a.index64, i);
+__device__ __forceinline__ Where find(const Move& a, uint64_t i) {
+  Where w = {-1, -1};
+  if (i < a.n) {
+    w.row = index_at(WRITE ? a.src : a.dst, a.index64, (uint32_t)i);
+    w.place = index_at(WRITE ? a.dst : a.src, a.index64, (uint32_t)i);
     const bool out_row = (uint64_t)w.row >= (uint64_t)a.num_rows, out_place = (uint64_t)w.place >= (uint64_t)a.c.rows;
     if (out_row | out_place) {
       atomicMax(a.status, 4);
@@ -98,115 +93,112 @@ __device__ __forceinline__ void store8(T* row, int e0, int dim, const float (&v)
   }
 }
 
-template <typename T, int VB, int BITS>
+// U heads of a row at a time: 2, or 1 for rows of one head.
+template <typename T, int VB, int BITS, int U>
 __global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, const T* __restrict__ rows) {
   const int lanes = 1 << a.lg, l = threadIdx.x & (lanes - 1);
-  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> a.lg);
-  float v[U][2][8];
-  Where w[U];
-  double when[U];
+  const Where w = find<true>(a, ((uint64_t)blockIdx.x * THREADS + threadIdx.x) >> a.lg);
+  const T* row = reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(rows) + (uint64_t)(uint32_t)w.row * a.row_bytes);
+  const uint64_t place = (uint32_t)w.place;
+  uint8_t* to = a.c.codes + place * (uint32_t)a.c.code_stride;
+  uint16_t* scales = reinterpret_cast<uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride);
+  if (a.times && l == 0 && w.place >= 0)
+    *reinterpret_cast<double*>(a.c.times + place * (uint32_t)a.c.time_stride) = w.row >= 0 ? __ldg(a.times + w.row) : 0.0;
+  for (int h = 0; h < a.c.heads; h += U) {
+    float v[U][2][8];
 #pragma unroll
-  for (int u = 0; u < U; ++u) w[u] = find<true>(a, g0 + u * (THREADS >> a.lg));
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    when[u] = 0.0;
-    if (w[u].row >= 0) {
-      const T* row = reinterpret_cast<const T*>(reinterpret_cast<const uint8_t*>(rows) + (uint64_t)(uint32_t)w[u].row * a.row_bytes) + w[u].head * a.c.dim;
-      load8<T, VB>(row, 8 * l, a.c.dim, v[u][0]);
-      load8<T, VB>(row, 8 * (l + lanes), a.c.dim, v[u][1]);
-      if (a.times && w[u].head == 0 && l == 0) when[u] = __ldg(a.times + w[u].row);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[u][0][j] = v[u][1][j] = 0.f;
-    }
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float amax = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) amax = max_nan(amax, max_nan(fabsf(v[u][0][j]), fabsf(v[u][1][j])));
-    amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 1));
-    if (lanes > 2) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 2));
-    if (lanes > 4) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 4));
-    const bool bad = !(amax <= 3.4028234e38f);
-    float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
-    if (amax < 7.8886091e-31f) s = 0.f;                                   // 2^-100
-    const float r = s > 0.f ? __frcp_rn(s) : 0.f;
-    // float bits of 1.5 * 2^23 + offset + code, added up with shifts; the fixed part of the sum is taken off at the end
-    constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
-    constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
-    uint32_t code[2][WORDS];
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-#pragma unroll
-      for (int q = 0; q < WORDS; ++q) {
-        uint32_t acc = 0, fixed = 0;
-#pragma unroll
-        for (int j = PER - 1; j >= 0; --j) {
-          acc = (acc << BITS) + __float_as_uint(fmaf(v[u][p][q * PER + j], r, kMagic));
-          fixed = (fixed << BITS) + 0x4b400000u;
-        }
-        code[p][q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
-      }
-    }
-    if (w[u].place >= 0) {
-      const uint64_t place = (uint32_t)w[u].place;
-      uint8_t* to = a.c.codes + place * (uint32_t)a.c.code_stride + w[u].head * a.c.code_bytes;
-      if constexpr (BITS == 4) {
-        reinterpret_cast<uint32_t*>(to)[l] = code[0][0];
-        reinterpret_cast<uint32_t*>(to)[l + lanes] = code[1][0];
+    for (int u = 0; u < U; ++u) {
+      if (w.row >= 0 && h + u < a.c.heads) {
+        load8<T, VB>(row + u * a.c.dim, 8 * l, a.c.dim, v[u][0]);
+        load8<T, VB>(row + u * a.c.dim, 8 * (l + lanes), a.c.dim, v[u][1]);
       } else {
-        reinterpret_cast<uint2*>(to)[l] = make_uint2(code[0][0], code[0][1]);
-        reinterpret_cast<uint2*>(to)[l + lanes] = make_uint2(code[1][0], code[1][1]);
-      }
-      if (l == 0) {
-        const uint16_t bits = bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
-        *reinterpret_cast<uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride + 2 * w[u].head) = bits;
-        if (a.times && w[u].head == 0) *reinterpret_cast<double*>(a.c.times + place * (uint32_t)a.c.time_stride) = when[u];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[u][0][j] = v[u][1][j] = 0.f;
       }
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float amax = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) amax = max_nan(amax, max_nan(fabsf(v[u][0][j]), fabsf(v[u][1][j])));
+      amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 1));
+      if (lanes > 2) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 2));
+      if (lanes > 4) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 4));
+      const bool bad = !(amax <= 3.4028234e38f);
+      float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
+      if (amax < 7.8886091e-31f) s = 0.f;                                 // 2^-100
+      const float r = s > 0.f ? __frcp_rn(s) : 0.f;
+      // float bits of 1.5 * 2^23 + offset + code, added up with shifts; the fixed part of the sum is taken off at the end
+      constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
+      constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+      uint32_t code[2][WORDS];
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+#pragma unroll
+        for (int q = 0; q < WORDS; ++q) {
+          uint32_t acc = 0, fixed = 0;
+#pragma unroll
+          for (int j = PER - 1; j >= 0; --j) {
+            acc = (acc << BITS) + __float_as_uint(fmaf(v[u][p][q * PER + j], r, kMagic));
+            fixed = (fixed << BITS) + 0x4b400000u;
+          }
+          code[p][q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
+        }
+      }
+      if (w.place >= 0 && h + u < a.c.heads) {
+        if constexpr (BITS == 4) {
+          reinterpret_cast<uint32_t*>(to + u * a.c.code_bytes)[l] = code[0][0];
+          reinterpret_cast<uint32_t*>(to + u * a.c.code_bytes)[l + lanes] = code[1][0];
+        } else {
+          reinterpret_cast<uint2*>(to + u * a.c.code_bytes)[l] = make_uint2(code[0][0], code[0][1]);
+          reinterpret_cast<uint2*>(to + u * a.c.code_bytes)[l + lanes] = make_uint2(code[1][0], code[1][1]);
+        }
+        if (l == 0) scales[h + u] = bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
+      }
+    }
+    row += U * a.c.dim;
+    to += U * a.c.code_bytes;
   }
 }
 
-template <typename T, int VB, int BITS>
+template <typename T, int VB, int BITS, int U>
 __global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __restrict__ rows) {
   const int lanes = 1 << a.lg, l = threadIdx.x & (lanes - 1);
-  const uint32_t g0 = (uint32_t)(((uint64_t)blockIdx.x * (THREADS * U) + threadIdx.x) >> a.lg);
   constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
-  Where w[U];
-  uint32_t code[U][2][WORDS];
-  uint32_t sb[U];
-  double when[U];
+  const Where w = find<false>(a, ((uint64_t)blockIdx.x * THREADS + threadIdx.x) >> a.lg);
+  if (w.row < 0) return;
+  T* row = reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(rows) + (uint64_t)(uint32_t)w.row * a.row_bytes);
+  const uint64_t place = (uint32_t)w.place;
+  const uint8_t* from = a.c.codes + place * (uint32_t)a.c.code_stride;
+  const uint16_t* scales = reinterpret_cast<const uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride);
+  if (a.times && l == 0)
+    a.times[w.row] = w.place >= 0 ? __ldg(reinterpret_cast<const double*>(a.c.times + place * (uint32_t)a.c.time_stride)) : 0.0;
+  for (int h = 0; h < a.c.heads; h += U) {
+    uint32_t code[U][2][WORDS], sb[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) w[u] = find<false>(a, g0 + u * (THREADS >> a.lg));
+    for (int u = 0; u < U; ++u) {
+      sb[u] = 0;                                               // an index outside reads as zeros: scale 0
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    sb[u] = 0;
-    when[u] = 0.0;
-#pragma unroll
-    for (int q = 0; q < WORDS; ++q) code[u][0][q] = code[u][1][q] = 0;     // an index outside reads as zeros: scale 0
-    if (w[u].place >= 0) {
-      const uint64_t place = (uint32_t)w[u].place;
-      const uint8_t* from = a.c.codes + place * (uint32_t)a.c.code_stride + w[u].head * a.c.code_bytes;
-      if constexpr (BITS == 4) {
-        code[u][0][0] = __ldg(reinterpret_cast<const uint32_t*>(from) + l);
-        code[u][1][0] = __ldg(reinterpret_cast<const uint32_t*>(from) + l + lanes);
-      } else {
-        const uint2 p = __ldg(reinterpret_cast<const uint2*>(from) + l), q = __ldg(reinterpret_cast<const uint2*>(from) + l + lanes);
-        code[u][0][0] = p.x;
-        code[u][0][1] = p.y;
-        code[u][1][0] = q.x;
-        code[u][1][1] = q.y;
+      for (int q = 0; q < WORDS; ++q) code[u][0][q] = code[u][1][q] = 0;
+      if (w.place >= 0 && h + u < a.c.heads) {
+        if constexpr (BITS == 4) {
+          code[u][0][0] = __ldg(reinterpret_cast<const uint32_t*>(from + u * a.c.code_bytes) + l);
+          code[u][1][0] = __ldg(reinterpret_cast<const uint32_t*>(from + u * a.c.code_bytes) + l + lanes);
+        } else {
+          const uint2 p = __ldg(reinterpret_cast<const uint2*>(from + u * a.c.code_bytes) + l);
+          const uint2 q = __ldg(reinterpret_cast<const uint2*>(from + u * a.c.code_bytes) + l + lanes);
+          code[u][0][0] = p.x;
+          code[u][0][1] = p.y;
+          code[u][1][0] = q.x;
+          code[u][1][1] = q.y;
+        }
+        sb[u] = __ldg(scales + h + u);
       }
-      sb[u] = __ldg(reinterpret_cast<const uint16_t*>(a.c.scales + place * (uint32_t)a.c.scale_stride + 2 * w[u].head));
-      if (a.times && w[u].head == 0 && l == 0) when[u] = __ldg(reinterpret_cast<const double*>(a.c.times + place * (uint32_t)a.c.time_stride));
     }
-  }
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    if (w[u].row >= 0) {
+    for (int u = 0; u < U; ++u) {
+      if (h + u >= a.c.heads) break;
       const float s = __uint_as_float(sb[u] << 16);
-      T* row = reinterpret_cast<T*>(reinterpret_cast<uint8_t*>(rows) + (uint64_t)(uint32_t)w[u].row * a.row_bytes) + w[u].head * a.c.dim;
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         float v[8];
@@ -216,19 +208,25 @@ __global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __
           const uint32_t x = (code[u][p][j / PER] >> (BITS * (j % PER))) & (BITS == 4 ? 0xfu : 0xffu);
           v[j] = (__uint_as_float(0x4b000000u | x) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
         }
-        store8<T, VB>(row, 8 * (l + p * lanes), a.c.dim, v);
+        store8<T, VB>(row + u * a.c.dim, 8 * (l + p * lanes), a.c.dim, v);
       }
-      if (a.times && w[u].head == 0 && l == 0) a.times[w[u].row] = when[u];
     }
+    row += U * a.c.dim;
+    from += U * a.c.code_bytes;
   }
+}
+
+template <bool WRITE, typename T, int VB, int BITS, int U>
+void launch_heads(const Move& a, void* rows, cudaStream_t s) {
+  const unsigned grid = (unsigned)((((uint64_t)a.n << a.lg) + THREADS - 1) / THREADS);
+  if (WRITE) cache_write_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
+  else cache_read_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (T*)rows);
 }
 
 template <bool WRITE, typename T, int VB, int BITS>
 void launch(const Move& a, void* rows, cudaStream_t s) {
-  const uint64_t threads = (uint64_t)a.groups << a.lg;
-  const unsigned grid = (unsigned)((threads + THREADS * U - 1) / (THREADS * U));
-  if (WRITE) cache_write_kernel<T, VB, BITS><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
-  else cache_read_kernel<T, VB, BITS><<<grid, THREADS, 0, s>>>(a, (T*)rows);
+  if (a.c.heads == 1) launch_heads<WRITE, T, VB, BITS, 1>(a, rows, s);
+  else launch_heads<WRITE, T, VB, BITS, 2>(a, rows, s);
 }
 
 // Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8 (heads of 50 in fp32), 4 (heads of 50
@@ -268,12 +266,7 @@ int run(const char* who, const tgnn_cache* cache, void* rows, int dtype, int64_t
   a.src = src;
   a.dst = dst;
   a.index64 = index_bits == 64;
-  a.groups = (uint32_t)(n * a.c.heads);
-  // division by heads > 1: with 2^b >= heads > 2^(b - 1), magic = ceil(2^(31 + b) / heads) is exact below 2^31
-  int b = 1;
-  while ((1 << b) < a.c.heads) ++b;
-  a.heads_magic = a.c.heads == 1 ? 0 : (uint32_t)(((1ull << (31 + b)) + a.c.heads - 1) / a.c.heads);
-  a.heads_shift = b - 1;
+  a.n = (uint32_t)n;
   a.times = times;
   a.status = status;
   const int pad = padded_dim(a.c.dim);

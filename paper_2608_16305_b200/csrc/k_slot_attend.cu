@@ -579,6 +579,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
 // dbias[i] = sum of the blocks' partial sums: a warp per entry, lanes and shuffles in a fixed order.
 __global__ void __launch_bounds__(256) bias_sum_kernel(const double* __restrict__ partial, int blocks, int entries, float* __restrict__ dbias) {
   const int i = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");           // its launch is prepared while the blocks' kernel runs
   if (i >= entries) return;
   double sum = 0.0;
 #pragma unroll 8
@@ -692,8 +693,16 @@ int run(const char* who, SlotArgs& a, int dtype, const void* out_like, float* db
   else e = launch_type<BACKWARD, __half>(a, blocks, s);
   if (e == cudaSuccess && BACKWARD && a.partial) {
     const int entries = a.heads * a.buckets;
-    bias_sum_kernel<<<(entries + 7) / 8, 256, 0, s>>>(a.partial, blocks, entries, dbias);
-    e = cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(entries + 7) / 8);
+    cfg.blockDim = dim3(256);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, bias_sum_kernel, (const double*)a.partial, blocks, entries, dbias);
   }
   if (e != cudaSuccess) {
     cudaGetLastError();

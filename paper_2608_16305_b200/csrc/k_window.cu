@@ -2,17 +2,18 @@
 // strictly earlier than the root's time, and (where asked for) the slots: the most recent `window` of them, then the first
 // `sinks` of what the window leaves out.
 //
-// One warp per root.  The lower bound is found by a 32-way search, as for the most-recent-k search: the lanes probe 32 spread
-// positions with independent loads and a ballot picks the sub-range, so a slice of 2*10^7 entries costs 5 dependent loads.  The
-// slots of the window lie side by side in the T-CSR; the lanes copy 32 of them at a time.  Small batches are bound by the chain of
-// dependent loads (root, slice, search, slots), large ones by the slots' bytes.
+// A warp takes two roots side by side, so that the dependent loads of one (node, slice, search, slots) wait together with the other's.
+// The lower bound is found by a 32-way search, as for the most-recent-k search: the lanes probe 32 spread positions with
+// independent loads and a ballot picks the sub-range, so a slice of 2*10^7 entries costs 5 dependent loads.  The slots of the window
+// lie side by side in the T-CSR; the lanes copy 32 of them at a time.  Small batches are bound by the chain of dependent loads, large
+// ones by the slots' bytes.
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
 
 namespace {
 
-__global__ void __launch_bounds__(256) sample_window_kernel(const int64_t* __restrict__ indptr, const int32_t* __restrict__ g_nbr,
+__global__ void __launch_bounds__(128) sample_window_kernel(const int64_t* __restrict__ indptr, const int32_t* __restrict__ g_nbr,
                                                             const int32_t* __restrict__ g_eid, const double* __restrict__ g_ts,
                                                             int64_t N, int64_t P, const int32_t* __restrict__ nodes,
                                                             const double* __restrict__ times, int n, int window, int sinks,
@@ -20,47 +21,87 @@ __global__ void __launch_bounds__(256) sample_window_kernel(const int64_t* __res
                                                             double* __restrict__ ts_out, int32_t* __restrict__ cnt_out,
                                                             int64_t* __restrict__ first_out, int32_t* __restrict__ len_out,
                                                             int32_t* status) {
+  constexpr int RW = 2;                                                   // roots of a warp
   const int lane = threadIdx.x & 31;
-  const int64_t root = (blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5;
-  if (root >= n) return;
-  const int node = nodes[root];
-  const double t = times[root];
-  int64_t base = 0, lo = 0, hi = 0;
-  const bool known = node >= 0 && node < N;
-  if (known) {
-    base = lo = indptr[node];
-    hi = indptr[node + 1];
+  const int64_t root0 = ((blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5) * RW;
+  if (root0 >= n) return;
+  int64_t base[RW], lo[RW], hi[RW];
+  double t[RW];
+  int node[RW];
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    node[i] = root0 + i < n ? nodes[root0 + i] : -1;
+    t[i] = root0 + i < n ? times[root0 + i] : 0.0;
   }
-  // a node outside the graph, or a slice outside the entries: reported, nothing visible
-  if (!known || base < 0 || hi < base || hi > P || hi - base > 0x7fffffff) {
-    if (lane == 0) atomicMax(status, 4);
-    base = lo = hi = 0;
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    const bool known = node[i] >= 0 && node[i] < N;
+    base[i] = known ? indptr[node[i]] : 0;
+    hi[i] = known ? indptr[node[i] + 1] : -1;
   }
-  while (hi - lo > 32) {
-    const int64_t len = hi - lo;
-    const int64_t idx = lo + ((int64_t)(lane + 1) * len) / 33;            // in [lo, hi), non-decreasing in lane
-    const int c = __popc(__ballot_sync(FULL, g_ts[idx] < t));
-    const int64_t idx_hi = __shfl_sync(FULL, idx, c < 32 ? c : 31);       // first probe with ts >= t
-    const int64_t idx_lo = __shfl_sync(FULL, idx, c > 0 ? c - 1 : 0);     // last probe with ts < t
-    if (c < 32) hi = idx_hi;
-    if (c > 0) lo = idx_lo + 1;
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    // a node outside the graph, or a slice outside the entries: reported, nothing visible
+    if (base[i] < 0 || hi[i] < base[i] || hi[i] > P || hi[i] - base[i] > 0x7fffffff) {
+      if (lane == 0 && root0 + i < n) atomicMax(status, 4);
+      base[i] = hi[i] = 0;
+    }
+    lo[i] = base[i];
   }
-  lo += __popc(__ballot_sync(FULL, lane < hi - lo && g_ts[lo + lane] < t));
-  const int len = (int)(lo - base);
-  const int nw = min(len, window), ns = min(len - nw, sinks), slots = window + sinks;
-  if (lane == 0) {
-    if (first_out) first_out[root] = base;
-    if (len_out) len_out[root] = len;
-    if (cnt_out) cnt_out[root] = nw + ns;
+  while (hi[0] - lo[0] > 32 || hi[1] - lo[1] > 32) {
+    int64_t idx[RW];
+    bool below[RW];
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+      idx[i] = lo[i] + ((int64_t)(lane + 1) * (hi[i] - lo[i])) / 33;      // in [lo, hi) for ranges of 33 and more, non-decreasing in lane
+      below[i] = hi[i] - lo[i] > 32 && g_ts[idx[i]] < t[i];
+    }
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+      if (hi[i] - lo[i] <= 32) continue;
+      const int c = __popc(__ballot_sync(FULL, below[i]));
+      const int64_t idx_hi = __shfl_sync(FULL, idx[i], c < 32 ? c : 31);  // first probe with ts >= t
+      const int64_t idx_lo = __shfl_sync(FULL, idx[i], c > 0 ? c - 1 : 0);// last probe with ts < t
+      if (c < 32) hi[i] = idx_hi;
+      if (c > 0) lo[i] = idx_lo + 1;
+    }
+  }
+  bool below[RW];
+#pragma unroll
+  for (int i = 0; i < RW; ++i) below[i] = lane < hi[i] - lo[i] && g_ts[lo[i] + lane] < t[i];
+  int len[RW], nw[RW], ns[RW];
+  const int slots = window + sinks;
+#pragma unroll
+  for (int i = 0; i < RW; ++i) {
+    len[i] = (int)(lo[i] + __popc(__ballot_sync(FULL, below[i])) - base[i]);
+    nw[i] = min(len[i], window);
+    ns[i] = min(len[i] - nw[i], sinks);
+    if (lane == 0 && root0 + i < n) {
+      if (first_out) first_out[root0 + i] = base[i];
+      if (len_out) len_out[root0 + i] = len[i];
+      if (cnt_out) cnt_out[root0 + i] = nw[i] + ns[i];
+    }
   }
   if (!nbr_out && !eid_out && !ts_out) return;
-  const int64_t row = root * slots;
   for (int j = lane; j < slots; j += 32) {
-    const bool in = j < nw + ns;
-    const int64_t e = j < nw ? base + len - 1 - j : base + (j - nw);
-    if (nbr_out) nbr_out[row + j] = in ? __ldg(g_nbr + e) : -1;
-    if (eid_out) eid_out[row + j] = in ? __ldg(g_eid + e) : -1;
-    if (ts_out) ts_out[row + j] = in ? __ldg(g_ts + e) : 0.0;
+    int nb[RW], ev[RW];
+    double tt[RW];
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+      const bool in = j < nw[i] + ns[i];
+      const int64_t e = j < nw[i] ? base[i] + len[i] - 1 - j : base[i] + (j - nw[i]);
+      nb[i] = nbr_out && in ? __ldg(g_nbr + e) : -1;
+      ev[i] = eid_out && in ? __ldg(g_eid + e) : -1;
+      tt[i] = ts_out && in ? __ldg(g_ts + e) : 0.0;
+    }
+#pragma unroll
+    for (int i = 0; i < RW; ++i) {
+      if (root0 + i >= n) continue;
+      const int64_t at = (root0 + i) * slots + j;
+      if (nbr_out) nbr_out[at] = nb[i];
+      if (eid_out) eid_out[at] = ev[i];
+      if (ts_out) ts_out[at] = tt[i];
+    }
   }
 }
 
@@ -85,8 +126,8 @@ extern "C" int tgnn_sample_window(const int64_t* indptr, const int32_t* nbr, con
         (uintptr_t)len_out | (uintptr_t)status) & 3))
     return fail(err_host, err_size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", who);
   if (n == 0) return TGNN_OK;
-  const unsigned grid = (unsigned)((n + 7) / 8);
-  sample_window_kernel<<<grid, 256, 0, (cudaStream_t)stream>>>(indptr, nbr, eid, ts, num_nodes, num_entries, nodes, times, (int)n, window,
+  const unsigned grid = (unsigned)((n + 7) / 8);                           // 4 warps of two roots
+  sample_window_kernel<<<grid, 128, 0, (cudaStream_t)stream>>>(indptr, nbr, eid, ts, num_nodes, num_entries, nodes, times, (int)n, window,
                                                               sinks, nbr_out, eid_out, ts_out, cnt_out, first_out, len_out, status);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return fail(err_host, err_size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(e));
