@@ -21,7 +21,7 @@
 // brings rows of its own, 20 to a few hundred, and each with its own mask.
 //
 // Work: a unit is a root, a cached head and up to 4 of its query heads (8 where more share it).  Units are handled by a warp, by a block of 4 warps
-// or by a cluster of 2 to 8 blocks whose partial results meet in distributed shared memory (no workspace, no atomics, sums in
+// or by a cluster of 2 to 16 blocks whose partial results meet in distributed shared memory (no workspace, no atomics, sums in
 // a fixed order); the launch takes more warps per unit while the units alone would leave SMs idle and each warp still has a few
 // tiles to walk.
 //
@@ -198,8 +198,8 @@ struct Seen {
 };
 
 // One tile on its way: codes by asynchronous copies to the warp's shared memory (keys, then values, row by row), the scales and time of
-// key `lane` in registers.
-template <int BITS, int DP>
+// one key in registers: key `lane`, or for a single head the lane's own one (8 (lane % 4) + lane / 4).
+template <int BITS, int DP, bool ONE>
 struct Rows {
   using T = Tile<BITS, DP>;
   uint32_t scales;
@@ -215,7 +215,7 @@ struct Rows {
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512 * i), "l"(kp) : "memory");
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + T::TK * T::RB + 512 * i), "l"(vp) : "memory");
     }
-    const int u = u0 + (lane & (T::TK - 1));
+    const int u = u0 + ((ONE ? 8 * (lane & 3) + (lane >> 2) : lane) & (T::TK - 1));
     const uint32_t e = seen.entry(u);
     const uint32_t ks = __ldg(reinterpret_cast<const uint16_t*>(seen.ks + (uint64_t)e * a.k_scale_stride));
     const uint32_t vs = __ldg(reinterpret_cast<const uint16_t*>(seen.vs + (uint64_t)e * a.v_scale_stride));
@@ -224,20 +224,30 @@ struct Rows {
   }
 };
 
-// A unit's running sums over the tiles that one warp walks, for 4 NH heads.  Lane (g, c) has head c of every four: its logits at keys
+// A unit's running sums over the tiles that one warp walks, for 4 NH heads; NH = 0: for a single one, which then fills all columns, so
+// that every lane has its logits and takes one key of the tile to itself (11 % less time than as one of four heads).
+// Lane (g, c) has head c of every four: its logits at keys
 // 16 b + g and 16 b + g + 8, its output columns g VD + i at o[i / 2][.][2 (i & 1) + {hi, lo}] in units of sc, its sum l over the
 // lane's own keys until finish().
+// The largest of a warp's values, NaN left out.
+__device__ __forceinline__ float max_warp(float x) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
+}
+
 template <int BITS, int DP, int NH>
 struct Walk {
   using T = Tile<BITS, DP>;
-  static constexpr int KS = DP / 16, MT = T::VD / 2;
-  float o[MT][NH][4];
-  float m[NH], l[NH], sc[NH], qfac[NH];
-  uint32_t qb[NH][KS][2];
+  static constexpr bool ONE = NH == 0;
+  static constexpr int KS = DP / 16, MT = T::VD / 2, X = ONE ? 1 : NH;
+  float o[MT][X][4];
+  float m[X], l[X], sc[X], qfac[X];
+  uint32_t qb[X][KS][2];
 
   __device__ __forceinline__ void none() {
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
+    for (int x = 0; x < X; ++x) {
       m[x] = -INFINITY;
       l[x] = sc[x] = 0.f;
 #pragma unroll
@@ -251,8 +261,8 @@ struct Walk {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     none();
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
-      const int h = 4 * x + (g >> 1);
+    for (int x = 0; x < X; ++x) {
+      const int h = ONE ? 0 : 4 * x + (g >> 1);
       float q[DP / 4];
       load_query<DP / 4>(a, (root * a.heads + head0 + h) * a.dim, c * (DP / 4), h < nh, q);
       float top = 0.f;
@@ -282,12 +292,12 @@ struct Walk {
                                        int u0, int nh) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     // logits: s[x][j] of head 4 x + c at key 8 j + g
-    float s[NH][T::NT];
+    float s[X][T::NT];
 #pragma unroll
     for (int b = 0; b < T::NT / 2; ++b) {
-      float acc[NH][4];
+      float acc[X][4];
 #pragma unroll
-      for (int x = 0; x < NH; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
+      for (int x = 0; x < X; ++x) acc[x][0] = acc[x][1] = acc[x][2] = acc[x][3] = 0.f;
       const auto r0 = load_piece<T::RB / 4>(rows + (16 * b + g) * T::RB + c * (T::RB / 4));
       const auto r1 = load_piece<T::RB / 4>(rows + (16 * b + 8 + g) * T::RB + c * (T::RB / 4));
 #pragma unroll
@@ -298,7 +308,7 @@ struct Walk {
           nibbles(k0, p);
           nibbles(k1, q);
 #pragma unroll
-          for (int x = 0; x < NH; ++x) {
+          for (int x = 0; x < X; ++x) {
             mma(acc[x], p[0], q[0], p[1], q[1], qb[x][2 * w][0], qb[x][2 * w][1]);
             mma(acc[x], p[2], q[2], p[3], q[3], qb[x][2 * w + 1][0], qb[x][2 * w + 1][1]);
           }
@@ -306,65 +316,99 @@ struct Walk {
           const uint32_t p0 = centre(__byte_perm(k0, 0x64646464u, 0x4140)), p1 = centre(__byte_perm(k0, 0x64646464u, 0x4342));
           const uint32_t q0 = centre(__byte_perm(k1, 0x64646464u, 0x4140)), q1 = centre(__byte_perm(k1, 0x64646464u, 0x4342));
 #pragma unroll
-          for (int x = 0; x < NH; ++x) mma(acc[x], p0, q0, p1, q1, qb[x][w][0], qb[x][w][1]);
+          for (int x = 0; x < X; ++x) mma(acc[x], p0, q0, p1, q1, qb[x][w][0], qb[x][w][1]);
         }
       }
 #pragma unroll
-      for (int x = 0; x < NH; ++x) {
+      for (int x = 0; x < X; ++x) {
         s[x][2 * b] = fmaf(acc[x][1], 1.f / kLo, acc[x][0]);
         s[x][2 * b + 1] = fmaf(acc[x][3], 1.f / kLo, acc[x][2]);
       }
     }
-    float vs[T::NT], top[NH];
+    uint32_t mine = 0;                                                // ONE: the weight of the lane's own key, hi and lo
+    if constexpr (ONE) {
+      const int j = c & (T::NT - 1), key = 8 * j + g;
+      float z = s[0][0];
 #pragma unroll
-    for (int x = 0; x < NH; ++x) top[x] = m[x];
+      for (int i = 1; i < T::NT; ++i) z = j == i ? s[0][i] : z;
+      z = fmaf(z, qfac[0] * __uint_as_float(scales << 16), __ldg(bias + bucket));
+      if (u0 + key >= seen.n) z = -INFINITY;
+      const float top = fmaxf(m[0], max_warp(z));
+      const float base = top == -INFINITY ? 0.f : top;               // nothing but -infinity so far: weights are 0
+      const float corr = exp2_fast((m[0] - base) * kLog2e);          // m = -infinity: 0
+      m[0] = top;
+      const float p = exp2_fast((z - base) * kLog2e);
+      l[0] = fmaf(l[0], corr, c < T::NT ? p : 0.f);                // 16 keys: lanes c >= 2 repeat the others'
+      const float w = p * __uint_as_float(scales & 0xffff0000u), wmax = max_warp(w);
+      const bool some = sc[0] != 0.f;                                // not the first tile: there are sums (corr may be 0)
+      sc[0] *= corr;                                                 // a larger maximum shrinks the unit of the sums, not the sums
+      const float need = __uint_as_float(min(max((__float_as_uint(wmax) >> 23) + 1u, 2u), 252u) << 23);   // 2^e > wmax
+      const float old = sc[0];
+      const bool grow = need > old;
+      sc[0] = grow ? need : old;
+      const float inv = rcp_fast(sc[0]);
+      if (grow && some) {
+        const float f = old * inv;
 #pragma unroll
-    for (int j = 0; j < T::NT; ++j) {
-      const int key = 8 * j + g;
-      const uint32_t two = __shfl_sync(FULL, scales, key);
-      const float ks = __uint_as_float(two << 16);
-      vs[j] = __uint_as_float(two & 0xffff0000u);
-      const int at = __shfl_sync(FULL, bucket, key);
-#pragma unroll
-      for (int x = 0; x < NH; ++x) {
-        const float z = fmaf(s[x][j], qfac[x] * ks, __ldg(bias + min(4 * x + c, nh - 1) * a.buckets + at));
-        s[x][j] = u0 + key < seen.n ? z : -INFINITY;
-        top[x] = fmaxf(top[x], s[x][j]);
+        for (int i = 0; i < MT; ++i) { o[i][0][0] *= f; o[i][0][1] *= f; o[i][0][2] *= f; o[i][0][3] *= f; }
       }
-    }
-    float wmax[NH];
+      const float ws = w * inv;
+      const __half hi = __float2half_rn(ws);
+      const __half lo = __float2half_rn((ws - __half2float(hi)) * kLo);
+      mine = (uint32_t)__half_as_ushort(hi) | (uint32_t)__half_as_ushort(lo) << 16;
+    } else {
+      float vs[T::NT], top[X];
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
-#pragma unroll
-      for (int w = 4; w < 32; w <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(FULL, top[x], w));
-      const float base = top[x] == -INFINITY ? 0.f : top[x];         // nothing but -infinity so far: weights are 0
-      const float corr = exp2_fast((m[x] - base) * kLog2e);          // m = -infinity: 0
-      m[x] = top[x];
-      float sum = 0.f;
-      wmax[x] = 0.f;
+      for (int x = 0; x < X; ++x) top[x] = m[x];
 #pragma unroll
       for (int j = 0; j < T::NT; ++j) {
-        const float p = exp2_fast((s[x][j] - base) * kLog2e);
-        sum += p;
-        s[x][j] = p * vs[j];
-        wmax[x] = fmaxf(wmax[x], s[x][j]);
+        const int key = 8 * j + g;
+        const uint32_t two = __shfl_sync(FULL, scales, key);
+        const float ks = __uint_as_float(two << 16);
+        vs[j] = __uint_as_float(two & 0xffff0000u);
+        const int at = __shfl_sync(FULL, bucket, key);
+#pragma unroll
+        for (int x = 0; x < X; ++x) {
+          const float z = fmaf(s[x][j], qfac[x] * ks, __ldg(bias + min(4 * x + c, nh - 1) * a.buckets + at));
+          s[x][j] = u0 + key < seen.n ? z : -INFINITY;
+          top[x] = fmaxf(top[x], s[x][j]);
+        }
       }
-      l[x] = fmaf(l[x], corr, sum);
-      sc[x] *= corr;                                                 // a larger maximum shrinks the unit of the sums, not the sums
+      float wmax[X];
 #pragma unroll
-      for (int w = 4; w < 32; w <<= 1) wmax[x] = fmaxf(wmax[x], __shfl_xor_sync(FULL, wmax[x], w));
-      const float need = __uint_as_float(min(max((__float_as_uint(wmax[x]) >> 23) + 1u, 2u), 252u) << 23);   // 2^e > wmax
-      const bool grow = need > sc[x];
-      const float old = sc[x];
-      sc[x] = grow ? need : old;
-      const float inv = rcp_fast(sc[x]);
-      if (__any_sync(FULL, grow)) {
-        const float f = grow ? old * inv : 1.f;
+      for (int x = 0; x < X; ++x) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) { o[i][x][0] *= f; o[i][x][1] *= f; o[i][x][2] *= f; o[i][x][3] *= f; }
+        for (int w = 4; w < 32; w <<= 1) top[x] = fmaxf(top[x], __shfl_xor_sync(FULL, top[x], w));
+        const float base = top[x] == -INFINITY ? 0.f : top[x];         // nothing but -infinity so far: weights are 0
+        const float corr = exp2_fast((m[x] - base) * kLog2e);          // m = -infinity: 0
+        m[x] = top[x];
+        float sum = 0.f;
+        wmax[x] = 0.f;
+#pragma unroll
+        for (int j = 0; j < T::NT; ++j) {
+          const float p = exp2_fast((s[x][j] - base) * kLog2e);
+          sum += p;
+          s[x][j] = p * vs[j];
+          wmax[x] = fmaxf(wmax[x], s[x][j]);
+        }
+        l[x] = fmaf(l[x], corr, sum);
+        const bool some = sc[x] != 0.f;                                // not the first tile: there are sums (corr may be 0)
+        sc[x] *= corr;                                                 // a larger maximum shrinks the unit of the sums, not the sums
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) wmax[x] = fmaxf(wmax[x], __shfl_xor_sync(FULL, wmax[x], w));
+        const float need = __uint_as_float(min(max((__float_as_uint(wmax[x]) >> 23) + 1u, 2u), 252u) << 23);   // 2^e > wmax
+        const bool grow = need > sc[x];
+        const float old = sc[x];
+        sc[x] = grow ? need : old;
+        const float inv = rcp_fast(sc[x]);
+        if (__any_sync(FULL, grow && some)) {
+          const float f = grow ? old * inv : 1.f;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) { o[i][x][0] *= f; o[i][x][1] *= f; o[i][x][2] *= f; o[i][x][3] *= f; }
+        }
+#pragma unroll
+        for (int j = 0; j < T::NT; ++j) s[x][j] *= inv;
       }
-#pragma unroll
-      for (int j = 0; j < T::NT; ++j) s[x][j] *= inv;
     }
     // output: 16 keys at a time, in the order c, c + 4, c + 8, c + 12 for lane (g, c), whose values' rows then lie in different banks.
     // The weights go from (key, head) lanes to (column, key) lanes: column g is head g / 2, hi or lo.
@@ -372,9 +416,17 @@ struct Walk {
     rows += T::TK * T::RB + g * T::VB + c * T::RB;
 #pragma unroll
     for (int t = 0; t < T::TK / 16; ++t) {
-      uint32_t pb[NH][2];
+      uint32_t pb[X][2];
+      if constexpr (ONE) {
+        const uint32_t sel = (g & 1) ? 0x7632 : 0x5410;              // hi or lo terms of two keys; key 8 i + k is lane 4 k + i's
 #pragma unroll
-      for (int x = 0; x < NH; ++x) {
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t ka = __shfl_sync(FULL, mine, 4 * c + 2 * t + e), kb = __shfl_sync(FULL, mine, 4 * c + 16 + 2 * t + e);
+          pb[0][e] = __byte_perm(ka, kb, sel);
+        }
+      } else {
+#pragma unroll
+      for (int x = 0; x < X; ++x) {
         uint32_t hi, lo;
         split2(s[x][2 * t], s[x][2 * t + 1], &hi, &lo);
         const uint32_t ha = __shfl_sync(FULL, hi, from), hb = __shfl_sync(FULL, hi, from + 16);
@@ -382,6 +434,7 @@ struct Walk {
         const uint32_t wa = (g & 1) ? la : ha, wb = (g & 1) ? lb : hb;
         pb[x][0] = __byte_perm(wa, wb, 0x5410);                      // keys c, c + 4
         pb[x][1] = __byte_perm(wa, wb, 0x7632);                      // keys c + 8, c + 12
+      }
       }
       const auto v0 = load_piece<T::VB>(rows + 16 * t * T::RB), v1 = load_piece<T::VB>(rows + (16 * t + 4) * T::RB);
       const auto v2 = load_piece<T::VB>(rows + (16 * t + 8) * T::RB), v3 = load_piece<T::VB>(rows + (16 * t + 12) * T::RB);
@@ -392,7 +445,7 @@ struct Walk {
           nibbles(__byte_perm(v0.w[h >> 1], v1.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), p);
           nibbles(__byte_perm(v2.w[h >> 1], v3.w[h >> 1], (h & 1) ? 0x7632 : 0x5410), q);
 #pragma unroll
-          for (int x = 0; x < NH; ++x) {
+          for (int x = 0; x < X; ++x) {
             mma(o[2 * h][x], p[0], p[1], q[0], q[1], pb[x][0], pb[x][1]);
             mma(o[2 * h + 1][x], p[2], p[3], q[2], q[3], pb[x][0], pb[x][1]);
           }
@@ -408,7 +461,7 @@ struct Walk {
             q[e] = centre(and_or(__byte_perm(v2.w[i >> 2], v3.w[i >> 2], sel), 0x00ff00ffu, 0x64006400u));
           }
 #pragma unroll
-          for (int x = 0; x < NH; ++x) mma(o[i / 2][x], p[0], p[1], q[0], q[1], pb[x][0], pb[x][1]);
+          for (int x = 0; x < X; ++x) mma(o[i / 2][x], p[0], p[1], q[0], q[1], pb[x][0], pb[x][1]);
         }
       }
     }
@@ -416,9 +469,9 @@ struct Walk {
 
   __device__ __forceinline__ void finish() {
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
+    for (int x = 0; x < X; ++x) {
 #pragma unroll
-      for (int w = 4; w < 32; w <<= 1) l[x] += __shfl_xor_sync(FULL, l[x], w);
+      for (int w = ONE ? 1 : 4; w < 32; w <<= 1) l[x] += __shfl_xor_sync(FULL, l[x], w);
     }
   }
   // output column g VD + i of head 4 x + c, in units of sc
@@ -430,9 +483,9 @@ struct Walk {
 // BY_BLOCK false: a warp per `take` neighbouring units (all of a root, or one).  true: all warps of a cluster (of one block or more)
 // work on one unit.
 template <int BITS, int DP, int NH, bool BY_BLOCK>
-__global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 128 ? 3 : 5) cached_attend_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP >= 128 || DP * NH >= 128 ? 3 : 5) cached_attend_kernel(const AttendArgs a) {
   using T = Tile<BITS, DP>;
-  constexpr int GH = 4 * NH;                                        // query heads of a unit
+  constexpr int X = NH == 0 ? 1 : NH, GH = 4 * X;                                       // query heads of a unit
   constexpr int STAGE = 2 * T::TK * T::RB;                          // a tile's keys and values
   __shared__ double s_bounds[kMaxBuckets + 1];
   __shared__ __align__(128) uint8_t s_rows[WARPS][2 * STAGE];
@@ -476,11 +529,11 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
   seen.ts = a.ts + first;
   const uint32_t to = (uint32_t)__cvta_generic_to_shared(my) + 16 * lane;
   for (int left = BY_BLOCK ? 1 : a.take; left > 0; --left) {
-    const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
+    const int head0 = kv * a.group + pass * GH, nh = NH == 0 ? 1 : min(GH, a.group - pass * GH);
     const float* bias = a.bias ? a.bias + (int64_t)head0 * a.buckets : &no_bias;
     if (worker < tiles) {
       // two tiles on their way: the query is prepared, and each tile worked on, while the next comes
-      Rows<BITS, DP> next;
+      Rows<BITS, DP, NH == 0> next;
       next.load(a, seen, worker, to);
       asm volatile("cp.async.commit_group;" ::: "memory");
       w.begin(a, root, head0, nh);
@@ -501,7 +554,7 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
     }
     if constexpr (!BY_BLOCK) {
 #pragma unroll
-      for (int x = 0; x < NH; ++x) {
+      for (int x = 0; x < X; ++x) {
         const int h = 4 * x + c;
         const float f = w.l[x] == 0.f ? 0.f : w.sc[x] * rcp_fast(w.l[x]);      // nothing seen, or nothing but -infinity: zeros
         const int64_t base = (root * a.heads + head0 + h) * a.dim;
@@ -529,13 +582,13 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP * NH >= 12
     }
   }
   if constexpr (BY_BLOCK) {
-    const int head0 = kv * a.group + pass * GH, nh = min(GH, a.group - pass * GH);
+    const int head0 = kv * a.group + pass * GH, nh = NH == 0 ? 1 : min(GH, a.group - pass * GH);
     __shared__ float s_m[WARPS][GH], s_l[WARPS][GH], b_m[GH], b_l[GH];
     static_assert(sizeof(s_rows) >= sizeof(float[WARPS][GH][DP + 4]), "the partial outputs take the rows' place");
     float(*s_o)[GH][DP + 4] = reinterpret_cast<float(*)[GH][DP + 4]>(&s_rows[0][0]);
     __syncthreads();                                                 // all warps are done with their rows
 #pragma unroll
-    for (int x = 0; x < NH; ++x) {
+    for (int x = 0; x < X; ++x) {
 #pragma unroll
       for (int i = 0; i < T::VD; ++i) s_o[wid][4 * x + c][g * T::VD + i] = w.value(x, i) * w.sc[x];
       if (g == 0) { s_m[wid][4 * x + c] = w.m[x]; s_l[wid][4 * x + c] = w.l[x]; }
@@ -598,7 +651,7 @@ Shape choose(int64_t roots, int per_root, int64_t tiles) {
   Shape s = {false, 1, tiles <= 1 && roots >= machine ? per_root : 1};
   if (tiles <= 2 || units >= 2 * machine) return s;
   s.by_block = true;
-  while (s.ranks < 8 && units * WARPS * s.ranks * 2 <= machine && tiles >= 2 * WARPS * s.ranks * 2) s.ranks *= 2;
+  while (s.ranks < 16 && units * WARPS * s.ranks * 2 <= machine && tiles >= 2 * WARPS * s.ranks * 2) s.ranks *= 2;
   return s;
 }
 
@@ -619,12 +672,16 @@ cudaError_t launch(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
+  if (sh.ranks > 8) {               // above the portable size: to be allowed per kernel and device
+    const cudaError_t e = cudaFuncSetAttribute(cached_attend_kernel<BITS, DP, NH, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
   return cudaLaunchKernelEx(&cfg, cached_attend_kernel<BITS, DP, NH, true>, a);
 }
 
 template <int BITS, int DP>
 cudaError_t launch_heads(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
-  return a.group > 4 ? launch<BITS, DP, 2>(a, sh, s) : launch<BITS, DP, 1>(a, sh, s);
+  return a.group > 4 ? launch<BITS, DP, 2>(a, sh, s) : a.group > 1 ? launch<BITS, DP, 1>(a, sh, s) : launch<BITS, DP, 0>(a, sh, s);
 }
 
 template <int BITS>
