@@ -185,21 +185,30 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
   const int64_t r = (int64_t)blockIdx.x * a.warps + wid;
   if (r >= a.n) return;
   const int cnt = min(max(a.cnt[r], 0), a.slots);
-  const bool several = cnt > a.chunk;
-  if (!several) fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
-  __syncwarp();
+  const bool several = cnt > a.chunk;                          // chunks are multiples of UN * RPI slots
+  bool filled = several;
   const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
   const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
   for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
     const int kv = kv0 + me.kc;
     for (int g = 0; g < a.group; ++g) {
       const int h = kv * a.group + g;
-      float q[S::N];
-      {
-        S raw;
-        raw.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
-        raw.floats(q);
+      // all first loads on their way before the first of them is waited for
+      const T* kp = kr + (int64_t)me.row * ROW + kv * D;
+      const T* vp = vr + (int64_t)me.row * ROW + kv * D;
+      S k[UN], v[UN], raw;
+#pragma unroll
+      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      raw.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
+#pragma unroll
+      for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      if (!filled) {
+        fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
+        __syncwarp();
+        filled = true;
       }
+      float q[S::N];
+      raw.floats(q);
       const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
       float m = -INFINITY, l = 0.f, acc[S::N];
 #pragma unroll
@@ -211,16 +220,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
           fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
           __syncwarp();
         }
-        const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
-        const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
         for (int s0 = c0 + me.row; s0 - me.row < c1; s0 += UN * me.RPI) {
-          S k[UN], v[UN];
-#pragma unroll
-          for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < c1);
-#pragma unroll
-          for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < c1);
-          kp += UN * me.RPI * ROW;
-          vp += UN * me.RPI * ROW;
           float z[UN];
 #pragma unroll
           for (int u = 0; u < UN; ++u) {
@@ -228,6 +228,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 #pragma unroll
             for (int j = 0; j < S::N; ++j) z[u] = fmaf(k[u].at(j), q[j], z[u]);
           }
+          // the next slots' keys come while these are weighed, their values while the next are
+          const int next = s0 + UN * me.RPI;
+          kp += UN * me.RPI * ROW;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
           if constexpr (P >= 16) {
             // the sums of four slots together, then back to all lanes of the segment
             Reduced<P, UN>::run(z, lane);
@@ -263,6 +268,9 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 #pragma unroll
             for (int j = 0; j < S::N; ++j) acc[j] = fmaf(p, v[u].at(j), acc[j]);
           }
+          vp += UN * me.RPI * ROW;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
         }
       }
       // the groups of lanes that shared a head's slots
@@ -326,32 +334,31 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
     for (int sweep = 0; sweep < (several ? 2 : 1); ++sweep) {
       for (int c0 = 0; c0 == 0 || c0 < cnt; c0 += a.chunk) {
         const int ns = min(cnt - c0, a.chunk);
-        fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane);
-        __syncwarp();
+        bool filled = false;
         // logits and dp of the chunk
         for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
           const int kv = kv0 + me.kc;
           for (int g = 0; g < a.group; ++g) {
             const int h = kv * a.group + g;
-            float q[S::N], go[S::N];
-            {
-              S raw;
-              raw.load(qr + h * D, me.part, D, true);
-              raw.floats(q);
-              raw.load(gr + h * D, me.part, D, true);
-              raw.floats(go);
-            }
-            const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
             const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
             const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
+            S k[UN], v[UN], raw, raw2;
+#pragma unroll
+            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
+#pragma unroll
+            for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
+            raw.load(qr + h * D, me.part, D, true);
+            raw2.load(gr + h * D, me.part, D, true);
+            if (!filled) {
+              fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane);
+              __syncwarp();
+              filled = true;
+            }
+            float q[S::N], go[S::N];
+            raw.floats(q);
+            raw2.floats(go);
+            const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
             for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
-              S k[UN], v[UN];
-#pragma unroll
-              for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
-#pragma unroll
-              for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
-              kp += UN * me.RPI * ROW;
-              vp += UN * me.RPI * ROW;
               float x[2 * UN];                                 // q . k of the four slots, then do . v
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
@@ -362,6 +369,14 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
                   x[UN + u] = fmaf(v[u].at(j), go[j], x[UN + u]);
                 }
               }
+              // the next slots' rows come while these sums are put together
+              const int next = s0 + UN * me.RPI;
+              kp += UN * me.RPI * ROW;
+              vp += UN * me.RPI * ROW;
+#pragma unroll
+              for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
+#pragma unroll
+              for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
               Reduced<P, 2 * UN>::run(x, lane);
               if (sums.first) {
 #pragma unroll
@@ -464,16 +479,18 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
             for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
             const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
             const float* wz = dp + me.row * H + h;
-            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
-              S k[UN];
+            S k[UN];
 #pragma unroll
-              for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, s0 + u * me.RPI < ns);
+            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
+            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
+              const int next = s0 + UN * me.RPI;
               kp += UN * me.RPI * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
                 const float w = s0 + u * me.RPI < ns ? wz[u * me.RPI * H] : 0.f;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) acc[j] = fmaf(w, k[u].at(j), acc[j]);
+                k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
               }
               wz += UN * me.RPI * H;
             }

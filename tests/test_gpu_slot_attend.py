@@ -249,3 +249,16 @@ def test_slots_without_roots(B):
     c = Case(B, 0, 5, 2, 2, 50, "f32", cnt=[])
     assert c.forward().numel() == 0
     assert not c.backward()[3].any()
+
+
+@pytest.mark.parametrize("R,H,KV,D,buckets", [(1, 2, 2, 50, 8), (11, 2, 2, 50, 8), (3, 64, 64, 20, 100), (600, 16, 16, 33, 7), (2000, 4, 4, 50, 5)])
+def test_slots_scratch_is_not_written_beyond_its_size(B, R, H, KV, D, buckets):
+    """Fewer roots than units of work, and more: the documented scratch suffices, and what lies behind it stays."""
+    c = Case(B, R, 4, H, KV, D, "f32", buckets=buckets)
+    n = B.slot_attend_scratch(R, H, buckets)
+    buf = torch.full((n + 4096,), 5.0, device="cuda")
+    g = [torch.empty_like(t) for t in (c.q, c.k, c.v, c.b["bias"])]
+    B.slot_attend_backward(c.q, c.k, c.v, c.cnt, c.do, *g[:3], **c.b, dbias=g[3], scratch=buf[:n])
+    assert (buf[n:] == 5).all()
+    for a, b in zip(g, c.backward()):
+        assert torch.equal(a, b)
