@@ -11,7 +11,7 @@
 // gain on one query per row.  The backward pass recomputes the weights and needs nothing of the forward pass.
 //
 // A warp takes a root.  The values of one (slot, cached head) lie side by side; P lanes hold such a segment, NV words of VB bytes each,
-// so that a warp loads 32 / P segments at once straight into registers, four deep for k and v.  A dot product is then VB / size
+// 8 values in all where there are as many, so that a warp loads 32 / P segments at once straight into registers, two to four deep for k and v.  A dot product is then VB / size
 // multiplications and log2(P) shuffles.  Forward, every group of P lanes runs a softmax of its own over its slots (maximum, sum and
 // output in registers; the groups of a head are merged at the end), so nothing is written between k and the output.  Backward,
 // logits and dp go to shared memory for the root's slots, weights and dz are formed there, and a second walk over k (which lies
@@ -147,7 +147,9 @@ struct Reduced {
   }
 };
 
-constexpr int UN = 4;                                          // segments of k and of v in flight per lane
+// Segments of k and of v in flight per lane: 64 bytes of each, 2 segments at least and 4 at most.
+template <typename S>
+constexpr int kDeep = sizeof(S) >= 32 ? 2 : 4;
 
 // Which segments a lane takes: 32 / P of them at a time, KC neighbouring cached heads of RPI neighbouring slots.
 template <int P>
@@ -172,6 +174,7 @@ __device__ __forceinline__ void fill_buckets(const SlotArgs& a, const double* s_
 template <typename T, int VB, int P, int NV>
 __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
+  constexpr int UN = kDeep<S>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -234,11 +237,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 #pragma unroll
           for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
           if constexpr (P >= 16) {
-            // the sums of four slots together, then back to all lanes of the segment
+            // the sums of all slots together, then back to all lanes of the segment
             Reduced<P, UN>::run(z, lane);
             const float mine = z[0];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) z[u] = __shfl_sync(FULL, mine, (lane & ~(P - 1)) | ((u & 2) ? P / 2 : 0) | ((u & 1) ? P / 4 : 0));
+            for (int u = 0; u < UN; ++u) z[u] = __shfl_sync(FULL, mine, (lane & ~(P - 1)) | (u & UN / 2 ? P / 2 : 0) | (UN == 4 && (u & 1) ? P / 4 : 0));
           } else {
 #pragma unroll
             for (int u = 0; u < UN; ++u) {
@@ -294,6 +297,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 template <typename T, int VB, int P, int NV>
 __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
+  constexpr int UN = kDeep<S>;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -621,26 +625,27 @@ cudaError_t launch_kernel(const SlotArgs& a, int blocks, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// Words of 16 bytes where every head of every row starts on one: 4 to 32 lanes per segment.  Pairs of values (heads of 50) and
-// single values (odd heads, odd bases) take a whole warp per segment.
+// Words of 16 bytes where every head of every row starts on one, pairs of values (heads of 50) or single ones (odd heads, odd
+// bases) otherwise; as many lanes per segment as 8 values each (4 single ones) need.  (Heads of 50 in fp32 over a whole warp, a pair
+// per lane, took 47 us for the 1800 roots of 20 slots that take 40 us this way: the sums' and weights' instructions serve four segments.)
 template <bool BACKWARD, typename T>
 cudaError_t launch_type(const SlotArgs& a, int blocks, cudaStream_t s) {
-  constexpr int V16 = 16 / (int)sizeof(T);
+  constexpr int ES = (int)sizeof(T), N16 = ES / 2;             // words of 16 bytes for 8 values
   const uint64_t at = (uint64_t)(uintptr_t)a.k | (uint64_t)(uintptr_t)a.v | (uint64_t)(uintptr_t)a.q | (uint64_t)(uintptr_t)a.out |
                       (uint64_t)(uintptr_t)a.dout | (uint64_t)(uintptr_t)a.dq | (uint64_t)(uintptr_t)a.dk | (uint64_t)(uintptr_t)a.dv |
-                      (uint64_t)(a.dim * (int)sizeof(T));
+                      (uint64_t)(a.dim * ES);
   if ((at & 15) == 0) {
-    const int words = a.dim / V16;
-    if (words <= 4) return launch_kernel<BACKWARD, T, 16, 4, 1>(a, blocks, s);
-    if (words <= 8) return launch_kernel<BACKWARD, T, 16, 8, 1>(a, blocks, s);
-    if (words <= 16) return launch_kernel<BACKWARD, T, 16, 16, 1>(a, blocks, s);
-    if constexpr (sizeof(T) == 4) return launch_kernel<BACKWARD, T, 16, 32, 1>(a, blocks, s);
+    if (a.dim <= 32) return launch_kernel<BACKWARD, T, 16, 4, N16>(a, blocks, s);
+    if (a.dim <= 64) return launch_kernel<BACKWARD, T, 16, 8, N16>(a, blocks, s);
+    return launch_kernel<BACKWARD, T, 16, 16, N16>(a, blocks, s);
   }
-  if ((at & (2 * sizeof(T) - 1)) == 0) {
-    if (a.dim <= 64) return launch_kernel<BACKWARD, T, 2 * (int)sizeof(T), 32, 1>(a, blocks, s);
-    return launch_kernel<BACKWARD, T, 2 * (int)sizeof(T), 32, 2>(a, blocks, s);
+  if ((at & (2 * ES - 1)) == 0) {
+    if (a.dim <= 32) return launch_kernel<BACKWARD, T, 2 * ES, 4, 4>(a, blocks, s);
+    if (a.dim <= 64) return launch_kernel<BACKWARD, T, 2 * ES, 8, 4>(a, blocks, s);
+    return launch_kernel<BACKWARD, T, 2 * ES, 16, 4>(a, blocks, s);
   }
-  return launch_kernel<BACKWARD, T, (int)sizeof(T), 32, 4>(a, blocks, s);
+  if (a.dim <= 32) return launch_kernel<BACKWARD, T, ES, 8, 4>(a, blocks, s);
+  return launch_kernel<BACKWARD, T, ES, 32, 4>(a, blocks, s);
 }
 
 constexpr int SMEM_BLOCK = 200 * 1024;     // of an SM's 227 KB, beside the bounds and what the system keeps
