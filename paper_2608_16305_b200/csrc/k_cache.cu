@@ -16,6 +16,8 @@
 // Both kernels are bound by HBM.  2 to 8 neighbouring lanes take a row, head after head, two heads at a time where there are two.  A lane
 // takes two pieces of 8 values of a head, half a head apart, so that the lanes of a row move whole sectors; the index arithmetic of
 // a row is done once.
+#include <type_traits>
+
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
@@ -96,6 +98,43 @@ __device__ __forceinline__ void store8(T* row, int e0, int dim, const float (&v)
   }
 }
 
+// The group's scale (the bits of a bf16) from its largest magnitude, and the codes of PIECES times 8 of its values.
+template <int BITS, int PIECES>
+__device__ __forceinline__ uint16_t quantise(float amax, const float (*v)[8], uint32_t (*code)[BITS == 4 ? 1 : 2]) {
+  const bool bad = !(amax <= 3.4028234e38f);
+  float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
+  if (amax < 7.8886091e-31f) s = 0.f;                                     // 2^-100
+  const float r = s > 0.f ? __frcp_rn(s) : 0.f;
+  // float bits of 1.5 * 2^23 + offset + code, added up with shifts; the fixed part of the sum is taken off at the end
+  constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
+  constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+#pragma unroll
+    for (int q = 0; q < WORDS; ++q) {
+      uint32_t acc = 0, fixed = 0;
+#pragma unroll
+      for (int j = PER - 1; j >= 0; --j) {
+        acc = (acc << BITS) + __float_as_uint(fmaf(v[p][q * PER + j], r, kMagic));
+        fixed = (fixed << BITS) + 0x4b400000u;
+      }
+      code[p][q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
+    }
+  }
+  return bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
+}
+
+// The 8 values of codes: a code under fp32's exponent for 2^23 reads as 2^23 + offset + code.
+template <int BITS>
+__device__ __forceinline__ void values(const uint32_t (&code)[BITS == 4 ? 1 : 2], float s, float (&v)[8]) {
+  constexpr int PER = BITS == 4 ? 8 : 4;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t x = (code[j / PER] >> (BITS * (j % PER))) & (BITS == 4 ? 0xfu : 0xffu);
+    v[j] = (__uint_as_float(0x4b000000u | x) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
+  }
+}
+
 // U heads of a row at a time: 2, or 1 for rows of one head.  (A million rows of 4 x 64 in bf16 in 4 bits, written and read: 298 us; four at
 // a time, whose registers leave half the warps, 312 to 340 us.)
 template <typename T, int VB, int BITS, int U>
@@ -127,27 +166,9 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, cons
       amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 1));
       if (lanes > 2) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 2));
       if (lanes > 4) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 4));
-      const bool bad = !(amax <= 3.4028234e38f);
-      float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
-      if (amax < 7.8886091e-31f) s = 0.f;                                 // 2^-100
-      const float r = s > 0.f ? __frcp_rn(s) : 0.f;
-      // float bits of 1.5 * 2^23 + offset + code, added up with shifts; the fixed part of the sum is taken off at the end
-      constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
-      constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+      constexpr int WORDS = BITS == 4 ? 1 : 2;
       uint32_t code[2][WORDS];
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-#pragma unroll
-        for (int q = 0; q < WORDS; ++q) {
-          uint32_t acc = 0, fixed = 0;
-#pragma unroll
-          for (int j = PER - 1; j >= 0; --j) {
-            acc = (acc << BITS) + __float_as_uint(fmaf(v[p][q * PER + j], r, kMagic));
-            fixed = (fixed << BITS) + 0x4b400000u;
-          }
-          code[p][q] = bad ? (BITS == 4 ? 0x88888888u : 0x80808080u) : acc - fixed;
-        }
-      }
+      const uint16_t sb = quantise<BITS, 2>(amax, v, code);
       if (w.place >= 0 && h + u < a.c.heads) {
         if constexpr (BITS == 4) {
           reinterpret_cast<uint32_t*>(to + u * a.c.code_bytes)[l] = code[0][0];
@@ -156,7 +177,7 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, cons
           reinterpret_cast<uint2*>(to + u * a.c.code_bytes)[l] = make_uint2(code[0][0], code[0][1]);
           reinterpret_cast<uint2*>(to + u * a.c.code_bytes)[l + lanes] = make_uint2(code[1][0], code[1][1]);
         }
-        if (l == 0) scales[h + u] = bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
+        if (l == 0) scales[h + u] = sb;
       }
     }
     row += U * a.c.dim;
@@ -205,17 +226,109 @@ __global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         float v[8];
-        // a code under fp32's exponent for 2^23 reads as 2^23 + offset + code
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t x = (code[u][p][j / PER] >> (BITS * (j % PER))) & (BITS == 4 ? 0xfu : 0xffu);
-          v[j] = (__uint_as_float(0x4b000000u | x) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
-        }
+        values<BITS>(code[u][p], s, v);
         store8<T, VB>(row + u * a.c.dim, 8 * (l + p * lanes), a.c.dim, v);
       }
     }
     row += U * a.c.dim;
     from += U * a.c.code_bytes;
+  }
+}
+
+// Rows whose heads start on no word of several values (odd heads, odd bases): read value by value in the order of the codes, the lanes
+// of a warp would touch a sector each.  Here a warp moves 32 / lanes whole groups (heads of rows, numbered row by row) in words of VB bytes that
+// lie side by side, and hands the values over in shared memory, as fp32; the codes' side is as above, 8 values per lane.  A group's
+// place in shared memory is a multiple of 8 and one long, which spreads the lanes' reads over the banks.
+template <typename T, int VB, int BITS, bool WRITE>
+__global__ void __launch_bounds__(THREADS) cache_narrow_kernel(const Move a, typename std::conditional<WRITE, const T, T>::type* __restrict__ rows) {
+  constexpr int VE = VB / (int)sizeof(T), N = 8 / VE, PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+  typedef typename Vec<VB>::type W;
+  union Word { W w; T x[VE]; };
+  __shared__ float s_values[THREADS / 32][256 + 8];
+  const int lane = threadIdx.x & 31, lg = a.lg + 1, lanes = 1 << lg, count = 32 >> lg, ld = 8 * lanes + 1;
+  float* mine = s_values[threadIdx.x >> 5];
+  const uint64_t g0 = ((uint64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * count, g = g0 + lane;
+  // lane i < count: where group g0 + i lies
+  Where w = {-1, -1};
+  int head = 0;
+  if (lane < count && g < (uint64_t)a.n * a.c.heads) {
+    const uint32_t i = (uint32_t)g / (uint32_t)a.c.heads;
+    head = (int)((uint32_t)g - i * (uint32_t)a.c.heads);
+    w = find<WRITE>(a, i);
+  }
+  if (a.times && head == 0 && (WRITE ? w.place : w.row) >= 0) {
+    double* in_cache = reinterpret_cast<double*>(a.c.times + (uint64_t)(uint32_t)w.place * (uint32_t)a.c.time_stride);
+    if (WRITE) *in_cache = w.row >= 0 ? __ldg(a.times + w.row) : 0.0;
+    else a.times[w.row] = w.place >= 0 ? __ldg(in_cache) : 0.0;
+  }
+  const int64_t row_at = w.row < 0 ? -1 : (int64_t)((uint64_t)(uint32_t)w.row * a.row_bytes) + (int64_t)head * a.c.dim * (int)sizeof(T);
+  const int per = a.c.dim / VE, magic = (65536 + per - 1) / per;     // word x of the warp belongs to group (x * magic) >> 16: exact below 256
+  const int own = lane >> lg, l = lane & (lanes - 1);                // the lane's group and its 8 values there
+  const int64_t place = __shfl_sync(FULL, w.place, own);
+  const int own_head = __shfl_sync(FULL, head, own);
+  uint8_t* codes = a.c.codes + (uint64_t)(uint32_t)place * (uint32_t)a.c.code_stride + own_head * a.c.code_bytes;
+  uint16_t* scale = reinterpret_cast<uint16_t*>(a.c.scales + (uint64_t)(uint32_t)place * (uint32_t)a.c.scale_stride) + own_head;
+  if constexpr (WRITE) {
+    Word raw[N];
+    int at[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int x = lane + 32 * j, grp = min((x * magic) >> 16, count - 1), off = x - grp * per;
+      const int64_t from = __shfl_sync(FULL, row_at, grp);
+      at[j] = off < per ? grp * ld + off * VE : -1;
+      raw[j].w = W();
+      if (off < per && from >= 0) raw[j].w = __ldg(reinterpret_cast<const W*>(reinterpret_cast<const uint8_t*>(rows) + from) + off);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (at[j] >= 0) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) mine[at[j] + e] = to_float<T>(raw[j].x[e]);
+      }
+    }
+    __syncwarp();
+    float v[8], amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = 8 * l + j < a.c.dim ? mine[own * ld + 8 * l + j] : 0.f;
+      amax = max_nan(amax, fabsf(v[j]));
+    }
+    for (int o = 1; o < lanes; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, o));
+    uint32_t code[WORDS];
+    const uint16_t sb = quantise<BITS, 1>(amax, &v, &code);
+    if (place < 0) return;
+    if constexpr (BITS == 4) reinterpret_cast<uint32_t*>(codes)[l] = code[0];
+    else reinterpret_cast<uint2*>(codes)[l] = make_uint2(code[0], code[WORDS - 1]);
+    if (l == 0) *scale = sb;
+  } else {
+    uint32_t code[WORDS] = {};
+    uint32_t sb = 0;
+    if (place >= 0) {
+      if constexpr (BITS == 4) {
+        code[0] = __ldg(reinterpret_cast<const uint32_t*>(codes) + l);
+      } else {
+        const uint2 p = __ldg(reinterpret_cast<const uint2*>(codes) + l);
+        code[0] = p.x;
+        code[WORDS - 1] = p.y;
+      }
+      sb = __ldg(scale);
+    }
+    float v[8];
+    values<BITS>(code, __uint_as_float(sb << 16), v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) mine[own * ld + 8 * l + j] = v[j];
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int x = lane + 32 * j, grp = min((x * magic) >> 16, count - 1), off = x - grp * per;
+      const int64_t to = __shfl_sync(FULL, row_at, grp);
+      if (off < per && to >= 0) {
+        Word out;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) out.x[e] = from_float<T>(mine[grp * ld + off * VE + e]);
+        reinterpret_cast<W*>(reinterpret_cast<uint8_t*>(rows) + to)[off] = out.w;
+      }
+    }
   }
 }
 
@@ -225,22 +338,36 @@ void launch_heads(const Move& a, void* rows, cudaStream_t s) {
   if (WRITE) cache_write_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
   else cache_read_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (T*)rows);
 }
-
 template <bool WRITE, typename T, int VB, int BITS>
-void launch(const Move& a, void* rows, cudaStream_t s) {
+void launch_rows(const Move& a, void* rows, cudaStream_t s) {
   if (a.c.heads == 1) launch_heads<WRITE, T, VB, BITS, 1>(a, rows, s);
   else launch_heads<WRITE, T, VB, BITS, 2>(a, rows, s);
 }
+template <bool WRITE, typename T, int VB, int BITS>
+void launch_narrow(const Move& a, void* rows, cudaStream_t s) {
+  const uint64_t lanes = ((uint64_t)a.n * a.c.heads) << (a.lg + 1);
+  cache_narrow_kernel<T, VB, BITS, WRITE><<<(unsigned)((lanes + THREADS - 1) / THREADS), THREADS, 0, s>>>(
+      a, (typename std::conditional<WRITE, const T, T>::type*)rows);
+}
 
-// Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8 (heads of 50 in fp32), 4 (heads of 50
-// in 16 bits) or single values.
+// Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8 or 4; by way of shared memory where that
+// is a single value, and for pairs in fp32 of heads up to 64 wide.  250 000 rows written in 4 bits and read, without the detour and with it:
+// 8 x 25 in fp32 443 and 237 us, 8 x 43 579 and 446, 8 x 50 440 and 376; but 4 x 86 314 and 372, 8 x 50 in bf16 289 and 373.
 template <bool WRITE, typename T, int BITS>
 void launch_aligned(const Move& a, void* rows, cudaStream_t s) {
-  const uint64_t at = (uint64_t)(uintptr_t)rows | (uint64_t)a.row_bytes | (uint64_t)(a.c.dim * (int)sizeof(T));
-  if ((at & 15) == 0) launch<WRITE, T, 16, BITS>(a, rows, s);
-  else if (sizeof(T) == 4 && (at & 7) == 0) launch<WRITE, T, 8, BITS>(a, rows, s);
-  else if ((at & 3) == 0) launch<WRITE, T, 4, BITS>(a, rows, s);
-  else launch<WRITE, T, sizeof(T), BITS>(a, rows, s);
+  constexpr int ES = (int)sizeof(T);
+  const uint64_t at = (uint64_t)(uintptr_t)rows | (uint64_t)a.row_bytes | (uint64_t)(a.c.dim * ES);
+  if ((at & 15) == 0) {
+    launch_rows<WRITE, T, 16, BITS>(a, rows, s);
+  } else if ((at & 7) == 0) {
+    if (ES == 4 && a.c.dim <= 64) launch_narrow<WRITE, T, 8, BITS>(a, rows, s);
+    else launch_rows<WRITE, T, 8, BITS>(a, rows, s);
+  } else if constexpr (ES == 2) {
+    if ((at & 3) == 0) launch_rows<WRITE, T, 4, BITS>(a, rows, s);
+    else launch_narrow<WRITE, T, 2, BITS>(a, rows, s);
+  } else {
+    launch_narrow<WRITE, T, 4, BITS>(a, rows, s);
+  }
 }
 
 template <bool WRITE>
