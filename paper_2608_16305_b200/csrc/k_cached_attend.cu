@@ -255,6 +255,50 @@ struct Walk {
     }
   }
 
+  // The query of a single head.  All eight lanes of a quarter need the same columns, so each prepares two or four of them and they meet
+  // in shared memory (`to`: 4 DP bytes of the warp's own), in the order in which the lanes read them: hi terms, then lo terms.
+  __device__ __forceinline__ void begin_one(const AttendArgs& a, int64_t root, int head, uint32_t* to) {
+    none();
+    const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+    constexpr int PAIRS = DP / 64 > 0 ? DP / 64 : 1;                 // of columns per lane (DP 32: every other lane has one)
+    float x[PAIRS][2], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) {
+      const int e = c * (DP / 4) + 2 * (g * PAIRS + i);
+      load_query<2>(a, (root * a.heads + head) * a.dim, e, DP >= 64 || g < 4, x[i]);
+      top = fmaxf(top, fmaxf(fabsf(x[i][0]), fabsf(x[i][1])));
+    }
+    top = max_warp(top);
+    // 2^e <= top < 2^(e + 1): scaled queries lie below 2 (infinities and NaN stay what they are)
+    const int e = min(max((int)(__float_as_uint(top) >> 23), 2), 252);
+    const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+    qfac[0] = a.scale * __uint_as_float((uint32_t)e << 23);
+    __half* hi = reinterpret_cast<__half*>(to) + c * (DP / 4);
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int d = 2 * (g * PAIRS + i) + k;                       // column of the quarter
+        // its place: columns j and j + 4 of every 8 share a word where nibbles are paired so
+        const int at = BITS == 4 ? (d & ~7) + 2 * (d & 3) + ((d >> 2) & 1) : d;
+        const float y = x[i][k] * down;
+        const __half h = __float2half_rn(y);
+        if (DP >= 64 || g < 4) {
+          hi[at] = h;
+          hi[DP + at] = __float2half_rn((y - __half2float(h)) * kLo);
+        }
+      }
+    }
+    __syncwarp();
+    const uint32_t* mine = to + (g & 1) * (DP / 2) + c * (DP / 8);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      qb[0][s][0] = mine[2 * s];
+      qb[0][s][1] = mine[2 * s + 1];
+    }
+    __syncwarp();                                                    // the next unit's query may be written
+  }
+
   // The query: lane (g, c) holds columns [c DP / 4, (c + 1) DP / 4) of head g / 2 of every four, the hi terms where g is even, lo
   // where it is odd, divided by a power of two.
   __device__ __forceinline__ void begin(const AttendArgs& a, int64_t root, int head0, int nh) {
@@ -489,6 +533,7 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP >= 128 || 
   constexpr int STAGE = 2 * T::TK * T::RB;                          // a tile's keys and values
   __shared__ double s_bounds[kMaxBuckets + 1];
   __shared__ __align__(128) uint8_t s_rows[WARPS][2 * STAGE];
+  __shared__ __align__(16) uint32_t s_query[NH == 0 ? WARPS : 1][DP];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
   uint8_t* my = s_rows[wid];
   if (a.bias) {
@@ -536,7 +581,8 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP >= 128 || 
       Rows<BITS, DP, NH == 0> next;
       next.load(a, seen, worker, to);
       asm volatile("cp.async.commit_group;" ::: "memory");
-      w.begin(a, root, head0, nh);
+      if constexpr (NH == 0) w.begin_one(a, root, head0, s_query[wid]);
+      else w.begin(a, root, head0, nh);
       int buf = 0, bucket = 0;                                      // (without a bias: bucket 0 of none)
       for (int tile = worker; tile < tiles; tile += workers) {
         const uint32_t scales = next.scales;
