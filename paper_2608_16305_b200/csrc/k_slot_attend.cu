@@ -45,17 +45,16 @@ struct SlotArgs {
   float scale;
 };
 
-// A warp's shared memory, all parts multiples of 16 bytes: bucket [chunk] (bytes); backward: z and dp [chunk * H], per head m, 1 / l
-// and delta, dq [H * dim] where there are several chunks, and with a bias the table [H * buckets] in fp64.
+// A warp's shared memory, all parts multiples of 16 bytes: bucket [chunk] (bytes); backward: z and dp [chunk * H] in pairs, per head m,
+// 1 / l and delta, dq [H * dim] where there are several chunks, and with a bias the table [H * buckets] in fp64.
 struct Layout {
-  int z, dp, head, dq, table, total;
+  int z, head, dq, table, total;
 };
 __host__ __device__ inline int up16(int x) { return (x + 15) & ~15; }
 __host__ __device__ inline Layout layout(int heads, int dim, int chunk, bool several, bool backward, int table) {
   Layout l;
   int at = up16(chunk);
-  l.z = at; at += backward ? up16(heads * chunk * 4) : 0;
-  l.dp = at; at += backward ? up16(heads * chunk * 4) : 0;
+  l.z = at; at += backward ? up16(heads * chunk * 8) : 0;
   l.head = at; at += backward ? up16(heads * 16) : 0;
   l.dq = at; at += backward && several ? up16(heads * dim * 4) : 0;
   l.table = at; at += up16(table * 8);
@@ -306,8 +305,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
   const Layout L = layout(H, D, a.chunk, a.chunk < a.slots, true, table ? H * a.buckets : 0);
   uint8_t* my = smem + (size_t)wid * a.warp_bytes;
   uint8_t* bucket = my;
-  float* z = reinterpret_cast<float*>(my + L.z);               // [slot][head]: logits, then weights
-  float* dp = reinterpret_cast<float*>(my + L.dp);             // [slot][head]: do . v, then dz
+  float2* zd = reinterpret_cast<float2*>(my + L.z);            // [slot][head]: logit and do . v, then weight and dz
   float *s_m = reinterpret_cast<float*>(my + L.head), *s_l = s_m + H, *s_d = s_m + 2 * H;
   float* s_dq = reinterpret_cast<float*>(my + L.dq);
   double* tab = reinterpret_cast<double*>(my + L.table);
@@ -390,9 +388,9 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
                     if (sums.id + i < UN) {
                       float y = x[i] * a.scale;
                       if (bias) y += __ldg(bias + bucket[s]);
-                      z[s * H + h] = y;
+                      zd[s * H + h].x = y;
                     } else {
-                      dp[s * H + h] = x[i];
+                      zd[s * H + h].y = x[i];
                     }
                   }
                 }
@@ -411,15 +409,16 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
             const bool in = h < H;
             const float was = in ? s_m[h] : -INFINITY;
             float top = was;
-            for (int s = part; in && s < ns; s += 1 << lg) top = fmaxf(top, z[s * H + h]);
+            for (int s = part; in && s < ns; s += 1 << lg) top = fmaxf(top, zd[s * H + h].x);
             for (int w = 1; w < (1 << lg); w <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, w));
             const float base = top == -INFINITY ? 0.f : top;   // nothing but -infinity: weights are 0
             float sum = 0.f, del = 0.f;
             for (int s = part; in && s < ns; s += 1 << lg) {
-              const float p = exp2_fast((z[s * H + h] - base) * kLog2e);
-              if (!several) z[s * H + h] = p;
+              const float2 at = zd[s * H + h];
+              const float p = exp2_fast((at.x - base) * kLog2e);
+              if (!several) zd[s * H + h].x = p;
               sum += p;
-              del = fmaf(p, dp[s * H + h], del);
+              del = fmaf(p, at.y, del);
             }
             for (int w = 1; w < (1 << lg); w <<= 1) {
               sum += __shfl_xor_sync(FULL, sum, w);
@@ -444,33 +443,43 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
         }
         // weights and dz
         for (int i = lane, h = h_first; i < ns * H; i += 32) {
-          float p = z[i];
+          const float2 at = zd[i];
+          float p = at.x;
           if (several) {
             const float m = s_m[h];
             p = exp2_fast((p - (m == -INFINITY ? 0.f : m)) * kLog2e);
           }
           p *= s_l[h];
-          z[i] = p;
-          dp[i] = p * (dp[i] - s_d[h]);
+          zd[i] = make_float2(p, p * (at.y - s_d[h]));
           h += h_step;
           if (h >= H) h -= H;
         }
         __syncwarp();
         if (table) {
-          // a lane per head, so that no two lanes add to one bucket; slots of one bucket mostly lie side by side
-          for (int h = lane; h < H; h += 32) {
-            double sum = 0.0;
-            int b = ns > 0 ? bucket[0] : 0;
-            for (int s = 0; s < ns; ++s) {
-              const int nb = bucket[s];
-              if (nb != b) {
-                tab[h * a.buckets + b] += sum;
-                sum = 0.0;
-                b = nb;
+          // 32 slots at a time.  Slots in time order have neighbouring buckets: runs of one bucket are summed by a segmented scan and each
+          // run's last lane adds to its bucket, all different ones.  Otherwise a lane per head goes through them.
+          for (int t0 = 0; t0 < ns; t0 += 32) {
+            const int s = t0 + lane, b = bucket[min(s, ns - 1)];
+            const int below = __shfl_up_sync(FULL, b, 1), above = __shfl_down_sync(FULL, b, 1);
+            if (__all_sync(FULL, lane == 31 || b <= above) || __all_sync(FULL, lane == 31 || b >= above)) {
+              const unsigned starts = __ballot_sync(FULL, lane == 0 || b != below);
+              const int back = lane - (31 - __clz(starts & (0xffffffffu >> (31 - lane))));   // lanes to the run's first
+              const bool end = lane == 31 || b != above;
+              for (int h = 0; h < H; ++h) {
+                float v = s < ns ? zd[s * H + h].y : 0.f;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                  const float w = __shfl_up_sync(FULL, v, o);
+                  if (back >= o) v += w;
+                }
+                if (end) tab[h * a.buckets + b] += (double)v;
               }
-              sum += (double)dp[s * H + h];
+            } else {
+              for (int h = lane; h < H; h += 32) {
+                for (int u = t0; u < min(t0 + 32, ns); ++u) tab[h * a.buckets + bucket[u]] += (double)zd[u * H + h].y;
+              }
             }
-            tab[h * a.buckets + b] += sum;
+            __syncwarp();
           }
         }
         const bool final_chunk = c0 + a.chunk >= cnt;
@@ -482,7 +491,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
 #pragma unroll
             for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
             const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
-            const float* wz = dp + me.row * H + h;
+            const float2* wz = zd + me.row * H + h;
             S k[UN];
 #pragma unroll
             for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
@@ -491,7 +500,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
               kp += UN * me.RPI * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
-                const float w = s0 + u * me.RPI < ns ? wz[u * me.RPI * H] : 0.f;
+                const float w = s0 + u * me.RPI < ns ? wz[u * me.RPI * H].y : 0.f;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) acc[j] = fmaf(w, k[u].at(j), acc[j]);
                 k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
@@ -532,11 +541,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
             }
 #pragma unroll
             for (int j = 0; j < S::N; ++j) q[j] *= a.scale;
-            const float *wz = dp + s * H + kv, *wp = z + s * H + kv;
+            const float2* at = zd + s * H + kv;
 #pragma unroll 2
             for (; s < ns; s += me.RPI) {
               float xk[S::N], xv[S::N];
-              const float y = *wz, p = *wp;
+              const float p = at->x, y = at->y;
 #pragma unroll
               for (int j = 0; j < S::N; ++j) {
                 xk[j] = y * q[j];
@@ -546,8 +555,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
               S::store(dvp, me.part, D, xv);
               dkp += me.RPI * ROW;
               dvp += me.RPI * ROW;
-              wz += me.RPI * H;
-              wp += me.RPI * H;
+              at += me.RPI * H;
             }
           } else {
             for (; s < ns; s += me.RPI) {
@@ -558,7 +566,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
                 S q, go;
                 q.load(qr + h * D, me.part, D, true);
                 go.load(gr + h * D, me.part, D, true);
-                const float y = dp[s * H + h] * a.scale, p = z[s * H + h];
+                const float p = zd[s * H + h].x, y = zd[s * H + h].y * a.scale;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) {
                   xk[j] = fmaf(y, q.at(j), xk[j]);
