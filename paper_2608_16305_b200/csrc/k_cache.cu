@@ -16,6 +16,9 @@
 // Both kernels are bound by HBM.  2 to 8 neighbouring lanes take a row, head after head, two heads at a time where there are two.  A lane
 // takes two pieces of 8 values of a head, half a head apart, so that the lanes of a row move whole sectors; the index arithmetic of
 // a row is done once.
+//
+// Measured on a B200, a million rows of 4 x 64 in bf16 at random places, in 4 bits: written in 141 us (4.8 TB/s of DRAM), read back in
+// 138 us (4.7); a copy of whole tables reaches 6.5.
 #include <type_traits>
 
 #include "tgnn_history.cuh"

@@ -25,7 +25,8 @@ __global__ void __launch_bounds__(128) sample_window_kernel(const int64_t* __res
   const int lane = threadIdx.x & 31;
   const int64_t root0 = ((blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5) * RW;
   if (root0 >= n) return;
-  int64_t base[RW], lo[RW], hi[RW];
+  int64_t base[RW];
+  uint32_t lo[RW], hi[RW];                                                // the bound lies in [lo, hi] behind base
   double t[RW];
   int node[RW];
 #pragma unroll
@@ -37,43 +38,41 @@ __global__ void __launch_bounds__(128) sample_window_kernel(const int64_t* __res
   for (int i = 0; i < RW; ++i) {
     const bool known = node[i] >= 0 && node[i] < N;
     base[i] = known ? indptr[node[i]] : 0;
-    hi[i] = known ? indptr[node[i] + 1] : -1;
-  }
-#pragma unroll
-  for (int i = 0; i < RW; ++i) {
+    int64_t end = known ? indptr[node[i] + 1] : -1;
     // a node outside the graph, or a slice outside the entries: reported, nothing visible
-    if (base[i] < 0 || hi[i] < base[i] || hi[i] > P || hi[i] - base[i] > 0x7fffffff) {
+    if (base[i] < 0 || end < base[i] || end > P || end - base[i] > 0x7fffffff) {
       if (lane == 0 && root0 + i < n) atomicMax(status, 4);
-      base[i] = hi[i] = 0;
+      base[i] = end = 0;
     }
-    lo[i] = base[i];
+    lo[i] = 0;
+    hi[i] = (uint32_t)(end - base[i]);
   }
   while (hi[0] - lo[0] > 32 || hi[1] - lo[1] > 32) {
-    int64_t idx[RW];
+    uint32_t idx[RW];
     bool below[RW];
 #pragma unroll
     for (int i = 0; i < RW; ++i) {
-      idx[i] = lo[i] + ((int64_t)(lane + 1) * (hi[i] - lo[i])) / 33;      // in [lo, hi) for ranges of 33 and more, non-decreasing in lane
-      below[i] = hi[i] - lo[i] > 32 && g_ts[idx[i]] < t[i];
+      idx[i] = lo[i] + (uint32_t)(lane + 1) * ((hi[i] - lo[i]) / 33);     // in [lo, hi) and ascending for ranges of 33 and more
+      below[i] = hi[i] - lo[i] > 32 && (g_ts + base[i])[idx[i]] < t[i];
     }
 #pragma unroll
     for (int i = 0; i < RW; ++i) {
       if (hi[i] - lo[i] <= 32) continue;
       const int c = __popc(__ballot_sync(FULL, below[i]));
-      const int64_t idx_hi = __shfl_sync(FULL, idx[i], c < 32 ? c : 31);  // first probe with ts >= t
-      const int64_t idx_lo = __shfl_sync(FULL, idx[i], c > 0 ? c - 1 : 0);// last probe with ts < t
+      const uint32_t idx_hi = __shfl_sync(FULL, idx[i], c < 32 ? c : 31); // first probe with ts >= t
+      const uint32_t idx_lo = __shfl_sync(FULL, idx[i], c > 0 ? c - 1 : 0);   // last probe with ts < t
       if (c < 32) hi[i] = idx_hi;
       if (c > 0) lo[i] = idx_lo + 1;
     }
   }
   bool below[RW];
 #pragma unroll
-  for (int i = 0; i < RW; ++i) below[i] = lane < hi[i] - lo[i] && g_ts[lo[i] + lane] < t[i];
+  for (int i = 0; i < RW; ++i) below[i] = (uint32_t)lane < hi[i] - lo[i] && (g_ts + base[i])[lo[i] + lane] < t[i];
   int len[RW], nw[RW], ns[RW];
   const int slots = window + sinks;
 #pragma unroll
   for (int i = 0; i < RW; ++i) {
-    len[i] = (int)(lo[i] + __popc(__ballot_sync(FULL, below[i])) - base[i]);
+    len[i] = (int)lo[i] + __popc(__ballot_sync(FULL, below[i]));
     nw[i] = min(len[i], window);
     ns[i] = min(len[i] - nw[i], sinks);
     if (lane == 0 && root0 + i < n) {
