@@ -582,7 +582,7 @@ TGNN_API int tgnn_cache_read(const tgnn_cache* cache_host, void* rows, int dtype
  *   fp64[num_buckets - 1] ascending, times: fp64[n] and ts: fp64[k.rows] are needed (num_buckets 1 to 128).  window >= 0, sinks >= 0,
  *   not both 0.  max_len: no root's len is above it, or 0 if unknown (it chooses the launch; results hold for any len).
  *   A root that sees nothing, or whose logits are all -infinity, gets zeros; entries that it does not see do not touch its result.
- *   A history outside the cache (first < 0, len < 0, first + len > rows) sees nothing, status 4.
+ *   A history outside the cache (first < 0, len < 0, first + len > rows) or of 2^31 - 64 entries and more sees nothing, status 4.
  *   n * kv_heads * ceil(heads / kv_heads / 8) is below 2^28.  Sums in an order fixed by the sizes and the device. */
 TGNN_API int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_host, const tgnn_cache* v_host, int64_t n, int heads,
                                 const int64_t* first, const int32_t* len, const float* bias, int num_buckets, const double* bounds,

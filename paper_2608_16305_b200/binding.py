@@ -67,8 +67,8 @@ _marshal = None
 
 
 def load_library():
-    """Loads the CUDA library and the marshalling module; raises if they have not been built."""
-    global _lib, _marshal
+    """Loads the CUDA library; raises if it has not been built."""
+    global _lib
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_16305_b200.build` "
@@ -140,15 +140,7 @@ def load_library():
         lib.tgnn_slot_attend_scratch.argtypes = [i64, i32, i32]
         lib.tgnn_slot_attend_scratch.restype = i64
         lib.tgnn_slot_attend_backward.argtypes = slot + [vp] * 8 + [i64]
-        try:
-            from . import _marshal as m
-        except ImportError as e:
-            raise RuntimeError(f"the marshalling module is missing or of another interpreter ({e}): build it with `python -m paper_2608_16305_b200.build`")
-        m.init((torch.int32, torch.int64, torch.float32, torch.float64, torch.bfloat16, torch.float16), torch._C._cuda_getDevice,
-               torch._C._cuda_getCurrentRawStream,
-               tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_sample_window, lib.tgnn_cache_write, lib.tgnn_cache_read, lib.tgnn_cached_attend,
-                                                           lib.tgnn_slot_attend, lib.tgnn_slot_attend_scratch, lib.tgnn_slot_attend_backward)))
-        _lib, _marshal = lib, m
+        _lib = lib
     return _lib
 
 
@@ -301,11 +293,27 @@ def unpack_rows(memory, last_update, nodes, packed, status) -> int:
 
 # ---- histories: sampling with sinks, row cache, attention over it, slot attention ----
 # Tensors are checked in csrc/marshal.c: type, device, contiguity and number of elements, TypeError otherwise.
+def _load_marshal():
+    """The marshalling module, with the entry points' addresses; raises if it has not been built."""
+    global _marshal
+    lib = load_library()
+    try:
+        from . import _marshal as m
+    except ImportError as e:
+        raise RuntimeError(f"the marshalling module is missing or of another interpreter ({e}): build it with "
+                           "`python -m paper_2608_16305_b200.build`") from e
+    m.init((torch.int32, torch.int64, torch.float32, torch.float64, torch.bfloat16, torch.float16), torch._C._cuda_getDevice,
+           torch._C._cuda_getCurrentRawStream,
+           tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_sample_window, lib.tgnn_cache_write, lib.tgnn_cache_read, lib.tgnn_cached_attend,
+                                                       lib.tgnn_slot_attend, lib.tgnn_slot_attend_scratch, lib.tgnn_slot_attend_backward)))
+    _marshal = m
+
+
 def _call(name: str, *args) -> int:
     """Calls an entry point through the marshalling module, on the current stream of its tensors' device; raises with the library's
     message."""
     if _marshal is None:
-        load_library()
+        _load_marshal()
     r = getattr(_marshal, name)(*args)
     if type(r) is int:                            # the tensors' device is not the current one
         with torch.cuda.device(r):

@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP >= 128 || 
   int64_t first = a.first[root];
   int len = a.len[root];
   seen.t = a.bias ? a.times[root] : 0.0;
-  if (first < 0 || len < 0 || first > a.rows - len) {
+  if (first < 0 || len < 0 || len > 0x7fffffff - 64 || first > a.rows - len) {   // (a tile's last index stays within int32)
     if (lane == 0) atomicMax(a.status, 4);
     first = len = 0;
   }

@@ -226,3 +226,76 @@ def test_calls_on_a_side_stream(H):
         got = h2.attend(q, nodes, times)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+def test_calls_that_overlap_on_two_streams(H):
+    """The same caches and inputs read by calls on two streams at once, each with outputs (and scratch) of its own."""
+    from paper_2608_16305_b200 import binding as B
+    cfg, s, indptr, nbr, eid, ts = _stream()
+    h = H.EventHistory(indptr, nbr, eid, ts, 2, 50, 300, 2, 4)
+    P, R, S = ts.numel(), 700, 40
+    g = torch.Generator(device="cuda").manual_seed(9)
+    mk = lambda *sh: torch.randn(*sh, generator=g, device="cuda")
+    h.append(torch.arange(P, device="cuda"), mk(P, 2, 50), mk(P, 2, 50))
+    nodes = torch.randint(0, cfg.num_nodes, (R,), generator=g, device="cuda", dtype=torch.int32)
+    times = torch.full((R,), 1e9, dtype=torch.float64, device="cuda")
+    bias = H.TimeBias.logarithmic(2, 16, 1.0, 3000.0)
+    bias.table.normal_(generator=g)
+    q, k, v, do = mk(R, 2, 50), mk(R, S, 2, 50), mk(R, S, 2, 50), mk(R, 2, 50)
+    cnt = torch.full((R,), S, dtype=torch.int32, device="cuda")
+    slot_ts = 1e9 - torch.cumsum(10 * torch.rand(R, S, generator=g, device="cuda", dtype=torch.float64), 1)
+
+    def run():
+        out = h.attend(q, nodes, times, bias)
+        grads = [torch.empty_like(t) for t in (q, k, v, bias.table)]
+        scratch = torch.empty(B.slot_attend_scratch(R, 2, 16), device="cuda")
+        B.slot_attend_backward(q, k, v, cnt, do, *grads[:3], bias=bias.table, bounds=bias.bounds, times=times, ts=slot_ts, dbias=grads[3],
+                               scratch=scratch)
+        return [out] + grads + [scratch]
+    want = run()[:5]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in range(2)], []
+    for _ in range(10):
+        for st in streams:
+            with torch.cuda.stream(st):
+                got.append(run())
+    torch.cuda.synchronize()
+    for res in got:
+        for a, b in zip(res, want):
+            assert torch.equal(a, b)
+
+
+def test_empty_batches_and_histories(H):
+    cfg, s, indptr, nbr, eid, ts = _stream(400)
+    h = H.EventHistory(indptr, nbr, eid, ts, 2, 50, 10, 2, 8)
+    e = lambda *sh, **kw: torch.empty(*sh, device="cuda", **kw)
+    assert h.attend(e(0, 2, 50), e(0, dtype=torch.int32), e(0, dtype=torch.float64)).shape == (0, 2, 50)
+    assert h.slots(e(0, dtype=torch.int32), e(0, dtype=torch.float64)).nbr.shape == (0, 12)
+    h.append(e(0, dtype=torch.int64), e(0, 2, 50), e(0, 2, 50))
+    # a graph without entries, and one without nodes
+    for ptr in (torch.zeros(6, dtype=torch.int64, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")):
+        none = H.EventHistory(ptr, e(0, dtype=torch.int32), e(0, dtype=torch.int32), e(0, dtype=torch.float64), 2, 50, 10, 2, 4)
+        nodes, times = torch.arange(3, dtype=torch.int32, device="cuda"), torch.ones(3, dtype=torch.float64, device="cuda")
+        bias = H.TimeBias.logarithmic(2, 4, 1.0, 9.0)
+        assert not none.attend(torch.ones(3, 2, 50, device="cuda"), nodes, times, bias).any()
+        assert none.slots(nodes, times).cnt.tolist() == [0, 0, 0] and none.status() == (0 if ptr.numel() > 1 else 4)
+    assert h.status() == 0
+
+
+def test_one_source_for_several_places_and_roots_that_share_a_history(H):
+    from paper_2608_16305_b200 import binding as B
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    x = torch.randn(5, 2, 50, device="cuda")
+    k, v = B.RowCache(40, 2, 50, 8), B.RowCache(40, 2, 50, 8)
+    src = torch.tensor([3, 3, 3, 1] * 10, device="cuda")
+    B.cache_write(k, x, st, src=src)
+    B.cache_write(v, x, st, src=src)
+    assert torch.equal(k.codes[0], k.codes[1]) and torch.equal(k.codes[0], k.codes[36])
+    q = torch.randn(1, 2, 50, device="cuda").expand(64, 2, 50).contiguous()
+    first, length = torch.full((64,), 4, dtype=torch.int64, device="cuda"), torch.full((64,), 33, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    B.cached_attend(q, k, v, first, length, 20, 3, out, st)
+    assert torch.equal(out, out[:1].expand_as(out)) and int(st.item()) == 0
+    rows = torch.empty(6, 100, device="cuda")
+    B.cache_read(k, rows, st, src=torch.tensor([0, 0, 4, 4, 3, 3], device="cuda"))
+    assert torch.equal(rows[0], rows[1]) and torch.equal(rows[0], rows[2]) and torch.equal(rows[4], rows[5])
