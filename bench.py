@@ -450,7 +450,8 @@ def run_partitioned(args, rank, world, device):
     owner = (np.arange(cfg.num_nodes, dtype=np.int64) * 2654435761 % 2 ** 32 % world).astype(np.int32)
     t0 = time.time()
     dw = T.PartitionedWorkload(stream, owner, world, rank, K_sync, device=device, efeat=efeat, keep_sync=True)
-    refresh = D.BoundaryRefresh(dw.refresh_plan(), cfg.d)
+    refresh = D.BoundaryRefresh(dw.refresh_plan(), cfg.d) if args.refresh_bits == 32 else \
+        D.QuantisedRefresh(dw.refresh_plan(), cfg.d, args.refresh_bits)
     torch.cuda.synchronize()
     prep_s = time.time() - t0
     weights = wl.make_weights(cfg.d, cfg.d_e, cfg.seed, model=args.model)
@@ -506,7 +507,7 @@ def run_partitioned(args, rank, world, device):
         "config": {"workload": f"{cfg.name}: {cfg.num_nodes} nodes, {cfg.num_events} events, batch {cfg.batch} (global), "
                                f"{world}-way hashed node partition, source-owned targets, K = {K_sync}",
                    "parallelism": f"{world} partitioned worker(s): scanned mixed batches, boundary refresh (all-to-all of "
-                                  "packed rows), gradient all-reduce, adaptive controller",
+                                  f"packed rows in {args.refresh_bits} bits), gradient all-reduce, adaptive controller",
                    "math_mode": args.math, "l2": "512 MB buffer written between timed steps",
                    "inputs": "resident in HBM", "preprocess_s": round(prep_s, 3)},
         "e2e": None, "gpu_launches": int(launches), "clocks": clk.summary(),
@@ -776,6 +777,8 @@ def main():
     ap.add_argument("--partitioned", action="store_true",
                     help="run the multi-worker form instead of independent replicas: one node-partitioned worker per "
                          "GPU with boundary refresh and gradient all-reduce (strong scaling over the same stream)")
+    ap.add_argument("--refresh-bits", type=int, default=32, choices=[32, 8, 4],
+                    help="with --partitioned: bits of a value in the boundary refresh's rows on the wire")
     ap.add_argument("--flush", default="auto", choices=["auto", "on", "off"],
                     help="write a 512 MB buffer between timed steps; auto: only for workloads whose own step does not already "
                          "stream several times the L2 size")

@@ -299,3 +299,45 @@ def test_one_source_for_several_places_and_roots_that_share_a_history(H):
     rows = torch.empty(6, 100, device="cuda")
     B.cache_read(k, rows, st, src=torch.tensor([0, 0, 4, 4, 3, 3], device="cuda"))
     assert torch.equal(rows[0], rows[1]) and torch.equal(rows[0], rows[2]) and torch.equal(rows[4], rows[5])
+
+
+def test_quantised_refresh_over_a_one_rank_communicator():
+    """The all-to-all of records on a real NCCL communicator (one rank: rows sent to itself) between the cache's kernels."""
+    import os
+    import socket
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = r"""
+import os, sys, numpy as np, torch, torch.distributed as dist
+sys.path.insert(0, %r)
+from oracle import history as oh
+from paper_2608_16305_b200 import distributed as D
+torch.cuda.set_device(0)
+dist.init_process_group("nccl", rank=0, world_size=1, init_method="tcp://127.0.0.1:" + os.environ["PORT"],
+                        device_id=torch.device("cuda", 0))
+N, n = 5000, 1200
+rng = np.random.default_rng(0)
+perm = rng.permutation(N)
+src, dst = perm[:n].astype(np.int32), perm[n:2 * n].astype(np.int32)
+for d, bits in ((100, 8), (100, 4), (344, 4)):
+    mem_h, lu_h = rng.standard_normal((N, d)).astype(np.float32), rng.random(N) * 1e5
+    mem, lu = torch.from_numpy(mem_h).cuda(), torch.from_numpy(lu_h).cuda()
+    plan = D.RefreshPlan.from_lists(torch.from_numpy(dst[None]).cuda(), np.array([[0, n]]), torch.from_numpy(src[None]).cuda(),
+                                    np.array([[0, n]]), 1, 0)
+    ref = D.QuantisedRefresh(plan, d, bits)
+    ref.run(0, mem, lu)
+    want, t = mem_h.copy(), lu_h.copy()
+    want[dst] = oh.dequantise(*oh.quantise(mem_h[src].reshape(n, ref.send.heads, -1), bits)).reshape(n, d)
+    t[dst] = lu_h[src]
+    assert int(ref.status.item()) == 0 and ref.rows_sent == n and ref.rows_received == n
+    assert np.array_equal(mem.cpu().numpy(), want) and np.array_equal(lu.cpu().numpy(), t)
+dist.destroy_process_group()
+print("ok")
+""" % root
+    sock = socket.socket()
+    sock.bind(("127.0.0.1", 0))
+    port = sock.getsockname()[1]
+    sock.close()
+    p = subprocess.run([sys.executable, "-c", code], env=dict(os.environ, PORT=str(port), NCCL_NVLS_ENABLE="0"), capture_output=True, timeout=240)
+    assert p.returncode == 0 and b"ok" in p.stdout, p.stderr.decode()[-3000:]
