@@ -262,3 +262,28 @@ def test_slots_scratch_is_not_written_beyond_its_size(B, R, H, KV, D, buckets):
     assert (buf[n:] == 5).all()
     for a, b in zip(g, c.backward()):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("S,H,KV,D", [(40, 2, 2, 16), (33, 8, 2, 16), (7, 1, 1, 16), (128, 4, 4, 32)])
+def test_slots_bias_gradient_sums_to_zero_over_the_buckets(B, dt, S, H, KV, D):
+    """A root's dz sum to 0, so a head's gradients of all buckets do.  Here dp is near 1000 and differs by a fraction, so that a delta rounded
+    to fp32 shows on every slot with one sign (U 1000 a root).  Allowed are the roundings of each dz (its weight, two differences, a
+    product) and five of a scan: 9 U sum |dz|, and those of the results."""
+    R = 64
+    c = Case(B, R, S, H, KV, D, dt, buckets=5, seed=S)
+    c.do.fill_(1.0)
+    c.v.normal_(generator=torch.Generator("cuda").manual_seed(S)).mul_(1.0 / 16).add_(1000.0 / D)
+    q, do, k, v = (t.double().cpu().numpy() for t in (c.q, c.do, c.k, c.v))
+    cnt, G = c.cnt.cpu().numpy(), H // KV
+    bias = c.b["bias"].double().cpu().numpy()
+    bk = np.searchsorted(c.b["bounds"].cpu().numpy(), (c.b["times"][:, None] - c.b["ts"]).cpu().numpy(), side="right")
+    z = D ** -0.5 * np.einsum("rkgd,rskd->rkgs", q.reshape(R, KV, G, D), k) + bias[:, bk].reshape(KV, G, R, S).transpose(2, 0, 1, 3)
+    z = np.where((np.arange(S)[None] < cnt[:, None])[:, None, None], z, -1e30)
+    p = np.exp(z - z.max(-1, keepdims=True)) * (z > -1e29)
+    p /= np.maximum(p.sum(-1, keepdims=True), 1e-300)
+    dp = np.einsum("rkgd,rskd->rkgs", do.reshape(R, KV, G, D), v)
+    dz = p * (np.abs(dp - (p * dp).sum(-1, keepdims=True)) + 2 * (D + 2) * U * np.abs(dp))
+    tol = 9 * U * dz.sum((0, 3)).reshape(H)
+    db = c.backward()[3].double().cpu().numpy()
+    assert (np.abs(db.sum(1)) <= tol + U * np.abs(db).sum(1)).all(), (db.sum(1), tol)
