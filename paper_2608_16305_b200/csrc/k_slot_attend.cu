@@ -152,9 +152,20 @@ struct Reduced {
   }
 };
 
+// Query heads of a cached head that a warp takes together: 4, 2 or 1, whatever divides their number.  One after another they read and
+// unpacked a root's rows again for each (6000 roots of 40 slots, 2 x 4 heads of 64, bf16: 76 us forward and 154 us backward; 55 and 106 us
+// by fours; 2 x 2 heads of 64 in fp32: 68 and 158 us; 49 and 116 us by twos).
+__host__ __device__ inline int heads_at_once(int group) { return (group & 3) == 0 ? 4 : (group & 1) == 0 ? 2 : 1; }
+
 // Segments of k and of v in flight per lane: 64 bytes of each, 2 segments at least and 4 at most.
 template <typename S>
 constexpr int kDeep = sizeof(S) >= 32 ? 2 : 4;
+// With four query heads at a time their registers leave room for two.
+template <typename S, int GT>
+constexpr int kDeepOf = GT >= 4 ? 2 : kDeep<S>;
+// Blocks per SM of the backward pass: four heads' q and do take 64 registers.
+template <int GT>
+constexpr int kBlocks = GT >= 4 ? 3 : 4;
 
 // Which segments a lane takes: 32 / P of them at a time, KC neighbouring cached heads of RPI neighbouring slots.
 template <int P>
@@ -299,10 +310,161 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
   }
 }
 
-template <typename T, int VB, int P, int NV>
-__global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const SlotArgs a) {
+// The same for query heads that share a cached head, GT of them at a time: k and v are loaded and unpacked once for them.  The sums of
+// UN slots and GT heads end on different lanes (value g * UN + u on the lane, or the lanes, that Reduced gives it), and each lane weighs its
+// own, instead of P lanes all of them; weights and corrections then go back to the segment.
+template <typename T, int VB, int P, int NV, int GT>
+__global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_group_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
-  constexpr int UN = kDeep<S>;
+  constexpr int UN = kDeepOf<S, GT>, N = GT * UN;
+  constexpr int C = N > P ? N / P : 1, SP = P > N ? P / N : 1;  // values per lane, lanes per value
+  static_assert(C <= UN, "a lane's values belong to one head");
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ double s_bounds[kMaxBuckets + 1];
+  const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+  uint8_t* bucket = smem + (size_t)wid * a.warp_bytes;
+  if (a.bias) {
+    stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
+    __syncthreads();
+  }
+  const Lanes<P> me(lane, a.kv_heads);
+  const Reduced<P, N> sums(lane);
+  const int my_g = sums.id / UN, my_u = sums.id % UN, base_lane = lane & ~(P - 1);
+  const int D = a.dim, ROW = a.kv_heads * D;
+  const int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  if (r >= a.n) return;
+  const int cnt = min(max(a.cnt[r], 0), a.slots);
+  const bool several = cnt > a.chunk;                          // chunks are multiples of UN * RPI slots
+  bool filled = several;
+  const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
+  const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
+  for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
+    const int kv = kv0 + me.kc;
+    for (int g0 = 0; g0 < a.group; g0 += GT) {
+      const int h0 = kv * a.group + g0;
+      const T* kp = kr + (int64_t)me.row * ROW + kv * D;
+      const T* vp = vr + (int64_t)me.row * ROW + kv * D;
+      S k[UN], v[UN];
+#pragma unroll
+      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      float q[GT][S::N], acc[GT][S::N];
+      {
+        S raw[GT];
+#pragma unroll
+        for (int g = 0; g < GT; ++g) raw[g].load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h0 + g) * D, me.part, D, true);
+#pragma unroll
+        for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+        if (!filled) {
+          fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
+          __syncwarp();
+          filled = true;
+        }
+#pragma unroll
+        for (int g = 0; g < GT; ++g) {
+          raw[g].floats(q[g]);
+#pragma unroll
+          for (int j = 0; j < S::N; ++j) acc[g][j] = 0.f;
+        }
+      }
+      const float* bias = a.bias ? a.bias + (h0 + my_g) * a.buckets : nullptr;
+      float m = -INFINITY, l = 0.f;                            // of the lane's head; l over the lane's slots
+      for (int c0 = 0; c0 < cnt; c0 += a.chunk) {
+        const int c1 = min(cnt, c0 + a.chunk);
+        if (several) {
+          __syncwarp();
+          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
+          __syncwarp();
+        }
+        for (int s0 = c0 + me.row; s0 - me.row < c1; s0 += UN * me.RPI) {
+          float z[N];
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+#pragma unroll
+            for (int g = 0; g < GT; ++g) z[g * UN + u] = 0.f;
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) {
+              const float x = k[u].at(j);
+#pragma unroll
+              for (int g = 0; g < GT; ++g) z[g * UN + u] = fmaf(x, q[g][j], z[g * UN + u]);
+            }
+          }
+          const int next = s0 + UN * me.RPI;
+          kp += UN * me.RPI * ROW;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
+          Reduced<P, N>::run(z, lane);
+          float top = m;
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            const int s = s0 + (my_u + i) * me.RPI;
+            z[i] *= a.scale;
+            if (bias && s < c1) z[i] += __ldg(bias + bucket[s - c0]);
+            if (s >= c1) z[i] = -INFINITY;
+            top = fmaxf(top, z[i]);
+          }
+#pragma unroll
+          for (int o = SP; o < SP * (UN / C); o <<= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+          const float base = top == -INFINITY ? 0.f : top;     // nothing but -infinity: weights are 0
+          const float corr = exp2_fast((m - base) * kLog2e);   // m = -infinity: 0
+          m = top;
+          l *= corr;
+          float p[C];
+#pragma unroll
+          for (int i = 0; i < C; ++i) {
+            p[i] = exp2_fast((z[i] - base) * kLog2e);
+            l += p[i];
+          }
+#pragma unroll
+          for (int g = 0; g < GT; ++g) {
+            const float f = __shfl_sync(FULL, corr, base_lane | (g * UN / C * SP));
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) acc[g][j] *= f;
+          }
+#pragma unroll
+          for (int u = 0; u < UN; ++u) {
+            float w[GT];
+#pragma unroll
+            for (int g = 0; g < GT; ++g) w[g] = __shfl_sync(FULL, p[(g * UN + u) % C], base_lane | ((g * UN + u) / C * SP));
+#pragma unroll
+            for (int j = 0; j < S::N; ++j) {
+              const float x = v[u].at(j);
+#pragma unroll
+              for (int g = 0; g < GT; ++g) acc[g][j] = fmaf(w[g], x, acc[g][j]);
+            }
+          }
+          vp += UN * me.RPI * ROW;
+#pragma unroll
+          for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
+        }
+      }
+#pragma unroll
+      for (int o = SP; o < SP * (UN / C); o <<= 1) l += __shfl_xor_sync(FULL, l, o);
+      // the groups of lanes that shared a head's slots
+#pragma unroll
+      for (int g = 0; g < GT; ++g) {
+        float gm = __shfl_sync(FULL, m, base_lane | (g * UN / C * SP)), gl = __shfl_sync(FULL, l, base_lane | (g * UN / C * SP));
+        for (int o = P * me.KC; o < 32; o <<= 1) {
+          const float om = __shfl_xor_sync(FULL, gm, o), top = fmaxf(gm, om);
+          const float base = top == -INFINITY ? 0.f : top;
+          const float f = exp2_fast((gm - base) * kLog2e), of = exp2_fast((om - base) * kLog2e);
+          gm = top;
+          gl = gl * f + __shfl_xor_sync(FULL, gl, o) * of;
+#pragma unroll
+          for (int j = 0; j < S::N; ++j) acc[g][j] = acc[g][j] * f + __shfl_xor_sync(FULL, acc[g][j], o) * of;
+        }
+        const float f = gl == 0.f ? 0.f : 1.f / gl;
+#pragma unroll
+        for (int j = 0; j < S::N; ++j) acc[g][j] *= f;
+        if (me.row == 0) S::store(reinterpret_cast<T*>(a.out) + (r * a.heads + h0 + g) * D, me.part, D, acc[g]);
+      }
+    }
+  }
+}
+
+template <typename T, int VB, int P, int NV, int GT>
+__global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_kernel(const SlotArgs a) {
+  using S = Seg<T, VB, P, NV>;
+  constexpr int UN = kDeepOf<S, GT>, N = 2 * GT * UN;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -322,7 +484,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
   }
   __syncthreads();
   const Lanes<P> me(lane, a.kv_heads);
-  const Reduced<P, 2 * UN> sums(lane);
+  const Reduced<P, N> sums(lane);
   const int h_first = lane % H, h_step = 32 % H;               // head of entry lane + 32 i of a [slot][head] array, by steps
   const int64_t stride = (int64_t)gridDim.x * a.warps;
   auto count = [&](int64_t r) { return r < a.n ? min(max(a.cnt[r], 0), a.slots) : 0; };
@@ -352,35 +514,45 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
         // logits and dp of the chunk
         for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
           const int kv = kv0 + me.kc;
-          for (int g = 0; g < a.group; ++g) {
-            const int h = kv * a.group + g;
+          for (int g0 = 0; g0 < a.group; g0 += GT) {
+            const int h0 = kv * a.group + g0;
             const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
             const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
-            S k[UN], v[UN], raw, raw2;
+            S k[UN], v[UN], raw[GT], raw2[GT];
 #pragma unroll
             for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
 #pragma unroll
             for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
-            raw.load(qr + h * D, me.part, D, true);
-            raw2.load(gr + h * D, me.part, D, true);
+#pragma unroll
+            for (int g = 0; g < GT; ++g) {
+              raw[g].load(qr + (h0 + g) * D, me.part, D, true);
+              raw2[g].load(gr + (h0 + g) * D, me.part, D, true);
+            }
             if (!filled) {
               fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane);
               __syncwarp();
               filled = true;
             }
-            float q[S::N], go[S::N];
-            raw.floats(q);
-            raw2.floats(go);
-            const float* bias = a.bias ? a.bias + h * a.buckets : nullptr;
+            float q[GT][S::N], go[GT][S::N];
+#pragma unroll
+            for (int g = 0; g < GT; ++g) {
+              raw[g].floats(q[g]);
+              raw2[g].floats(go[g]);
+            }
             for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
-              float x[2 * UN];                                 // q . k of the four slots, then do . v
+              float x[N];                                      // q . k of the heads' slots, then do . v
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
-                x[u] = x[UN + u] = 0.f;
+#pragma unroll
+                for (int g = 0; g < GT; ++g) x[g * UN + u] = x[(GT + g) * UN + u] = 0.f;
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) {
-                  x[u] = fmaf(k[u].at(j), q[j], x[u]);
-                  x[UN + u] = fmaf(v[u].at(j), go[j], x[UN + u]);
+                  const float xk = k[u].at(j), xv = v[u].at(j);
+#pragma unroll
+                  for (int g = 0; g < GT; ++g) {
+                    x[g * UN + u] = fmaf(xk, q[g][j], x[g * UN + u]);
+                    x[(GT + g) * UN + u] = fmaf(xv, go[g][j], x[(GT + g) * UN + u]);
+                  }
                 }
               }
               // the next slots' rows come while these sums are put together
@@ -391,15 +563,15 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
               for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
 #pragma unroll
               for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
-              Reduced<P, 2 * UN>::run(x, lane);
+              Reduced<P, N>::run(x, lane);
               if (sums.first) {
 #pragma unroll
-                for (int i = 0; i < (2 * UN > P ? 2 * UN / P : 1); ++i) {
-                  const int s = s0 + ((sums.id + i) & (UN - 1)) * me.RPI;
+                for (int i = 0; i < (N > P ? N / P : 1); ++i) {
+                  const int s = s0 + ((sums.id + i) & (UN - 1)) * me.RPI, h = h0 + (sums.id + i) / UN % GT;
                   if (s < ns) {
-                    if (sums.id + i < UN) {
+                    if (sums.id + i < GT * UN) {
                       float y = x[i] * a.scale;
-                      if (bias) y += __ldg(bias + bucket[s]);
+                      if (a.bias) y += __ldg(a.bias + h * a.buckets + bucket[s]);
                       zd[s * H + h].x = y;
                     } else {
                       zd[s * H + h].y = x[i];
@@ -501,13 +673,16 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
         const bool final_chunk = c0 + a.chunk >= cnt;
         for (int kv0 = 0; kv0 < a.kv_heads; kv0 += me.KC) {
           const int kv = kv0 + me.kc;
-          for (int g = 0; g < a.group; ++g) {
-            const int h = kv * a.group + g;
-            float acc[S::N];
+          for (int g0 = 0; g0 < a.group; g0 += GT) {
+            const int h0 = kv * a.group + g0;
+            float acc[GT][S::N];
 #pragma unroll
-            for (int j = 0; j < S::N; ++j) acc[j] = 0.f;
+            for (int g = 0; g < GT; ++g) {
+#pragma unroll
+              for (int j = 0; j < S::N; ++j) acc[g][j] = 0.f;
+            }
             const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
-            const float2* wz = zd + me.row * H + h;
+            const float2* wz = zd + me.row * H + h0;
             S k[UN];
 #pragma unroll
             for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
@@ -516,56 +691,74 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_backward_kernel(const 
               kp += UN * me.RPI * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
-                const float w = s0 + u * me.RPI < ns ? wz[u * me.RPI * H].y : 0.f;
+                float w[GT];
 #pragma unroll
-                for (int j = 0; j < S::N; ++j) acc[j] = fmaf(w, k[u].at(j), acc[j]);
+                for (int g = 0; g < GT; ++g) w[g] = s0 + u * me.RPI < ns ? wz[u * me.RPI * H + g].y : 0.f;
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) {
+                  const float x = k[u].at(j);
+#pragma unroll
+                  for (int g = 0; g < GT; ++g) acc[g][j] = fmaf(w[g], x, acc[g][j]);
+                }
                 k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
               }
               wz += UN * me.RPI * H;
             }
-            for (int o = P * me.KC; o < 32; o <<= 1) {
 #pragma unroll
-              for (int j = 0; j < S::N; ++j) acc[j] += __shfl_xor_sync(FULL, acc[j], o);
-            }
-            if (several && me.row == 0) {                      // carried from chunk to chunk
+            for (int g = 0; g < GT; ++g) {
+              for (int o = P * me.KC; o < 32; o <<= 1) {
 #pragma unroll
-              for (int j = 0; j < S::N; ++j) {
-                const int e = ((j / S::VE) * P + me.part) * S::VE + j % S::VE;
-                if (e < D) {
-                  if (c0 > 0) acc[j] += s_dq[h * D + e];
-                  if (!final_chunk) s_dq[h * D + e] = acc[j];
+                for (int j = 0; j < S::N; ++j) acc[g][j] += __shfl_xor_sync(FULL, acc[g][j], o);
+              }
+              if (several && me.row == 0) {                    // carried from chunk to chunk
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) {
+                  const int e = ((j / S::VE) * P + me.part) * S::VE + j % S::VE;
+                  if (e < D) {
+                    if (c0 > 0) acc[g][j] += s_dq[(h0 + g) * D + e];
+                    if (!final_chunk) s_dq[(h0 + g) * D + e] = acc[g][j];
+                  }
                 }
               }
-            }
-            if (final_chunk && me.row == 0) {
+              if (final_chunk && me.row == 0) {
 #pragma unroll
-              for (int j = 0; j < S::N; ++j) acc[j] *= a.scale;
-              S::store(dqr + h * D, me.part, D, acc);
+                for (int j = 0; j < S::N; ++j) acc[g][j] *= a.scale;
+                S::store(dqr + (h0 + g) * D, me.part, D, acc[g]);
+              }
             }
           }
           T* dkp = dkr + (int64_t)(c0 + me.row) * ROW + kv * D;
           T* dvp = dvr + (int64_t)(c0 + me.row) * ROW + kv * D;
           int s = me.row;
-          if (a.group == 1) {
-            float q[S::N], go[S::N];
+          if (a.group == GT) {
+            float q[GT][S::N], go[GT][S::N];
             {
-              S raw;
-              raw.load(qr + kv * D, me.part, D, true);
-              raw.floats(q);
-              raw.load(gr + kv * D, me.part, D, true);
-              raw.floats(go);
-            }
+              S raw[GT], raw2[GT];
 #pragma unroll
-            for (int j = 0; j < S::N; ++j) q[j] *= a.scale;
-            const float2* at = zd + s * H + kv;
+              for (int g = 0; g < GT; ++g) {
+                raw[g].load(qr + (kv * GT + g) * D, me.part, D, true);
+                raw2[g].load(gr + (kv * GT + g) * D, me.part, D, true);
+              }
+#pragma unroll
+              for (int g = 0; g < GT; ++g) {
+                raw[g].floats(q[g]);
+                raw2[g].floats(go[g]);
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) q[g][j] *= a.scale;
+              }
+            }
+            const float2* at = zd + s * H + kv * GT;
 #pragma unroll 2
             for (; s < ns; s += me.RPI) {
               float xk[S::N], xv[S::N];
-              const float p = at->x, y = at->y;
 #pragma unroll
-              for (int j = 0; j < S::N; ++j) {
-                xk[j] = y * q[j];
-                xv[j] = p * go[j];
+              for (int g = 0; g < GT; ++g) {
+                const float p = at[g].x, y = at[g].y;
+#pragma unroll
+                for (int j = 0; j < S::N; ++j) {
+                  xk[j] = g == 0 ? y * q[g][j] : fmaf(y, q[g][j], xk[j]);
+                  xv[j] = g == 0 ? p * go[g][j] : fmaf(p, go[g][j], xv[j]);
+                }
               }
               S::store(dkp, me.part, D, xk);
               S::store(dvp, me.part, D, xv);
@@ -637,9 +830,19 @@ __global__ void __launch_bounds__(256) bias_sum_kernel(const double* __restrict_
   if (lane == 0) dbias[i] = (float)sum;
 }
 
+template <bool BACKWARD, typename T, int VB, int P, int NV, int GT>
+auto kernel_of() {
+  if constexpr (BACKWARD) return slot_backward_kernel<T, VB, P, NV, GT>;
+  else if constexpr (GT > 1) return slot_forward_group_kernel<T, VB, P, NV, GT>;
+  else return slot_forward_kernel<T, VB, P, NV>;
+}
+
 template <bool BACKWARD, typename T, int VB, int P, int NV>
 cudaError_t launch_kernel(const SlotArgs& a, int blocks, cudaStream_t s) {
-  const auto kernel = BACKWARD ? slot_backward_kernel<T, VB, P, NV> : slot_forward_kernel<T, VB, P, NV>;
+  const int gt = heads_at_once(a.group);
+  const auto kernel = gt == 4   ? kernel_of<BACKWARD, T, VB, P, NV, 4>()
+                      : gt == 2 ? kernel_of<BACKWARD, T, VB, P, NV, 2>()
+                                : kernel_of<BACKWARD, T, VB, P, NV, 1>();
   const int bytes = a.warps * a.warp_bytes;
   if (bytes > 46 * 1024) {          // more than a kernel has without asking for it (per device; asking again costs little)
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -693,7 +896,8 @@ int grid_of(const SlotArgs& a, bool backward) {
   if (!backward) return (int)want;
   int resident = (int)((220 * 1024) / ((int64_t)a.warps * a.warp_bytes + 2048));
   if (resident < 1) resident = 1;
-  if (resident > 16 / a.warps) resident = 16 / a.warps;
+  const int warps = 4 * (heads_at_once(a.group) == 4 ? kBlocks<4> : kBlocks<1>);
+  if (resident > warps / a.warps) resident = warps / a.warps;
   int64_t most = (int64_t)num_sms() * resident;
   if (most > MAX_BLOCKS) most = MAX_BLOCKS;
   return (int)(want < most ? want : most);
