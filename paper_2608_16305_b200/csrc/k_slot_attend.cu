@@ -10,9 +10,9 @@
 // (backward), so both passes are bound by HBM: k and v in, and for the backward pass dk and dv out.  Tensor cores have nothing to
 // gain on one query per row.  The backward pass recomputes the weights and needs nothing of the forward pass.
 //
-// A warp takes a root.  The values of one (slot, cached head) lie side by side; P lanes hold such a segment, NV words of VB bytes each,
-// 8 values in all where there are as many, so that a warp loads 32 / P segments at once straight into registers, two to four deep for k and v.  A dot product is then VB / size
-// multiplications and log2(P) shuffles.  Forward, every group of P lanes runs a softmax of its own over its slots (maximum, sum and
+// A warp takes a root, or a block's warps one together where roots are few.  The values of one (slot, cached head) lie side by side; P lanes
+// hold such a segment, NV words of VB bytes each, 8 values in all where there are as many, so that a warp loads 32 / P segments at once
+// straight into registers, two to four deep for k and v.  A dot product is then VB / size multiplications and log2(P) shuffles.  Forward, every group of P lanes runs a softmax of its own over its slots (maximum, sum and
 // output in registers; the groups of a head are merged at the end), so nothing is written between k and the output.  Backward,
 // logits and dp go to shared memory for the root's slots, weights and dz are formed there, and a second walk over k (which lies
 // in L1 or L2 by then) sums dq while dk and dv are written.  Roots with more slots than a warp's shared memory holds are taken in
@@ -21,8 +21,8 @@
 // warp keeps a table of its own and a second kernel adds the blocks' tables in a fixed order, so no atomics decide on a result.
 // Logits stay in natural units: a bias of the type's lowest value is then still finite.
 //
-// Measured on a B200, 14 400 roots of 64 slots, 4 heads of 32 in bf16: forward 91 us at 5.1 TB/s, backward 198 us at 4.9 TB/s of DRAM (a copy
-// reaches 6.5); 1800 roots of 20 slots, 2 heads of 50 in fp32: 12 and 20 us, a single wave of 12 warps per SM, bound by the latency of a
+// Measured on a B200, 14 400 roots of 64 slots, 4 heads of 32 in bf16: forward 89 us at 5.3 TB/s, backward 198 us at 4.9 TB/s of DRAM (a copy
+// reaches 6.5); 1800 roots of 20 slots, 2 heads of 50 in fp32: 10 and 20 us, a single wave of 12 warps per SM, bound by the latency of a
 // root's chain of loads and sums.
 #include "tgnn_history.cuh"
 
@@ -45,25 +45,28 @@ struct SlotArgs {
   int buckets;
   int chunk;                             // slots of a chunk
   int warps;
-  int warp_bytes;                        // shared memory of a warp
+  int team;                              // warps that share a root: 1, or all of a block
+  int warp_bytes;                        // shared memory of a warp, or of a block that shares a root
   float scale;
 };
 
-// A warp's shared memory, all parts multiples of 16 bytes: bucket [chunk] (bytes); backward: z and dp [chunk * H] in pairs, per head m,
+// Shared memory of a warp, or of a block that shares a root, all parts multiples of 16 bytes: bucket [chunk] (bytes); backward: z and dp [chunk * H] in pairs, per head m,
 // 1 / l and delta, dq [H * dim] and the running l and delta in fp64 where there are several chunks, and with a bias the table
-// [H * buckets] in fp64.
+// [H * buckets] in fp64 for every warp; where warps share a root, what they put together: outputs or dq of the heads in hand, and forward m and l.
+constexpr int RED = 256;                   // values of the heads that a warp has in hand, per query head of a cached head: 32 lanes of 8
 struct Layout {
-  int z, head, dq, sums, table, total;
+  int z, head, dq, sums, table, red, total;
 };
 __host__ __device__ inline int up16(int x) { return (x + 15) & ~15; }
-__host__ __device__ inline Layout layout(int heads, int dim, int chunk, bool several, bool backward, int table) {
+__host__ __device__ inline Layout layout(int heads, int dim, int chunk, bool several, bool backward, int table, int team, int together) {
   Layout l;
   int at = up16(chunk);
   l.z = at; at += backward ? up16(heads * chunk * 8) : 0;
   l.head = at; at += backward ? up16(heads * 16) : 0;
   l.dq = at; at += backward && several ? up16(heads * dim * 4) : 0;
   l.sums = at; at += backward && several ? heads * 16 : 0;
-  l.table = at; at += up16(table * 8);
+  l.table = at; at += up16(table * team * 8);
+  l.red = at; at += team > 1 ? team * together * (RED + 16) * 4 : 0;
   l.total = at;
   return l;
 }
@@ -181,10 +184,48 @@ struct Lanes {
   }
 };
 
-__device__ __forceinline__ void fill_buckets(const SlotArgs& a, const double* s_bounds, uint8_t* bucket, int64_t r, int s0, int s1, int lane) {
+__device__ __forceinline__ void fill_buckets(const SlotArgs& a, const double* s_bounds, uint8_t* bucket, int64_t r, int s0, int s1, int first, int step) {
   if (!a.bias) return;
   const double t = a.times[r];
-  for (int s = s0 + lane; s < s1; s += 32) bucket[s - s0] = (uint8_t)bucket_of(s_bounds, a.buckets - 1, t - __ldg(a.ts + r * a.slots + s));
+  for (int s = s0 + first; s < s1; s += step) bucket[s - s0] = (uint8_t)bucket_of(s_bounds, a.buckets - 1, t - __ldg(a.ts + r * a.slots + s));
+}
+
+// Of warps that share a root, or of one that has it alone.
+__device__ __forceinline__ void sync_team(int team) {
+  if (team > 1) __syncthreads();
+  else __syncwarp();
+}
+
+// A lane's values of one head in hand, to row e of the block's.
+template <typename S, int P>
+__device__ __forceinline__ void put_team(float* red, int e, int dim, int part, const float (&x)[S::N]) {
+#pragma unroll
+  for (int j = 0; j < S::N; ++j) {
+    const int d = ((j / S::VE) * P + part) * S::VE + j % S::VE;
+    if (d < dim) red[e * dim + d] = x[j];
+  }
+}
+
+// The outputs of the warps that share a root put together: per warp and head in hand m, l and acc (not divided by l).  All
+// threads of the block.
+template <typename T>
+__device__ __forceinline__ void merge_team(const SlotArgs& a, const float* red, int heads_in_hand, int together, int64_t r, int kv0, int g0) {
+  const int D = a.dim, size = heads_in_hand * D;
+  const float2* ml = reinterpret_cast<const float2*>(red + a.team * together * RED);
+  for (int i = threadIdx.x; i < size; i += blockDim.x) {
+    const int e = i / D, d = i - e * D;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+    for (int w = 0; w < a.team; ++w) m = fmaxf(m, ml[w * heads_in_hand + e].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int w = 0; w < a.team; ++w) {
+      const float2 at = ml[w * heads_in_hand + e];
+      const float f = exp2_fast((at.x - base) * kLog2e);
+      l = fmaf(at.y, f, l);
+      o = fmaf(red[w * size + i], f, o);
+    }
+    const int h = (kv0 + e / together) * a.group + g0 + e % together;
+    reinterpret_cast<T*>(a.out)[(r * a.heads + h) * D + d] = from_float<T>(l == 0.f ? 0.f : o / l);
+  }
 }
 
 template <typename T, int VB, int P, int NV>
@@ -194,17 +235,19 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  uint8_t* bucket = smem + (size_t)wid * a.warp_bytes;
+  const int team = a.team, sub = team > 1 ? wid : 0;
+  uint8_t* bucket = smem + (team > 1 ? 0 : (size_t)wid * a.warp_bytes);
   if (a.bias) {
     stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
     __syncthreads();
   }
   const Lanes<P> me(lane, a.kv_heads);
   const int D = a.dim, ROW = a.kv_heads * D;
-  const int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  const int64_t r = team > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * a.warps + wid;
   if (r >= a.n) return;
   const int cnt = min(max(a.cnt[r], 0), a.slots);
-  const bool several = cnt > a.chunk;                          // chunks are multiples of UN * RPI slots
+  const bool several = cnt > a.chunk;                          // chunks are multiples of the team's UN * RPI slots
+  const int row = me.row + sub * UN * me.RPI, step = team * UN * me.RPI;
   bool filled = several;
   const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
   const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
@@ -213,17 +256,17 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
     for (int g = 0; g < a.group; ++g) {
       const int h = kv * a.group + g;
       // all first loads on their way before the first of them is waited for
-      const T* kp = kr + (int64_t)me.row * ROW + kv * D;
-      const T* vp = vr + (int64_t)me.row * ROW + kv * D;
+      const T* kp = kr + (int64_t)row * ROW + kv * D;
+      const T* vp = vr + (int64_t)row * ROW + kv * D;
       S k[UN], v[UN], raw;
 #pragma unroll
-      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < cnt);
       raw.load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h) * D, me.part, D, true);
 #pragma unroll
-      for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < cnt);
       if (!filled) {
-        fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
-        __syncwarp();
+        fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane + 32 * sub, 32 * team);
+        sync_team(team);
         filled = true;
       }
       float q[S::N];
@@ -235,11 +278,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
       for (int c0 = 0; c0 < cnt; c0 += a.chunk) {
         const int c1 = min(cnt, c0 + a.chunk);
         if (several) {
-          __syncwarp();
-          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
-          __syncwarp();
+          sync_team(team);
+          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane + 32 * sub, 32 * team);
+          sync_team(team);
         }
-        for (int s0 = c0 + me.row; s0 - me.row < c1; s0 += UN * me.RPI) {
+        for (int s0 = c0 + row; s0 - me.row < c1; s0 += step) {
           float z[UN];
 #pragma unroll
           for (int u = 0; u < UN; ++u) {
@@ -248,8 +291,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
             for (int j = 0; j < S::N; ++j) z[u] = fmaf(k[u].at(j), q[j], z[u]);
           }
           // the next slots' keys come while these are weighed, their values while the next are
-          const int next = s0 + UN * me.RPI;
-          kp += UN * me.RPI * ROW;
+          const int next = s0 + step;
+          kp += step * ROW;
 #pragma unroll
           for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
           if constexpr (P >= 16) {
@@ -287,7 +330,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 #pragma unroll
             for (int j = 0; j < S::N; ++j) acc[j] = fmaf(p, v[u].at(j), acc[j]);
           }
-          vp += UN * me.RPI * ROW;
+          vp += step * ROW;
 #pragma unroll
           for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
         }
@@ -301,6 +344,15 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
         l = l * f + __shfl_xor_sync(FULL, l, o) * of;
 #pragma unroll
         for (int j = 0; j < S::N; ++j) acc[j] = acc[j] * f + __shfl_xor_sync(FULL, acc[j], o) * of;
+      }
+      if (team > 1) {
+        float* red = reinterpret_cast<float*>(smem + layout(a.heads, D, a.chunk, false, false, 0, team, 1).red);
+        if (me.row == 0) put_team<S, P>(red, sub * me.KC + me.kc, D, me.part, acc);
+        if (me.row == 0 && me.part == 0) reinterpret_cast<float2*>(red + team * RED)[sub * me.KC + me.kc] = make_float2(m, l);
+        __syncthreads();
+        merge_team<T>(a, red, me.KC, 1, r, kv0, g);
+        __syncthreads();                                       // before the next heads overwrite it
+        continue;
       }
       const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -322,7 +374,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ double s_bounds[kMaxBuckets + 1];
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-  uint8_t* bucket = smem + (size_t)wid * a.warp_bytes;
+  const int team = a.team, sub = team > 1 ? wid : 0;
+  uint8_t* bucket = smem + (team > 1 ? 0 : (size_t)wid * a.warp_bytes);
   if (a.bias) {
     stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
     __syncthreads();
@@ -331,10 +384,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
   const Reduced<P, N> sums(lane);
   const int my_g = sums.id / UN, my_u = sums.id % UN, base_lane = lane & ~(P - 1);
   const int D = a.dim, ROW = a.kv_heads * D;
-  const int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  const int64_t r = team > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * a.warps + wid;
   if (r >= a.n) return;
   const int cnt = min(max(a.cnt[r], 0), a.slots);
-  const bool several = cnt > a.chunk;                          // chunks are multiples of UN * RPI slots
+  const bool several = cnt > a.chunk;                          // chunks are multiples of the team's UN * RPI slots
+  const int row = me.row + sub * UN * me.RPI, step = team * UN * me.RPI;
   bool filled = several;
   const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
   const T* vr = reinterpret_cast<const T*>(a.v) + r * a.slots * ROW;
@@ -342,21 +396,21 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
     const int kv = kv0 + me.kc;
     for (int g0 = 0; g0 < a.group; g0 += GT) {
       const int h0 = kv * a.group + g0;
-      const T* kp = kr + (int64_t)me.row * ROW + kv * D;
-      const T* vp = vr + (int64_t)me.row * ROW + kv * D;
+      const T* kp = kr + (int64_t)row * ROW + kv * D;
+      const T* vp = vr + (int64_t)row * ROW + kv * D;
       S k[UN], v[UN];
 #pragma unroll
-      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+      for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < cnt);
       float q[GT][S::N], acc[GT][S::N];
       {
         S raw[GT];
 #pragma unroll
         for (int g = 0; g < GT; ++g) raw[g].load(reinterpret_cast<const T*>(a.q) + (r * a.heads + h0 + g) * D, me.part, D, true);
 #pragma unroll
-        for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < cnt);
+        for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < cnt);
         if (!filled) {
-          fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane);
-          __syncwarp();
+          fill_buckets(a, s_bounds, bucket, r, 0, cnt, lane + 32 * sub, 32 * team);
+          sync_team(team);
           filled = true;
         }
 #pragma unroll
@@ -371,11 +425,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
       for (int c0 = 0; c0 < cnt; c0 += a.chunk) {
         const int c1 = min(cnt, c0 + a.chunk);
         if (several) {
-          __syncwarp();
-          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane);
-          __syncwarp();
+          sync_team(team);
+          fill_buckets(a, s_bounds, bucket, r, c0, c1, lane + 32 * sub, 32 * team);
+          sync_team(team);
         }
-        for (int s0 = c0 + me.row; s0 - me.row < c1; s0 += UN * me.RPI) {
+        for (int s0 = c0 + row; s0 - me.row < c1; s0 += step) {
           float z[N];
 #pragma unroll
           for (int u = 0; u < UN; ++u) {
@@ -388,8 +442,8 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
               for (int g = 0; g < GT; ++g) z[g * UN + u] = fmaf(x, q[g][j], z[g * UN + u]);
             }
           }
-          const int next = s0 + UN * me.RPI;
-          kp += UN * me.RPI * ROW;
+          const int next = s0 + step;
+          kp += step * ROW;
 #pragma unroll
           for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
           Reduced<P, N>::run(z, lane);
@@ -432,7 +486,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
               for (int g = 0; g < GT; ++g) acc[g][j] = fmaf(w[g], x, acc[g][j]);
             }
           }
-          vp += UN * me.RPI * ROW;
+          vp += step * ROW;
 #pragma unroll
           for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < cnt);
         }
@@ -440,6 +494,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
 #pragma unroll
       for (int o = SP; o < SP * (UN / C); o <<= 1) l += __shfl_xor_sync(FULL, l, o);
       // the groups of lanes that shared a head's slots
+      float* red = reinterpret_cast<float*>(smem + layout(a.heads, D, a.chunk, false, false, 0, team, GT).red);
 #pragma unroll
       for (int g = 0; g < GT; ++g) {
         float gm = __shfl_sync(FULL, m, base_lane | (g * UN / C * SP)), gl = __shfl_sync(FULL, l, base_lane | (g * UN / C * SP));
@@ -452,10 +507,21 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_grou
 #pragma unroll
           for (int j = 0; j < S::N; ++j) acc[g][j] = acc[g][j] * f + __shfl_xor_sync(FULL, acc[g][j], o) * of;
         }
+        if (team > 1) {
+          const int e = (sub * me.KC + me.kc) * GT + g;
+          if (me.row == 0) put_team<S, P>(red, e, D, me.part, acc[g]);
+          if (me.row == 0 && me.part == 0) reinterpret_cast<float2*>(red + team * GT * RED)[e] = make_float2(gm, gl);
+          continue;
+        }
         const float f = gl == 0.f ? 0.f : 1.f / gl;
 #pragma unroll
         for (int j = 0; j < S::N; ++j) acc[g][j] *= f;
         if (me.row == 0) S::store(reinterpret_cast<T*>(a.out) + (r * a.heads + h0 + g) * D, me.part, D, acc[g]);
+      }
+      if (team > 1) {
+        __syncthreads();
+        merge_team<T>(a, red, me.KC * GT, GT, r, kv0, g0);
+        __syncthreads();                                       // before the next heads overwrite it
       }
     }
   }
@@ -470,14 +536,16 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   const int H = a.heads, D = a.dim, ROW = a.kv_heads * D;
   const bool table = a.partial != nullptr;
-  const Layout L = layout(H, D, a.chunk, a.chunk < a.slots, true, table ? H * a.buckets : 0);
-  uint8_t* my = smem + (size_t)wid * a.warp_bytes;
+  const int team = a.team, sub = team > 1 ? wid : 0;
+  const Layout L = layout(H, D, a.chunk, a.chunk < a.slots, true, table ? H * a.buckets : 0, team, GT);
+  uint8_t* my = smem + (team > 1 ? 0 : (size_t)wid * a.warp_bytes);
   uint8_t* bucket = my;
   float2* zd = reinterpret_cast<float2*>(my + L.z);            // [slot][head]: logit and do . v, then weight and dz
   float4* s_head = reinterpret_cast<float4*>(my + L.head);     // m, 1 / l, delta in two terms
   double2* s_sums = reinterpret_cast<double2*>(my + L.sums);   // l and l * delta so far
   float* s_dq = reinterpret_cast<float*>(my + L.dq);
-  double* tab = reinterpret_cast<double*>(my + L.table);
+  double* tab = reinterpret_cast<double*>(my + L.table) + sub * H * a.buckets;
+  float* red = reinterpret_cast<float*>(my + L.red);
   if (a.bias) stage_bounds(s_bounds, a.bounds, a.buckets - 1, threadIdx.x, blockDim.x);
   if (table) {
     for (int i = lane; i < H * a.buckets; i += 32) tab[i] = 0.0;
@@ -485,10 +553,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
   __syncthreads();
   const Lanes<P> me(lane, a.kv_heads);
   const Reduced<P, N> sums(lane);
-  const int h_first = lane % H, h_step = 32 % H;               // head of entry lane + 32 i of a [slot][head] array, by steps
-  const int64_t stride = (int64_t)gridDim.x * a.warps;
+  const int h_first = (lane + 32 * sub) % H, h_step = 32 * team % H;   // head of entry lane + 32 (sub + team i) of a [slot][head] array, by steps
+  const int64_t stride = (int64_t)gridDim.x * (team > 1 ? 1 : a.warps);
+  const int row = me.row + sub * UN * me.RPI, step = team * UN * me.RPI;
   auto count = [&](int64_t r) { return r < a.n ? min(max(a.cnt[r], 0), a.slots) : 0; };
-  int64_t r = (int64_t)blockIdx.x * a.warps + wid;
+  int64_t r = team > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * a.warps + wid;
   int cnt = count(r), next_cnt = count(r + stride);
   for (; r < a.n; r += stride, cnt = next_cnt, next_cnt = count(r + stride)) {
     const T* kr = reinterpret_cast<const T*>(a.k) + r * a.slots * ROW;
@@ -500,11 +569,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
     T* dqr = reinterpret_cast<T*>(a.dq) + r * H * D;
     const bool several = cnt > a.chunk;
     if (several) {
-      for (int h = lane; h < H; h += 32) {
+      for (int h = lane + 32 * sub; h < H; h += 32 * team) {
         s_head[h].x = -INFINITY;
         s_sums[h] = make_double2(0.0, 0.0);
       }
-      __syncwarp();
+      sync_team(team);
     }
 
     for (int sweep = 0; sweep < (several ? 2 : 1); ++sweep) {
@@ -516,21 +585,21 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
           const int kv = kv0 + me.kc;
           for (int g0 = 0; g0 < a.group; g0 += GT) {
             const int h0 = kv * a.group + g0;
-            const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
-            const T* vp = vr + (int64_t)(c0 + me.row) * ROW + kv * D;
+            const T* kp = kr + (int64_t)(c0 + row) * ROW + kv * D;
+            const T* vp = vr + (int64_t)(c0 + row) * ROW + kv * D;
             S k[UN], v[UN], raw[GT], raw2[GT];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
+            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < ns);
 #pragma unroll
-            for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
+            for (int u = 0; u < UN; ++u) v[u].load(vp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < ns);
 #pragma unroll
             for (int g = 0; g < GT; ++g) {
               raw[g].load(qr + (h0 + g) * D, me.part, D, true);
               raw2[g].load(gr + (h0 + g) * D, me.part, D, true);
             }
             if (!filled) {
-              fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane);
-              __syncwarp();
+              fill_buckets(a, s_bounds, bucket, r, c0, c0 + ns, lane + 32 * sub, 32 * team);
+              sync_team(team);
               filled = true;
             }
             float q[GT][S::N], go[GT][S::N];
@@ -539,7 +608,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
               raw[g].floats(q[g]);
               raw2[g].floats(go[g]);
             }
-            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
+            for (int s0 = row; s0 - me.row < ns; s0 += step) {
               float x[N];                                      // q . k of the heads' slots, then do . v
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
@@ -556,9 +625,9 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
                 }
               }
               // the next slots' rows come while these sums are put together
-              const int next = s0 + UN * me.RPI;
-              kp += UN * me.RPI * ROW;
-              vp += UN * me.RPI * ROW;
+              const int next = s0 + step;
+              kp += step * ROW;
+              vp += step * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
 #pragma unroll
@@ -582,7 +651,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
             }
           }
         }
-        __syncwarp();
+        sync_team(team);
         if (sweep == 0) {
           // Maximum, sum and delta: 2^lg lanes per head, 32 / 2^lg heads at a time.  Sum and delta in fp64, delta kept in two terms:
           // a root's dz sum to 0, and what delta is off by falls on all of them with one sign.  In fp32 that decided the bias's gradient where
@@ -590,7 +659,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
           int lg = 5;
           while (lg > 0 && (H << lg) > 32) --lg;
           const int per = 32 >> lg, part = lane & ((1 << lg) - 1);
-          for (int h0 = 0; h0 < H; h0 += per) {
+          for (int h0 = sub * per; h0 < H; h0 += team * per) {
             const int h = h0 + (lane >> lg);
             const bool in = h < H;
             const float was = several && in ? s_head[h].x : -INFINITY;
@@ -626,11 +695,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
               s_head[h] = make_float4(top, rl, hi, isfinite(hi) ? (float)(del - (double)hi) : 0.f);
             }
           }
-          __syncwarp();
+          sync_team(team);
           if (several) continue;
         }
         // weights and dz
-        for (int i = lane, h = h_first; i < ns * H; i += 32) {
+        for (int i = lane + 32 * sub, h = h_first; i < ns * H; i += 32 * team) {
           const float2 at = zd[i];
           const float4 head = s_head[h];
           float p = at.x;
@@ -642,11 +711,11 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
           h += h_step;
           if (h >= H) h -= H;
         }
-        __syncwarp();
+        sync_team(team);
         if (table) {
           // 32 slots at a time.  Slots in time order have neighbouring buckets: runs of one bucket are summed by a segmented scan and each
           // run's last lane adds to its bucket, all different ones.  Otherwise a lane per head goes through them.
-          for (int t0 = 0; t0 < ns; t0 += 32) {
+          for (int t0 = 32 * sub; t0 < ns; t0 += 32 * team) {
             const int s = t0 + lane, b = bucket[min(s, ns - 1)];
             const int below = __shfl_up_sync(FULL, b, 1), above = __shfl_down_sync(FULL, b, 1);
             if (__all_sync(FULL, lane == 31 || b <= above) || __all_sync(FULL, lane == 31 || b >= above)) {
@@ -681,14 +750,14 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
 #pragma unroll
               for (int j = 0; j < S::N; ++j) acc[g][j] = 0.f;
             }
-            const T* kp = kr + (int64_t)(c0 + me.row) * ROW + kv * D;
-            const float2* wz = zd + me.row * H + h0;
+            const T* kp = kr + (int64_t)(c0 + row) * ROW + kv * D;
+            const float2* wz = zd + row * H + h0;
             S k[UN];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, me.row + u * me.RPI < ns);
-            for (int s0 = me.row; s0 - me.row < ns; s0 += UN * me.RPI) {
-              const int next = s0 + UN * me.RPI;
-              kp += UN * me.RPI * ROW;
+            for (int u = 0; u < UN; ++u) k[u].load(kp + u * me.RPI * ROW, me.part, D, row + u * me.RPI < ns);
+            for (int s0 = row; s0 - me.row < ns; s0 += step) {
+              const int next = s0 + step;
+              kp += step * ROW;
 #pragma unroll
               for (int u = 0; u < UN; ++u) {
                 float w[GT];
@@ -702,13 +771,17 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
                 }
                 k[u].load(kp + u * me.RPI * ROW, me.part, D, next + u * me.RPI < ns);
               }
-              wz += UN * me.RPI * H;
+              wz += step * H;
             }
 #pragma unroll
             for (int g = 0; g < GT; ++g) {
               for (int o = P * me.KC; o < 32; o <<= 1) {
 #pragma unroll
                 for (int j = 0; j < S::N; ++j) acc[g][j] += __shfl_xor_sync(FULL, acc[g][j], o);
+              }
+              if (team > 1) {
+                if (me.row == 0) put_team<S, P>(red, (sub * me.KC + me.kc) * GT + g, D, me.part, acc[g]);
+                continue;
               }
               if (several && me.row == 0) {                    // carried from chunk to chunk
 #pragma unroll
@@ -726,10 +799,24 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
                 S::store(dqr + (h0 + g) * D, me.part, D, acc[g]);
               }
             }
+            if (team > 1) {
+              __syncthreads();
+              const int size = me.KC * GT * D;
+              for (int i = threadIdx.x; i < size; i += blockDim.x) {
+                const int e = i / D, at = ((kv0 + e / GT) * a.group + g0 + e % GT) * D + (i - e * D);
+                float x = 0.f;
+                for (int w = 0; w < team; ++w) x += red[w * size + i];
+                if (c0 > 0) x += s_dq[at];
+                if (!final_chunk) s_dq[at] = x;
+                else dqr[at] = from_float<T>(x * a.scale);
+              }
+              __syncthreads();                                 // before the next heads overwrite it
+            }
           }
-          T* dkp = dkr + (int64_t)(c0 + me.row) * ROW + kv * D;
-          T* dvp = dvr + (int64_t)(c0 + me.row) * ROW + kv * D;
-          int s = me.row;
+          const int own = me.row + sub * me.RPI, each = team * me.RPI;
+          T* dkp = dkr + (int64_t)(c0 + own) * ROW + kv * D;
+          T* dvp = dvr + (int64_t)(c0 + own) * ROW + kv * D;
+          int s = own;
           if (a.group == GT) {
             float q[GT][S::N], go[GT][S::N];
             {
@@ -749,7 +836,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
             }
             const float2* at = zd + s * H + kv * GT;
 #pragma unroll 2
-            for (; s < ns; s += me.RPI) {
+            for (; s < ns; s += each) {
               float xk[S::N], xv[S::N];
 #pragma unroll
               for (int g = 0; g < GT; ++g) {
@@ -762,12 +849,12 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
               }
               S::store(dkp, me.part, D, xk);
               S::store(dvp, me.part, D, xv);
-              dkp += me.RPI * ROW;
-              dvp += me.RPI * ROW;
-              at += me.RPI * H;
+              dkp += each * ROW;
+              dvp += each * ROW;
+              at += each * H;
             }
           } else {
-            for (; s < ns; s += me.RPI) {
+            for (; s < ns; s += each) {
               float xk[S::N], xv[S::N];
 #pragma unroll
               for (int j = 0; j < S::N; ++j) xk[j] = xv[j] = 0.f;
@@ -784,23 +871,23 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
               }
               S::store(dkp, me.part, D, xk);
               S::store(dvp, me.part, D, xv);
-              dkp += me.RPI * ROW;
-              dvp += me.RPI * ROW;
+              dkp += each * ROW;
+              dvp += each * ROW;
             }
           }
           if (final_chunk) {                                   // behind the last slot that counts: zeros
             float zero[S::N];
 #pragma unroll
             for (int j = 0; j < S::N; ++j) zero[j] = 0.f;
-            for (; s < a.slots - c0; s += me.RPI) {
+            for (; s < a.slots - c0; s += each) {
               S::store(dkp, me.part, D, zero);
               S::store(dvp, me.part, D, zero);
-              dkp += me.RPI * ROW;
-              dvp += me.RPI * ROW;
+              dkp += each * ROW;
+              dvp += each * ROW;
             }
           }
         }
-        __syncwarp();                                          // before the next chunk or root overwrites what was read
+        sync_team(team);                                       // before the next chunk or root overwrites what was read
       }
     }
   }
@@ -808,26 +895,36 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_backward_ker
     __syncthreads();
     for (int i = threadIdx.x; i < H * a.buckets; i += blockDim.x) {
       double sum = 0.0;
-      for (int w = 0; w < a.warps; ++w) sum += reinterpret_cast<const double*>(smem + (size_t)w * a.warp_bytes + L.table)[i];
+      for (int w = 0; w < a.warps; ++w) sum += reinterpret_cast<const double*>(smem + L.table + (size_t)w * (team > 1 ? H * a.buckets * 8 : a.warp_bytes))[i];
       a.partial[(int64_t)blockIdx.x * H * a.buckets + i] = sum;
     }
   }
 }
 
-// dbias[i] = sum of the blocks' partial sums: a warp per entry, lanes and shuffles in a fixed order.
-__global__ void __launch_bounds__(256) bias_sum_kernel(const double* __restrict__ partial, int blocks, int entries, float* __restrict__ dbias) {
-  const int i = (blockIdx.x * 256 + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+// dbias[i] = sum of the blocks' partial sums, in a fixed order: four entries (a sector) by 256 threads each, so that every thread's
+// loads are on their way at once.  (A warp per entry spent 10 us on the tables of 1100 blocks.)
+__global__ void __launch_bounds__(1024) bias_sum_kernel(const double* __restrict__ partial, int blocks, int entries, float* __restrict__ dbias) {
+  __shared__ double s_sum[32][4];
+  const int i = blockIdx.x * 4 + (threadIdx.x & 3), lane = threadIdx.x & 31;
   asm volatile("griddepcontrol.wait;" ::: "memory");           // its launch is prepared while the blocks' kernel runs
-  if (i >= entries) return;
-  double sum = 0.0;
-#pragma unroll 8
-  for (int j = 0; j < (MAX_BLOCKS + 31) / 32; ++j) {           // a fixed number, so that the loads do not wait for one another
-    const int b = 32 * j + lane;
-    sum += b < blocks ? partial[(int64_t)b * entries + i] : 0.0;
-    if (32 * j + 32 >= blocks) break;
+  double x[MAX_BLOCKS / 256];
+#pragma unroll
+  for (int j = 0; j < MAX_BLOCKS / 256; ++j) {
+    const int b = (threadIdx.x >> 2) + 256 * j;
+    x[j] = b < blocks && i < entries ? partial[(int64_t)b * entries + i] : 0.0;
   }
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
-  if (lane == 0) dbias[i] = (float)sum;
+  double sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < MAX_BLOCKS / 256; ++j) sum += x[j];
+  for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
+  if (lane < 4) s_sum[threadIdx.x >> 5][lane] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;
+  sum = 0.0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum += s_sum[(lane >> 2) + 8 * j][lane & 3];
+  for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(FULL, sum, o);
+  if (lane < 4 && i < entries) dbias[i] = (float)sum;
 }
 
 template <bool BACKWARD, typename T, int VB, int P, int NV, int GT>
@@ -837,18 +934,62 @@ auto kernel_of() {
   else return slot_forward_kernel<T, VB, P, NV>;
 }
 
+constexpr int SMEM_BLOCK = 200 * 1024;     // of an SM's 227 KB, beside the bounds and what the system keeps
+
+// Slots of a chunk, warps of a block and warps per root.  Forward a slot takes a byte: chunks of 4096.  Backward logits and dp of a chunk take
+// 8 * heads bytes a slot: 12 KB of them, so that 16 warps have room on an SM.  `step`: slots that a warp has in flight.  A block's warps
+// share a root where they all fit on the GPU at once and each has a step of its own (500 roots of 100 slots, 2 heads of 64 in fp32: 16
+// us forward and 41 us backward with a warp per root, 10 and 26 us with four; 60 roots of 100 slots, 2 x 4 heads of 64 in bf16: 19 and 42, 11 and
+// 21 us; with fewer slots than a step per warp nothing is gained).  0: a warp's share exceeds shared memory.
+int plan(SlotArgs* a, bool backward, int step) {
+  const int table = backward && a->partial ? a->heads * a->buckets : 0, together = heads_at_once(a->group);
+  int chunk = backward ? 12 * 1024 / (8 * a->heads) : 4096;
+  if (chunk > a->slots) chunk = a->slots;
+  a->chunk = chunk;
+  auto bytes = [&](int team) { return layout(a->heads, a->dim, chunk, chunk < a->slots, backward, table, team, together).total; };
+  const int room = num_sms() * (together == 4 ? 4 * kBlocks<4> : 4 * kBlocks<1>);
+  int team = MAX_WARPS;
+  while (team > 1 && (team * a->n > room || (backward && a->n > MAX_BLOCKS) || team * step > a->slots || bytes(team) > SMEM_BLOCK / 4)) team >>= 1;
+  a->team = team;
+  a->warp_bytes = bytes(team);
+  if (team > 1) {
+    a->warps = team;
+    return team;
+  }
+  int w = MAX_WARPS;
+  while (w > 1 && (w * a->warp_bytes > SMEM_BLOCK / 4 || w * (int64_t)num_sms() > a->n)) w >>= 1;   // four blocks to an SM; few roots: over all SMs
+  a->warps = w;
+  return w * a->warp_bytes <= SMEM_BLOCK ? w : 0;
+}
+
+int grid_of(const SlotArgs& a, bool backward) {
+  const int roots = a.team > 1 ? 1 : a.warps, bytes = roots * a.warp_bytes;   // of a block
+  const int64_t want = (a.n + roots - 1) / roots;
+  if (!backward) return (int)want;
+  int resident = (220 * 1024) / (bytes + 2048);
+  if (resident < 1) resident = 1;
+  const int warps = 4 * (heads_at_once(a.group) == 4 ? kBlocks<4> : kBlocks<1>);
+  if (resident > warps / a.warps) resident = warps / a.warps;
+  int64_t most = (int64_t)num_sms() * resident;
+  if (most > MAX_BLOCKS) most = MAX_BLOCKS;
+  return (int)(want < most ? want : most);
+}
+
 template <bool BACKWARD, typename T, int VB, int P, int NV>
-cudaError_t launch_kernel(const SlotArgs& a, int blocks, cudaStream_t s) {
+cudaError_t launch_kernel(SlotArgs& a, int* blocks, cudaStream_t s) {
   const int gt = heads_at_once(a.group);
+  const int kc = a.kv_heads & -a.kv_heads, deep = gt == 4 ? kDeepOf<Seg<T, VB, P, NV>, 4> : kDeepOf<Seg<T, VB, P, NV>, 1>;
+  if (!plan(&a, BACKWARD, deep * (32 / P) / (kc < 32 / P ? kc : 32 / P))) return cudaErrorInvalidConfiguration;
+  *blocks = grid_of(a, BACKWARD);
   const auto kernel = gt == 4   ? kernel_of<BACKWARD, T, VB, P, NV, 4>()
                       : gt == 2 ? kernel_of<BACKWARD, T, VB, P, NV, 2>()
                                 : kernel_of<BACKWARD, T, VB, P, NV, 1>();
-  const int bytes = a.warps * a.warp_bytes;
+  const int bytes = (a.team > 1 ? 1 : a.warps) * a.warp_bytes;
   if (bytes > 46 * 1024) {          // more than a kernel has without asking for it (per device; asking again costs little)
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
   }
-  kernel<<<blocks, 32 * a.warps, bytes, s>>>(a);
+  kernel<<<*blocks, 32 * a.warps, bytes, s>>>(a);
   return cudaGetLastError();
 }
 
@@ -856,7 +997,7 @@ cudaError_t launch_kernel(const SlotArgs& a, int blocks, cudaStream_t s) {
 // bases) otherwise; as many lanes per segment as 8 values each (4 single ones) need.  (Heads of 50 in fp32 over a whole warp, a pair
 // per lane, took 47 us for the 1800 roots of 20 slots that take 40 us this way: the sums' and weights' instructions serve four segments.)
 template <bool BACKWARD, typename T>
-cudaError_t launch_type(const SlotArgs& a, int blocks, cudaStream_t s) {
+cudaError_t launch_type(SlotArgs& a, int* blocks, cudaStream_t s) {
   constexpr int ES = (int)sizeof(T), N16 = ES / 2;             // words of 16 bytes for 8 values
   const uint64_t at = (uint64_t)(uintptr_t)a.k | (uint64_t)(uintptr_t)a.v | (uint64_t)(uintptr_t)a.q | (uint64_t)(uintptr_t)a.out |
                       (uint64_t)(uintptr_t)a.dout | (uint64_t)(uintptr_t)a.dq | (uint64_t)(uintptr_t)a.dk | (uint64_t)(uintptr_t)a.dv |
@@ -873,34 +1014,6 @@ cudaError_t launch_type(const SlotArgs& a, int blocks, cudaStream_t s) {
   }
   if (a.dim <= 32) return launch_kernel<BACKWARD, T, ES, 8, 4>(a, blocks, s);
   return launch_kernel<BACKWARD, T, ES, 32, 4>(a, blocks, s);
-}
-
-constexpr int SMEM_BLOCK = 200 * 1024;     // of an SM's 227 KB, beside the bounds and what the system keeps
-
-// Slots of a chunk and warps of a block.  Forward a slot takes a byte: chunks of 4096.  Backward logits and dp of a chunk take
-// 8 * heads bytes a slot: 12 KB of them, so that 16 warps have room on an SM.  false: a warp's share exceeds shared memory.
-bool plan(SlotArgs* a, bool backward) {
-  const int table = backward && a->partial ? a->heads * a->buckets : 0;
-  int chunk = backward ? 12 * 1024 / (8 * a->heads) : 4096;
-  if (chunk > a->slots) chunk = a->slots;
-  a->chunk = chunk;
-  a->warp_bytes = layout(a->heads, a->dim, chunk, chunk < a->slots, backward, table).total;
-  int w = MAX_WARPS;
-  while (w > 1 && (w * a->warp_bytes > SMEM_BLOCK / 4 || w * (int64_t)num_sms() > a->n)) w >>= 1;   // four blocks to an SM; few roots: over all SMs
-  a->warps = w;
-  return w * a->warp_bytes <= SMEM_BLOCK;
-}
-
-int grid_of(const SlotArgs& a, bool backward) {
-  const int64_t want = (a.n + a.warps - 1) / a.warps;
-  if (!backward) return (int)want;
-  int resident = (int)((220 * 1024) / ((int64_t)a.warps * a.warp_bytes + 2048));
-  if (resident < 1) resident = 1;
-  const int warps = 4 * (heads_at_once(a.group) == 4 ? kBlocks<4> : kBlocks<1>);
-  if (resident > warps / a.warps) resident = warps / a.warps;
-  int64_t most = (int64_t)num_sms() * resident;
-  if (most > MAX_BLOCKS) most = MAX_BLOCKS;
-  return (int)(want < most ? want : most);
 }
 
 template <bool BACKWARD>
@@ -934,18 +1047,18 @@ int run(const char* who, SlotArgs& a, int dtype, const void* out_like, float* db
   }
   a.group = a.heads / a.kv_heads;
   a.partial = dbias ? reinterpret_cast<double*>(scratch) : nullptr;
-  if (!plan(&a, BACKWARD))
-    return fail(err, size, TGNN_ECAPACITY, "%s: %d heads with %d buckets exceed shared memory", who, a.heads, a.buckets);
-  const int blocks = grid_of(a, BACKWARD);
+  int blocks = 0;
   cudaError_t e;
-  if (dtype == TGNN_F32) e = launch_type<BACKWARD, float>(a, blocks, s);
-  else if (dtype == TGNN_BF16) e = launch_type<BACKWARD, __nv_bfloat16>(a, blocks, s);
-  else e = launch_type<BACKWARD, __half>(a, blocks, s);
+  if (dtype == TGNN_F32) e = launch_type<BACKWARD, float>(a, &blocks, s);
+  else if (dtype == TGNN_BF16) e = launch_type<BACKWARD, __nv_bfloat16>(a, &blocks, s);
+  else e = launch_type<BACKWARD, __half>(a, &blocks, s);
+  if (blocks == 0)
+    return fail(err, size, TGNN_ECAPACITY, "%s: %d heads with %d buckets exceed shared memory", who, a.heads, a.buckets);
   if (e == cudaSuccess && BACKWARD && a.partial) {
     const int entries = a.heads * a.buckets;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(entries + 7) / 8);
-    cfg.blockDim = dim3(256);
+    cfg.gridDim = dim3((unsigned)(entries + 3) / 4);
+    cfg.blockDim = dim3(1024);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -287,3 +287,34 @@ def test_slots_bias_gradient_sums_to_zero_over_the_buckets(B, dt, S, H, KV, D):
     tol = 9 * U * dz.sum((0, 3)).reshape(H)
     db = c.backward()[3].double().cpu().numpy()
     assert (np.abs(db.sum(1)) <= tol + U * np.abs(db).sum(1)).all(), (db.sum(1), tol)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("H,KV,D", [(2, 2, 50), (4, 2, 33), (8, 2, 64), (3, 1, 16), (6, 3, 100), (8, 1, 128), (12, 3, 25), (24, 2, 8), (4, 4, 5)])
+@pytest.mark.parametrize("R,S", [(3, 100), (60, 37), (1000, 20)])
+def test_slots_query_heads_together_and_warps_together(B, dt, R, S, H, KV, D):
+    """Query heads of a cached head by ones, twos and fours, several times over; a root by four warps, by two, by one."""
+    c = Case(B, R, S, H, KV, D, dt, seed=R + H)
+    out, grads = c.check()
+    assert torch.equal(out, c.forward())
+    for a, b in zip(grads, c.backward()):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("R,S,H,KV,D", [(1300, 30, 128, 64, 4), (1300, 70, 64, 16, 3), (3, 5000, 1, 1, 2), (1200, 4200, 1, 1, 2), (5, 4101, 4, 2, 20),
+                                        (590, 400, 8, 2, 6), (1024, 200, 8, 8, 4), (1025, 200, 8, 8, 4)])
+def test_slots_in_several_chunks_by_one_and_more_warps(B, R, S, H, KV, D):
+    Case(B, R, S, H, KV, D, "f32", seed=S).check()
+
+
+def test_slots_masked_buckets_by_more_warps(B):
+    """Buckets at -infinity and at the type's lowest value, rows without a slot, where warps share a root and heads are taken together."""
+    for R, S, H, KV in ((20, 150, 8, 2), (20, 150, 2, 2), (900, 40, 4, 2)):
+        c = Case(B, R, S, H, KV, 32, "f32", seed=R + H, cnt=[0] + [S] * (R - 1))
+        c.b["bias"][:, 1::2] = float("-inf")
+        c.check()
+        c.b["bias"][:] = torch.finfo(torch.float32).min
+        out, grads = c.forward(), c.backward()
+        assert all(bool(torch.isfinite(t).all()) for t in (out, *grads)) and not out[0].any()
+        c.b["bias"][:] = float("-inf")
+        assert not c.forward().any() and not any(g.any() for g in c.backward())
