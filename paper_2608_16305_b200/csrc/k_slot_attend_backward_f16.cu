@@ -1,0 +1,8 @@
+// Slot attention, the backward pass's kernels for fp16: slot_attend.cuh.
+#include "slot_attend.cuh"
+
+namespace tgnn_slots {
+
+template cudaError_t launch_type<true, __half>(SlotArgs&, int*, cudaStream_t);
+
+}  // namespace tgnn_slots
