@@ -21,7 +21,7 @@
 // warp keeps a table of its own and a second kernel adds the blocks' tables in a fixed order, so no atomics decide on a result.
 // Logits stay in natural units: a bias of the type's lowest value is then still finite.
 //
-// Measured on a B200, 14 400 roots of 64 slots, 4 heads of 32 in bf16: forward 89 us at 5.3 TB/s, backward 198 us at 4.9 TB/s of DRAM (a copy
+// Measured on a B200, 14 400 roots of 64 slots, 4 heads of 32 in bf16: forward 89 us at 5.2 TB/s, backward 204 us at 4.75 TB/s of DRAM (a copy
 // reaches 6.5); 1800 roots of 20 slots, 2 heads of 50 in fp32: 10 and 20 us, a single wave of 12 warps per SM, bound by the latency of a
 // root's chain of loads and sums.
 #pragma once
@@ -158,8 +158,8 @@ struct Reduced {
 };
 
 // Query heads of a cached head that a warp takes together: 4, 2 or 1, whatever divides their number.  One after another they read and
-// unpacked a root's rows again for each (6000 roots of 40 slots, 2 x 4 heads of 64, bf16: 76 us forward and 154 us backward; 55 and 106 us
-// by fours; 2 x 2 heads of 64 in fp32: 68 and 158 us; 49 and 116 us by twos).
+// unpacked a root's rows again for each (6000 roots of 40 slots, 2 x 4 heads of 64, bf16: 76 us forward and 154 us backward; 49 and 103 us
+// by fours; 2 x 2 heads of 64 in fp32: 68 and 158 us; 49 and 110 us by twos).
 __host__ __device__ inline int heads_at_once(int group) { return (group & 3) == 0 ? 4 : (group & 1) == 0 ? 2 : 1; }
 
 // Segments of k and of v in flight per lane: 64 bytes of each, 2 segments at least and 4 at most.
@@ -168,7 +168,8 @@ constexpr int kDeep = sizeof(S) >= 32 ? 2 : 4;
 // With four query heads at a time their registers leave room for two.
 template <typename S, int GT>
 constexpr int kDeepOf = GT >= 4 ? 2 : kDeep<S>;
-// Blocks per SM of the backward pass: four heads' q and do take 64 registers.
+// Blocks per SM of the backward pass, and of the forward pass in fp32: four heads' q and do, or q and output, take 64 registers.  (16-bit
+// rows leave room for a fourth block in the forward pass: 49 instead of 57 us for 6000 roots of 40 slots, 2 x 4 heads of 64.)
 template <int GT>
 constexpr int kBlocks = GT >= 4 ? 3 : 4;
 
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(32 * MAX_WARPS, 4) slot_forward_kernel(const S
 // UN slots and GT heads end on different lanes (value g * UN + u on the lane, or the lanes, that Reduced gives it), and each lane weighs its
 // own, instead of P lanes all of them; weights and corrections then go back to the segment.
 template <typename T, int VB, int P, int NV, int GT>
-__global__ void __launch_bounds__(32 * MAX_WARPS, kBlocks<GT>) slot_forward_group_kernel(const SlotArgs a) {
+__global__ void __launch_bounds__(32 * MAX_WARPS, sizeof(T) == 2 ? 4 : kBlocks<GT>) slot_forward_group_kernel(const SlotArgs a) {
   using S = Seg<T, VB, P, NV>;
   constexpr int UN = kDeepOf<S, GT>, N = GT * UN;
   constexpr int C = N > P ? N / P : 1, SP = P > N ? P / N : 1;  // values per lane, lanes per value
