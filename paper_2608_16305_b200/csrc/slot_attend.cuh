@@ -988,8 +988,10 @@ cudaError_t launch_kernel(SlotArgs& a, int* blocks, cudaStream_t s) {
                       : gt == 2 ? kernel_of<BACKWARD, T, VB, P, NV, 2>()
                                 : kernel_of<BACKWARD, T, VB, P, NV, 1>();
   const int bytes = (a.team > 1 ? 1 : a.warps) * a.warp_bytes;
-  if (bytes > 46 * 1024) {          // more than a kernel has without asking for it (per device; asking again costs little)
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (bytes > 46 * 1024) {
+    // More than a kernel has without asking for it.  What is asked for is kept per kernel and device, and another thread's call may ask between
+    // this one's question and its launch: so it is always the most that any plan takes, never this call's bytes.  (Asking again costs little.)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BLOCK);
     if (e != cudaSuccess) return e;
   }
   kernel<<<*blocks, 32 * a.warps, bytes, s>>>(a);
