@@ -539,7 +539,8 @@ TGNN_API int tgnn_sample_window(const int64_t* indptr, const int32_t* nbr, const
 
 /* Row cache.  A row is `heads` groups of `dim` values (1 to 128).  A group is held as codes of 4 or 8 bits and one scale:
  *   amax = max |x|; L = 7 or 127; scale = fp32(amax * fp32(1 / L)) rounded up to bf16; r = fp32(1 / scale);
- *   code = the integer nearest to x * r, ties to even; the value read back is code * scale.
+ *   code = the integer nearest to x * r, ties to even; the value read back is code * scale, held at the row type's largest finite
+ *   value where the scale's rounding (2^-7 at most) takes it past that, so that a finite row reads back finite in its own type.
  *   A group with amax < 2^-100 is held as zeros; one with an infinity or a NaN reads back as NaN, all of it.
  * Row p has its codes at codes + p * code_stride (heads x tgnn_cache_code_bytes(dim, bits) bytes: a head's values in order, low bits
  * first, each code + 8 or + 128, padded to 32, 64 or 128 values), its scales at scales + p * scale_stride (bf16[heads]) and its time
@@ -582,6 +583,7 @@ TGNN_API int tgnn_cache_read(const tgnn_cache* cache_host, void* rows, int dtype
  *   fp64[num_buckets - 1] ascending, times: fp64[n] and ts: fp64[k.rows] are needed (num_buckets 1 to 128).  window >= 0, sinks >= 0,
  *   not both 0.  max_len: no root's len is above it, or 0 if unknown (it chooses the launch; results hold for any len).
  *   A root that sees nothing, or whose logits are all -infinity, gets zeros; entries that it does not see do not touch its result.
+ *   v_j is code * scale; a result in fp16 is held at fp16's largest finite value where the scale's rounding takes it past that.
  *   A history outside the cache (first < 0, len < 0, first + len > rows) or of 2^31 - 64 entries and more sees nothing, status 4.
  *   n * kv_heads * ceil(heads / kv_heads / 8) is below 2^28.  Sums in an order fixed by the sizes and the device. */
 TGNN_API int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_host, const tgnn_cache* v_host, int64_t n, int heads,

@@ -48,8 +48,11 @@ def quantise(x, bits):
     return codes.astype(np.int64), np.where(bad, np.float32(np.nan), s).astype(np.float32)
 
 
-def dequantise(codes, scales):
-    return codes.astype(np.float64) * scales[..., None].astype(np.float64)
+def dequantise(codes, scales, most=float(np.finfo(np.float32).max)):
+    """Code times scale.  The scale is rounded up to bf16, so the product may pass the row type's largest finite value `most` by 2^-7 of
+    it: it is held there; what is further out is left as it is."""
+    x = codes.astype(np.float64) * scales[..., None].astype(np.float64)
+    return np.where((np.abs(x) > most) & (np.abs(x) <= most * (1 + 2.0 ** -7) * (1 + 2.0 ** -20)), np.copysign(most, x), x)
 
 
 def bucket(bounds, dt):

@@ -6,6 +6,8 @@
 // in 16 bits, as bf16, for its fp32 range: more of its bits would be lost on codes of 8 bits or less, and 2 bytes beside 16 to 128
 // of codes cost 2 to 12 % where fp32 would cost 3 to 25 %.  A group below 2^-100 is held as zeros (scale 0) so that 1 / scale
 // stays in range; a group with an infinity or a NaN has scale NaN and reads back as NaN, all of it, instead of as wrong numbers.
+// (Read back, the largest code may then lie past the row type's largest finite value, by 2^-7 of it at most: it is held at that value, so that
+// finite rows stay finite.  A wider row read as fp16 is infinite beyond that, as by any conversion.)
 // The product is rounded to an integer by one fused multiply-add onto 1.5 * 2^23, where fp32's spacing is 1: the exact
 // product is rounded once, so codes do not depend on how a quotient was computed.  Codes are stored with an offset (8 or 128), which
 // leaves them in the low bits of that sum; a word of them is put together by shifted adds.
@@ -127,14 +129,18 @@ __device__ __forceinline__ uint16_t quantise(float amax, const float (*v)[8], ui
   return bad ? (uint16_t)0x7fc0u : (uint16_t)(__float_as_uint(s) >> 16);
 }
 
-// The 8 values of codes: a code under fp32's exponent for 2^23 reads as 2^23 + offset + code.
-template <int BITS>
+// The 8 values of codes, for rows of T: a code under fp32's exponent for 2^23 reads as 2^23 + offset + code.
+template <typename T, int BITS>
 __device__ __forceinline__ void values(const uint32_t (&code)[BITS == 4 ? 1 : 2], float s, float (&v)[8]) {
   constexpr int PER = BITS == 4 ? 8 : 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const uint32_t x = (code[j / PER] >> (BITS * (j % PER))) & (BITS == 4 ? 0xfu : 0xffu);
     v[j] = (__uint_as_float(0x4b000000u | x) - (8388608.f + (BITS == 4 ? 8.f : 128.f))) * s;
+  }
+  if (s * (BITS == 4 ? 7.f : 127.f) > Range<T>::most) {         // (NaN is not)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
   }
 }
 
@@ -188,8 +194,11 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, cons
   }
 }
 
+// Eight blocks to an SM where a row moves in 16-byte words: the branch for the end of the type's range, hardly ever taken, would cost registers (a million
+// rows of 4 x 64 in fp32 from 8 bits: 318 us, 343 without that branch and without the bound).  Narrower words are better off with registers for
+// all their addresses than with more warps (400 000 rows of 8 x 50 in bf16 from 4 bits: 223 us, 340 with the bound).
 template <typename T, int VB, int BITS, int U>
-__global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __restrict__ rows) {
+__global__ void __launch_bounds__(THREADS, VB == 16 ? 8 : 1) cache_read_kernel(const Move a, T* __restrict__ rows) {
   const int lanes = 1 << a.lg, l = threadIdx.x & (lanes - 1);
   constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
   const Where w = find<false>(a, ((uint64_t)blockIdx.x * THREADS + threadIdx.x) >> a.lg);
@@ -229,7 +238,7 @@ __global__ void __launch_bounds__(THREADS) cache_read_kernel(const Move a, T* __
 #pragma unroll
       for (int p = 0; p < 2; ++p) {
         float v[8];
-        values<BITS>(code[u][p], s, v);
+        values<T, BITS>(code[u][p], s, v);
         store8<T, VB>(row + u * a.c.dim, 8 * (l + p * lanes), a.c.dim, v);
       }
     }
@@ -317,7 +326,7 @@ __global__ void __launch_bounds__(THREADS) cache_narrow_kernel(const Move a, typ
       sb = __ldg(scale);
     }
     float v[8];
-    values<BITS>(code, __uint_as_float(sb << 16), v);
+    values<T, BITS>(code, __uint_as_float(sb << 16), v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) mine[own * ld + 8 * l + j] = v[j];
     __syncwarp();

@@ -162,10 +162,11 @@ __device__ __forceinline__ void load_query(const AttendArgs& a, int64_t base, in
     }
   }
 }
+// (fp16: a mean of values that a cache holds at the type's end, which its rounded scale puts up to 2^-7 past it, stays finite.)
 __device__ __forceinline__ void store_out(const AttendArgs& a, int64_t i, float x) {
   if (a.dtype == TGNN_F32) reinterpret_cast<float*>(a.out)[i] = x;
   else if (a.dtype == TGNN_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[i] = __float2bfloat16_rn(x);
-  else reinterpret_cast<__half*>(a.out)[i] = __float2half_rn(x);
+  else reinterpret_cast<__half*>(a.out)[i] = __float2half_rn(within<__half>(x));
 }
 // Columns e and e + 1 of an output row: e is even, the row a pair's multiple long.
 __device__ __forceinline__ void store_pair(const AttendArgs& a, int64_t i, float x, float y) {
@@ -174,7 +175,7 @@ __device__ __forceinline__ void store_pair(const AttendArgs& a, int64_t i, float
   } else if (a.dtype == TGNN_BF16) {
     *reinterpret_cast<__nv_bfloat162*>(reinterpret_cast<__nv_bfloat16*>(a.out) + i) = __floats2bfloat162_rn(x, y);
   } else {
-    *reinterpret_cast<__half2*>(reinterpret_cast<__half*>(a.out) + i) = __floats2half2_rn(x, y);
+    *reinterpret_cast<__half2*>(reinterpret_cast<__half*>(a.out) + i) = __floats2half2_rn(within<__half>(x), within<__half>(y));
   }
 }
 

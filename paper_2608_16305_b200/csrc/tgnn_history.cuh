@@ -62,6 +62,21 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 
+// The row types' largest finite values, and how far a finite row's values may pass them: a cache's scale is rounded up to bf16, so the
+// largest code times the scale lies up to 2^-7 above the group's largest magnitude.  fp16 has numbers of fp32 beyond that, which convert to
+// infinity; of fp32 and bf16 nothing finite is further out.
+template <typename T>
+struct Range { static constexpr float most = 3.40282347e38f, edge = INFINITY; };
+template <>
+struct Range<__nv_bfloat16> { static constexpr float most = 3.38953139e38f, edge = INFINITY; };
+template <>
+struct Range<__half> { static constexpr float most = 65504.f, edge = 66016.f; };   // 65504 (1 + 2^-7) is 66015.75
+// x, or the largest finite value where x is past it by no more than that; NaN stays.
+template <typename T>
+__device__ __forceinline__ float within(float x) {
+  return fabsf(x) > Range<T>::most && fabsf(x) <= Range<T>::edge ? copysignf(Range<T>::most, x) : x;
+}
+
 // Words of VB bytes.
 template <int VB>
 struct Vec;
