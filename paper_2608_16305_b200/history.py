@@ -45,7 +45,7 @@ class Slots(NamedTuple):
 
 
 class EventHistory:
-    """Quantised keys and values of every entry of a T-CSR (indptr, nbr, eid, ts: device tensors)."""
+    """Quantised keys and values of every entry of a T-CSR (indptr, nbr, eid, ts: device tensors, which stay as they are while it is used)."""
 
     def __init__(self, indptr, nbr, eid, ts, kv_heads: int, dim: int, window: int, sinks: int = 0, bits: int = 4):
         self.indptr, self.nbr, self.eid, self.ts = indptr, nbr, eid, ts
@@ -60,10 +60,19 @@ class EventHistory:
         return int(self._status.item())
 
     def places(self, first_event: int, last_event: int) -> torch.Tensor:
-        """Places of the entries of events [first_event, last_event), two per event, event by event."""
+        """Places of the entries of events [first_event, last_event), two per event, event by event; events outside the T-CSR have none.
+        The T-CSR has to number its events one after the other, from any number on, with two entries each: ValueError otherwise
+        (looked at on the first call, which reads the device)."""
         if self._places is None:                       # a stream's entries, ordered by event once
-            self._places = torch.argsort(self.eid, stable=True)
-        return self._places[2 * first_event:2 * last_event]
+            order = torch.argsort(self.eid, stable=True)
+            ids = self.eid[order]
+            base = int(ids[0]) if ids.numel() else 0
+            want = torch.arange(ids.numel() // 2, dtype=ids.dtype, device=ids.device) + base
+            if not torch.equal(ids, want.repeat_interleave(2)):
+                raise ValueError("the T-CSR's events are not numbered one after the other with two entries each")
+            self._first_event, self._places = base, order
+        a = max(0, first_event - self._first_event)
+        return self._places[2 * a:2 * max(a, last_event - self._first_event)]
 
     def append(self, places: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> None:
         """Keys and values [n, kv_heads, dim] of the entries at `places` (distinct), quantised as they are written."""
