@@ -108,6 +108,14 @@ static PyObject* result(int rc, const char* err) {
     if (st < 0) return NULL;                                   \
     if (st == 0) return PyLong_FromLongLong(dev);              \
   }
+/* The library's call, with the interpreter free for other threads (a launch may wait for a full queue or for a module's first loading); the caller
+ * holds the tensors meanwhile. */
+#define CALL(call)       \
+  int rc;                \
+  Py_BEGIN_ALLOW_THREADS \
+  rc = call;             \
+  Py_END_ALLOW_THREADS   \
+  return result(rc, err)
 #define ARGS(n)                                                                    \
   if (nargs != (n)) return PyErr_Format(PyExc_TypeError, "expected %d arguments", n)
 static int number(PyObject* o, long long* v) {
@@ -161,9 +169,8 @@ static PyObject* py_sample_window(PyObject* self, PyObject* const* a, Py_ssize_t
       vec(a[14], I32, dev, 1, 0, "status", &status))
     return NULL;
   STREAM(dev);
-  const int rc = fn.sample_window(indptr, nbr, eid, ts, N, P, nodes, times, n, window, sinks, o_nbr, o_eid, o_ts, cnt, first, len, status, stream,
-                                  err, sizeof err);
-  return result(rc, err);
+  CALL(fn.sample_window(indptr, nbr, eid, ts, N, P, nodes, times, n, window, sinks, o_nbr, o_eid, o_ts, cnt, first, len, status, stream,
+       err, sizeof err));
 }
 
 /* write, cache address, device, cache rows, heads, dim, rows, status, src, dst, times */
@@ -220,9 +227,8 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
   if (PyErr_Occurred() || vec(a[10], F64, dev, num, 0, "times", &times) || vec(a[7], I32, dev, 1, 0, "status", &status)) return NULL;
   STREAM(dev);
   void* p = (void*)(uintptr_t)base;
-  const int rc = write ? fn.cache_write(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err)
-                       : fn.cache_read(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err);
-  return result(rc, err);
+  CALL((write ? fn.cache_write(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err)
+              : fn.cache_read(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err)));
 }
 
 struct bias {
@@ -275,9 +281,8 @@ static PyObject* py_cached_attend(PyObject* self, PyObject* const* a, Py_ssize_t
     return NULL;
   STREAM(dev);
   const float s = (float)(a[11] == Py_None ? 1.0 / __builtin_sqrt((double)dim) : scale);
-  const int rc = fn.cached_attend(q, row_type(kind), k, v, n, (int)sh[1], first, len, b.table, b.buckets, b.bounds, b.times, b.ts, window, sinks,
-                                  max_len, s, out, status, stream, err, sizeof err);
-  return result(rc, err);
+  CALL(fn.cached_attend(q, row_type(kind), k, v, n, (int)sh[1], first, len, b.table, b.buckets, b.bounds, b.times, b.ts, window, sinks,
+       max_len, s, out, status, stream, err, sizeof err));
 }
 
 struct slots {
@@ -322,9 +327,8 @@ static PyObject* py_slot_attend(PyObject* self, PyObject* const* a, Py_ssize_t n
   void* out;
   if (slot_args(a, &s) || vec(a[9], s.kind, s.dev, s.values, 0, "out", &out)) return NULL;
   STREAM(s.dev);
-  const int rc = fn.slot_attend(s.q, s.k, s.v, row_type(s.kind), s.n, s.slots, s.heads, s.kv, s.dim, s.cnt, s.b.table, s.b.buckets, s.b.bounds,
-                                s.b.times, s.b.ts, s.scale, out, stream, err, sizeof err);
-  return result(rc, err);
+  CALL(fn.slot_attend(s.q, s.k, s.v, row_type(s.kind), s.n, s.slots, s.heads, s.kv, s.dim, s.cnt, s.b.table, s.b.buckets, s.b.bounds,
+       s.b.times, s.b.ts, s.scale, out, stream, err, sizeof err));
 }
 
 /* q, k, v, cnt, scale, bias, bounds, times, ts, dout, dq, dk, dv, dbias, scratch */
@@ -347,9 +351,8 @@ static PyObject* py_slot_attend_backward(PyObject* self, PyObject* const* a, Py_
     if (vec(a[14], F32, s.dev, need < 0 ? 0 : need, 1, "scratch", &scratch)) return NULL;
   }
   STREAM(s.dev);
-  const int rc = fn.slot_attend_backward(s.q, s.k, s.v, row_type(s.kind), s.n, s.slots, s.heads, s.kv, s.dim, s.cnt, s.b.table, s.b.buckets,
-                                         s.b.bounds, s.b.times, s.b.ts, s.scale, dout, dq, dk, dv, dbias, scratch, stream, err, sizeof err);
-  return result(rc, err);
+  CALL(fn.slot_attend_backward(s.q, s.k, s.v, row_type(s.kind), s.n, s.slots, s.heads, s.kv, s.dim, s.cnt, s.b.table, s.b.buckets,
+       s.b.bounds, s.b.times, s.b.ts, s.scale, dout, dq, dk, dv, dbias, scratch, stream, err, sizeof err));
 }
 
 /* (dtypes in the order of the enumeration), current device's and current stream's callables, (addresses of the entry points) */

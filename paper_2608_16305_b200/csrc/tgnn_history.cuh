@@ -1,6 +1,7 @@
 // What the history operators share (row cache, attention over it, slot attention): error texts, row types, the time
 // buckets and the view of a row cache.
 #pragma once
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 
@@ -33,14 +34,14 @@ inline bool known_dtype(int dtype) { return dtype == TGNN_F32 || dtype == TGNN_B
 // Values that a head's codes are padded to: the readers' tiles of 32, 64 or 128.
 inline int padded_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
 
-// Multiprocessors of the current device (asked for once per device; the answer cannot change).
+// Multiprocessors of the current device (asked for once per device, by any thread; the answer cannot change).
 inline int num_sms() {
-  static int cached[64] = {};
+  static std::atomic<int> cached[64];
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return 148;
-  if (dev >= 0 && dev < 64 && cached[dev]) return cached[dev];
+  if (dev >= 0 && dev < 64 && (n = cached[dev].load(std::memory_order_relaxed)) > 0) return n;
   if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
-  if (dev >= 0 && dev < 64) cached[dev] = n;
+  if (dev >= 0 && dev < 64) cached[dev].store(n, std::memory_order_relaxed);
   return n;
 }
 
