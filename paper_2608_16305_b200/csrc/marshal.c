@@ -33,15 +33,17 @@ static struct {
                               char*, int64_t);
 } fn;
 
-/* t.name() or t.name(i) as an integer; -1 where t has no such thing (what needed it then raises TypeError) */
+/* t.name() or t.name(i) as an integer.  -1 where t has no such thing, or one that gives no number (what needed it then raises TypeError), and where it
+ * raises: that exception stays, whatever is asked next says -1 as well, and the caller sees it. */
 static long long integer(PyObject* r) {
   const long long v = !r ? -1 : r == Py_True ? 1 : r == Py_False ? 0 : PyLong_AsLongLong(r);
   Py_XDECREF(r);
-  if (v == -1) PyErr_Clear();
+  if (v == -1 && PyErr_Occurred() && (PyErr_ExceptionMatches(PyExc_AttributeError) || PyErr_ExceptionMatches(PyExc_TypeError))) PyErr_Clear();
   return v;
 }
-static long long ask(PyObject* t, PyObject* name) { return integer(PyObject_CallMethodNoArgs(t, name)); }
+static long long ask(PyObject* t, PyObject* name) { return PyErr_Occurred() ? -1 : integer(PyObject_CallMethodNoArgs(t, name)); }
 static long long ask1(PyObject* t, PyObject* name, long i) {
+  if (PyErr_Occurred()) return -1;
   PyObject* arg = PyLong_FromLong(i);
   if (!arg) return -1;
   const long long v = integer(PyObject_CallMethodOneArg(t, name, arg));
@@ -49,9 +51,10 @@ static long long ask1(PyObject* t, PyObject* name, long i) {
   return v;
 }
 static int kind_of(PyObject* t) { /* -1: of no kind that is used here, or no tensor at all */
+  if (PyErr_Occurred()) return -1;
   PyObject* d = PyObject_GetAttr(t, s_dtype);
   if (!d) {
-    PyErr_Clear();
+    if (PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
     return -1;
   }
   Py_DECREF(d); /* dtypes live as long as the interpreter */
@@ -61,11 +64,24 @@ static int kind_of(PyObject* t) { /* -1: of no kind that is used here, or no ten
 }
 static int row_type(int kind) { return kind == F32 ? TGNN_F32 : kind == BF16 ? TGNN_BF16 : TGNN_F16; }
 
-static int refuse(PyObject* t, const char* name, const char* want, long long n, long long dev) {
+static int refuse(PyObject* t, const char* name, const char* want, long long n, long long dev) { /* an exception that is there stays */
+  const long long has = n >= 0 ? ask(t, s_numel) : 0;
+  if (PyErr_Occurred()) return -1;
   if (n >= 0) PyErr_Format(PyExc_TypeError, "%s: expected a contiguous %s tensor of %lld elements on CUDA device %lld, got %lld in a %s", name,
-                           want, n, dev, ask(t, s_numel), Py_TYPE(t)->tp_name);
+                           want, n, dev, has, Py_TYPE(t)->tp_name);
   else PyErr_Format(PyExc_TypeError, "%s: expected a %s tensor on a CUDA device, got a %s", name, want, Py_TYPE(t)->tp_name);
   return -1;
+}
+
+/* t.data_ptr(), which a tensor without storage raises for */
+static int address(PyObject* t, const char* name, void** out) {
+  const long long v = ask(t, s_data_ptr);
+  if (v == -1) { /* no tensor lies there */
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_TypeError, "%s: a %s has no address", name, Py_TYPE(t)->tp_name);
+    return -1;
+  }
+  *out = (void*)(uintptr_t)v;
+  return 0;
 }
 
 /* Address of a contiguous tensor of n elements (at least n, or any number where n < 0) on the device; None -> NULL.  -1: refused. */
@@ -76,8 +92,7 @@ static int vec(PyObject* t, int kind, long long dev, long long n, int at_least, 
   if (kind_of(t) != kind || ask(t, s_get_device) != dev || ask(t, s_is_contiguous) != 1) return refuse(t, name, g_name[kind], n, dev);
   const long long m = ask(t, s_numel);
   if (m < 0 || (at_least ? m < n : m != n)) return refuse(t, name, g_name[kind], n, dev);
-  *p = (void*)(uintptr_t)ask(t, s_data_ptr);
-  return 0;
+  return address(t, name, p);
 }
 
 /* The current stream of device dev, if it is the current device: 1; another one is current: 0; an exception is set: -1 */
@@ -134,11 +149,11 @@ static int small(PyObject* o, int* v) { /* an int of the C interface */
 }
 static int shape(PyObject* t, int dims, long long* out, const char* name) {
   if (ask(t, s_dim) != dims) {
-    PyErr_Format(PyExc_TypeError, "%s: expected a tensor of %d dimensions", name, dims);
+    if (!PyErr_Occurred()) PyErr_Format(PyExc_TypeError, "%s: expected a tensor of %d dimensions", name, dims);
     return -1;
   }
   for (int i = 0; i < dims; ++i) out[i] = ask1(t, s_size, i);
-  return 0;
+  return PyErr_Occurred() ? -1 : 0;
 }
 static int sizes_fit(const long long* v, int n) {
   for (int i = 0; i < n; ++i)
@@ -223,10 +238,9 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
   }
   double* times;
   int32_t* status;
-  const long long base = ask(rows, s_data_ptr);
-  if (PyErr_Occurred() || vec(a[10], F64, dev, num, 0, "times", &times) || vec(a[7], I32, dev, 1, 0, "status", &status)) return NULL;
+  void* p;
+  if (address(rows, "rows", &p) || vec(a[10], F64, dev, num, 0, "times", &times) || vec(a[7], I32, dev, 1, 0, "status", &status)) return NULL;
   STREAM(dev);
-  void* p = (void*)(uintptr_t)base;
   CALL((write ? fn.cache_write(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err)
               : fn.cache_read(c, p, row_type(kind), num, stride, idx[0], idx[1], bits, n, times, status, stream, err, sizeof err)));
 }

@@ -116,3 +116,58 @@ def test_other_threads_run_while_the_library_is_called(loaded, name):
     released.value = 1
     th.join()
     assert got == [None]
+
+
+class _Broken(Tensor):
+    def __init__(self, method, error, *a):
+        super().__init__(*a)
+
+        def fail(*args):
+            raise error
+        setattr(self, method, fail)
+
+
+def _tensors(name):
+    return [i for i, a in enumerate(_calls()[name]) if isinstance(a, Tensor)]
+
+
+@pytest.mark.parametrize("method", ["data_ptr", "numel", "get_device", "is_contiguous"])
+@pytest.mark.parametrize("name", list(_calls()))
+def test_what_a_tensors_method_raises_is_what_the_call_raises(loaded, name, method):
+    """A tensor without storage (a fake one) raises when it is asked for its address: the caller sees that, not an address that is refused."""
+    m, fake = loaded
+    C.c_int.in_dll(fake, "released").value = 1
+    for error in (RuntimeError("it has no storage"), KeyboardInterrupt()):
+        seen = 0
+        for i in _tensors(name):
+            args = _calls()[name]
+            args[i] = _Broken(method, error, args[i].dtype, *args[i].shape)
+            try:
+                assert _function(m, name)(*args) is None           # (not every tensor is asked everything)
+            except type(error) as e:
+                assert e is error
+                seen += 1
+        assert seen >= (len(_tensors(name)) if method == "data_ptr" else 1)
+
+
+@pytest.mark.parametrize("name", list(_calls()))
+def test_what_is_no_tensor_raises_type_error(loaded, name):
+    m, fake = loaded
+    C.c_int.in_dll(fake, "released").value = 1
+
+    class Bare:
+        pass
+    for i in _tensors(name):
+        for gone in ("data_ptr", "numel", "get_device"):
+            args = _calls()[name]
+            t, bare = args[i], Bare()
+            for method in ("get_device", "is_contiguous", "numel", "dim", "size", "stride", "data_ptr"):
+                if method != gone:
+                    setattr(bare, method, getattr(t, method))
+            bare.dtype = t.dtype
+            args[i] = bare
+            try:
+                assert _function(m, name)(*args) is None and gone != "data_ptr"
+            except TypeError as e:
+                assert str(e)
+    assert _function(m, name)(*_calls()[name]) is None             # and nothing of it is left behind
