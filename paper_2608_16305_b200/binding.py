@@ -323,6 +323,14 @@ def _call(name: str, *args) -> int:
     return TGNN_OK
 
 
+def record_bytes(heads: int, dim: int, bits: int, times: bool = True) -> int:
+    """Bytes of a row that is kept as one record: codes (a group of `dim` padded to 32, 64 or 128 values), time, scales, in steps of 16."""
+    if not (1 <= heads <= 1024 and 1 <= dim <= 128 and bits in (4, 8)):
+        raise TgnnError(TGNN_EINVAL, f"record of {heads} heads of {dim} values in {bits} bits")
+    codes = (32 if dim <= 32 else 64 if dim <= 64 else 128) * bits // 8
+    return (heads * codes + (8 if times else 0) + 2 * heads + 15) // 16 * 16
+
+
 class RowCache:
     """Rows of `heads` groups of `dim` values held in 4 or 8 bits, with a scale per group and (times) an fp64 time per row.
 
@@ -341,7 +349,7 @@ class RowCache:
         if record:
             at_time = heads * gb
             at_scale = at_time + (8 if times else 0)
-            self.record_bytes = (at_scale + 2 * heads + 15) // 16 * 16
+            self.record_bytes = record_bytes(heads, dim, bits, times)
             self.codes = self.scales = self.times = None
             self.data = torch.zeros((rows, self.record_bytes), dtype=torch.uint8, device=dev)
             p, r = self.data.data_ptr(), self.record_bytes

@@ -105,15 +105,21 @@ class BoundaryRefresh:
 
 
 class QuantisedRefresh(BoundaryRefresh):
-    """The same refresh with the rows in 8 or 4 bits on the wire: a record holds a row's codes, its scales (one per group of at most
-    128 values) and its last-update time, which stays exact.  For d = 100 a record takes 144 (8 bits) or 80 (4 bits) bytes instead of
-    408.  A received row is within half a step, amax / 127 or amax / 7 of its group, of the owner's."""
+    """The same refresh with the rows in 8 or 4 bits on the wire: a record holds a row's codes, its scales (one per group; the fewest groups of
+    at most 128 values that divide d) and its last-update time, which stays exact.  For d = 100 a record takes 144 (8 bits) or 80 (4 bits)
+    bytes instead of 408.  A received row is within half a step of the owner's; a step is the group's scale, amax / 127 or amax / 7 and up to 1/128
+    of that more, since scales are rounded up to bf16.  ValueError where the groups are so narrow that a record (they
+    are padded to 32, 64 or 128 values) would be no smaller than the fp32 row: d up to 10 (8 bits) or 6 (4 bits), and d whose largest divisor up
+    to 128 is at most 8 or 4."""
 
     def __init__(self, plan: RefreshPlan, d: int, bits: int = 8, group=None, cache: Callable = B.RowCache, write: Callable = B.cache_write,
                  read: Callable = B.cache_read):
         self.plan, self.d, self.group, self.bits = plan, d, group, bits
         self._write, self._read = write, read
         heads = next(h for h in range(1, d + 1) if d % h == 0 and d // h <= 128)
+        if heads > 1024 or B.record_bytes(heads, d // heads, bits) >= 4 * d + 8:
+            raise ValueError(f"rows of {d} values: a record of {heads} groups in {bits} bits is no smaller than the fp32 row of {4 * d + 8} bytes, "
+                             "which BoundaryRefresh sends")
         dev = plan.recv_nodes.device
         self.send = cache(plan.cap, heads, d // heads, bits, device=dev, record=True)
         self.recv = cache(plan.cap, heads, d // heads, bits, device=dev, record=True)
