@@ -6,6 +6,7 @@ import os
 import subprocess
 import sys
 import sysconfig
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -23,22 +24,39 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def _stale(built: str, deps) -> bool:
+    return not os.path.exists(built) or any(os.path.getmtime(p) > os.path.getmtime(built) for p in deps)
+
+
+def _headers():
+    return glob.glob(os.path.join(HERE, "..", "include", "*.h"))
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(MARSHAL):
-        return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(MARSHAL))
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.c")) + glob.glob(os.path.join(HERE, "..", "include", "*.h"))
-    return any(os.path.getmtime(p) > t for p in deps)
+    return _stale(LIB, sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + _headers())
+
+
+def build_marshal() -> None:
+    """The history operators' argument marshalling, which needs a C compiler and Python's headers.  Where it cannot be built there is none (nor an
+    older one), and everything but those operators works from Python; calling one says so."""
+    part = f"{MARSHAL}.{os.getpid()}"                 # put in place at once: other processes may be loading it
+    try:
+        subprocess.check_call([os.environ.get("CC", "gcc"), "-shared", "-fPIC", "-O2", "-Wall", "-I", sysconfig.get_paths()["include"], "-o", part,
+                               os.path.join(CSRC, "marshal.c")])
+        os.replace(part, MARSHAL)
+    except (OSError, subprocess.CalledProcessError) as e:
+        for p in (part, MARSHAL):
+            if os.path.exists(p):
+                os.remove(p)
+        warnings.warn(f"the history operators cannot be called from Python, their argument marshalling was not built: {e}")
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources()
-    subprocess.check_call(cmd)
-    subprocess.check_call([os.environ.get("CC", "gcc"), "-shared", "-fPIC", "-O2", "-Wall", "-I", sysconfig.get_paths()["include"], "-o", MARSHAL,
-                           os.path.join(CSRC, "marshal.c")])
+    if force or needs_build():
+        nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+        subprocess.check_call([nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + sources())
+    if force or _stale(MARSHAL, [os.path.join(CSRC, "marshal.c")] + _headers()):
+        build_marshal()
     return LIB
 
 
