@@ -33,7 +33,7 @@ def _headers():
 
 
 def needs_build() -> bool:
-    return _stale(LIB, sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + _headers())
+    return _stale(LIB, sources() + glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h")) + _headers())
 
 
 def build_marshal() -> None:

@@ -33,6 +33,7 @@
 // smallest calls are bound by the chain of dependent loads (length, rows, then the sums' meeting).
 #include <cooperative_groups.h>
 
+#include "attend_shape.h"
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
@@ -40,7 +41,7 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int WARPS = 4;
+constexpr int WARPS = kAttendWarps;
 constexpr float kLo = 2048.f;             // lo terms are held times 2^11, clear of fp16's subnormals
 
 struct AttendArgs {
@@ -689,59 +690,53 @@ __global__ void __launch_bounds__(32 * WARPS, DP * NH >= 256 ? 2 : DP >= 128 || 
   }
 }
 
-// Warps on one unit: by warp, unless the units leave most of the machine's warps without work and a unit has more tiles than
-// a warp should walk alone.  By warp, a warp takes all units of a root where they have a single tile and the roots alone fill the
-// machine (14 400 roots of 21 entries: 51 against 55 us; with more tiles single units balance better, 278 against 315 us for 12 000
-// roots of 520).
-struct Shape {
-  bool by_block;
-  int ranks, take;
-};
-Shape choose(int64_t roots, int per_root, int64_t tiles) {
-  const int64_t units = roots * per_root;
-  const int64_t machine = (int64_t)num_sms() * 12;                   // warps that are resident together
-  Shape s = {false, 1, tiles <= 1 && roots >= machine ? per_root : 1};
-  if (tiles <= 2 || units >= 2 * machine) return s;
-  s.by_block = true;
-  while (s.ranks < 16 && units * WARPS * s.ranks * 2 <= machine && tiles >= 2 * WARPS * s.ranks * 2) s.ranks *= 2;
-  return s;
-}
-
+// Launches over `roots` roots whose windows have up to `tiles` tiles.
 template <int BITS, int DP, int NH>
-cudaError_t launch(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
+cudaError_t launch(AttendArgs& a, int64_t roots, int64_t tiles, cudaStream_t s) {
+  const auto by_block = cached_attend_kernel<BITS, DP, NH, true>;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.blockDim = dim3(32 * WARPS);
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  auto of = [&](int ranks) {
+    cfg.gridDim = dim3(a.units * (unsigned)ranks);
+    at[0].val.clusterDim.x = (unsigned)ranks;
+  };
+  // Above the portable size a cluster has to be allowed, per kernel and device, and a device (or the part of it that the context has) may hold none.
+  auto fits = [&](int ranks) {
+    of(ranks);
+    int clusters = 0;
+    const bool ok = cudaFuncSetAttribute(by_block, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                    cudaOccupancyMaxActiveClusters(&clusters, by_block, &cfg) == cudaSuccess && clusters > 0;
+    if (!ok) cudaGetLastError();
+    return ok;
+  };
+  const AttendShape sh = choose_attend_shape(roots, a.kv_heads * a.passes, tiles, num_sms(), fits);
+  a.take = sh.take;
   if (!sh.by_block) {
     const unsigned per = (unsigned)(WARPS * a.take);
     cached_attend_kernel<BITS, DP, NH, false><<<(a.units + per - 1) / per, 32 * WARPS, 0, s>>>(a);
     return cudaGetLastError();
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.units * (unsigned)sh.ranks);
-  cfg.blockDim = dim3(32 * WARPS);
-  cfg.stream = s;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)sh.ranks;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  if (sh.ranks > 8) {               // above the portable size: to be allowed per kernel and device
-    const cudaError_t e = cudaFuncSetAttribute(cached_attend_kernel<BITS, DP, NH, true>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-  }
-  return cudaLaunchKernelEx(&cfg, cached_attend_kernel<BITS, DP, NH, true>, a);
+  of(sh.ranks);
+  return cudaLaunchKernelEx(&cfg, by_block, (const AttendArgs)a);
 }
 
 template <int BITS, int DP>
-cudaError_t launch_heads(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
-  return a.group > 4 ? launch<BITS, DP, 2>(a, sh, s) : a.group > 1 ? launch<BITS, DP, 1>(a, sh, s) : launch<BITS, DP, 0>(a, sh, s);
+cudaError_t launch_heads(AttendArgs& a, int64_t roots, int64_t tiles, cudaStream_t s) {
+  return a.group > 4 ? launch<BITS, DP, 2>(a, roots, tiles, s) : a.group > 1 ? launch<BITS, DP, 1>(a, roots, tiles, s) : launch<BITS, DP, 0>(a, roots, tiles, s);
 }
 
 template <int BITS>
-cudaError_t launch_dim(const AttendArgs& a, const Shape& sh, cudaStream_t s) {
+cudaError_t launch_dim(AttendArgs& a, int64_t roots, int64_t tiles, cudaStream_t s) {
   switch (padded_dim(a.dim)) {
-    case 32: return launch_heads<BITS, 32>(a, sh, s);
-    case 64: return launch_heads<BITS, 64>(a, sh, s);
-    default: return launch_heads<BITS, 128>(a, sh, s);
+    case 32: return launch_heads<BITS, 32>(a, roots, tiles, s);
+    case 64: return launch_heads<BITS, 64>(a, roots, tiles, s);
+    default: return launch_heads<BITS, 128>(a, roots, tiles, s);
   }
 }
 
@@ -808,10 +803,9 @@ extern "C" int tgnn_cached_attend(const void* q, int dtype, const tgnn_cache* k_
   if (max_len > 0 && max_len < see) see = max_len;
   if (k.rows < see) see = k.rows;
   const int tk = k.bits * padded_dim(k.dim) >= 1024 ? 16 : 32;
-  const Shape sh = choose(n, k.heads * a.passes, (see + tk - 1) / tk);
-  a.take = sh.take;
+  const int64_t tiles = (see + tk - 1) / tk;
   a.pairs = k.dim % 2 == 0 && (((uintptr_t)q | (uintptr_t)out) & (2 * es + 1)) == 0;
-  const cudaError_t e = k.bits == 4 ? launch_dim<4>(a, sh, (cudaStream_t)stream) : launch_dim<8>(a, sh, (cudaStream_t)stream);
+  const cudaError_t e = k.bits == 4 ? launch_dim<4>(a, n, tiles, (cudaStream_t)stream) : launch_dim<8>(a, n, tiles, (cudaStream_t)stream);
   if (e != cudaSuccess) {
     cudaGetLastError();
     return fail(err_host, err_size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(e));
