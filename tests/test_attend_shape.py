@@ -57,3 +57,11 @@ def test_work_is_shared_out_once(shape):
                     assert ranks in (1, 2, 4, 8, 16) and take in (1, per_root)
                     assert (ranks == 1 or by_block) and (take == 1 or not by_block) and (take == 1 or tiles <= 1) and (not by_block or tiles > 2)
                     assert ranks == 1 or 4 * ranks <= tiles
+
+
+def test_short_windows_of_many_units_go_by_warp(shape):
+    """1700 roots of two heads over three tiles have a warp each (a block each took 22.7 us, a warp each 16.5); over long windows a block each up to
+    twice as many units."""
+    assert shape(1700, 2, 3)[0] is False and shape(1776, 1, 16)[0] is False
+    assert shape(880, 2, 3)[0] is True and shape(1775, 1, 16)[0] is True
+    assert shape(1776, 1, 17)[0] is True and shape(3551, 1, 125)[0] is True and shape(3552, 1, 125)[0] is False
