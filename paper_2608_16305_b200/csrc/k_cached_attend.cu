@@ -231,11 +231,6 @@ struct Rows {
   }
 };
 
-// A unit's running sums over the tiles that one warp walks, for 4 NH heads; NH = 0: for a single one, which then fills all columns, so
-// that every lane has its logits and takes one key of the tile to itself (11 % less time than as one of four heads).
-// Lane (g, c) has head c of every four: its logits at keys
-// 16 b + g and 16 b + g + 8, its output columns g VD + i at o[i / 2][.][2 (i & 1) + {hi, lo}] in units of sc, its sum l over the
-// lane's own keys until finish().
 // The largest of a warp's values, NaN left out.
 __device__ __forceinline__ float max_warp(float x) {
   float r;
@@ -243,6 +238,11 @@ __device__ __forceinline__ float max_warp(float x) {
   return r;
 }
 
+// A unit's running sums over the tiles that one warp walks, for 4 NH heads; NH = 0: for a single one, which then fills all columns, so
+// that every lane has its logits and takes one key of the tile to itself (11 % less time than as one of four heads).
+// Lane (g, c) has head c of every four: its logits at keys
+// 16 b + g and 16 b + g + 8, its output columns g VD + i at o[i / 2][.][2 (i & 1) + {hi, lo}] in units of sc, its sum l over the
+// lane's own keys until finish().
 template <int BITS, int DP, int NH>
 struct Walk {
   using T = Tile<BITS, DP>;
@@ -306,14 +306,14 @@ struct Walk {
     __syncwarp();                                                    // the next unit's query may be written
   }
 
-  // The query: lane (g, c) holds columns [c DP / 4, (c + 1) DP / 4) of head g / 2 of every four, the hi terms where g is even, lo
+  // The query of several heads: lane (g, c) holds columns [c DP / 4, (c + 1) DP / 4) of head g / 2 of every four, the hi terms where g is even, lo
   // where it is odd, divided by a power of two.
   __device__ __forceinline__ void begin(const AttendArgs& a, int64_t root, int head0, int nh) {
     const int lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
     none();
 #pragma unroll
     for (int x = 0; x < X; ++x) {
-      const int h = ONE ? 0 : 4 * x + (g >> 1);
+      const int h = 4 * x + (g >> 1);
       float q[DP / 4];
       load_query<DP / 4>(a, (root * a.heads + head0 + h) * a.dim, c * (DP / 4), h < nh, q);
       float top = 0.f;
