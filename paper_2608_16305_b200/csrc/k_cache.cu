@@ -21,8 +21,6 @@
 //
 // Measured on a B200, a million rows of 4 x 64 in bf16 at random places, in 4 bits: written in 141 us (4.8 TB/s of DRAM), read back in
 // 138 us (4.7); a copy of whole tables reaches 6.5.
-#include <type_traits>
-
 #include "tgnn_history.cuh"
 
 using namespace tgnn_history;
@@ -103,8 +101,8 @@ __device__ __forceinline__ void store8(T* row, int e0, int dim, const float (&v)
   }
 }
 
-// The group's scale (the bits of a bf16) from its largest magnitude, and the codes of PIECES times 8 of its values.
-template <int BITS, int PIECES>
+// The group's scale (the bits of a bf16) from its largest magnitude, and the codes of two times 8 of its values.
+template <int BITS>
 __device__ __forceinline__ uint16_t quantise(float amax, const float (*v)[8], uint32_t (*code)[BITS == 4 ? 1 : 2]) {
   const bool bad = !(amax <= 3.4028234e38f);
   float s = __uint_as_float((__float_as_uint(__fmul_rn(amax, BITS == 4 ? 1.f / 7.f : 1.f / 127.f)) + 0xffffu) & 0xffff0000u);
@@ -114,7 +112,7 @@ __device__ __forceinline__ uint16_t quantise(float amax, const float (*v)[8], ui
   constexpr float kMagic = 12582912.f + (BITS == 4 ? 8.f : 128.f);
   constexpr int PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p) {
+  for (int p = 0; p < 2; ++p) {
 #pragma unroll
     for (int q = 0; q < WORDS; ++q) {
       uint32_t acc = 0, fixed = 0;
@@ -177,7 +175,7 @@ __global__ void __launch_bounds__(THREADS) cache_write_kernel(const Move a, cons
       if (lanes > 4) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, 4));
       constexpr int WORDS = BITS == 4 ? 1 : 2;
       uint32_t code[2][WORDS];
-      const uint16_t sb = quantise<BITS, 2>(amax, v, code);
+      const uint16_t sb = quantise<BITS>(amax, v, code);
       if (w.place >= 0 && h + u < a.c.heads) {
         if constexpr (BITS == 4) {
           reinterpret_cast<uint32_t*>(to + u * a.c.code_bytes)[l] = code[0][0];
@@ -247,13 +245,13 @@ __global__ void __launch_bounds__(THREADS, VB == 16 ? 8 : 1) cache_read_kernel(c
   }
 }
 
-// Rows whose heads start on no word of several values (odd heads, odd bases): read value by value in the order of the codes, the lanes
-// of a warp would touch a sector each.  Here a warp moves 32 / lanes whole groups (heads of rows, numbered row by row) in words of VB bytes that
-// lie side by side, and hands the values over in shared memory, as fp32; the codes' side is as above, 8 values per lane.  A group's
-// place in shared memory is a multiple of 8 and one long, which spreads the lanes' reads over the banks.
-template <typename T, int VB, int BITS, bool WRITE>
-__global__ void __launch_bounds__(THREADS) cache_narrow_kernel(const Move a, typename std::conditional<WRITE, const T, T>::type* __restrict__ rows) {
-  constexpr int VE = VB / (int)sizeof(T), N = 8 / VE, PER = BITS == 4 ? 8 : 4, WORDS = 8 / PER;
+// Reading into rows whose heads start on no word of several values (odd heads, odd bases): written value by value in the order of the codes, the
+// lanes of a warp would touch a sector each.  Here a warp moves 32 / lanes whole groups (heads of rows, numbered row by row): 8 values per lane as above
+// go to shared memory, as fp32, and from there in words of VB bytes that lie side by side.  A group's
+// place in shared memory is a multiple of 8 and one long, which spreads the lanes' accesses over the banks.
+template <typename T, int VB, int BITS>
+__global__ void __launch_bounds__(THREADS) cache_read_narrow_kernel(const Move a, T* __restrict__ rows) {
+  constexpr int VE = VB / (int)sizeof(T), N = 8 / VE, WORDS = BITS == 4 ? 1 : 2;
   typedef typename Vec<VB>::type W;
   union Word { W w; T x[VE]; };
   __shared__ float s_values[THREADS / 32][256 + 8];
@@ -266,80 +264,42 @@ __global__ void __launch_bounds__(THREADS) cache_narrow_kernel(const Move a, typ
   if (lane < count && g < (uint64_t)a.n * a.c.heads) {
     const uint32_t i = (uint32_t)g / (uint32_t)a.c.heads;
     head = (int)((uint32_t)g - i * (uint32_t)a.c.heads);
-    w = find<WRITE>(a, i);
+    w = find<false>(a, i);
   }
-  if (a.times && head == 0 && (WRITE ? w.place : w.row) >= 0) {
-    double* in_cache = reinterpret_cast<double*>(a.c.times + (uint64_t)(uint32_t)w.place * (uint32_t)a.c.time_stride);
-    if (WRITE) *in_cache = w.row >= 0 ? __ldg(a.times + w.row) : 0.0;
-    else a.times[w.row] = w.place >= 0 ? __ldg(in_cache) : 0.0;
-  }
+  if (a.times && head == 0 && w.row >= 0)
+    a.times[w.row] = w.place >= 0 ? __ldg(reinterpret_cast<const double*>(a.c.times + (uint64_t)(uint32_t)w.place * (uint32_t)a.c.time_stride)) : 0.0;
   const int64_t row_at = w.row < 0 ? -1 : (int64_t)((uint64_t)(uint32_t)w.row * a.row_bytes) + (int64_t)head * a.c.dim * (int)sizeof(T);
   const int per = a.c.dim / VE, magic = (65536 + per - 1) / per;     // word x of the warp belongs to group (x * magic) >> 16: exact below 256
   const int own = lane >> lg, l = lane & (lanes - 1);                // the lane's group and its 8 values there
   const int64_t place = __shfl_sync(FULL, w.place, own);
   const int own_head = __shfl_sync(FULL, head, own);
-  uint8_t* codes = a.c.codes + (uint64_t)(uint32_t)place * (uint32_t)a.c.code_stride + own_head * a.c.code_bytes;
-  uint16_t* scale = reinterpret_cast<uint16_t*>(a.c.scales + (uint64_t)(uint32_t)place * (uint32_t)a.c.scale_stride) + own_head;
-  if constexpr (WRITE) {
-    Word raw[N];
-    int at[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int x = lane + 32 * j, grp = min((x * magic) >> 16, count - 1), off = x - grp * per;
-      const int64_t from = __shfl_sync(FULL, row_at, grp);
-      at[j] = off < per ? grp * ld + off * VE : -1;
-      raw[j].w = W();
-      if (off < per && from >= 0) raw[j].w = __ldg(reinterpret_cast<const W*>(reinterpret_cast<const uint8_t*>(rows) + from) + off);
+  uint32_t code[WORDS] = {};
+  uint32_t sb = 0;
+  if (place >= 0) {
+    const uint8_t* codes = a.c.codes + (uint64_t)place * (uint32_t)a.c.code_stride + own_head * a.c.code_bytes;
+    if constexpr (BITS == 4) {
+      code[0] = __ldg(reinterpret_cast<const uint32_t*>(codes) + l);
+    } else {
+      const uint2 p = __ldg(reinterpret_cast<const uint2*>(codes) + l);
+      code[0] = p.x;
+      code[WORDS - 1] = p.y;
     }
+    sb = __ldg(reinterpret_cast<const uint16_t*>(a.c.scales + (uint64_t)place * (uint32_t)a.c.scale_stride) + own_head);
+  }
+  float v[8];
+  values<T, BITS>(code, __uint_as_float(sb << 16), v);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      if (at[j] >= 0) {
+  for (int j = 0; j < 8; ++j) mine[own * ld + 8 * l + j] = v[j];
+  __syncwarp();
 #pragma unroll
-        for (int e = 0; e < VE; ++e) mine[at[j] + e] = to_float<T>(raw[j].x[e]);
-      }
-    }
-    __syncwarp();
-    float v[8], amax = 0.f;
+  for (int j = 0; j < N; ++j) {
+    const int x = lane + 32 * j, grp = min((x * magic) >> 16, count - 1), off = x - grp * per;
+    const int64_t to = __shfl_sync(FULL, row_at, grp);
+    if (off < per && to >= 0) {
+      Word out;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      v[j] = 8 * l + j < a.c.dim ? mine[own * ld + 8 * l + j] : 0.f;
-      amax = max_nan(amax, fabsf(v[j]));
-    }
-    for (int o = 1; o < lanes; o <<= 1) amax = max_nan(amax, __shfl_xor_sync(FULL, amax, o));
-    uint32_t code[WORDS];
-    const uint16_t sb = quantise<BITS, 1>(amax, &v, &code);
-    if (place < 0) return;
-    if constexpr (BITS == 4) reinterpret_cast<uint32_t*>(codes)[l] = code[0];
-    else reinterpret_cast<uint2*>(codes)[l] = make_uint2(code[0], code[WORDS - 1]);
-    if (l == 0) *scale = sb;
-  } else {
-    uint32_t code[WORDS] = {};
-    uint32_t sb = 0;
-    if (place >= 0) {
-      if constexpr (BITS == 4) {
-        code[0] = __ldg(reinterpret_cast<const uint32_t*>(codes) + l);
-      } else {
-        const uint2 p = __ldg(reinterpret_cast<const uint2*>(codes) + l);
-        code[0] = p.x;
-        code[WORDS - 1] = p.y;
-      }
-      sb = __ldg(scale);
-    }
-    float v[8];
-    values<T, BITS>(code, __uint_as_float(sb << 16), v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) mine[own * ld + 8 * l + j] = v[j];
-    __syncwarp();
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int x = lane + 32 * j, grp = min((x * magic) >> 16, count - 1), off = x - grp * per;
-      const int64_t to = __shfl_sync(FULL, row_at, grp);
-      if (off < per && to >= 0) {
-        Word out;
-#pragma unroll
-        for (int e = 0; e < VE; ++e) out.x[e] = from_float<T>(mine[grp * ld + off * VE + e]);
-        reinterpret_cast<W*>(reinterpret_cast<uint8_t*>(rows) + to)[off] = out.w;
-      }
+      for (int e = 0; e < VE; ++e) out.x[e] = from_float<T>(mine[grp * ld + off * VE + e]);
+      reinterpret_cast<W*>(reinterpret_cast<uint8_t*>(rows) + to)[off] = out.w;
     }
   }
 }
@@ -347,7 +307,7 @@ __global__ void __launch_bounds__(THREADS) cache_narrow_kernel(const Move a, typ
 template <bool WRITE, typename T, int VB, int BITS, int U>
 void launch_heads(const Move& a, void* rows, cudaStream_t s) {
   const unsigned grid = (unsigned)((((uint64_t)a.n << a.lg) + THREADS - 1) / THREADS);
-  if (WRITE) cache_write_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
+  if constexpr (WRITE) cache_write_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (const T*)rows);
   else cache_read_kernel<T, VB, BITS, U><<<grid, THREADS, 0, s>>>(a, (T*)rows);
 }
 template <bool WRITE, typename T, int VB, int BITS>
@@ -355,16 +315,17 @@ void launch_rows(const Move& a, void* rows, cudaStream_t s) {
   if (a.c.heads == 1) launch_heads<WRITE, T, VB, BITS, 1>(a, rows, s);
   else launch_heads<WRITE, T, VB, BITS, 2>(a, rows, s);
 }
-template <bool WRITE, typename T, int VB, int BITS>
-void launch_narrow(const Move& a, void* rows, cudaStream_t s) {
+template <typename T, int VB, int BITS>
+void launch_read_narrow(const Move& a, void* rows, cudaStream_t s) {
   const uint64_t lanes = ((uint64_t)a.n * a.c.heads) << (a.lg + 1);
-  cache_narrow_kernel<T, VB, BITS, WRITE><<<(unsigned)((lanes + THREADS - 1) / THREADS), THREADS, 0, s>>>(
-      a, (typename std::conditional<WRITE, const T, T>::type*)rows);
+  cache_read_narrow_kernel<T, VB, BITS><<<(unsigned)((lanes + THREADS - 1) / THREADS), THREADS, 0, s>>>(a, (T*)rows);
 }
 
-// Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8 or 4; by way of shared memory where that
-// is a single value, and for pairs in fp32 of heads up to 64 wide.  250 000 rows written in 4 bits and read, without the detour and with it:
-// 8 x 25 in fp32 443 and 237 us, 8 x 43 579 and 446, 8 x 50 440 and 376; but 4 x 86 314 and 372, 8 x 50 in bf16 289 and 373.
+// Rows move in words of 16 bytes where base, row stride and head all start on one, else of 8, 4 or 2.  They are read by way of shared memory where
+// that is a single value, and for pairs in fp32 of heads up to 64 wide, and always written straight from their words.
+// 250 000 rows, straight and by shared memory, us.  Read from 4 bits: 8 x 25 in fp32 265 and 105, 8 x 43 347 and 199, 8 x 50 224 and 169,
+// 8 x 43 in bf16 382 and 200, but 4 x 86 in fp32 164 and 164, 8 x 50 in bf16 139 and 169.  Written: 8 x 25 in fp32 118 and 119, 8 x 43 149 and 234, 8 x 50 103
+// and 192, 8 x 43 in bf16 128 and 240.
 template <bool WRITE, typename T, int BITS>
 void launch_aligned(const Move& a, void* rows, cudaStream_t s) {
   constexpr int ES = (int)sizeof(T);
@@ -372,13 +333,16 @@ void launch_aligned(const Move& a, void* rows, cudaStream_t s) {
   if ((at & 15) == 0) {
     launch_rows<WRITE, T, 16, BITS>(a, rows, s);
   } else if ((at & 7) == 0) {
-    if (ES == 4 && a.c.dim <= 64) launch_narrow<WRITE, T, 8, BITS>(a, rows, s);
-    else launch_rows<WRITE, T, 8, BITS>(a, rows, s);
-  } else if constexpr (ES == 2) {
-    if ((at & 3) == 0) launch_rows<WRITE, T, 4, BITS>(a, rows, s);
-    else launch_narrow<WRITE, T, 2, BITS>(a, rows, s);
+    if constexpr (!WRITE && ES == 4) {
+      if (a.c.dim <= 64) return launch_read_narrow<T, 8, BITS>(a, rows, s);
+    }
+    launch_rows<WRITE, T, 8, BITS>(a, rows, s);
+  } else if (ES == 2 && (at & 3) == 0) {
+    if constexpr (ES == 2) launch_rows<WRITE, T, 4, BITS>(a, rows, s);
+  } else if constexpr (WRITE) {
+    launch_rows<WRITE, T, ES, BITS>(a, rows, s);
   } else {
-    launch_narrow<WRITE, T, 4, BITS>(a, rows, s);
+    launch_read_narrow<T, ES, BITS>(a, rows, s);
   }
 }
 
