@@ -68,3 +68,72 @@ def test_calls_of_two_threads_that_need_different_amounts_of_shared_memory():
     for j, w in zip(jobs, want):
         for a, b in zip(j.out, w):
             assert a is None or torch.equal(a, b)
+
+
+def test_python_threads_that_score_and_train_at_once():
+    """Two Python threads on streams of their own through the public operators (the interpreter is free during a call): each gets what it gets alone."""
+    from paper_2608_16305_b200 import history as H
+    from paper_2608_16305_b200 import workload as wl
+    import numpy as np
+    cfg = wl.scaled(wl.CONFIGS["tiny"], num_events=2000)
+    s = wl.make_stream(cfg)
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    h = H.EventHistory(dev(s.indptr), dev(s.nbr), dev(s.eid), dev(s.ts), 2, 50, 1000, 2, 4)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    mk = lambda *sh: torch.randn(*sh, generator=g, device="cuda")
+    P, R, S = h.ts.numel(), 300, 30
+    h.append(torch.arange(P, device="cuda"), mk(P, 2, 50), mk(P, 2, 50))
+    nodes = torch.randint(0, cfg.num_nodes, (R,), generator=g, device="cuda", dtype=torch.int32)
+    times = torch.full((R,), 1e9, dtype=torch.float64, device="cuda")
+    bias = H.TimeBias.logarithmic(2, 16, 1.0, 3000.0)
+    bias.table.normal_(generator=g)
+    q, k, v = mk(R, 2, 50), mk(R, S, 2, 50).requires_grad_(), mk(R, S, 2, 50).requires_grad_()
+    cnt = torch.full((R,), S, dtype=torch.int32, device="cuda")
+    ts = 1e9 * torch.rand(R, S, generator=g, device="cuda", dtype=torch.float64)
+    score = lambda: [h.attend(q, nodes, times, bias), h.attend(q[:3].contiguous(), nodes[:3], times[:3], bias)]
+    train = lambda: list(torch.autograd.grad(H.slot_attention(q, k, v, cnt, bias, times, ts).square().sum(), (k, v)))
+    want = [score(), train()]
+    torch.cuda.synchronize()
+    got, start = [[], []], threading.Barrier(2)
+
+    def work(i, f):
+        torch.cuda.set_device(0)
+        start.wait()
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(100):
+                got[i].append(f())
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=work, args=a) for a in ((0, score), (1, train))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for res, w in zip(got, want):
+        assert len(res) == 100
+        for r in res:
+            assert all(torch.equal(a, b) for a, b in zip(r, w))
+
+
+@pytest.mark.parametrize("roots,length", [(3, 40000), (3, 300), (200, 9000), (5000, 100)])
+def test_every_launch_shape_captured(roots, length):
+    """Clusters of 16 blocks and fewer, blocks and warps per unit, in a graph: what is asked of the device before a launch is allowed there."""
+    from paper_2608_16305_b200 import binding as B
+    P, st = length + 50, torch.zeros(1, dtype=torch.int32, device="cuda")
+    k, v = B.RowCache(P, 1, 50, 4), B.RowCache(P, 1, 50, 4)
+    g = torch.Generator(device="cuda").manual_seed(roots)
+    B.cache_write(k, torch.randn(P, 1, 50, generator=g, device="cuda"), st)
+    B.cache_write(v, torch.randn(P, 1, 50, generator=g, device="cuda"), st)
+    q = torch.randn(roots, 1, 50, generator=g, device="cuda")
+    first = torch.randint(0, 50, (roots,), generator=g, device="cuda")
+    n = torch.full((roots,), length, dtype=torch.int32, device="cuda")
+    out, again = torch.zeros_like(q), torch.zeros_like(q)
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        B.cached_attend(q, k, v, first, n, length, 0, out, st)
+    for _ in range(2):
+        q.normal_(generator=g)
+        graph.replay()
+        B.cached_attend(q, k, v, first, n, length, 0, again, st)
+        assert torch.equal(out, again) and out.abs().sum() > 0
+    assert int(st.item()) == 0
