@@ -8,7 +8,8 @@
 // Both products run on the tensor cores (m16n8k16, fp16 operands, fp32 sums) although a root has a single query: what they save is not
 // the multiplications but the conversion of every code to fp32 and the sums across lanes.  Codes are the 16-row operand (16 keys,
 // or 16 columns of the values), queries and weights the 8 columns: two for each of four query heads that share a cached head.
-// Those two hold a number x as hi + lo / 2048 in fp16 (22 bits), and both products of a head end up in one thread.
+// Those two hold a number x as hi + lo / 2048 in fp16 (22 bits), and both products of a head end up in one thread.  (Weights below 2^-14 of the
+// largest have fewer, those below 2^-36 of it are lost: less than fp32's sums lose beside the largest.)
 // Codes go in as fp16 integers (exact), centred: their bits under the exponent of 1024 minus 1024 and the stored offset.  (Under a zero
 // exponent a mask alone would unpack them, but the tensor core lines products up by their nominal exponents, and sums of such
 // numbers came out at 2^-17.)  Scales are applied to the other side: ks_j to the finished logits, vs_j to the weights.  fp16's range is
