@@ -34,16 +34,16 @@ static struct {
 } fn;
 
 /* t.name() or t.name(i) as an integer.  -1 where t has no such thing, or one that gives no number (what needed it then raises TypeError), and where it
- * raises: that exception stays, whatever is asked next says -1 as well, and the caller sees it. */
+ * raises: that exception stays, and nothing is asked after it but for the caller to see it (failed() looks, at answers below 0 only). */
 static long long integer(PyObject* r) {
   const long long v = !r ? -1 : r == Py_True ? 1 : r == Py_False ? 0 : PyLong_AsLongLong(r);
   Py_XDECREF(r);
   if (v == -1 && PyErr_Occurred() && (PyErr_ExceptionMatches(PyExc_AttributeError) || PyErr_ExceptionMatches(PyExc_TypeError))) PyErr_Clear();
   return v;
 }
-static long long ask(PyObject* t, PyObject* name) { return PyErr_Occurred() ? -1 : integer(PyObject_CallMethodNoArgs(t, name)); }
+static int failed(long long v) { return v < 0 && PyErr_Occurred(); }
+static long long ask(PyObject* t, PyObject* name) { return integer(PyObject_CallMethodNoArgs(t, name)); }
 static long long ask1(PyObject* t, PyObject* name, long i) {
-  if (PyErr_Occurred()) return -1;
   PyObject* arg = PyLong_FromLong(i);
   if (!arg) return -1;
   const long long v = integer(PyObject_CallMethodOneArg(t, name, arg));
@@ -51,7 +51,6 @@ static long long ask1(PyObject* t, PyObject* name, long i) {
   return v;
 }
 static int kind_of(PyObject* t) { /* -1: of no kind that is used here, or no tensor at all */
-  if (PyErr_Occurred()) return -1;
   PyObject* d = PyObject_GetAttr(t, s_dtype);
   if (!d) {
     if (PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
@@ -65,11 +64,18 @@ static int kind_of(PyObject* t) { /* -1: of no kind that is used here, or no ten
 static int row_type(int kind) { return kind == F32 ? TGNN_F32 : kind == BF16 ? TGNN_BF16 : TGNN_F16; }
 
 static int refuse(PyObject* t, const char* name, const char* want, long long n, long long dev) { /* an exception that is there stays */
-  const long long has = n >= 0 ? ask(t, s_numel) : 0;
   if (PyErr_Occurred()) return -1;
+  const long long has = n >= 0 ? ask(t, s_numel) : 0;
+  if (failed(has)) return -1;
   if (n >= 0) PyErr_Format(PyExc_TypeError, "%s: expected a contiguous %s tensor of %lld elements on CUDA device %lld, got %lld in a %s", name,
                            want, n, dev, has, Py_TYPE(t)->tp_name);
   else PyErr_Format(PyExc_TypeError, "%s: expected a %s tensor on a CUDA device, got a %s", name, want, Py_TYPE(t)->tp_name);
+  return -1;
+}
+static int refuse_vec(PyObject* t, const char* name, int kind, long long n, int at_least, long long dev) {
+  if (!at_least || PyErr_Occurred()) return refuse(t, name, g_name[kind], n, dev);
+  PyErr_Format(PyExc_TypeError, "%s: expected a contiguous %s tensor of at least %lld elements on CUDA device %lld, got a %s", name, g_name[kind], n, dev,
+               Py_TYPE(t)->tp_name);
   return -1;
 }
 
@@ -84,15 +90,20 @@ static int address(PyObject* t, const char* name, void** out) {
   return 0;
 }
 
-/* Address of a contiguous tensor of n elements (at least n, or any number where n < 0) on the device; None -> NULL.  -1: refused. */
-static int vec(PyObject* t, int kind, long long dev, long long n, int at_least, const char* name, void* out) {
+/* Address of a contiguous tensor on the device of n elements, or at least n; *has = how many there are.  None -> NULL and -1.  -1: refused. */
+static int vec_n(PyObject* t, int kind, long long dev, long long n, int at_least, const char* name, void* out, long long* has) {
   void** p = (void**)out;
   *p = NULL;
+  *has = -1;
   if (t == Py_None) return 0;
-  if (kind_of(t) != kind || ask(t, s_get_device) != dev || ask(t, s_is_contiguous) != 1) return refuse(t, name, g_name[kind], n, dev);
-  const long long m = ask(t, s_numel);
-  if (m < 0 || (at_least ? m < n : m != n)) return refuse(t, name, g_name[kind], n, dev);
+  if (kind_of(t) != kind || ask(t, s_get_device) != dev || ask(t, s_is_contiguous) != 1) return refuse_vec(t, name, kind, n, at_least, dev);
+  *has = ask(t, s_numel);
+  if (*has < 0 || (at_least ? *has < n : *has != n)) return refuse_vec(t, name, kind, n, at_least, dev);
   return address(t, name, p);
+}
+static int vec(PyObject* t, int kind, long long dev, long long n, int at_least, const char* name, void* out) {
+  long long has;
+  return vec_n(t, kind, dev, n, at_least, name, out, &has);
 }
 
 /* The current stream of device dev, if it is the current device: 1; another one is current: 0; an exception is set: -1 */
@@ -152,8 +163,11 @@ static int shape(PyObject* t, int dims, long long* out, const char* name) {
     if (!PyErr_Occurred()) PyErr_Format(PyExc_TypeError, "%s: expected a tensor of %d dimensions", name, dims);
     return -1;
   }
-  for (int i = 0; i < dims; ++i) out[i] = ask1(t, s_size, i);
-  return PyErr_Occurred() ? -1 : 0;
+  for (int i = 0; i < dims; ++i) {
+    out[i] = ask1(t, s_size, i);
+    if (failed(out[i])) return -1;
+  }
+  return 0;
 }
 static int sizes_fit(const long long* v, int n) {
   for (int i = 0; i < n; ++i)
@@ -173,11 +187,13 @@ static PyObject* py_sample_window(PyObject* self, PyObject* const* a, Py_ssize_t
   int window, sinks;
   const long long dev = ask(a[3], s_get_device);
   if (dev < 0) return refuse(a[3], "ts", "float64", -1, 0), NULL;
-  const long long n = ask(a[4], s_numel), P = ask(a[3], s_numel), N = ask(a[0], s_numel) - 1;
-  if (PyErr_Occurred() || small(a[6], &window) || small(a[7], &sinks)) return NULL;
+  long long n, P, N;
+  if (small(a[6], &window) || small(a[7], &sinks) || vec_n(a[0], I64, dev, 1, 1, "indptr", &indptr, &N) ||
+      vec_n(a[3], F64, dev, 0, 1, "ts", &ts, &P) || vec_n(a[4], I32, dev, 0, 1, "nodes", &nodes, &n))
+    return NULL;
+  --N; /* nodes */
   const long long S = n * ((long long)window + sinks);
-  if (vec(a[0], I64, dev, 1, 1, "indptr", &indptr) || vec(a[1], I32, dev, P, 0, "nbr", &nbr) || vec(a[2], I32, dev, P, 0, "eid", &eid) ||
-      vec(a[3], F64, dev, P, 0, "ts", &ts) || vec(a[4], I32, dev, n, 0, "nodes", &nodes) || vec(a[5], F64, dev, n, 0, "times", &times) ||
+  if (vec(a[1], I32, dev, P, 0, "nbr", &nbr) || vec(a[2], I32, dev, P, 0, "eid", &eid) || vec(a[5], F64, dev, n, 0, "times", &times) ||
       vec(a[8], I32, dev, S, 0, "nbr_out", &o_nbr) || vec(a[9], I32, dev, S, 0, "eid_out", &o_eid) ||
       vec(a[10], F64, dev, S, 0, "ts_out", &o_ts) || vec(a[11], I32, dev, n, 0, "cnt_out", &cnt) ||
       vec(a[12], I64, dev, n, 0, "first_out", &first) || vec(a[13], I32, dev, n, 0, "len_out", &len) ||
@@ -199,7 +215,7 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
   const int kind = kind_of(rows);
   if (kind < F32 || kind == F64 || ask(rows, s_get_device) != dev) return refuse(rows, "rows", "float32, bfloat16 or float16", -1, dev), NULL;
   const long long d = ask(rows, s_dim), num = d < 1 ? -1 : ask1(rows, s_size, 0);
-  if (PyErr_Occurred()) return NULL;
+  if (failed(num)) return NULL;
   if (!(d == 2 && ask1(rows, s_size, 1) == heads * dim) && !(d == 3 && ask1(rows, s_size, 1) == heads && ask1(rows, s_size, 2) == dim)) {
     if (!PyErr_Occurred()) PyErr_Format(PyExc_TypeError, "rows: expected rows of %lld x %lld values", heads, dim);
     return NULL;
@@ -208,7 +224,8 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
   stride = heads * dim;
   if (dense != 1) { /* rows apart, the values of one side by side */
     if (PyErr_Occurred()) return NULL;
-    const long long s1 = ask1(rows, s_stride, 1), s2 = d == 3 ? ask1(rows, s_stride, 2) : 1;
+    long long s1, s2 = 1;
+    if (failed(s1 = ask1(rows, s_stride, 1)) || (d == 3 && failed(s2 = ask1(rows, s_stride, 2)))) return NULL;
     const int inner = d == 2 ? s1 == 1 || stride == 1 : (s1 == dim || heads == 1) && (s2 == 1 || dim == 1);
     if (num > 1) stride = ask1(rows, s_stride, 0);
     if (PyErr_Occurred()) return NULL;
@@ -228,8 +245,8 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
     if (t == Py_None) continue;
     kinds[i] = kind_of(t);
     if (kinds[i] != I32 && kinds[i] != I64) return refuse(t, i ? "dst" : "src", "int32 or int64", -1, dev), NULL;
-    if (vec(t, kinds[i], dev, 0, 1, i ? "dst" : "src", &idx[i])) return NULL;
-    count[i] = n = ask(t, s_numel);
+    if (vec_n(t, kinds[i], dev, 0, 1, i ? "dst" : "src", &idx[i], &count[i])) return NULL;
+    n = count[i];
     bits = kinds[i] == I64 ? 64 : 32;
   }
   if (kinds[0] >= 0 && kinds[1] >= 0 && (kinds[0] != kinds[1] || count[0] != count[1])) {

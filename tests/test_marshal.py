@@ -131,7 +131,7 @@ def _tensors(name):
     return [i for i, a in enumerate(_calls()[name]) if isinstance(a, Tensor)]
 
 
-@pytest.mark.parametrize("method", ["data_ptr", "numel", "get_device", "is_contiguous"])
+@pytest.mark.parametrize("method", ["data_ptr", "numel", "get_device", "is_contiguous", "dim", "size", "stride"])
 @pytest.mark.parametrize("name", list(_calls()))
 def test_what_a_tensors_method_raises_is_what_the_call_raises(loaded, name, method):
     """A tensor without storage (a fake one) raises when it is asked for its address: the caller sees that, not an address that is refused."""
@@ -147,7 +147,30 @@ def test_what_a_tensors_method_raises_is_what_the_call_raises(loaded, name, meth
             except type(error) as e:
                 assert e is error
                 seen += 1
-        assert seen >= (len(_tensors(name)) if method == "data_ptr" else 1)
+        # dimensions are asked for where a shape is looked at, strides of rows that are apart (below) only
+        asks = name != "sample_window" if method in ("dim", "size") else method != "stride"
+        assert seen >= (len(_tensors(name)) if method == "data_ptr" else int(asks))
+
+
+@pytest.mark.parametrize("name", ["cache_write", "cache_read"])
+@pytest.mark.parametrize("which", [0, 1, 2])
+def test_what_the_strides_of_rows_raise(loaded, name, which):
+    m, fake = loaded
+    C.c_int.in_dll(fake, "released").value = 1
+    args, error = _calls()[name], ValueError("no strides")
+
+    class Apart(Tensor):
+        def is_contiguous(self):
+            return False
+
+        def stride(self, i):
+            if i == which:
+                raise error
+            return super().stride(i)
+    args[6] = Apart(F32, 7, 2, 8)
+    with pytest.raises(ValueError) as e:
+        _function(m, name)(*args)
+    assert e.value is error
 
 
 @pytest.mark.parametrize("name", list(_calls()))
