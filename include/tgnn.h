@@ -610,6 +610,59 @@ TGNN_API int tgnn_slot_attend_backward(const void* q, const void* k, const void*
                                        void* dq, void* dk, void* dv, float* dbias, float* scratch, void* stream, char* err_host,
                                        int64_t err_size);
 
+/* ---- a learned table of nodes: rows looked up, AdamW ------------------------------------------------------------------
+ * What trains a table with one row per node: its rows are looked up by id (neighbor slots, roots), and all tensors are stepped at once.
+ * Stateless, device pointers (except *_host), work enqueued on `stream` of the current device, nothing allocated; errors as above.
+ * status: device int32, NOT zeroed by these calls; 4 is recorded for an index beyond its table.  A scratch buffer (256-byte aligned) belongs to
+ * the call until the call's work has ended (calls that may overlap, two captured graphs among them, need one each); contents undefined after.
+ *
+ * tgnn_lookup: out[i] = scale * table[ids[i]], i < n.  table: [rows, dim] of `dtype`, out: [n, dim] of `out_dtype` (TGNN_F32, TGNN_BF16,
+ *   TGNN_F16 each), dense; ids of index_bits (32 or 64) bits.  An id below 0 (an unused slot) gives zeros; one beyond the table too, status 4.
+ * tgnn_lookup_backward: dtable[r] = scale * sum of dout[i] over ids[i] = r, in fp32 and in an order fixed by the sizes (the same call gives the
+ *   same bits), rounded once; every row is overwritten, with zeros where no id names it.  scratch: tgnn_lookup_scratch(n, rows, dim) bytes.
+ * dim 1 to 8192; rows and n below 2^31 - 1.  No output may alias an input. */
+TGNN_API int tgnn_lookup(const void* table, int dtype, int64_t rows, int dim, const void* ids, int index_bits, int64_t n, float scale,
+                         void* out, int out_dtype, int32_t* status, void* stream, char* err_host, int64_t err_size);
+TGNN_API int64_t tgnn_lookup_scratch(int64_t n, int64_t rows, int dim); /* -1 if out of range */
+TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, int64_t n, const void* dout, int out_dtype, int64_t rows, int dim,
+                                  float scale, void* dtable, int dtype, void* scratch, int32_t* status, void* stream, char* err_host,
+                                  int64_t err_size);
+
+/* tgnn_adamw_step: one AdamW step of all tensors, t = steps[0] + 1:
+ *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + ((1 - beta2) g) g
+ *   param -= lr * (weight_decay * param + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * param: fp32; grad: fp32, bf16 or fp16; copy: bf16 or fp16, the new parameters rounded, or NULL.  tensors_host is read during the call only
+ * (it travels as kernel parameters; a captured call keeps its addresses, and lr and the other numbers as they were).
+ * steps: device int64[2], zeros at first: steps taken, and a word of the library's; advanced by the call.  Calls on one `steps` do not overlap.
+ * state_bits 32: m, v are fp32[numel].  8: m is int8, v uint8 [numel], with a scale (fp32) per block of 256 values each
+ * (tgnn_adamw_blocks(numel) of them), all zeros at first.  With L = 127 (m) or 255 (u = sqrt v), every operation rounded to fp32:
+ *   top = the block's largest magnitude; scale = top * fp32(1 / L^2), y = |x| * (1 / scale); c = floor(sqrt(y)), L at most;
+ *   c + 1 instead if y - c^2 > a (2 c + 1) and c < L; u that is not 0 has c = 1 at least; value = c^2 * scale, with m's sign; v = u * u.
+ *   a = (h + 0.5) / 65536, h = 16 bits of SplitMix64's finaliser of seed ^ t * 0x9E3779B97F4A7C15 ^ (tensor * 2^40 + element / 2) *
+ *   0xC2B2AE3D27D4EB4F: bits 0-15 for m and 16-31 for u of even elements, 32-47 and 48-63 of odd ones.  So a value's mean is itself.
+ *   A block below 2^-60 is held as zeros, one with an infinity or a NaN reads back as NaN, all of it.
+ * tgnn_adamw_moments: m and v of states in 8 bits as fp32 values (m_out_host, v_out_host: a device pointer per tensor; param, grad, copy unused).
+ * Tensors of no elements are passed over.  Up to 2^20 tensors. */
+typedef struct tgnn_adamw_tensor {
+  float* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  int64_t numel;
+  float weight_decay;
+  int32_t grad_dtype;
+  int32_t copy_dtype;
+  int32_t reserved;
+} tgnn_adamw_tensor;
+TGNN_API int64_t tgnn_adamw_blocks(int64_t numel);
+TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, int count, int state_bits, int64_t* steps, double lr, double beta1,
+                             double beta2, double eps, double grad_scale, uint64_t seed, void* stream, char* err_host, int64_t err_size);
+TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count, float* const* m_out_host, float* const* v_out_host,
+                                void* stream, char* err_host, int64_t err_size);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,5 +1,5 @@
 """Thin ctypes binding of libtgnn_b200.so: same names as the C ABI, argument
-marshalling only (the history operators' in C, csrc/marshal.c).  torch is used for device memory and streams; every step of
+marshalling only (the history and node-table operators' in C, csrc/marshal.c).  torch is used for device memory and streams; every step of
 the path runs in the library's CUDA kernels.  There is no CPU fallback: loading
 fails loudly when the shared library is missing."""
 from __future__ import annotations
@@ -38,7 +38,8 @@ EXPORTS = ("tgnn_create", "tgnn_destroy", "tgnn_last_error", "tgnn_param_count",
            "tgnn_build_mixed", "tgnn_set_grad_sync", "tgnn_grad_buffer", "tgnn_apply_gradient", "tgnn_refresh_plan",
            "tgnn_pack_rows", "tgnn_unpack_rows", "tgnn_debug_get_embeddings", "tgnn_debug_gemm_split",
            "tgnn_clear_status", "tgnn_order_streams", "tgnn_sample_window", "tgnn_cache_code_bytes", "tgnn_cache_write",
-           "tgnn_cache_read", "tgnn_cached_attend", "tgnn_slot_attend", "tgnn_slot_attend_scratch", "tgnn_slot_attend_backward")
+           "tgnn_cache_read", "tgnn_cached_attend", "tgnn_slot_attend", "tgnn_slot_attend_scratch", "tgnn_slot_attend_backward",
+           "tgnn_lookup", "tgnn_lookup_scratch", "tgnn_lookup_backward", "tgnn_adamw_blocks", "tgnn_adamw_step", "tgnn_adamw_moments")
 TGNN_STATIC_MAX_NODES = 65536
 
 
@@ -54,6 +55,12 @@ class TgnnCache(C.Structure):
     _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("times", C.c_void_p), ("rows", C.c_int64),
                 ("code_stride", C.c_int64), ("scale_stride", C.c_int64), ("time_stride", C.c_int64),
                 ("heads", C.c_int32), ("dim", C.c_int32), ("bits", C.c_int32), ("reserved", C.c_int32)]
+
+
+class TgnnAdamwTensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("copy", C.c_void_p), ("numel", C.c_int64), ("weight_decay", C.c_float),
+                ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("reserved", C.c_int32)]
 
 
 class TgnnError(RuntimeError):
@@ -140,6 +147,15 @@ def load_library():
         lib.tgnn_slot_attend_scratch.argtypes = [i64, i32, i32]
         lib.tgnn_slot_attend_scratch.restype = i64
         lib.tgnn_slot_attend_backward.argtypes = slot + [vp] * 8 + [i64]
+        lib.tgnn_lookup.argtypes = [vp, i32, i64, i32, vp, i32, i64, f32, vp, i32, vp, vp, vp, i64]
+        lib.tgnn_lookup_scratch.argtypes = [i64, i64, i32]
+        lib.tgnn_lookup_backward.argtypes = [vp, i32, i64, vp, i32, i64, i32, f32, vp, i32, vp, vp, vp, vp, i64]
+        lib.tgnn_adamw_blocks.argtypes = [i64]
+        for fn in (lib.tgnn_lookup_scratch, lib.tgnn_adamw_blocks):
+            fn.restype = i64
+        ap = C.POINTER(TgnnAdamwTensor)
+        lib.tgnn_adamw_step.argtypes = [ap, i32, i32, vp, f64, f64, f64, f64, f64, u64, vp, vp, i64]
+        lib.tgnn_adamw_moments.argtypes = [ap, i32, vp, vp, vp, vp, i64]
         _lib = lib
     return _lib
 
@@ -306,6 +322,9 @@ def _load_marshal():
            torch._C._cuda_getCurrentRawStream,
            tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_sample_window, lib.tgnn_cache_write, lib.tgnn_cache_read, lib.tgnn_cached_attend,
                                                        lib.tgnn_slot_attend, lib.tgnn_slot_attend_scratch, lib.tgnn_slot_attend_backward)))
+    m.init_table((torch.uint8, torch.int8),
+                 tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_lookup, lib.tgnn_lookup_scratch, lib.tgnn_lookup_backward,
+                                                             lib.tgnn_adamw_step, lib.tgnn_adamw_moments)))
     _marshal = m
 
 
@@ -412,6 +431,46 @@ def slot_attend_backward(q, k, v, cnt, dout, dq, dk, dv, bias=None, bounds=None,
                          scale: Optional[float] = None) -> int:
     """tgnn_slot_attend_backward: gradients of slot_attend for dout, all overwritten."""
     return _call("slot_attend_backward", q, k, v, cnt, scale, bias, bounds, times, ts, dout, dq, dk, dv, dbias, scratch)
+
+
+# ---- a learned table of nodes: lookup, AdamW (tensors are checked in csrc/marshal.c too) ----
+def lookup(table, ids, out, status, scale: float = 1.0) -> int:
+    """tgnn_lookup: out[i] = scale * table[ids[i]], zeros where ids[i] < 0.  table [rows, dim], ids int32 or int64 of any shape, out one row
+    per id; fp32, bf16 or fp16 rows on either side."""
+    return _call("lookup", table, ids, out, scale, status)
+
+
+def _size(n: int, what: str) -> int:
+    if n < 0:
+        raise TgnnError(TGNN_EINVAL, f"{what}: size out of range")
+    return n
+
+
+def lookup_scratch(n: int, rows: int, dim: int) -> int:
+    """Bytes (elements of a uint8 tensor) that tgnn_lookup_backward needs as scratch."""
+    return _size(load_library().tgnn_lookup_scratch(n, rows, dim), "tgnn_lookup_scratch")
+
+
+def lookup_backward(ids, dout, dtable, scratch, status, scale: float = 1.0) -> int:
+    """tgnn_lookup_backward: dtable [rows, dim], all of it overwritten, from dout, one row per id."""
+    return _call("lookup_backward", ids, dout, dtable, scratch, scale, status)
+
+
+def adamw_blocks(numel: int) -> int:
+    """Scales per moment that a tensor of numel elements has in 8 bits."""
+    return _size(load_library().tgnn_adamw_blocks(numel), "tgnn_adamw_blocks")
+
+
+def adamw_step(tensors, bits: int, device: int, steps, params, grads, lr: float, beta1: float, beta2: float, eps: float, grad_scale: float = 1.0,
+               seed: int = 0) -> int:
+    """tgnn_adamw_step: `tensors` is an array of TgnnAdamwTensor whose moments, sizes, decays and copies are set; parameters and gradients (lists; a
+    gradient may be None: that tensor stays as it is) are filled in for the call."""
+    return _call("adamw_step", C.addressof(tensors), bits, device, steps, lr, beta1, beta2, eps, grad_scale, seed, params, grads)
+
+
+def adamw_moments(tensors, device: int, m_out, v_out) -> int:
+    """tgnn_adamw_moments: values of 8-bit moments; m_out, v_out: arrays of c_void_p, one fp32 tensor's address each."""
+    return _call("adamw_moments", C.addressof(tensors), len(tensors), C.addressof(m_out), C.addressof(v_out), device)
 
 
 class Controller:

@@ -1,0 +1,428 @@
+// One AdamW step over many tensors in one launch, with moments in 32 or 8 bits.
+//
+//   g = grad * grad_scale;  m' = b1 m + (1 - b1) g;  v' = b2 v + ((1 - b2) g) g
+//   p' = p - lr (decay p + (m' / (1 - b1^t)) / (sqrt(v' / (1 - b2^t)) + eps))
+//
+// In 8 bits a block of 256 values has one scale each for m and for u = sqrt(v), and a value is c^2 * scale: codes that are squares
+// resolve 16129 (m) and 65025 (u) to 1 within a block.  A value becomes one of its two neighbours by chance, so that the mean is right:
+// a second moment that decays by 0.1 % a step would stay on its code for ever if it were rounded to the nearest.  u keeps code 1 where it is not 0, so
+// that no step divides by eps alone.  Every operation up to the codes is one rounded fp32 operation (no contraction): codes are
+// the same on every implementation.
+//
+// A warp takes 256 values at a time, eight per lane as two groups of four, which are 16-byte words of fp32 and 4-byte words of codes.
+// Tensors are described in the kernel's parameters: nothing is copied to the device ahead of the launch, and a captured graph
+// keeps them.  Bound by bytes: 28 per value with fp32 gradients and moments, 16 with moments in 8 bits.
+#include "tgnn_table.cuh"
+
+using namespace tgnn_table;
+
+namespace {
+
+constexpr int kBlock = 256;                   // values per scale
+constexpr int kThreads = 256;
+constexpr float kLeast = 8.6736174e-19f;      // 2^-60: a block below it holds zeros
+
+struct One {
+  float* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;
+  int64_t n;
+  float decay;
+  int8_t g_dtype, copy_dtype, wide;           // wide: every address is a multiple of four values
+};
+template <int MAX>
+struct Many {
+  One t[MAX];
+  uint32_t end[MAX];                          // chunks up to and with tensor i
+  int64_t* steps;                             // {steps done, blocks of this step that have read it}
+  uint64_t seed;
+  int64_t first;                              // place of t[0] in the caller's list
+  double b1, b2, eps;
+  float lr, grad_scale, b1f, b2f, n1, n2;
+  uint32_t blocks;                            // of the launch that ends the step; 0: a later one does
+  int count;
+  int per_chunk;                              // values per thread block, a multiple of 2048
+};
+
+__device__ __forceinline__ uint64_t mix(uint64_t z) {  // SplitMix64's finaliser
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+
+// 1 - b^t in fp64 by squaring.
+__device__ __forceinline__ double one_minus_power(double b, int64_t t) {
+  double r = 1.0;
+  for (; t > 0; t >>= 1, b *= b)
+    if (t & 1) r *= b;
+  return 1.0 - r;
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(const T* p, int64_t at, int64_t n, bool wide, float* x) {
+  if (wide && at + 4 <= n) {
+    reinterpret_cast<const Group<T, 4>*>(p + at)->get(x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = at + i < n ? tgnn_history::to_float<T>(p[at + i]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int64_t at, int64_t n, bool wide, const float* x) {
+  if (wide && at + 4 <= n) {
+    Group<T, 4> g;
+    g.set(x);
+    *reinterpret_cast<Group<T, 4>*>(p + at) = g;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i < n) p[at + i] = tgnn_history::from_float<T>(x[i]);
+  }
+}
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t at, int64_t n, bool wide) {
+  if (wide && at + 4 <= n) return *reinterpret_cast<const uint32_t*>(p + at);
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (at + i < n) w |= (uint32_t)p[at + i] << (8 * i);
+  return w;
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, int64_t at, int64_t n, bool wide, uint32_t w) {
+  if (wide && at + 4 <= n) *reinterpret_cast<uint32_t*>(p + at) = w;
+  else
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (at + i < n) p[at + i] = (uint8_t)(w >> (8 * i));
+}
+__device__ __forceinline__ float signed_square(uint32_t byte, float scale) {
+  const float c = (float)(int8_t)byte;
+  return __fmul_rn(c * fabsf(c), scale);      // squares up to 16129 are exact
+}
+__device__ __forceinline__ float square(uint32_t byte, float scale) {
+  const float c = (float)(byte & 255u);
+  return __fmul_rn(c * c, scale);
+}
+
+// Scale of a block whose largest magnitude (as bits, so that NaN stays on top) is `top`, and its reciprocal.
+__device__ __forceinline__ float scale_of(uint32_t top_bits, float per, float* back) {
+  const float top = __uint_as_float(top_bits);
+  *back = 0.f;
+  if (top_bits >= 0x7f800000u) return __uint_as_float(0x7fc00000u);           // reads back as NaN, all of it
+  if (top < kLeast) return 0.f;
+  const float s = __fmul_rn(top, per);
+  *back = __frcp_rn(s);
+  return s;
+}
+// The code of magnitude |x|: floor of the root, and one more by chance a in (0, 1).
+__device__ __forceinline__ float code_of(float x, float back, float a, float most) {
+  const float y = __fmul_rn(fabsf(x), back);
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
+  float c = floorf(r);                        // within one of the root's floor; made exact here (squares are exact)
+  if (c * c > y) c -= 1.f;
+  if ((c + 1.f) * (c + 1.f) <= y) c += 1.f;
+  c = fminf(c, most);
+  if (y - c * c > __fmul_rn(a, 2.f * c + 1.f) && c < most) c += 1.f;          // the difference is exact too
+  return c;
+}
+__device__ __forceinline__ uint32_t warp_max(uint32_t x) { return __reduce_max_sync(FULL, x); }
+__device__ __forceinline__ float chance(uint32_t bits16) { return __fmul_rn((float)bits16 + 0.5f, 1.f / 65536.f); }
+
+template <int BITS, int MAX>
+__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Many<MAX> a) {
+  __shared__ float s_c1, s_c2;
+  __shared__ uint64_t s_salt;
+  if (threadIdx.x == 0) {
+    const int64_t t = *reinterpret_cast<volatile int64_t*>(a.steps) + 1;
+    if (a.blocks > 0) {
+      // the last block to have read the counter advances it: the others do not look at it again
+      const unsigned long long before = atomicAdd(reinterpret_cast<unsigned long long*>(a.steps + 1), 1ull);
+      if (before == a.blocks - 1) {
+        a.steps[0] = t;
+        a.steps[1] = 0;
+      }
+    }
+    s_c1 = (float)(1.0 / one_minus_power(a.b1, t));
+    s_c2 = (float)rsqrt(one_minus_power(a.b2, t));
+    s_salt = a.seed ^ ((uint64_t)t * 0x9E3779B97F4A7C15ull);
+  }
+  int lo = 0, hi = a.count - 1;               // the tensor of this chunk: the first whose chunks end behind it
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.end[mid] > blockIdx.x) hi = mid;
+    else lo = mid + 1;
+  }
+  const One& o = a.t[lo];
+  const int64_t begin = (int64_t)(blockIdx.x - (lo ? a.end[lo - 1] : 0)) * a.per_chunk;
+  const int64_t n = o.n, stop = min(n, begin + a.per_chunk);
+  const bool wide = o.wide;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __syncthreads();
+  const float c1 = s_c1, c2 = s_c2, eps = (float)a.eps;
+  const uint64_t salt = s_salt;
+  for (int64_t at0 = begin + warp * kBlock; at0 < stop; at0 += (kThreads / 32) * kBlock) {
+    float p[8], g[8], m[8], v[8];
+    const int64_t at[2] = {at0 + 4 * lane, at0 + 128 + 4 * lane};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      load4(o.p, at[h], n, wide, p + 4 * h);
+      if (o.g_dtype == TGNN_F32) load4(static_cast<const float*>(o.g), at[h], n, wide, g + 4 * h);
+      else if (o.g_dtype == TGNN_BF16) load4(static_cast<const __nv_bfloat16*>(o.g), at[h], n, wide, g + 4 * h);
+      else load4(static_cast<const __half*>(o.g), at[h], n, wide, g + 4 * h);
+    }
+    const int64_t block = at0 / kBlock;
+    if (BITS == 8) {
+      uint32_t wm[2], wv[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        wm[h] = load_codes(static_cast<const uint8_t*>(o.m), at[h], n, wide);
+        wv[h] = load_codes(static_cast<const uint8_t*>(o.v), at[h], n, wide);
+      }
+      const float sm = o.m_scale[block], sv = o.v_scale[block];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        m[i] = signed_square(wm[i >> 2] >> (8 * (i & 3)), sm);
+        const float u = square(wv[i >> 2] >> (8 * (i & 3)), sv);
+        v[i] = __fmul_rn(u, u);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        load4(static_cast<const float*>(o.m), at[h], n, wide, m + 4 * h);
+        load4(static_cast<const float*>(o.v), at[h], n, wide, v + 4 * h);
+      }
+    }
+    float u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = __fmul_rn(g[i], a.grad_scale);
+      m[i] = __fadd_rn(__fmul_rn(m[i], a.b1f), __fmul_rn(x, a.n1));
+      v[i] = __fadd_rn(__fmul_rn(v[i], a.b2f), __fmul_rn(__fmul_rn(x, a.n2), x));
+      u[i] = __fsqrt_rn(v[i]);
+      // 1 - lr decay would round to fp32: the change is formed and taken off instead
+      p[i] -= a.lr * fmaf(o.decay, p[i], __fdividef(m[i] * c1, fmaf(u[i], c2, eps)));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      store4(o.p, at[h], n, wide, p + 4 * h);
+      if (o.copy) {
+        if (o.copy_dtype == TGNN_BF16) store4(static_cast<__nv_bfloat16*>(o.copy), at[h], n, wide, p + 4 * h);
+        else store4(static_cast<__half*>(o.copy), at[h], n, wide, p + 4 * h);
+      }
+    }
+    if (BITS == 8) {
+      uint32_t tm = 0, tu = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {           // places behind the end were read as zeros and are zeros still
+        tm = max(tm, __float_as_uint(m[i]) & 0x7fffffffu);
+        tu = max(tu, __float_as_uint(u[i]) & 0x7fffffffu);
+      }
+      float bm, bu;
+      const float sm = scale_of(warp_max(tm), 1.f / 16129.f, &bm), su = scale_of(warp_max(tu), 1.f / 65025.f, &bu);
+      if (lane == 0) {
+        o.m_scale[block] = sm;
+        o.v_scale[block] = su;
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t wm = 0, wv = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const uint64_t pair = ((uint64_t)(a.first + lo) << 40) + (uint64_t)((at[h] + j) >> 1);
+          const uint64_t r = mix(salt ^ (pair * 0xC2B2AE3D27D4EB4Full));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int i = 4 * h + j + e;
+            const uint32_t w = (uint32_t)(r >> (32 * e));
+            const float cm = code_of(m[i], bm, chance(w & 0xffffu), 127.f);
+            float cu = code_of(u[i], bu, chance(w >> 16), 255.f);
+            if (cu == 0.f && u[i] > 0.f && bu > 0.f) cu = 1.f;
+            wm |= ((uint32_t)(int)copysignf(cm, m[i]) & 255u) << (8 * (j + e));
+            wv |= (uint32_t)cu << (8 * (j + e));
+          }
+        }
+        store_codes(static_cast<uint8_t*>(o.m), at[h], n, wide, wm);
+        store_codes(static_cast<uint8_t*>(o.v), at[h], n, wide, wv);
+      }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        store4(static_cast<float*>(o.m), at[h], n, wide, m + 4 * h);
+        store4(static_cast<float*>(o.v), at[h], n, wide, v + 4 * h);
+      }
+    }
+  }
+}
+
+// Moments in 8 bits as values: m into p's place of the description, v into copy's.
+template <int MAX>
+__global__ void __launch_bounds__(kThreads) moments_kernel(const __grid_constant__ Many<MAX> a) {
+  int lo = 0, hi = a.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.end[mid] > blockIdx.x) hi = mid;
+    else lo = mid + 1;
+  }
+  const One& o = a.t[lo];
+  const int64_t begin = (int64_t)(blockIdx.x - (lo ? a.end[lo - 1] : 0)) * a.per_chunk;
+  const int64_t n = o.n, stop = min(n, begin + a.per_chunk);
+  const bool wide = o.wide;
+  for (int64_t at = begin + 4 * threadIdx.x; at < stop; at += 4 * kThreads) {
+    const uint32_t wm = load_codes(static_cast<const uint8_t*>(o.m), at, n, wide), wv = load_codes(static_cast<const uint8_t*>(o.v), at, n, wide);
+    const float sm = o.m_scale[at / kBlock], sv = o.v_scale[at / kBlock];
+    float m[4], v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = signed_square(wm >> (8 * i), sm);
+      const float u = square(wv >> (8 * i), sv);
+      v[i] = __fmul_rn(u, u);
+    }
+    store4(o.p, at, n, wide, m);
+    store4(static_cast<float*>(o.copy), at, n, wide, v);
+  }
+}
+
+// Values per thread block: 2048 while that leaves no multiprocessor idle, more where there is more, so that a block's set-up (the powers of b1
+// and b2, 0.3 us) is a small part of it.
+int per_chunk_of(int64_t values) {
+  const int64_t per_block = values / (16 * num_sms());
+  return per_block >= 8192 ? 8192 : per_block >= 4096 ? 4096 : 2048;
+}
+
+template <int MAX, typename K>
+void launch(K kernel, Chain& c, const tgnn_adamw_tensor* t, float* const* m_out, float* const* v_out, int from, int count, int bits, Many<MAX>& a,
+            bool ends, int per_chunk) {
+  uint64_t chunks = 0;
+  a.first = from;
+  a.count = count;
+  a.per_chunk = per_chunk;
+  for (int i = 0; i < count; ++i) {
+    const tgnn_adamw_tensor& x = t[from + i];
+    One& o = a.t[i];
+    o.p = m_out ? m_out[from + i] : x.param;
+    o.g = x.grad;
+    o.m = x.m;
+    o.v = x.v;
+    o.m_scale = x.m_scale;
+    o.v_scale = x.v_scale;
+    o.copy = v_out ? v_out[from + i] : x.copy;
+    o.n = x.numel;
+    o.decay = x.weight_decay;
+    o.g_dtype = (int8_t)x.grad_dtype;
+    o.copy_dtype = (int8_t)x.copy_dtype;
+    const uintptr_t mv = (uintptr_t)x.m | (uintptr_t)x.v;
+    o.wide = ((uintptr_t)o.p & 15) == 0 && (mv & (bits == 8 ? 3 : 15)) == 0 && ((uintptr_t)o.copy & (v_out ? 15 : 7)) == 0 &&
+             (m_out || ((uintptr_t)x.grad & (4 * elem_bytes(x.grad_dtype) - 1)) == 0);
+    chunks += (uint64_t)((x.numel + per_chunk - 1) / per_chunk);
+    a.end[i] = (uint32_t)chunks;
+  }
+  a.blocks = ends ? (uint32_t)chunks : 0;
+  if (chunks) c(kernel, dim3((unsigned)chunks), dim3(kThreads), 0, a);
+}
+
+int check(const char* who, const tgnn_adamw_tensor* t, int count, int bits, bool read, int64_t* values, int* used, char* err, int64_t size) {
+  if (bits != 8 && bits != 32) return fail(err, size, TGNN_EINVAL, "%s: state_bits is 8 or 32", who);
+  if (count < 0 || (count > 0 && !t)) return fail(err, size, TGNN_EINVAL, "%s: no tensors given", who);
+  if (count > 1 << 20) return fail(err, size, TGNN_ECAPACITY, "%s: more than 2^20 tensors", who);
+  *values = 0;
+  *used = 0;
+  for (int i = 0; i < count; ++i) {
+    const tgnn_adamw_tensor& x = t[i];
+    if (x.numel < 0 || x.numel > 1ll << 40) return fail(err, size, TGNN_EINVAL, "%s: tensor %d: size out of range", who, i);
+    if (x.numel == 0) continue;
+    if (!x.m || !x.v || (bits == 8 && (!x.m_scale || !x.v_scale)) || (!read && (!x.param || !x.grad)))
+      return fail(err, size, TGNN_EINVAL, "%s: tensor %d: null pointer", who, i);
+    if (!read && (!known_dtype(x.grad_dtype) || (x.copy && x.copy_dtype != TGNN_BF16 && x.copy_dtype != TGNN_F16)))
+      return fail(err, size, TGNN_EINVAL, "%s: tensor %d: a gradient is fp32, bf16 or fp16, a copy bf16 or fp16", who, i);
+    if (((uintptr_t)x.param & 3) || ((bits == 32) && (((uintptr_t)x.m | (uintptr_t)x.v) & 3)) || (((uintptr_t)x.m_scale | (uintptr_t)x.v_scale) & 3) ||
+        ((uintptr_t)x.copy & 1) || (!read && ((uintptr_t)x.grad & (elem_bytes(x.grad_dtype) - 1))))
+      return fail(err, size, TGNN_EINVAL, "%s: tensor %d: a pointer is not aligned to its element", who, i);
+    *values += x.numel;
+    *used = i + 1;
+  }
+  if (*values > 1ll << 42) return fail(err, size, TGNN_ECAPACITY, "%s: more than 2^42 values", who);
+  return TGNN_OK;
+}
+
+constexpr int kFew = 40, kMost = 360;          // tensors of one launch: 4 KB of parameters, or 32 KB
+
+}  // namespace
+
+extern "C" TGNN_API int64_t tgnn_adamw_blocks(int64_t numel) { return numel < 0 ? -1 : (numel + kBlock - 1) / kBlock; }
+
+extern "C" TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, int count, int state_bits, int64_t* steps, double lr, double beta1,
+                                        double beta2, double eps, double grad_scale, uint64_t seed, void* stream, char* err, int64_t err_size) {
+  const char* who = "tgnn_adamw_step";
+  int64_t values;
+  int used;
+  if (int rc = check(who, tensors_host, count, state_bits, false, &values, &used, err, err_size)) return rc;
+  if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(grad_scale - grad_scale == 0))
+    return fail(err, err_size, TGNN_EINVAL, "%s: lr >= 0, 0 <= beta < 1, eps >= 0 and a finite grad_scale are needed", who);
+  if (!steps || ((uintptr_t)steps & 7)) return fail(err, err_size, TGNN_EINVAL, "%s: steps is null or not 8-byte aligned", who);
+  if (values == 0) return TGNN_OK;
+  const int per = per_chunk_of(values);
+  Chain c(stream);
+  auto fill = [&](auto& a) {
+    a.steps = steps;
+    a.seed = seed;
+    a.b1 = beta1;
+    a.b2 = beta2;
+    a.eps = eps;
+    a.lr = (float)lr;
+    a.grad_scale = (float)grad_scale;
+    a.b1f = (float)beta1;
+    a.b2f = (float)beta2;
+    a.n1 = 1.f - a.b1f;
+    a.n2 = 1.f - a.b2f;
+  };
+  for (int from = 0; from < used;) {
+    c.first = true;                            // launches of one step touch different tensors, and the counter in stream order
+    if (used - from <= kFew) {
+      Many<kFew> a;
+      fill(a);
+      launch(state_bits == 8 ? adamw_kernel<8, kFew> : adamw_kernel<32, kFew>, c, tensors_host, nullptr, nullptr, from, used - from, state_bits, a, true,
+             per);
+      from = used;
+    } else {
+      Many<kMost> a;
+      fill(a);
+      const int now = used - from < kMost ? used - from : kMost;
+      launch(state_bits == 8 ? adamw_kernel<8, kMost> : adamw_kernel<32, kMost>, c, tensors_host, nullptr, nullptr, from, now, state_bits, a,
+             from + now == used, per);
+      from += now;
+    }
+  }
+  return c.end(who, err, err_size);
+}
+
+extern "C" TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count, float* const* m_out_host, float* const* v_out_host,
+                                           void* stream, char* err, int64_t err_size) {
+  const char* who = "tgnn_adamw_moments";
+  int64_t values;
+  int used;
+  if (int rc = check(who, tensors_host, count, 8, true, &values, &used, err, err_size)) return rc;
+  if (values == 0) return TGNN_OK;
+  if (!m_out_host || !v_out_host) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", who);
+  for (int i = 0; i < used; ++i)
+    if (tensors_host[i].numel > 0 && (!m_out_host[i] || !v_out_host[i] || (((uintptr_t)m_out_host[i] | (uintptr_t)v_out_host[i]) & 3)))
+      return fail(err, err_size, TGNN_EINVAL, "%s: tensor %d: an output is null or not aligned", who, i);
+  const int per = per_chunk_of(values);
+  Chain c(stream);
+  for (int from = 0; from < used;) {
+    c.first = true;
+    const int most = used - from <= kFew ? kFew : kMost, now = used - from < most ? used - from : most;
+    if (most == kFew) {
+      Many<kFew> a = {};
+      launch(moments_kernel<kFew>, c, tensors_host, m_out_host, v_out_host, from, now, 8, a, false, per);
+    } else {
+      Many<kMost> a = {};
+      launch(moments_kernel<kMost>, c, tensors_host, m_out_host, v_out_host, from, now, 8, a, false, per);
+    }
+    from += now;
+  }
+  return c.end(who, err, err_size);
+}

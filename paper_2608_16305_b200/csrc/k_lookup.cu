@@ -1,0 +1,699 @@
+// Rows of a table by id, scaled, and the gradient of the table.
+//
+// out[i] = scale * table[ids[i]] is a gather: bytes of the distinct rows and of the output bound it.  The gradient,
+// dtable[r] = scale * sum of dout[i] over ids[i] = r, is summed in a fixed order instead of by atomics: ids are sorted with their places
+// (least digit first, 8 bits at most at a time, stable), and runs of equal ids in the sorted order are summed.  Chunks of that order go to groups of
+// lanes; a run inside one chunk is written at once, a run across chunks leaves one partial sum per chunk, which a last kernel adds in
+// order.  Rows that no id names are zeros: the blocks beside the sorting ones write them while the sort, which waits on latency, runs.
+#include "tgnn_table.cuh"
+
+using namespace tgnn_table;
+
+namespace {
+
+constexpr int kOneBlock = 12288;    // ids that one block sorts in its shared memory (180 KB)
+constexpr int kSortThreads = 1024;
+constexpr int kTile = 8 * kSortThreads;
+constexpr int kMaxSortBlocks = 148;
+constexpr int kDigits = 256;
+
+// ------------------------------------------------------------------------------------------------------------ forward --
+struct GatherArgs {
+  const void* table;
+  const void* ids;
+  void* out;
+  int32_t* status;
+  int64_t rows, n;
+  float scale;
+  int dim, groups;        // groups of V values per row
+  int rows_per_block;
+  uint32_t magic;         // ceil(2^32 / groups): x * magic >> 32 = x / groups for x * groups < 2^32; 0 for groups = 1
+};
+
+template <typename TT, typename TO, int V, typename I>
+__global__ void __launch_bounds__(256) lookup_kernel(const GatherArgs a) {
+  const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
+  const int count = (int)min((int64_t)a.rows_per_block, a.n - r0) * a.groups;
+  const I* ids = static_cast<const I*>(a.ids) + r0;
+  const TT* table = static_cast<const TT*>(a.table);
+  TO* out = static_cast<TO*>(a.out) + r0 * a.dim;
+  constexpr int U = 4;
+  for (int x0 = threadIdx.x; x0 < count; x0 += 256 * U) {
+    int row[U];
+    int64_t id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + 256 * u;
+      row[u] = a.magic ? (int)__umulhi((uint32_t)x, a.magic) : x;
+      id[u] = x < count ? (int64_t)ids[row[u]] : -1;
+    }
+    Group<TT, V> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + 256 * u;
+      if (id[u] >= 0 && id[u] < a.rows)
+        v[u] = *reinterpret_cast<const Group<TT, V>*>(table + id[u] * a.dim + (x - row[u] * a.groups) * V);
+      else if (id[u] >= a.rows) {
+        *a.status = 4;
+        id[u] = -1;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int x = x0 + 256 * u;
+      if (x >= count) break;
+      float f[V];
+      if (id[u] >= 0) {
+        v[u].get(f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] *= a.scale;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = 0.f;
+      }
+      TO* p = out + (int64_t)x * V;
+      constexpr int W = V * sizeof(TO) > 16 ? 16 / (int)sizeof(TO) : V;      // values per store
+#pragma unroll
+      for (int i = 0; i < V; i += W) {
+        Group<TO, W> g;
+        g.set(f + i);
+        *reinterpret_cast<Group<TO, W>*>(p + i) = g;
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------------------------------------------- sort --
+struct SortArgs {
+  const void* ids;
+  int index_bits;
+  int64_t rows;
+  uint32_t n;
+  const uint2* in;        // (id, place) of the pass before; nullptr: the ids themselves
+  uint2* out;
+  uint32_t* hist;         // [sort blocks][kDigits]
+  int32_t* status;        // checked on the first look at the ids; nullptr afterwards
+  uint32_t* counter;      // zeroed by the first kernel
+  int shift, width;       // the digit
+  int passes;             // one-block sort: how many digits, `width` bits each
+  int sort_blocks;
+  uint32_t per_block;
+  char* zero;             // dtable: blocks behind the sorting ones fill their share of it with zeros
+  int64_t zero_bytes;
+  int share, shares;
+};
+
+// An id as a key: ids below 0 and outside the table come last, as `rows`.
+__device__ __forceinline__ uint32_t key_of(const SortArgs& a, uint32_t i) {
+  const int64_t id = a.index_bits == 64 ? static_cast<const int64_t*>(a.ids)[i] : static_cast<const int32_t*>(a.ids)[i];
+  if (id >= 0 && id < a.rows) return (uint32_t)id;
+  if (id >= 0 && a.status) *a.status = 4;
+  return (uint32_t)a.rows;
+}
+
+__device__ __forceinline__ void fill_zero(const SortArgs& a, int block, int blocks) {
+  char* lo = reinterpret_cast<char*>(((uintptr_t)a.zero + 15) & ~(uintptr_t)15);
+  char* end = a.zero + a.zero_bytes;
+  if (lo > end) lo = end;
+  const int64_t words = (end - lo) >> 4;
+  const int64_t w0 = words * a.share / a.shares, w1 = words * (a.share + 1) / a.shares;
+  for (int64_t w = w0 + (int64_t)block * blockDim.x + threadIdx.x; w < w1; w += (int64_t)blocks * blockDim.x)
+    __stcs(reinterpret_cast<uint4*>(lo) + w, make_uint4(0, 0, 0, 0));
+  if (a.share == 0 && block == 0 && threadIdx.x == 0) {                       // what lies before and behind whole words, by 2 bytes
+    for (char* p = a.zero; p < lo; p += 2) *reinterpret_cast<uint16_t*>(p) = 0;
+    for (char* p = lo + 16 * words; p < end; p += 2) *reinterpret_cast<uint16_t*>(p) = 0;
+  }
+}
+
+// Ranks of a warp's keys among those of the warp with the same digit, in order: lanes, then rounds.  `mine` counts the warp's digits.
+template <int K>
+__device__ __forceinline__ void rank_keys(const uint32_t (&digit)[K], uint32_t (&rank)[K], uint32_t* mine, int lane) {
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const unsigned same = __match_any_sync(FULL, digit[k]);
+    const int leader = __ffs(same) - 1;
+    uint32_t before = 0;
+    if (lane == leader && digit[k] < kDigits) {
+      before = mine[digit[k]];
+      mine[digit[k]] = before + __popc(same);
+    }
+    before = __shfl_sync(FULL, before, leader);
+    rank[k] = before + __popc(same & ((1u << lane) - 1));
+    __syncwarp();
+  }
+}
+
+// counts[warp][digit] -> where that warp's keys of the digit begin within the block, total[digit] = keys of the block.  1024 threads: four
+// groups of eight warps, a thread per group and digit.
+__device__ __forceinline__ void scan_warps(uint32_t (*counts)[kDigits], uint32_t (*part)[kDigits], uint32_t* total) {
+  const int d = threadIdx.x & (kDigits - 1), grp = threadIdx.x >> 8;
+  uint32_t c[8], sum = 0;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    c[w] = counts[8 * grp + w][d];
+    const uint32_t x = c[w];
+    c[w] = sum;
+    sum += x;
+  }
+  part[grp][d] = sum;
+  __syncthreads();
+  uint32_t at = 0;
+  for (int g = 0; g < grp; ++g) at += part[g][d];
+  if (grp == 3) total[d] = at + sum;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) counts[8 * grp + w][d] = c[w] + at;
+  __syncthreads();
+}
+
+// Exclusive sums of total[] into base[], by the first eight warps.
+__device__ __forceinline__ void scan_digits(const uint32_t* total, uint32_t* base, uint32_t* warp_sum) {
+  const int t = threadIdx.x, lane = t & 31;
+  uint32_t x = 0, inc = 0;
+  if (t < kDigits) {
+    x = inc = total[t];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(FULL, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) warp_sum[t >> 5] = inc;
+  }
+  __syncthreads();
+  if (t < kDigits) {
+    uint32_t at = inc - x;
+    for (int w = 0; w < (t >> 5); ++w) at += warp_sum[w];
+    base[t] = at;
+  }
+  __syncthreads();
+}
+
+// Up to 12288 ids: one block takes all digits in its shared memory, the others fill zeros.
+struct OneBlock {
+  uint32_t key[2][kOneBlock];
+  uint16_t place[2][kOneBlock];
+  uint32_t counts[32][kDigits];
+};
+__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const SortArgs a) {
+  extern __shared__ unsigned char raw[];
+  OneBlock& s = *reinterpret_cast<OneBlock*>(raw);
+  __shared__ uint32_t part[4][kDigits], total[kDigits], base[kDigits], warp_sum[8];
+  chain_release();
+  if (blockIdx.x > 0) {
+    fill_zero(a, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  constexpr int K = kOneBlock / kSortThreads;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const uint32_t span = (uint32_t)up(a.n, kSortThreads) / 32;                 // places per warp, a multiple of 32
+  if (t == 0) *a.counter = 0;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const uint32_t i = warp * span + 32 * k + lane;
+    if (32u * k < span && i < a.n) {
+      s.key[0][i] = key_of(a, i);
+      s.place[0][i] = (uint16_t)i;
+    }
+  }
+  for (int p = 0; p < a.passes; ++p) {
+    for (int i = t; i < 32 * kDigits; i += kSortThreads) (&s.counts[0][0])[i] = 0;
+    __syncthreads();
+    const uint32_t *key = s.key[p & 1];
+    const uint16_t* place = s.place[p & 1];
+    const int shift = p * a.width;
+    const uint32_t mask = (1u << a.width) - 1;
+    uint32_t digit[K], rank[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t i = warp * span + 32 * k + lane;
+      digit[k] = 32u * k < span && i < a.n ? (key[i] >> shift) & mask : kDigits;
+    }
+    if (span == K * 32) rank_keys<K>(digit, rank, s.counts[warp], lane);
+    else
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (32u * k < span) rank_keys<1>(reinterpret_cast<uint32_t(&)[1]>(digit[k]), reinterpret_cast<uint32_t(&)[1]>(rank[k]), s.counts[warp], lane);
+    __syncthreads();
+    scan_warps(s.counts, part, total);
+    scan_digits(total, base, warp_sum);
+    const bool last = p == a.passes - 1;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (digit[k] >= kDigits) continue;
+      const uint32_t i = warp * span + 32 * k + lane;
+      const uint32_t to = base[digit[k]] + s.counts[warp][digit[k]] + rank[k];
+      if (last) a.out[to] = make_uint2(key[i], place[i]);
+      else {
+        s.key[(p + 1) & 1][to] = key[i];
+        s.place[(p + 1) & 1][to] = place[i];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Many ids: per digit, a kernel that counts the digits of every block's share and one that moves the keys.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
+  __shared__ uint32_t count[kDigits];
+  chain_wait();
+  chain_release();
+  if ((int)blockIdx.x >= a.sort_blocks) {
+    fill_zero(a, blockIdx.x - a.sort_blocks, gridDim.x - a.sort_blocks);
+    return;
+  }
+  const uint32_t lo = blockIdx.x * a.per_block, hi = min(a.n, lo + a.per_block);
+  const uint32_t mask = (1u << a.width) - 1;
+  if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.counter = 0;
+  __syncthreads();
+  for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
+    const uint32_t d = ((a.in ? a.in[i].x : key_of(a, i)) >> a.shift) & mask;
+    const unsigned same = __match_any_sync(__activemask(), d);                // hubs: one addition per warp and digit
+    if ((threadIdx.x & 31) == __ffs(same) - 1) atomicAdd(count + d, __popc(same));
+  }
+  __syncthreads();
+  if (threadIdx.x < kDigits) a.hist[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs a) {
+  __shared__ uint32_t counts[32][kDigits];
+  __shared__ uint32_t part[4][kDigits], total[kDigits], base[kDigits], warp_sum[8];
+  chain_wait();
+  chain_release();
+  if ((int)blockIdx.x >= a.sort_blocks) {
+    fill_zero(a, blockIdx.x - a.sort_blocks, gridDim.x - a.sort_blocks);
+    return;
+  }
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  {  // where this block's keys of every digit begin: all keys of smaller digits, and the blocks before it
+    const int d = t & (kDigits - 1), grp = t >> 8, me = blockIdx.x;
+    const int b0 = a.sort_blocks * grp / 4, b1 = a.sort_blocks * (grp + 1) / 4;
+    uint32_t all = 0, before = 0;
+#pragma unroll 8
+    for (int b = b0; b < b1; ++b) {
+      const uint32_t x = a.hist[b * kDigits + d];
+      all += x;
+      before += b < me ? x : 0;
+    }
+    part[grp][d] = all;
+    counts[grp][d] = before;
+    __syncthreads();
+    if (t < kDigits) total[t] = part[0][t] + part[1][t] + part[2][t] + part[3][t];
+    __syncthreads();
+    scan_digits(total, base, warp_sum);
+    if (t < kDigits) base[t] += counts[0][t] + counts[1][t] + counts[2][t] + counts[3][t];
+    __syncthreads();
+  }
+  const uint32_t lo = blockIdx.x * a.per_block, hi = min(a.n, lo + a.per_block);
+  const uint32_t mask = (1u << a.width) - 1;
+  constexpr int K = kTile / kSortThreads;
+  for (uint32_t tile = lo; tile < hi; tile += kTile) {
+    for (int i = t; i < 32 * kDigits; i += kSortThreads) (&counts[0][0])[i] = 0;
+    __syncthreads();
+    uint2 kp[K];
+    uint32_t digit[K], rank[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t i = tile + warp * (32 * K) + 32 * k + lane;
+      digit[k] = kDigits;
+      if (i < hi) {
+        kp[k] = a.in ? a.in[i] : make_uint2(key_of(a, i), i);
+        digit[k] = (kp[k].x >> a.shift) & mask;
+      }
+    }
+    rank_keys<K>(digit, rank, counts[warp], lane);
+    __syncthreads();
+    scan_warps(counts, part, total);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (digit[k] < kDigits) a.out[base[digit[k]] + counts[warp][digit[k]] + rank[k]] = kp[k];
+    __syncthreads();
+    if (t < kDigits) base[t] += total[t];
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------------- run sums --
+struct SumArgs {
+  const uint2* sorted;
+  const void* dout;
+  void* dtable;
+  int dtype;              // of dtable
+  float* partial;         // [chunk][head, tail][dim]
+  uint8_t* through;       // [chunk]: the run at its start goes on behind its end
+  uint32_t* list;         // chunks at whose end a run that begins in them goes on
+  uint32_t* counter;
+  uint32_t n, rows;
+  int dim, groups, chunk;
+  float scale;
+};
+
+__device__ __forceinline__ void store_row(void* base, int dtype, int64_t at, float x) {
+  if (dtype == TGNN_F32) static_cast<float*>(base)[at] = x;
+  else if (dtype == TGNN_BF16) static_cast<__nv_bfloat16*>(base)[at] = __float2bfloat16_rn(x);
+  else static_cast<__half*>(base)[at] = __float2half_rn(x);
+}
+template <int V>
+__device__ __forceinline__ void store_values(void* base, int dtype, int64_t at, const float* x) {
+  if (dtype == TGNN_F32) {
+    constexpr int W = V > 4 ? 4 : V;
+#pragma unroll
+    for (int i = 0; i < V; i += W) {
+      Group<float, W> g;
+      g.set(x + i);
+      if (V == 1 || (((uintptr_t)base & (4 * W - 1)) == 0)) *reinterpret_cast<Group<float, W>*>(static_cast<float*>(base) + at + i) = g;
+      else
+        for (int j = 0; j < W; ++j) static_cast<float*>(base)[at + i + j] = x[i + j];
+    }
+  } else {
+    const bool wide = ((uintptr_t)base & (2 * V - 1)) == 0;
+    if (wide) {
+      if (dtype == TGNN_BF16) {
+        Group<__nv_bfloat16, V> g;
+        g.set(x);
+        *reinterpret_cast<Group<__nv_bfloat16, V>*>(static_cast<__nv_bfloat16*>(base) + at) = g;
+      } else {
+        Group<__half, V> g;
+        g.set(x);
+        *reinterpret_cast<Group<__half, V>*>(static_cast<__half*>(base) + at) = g;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) store_row(base, dtype, at + i, x[i]);
+    }
+  }
+}
+
+// G lanes take a chunk of the sorted order and V values each of a slice of G * V columns (grid.y slices).  Eight rows are asked for before
+// the first is added.
+template <typename T, int V, int G>
+__global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
+  chain_wait();
+  chain_release();
+  const int lane = threadIdx.x & (G - 1);
+  const uint32_t chunk = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const int col = blockIdx.y * G + lane;
+  const int64_t t0 = (int64_t)chunk * a.chunk;
+  if (t0 >= a.n) return;
+  const uint32_t end = (uint32_t)min((int64_t)a.n, t0 + a.chunk);
+  const bool active = col < a.groups;
+  const T* dout = static_cast<const T*>(a.dout) + col * V;
+  uint32_t cur = a.sorted[t0].x;
+  bool head = t0 > 0 && cur < a.rows && a.sorted[t0 - 1].x == cur;            // the first run began in an earlier chunk
+  float acc[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] = 0.f;
+  constexpr int U = 8;
+  auto write = [&](bool to_partial, int slot) {
+    if (!active) return;
+    if (to_partial) {
+      float* p = a.partial + ((int64_t)2 * chunk + slot) * a.dim + col * V;
+#pragma unroll
+      for (int i = 0; i < V; ++i) p[i] = acc[i];
+    } else {
+      float x[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[i] = acc[i] * a.scale;
+      store_values<V>(a.dtable, a.dtype, (int64_t)cur * a.dim + col * V, x);
+    }
+  };
+  bool whole = true;                                                          // no run has ended yet
+  for (uint32_t t = (uint32_t)t0; t < end && cur < a.rows; t += U) {
+    uint2 kp[U];
+    Group<T, V> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) kp[u] = t + u < end ? a.sorted[t + u] : make_uint2(0xffffffffu, 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (active && kp[u].x < a.rows) v[u] = *reinterpret_cast<const Group<T, V>*>(dout + (int64_t)kp[u].y * a.dim);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (t + u >= end) break;
+      if (kp[u].x != cur) {
+        write(head, 0);
+        head = whole = false;
+        cur = kp[u].x;
+        if (cur >= a.rows) break;
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = 0.f;
+      }
+      float f[V];
+      v[u].get(f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += f[i];
+    }
+  }
+  bool goes_on = false;
+  if (cur < a.rows) {
+    goes_on = end < a.n && a.sorted[end].x == cur;
+    if (head) write(true, 0);
+    else write(goes_on, 1);
+  }
+  if (lane == 0 && blockIdx.y == 0) {
+    a.through[chunk] = head && whole && goes_on;
+    if (goes_on && !head) a.list[atomicAdd(a.counter, 1u)] = chunk;
+  }
+}
+
+// Runs across chunks: tail of the chunk that they begin in, then the heads of the next ones.  A block per run and 32 columns, eight warps that take every
+// eighth part; the list's order does not matter.
+__global__ void __launch_bounds__(256) run_join_kernel(const SumArgs a, uint32_t chunks) {
+  chain_wait();
+  chain_release();
+  __shared__ float sum[8][32];
+  __shared__ uint32_t s_last;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t runs = *a.counter;
+  for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
+    const uint32_t c0 = a.list[r];
+    uint32_t last = c0 + 1;                                                   // the last chunk that the run reaches
+    for (;; last += 256) {
+      if (threadIdx.x == 0) s_last = 0xffffffffu;
+      __syncthreads();
+      const uint32_t c = last + threadIdx.x;
+      if (c >= chunks || !a.through[c]) atomicMin(&s_last, c);
+      __syncthreads();
+      const uint32_t x = s_last;
+      __syncthreads();
+      if (x != 0xffffffffu) {
+        last = min(x, chunks - 1);
+        break;
+      }
+    }
+    const uint32_t id = a.sorted[(int64_t)(c0 + 1) * a.chunk].x;
+    for (int col = blockIdx.y * 32 + lane; col - lane < a.dim; col += gridDim.y * 32) {
+      float x = 0.f;
+      if (col < a.dim) {
+        if (warp == 0) x = a.partial[((int64_t)2 * c0 + 1) * a.dim + col];
+#pragma unroll 4
+        for (uint32_t c = c0 + 1 + warp; c <= last; c += 8) x += a.partial[(int64_t)2 * c * a.dim + col];
+      }
+      sum[warp][lane] = x;
+      __syncthreads();
+      if (warp == 0 && col < a.dim) {
+        float y = sum[0][lane];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) y += sum[w][lane];
+        store_row(a.dtable, a.dtype, (int64_t)id * a.dim + col, y * a.scale);
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------- host side --
+template <typename TT, typename TO, int V>
+void gather(Chain& c, const GatherArgs& a, int bits, unsigned blocks) {
+  if (bits == 64) c(lookup_kernel<TT, TO, V, int64_t>, dim3(blocks), dim3(256), 0, a);
+  else c(lookup_kernel<TT, TO, V, int32_t>, dim3(blocks), dim3(256), 0, a);
+}
+template <typename TT, typename TO>
+void gather_type(Chain& c, GatherArgs a, int bits) {
+  // the widest group of values that divides a row and that both sides' addresses allow
+  constexpr int W = 16 / (int)sizeof(TT);
+  auto fits = [&](int v) {
+    const int wo = v * (int)sizeof(TO) > 16 ? 16 : v * (int)sizeof(TO);
+    return a.dim % v == 0 && ((uintptr_t)a.table & (v * sizeof(TT) - 1)) == 0 && ((uintptr_t)a.out & (wo - 1)) == 0;
+  };
+  const int v = fits(W) ? W : fits(2) ? 2 : 1;
+  a.groups = a.dim / v;
+  a.magic = a.groups == 1 ? 0 : (uint32_t)(((1ull << 32) + a.groups - 1) / a.groups);
+  a.rows_per_block = a.groups >= 1024 ? 1 : 1024 / a.groups;
+  // few rows: fewer per block, so that they reach every multiprocessor
+  while (a.rows_per_block > 1 && (int64_t)a.rows_per_block * 2 * num_sms() > a.n && a.rows_per_block * a.groups > 256) a.rows_per_block /= 2;
+  const unsigned blocks = (unsigned)((a.n + a.rows_per_block - 1) / a.rows_per_block);
+  if (v == W) gather<TT, TO, W>(c, a, bits, blocks);
+  else if (v == 2) gather<TT, TO, 2>(c, a, bits, blocks);
+  else gather<TT, TO, 1>(c, a, bits, blocks);
+}
+template <typename TT>
+void gather_out(Chain& c, const GatherArgs& a, int out_dtype, int bits) {
+  if (out_dtype == TGNN_F32) gather_type<TT, float>(c, a, bits);
+  else if (out_dtype == TGNN_BF16) gather_type<TT, __nv_bfloat16>(c, a, bits);
+  else gather_type<TT, __half>(c, a, bits);
+}
+
+template <typename T, int V>
+void sum_lanes(Chain& c, const SumArgs& a, uint32_t chunks) {
+  auto go = [&](auto kernel, int g) { c(kernel, dim3((chunks + 256 / g - 1) / (256 / g), (a.groups + g - 1) / g), dim3(256), 0, a); };
+  if (a.groups <= 8) go(run_sum_kernel<T, V, 8>, 8);
+  else if (a.groups <= 16) go(run_sum_kernel<T, V, 16>, 16);
+  else go(run_sum_kernel<T, V, 32>, 32);
+}
+template <typename T>
+void sum_type(Chain& c, SumArgs a, uint32_t chunks) {
+  constexpr int W = 16 / (int)sizeof(T);
+  auto fits = [&](int v) { return a.dim % v == 0 && ((uintptr_t)a.dout & (v * sizeof(T) - 1)) == 0; };
+  const int v = fits(W) ? W : fits(2) ? 2 : 1;
+  a.groups = a.dim / v;
+  if (v == W) sum_lanes<T, W>(c, a, chunks);
+  else if (v == 2) sum_lanes<T, 2>(c, a, chunks);
+  else sum_lanes<T, 1>(c, a, chunks);
+}
+
+// Ids per chunk: few enough that the chunks fill the device, and so many that a hub's run has few parts.
+int chunk_of(int64_t n) { return n <= 1 << 16 ? 16 : n <= 1 << 18 ? 32 : n <= 1 << 19 ? 64 : 128; }
+
+struct Scratch {
+  int64_t sorted[2], hist, through, list, counter, partial, bytes;
+};
+Scratch layout(int64_t n, int dim) {
+  const int64_t chunks = (n + chunk_of(n) - 1) / chunk_of(n);
+  Scratch s;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t p = at;
+    at += up(bytes, 256);
+    return p;
+  };
+  s.sorted[0] = take(8 * n);
+  s.sorted[1] = n > kOneBlock ? take(8 * n) : s.sorted[0];
+  s.hist = take(4ll * kMaxSortBlocks * kDigits);
+  s.through = take(chunks);
+  s.list = take(4 * chunks);
+  s.counter = take(4);
+  s.partial = take(8ll * chunks * dim);
+  s.bytes = at;
+  return s;
+}
+
+int check(const char* who, int64_t rows, int dim, int index_bits, int64_t n, int dtype, int out_dtype, char* err, int64_t size) {
+  if (!known_dtype(dtype) || !known_dtype(out_dtype)) return fail(err, size, TGNN_EINVAL, "%s: unknown dtype", who);
+  if (index_bits != 32 && index_bits != 64) return fail(err, size, TGNN_EINVAL, "%s: index_bits is 32 or 64", who);
+  if (rows < 0 || n < 0 || dim < 1 || dim > 8192) return fail(err, size, TGNN_EINVAL, "%s: size out of range (dim 1 to 8192)", who);
+  if (rows >= 0x7fffffff || n >= 0x7fffffff) return fail(err, size, TGNN_ECAPACITY, "%s: rows or n beyond int32", who);
+  return TGNN_OK;
+}
+
+}  // namespace
+
+extern "C" TGNN_API int tgnn_lookup(const void* table, int dtype, int64_t rows, int dim, const void* ids, int index_bits, int64_t n, float scale,
+                                    void* out, int out_dtype, int32_t* status, void* stream, char* err, int64_t err_size) {
+  const char* who = "tgnn_lookup";
+  if (int rc = check(who, rows, dim, index_bits, n, dtype, out_dtype, err, err_size)) return rc;
+  if (n == 0) return TGNN_OK;
+  if ((rows > 0 && !table) || !ids || !out || !status) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", who);
+  if (((uintptr_t)table & (elem_bytes(dtype) - 1)) || ((uintptr_t)out & (elem_bytes(out_dtype) - 1)) || ((uintptr_t)ids & (index_bits / 8 - 1)) ||
+      ((uintptr_t)status & 3))
+    return fail(err, err_size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", who);
+  GatherArgs a = {};
+  a.table = table;
+  a.ids = ids;
+  a.out = out;
+  a.status = status;
+  a.rows = rows;
+  a.n = n;
+  a.scale = scale;
+  a.dim = dim;
+  Chain c(stream);
+  if (dtype == TGNN_F32) gather_out<float>(c, a, out_dtype, index_bits);
+  else if (dtype == TGNN_BF16) gather_out<__nv_bfloat16>(c, a, out_dtype, index_bits);
+  else gather_out<__half>(c, a, out_dtype, index_bits);
+  return c.end(who, err, err_size);
+}
+
+extern "C" TGNN_API int64_t tgnn_lookup_scratch(int64_t n, int64_t rows, int dim) {
+  if (n < 0 || rows < 0 || n >= 0x7fffffff || rows >= 0x7fffffff || dim < 1 || dim > 8192) return -1;
+  return layout(n, dim).bytes;
+}
+
+extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, int64_t n, const void* dout, int out_dtype, int64_t rows, int dim,
+                                             float scale, void* dtable, int dtype, void* scratch, int32_t* status, void* stream, char* err,
+                                             int64_t err_size) {
+  const char* who = "tgnn_lookup_backward";
+  if (int rc = check(who, rows, dim, index_bits, n, dtype, out_dtype, err, err_size)) return rc;
+  if ((rows > 0 && !dtable) || (n > 0 && (!ids || !dout || !scratch || !status))) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", who);
+  if (((uintptr_t)dtable & (elem_bytes(dtype) - 1)) || ((uintptr_t)dout & (elem_bytes(out_dtype) - 1)) ||
+      ((uintptr_t)ids & (index_bits / 8 - 1)) || ((uintptr_t)scratch & 255) || ((uintptr_t)status & 3))
+    return fail(err, err_size, TGNN_EINVAL, "%s: a pointer is not aligned (scratch to 256 bytes, the others to their elements)", who);
+  const int64_t bytes = rows * dim * elem_bytes(dtype);
+  if (n == 0) {
+    if (bytes > 0 && cudaMemsetAsync(dtable, 0, (size_t)bytes, (cudaStream_t)stream) != cudaSuccess)
+      return fail(err, err_size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(cudaGetLastError()));
+    return TGNN_OK;
+  }
+  const Scratch l = layout(n, dim);
+  char* base = static_cast<char*>(scratch);
+  int key_bits = 1;
+  while ((rows >> key_bits) != 0) ++key_bits;
+  SortArgs s = {};
+  s.ids = ids;
+  s.index_bits = index_bits;
+  s.rows = rows;
+  s.n = (uint32_t)n;
+  s.hist = reinterpret_cast<uint32_t*>(base + l.hist);
+  s.status = status;
+  s.counter = reinterpret_cast<uint32_t*>(base + l.counter);
+  s.zero = static_cast<char*>(dtable);
+  s.zero_bytes = bytes;
+  s.passes = (key_bits + 7) / 8;
+  s.width = (key_bits + s.passes - 1) / s.passes;
+  const int sms = num_sms();
+  const int fillers = (int)(bytes >> 14 >= 4 * sms ? 4 * sms : (bytes >> 14) + 1);
+  Chain c(stream);
+  int sorted = 0;
+  if (n <= kOneBlock) {
+    c.e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(OneBlock));
+    s.out = reinterpret_cast<uint2*>(base + l.sorted[0]);
+    s.shares = 1;
+    c(sort_one_kernel, dim3(1 + fillers), dim3(kSortThreads), sizeof(OneBlock), s);
+  } else {
+    const int64_t tiles = (n + kTile - 1) / kTile;
+    s.sort_blocks = (int)(tiles < kMaxSortBlocks ? tiles : kMaxSortBlocks);
+    s.per_block = (uint32_t)((n + s.sort_blocks - 1) / s.sort_blocks);
+    s.shares = 2 * s.passes;
+    for (int p = 0; p < s.passes; ++p) {
+      s.shift = p * s.width;
+      s.in = p ? reinterpret_cast<uint2*>(base + l.sorted[sorted]) : nullptr;
+      sorted = p & 1;
+      s.out = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
+      s.share = 2 * p;
+      c(sort_count_kernel, dim3(s.sort_blocks + fillers), dim3(kSortThreads), 0, s);
+      s.share = 2 * p + 1;
+      s.status = nullptr;
+      c(sort_move_kernel, dim3(s.sort_blocks + fillers), dim3(kSortThreads), 0, s);
+    }
+  }
+  SumArgs a = {};
+  a.sorted = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
+  a.dout = dout;
+  a.dtable = dtable;
+  a.dtype = dtype;
+  a.partial = reinterpret_cast<float*>(base + l.partial);
+  a.through = reinterpret_cast<uint8_t*>(base + l.through);
+  a.list = reinterpret_cast<uint32_t*>(base + l.list);
+  a.counter = s.counter;
+  a.n = (uint32_t)n;
+  a.rows = (uint32_t)rows;
+  a.dim = dim;
+  a.chunk = chunk_of(n);
+  a.scale = scale;
+  const uint32_t chunks = (uint32_t)((n + a.chunk - 1) / a.chunk);
+  if (out_dtype == TGNN_F32) sum_type<float>(c, a, chunks);
+  else if (out_dtype == TGNN_BF16) sum_type<__nv_bfloat16>(c, a, chunks);
+  else sum_type<__half>(c, a, chunks);
+  if (chunks > 1) {
+    const unsigned y = (unsigned)(dim + 31) / 32, x = (unsigned)(8 * sms) / (y < 8 ? y : 8);
+    c(run_join_kernel, dim3(chunks < x ? chunks : x, y), dim3(256), 0, a, chunks);
+  }
+  return c.end(who, err, err_size);
+}

@@ -1,4 +1,4 @@
-/* Argument marshalling of the history operators for Python, without ctypes: checks of the tensors, then the call of the C entry
+/* Argument marshalling of the history and node-table operators for Python, without ctypes: checks of the tensors, then the call of the C entry
  * point.  A call through ctypes spends 10 us on twenty arguments, more than its kernels take on small batches; here a tensor costs 0.2 us.
  * Plain CPython API; tensors are asked through their own methods, so nothing is linked against torch.
  *
@@ -11,9 +11,9 @@
 #include "../../include/tgnn.h"
 
 static PyObject *s_dtype, *s_get_device, *s_is_contiguous, *s_numel, *s_data_ptr, *s_size, *s_dim, *s_stride;
-enum { I32, I64, F32, F64, BF16, F16, KINDS };
-static PyObject* g_dtype[KINDS];
-static const char* const g_name[KINDS] = {"int32", "int64", "float32", "float64", "bfloat16", "float16"};
+enum { I32, I64, F32, F64, BF16, F16, KINDS, U8 = KINDS, I8, ALL };
+static PyObject* g_dtype[ALL];
+static const char* const g_name[ALL] = {"int32", "int64", "float32", "float64", "bfloat16", "float16", "uint8", "int8"};
 static PyObject *g_device, *g_stream;
 
 static struct {
@@ -57,10 +57,11 @@ static int kind_of(PyObject* t) { /* -1: of no kind that is used here, or no ten
     return -1;
   }
   Py_DECREF(d); /* dtypes live as long as the interpreter */
-  for (int k = 0; k < KINDS; ++k)
+  for (int k = 0; k < ALL; ++k)
     if (d == g_dtype[k]) return k;
   return -1;
 }
+static int is_row(int kind) { return kind == F32 || kind == BF16 || kind == F16; }
 static int row_type(int kind) { return kind == F32 ? TGNN_F32 : kind == BF16 ? TGNN_BF16 : TGNN_F16; }
 
 static int refuse(PyObject* t, const char* name, const char* want, long long n, long long dev) { /* an exception that is there stays */
@@ -213,7 +214,7 @@ static PyObject* py_cache_move(PyObject* self, PyObject* const* a, Py_ssize_t na
   if (number(a[2], &dev) || number(a[3], &cache_rows) || number(a[4], &heads) || number(a[5], &dim)) return NULL;
   PyObject* rows = a[6];
   const int kind = kind_of(rows);
-  if (kind < F32 || kind == F64 || ask(rows, s_get_device) != dev) return refuse(rows, "rows", "float32, bfloat16 or float16", -1, dev), NULL;
+  if (!is_row(kind) || ask(rows, s_get_device) != dev) return refuse(rows, "rows", "float32, bfloat16 or float16", -1, dev), NULL;
   const long long d = ask(rows, s_dim), num = d < 1 ? -1 : ask1(rows, s_size, 0);
   if (failed(num)) return NULL;
   if (!(d == 2 && ask1(rows, s_size, 1) == heads * dim) && !(d == 3 && ask1(rows, s_size, 1) == heads && ask1(rows, s_size, 2) == dim)) {
@@ -297,7 +298,7 @@ static PyObject* py_cached_attend(PyObject* self, PyObject* const* a, Py_ssize_t
   if (number(a[2], &dev) || number(a[3], &rows) || number(a[4], &dim) || small(a[8], &window) || small(a[9], &sinks) || small(a[10], &max_len))
     return NULL;
   const int kind = kind_of(a[5]);
-  if (kind < F32 || kind == F64) return refuse(a[5], "q", "float32, bfloat16 or float16", -1, dev), NULL;
+  if (!is_row(kind)) return refuse(a[5], "q", "float32, bfloat16 or float16", -1, dev), NULL;
   if (shape(a[5], 3, sh, "q") || sizes_fit(sh + 1, 2)) return NULL;
   if (sh[2] != dim) return PyErr_Format(PyExc_TypeError, "q: expected [n, heads, dim = %lld]", dim);
   const long long n = sh[0];
@@ -328,7 +329,7 @@ struct slots {
 static int slot_args(PyObject* const* a, struct slots* s) {
   long long sh[3], rw[4];
   s->kind = kind_of(a[0]);
-  s->dev = s->kind < F32 || s->kind == F64 ? -1 : ask(a[0], s_get_device);
+  s->dev = !is_row(s->kind) ? -1 : ask(a[0], s_get_device);
   if (s->dev < 0) return refuse(a[0], "q", "float32, bfloat16 or float16", -1, 0);
   if (shape(a[0], 3, sh, "q") || shape(a[1], 4, rw, "k") || sizes_fit(sh + 1, 2) || sizes_fit(rw + 1, 2)) return -1;
   if (rw[0] != sh[0] || rw[3] != sh[2]) {
@@ -402,12 +403,163 @@ static PyObject* py_init(PyObject* self, PyObject* args) {
   Py_RETURN_NONE;
 }
 
+/* ---- node-table operators ---- */
+static struct {
+  int (*lookup)(const void*, int, int64_t, int, const void*, int, int64_t, float, void*, int, int32_t*, void*, char*, int64_t);
+  int64_t (*lookup_scratch)(int64_t, int64_t, int);
+  int (*lookup_backward)(const void*, int, int64_t, const void*, int, int64_t, int, float, void*, int, void*, int32_t*, void*, char*, int64_t);
+  int (*adamw_step)(const tgnn_adamw_tensor*, int, int, int64_t*, double, double, double, double, double, uint64_t, void*, char*, int64_t);
+  int (*adamw_moments)(const tgnn_adamw_tensor*, int, float* const*, float* const*, void*, char*, int64_t);
+} table_fn;
+
+/* A dense 2D tensor of rows of any row type; dev < 0: on any device */
+static int matrix(PyObject* t, long long* dev, const char* name, int* kind, long long* sh, void** p) {
+  *kind = kind_of(t);
+  const long long on = !is_row(*kind) ? -1 : ask(t, s_get_device);
+  if (on < 0 || (*dev >= 0 && on != *dev)) return refuse(t, name, "float32, bfloat16 or float16", -1, *dev);
+  *dev = on;
+  if (shape(t, 2, sh, name) || sizes_fit(sh + 1, 1)) return -1;
+  return vec(t, *kind, on, sh[0] * sh[1], 0, name, p);
+}
+static int indices(PyObject* t, long long dev, const char* name, int* bits, long long* n, void** p) {
+  const int kind = kind_of(t);
+  if (kind != I32 && kind != I64) return refuse(t, name, "int32 or int64", -1, dev);
+  *bits = kind == I64 ? 64 : 32;
+  return vec_n(t, kind, dev, 0, 1, name, p, n);
+}
+/* rows of any row type, n * dim values in any shape */
+static int rows_of(PyObject* t, long long dev, long long values, const char* name, int* kind, void** p) {
+  *kind = kind_of(t);
+  if (!is_row(*kind)) return refuse(t, name, "float32, bfloat16 or float16", -1, dev);
+  return vec(t, *kind, dev, values, 0, name, p);
+}
+static int scratch_of(PyObject* t, long long dev, long long need, void** p) {
+  if (t == Py_None) {
+    PyErr_SetString(PyExc_TypeError, "scratch: expected a uint8 tensor");
+    return -1;
+  }
+  return vec(t, U8, dev, need < 0 ? 0 : need, 1, "scratch", p);
+}
+static int must(PyObject* t, const char* name) {
+  if (t != Py_None) return 0;
+  PyErr_Format(PyExc_TypeError, "%s: expected a tensor, got None", name);
+  return -1;
+}
+
+/* table, ids, out, scale, status */
+static PyObject* py_lookup(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(5);
+  long long dev = -1, sh[2], n;
+  int kind, out_kind, bits;
+  void *table, *ids, *out;
+  int32_t* status;
+  const double scale = PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred() || matrix(a[0], &dev, "table", &kind, sh, &table) || indices(a[1], dev, "ids", &bits, &n, &ids) ||
+      rows_of(a[2], dev, n * sh[1], "out", &out_kind, &out) || must(a[4], "status") || vec(a[4], I32, dev, 1, 0, "status", &status))
+    return NULL;
+  STREAM(dev);
+  CALL(table_fn.lookup(table, row_type(kind), sh[0], (int)sh[1], ids, bits, n, (float)scale, out, row_type(out_kind), status, stream, err, sizeof err));
+}
+
+/* ids, dout, dtable, scratch, scale, status */
+static PyObject* py_lookup_backward(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(6);
+  long long dev = -1, sh[2], n;
+  int kind, out_kind, bits;
+  void *dtable, *ids, *dout, *scratch;
+  int32_t* status;
+  const double scale = PyFloat_AsDouble(a[4]);
+  if (PyErr_Occurred() || matrix(a[2], &dev, "dtable", &kind, sh, &dtable) || indices(a[0], dev, "ids", &bits, &n, &ids) ||
+      rows_of(a[1], dev, n * sh[1], "dout", &out_kind, &dout) || scratch_of(a[3], dev, table_fn.lookup_scratch(n, sh[0], (int)sh[1]), &scratch) ||
+      must(a[5], "status") || vec(a[5], I32, dev, 1, 0, "status", &status))
+    return NULL;
+  STREAM(dev);
+  CALL(table_fn.lookup_backward(ids, bits, n, dout, row_type(out_kind), sh[0], (int)sh[1], (float)scale, dtable, row_type(kind), scratch, status,
+       stream, err, sizeof err));
+}
+
+/* descriptions' address, bits, device, steps, lr, beta1, beta2, eps, grad_scale, seed, params, grads (lists; a gradient may be None) */
+static PyObject* py_adamw_step(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(12);
+  const tgnn_adamw_tensor* held = (const tgnn_adamw_tensor*)PyLong_AsVoidPtr(a[0]);
+  long long dev;
+  int bits;
+  double x[5];
+  int64_t* steps;
+  if (small(a[1], &bits) || number(a[2], &dev)) return NULL;
+  for (int i = 0; i < 5; ++i) x[i] = PyFloat_AsDouble(a[4 + i]);
+  const uint64_t seed = PyLong_AsUnsignedLongLongMask(a[9]);
+  if (PyErr_Occurred() || must(a[3], "steps") || vec(a[3], I64, dev, 2, 0, "steps", &steps)) return NULL;
+  if (!PyList_Check(a[10]) || !PyList_Check(a[11]) || PyList_GET_SIZE(a[10]) != PyList_GET_SIZE(a[11]))
+    return PyErr_Format(PyExc_TypeError, "expected as many gradients as parameters");
+  const Py_ssize_t count = PyList_GET_SIZE(a[10]);
+  tgnn_adamw_tensor* t = (tgnn_adamw_tensor*)PyMem_Malloc((count ? count : 1) * sizeof *t);
+  if (!t) return PyErr_NoMemory();
+  memcpy(t, held, count * sizeof *t);
+  int bad = 0;
+  for (Py_ssize_t i = 0; i < count && !bad; ++i) {
+    PyObject* g = PyList_GET_ITEM(a[11], i);
+    if (g == Py_None) {
+      t[i].numel = 0;
+      continue;
+    }
+    const int kind = kind_of(g);
+    if (!is_row(kind)) bad = refuse(g, "grad", "float32, bfloat16 or float16", -1, dev);
+    else bad = vec(PyList_GET_ITEM(a[10], i), F32, dev, t[i].numel, 0, "param", &t[i].param) || vec(g, kind, dev, t[i].numel, 0, "grad", &t[i].grad);
+    t[i].grad_dtype = row_type(kind);
+  }
+  void* stream;
+  char err[512] = "";
+  const int st = bad ? -1 : stream_of(dev, &stream);
+  if (st < 1) {
+    PyMem_Free(t);
+    return st < 0 ? NULL : PyLong_FromLongLong(dev);
+  }
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = table_fn.adamw_step(t, (int)count, bits, steps, x[0], x[1], x[2], x[3], x[4], seed, stream, err, sizeof err);
+  Py_END_ALLOW_THREADS
+  PyMem_Free(t);
+  return result(rc, err);
+}
+
+/* descriptions' address, count, addresses of the outputs' pointers (m, v), device */
+static PyObject* py_adamw_moments(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(5);
+  const tgnn_adamw_tensor* t = (const tgnn_adamw_tensor*)PyLong_AsVoidPtr(a[0]);
+  float *const *m = (float* const*)PyLong_AsVoidPtr(a[2]), *const *v = (float* const*)PyLong_AsVoidPtr(a[3]);
+  long long dev;
+  int count;
+  if (small(a[1], &count) || number(a[4], &dev) || PyErr_Occurred()) return NULL;
+  STREAM(dev);
+  CALL(table_fn.adamw_moments(t, count, m, v, stream, err, sizeof err));
+}
+
+/* (uint8, int8), (addresses of the node-table entry points); after init */
+static PyObject* py_init_table(PyObject* self, PyObject* args) {
+  PyObject *dt, *at;
+  if (!PyArg_ParseTuple(args, "O!O!", &PyTuple_Type, &dt, &PyTuple_Type, &at)) return NULL;
+  if (PyTuple_GET_SIZE(dt) != ALL - KINDS || PyTuple_GET_SIZE(at) * sizeof(void*) != sizeof table_fn)
+    return PyErr_Format(PyExc_TypeError, "expected %d dtypes and %d addresses", (int)(ALL - KINDS), (int)(sizeof table_fn / sizeof(void*)));
+  void* p[sizeof table_fn / sizeof(void*)];
+  for (size_t i = 0; i < sizeof table_fn / sizeof(void*); ++i) p[i] = PyLong_AsVoidPtr(PyTuple_GET_ITEM(at, i));
+  if (PyErr_Occurred()) return NULL;
+  for (int k = KINDS; k < ALL; ++k) Py_INCREF(g_dtype[k] = PyTuple_GET_ITEM(dt, k - KINDS));
+  memcpy(&table_fn, p, sizeof table_fn);
+  Py_RETURN_NONE;
+}
+
 static PyMethodDef methods[] = {{"init", py_init, METH_VARARGS, NULL},
                                 {"sample_window", (PyCFunction)(void (*)(void))py_sample_window, METH_FASTCALL, NULL},
                                 {"cache_move", (PyCFunction)(void (*)(void))py_cache_move, METH_FASTCALL, NULL},
                                 {"cached_attend", (PyCFunction)(void (*)(void))py_cached_attend, METH_FASTCALL, NULL},
                                 {"slot_attend", (PyCFunction)(void (*)(void))py_slot_attend, METH_FASTCALL, NULL},
                                 {"slot_attend_backward", (PyCFunction)(void (*)(void))py_slot_attend_backward, METH_FASTCALL, NULL},
+                                {"init_table", py_init_table, METH_VARARGS, NULL},
+                                {"lookup", (PyCFunction)(void (*)(void))py_lookup, METH_FASTCALL, NULL},
+                                {"lookup_backward", (PyCFunction)(void (*)(void))py_lookup_backward, METH_FASTCALL, NULL},
+                                {"adamw_step", (PyCFunction)(void (*)(void))py_adamw_step, METH_FASTCALL, NULL},
+                                {"adamw_moments", (PyCFunction)(void (*)(void))py_adamw_moments, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
