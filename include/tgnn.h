@@ -610,8 +610,9 @@ TGNN_API int tgnn_slot_attend_backward(const void* q, const void* k, const void*
                                        void* dq, void* dk, void* dv, float* dbias, float* scratch, void* stream, char* err_host,
                                        int64_t err_size);
 
-/* ---- a learned table of nodes: rows looked up, AdamW ------------------------------------------------------------------
- * What trains a table with one row per node: its rows are looked up by id (neighbor slots, roots), and all tensors are stepped at once.
+/* ---- a learned table of nodes: rows looked up, the loss of a destination among all nodes, AdamW ----------------------
+ * What trains a table with one row per node: its rows are looked up by id (neighbor slots, roots), every root is scored against all
+ * rows (which node comes next, instead of one sampled negative), and all tensors are stepped at once.
  * Stateless, device pointers (except *_host), work enqueued on `stream` of the current device, nothing allocated; errors as above.
  * status: device int32, NOT zeroed by these calls; 4 is recorded for an index beyond its table.  A scratch buffer (256-byte aligned) belongs to
  * the call until the call's work has ended (calls that may overlap, two captured graphs among them, need one each); contents undefined after.
@@ -662,6 +663,29 @@ TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, int count, i
                              double beta2, double eps, double grad_scale, uint64_t seed, void* stream, char* err_host, int64_t err_size);
 TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count, float* const* m_out_host, float* const* v_out_host,
                                 void* stream, char* err_host, int64_t err_size);
+
+/* tgnn_destination_loss: softmax cross entropy of every root's target among all rows of the table, the logits never kept:
+ *   z[i, j] = scale * q[i] . table[j] + bias[j];   loss[i] = log(sum_j exp z[i, j]) - z[i, target[i]]
+ *   q: [n, dim], table: [rows, dim] of `dtype` (TGNN_F32, TGNN_BF16), dense; target of index_bits bits; bias: fp32[rows] or NULL; loss: fp32[n].
+ *   target[i] < 0: the root takes no part (a masked event): loss 0, and whatever its row holds touches nothing.  Beyond the table: the same, status 4.
+ *   A bias of -infinity hides a node (its row has to be finite all the same); one of the type's lowest value works as any finite one.  Where the target
+ *   is hidden the loss is +infinity; where all nodes are, too, and the root has no gradient.
+ *   kept: fp32[tgnn_destination_loss_kept(n, dim)], what the backward pass needs, or NULL where there will be none.
+ * tgnn_destination_loss_backward: with dloss: fp32[n] and p = softmax of z[i], dz[i, j] = dloss[i] (p[j] - [j = target[i]]):
+ *   dq[i] = scale * sum_j dz[i, j] table[j], dtable[j] = scale * sum_i dz[i, j] q[i] (of `dtype`), dbias[j] = sum_i dz[i, j] (fp32);
+ *   each may be NULL where it is not wanted.  Everything asked for is overwritten, in an order fixed by the sizes and the device.  kept as the
+ *   forward pass left it, for the same inputs.
+ * scratch: tgnn_destination_loss_scratch(n, rows, dim, dtype) bytes, in both directions.
+ * dim 1 to 256; rows 1 to 2^31 - 2^16, n below 2^31 - 2^16.  No output may alias an input. */
+TGNN_API int64_t tgnn_destination_loss_kept(int64_t n, int dim);
+TGNN_API int64_t tgnn_destination_loss_scratch(int64_t n, int64_t rows, int dim, int dtype);
+TGNN_API int tgnn_destination_loss(const void* q, const void* table, int dtype, int64_t n, int64_t rows, int dim, const void* target,
+                                   int index_bits, const float* bias, float scale, float* loss, float* kept, void* scratch, int32_t* status,
+                                   void* stream, char* err_host, int64_t err_size);
+TGNN_API int tgnn_destination_loss_backward(const void* q, const void* table, int dtype, int64_t n, int64_t rows, int dim, const void* target,
+                                            int index_bits, const float* bias, float scale, const float* kept, const float* dloss, void* dq,
+                                            void* dtable, float* dbias, void* scratch, int32_t* status, void* stream, char* err_host,
+                                            int64_t err_size);
 
 #ifdef __cplusplus
 }

@@ -39,7 +39,8 @@ EXPORTS = ("tgnn_create", "tgnn_destroy", "tgnn_last_error", "tgnn_param_count",
            "tgnn_pack_rows", "tgnn_unpack_rows", "tgnn_debug_get_embeddings", "tgnn_debug_gemm_split",
            "tgnn_clear_status", "tgnn_order_streams", "tgnn_sample_window", "tgnn_cache_code_bytes", "tgnn_cache_write",
            "tgnn_cache_read", "tgnn_cached_attend", "tgnn_slot_attend", "tgnn_slot_attend_scratch", "tgnn_slot_attend_backward",
-           "tgnn_lookup", "tgnn_lookup_scratch", "tgnn_lookup_backward", "tgnn_adamw_blocks", "tgnn_adamw_step", "tgnn_adamw_moments")
+           "tgnn_lookup", "tgnn_lookup_scratch", "tgnn_lookup_backward", "tgnn_destination_loss", "tgnn_destination_loss_kept",
+           "tgnn_destination_loss_scratch", "tgnn_destination_loss_backward", "tgnn_adamw_blocks", "tgnn_adamw_step", "tgnn_adamw_moments")
 TGNN_STATIC_MAX_NODES = 65536
 
 
@@ -150,8 +151,13 @@ def load_library():
         lib.tgnn_lookup.argtypes = [vp, i32, i64, i32, vp, i32, i64, f32, vp, i32, vp, vp, vp, i64]
         lib.tgnn_lookup_scratch.argtypes = [i64, i64, i32]
         lib.tgnn_lookup_backward.argtypes = [vp, i32, i64, vp, i32, i64, i32, f32, vp, i32, vp, vp, vp, vp, i64]
+        lib.tgnn_destination_loss_kept.argtypes = [i64, i32]
+        lib.tgnn_destination_loss_scratch.argtypes = [i64, i64, i32, i32]
+        loss = [vp, vp, i32, i64, i64, i32, vp, i32, vp, f32]
+        lib.tgnn_destination_loss.argtypes = loss + [vp] * 6 + [i64]
+        lib.tgnn_destination_loss_backward.argtypes = loss + [vp] * 9 + [i64]
         lib.tgnn_adamw_blocks.argtypes = [i64]
-        for fn in (lib.tgnn_lookup_scratch, lib.tgnn_adamw_blocks):
+        for fn in (lib.tgnn_lookup_scratch, lib.tgnn_destination_loss_kept, lib.tgnn_destination_loss_scratch, lib.tgnn_adamw_blocks):
             fn.restype = i64
         ap = C.POINTER(TgnnAdamwTensor)
         lib.tgnn_adamw_step.argtypes = [ap, i32, i32, vp, f64, f64, f64, f64, f64, u64, vp, vp, i64]
@@ -324,7 +330,8 @@ def _load_marshal():
                                                        lib.tgnn_slot_attend, lib.tgnn_slot_attend_scratch, lib.tgnn_slot_attend_backward)))
     m.init_table((torch.uint8, torch.int8),
                  tuple(C.cast(f, C.c_void_p).value for f in (lib.tgnn_lookup, lib.tgnn_lookup_scratch, lib.tgnn_lookup_backward,
-                                                             lib.tgnn_adamw_step, lib.tgnn_adamw_moments)))
+                                                             lib.tgnn_destination_loss_kept, lib.tgnn_destination_loss_scratch, lib.tgnn_destination_loss,
+                                                             lib.tgnn_destination_loss_backward, lib.tgnn_adamw_step, lib.tgnn_adamw_moments)))
     _marshal = m
 
 
@@ -433,7 +440,7 @@ def slot_attend_backward(q, k, v, cnt, dout, dq, dk, dv, bias=None, bounds=None,
     return _call("slot_attend_backward", q, k, v, cnt, scale, bias, bounds, times, ts, dout, dq, dk, dv, dbias, scratch)
 
 
-# ---- a learned table of nodes: lookup, AdamW (tensors are checked in csrc/marshal.c too) ----
+# ---- a learned table of nodes: lookup, destination loss, AdamW (tensors are checked in csrc/marshal.c too) ----
 def lookup(table, ids, out, status, scale: float = 1.0) -> int:
     """tgnn_lookup: out[i] = scale * table[ids[i]], zeros where ids[i] < 0.  table [rows, dim], ids int32 or int64 of any shape, out one row
     per id; fp32, bf16 or fp16 rows on either side."""
@@ -454,6 +461,28 @@ def lookup_scratch(n: int, rows: int, dim: int) -> int:
 def lookup_backward(ids, dout, dtable, scratch, status, scale: float = 1.0) -> int:
     """tgnn_lookup_backward: dtable [rows, dim], all of it overwritten, from dout, one row per id."""
     return _call("lookup_backward", ids, dout, dtable, scratch, scale, status)
+
+
+def destination_loss_kept(n: int, dim: int) -> int:
+    """fp32 elements that the forward pass keeps for the backward pass."""
+    return _size(load_library().tgnn_destination_loss_kept(n, dim), "tgnn_destination_loss_kept")
+
+
+def destination_loss_scratch(n: int, rows: int, dim: int, dtype: torch.dtype) -> int:
+    """Bytes (elements of a uint8 tensor) that both passes need as scratch, for rows of the dtype."""
+    code = {torch.float32: TGNN_F32, torch.bfloat16: TGNN_BF16}.get(dtype, TGNN_F16)
+    return _size(load_library().tgnn_destination_loss_scratch(n, rows, dim, code), "tgnn_destination_loss_scratch")
+
+
+def destination_loss(q, table, target, loss, scratch, status, bias=None, kept=None, scale: Optional[float] = None) -> int:
+    """tgnn_destination_loss: loss [n] of target [n] (int32 or int64, below 0: takes no part) among all rows of table [rows, dim] for q [n, dim],
+    both fp32 or bf16; bias fp32 [rows]; kept where a backward pass follows.  scale defaults to 1 / sqrt(dim)."""
+    return _call("destination_loss", q, table, target, bias, scale, scratch, status, loss, kept)
+
+
+def destination_loss_backward(q, table, target, kept, dloss, dq, dtable, scratch, status, bias=None, dbias=None, scale: Optional[float] = None) -> int:
+    """tgnn_destination_loss_backward: gradients for dloss [n]; dq, dtable and dbias may be None."""
+    return _call("destination_loss_backward", q, table, target, bias, scale, scratch, status, kept, dloss, dq, dtable, dbias)
 
 
 def adamw_blocks(numel: int) -> int:

@@ -1,0 +1,1239 @@
+// Softmax cross entropy of a root's target among all rows of a table, and its gradients, without a row of logits in memory.
+//
+//   z[i, j] = scale q_i . t_j + b_j;   loss_i = log sum_j exp z[i, j] - z[i, y_i]
+//   dz[i, j] = g_i (p[i, j] - [j = y_i]);   dq_i = scale sum_j dz[i, j] t_j;   dt_j = scale sum_i dz[i, j] q_i;   db_j = sum_i dz[i, j]
+//
+// dq_i is g_i scale times the weighted mean of the table's rows less the target's row, whatever g_i turns out to be: an attention over the table
+// with the rows as keys and values.  So the forward pass forms it beside the sum (one product more, no second pass over the
+// logits), and the backward pass is the gradient of the table alone, an attention the other way round: rows of the table are the queries, roots are
+// keys and values, and a weight is exp(z - m_i) w_i with the roots' maxima and factors known.  8 n rows dim operations in all,
+// two exponentials per logit, no atomics.
+//
+// The target is left out of every sum and put in at the end: with r = sum of the others' weights over the target's, loss = log(1 + r),
+// 1 - p = r / (1 + r), and dq is (mean of the others - target's row) (1 - p).  What is nearly certain keeps its relative
+// accuracy (a loss of 1e-9 is one; a weight rounded to bf16 would leave 2^-8 of it where 1 - p belongs).
+//
+// One kernel does both directions.  A thread block holds 128 or 256 rows of one matrix (A) in shared memory and walks tiles of 128 (64) rows of the
+// other (T): S = A T' on the tensor cores into tensor memory, weights P from S in registers (a thread has a row), P back to
+// tensor memory, O += P T with the same tile as the second operand.  Two groups of 128 rows (or two buffers of S) keep the tensor cores busy
+// while weights are formed.  All tiles, in order of A's rows, are split evenly over the blocks: a block's first and last group of rows may be
+// shared with others and go to scratch as parts, which a last kernel joins.
+//
+// bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes: 128 * 17 000 rows of 100 take 3 us).  fp32 rows are split into
+// two fp16 numbers each, hi + lo, after a multiplication by a power of two that puts the matrix's largest magnitude below 2^14: 22 bits for what
+// is within 2^-17 of the largest, and a product takes three passes (hi hi, hi lo, lo hi).  Weights are split the same way, in units that put the
+// largest near 2^15.
+#include <cuda.h>
+
+#include "tgnn_table.cuh"
+#include "tgnn_tensor_map.cuh"
+
+using namespace tgnn_table;
+
+namespace {
+
+constexpr unsigned kSpin = 1u << 22;
+constexpr int kMaxBlocks = 160;             // thread blocks of the main kernel, one per multiprocessor
+constexpr int kSmem = 226 * 1024;           // dynamic shared memory; the static part is below 1 KB
+constexpr int kMaxParts = 592;              // partial maxima of the fp32 rows
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLowest = -3.40282347e38f;
+
+enum Mode { LOSS = 0, FORWARD = 1, BACKWARD = 2 };
+
+struct Layout {                              // of the scratch buffer, bytes
+  int64_t count, act, parts, qp, tp, cols, slots, full, bytes;
+};
+struct Shape {
+  int64_t n, rows;
+  int dim, dp, planes;                       // dp: dim in steps of 64, what a plane of a row takes
+  int od;                                    // columns of O, dim in steps of 16
+};
+__host__ __device__ inline int pitch_of(const Shape& s) { return s.od + 4; }
+
+struct Prep {
+  Shape s;
+  const void* q;
+  const void* table;
+  const void* target;
+  int index_bits, dtype, copy_table;
+  const float* bias;
+  const float* dloss;
+  const float* kept;
+  void* dq;
+  float* loss;
+  float scale;
+  int backward, tile;
+  int32_t* count;                            // [0]: roots that take part
+  int32_t* act;                              // their indices
+  float* parts;                              // [q, table, dloss][kMaxParts]
+  uint16_t* qp;
+  uint16_t* tp;
+  float* cols;                               // what a tile's columns need, tile by tile
+  int32_t* status;
+};
+
+__device__ __forceinline__ int64_t target_of(const Prep& a, int64_t i) {
+  return a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : (int64_t)static_cast<const int32_t*>(a.target)[i];
+}
+__device__ __forceinline__ float value_of(const void* p, int dtype, int64_t i) {
+  return dtype == TGNN_F32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+// A bias in units of log 2; finite ones stay finite.
+__device__ __forceinline__ float bias2(float b) {
+  const float x = b * kLog2e;
+  return b > -INFINITY ? fmaxf(x, kLowest) : x;
+}
+
+// 2^e such that a magnitude up to `top` times it is at most 2^14.
+__device__ __forceinline__ float unit_of(float top) {
+  if (!(top > 0.f)) return 1.f;
+  int e;
+  frexpf(fminf(top, 3e38f), &e);
+  return ldexpf(1.f, max(-110, min(110, 14 - e)));
+}
+__device__ __forceinline__ float largest(const float* parts, float* s_red) {  // of kMaxParts values, by the whole block
+  float x = 0.f;
+  for (int i = threadIdx.x; i < kMaxParts; i += blockDim.x) x = fmaxf(x, parts[i]);
+  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = x;
+  __syncthreads();
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) x = fmaxf(x, s_red[w]);
+  return x;
+}
+
+// Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows.
+__global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
+  chain_wait();
+  chain_release();
+  __shared__ int s_sum[32];
+  __shared__ float s_red[32];
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  if (blockIdx.x > 0) {
+    const int b = blockIdx.x - 1, nb = gridDim.x - 1;
+    float top[3] = {0.f, 0.f, 0.f};
+    const int64_t values = a.s.rows * a.s.dim;
+    for (int64_t i = (int64_t)b * 1024 + t; i < values; i += (int64_t)nb * 1024)
+      top[1] = fmaxf(top[1], fabsf(static_cast<const float*>(a.table)[i]));
+    for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n; r += (int64_t)nb * 32) {
+      const int64_t y = target_of(a, r);
+      if (y < 0 || y >= a.s.rows) continue;
+      for (int c = lane; c < a.s.dim; c += 32) top[0] = fmaxf(top[0], fabsf(static_cast<const float*>(a.q)[r * a.s.dim + c]));
+      if (a.backward) top[2] = fmaxf(top[2], fabsf(a.dloss[r]));
+    }
+    for (int k = 0; k < 3; ++k) {
+      float x = top[k];
+      for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
+      __syncthreads();
+      if (lane == 0) s_red[warp] = x;
+      __syncthreads();
+      if (t == 0) {
+        for (int w = 1; w < 32; ++w) x = fmaxf(x, s_red[w]);
+        a.parts[k * kMaxParts + b] = x;
+        for (int i = b + nb; i < kMaxParts; i += nb) a.parts[k * kMaxParts + i] = 0.f;
+      }
+    }
+    return;
+  }
+  int done = 0;
+  constexpr int K = 4;
+  for (int64_t base = 0; base < a.s.n; base += 1024 * K) {
+    bool in[K];
+    int mine = 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int64_t i = base + (int64_t)t * K + k;
+      in[k] = false;
+      if (i < a.s.n) {
+        const int64_t y = target_of(a, i);
+        in[k] = y >= 0 && y < a.s.rows;
+        if (y >= a.s.rows) *a.status = 4;
+        if (!in[k] && !a.backward) a.loss[i] = 0.f;
+      }
+      mine += in[k];
+    }
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(FULL, inc, o);
+      if (lane >= o) inc += x;
+    }
+    if (lane == 31) s_sum[warp] = inc;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < 32; ++w) {
+      before += w < warp ? s_sum[w] : 0;
+      all += s_sum[w];
+    }
+    int at = done + before + inc - mine;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (in[k]) a.act[at++] = (int)(base + (int64_t)t * K + k);
+    done += all;
+    __syncthreads();
+  }
+  if (t == 0) a.count[0] = done;
+}
+
+// Operands and columns: rows of q that take part (and zeros up to a multiple of 128), the table where it is copied, and what the columns of a tile
+// need; backward also dq.
+__global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
+  chain_wait();
+  chain_release();
+  __shared__ float s_red[8];
+  const int t = threadIdx.x, lane = t & 31;
+  const int64_t worker = (int64_t)blockIdx.x * 8 + (t >> 5), workers = (int64_t)gridDim.x * 8;
+  const int64_t live = a.count[0], padded = up(live, 128);
+  const bool split = a.s.planes == 2;
+  float uq = 1.f, ut = 1.f, ug = 1.f;
+  if (split) {
+    uq = unit_of(largest(a.parts, s_red));
+    ut = unit_of(largest(a.parts + kMaxParts, s_red));
+    if (a.backward) ug = 2.f * unit_of(largest(a.parts + 2 * kMaxParts, s_red));   // |g| up to 2^15
+  }
+  const int dp = a.s.dp, dim = a.s.dim;
+  auto operand = [&](const void* src, int64_t row, uint16_t* to, float unit) {     // a row, 2 values at a time
+    for (int c = 2 * lane; c < dp; c += 64) {
+      float x = 0.f, y = 0.f;
+      if (row >= 0) {
+        if (c < dim) x = value_of(src, a.dtype, row * dim + c);
+        if (c + 1 < dim) y = value_of(src, a.dtype, row * dim + c + 1);
+      }
+      if (split) {
+        x *= unit;
+        y *= unit;
+        const __half2 h = __floats2half2_rn(x, y);
+        const float2 f = __half22float2(h);
+        *reinterpret_cast<__half2*>(to + c) = h;
+        *reinterpret_cast<__half2*>(to + dp + c) = __floats2half2_rn(x - f.x, y - f.y);
+      } else {
+        *reinterpret_cast<__nv_bfloat162*>(to + c) = __floats2bfloat162_rn(x, y);  // exact: the values were bf16
+      }
+    }
+  };
+  const int64_t wide = (int64_t)a.s.planes * dp;
+  for (int64_t i = worker; i < padded; i += workers) operand(a.q, i < live ? a.act[i] : -1, a.qp + i * wide, uq);
+  if (a.copy_table)
+    for (int64_t i = worker; i < a.s.rows; i += workers) operand(a.table, i, a.tp + i * wide, ut);
+  const int64_t thread = (int64_t)blockIdx.x * 256 + t, threads = (int64_t)gridDim.x * 256;
+  if (!a.backward) {
+    const int64_t cols = up(a.s.rows, a.tile);
+    for (int64_t j = thread; j < cols; j += threads) a.cols[j] = j >= a.s.rows ? -INFINITY : a.bias ? bias2(a.bias[j]) : 0.f;
+    return;
+  }
+  const int64_t cols = up(live, a.tile);
+  for (int64_t j = thread; j < cols; j += threads) {
+    float* p = a.cols + (j / a.tile) * 4 * a.tile + j % a.tile;
+    const int64_t i = j < live ? a.act[j] : -1;
+    const float g = i >= 0 ? a.dloss[i] * ug : 0.f;
+    p[0] = i >= 0 ? a.kept[i] : INFINITY;
+    p[a.tile] = i >= 0 ? g * a.kept[a.s.n + i] : 0.f;
+    p[2 * a.tile] = i >= 0 ? -g * a.kept[2 * a.s.n + i] : 0.f;
+    reinterpret_cast<int32_t*>(p)[3 * a.tile] = i >= 0 ? (int32_t)target_of(a, i) : -1;
+  }
+}
+
+// dq_i = g_i scale (what the forward pass kept).
+__global__ void __launch_bounds__(256) dq_kernel(const Prep a) {
+  chain_wait();
+  chain_release();
+  const int64_t values = a.s.n * a.s.dim;
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < values; x += (int64_t)gridDim.x * 256) {
+    const int64_t i = x / a.s.dim, y = target_of(a, i);
+    const float v = y >= 0 && y < a.s.rows ? a.dloss[i] * a.scale * a.kept[3 * a.s.n + x] : 0.f;
+    if (a.dtype == TGNN_F32) static_cast<float*>(a.dq)[x] = v;
+    else static_cast<__nv_bfloat16*>(a.dq)[x] = __float2bfloat16_rn(v);
+  }
+}
+
+// -------------------------------------------------------------------------------------------------- the main kernel --
+struct Main {
+  CUtensorMap a_map, t_map;
+  Shape s;
+  const int32_t* count;
+  const int32_t* act;
+  const float* parts;
+  const float* cols;
+  const void* target;
+  int index_bits;
+  const float* bias;
+  float* slots;              // parts: two per block, [rows of a group][pitch]
+  float* full;               // forward, groups of rows that one block has to itself: {m, l, target's z} of every live root
+  float* kept;
+  void* dtable;
+  float* dbias;
+  int dtype;
+  float scale;
+  int chunks, ksteps, stages, ahead;   // chunks of 64 columns in shared memory, steps of 16 of a product over dim
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Bounded wait on a phase; gives up early when another role has.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  for (unsigned it = 0; it < kSpin; ++it) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (done) return true;
+    if ((it & 63) == 63 && *abort_flag) return false;
+  }
+  return false;
+}
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46 |
+         (uint64_t)2 << 61;                  // the architecture's version, 128-byte swizzle
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {  // A in tensor memory
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+#define REGS32(M, r, o)                                                                                                                  \
+  M(r[o + 0]), M(r[o + 1]), M(r[o + 2]), M(r[o + 3]), M(r[o + 4]), M(r[o + 5]), M(r[o + 6]), M(r[o + 7]), M(r[o + 8]), M(r[o + 9]),       \
+      M(r[o + 10]), M(r[o + 11]), M(r[o + 12]), M(r[o + 13]), M(r[o + 14]), M(r[o + 15]), M(r[o + 16]), M(r[o + 17]), M(r[o + 18]),       \
+      M(r[o + 19]), M(r[o + 20]), M(r[o + 21]), M(r[o + 22]), M(r[o + 23]), M(r[o + 24]), M(r[o + 25]), M(r[o + 26]), M(r[o + 27]),       \
+      M(r[o + 28]), M(r[o + 29]), M(r[o + 30]), M(r[o + 31])
+#define AS_OUT(x) "=f"(x)
+#define AS_IN(x) "r"(x)
+#define AS_INF(x) "f"(x)
+#define LIST32                                                                                                                           \
+  "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}"
+#define LIST32_1                                                                                                                         \
+  "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32}"
+#define TMEM_LD32(r, o, addr) asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " LIST32 ", [%32];" : REGS32(AS_OUT, r, o) : "r"(addr))
+#define TMEM_ST32(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_IN, r, o) : "memory")
+#define TMEM_ST32F(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_INF, r, o) : "memory")
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// The blocks' shares of the tiles: block c has tiles [begin(c), begin(c + 1)), and tile x belongs to block owner(x).
+struct Share {
+  int64_t total;
+  int blocks;                                // with a tile at least
+  __device__ __forceinline__ Share(int64_t t, int launched) : total(t), blocks((int)min(t, (int64_t)launched)) {}
+  __device__ __forceinline__ int64_t begin(int c) const { return total * c / blocks; }
+  __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * blocks - 1) / total); }
+};
+// Where block c puts its part of row group r: its first group's place or its last one's.
+__device__ __forceinline__ int slot_of(const Share& sh, int64_t col_tiles, int c, int64_t r) { return sh.begin(c) / col_tiles == r ? 2 * c : 2 * c + 1; }
+
+template <int PL>
+__device__ __forceinline__ uint32_t pack_hi(float x, float y) {
+  if (PL == 2) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_lo(float x, float y, uint32_t hi) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  const __half2 l = __floats2half2_rn(x - f.x, y - f.y);
+  return *reinterpret_cast<const uint32_t*>(&l);
+}
+
+// MODE; PL planes per operand (2: fp32 rows); NH groups of 128 rows of A; NT rows of T per tile.
+template <int MODE, int PL, int NH, int NT>
+__global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[2], s_pfull[2], s_pv[2];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort;
+  constexpr int R = 128 * NH;
+  constexpr int COL_BYTES = (MODE == BACKWARD ? 16 : 4) * NT;
+  constexpr float SHIFT = PL == 2 ? 7.f : 0.f;         // weights up to 2^(8 + 7): what fp16 holds, with 2^-32 of the largest above its smallest
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  const uint32_t a_chunk = R * 128, t_chunk = NT * 128;
+  const uint32_t a_bytes = PL * g.chunks * a_chunk, t_bytes = PL * g.chunks * t_chunk;
+  const uint32_t a_base = smem_u32(smem), t_base = a_base + a_bytes;
+  unsigned char* col_base = smem + a_bytes + g.stages * t_bytes;
+
+  if (tid == 0) {
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(smem_u32(&s_full[i]), 1);
+      mbar_init(smem_u32(&s_empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&s_sfull[i]), 1);
+      mbar_init(smem_u32(&s_pfull[i]), 4);
+      mbar_init(smem_u32(&s_pv[i]), 1);
+    }
+    mbar_init(smem_u32(&s_afull), 1);
+    mbar_init(smem_u32(&s_aempty), 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  volatile int* abort_flag = &s_abort;
+  chain_wait();
+  chain_release();
+
+  const int64_t live = g.count[0];
+  const int64_t a_rows = MODE == BACKWARD ? g.s.rows : live, t_rows = MODE == BACKWARD ? live : g.s.rows;
+  const int64_t col_tiles = (t_rows + NT - 1) / NT;
+  const Share sh((a_rows + R - 1) / R * col_tiles, gridDim.x);
+  const bool idle = (int)blockIdx.x >= sh.blocks;
+  const int64_t x0 = idle ? 0 : sh.begin(blockIdx.x), x1 = idle ? 0 : sh.begin(blockIdx.x + 1);
+  const uint32_t o_base = tmem + 2 * NT;
+
+  if (idle) {
+    // fewer tiles than blocks
+  } else if (warp == 0) {
+    // ---------------------------------------------------------------- copies
+    if (lane == 0) {
+      bool ok = true;
+      uint32_t tile = 0, seg = 0;
+      for (int64_t x = x0; x < x1 && ok; ++x, ++tile) {
+        const int64_t r = x / col_tiles, j = x - r * col_tiles;
+        if (x == x0 || j == 0) {
+          ok = mbar_wait(smem_u32(&s_aempty), (seg & 1) ^ 1, abort_flag);
+          if (!ok) break;
+          mbar_expect(smem_u32(&s_afull), a_bytes);
+          for (int c = 0; c < PL * g.chunks; ++c)
+            tma_2d(a_base + c * a_chunk, &g.a_map, 64 * c, (int)(r * R), smem_u32(&s_afull));
+          ++seg;
+        }
+        const uint32_t st = tile % (uint32_t)g.stages;
+        ok = mbar_wait(smem_u32(&s_empty[st]), ((tile / (uint32_t)g.stages) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        const uint32_t bar = smem_u32(&s_full[st]);
+        mbar_expect(bar, t_bytes + COL_BYTES);
+        for (int c = 0; c < PL * g.chunks; ++c) tma_2d(t_base + st * t_bytes + c * t_chunk, &g.t_map, 64 * c, (int)(j * NT), bar);
+        bulk(smem_u32(col_base + st * COL_BYTES), reinterpret_cast<const char*>(g.cols) + j * COL_BYTES, COL_BYTES, bar);
+      }
+      if (!ok) {
+        s_abort = 1;
+        atomicCAS(g.status, 0, TGNN_ETIMEOUT);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- matrix instructions
+    if (lane == 0) {
+      bool ok = true;
+      const uint32_t fmt = PL == 2 ? 0u : 1u;            // fp16 or bf16, both operands
+      const uint32_t id_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(NT >> 3) << 17) | (8u << 24);
+      const uint32_t id_o = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(g.s.od >> 3) << 17) | (8u << 24);
+      const int64_t units = (x1 - x0) * NH;
+      uint32_t seg = 0;
+      const int64_t first_j = x0 % col_tiles;
+      auto product_s = [&](int64_t v) {                  // S of unit v
+        const int64_t tile = v / NH;
+        const int h = (int)(v % NH);
+        const uint32_t buf = (uint32_t)(v & 1);
+        const int64_t j = (first_j + tile) % col_tiles;
+        if (h == 0 && (tile == 0 || j == 0)) {
+          if (!mbar_wait(smem_u32(&s_afull), seg & 1, abort_flag)) return false;
+          ++seg;
+        }
+        const uint32_t st = (uint32_t)(tile % g.stages);
+        if (h == 0 && !mbar_wait(smem_u32(&s_full[st]), (uint32_t)(tile / g.stages) & 1, abort_flag)) return false;
+        if (v >= 2 && !mbar_wait(MODE == LOSS ? smem_u32(&s_pfull[buf]) : smem_u32(&s_pv[buf]), (uint32_t)((v - 2) >> 1) & 1, abort_flag)) return false;
+        fence_after();
+        const uint32_t a0 = a_base + h * 128 * 128, t0 = t_base + st * t_bytes;
+        uint32_t acc = 0;
+#pragma unroll
+        for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) { // hi hi, hi lo, lo hi
+          const uint32_t ap = a0 + (pr == 2 ? g.chunks * a_chunk : 0), tp = t0 + (pr == 1 ? g.chunks * t_chunk : 0);
+          for (int ks = 0; ks < g.ksteps; ++ks) {
+            mma(tmem + buf * NT, make_desc(ap + (ks >> 2) * a_chunk + (ks & 3) * 32, 16, 1024),
+                make_desc(tp + (ks >> 2) * t_chunk + (ks & 3) * 32, 16, 1024), id_s, acc);
+            acc = 1;
+          }
+        }
+        commit(smem_u32(&s_sfull[buf]));
+        if (h == NH - 1 && (j == col_tiles - 1 || tile == x1 - x0 - 1)) commit(smem_u32(&s_aempty));
+        return true;
+      };
+      for (int64_t v = 0; v < g.ahead && v < units && ok; ++v) ok = product_s(v);
+      for (int64_t u = 0; u < units && ok; ++u) {
+        const int64_t tile = u / NH;
+        const int h = (int)(u % NH);
+        const uint32_t buf = (uint32_t)(u & 1), st = (uint32_t)(tile % g.stages);
+        if (MODE == LOSS) {
+          if (h == NH - 1) {                             // every group has read its S of this tile, and its columns
+            ok = mbar_wait(smem_u32(&s_pfull[buf]), (uint32_t)(u >> 1) & 1, abort_flag);
+            if (ok && NH == 2) ok = mbar_wait(smem_u32(&s_pfull[buf ^ 1]), (uint32_t)(u >> 1) & 1, abort_flag);
+            if (!ok) break;
+            mbar_arrive(smem_u32(&s_empty[st]));
+          }
+        } else {
+          ok = mbar_wait(smem_u32(&s_pfull[buf]), (uint32_t)(u >> 1) & 1, abort_flag);
+          if (!ok) break;
+          fence_after();
+          const int64_t j = (first_j + tile) % col_tiles;
+          uint32_t acc = tile == 0 || j == 0 ? 0u : 1u;
+          const uint32_t o = o_base + h * 128, p0 = tmem + buf * NT, t0 = t_base + st * t_bytes;
+#pragma unroll
+          for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) {
+            const uint32_t p = p0 + (pr == 2 ? NT / 2 : 0), tp = t0 + (pr == 1 ? g.chunks * t_chunk : 0);
+#pragma unroll
+            for (int ks = 0; ks < NT / 16; ++ks) {
+              mma_ta(o, p + 8 * ks, make_desc(tp + 2048 * ks, t_chunk, 1024), id_o, acc);
+              acc = 1;
+            }
+          }
+          commit(smem_u32(&s_pv[buf]));
+          if (h == NH - 1) commit(smem_u32(&s_empty[st]));
+        }
+        if (u + g.ahead < units) ok = product_s(u + g.ahead);
+      }
+      if (!ok) {
+        s_abort = 1;
+        atomicCAS(g.status, 0, TGNN_ETIMEOUT);
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- weights: a thread has a row of A
+    const int grp = (warp - 2) >> 2, quarter = warp & 3;
+    const int row_in = 128 * grp + 32 * quarter + lane;  // within the block's group of rows
+    const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
+    const uint32_t o_addr = o_base + grp * 128 + lane_base;
+    const int pitch = pitch_of(g.s);
+    float uq = 1.f, ut = 1.f, ug = 1.f;
+    if (PL == 2) {
+      float top[3] = {0.f, 0.f, 0.f};
+      for (int k = 0; k < (MODE == BACKWARD ? 3 : 2); ++k) {
+        for (int i = lane; i < kMaxParts; i += 32) top[k] = fmaxf(top[k], g.parts[k * kMaxParts + i]);
+        for (int o = 16; o; o >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], o));
+      }
+      uq = unit_of(top[0]);
+      ut = unit_of(top[1]);
+      if (MODE == BACKWARD) ug = 2.f * unit_of(top[2]);
+    }
+    const float factor = g.scale * kLog2e / uq / ut;
+    bool ok = true;
+    float m = -INFINITY, l = 0.f, zt = -INFINITY, rb = 0.f, sum = 0.f;
+    int64_t row = 0;
+    int64_t tgt = -1;
+    bool valid = false;
+    uint32_t tile = 0;
+    for (int64_t x = x0; x < x1 && ok; ++x, ++tile) {
+      const int64_t r = x / col_tiles, j = x - r * col_tiles;
+      const bool start = x == x0 || j == 0, end = j == col_tiles - 1 || x == x1 - 1;
+      if (start) {
+        row = r * R + row_in;
+        valid = row < a_rows;
+        m = -INFINITY;
+        l = sum = 0.f;
+        zt = -INFINITY;
+        rb = 0.f;
+        tgt = -1;
+        if (MODE == BACKWARD) {
+          if (valid && g.bias) rb = bias2(g.bias[row]);
+        } else if (valid) {
+          const int i = g.act[row];
+          tgt = g.index_bits == 64 ? static_cast<const int64_t*>(g.target)[i] : static_cast<const int32_t*>(g.target)[i];
+        }
+      }
+      const uint32_t u = NH == 2 ? 2 * tile + grp : tile;
+      const uint32_t buf = u & 1, st = tile % (uint32_t)g.stages;
+      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_sfull[buf]), (u >> 1) & 1, abort_flag));
+      if (!ok) break;
+      fence_after();
+      const uint32_t s_addr = tmem + buf * NT + lane_base;
+      const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES);
+      float s[NT];
+#pragma unroll
+      for (int c = 0; c < NT; c += 32) TMEM_LD32(s, c, s_addr + c);
+      // the columns came with the tile, and S is complete only after it
+      wait_ld();
+      if (MODE != BACKWARD) {
+#pragma unroll
+        for (int k = 0; k < NT; k += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(col + k);
+          s[k] = fmaf(s[k], factor, b.x);
+          s[k + 1] = fmaf(s[k + 1], factor, b.y);
+          s[k + 2] = fmaf(s[k + 2], factor, b.z);
+          s[k + 3] = fmaf(s[k + 3], factor, b.w);
+        }
+        const int64_t ahead = tgt - j * NT;
+        const int hit = ahead >= 0 && ahead < NT ? (int)ahead : -1;
+        if (__any_sync(FULL, hit >= 0)) {    // the target is left out
+#pragma unroll
+          for (int k = 0; k < NT; ++k)
+            if (hit == k) {
+              zt = s[k];
+              s[k] = -INFINITY;
+            }
+        }
+        float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+#pragma unroll
+        for (int k = 4; k < NT; k += 4) {
+          t0 = fmaxf(t0, s[k]);
+          t1 = fmaxf(t1, s[k + 1]);
+          t2 = fmaxf(t2, s[k + 2]);
+          t3 = fmaxf(t3, s[k + 3]);
+        }
+        const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+        // The reference is moved only when a weight would pass 2^8: O has then to be multiplied, which is rare after a row's first tiles.
+        if (__any_sync(FULL, top > m + 8.f)) {
+          const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : exp2f(m - now);
+          l *= f;
+          m = now;
+          if (MODE == FORWARD && !start) {
+            if (NH == 1) {                               // O of this group is at rest once the unit before has been added
+              const uint32_t w = u - 1;
+              ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[w & 1]), (w >> 1) & 1, abort_flag));
+              if (!ok) break;
+              fence_after();
+            }
+            for (int c = 0; c < g.s.od; c += 32) {       // od in steps of 16: the last step may pass it, inside the group's columns
+              float o[32];
+              TMEM_LD32(o, 0, o_addr + c);
+              wait_ld();
+#pragma unroll
+              for (int k = 0; k < 32; ++k) o[k] *= f;
+              TMEM_ST32F(o_addr + c, o, 0);
+            }
+            wait_st();
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        // (the shift is added to the difference: beside a mask's lowest value it would be lost)
+        auto weight = [](float x) { return tgnn_history::exp2_fast(PL == 2 ? x + SHIFT : x); };
+        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+#pragma unroll
+        for (int c = 0; c < NT; c += 64) {
+          uint32_t hi[32];
+#pragma unroll
+          for (int k = 0; k < 64; k += 4) {
+            float* p = s + c + k;
+            p[0] = weight(p[0] - ref);
+            p[1] = weight(p[1] - ref);
+            p[2] = weight(p[2] - ref);
+            p[3] = weight(p[3] - ref);
+            l0 += p[0];
+            l1 += p[1];
+            l2 += p[2];
+            l3 += p[3];
+            if (MODE == FORWARD) {
+              hi[k / 2] = pack_hi<PL>(p[0], p[1]);
+              hi[k / 2 + 1] = pack_hi<PL>(p[2], p[3]);
+            }
+          }
+          if (MODE == FORWARD) {
+            TMEM_ST32(s_addr + c / 2, hi, 0);
+            if (PL == 2) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k) hi[k] = pack_lo(s[c + 2 * k], s[c + 2 * k + 1], hi[k]);
+              TMEM_ST32(s_addr + NT / 2 + c / 2, hi, 0);
+            }
+          }
+        }
+        l += (l0 + l1) + (l2 + l3);
+      } else {
+        const int32_t* ct = reinterpret_cast<const int32_t*>(col + 3 * NT);
+#pragma unroll
+        for (int k = 0; k < NT; k += 4) {
+          const float4 cm = *reinterpret_cast<const float4*>(col + k), cw = *reinterpret_cast<const float4*>(col + NT + k);
+          s[k] = tgnn_history::exp2_fast(fmaf(s[k], factor, rb) - cm.x) * cw.x;
+          s[k + 1] = tgnn_history::exp2_fast(fmaf(s[k + 1], factor, rb) - cm.y) * cw.y;
+          s[k + 2] = tgnn_history::exp2_fast(fmaf(s[k + 2], factor, rb) - cm.z) * cw.z;
+          s[k + 3] = tgnn_history::exp2_fast(fmaf(s[k + 3], factor, rb) - cm.w) * cw.w;
+        }
+        // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight
+        const int64_t row0 = r * R + 128 * grp + 32 * quarter;
+#pragma unroll
+        for (int c = 0; c < NT / 32; ++c) {
+          const int64_t v = (int64_t)ct[32 * c + lane] - row0;
+          unsigned hits = __ballot_sync(FULL, v >= 0 && v < 32);
+          while (hits) {
+            const int k = __ffs(hits) - 1;
+            hits &= hits - 1;
+            const int who = __shfl_sync(FULL, (int)v, k);
+            const float fix = col[2 * NT + 32 * c + k];
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i == k && who == lane) s[32 * c + i] = fix;
+          }
+        }
+        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+#pragma unroll
+        for (int c = 0; c < NT; c += 64) {
+          uint32_t hi[32];
+#pragma unroll
+          for (int k = 0; k < 64; k += 4) {
+            const float* p = s + c + k;
+            l0 += p[0];
+            l1 += p[1];
+            l2 += p[2];
+            l3 += p[3];
+            hi[k / 2] = pack_hi<PL>(p[0], p[1]);
+            hi[k / 2 + 1] = pack_hi<PL>(p[2], p[3]);
+          }
+          TMEM_ST32(s_addr + c / 2, hi, 0);
+          if (PL == 2) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) hi[k] = pack_lo(s[c + 2 * k], s[c + 2 * k + 1], hi[k]);
+            TMEM_ST32(s_addr + NT / 2 + c / 2, hi, 0);
+          }
+        }
+        sum += (l0 + l1) + (l2 + l3);
+      }
+      wait_st();
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_pfull[buf]));
+      if (!end) continue;
+
+      // the group's rows are done as far as this block goes
+      const bool alone = sh.begin(blockIdx.x) <= r * col_tiles && x1 >= (r + 1) * col_tiles;
+      float* part = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
+      if (MODE != BACKWARD && valid) {
+        float* to = alone ? g.full + 3 * row : part + g.s.od;
+        to[0] = m;
+        to[1] = l;
+        to[2] = zt;
+      }
+      if (MODE == LOSS) continue;
+      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[buf]), (u >> 1) & 1, abort_flag));
+      if (!ok) break;
+      fence_after();
+      if (MODE == BACKWARD && valid) {
+        if (alone) {
+          if (g.dbias) g.dbias[row] = sum / ug;
+        } else {
+          part[g.s.od] = sum;
+        }
+      }
+      const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
+      const int dim = g.s.dim;
+      float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
+      for (int c = 0; c < g.s.od; c += 32) {
+        float o[32];
+        __syncwarp();                                    // lanes without a row have gone ahead
+        TMEM_LD32(o, 0, o_addr + c);
+        wait_ld();
+        if (!valid) {
+        } else if (!alone) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4)
+            if (c + k < g.s.od) *reinterpret_cast<float4*>(part + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+        } else if (MODE == FORWARD) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (c + k < dim) home[c + k] = o[k];
+        } else if (g.dtable) {
+          if (g.dtype == TGNN_F32) {
+            float* to = static_cast<float*>(g.dtable) + row * dim + c;
+            if (dim % 4 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 4)
+                if (c + k < dim) *reinterpret_cast<float4*>(to + k) = make_float4(o[k] * out, o[k + 1] * out, o[k + 2] * out, o[k + 3] * out);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (c + k < dim) to[k] = o[k] * out;
+            }
+          } else {
+            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
+            if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 4)
+                if (c + k < dim) *reinterpret_cast<uint2*>(to + k) = make_uint2(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out));
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (c + k < dim) to[k] = __float2bfloat16_rn(o[k] * out);
+            }
+          }
+        }
+      }
+      __syncwarp();
+      fence_before();
+    }
+    if (!ok && lane == 0) {
+      s_abort = 1;
+      atomicCAS(g.status, 0, TGNN_ETIMEOUT);
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (s_abort && warp == 0)
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);       // copies asked for may still be on their way into this block's memory
+  __syncthreads();
+  if (warp == 1) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------- joins --
+struct Join {
+  Shape s;
+  const int32_t* count;
+  const int32_t* act;
+  const float* parts;
+  const float* slots;
+  const float* full;
+  const void* table;
+  const void* target;
+  int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles
+  float scale;
+  float* loss;
+  float* kept;
+  void* dtable;
+  float* dbias;
+};
+
+// A block per live root: eight warps take the parts in turn, then loss, m, 1 / l, 1 - p and the direction of dq.
+__global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
+  chain_wait();
+  chain_release();
+  __shared__ float s_m[8], s_l[8], s_o[8][256];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t live = a.count[0];
+  const int64_t col_tiles = (a.s.rows + a.tile - 1) / a.tile;
+  const Share sh((live + a.group - 1) / a.group * col_tiles, a.blocks);
+  const int pitch = pitch_of(a.s), dim = a.s.dim;
+  for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
+    const int64_t r = row / a.group, in = row - r * a.group;
+    const int i = a.act[row];
+    const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
+    const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
+    float* dir = a.kept ? a.kept + 3 * a.s.n + (int64_t)i * dim : nullptr;
+    float M, L, zt;
+    if (c0 == c1) {
+      M = a.full[3 * row];
+      L = a.full[3 * row + 1];
+      zt = a.full[3 * row + 2];
+      if (dir)
+        for (int c = threadIdx.x; c < dim; c += 256) s_o[0][c] = dir[c];
+      __syncthreads();
+    } else {
+      auto part = [&](int c) { return a.slots + ((int64_t)slot_of(sh, col_tiles, c, r) * a.group + in) * pitch; };
+      float m = -INFINITY;
+      for (int c = c0 + (int)threadIdx.x; c <= c1; c += 256) m = fmaxf(m, part(c)[a.s.od]);
+      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
+      if (lane == 0) s_m[warp] = m;
+      __syncthreads();
+      M = s_m[0];
+      for (int w = 1; w < 8; ++w) M = fmaxf(M, s_m[w]);
+      const float ref = M == -INFINITY ? 0.f : M;
+      float l = 0.f, o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = 0.f;
+      for (int c = c0 + warp; c <= c1; c += 8) {
+        const float* p = part(c);
+        const float f = exp2f(p[a.s.od] - ref);
+        l = fmaf(p[a.s.od + 1], f, l);
+        if (dir) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (lane + 32 * k < dim) o[k] = fmaf(p[lane + 32 * k], f, o[k]);
+        }
+      }
+      if (lane == 0) s_l[warp] = l;
+      if (dir)
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (lane + 32 * k < dim) s_o[warp][lane + 32 * k] = o[k];
+      __syncthreads();
+      L = s_l[0];
+      for (int w = 1; w < 8; ++w) L += s_l[w];
+      zt = part(sh.owner(r * col_tiles + y / a.tile))[a.s.od + 2];
+      if (dir)
+        for (int c = threadIdx.x; c < dim; c += 256) {
+          float x = s_o[0][c];
+          for (int w = 1; w < 8; ++w) x += s_o[w][c];
+          s_o[0][c] = x;
+        }
+      __syncthreads();
+    }
+    // L counts in units of 2^shift, O in units of 2^shift and of the table's unit
+    const float shift = a.s.planes == 2 ? 7.f : 0.f;
+    const float d = (M - zt) + (log2f(L) - shift);        // log2 of the others' weight over the target's
+    const bool none = L == 0.f, lost = zt == -INFINITY;
+    float loss, miss, mm, inv;
+    if (none) {                                           // no other node in sight
+      loss = lost ? INFINITY : zt - zt;
+      miss = 0.f;
+      mm = lost ? INFINITY : zt;                          // weights of 0 where nothing is in sight
+      inv = lost ? 0.f : 1.f;
+    } else if (lost) {
+      loss = INFINITY;
+      miss = 1.f;
+      mm = M;
+      inv = exp2f(shift) / L;
+    } else {
+      const float small = exp2f(-fabsf(d));               // the smaller side over the larger
+      loss = kLn2 * fmaxf(d, 0.f) + log1pf(small);
+      miss = (d > 0.f ? 1.f : small) / (1.f + small);
+      mm = fmaxf(M, zt);
+      inv = 1.f / (exp2f(zt - mm) + L * exp2f((M - mm) - shift));
+    }
+    if (d != d && !none && !lost) loss = miss = mm = d;   // NaN stays
+    if (threadIdx.x == 0) {
+      a.loss[i] = loss;
+      if (a.kept) {
+        a.kept[i] = mm;
+        a.kept[a.s.n + i] = inv;
+        a.kept[2 * a.s.n + i] = miss;
+      }
+    }
+    if (dir) {
+      float ut = 1.f;
+      if (a.s.planes == 2) {
+        float top = 0.f;
+        for (int k = lane; k < kMaxParts; k += 32) top = fmaxf(top, a.parts[kMaxParts + k]);
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+        ut = unit_of(top);
+      }
+      const float per = none ? 0.f : 1.f / L;
+      for (int c = threadIdx.x; c < dim; c += 256) {
+        const float ty = value_of(a.table, a.dtype, y * dim + c);
+        dir[c] = none ? 0.f : (s_o[0][c] * per / ut - ty) * miss;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Groups of table rows that several blocks share: block b takes the group that begins before the boundary between blocks b - 1 and b, if that is the
+// group's first one; grid.y parts of its rows.  Without any live root, zeros everywhere.
+__global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
+  chain_wait();
+  chain_release();
+  const int64_t live = a.count[0];
+  const int dim = a.s.dim, pitch = pitch_of(a.s);
+  auto put = [&](int64_t x, float v) {
+    if (a.dtype == TGNN_F32) static_cast<float*>(a.dtable)[x] = v;
+    else static_cast<__nv_bfloat16*>(a.dtable)[x] = __float2bfloat16_rn(v);
+  };
+  if (live == 0) {
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x, all = (int64_t)gridDim.x * gridDim.y * 256;
+    if (a.dtable)
+      for (int64_t x = t; x < a.s.rows * dim; x += all) put(x, 0.f);
+    if (a.dbias)
+      for (int64_t x = t; x < a.s.rows; x += all) a.dbias[x] = 0.f;
+    return;
+  }
+  const int64_t col_tiles = (live + a.tile - 1) / a.tile;
+  const Share sh((a.s.rows + a.group - 1) / a.group * col_tiles, a.blocks);
+  const int b = blockIdx.x + 1;
+  if (b >= sh.blocks) return;
+  const int64_t x = sh.begin(b), r = x / col_tiles;
+  if (x % col_tiles == 0) return;
+  const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
+  if (b != c0 + 1) return;
+  float uq = 1.f, ug = 1.f;
+  if (a.s.planes == 2) {
+    __shared__ float s_red[8];
+    uq = unit_of(largest(a.parts, s_red));
+    ug = 2.f * unit_of(largest(a.parts + 2 * kMaxParts, s_red));
+  }
+  const float out = a.scale / ug / uq;
+  const int rows = a.group / (int)gridDim.y;
+  const int cols = dim + (a.dbias ? 1 : 0);
+  for (int e = threadIdx.x; e < rows * cols; e += 256) {
+    const int in = blockIdx.y * rows + e / cols, c = e % cols;
+    const int64_t row = r * a.group + in;
+    if (row >= a.s.rows) break;
+    float v = 0.f;
+    for (int k = c0; k <= c1; ++k) v += a.slots[((int64_t)slot_of(sh, col_tiles, k, r) * a.group + in) * pitch + (c < dim ? c : a.s.od)];
+    if (c == dim) a.dbias[row] = v / ug;
+    else if (a.dtable) put(row * dim + c, v * out);
+  }
+}
+
+// --------------------------------------------------------------------------------------------------------- host side --
+struct Form {
+  int planes, group, tile;                    // of the main kernel
+};
+Form form_of(int dim, int dtype) {
+  if (dtype == TGNN_F32) return {2, 128, dim <= 128 ? 128 : 64};
+  return {1, dim <= 128 ? 256 : 128, 128};
+}
+Shape shape_of(int64_t n, int64_t rows, int dim, int dtype) {
+  Shape s;
+  s.n = n;
+  s.rows = rows;
+  s.dim = dim;
+  s.dp = (dim + 63) / 64 * 64;
+  s.planes = dtype == TGNN_F32 ? 2 : 1;
+  s.od = (dim + 15) / 16 * 16;
+  return s;
+}
+Layout layout(const Shape& s, int dtype) {
+  const Form f = form_of(s.dim, dtype);
+  Layout l;
+  int64_t at = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t p = at;
+    at += up(bytes, 256);
+    return p;
+  };
+  l.count = take(4);
+  l.act = take(4 * s.n);
+  l.parts = take(4ll * 3 * kMaxParts);
+  l.qp = take(2ll * up(s.n, 128) * s.planes * s.dp);
+  l.tp = take(2ll * s.rows * s.planes * s.dp);
+  const int64_t forward = 4ll * up(s.rows, f.tile), backward = 16ll * up(s.n, f.tile);
+  l.cols = take(forward > backward ? forward : backward);
+  const int64_t tiles = (up(s.n, 128) / 128 + 1) * (up(s.rows, 64) / 64 + 1);   // of either direction, at most
+  l.slots = take(4ll * 2 * (tiles < kMaxBlocks ? tiles : kMaxBlocks) * f.group * pitch_of(s));
+  l.full = take(12ll * s.n);
+  l.bytes = at;
+  return l;
+}
+
+bool encode(CUtensorMap* map, const void* base, int64_t width, int64_t rows, int64_t pitch_bytes, int box_rows) {
+  const tgnn::TensorMapEncodeFn enc = tgnn::tensor_map_encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)pitch_bytes};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, step[2] = {1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int MODE>
+void launch_main(Chain& c, const Main& m, int blocks, size_t smem) {
+  auto go = [&](auto kernel, int threads) {
+    if (c.e == cudaSuccess) c.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    c(kernel, dim3(blocks), dim3(threads), smem, m);
+  };
+  if (m.s.planes == 2) {
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128>, 192);
+    else go(destination_kernel<MODE, 2, 1, 64>, 192);
+  } else {
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128>, 320);
+    else go(destination_kernel<MODE, 1, 1, 128>, 192);
+  }
+}
+
+struct Call {
+  const char* who;
+  const void *q, *table;
+  int dtype;
+  int64_t n, rows;
+  int dim;
+  const void* target;
+  int index_bits;
+  const float* bias;
+  float scale;
+  void* scratch;
+  int32_t* status;
+  void* stream;
+  char* err;
+  int64_t err_size;
+};
+
+bool sizes_ok(int64_t n, int64_t rows, int dim) {
+  return n >= 0 && n < 0x7fff0000ll && rows >= 0 && rows <= 0x7fff0000ll && dim >= 1 && dim <= 256;
+}
+
+int check(const Call& a) {
+  if (a.dtype != TGNN_F32 && a.dtype != TGNN_BF16) return fail(a.err, a.err_size, TGNN_EINVAL, "%s: rows are fp32 or bf16", a.who);
+  if (a.index_bits != 32 && a.index_bits != 64) return fail(a.err, a.err_size, TGNN_EINVAL, "%s: index_bits is 32 or 64", a.who);
+  if (!sizes_ok(a.n, a.rows, a.dim) || a.rows < 1)
+    return fail(a.err, a.err_size, TGNN_EINVAL, "%s: size out of range (dim 1 to 256, rows from 1, n and rows to 2^31 - 2^16)", a.who);
+  if (!(a.scale - a.scale == 0)) return fail(a.err, a.err_size, TGNN_EINVAL, "%s: scale is not finite", a.who);
+  if (!a.table || !a.status || !a.scratch || (a.n > 0 && (!a.q || !a.target))) return fail(a.err, a.err_size, TGNN_EINVAL, "%s: null pointer", a.who);
+  if ((((uintptr_t)a.q | (uintptr_t)a.table) & (elem_bytes(a.dtype) - 1)) || ((uintptr_t)a.target & (a.index_bits / 8 - 1)) ||
+      (((uintptr_t)a.bias | (uintptr_t)a.status) & 3) || ((uintptr_t)a.scratch & 255))
+    return fail(a.err, a.err_size, TGNN_EINVAL, "%s: a pointer is not aligned (scratch to 256 bytes, the others to their elements)", a.who);
+  return TGNN_OK;
+}
+
+// begin, prep and main kernels of one direction
+template <int MODE>
+int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, void* dtable, float* dbias, Join* j) {
+  const Shape s = shape_of(a.n, a.rows, a.dim, a.dtype);
+  const Form f = form_of(a.dim, a.dtype);
+  const Layout l = layout(s, a.dtype);
+  char* base = static_cast<char*>(a.scratch);
+  const int sms = num_sms() < kMaxBlocks ? num_sms() : kMaxBlocks;
+  const bool direct = a.dtype == TGNN_BF16 && a.dim >= 64 && a.dim % 8 == 0 && ((uintptr_t)a.table & 15) == 0;
+  Prep p = {};
+  p.s = s;
+  p.q = a.q;
+  p.table = a.table;
+  p.target = a.target;
+  p.index_bits = a.index_bits;
+  p.dtype = a.dtype;
+  p.copy_table = !direct;
+  p.bias = a.bias;
+  p.dloss = dloss;
+  p.kept = kept;
+  p.loss = loss;
+  p.scale = a.scale;
+  p.backward = MODE == BACKWARD;
+  p.tile = f.tile;
+  p.count = reinterpret_cast<int32_t*>(base + l.count);
+  p.act = reinterpret_cast<int32_t*>(base + l.act);
+  p.parts = reinterpret_cast<float*>(base + l.parts);
+  p.qp = reinterpret_cast<uint16_t*>(base + l.qp);
+  p.tp = reinterpret_cast<uint16_t*>(base + l.tp);
+  p.cols = reinterpret_cast<float*>(base + l.cols);
+  p.status = a.status;
+  Main m = {};
+  m.s = s;
+  m.count = p.count;
+  m.act = p.act;
+  m.parts = p.parts;
+  m.cols = p.cols;
+  m.target = a.target;
+  m.index_bits = a.index_bits;
+  m.bias = a.bias;
+  m.slots = reinterpret_cast<float*>(base + l.slots);
+  m.full = reinterpret_cast<float*>(base + l.full);
+  m.kept = kept;
+  m.dtable = dtable;
+  m.dbias = dbias;
+  m.dtype = a.dtype;
+  m.scale = a.scale;
+  m.chunks = s.dp / 64;
+  m.ksteps = s.od / 16;
+  m.status = a.status;
+  const int64_t pitch = 2ll * s.planes * s.dp;
+  const void* rows = direct ? a.table : p.tp;
+  const int64_t width = direct ? a.dim : s.planes * s.dp, t_pitch = direct ? 2ll * a.dim : pitch;
+  const int q_box = MODE == BACKWARD ? f.tile : f.group, t_box = MODE == BACKWARD ? f.group : f.tile;
+  if (!encode(MODE == BACKWARD ? &m.t_map : &m.a_map, p.qp, s.planes * s.dp, up(s.n, 128), pitch, q_box) ||
+      !encode(MODE == BACKWARD ? &m.a_map : &m.t_map, rows, width, s.rows, t_pitch, t_box))
+    return fail(a.err, a.err_size, TGNN_ECUDA, "%s: a tensor map could not be made", a.who);
+  const int a_bytes = s.planes * m.chunks * f.group * 128, t_bytes = s.planes * m.chunks * f.tile * 128 + (MODE == BACKWARD ? 16 : 4) * f.tile;
+  m.stages = (kSmem - 1024 - a_bytes) / t_bytes;
+  if (m.stages > 4) m.stages = 4;
+  m.ahead = m.stages > 1 ? 2 : 1;
+  const size_t smem = 1024 + a_bytes + (size_t)m.stages * t_bytes;
+  const int blocks_of_parts = s.planes == 2 ? (int)(a.rows * a.dim >> 14 >= 4 * 148 - 1 ? 4 * 148 - 1 : (a.rows * a.dim >> 14) + 1) : 0;
+  c(begin_kernel, dim3(1 + blocks_of_parts), dim3(1024), 0, p);
+  const int64_t work = (direct ? 0 : a.rows) + a.n + (MODE == BACKWARD ? a.n : a.rows) / 32;
+  c(prep_kernel, dim3((unsigned)(work / 16 >= 8 * sms ? 8 * sms : work / 16 + 1)), dim3(256), 0, p);
+  const int64_t r_tiles = ((MODE == BACKWARD ? a.rows : a.n) + f.group - 1) / f.group, c_tiles = ((MODE == BACKWARD ? a.n : a.rows) + f.tile - 1) / f.tile;
+  const int blocks = (int)(r_tiles * c_tiles < sms ? r_tiles * c_tiles : sms);
+  launch_main<MODE>(c, m, blocks, smem);
+  *j = Join{};
+  j->s = s;
+  j->count = p.count;
+  j->act = p.act;
+  j->parts = p.parts;
+  j->slots = m.slots;
+  j->full = m.full;
+  j->table = a.table;
+  j->target = a.target;
+  j->index_bits = a.index_bits;
+  j->dtype = a.dtype;
+  j->blocks = blocks;
+  j->group = f.group;
+  j->tile = f.tile;
+  j->scale = a.scale;
+  j->loss = loss;
+  j->kept = kept;
+  j->dtable = dtable;
+  j->dbias = dbias;
+  return TGNN_OK;
+}
+
+}  // namespace
+
+extern "C" TGNN_API int64_t tgnn_destination_loss_kept(int64_t n, int dim) { return n < 0 || dim < 1 || dim > 256 ? -1 : n * (3 + dim); }
+
+extern "C" TGNN_API int64_t tgnn_destination_loss_scratch(int64_t n, int64_t rows, int dim, int dtype) {
+  if (!sizes_ok(n, rows, dim) || (dtype != TGNN_F32 && dtype != TGNN_BF16)) return -1;
+  return layout(shape_of(n, rows, dim, dtype), dtype).bytes;
+}
+
+extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, int dtype, int64_t n, int64_t rows, int dim, const void* target,
+                                              int index_bits, const float* bias, float scale, float* loss, float* kept, void* scratch,
+                                              int32_t* status, void* stream, char* err, int64_t err_size) {
+  const Call a = {"tgnn_destination_loss", q, table, dtype, n, rows, dim, target, index_bits, bias, scale, scratch, status, stream, err, err_size};
+  if (int rc = check(a)) return rc;
+  if (n == 0) return TGNN_OK;
+  if (!loss || (((uintptr_t)loss | (uintptr_t)kept) & 3)) return fail(err, err_size, TGNN_EINVAL, "%s: loss is null, or loss or kept not aligned", a.who);
+  Chain c(stream);
+  Join j;
+  const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, &j);
+  if (rc) return rc;
+  c(join_roots_kernel, dim3((unsigned)(n < 8 * num_sms() ? n : 8 * num_sms())), dim3(256), 0, j);
+  return c.end(a.who, err, err_size);
+}
+
+extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void* table, int dtype, int64_t n, int64_t rows, int dim,
+                                                       const void* target, int index_bits, const float* bias, float scale, const float* kept,
+                                                       const float* dloss, void* dq, void* dtable, float* dbias, void* scratch, int32_t* status,
+                                                       void* stream, char* err, int64_t err_size) {
+  const Call a = {"tgnn_destination_loss_backward", q, table, dtype, n, rows, dim, target, index_bits, bias, scale, scratch, status, stream, err,
+                  err_size};
+  if (int rc = check(a)) return rc;
+  if (n > 0 && (!kept || !dloss)) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", a.who);
+  if ((((uintptr_t)dq | (uintptr_t)dtable) & (elem_bytes(dtype) - 1)) || (((uintptr_t)kept | (uintptr_t)dloss | (uintptr_t)dbias) & 3))
+    return fail(err, err_size, TGNN_EINVAL, "%s: a pointer is not aligned to its element", a.who);
+  cudaStream_t s = (cudaStream_t)stream;
+  if (n == 0) {
+    cudaError_t e = dtable ? cudaMemsetAsync(dtable, 0, (size_t)(rows * dim * elem_bytes(dtype)), s) : cudaSuccess;
+    if (e == cudaSuccess && dbias) e = cudaMemsetAsync(dbias, 0, (size_t)(4 * rows), s);
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      return fail(err, err_size, TGNN_ECUDA, "%s: %s", a.who, cudaGetErrorString(e));
+    }
+    return TGNN_OK;
+  }
+  Chain c(stream);
+  if (dq) {
+    Prep p = {};
+    p.s = shape_of(n, rows, dim, dtype);
+    p.target = target;
+    p.index_bits = index_bits;
+    p.dtype = dtype;
+    p.dloss = dloss;
+    p.kept = kept;
+    p.dq = dq;
+    p.scale = scale;
+    const int64_t blocks = (n * dim + 1023) / 1024;
+    c(dq_kernel, dim3((unsigned)(blocks < 8 * num_sms() ? blocks : 8 * num_sms())), dim3(256), 0, p);
+  }
+  if (dtable || dbias) {
+    Join j;
+    if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dtable, dbias, &j)) return rc;
+    c(join_table_kernel, dim3((unsigned)j.blocks, 8), dim3(256), 0, j);
+  }
+  return c.end(a.who, err, err_size);
+}

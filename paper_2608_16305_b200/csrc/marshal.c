@@ -408,6 +408,12 @@ static struct {
   int (*lookup)(const void*, int, int64_t, int, const void*, int, int64_t, float, void*, int, int32_t*, void*, char*, int64_t);
   int64_t (*lookup_scratch)(int64_t, int64_t, int);
   int (*lookup_backward)(const void*, int, int64_t, const void*, int, int64_t, int, float, void*, int, void*, int32_t*, void*, char*, int64_t);
+  int64_t (*loss_kept)(int64_t, int);
+  int64_t (*loss_scratch)(int64_t, int64_t, int, int);
+  int (*loss)(const void*, const void*, int, int64_t, int64_t, int, const void*, int, const float*, float, float*, float*, void*, int32_t*, void*,
+              char*, int64_t);
+  int (*loss_backward)(const void*, const void*, int, int64_t, int64_t, int, const void*, int, const float*, float, const float*, const float*, void*,
+                       void*, float*, void*, int32_t*, void*, char*, int64_t);
   int (*adamw_step)(const tgnn_adamw_tensor*, int, int, int64_t*, double, double, double, double, double, uint64_t, void*, char*, int64_t);
   int (*adamw_moments)(const tgnn_adamw_tensor*, int, float* const*, float* const*, void*, char*, int64_t);
 } table_fn;
@@ -476,6 +482,66 @@ static PyObject* py_lookup_backward(PyObject* self, PyObject* const* a, Py_ssize
   STREAM(dev);
   CALL(table_fn.lookup_backward(ids, bits, n, dout, row_type(out_kind), sh[0], (int)sh[1], (float)scale, dtable, row_type(kind), scratch, status,
        stream, err, sizeof err));
+}
+
+struct loss {
+  void *q, *table, *target, *scratch;
+  float* bias;
+  int32_t* status;
+  long long dev, n, rows;
+  int kind, bits, dim;
+  float scale;
+};
+/* q, table, target, bias, scale or None, scratch, status */
+static int loss_args(PyObject* const* a, struct loss* l) {
+  long long sh[2], rw[2], n;
+  int kind;
+  l->dev = -1;
+  if (matrix(a[0], &l->dev, "q", &l->kind, sh, &l->q) || matrix(a[1], &l->dev, "table", &kind, rw, &l->table) ||
+      indices(a[2], l->dev, "target", &l->bits, &n, &l->target))
+    return -1;
+  if (kind != l->kind || rw[1] != sh[1] || n != sh[0]) {
+    PyErr_SetString(PyExc_TypeError, "expected q [n, dim], table [rows, dim] of one type and target [n]");
+    return -1;
+  }
+  l->n = n;
+  l->rows = rw[0];
+  l->dim = (int)sh[1];
+  const double scale = a[4] == Py_None ? 1.0 / __builtin_sqrt((double)(l->dim < 1 ? 1 : l->dim)) : PyFloat_AsDouble(a[4]);
+  l->scale = (float)scale;
+  return PyErr_Occurred() || vec(a[3], F32, l->dev, l->rows, 0, "bias", &l->bias) ||
+                 scratch_of(a[5], l->dev, table_fn.loss_scratch(l->n, l->rows, l->dim, row_type(l->kind)), &l->scratch) || must(a[6], "status") ||
+                 vec(a[6], I32, l->dev, 1, 0, "status", &l->status)
+             ? -1
+             : 0;
+}
+
+/* q, table, target, bias, scale or None, scratch, status, loss, kept */
+static PyObject* py_destination_loss(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(9);
+  struct loss l;
+  float *loss, *kept;
+  if (loss_args(a, &l) || must(a[7], "loss") || vec(a[7], F32, l.dev, l.n, 0, "loss", &loss) ||
+      vec(a[8], F32, l.dev, table_fn.loss_kept(l.n, l.dim), 0, "kept", &kept))
+    return NULL;
+  STREAM(l.dev);
+  CALL(table_fn.loss(l.q, l.table, row_type(l.kind), l.n, l.rows, l.dim, l.target, l.bits, l.bias, l.scale, loss, kept, l.scratch, l.status, stream,
+       err, sizeof err));
+}
+
+/* q, table, target, bias, scale or None, scratch, status, kept, dloss, dq, dtable, dbias */
+static PyObject* py_destination_loss_backward(PyObject* self, PyObject* const* a, Py_ssize_t nargs) {
+  ARGS(12);
+  struct loss l;
+  float *kept, *dloss, *dbias;
+  void *dq, *dtable;
+  if (loss_args(a, &l) || must(a[7], "kept") || vec(a[7], F32, l.dev, table_fn.loss_kept(l.n, l.dim), 0, "kept", &kept) || must(a[8], "dloss") ||
+      vec(a[8], F32, l.dev, l.n, 0, "dloss", &dloss) || vec(a[9], l.kind, l.dev, l.n * l.dim, 0, "dq", &dq) ||
+      vec(a[10], l.kind, l.dev, l.rows * l.dim, 0, "dtable", &dtable) || vec(a[11], F32, l.dev, l.rows, 0, "dbias", &dbias))
+    return NULL;
+  STREAM(l.dev);
+  CALL(table_fn.loss_backward(l.q, l.table, row_type(l.kind), l.n, l.rows, l.dim, l.target, l.bits, l.bias, l.scale, kept, dloss, dq, dtable, dbias,
+       l.scratch, l.status, stream, err, sizeof err));
 }
 
 /* descriptions' address, bits, device, steps, lr, beta1, beta2, eps, grad_scale, seed, params, grads (lists; a gradient may be None) */
@@ -558,6 +624,8 @@ static PyMethodDef methods[] = {{"init", py_init, METH_VARARGS, NULL},
                                 {"init_table", py_init_table, METH_VARARGS, NULL},
                                 {"lookup", (PyCFunction)(void (*)(void))py_lookup, METH_FASTCALL, NULL},
                                 {"lookup_backward", (PyCFunction)(void (*)(void))py_lookup_backward, METH_FASTCALL, NULL},
+                                {"destination_loss", (PyCFunction)(void (*)(void))py_destination_loss, METH_FASTCALL, NULL},
+                                {"destination_loss_backward", (PyCFunction)(void (*)(void))py_destination_loss_backward, METH_FASTCALL, NULL},
                                 {"adamw_step", (PyCFunction)(void (*)(void))py_adamw_step, METH_FASTCALL, NULL},
                                 {"adamw_moments", (PyCFunction)(void (*)(void))py_adamw_moments, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};

@@ -1,6 +1,10 @@
-"""A learned table of nodes: rows looked up, and the optimizer of the table and of what else is learned, under autograd.
+"""A learned table of nodes: rows looked up, every root's next destination scored among all nodes, and the optimizer of both.
+
+The link head scores an event against one sampled negative; here a root answers with a distribution over all nodes, whose rows are
+learned, and the same table gives the rows of neighbor slots.  All under autograd, without a row of logits in memory.
 
     lookup(table, ids)                 tgnn_lookup, its gradient by tgnn_lookup_backward
+    destination_loss(q, table, target) tgnn_destination_loss, its gradients by tgnn_destination_loss_backward
     AdamW(params, ...)                 tgnn_adamw_step: all tensors in one launch, moments in 32 or 8 bits
 
 All arithmetic happens inside the library.
@@ -42,6 +46,42 @@ def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: Op
     """scale * table[ids] as [*ids.shape, dim] of `dtype` (the table's own by default), zeros where an id is below 0; differentiable in the table.
     status: int32 [1], set to 4 where an id is beyond the table (such a row is zeros, too)."""
     return _Lookup.apply(table, ids, float(scale), table.dtype if dtype is None else dtype, status)
+
+
+class _DestinationLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, table, bias, target, scale, status):
+        q, table, target = q.contiguous(), table.contiguous(), target.contiguous()
+        bias = None if bias is None else bias.contiguous()
+        (n, dim), rows, dev = q.shape, table.shape[0], q.device
+        loss = torch.empty(n, device=dev)
+        wanted = any(ctx.needs_input_grad[:3])
+        kept = torch.empty(B.destination_loss_kept(n, dim), device=dev) if wanted else None
+        scratch = torch.empty(B.destination_loss_scratch(n, rows, dim, q.dtype), dtype=torch.uint8, device=dev)
+        status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
+        B.destination_loss(q, table, target, loss, scratch, status, bias=bias, kept=kept, scale=scale)
+        ctx.save_for_backward(q, table, bias, target, kept)
+        ctx.scale, ctx.status = scale, status
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dloss):
+        q, table, bias, target, kept = ctx.saved_tensors
+        like = lambda x, i: torch.empty_like(x) if x is not None and ctx.needs_input_grad[i] else None
+        dq, dtable, dbias = like(q, 0), like(table, 1), like(bias, 2)
+        scratch = torch.empty(B.destination_loss_scratch(q.shape[0], table.shape[0], q.shape[1], q.dtype), dtype=torch.uint8, device=q.device)
+        B.destination_loss_backward(q, table, target, kept, dloss.contiguous(), dq, dtable, scratch, ctx.status, bias=bias, dbias=dbias,
+                                    scale=ctx.scale)
+        return dq, dtable, dbias, None, None, None
+
+
+def destination_loss(q: torch.Tensor, table: torch.Tensor, target: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                     scale: Optional[float] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Cross entropy [n] (fp32) of target [n] among all rows of table [rows, dim] for q [n, dim]: logits scale * q . row + bias, scale 1 / sqrt(dim) by
+    default.  A target below 0 takes no part: loss 0, no gradient.  Differentiable in q, table and bias; fp32 or bf16 rows, bias fp32.
+    status: int32 [1], set to 4 where a target is beyond the table (which takes no part either)."""
+    return _DestinationLoss.apply(q, table, bias, target, scale, status)
 
 
 class AdamW:
