@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
     float* p = a.cols + (j / a.tile) * 4 * a.tile + j % a.tile;
     const int64_t i = j < live ? a.act[j] : -1;
     const float g = i >= 0 ? a.dloss[i] * ug : 0.f;
-    p[0] = i >= 0 ? a.kept[i] : INFINITY;
+    p[0] = i >= 0 ? -a.kept[i] : -INFINITY;
     p[a.tile] = i >= 0 ? g * a.kept[a.s.n + i] : 0.f;
     p[2 * a.tile] = i >= 0 ? -g * a.kept[2 * a.s.n + i] : 0.f;
     reinterpret_cast<int32_t*>(p)[3 * a.tile] = i >= 0 ? (int32_t)target_of(a, i) : -1;
@@ -328,6 +328,7 @@ __device__ __forceinline__ void commit(uint32_t bar) {
       M(r[o + 19]), M(r[o + 20]), M(r[o + 21]), M(r[o + 22]), M(r[o + 23]), M(r[o + 24]), M(r[o + 25]), M(r[o + 26]), M(r[o + 27]),       \
       M(r[o + 28]), M(r[o + 29]), M(r[o + 30]), M(r[o + 31])
 #define AS_OUT(x) "=f"(x)
+#define AS_BOTH(x) "+f"(x)
 #define AS_IN(x) "r"(x)
 #define AS_INF(x) "f"(x)
 #define LIST32                                                                                                                           \
@@ -337,7 +338,8 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 #define TMEM_LD32(r, o, addr) asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " LIST32 ", [%32];" : REGS32(AS_OUT, r, o) : "r"(addr))
 #define TMEM_ST32(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_IN, r, o) : "memory")
 #define TMEM_ST32F(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_INF, r, o) : "memory")
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// the wait, with the loaded registers as its results: nothing that reads them is moved ahead of it
+#define WAIT_LD32(r) asm volatile("tcgen05.wait::ld.sync.aligned;" : REGS32(AS_BOTH, r, 0)::"memory")
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -352,6 +354,30 @@ struct Share {
 };
 // Where block c puts its part of row group r: its first group's place or its last one's.
 __device__ __forceinline__ int slot_of(const Share& sh, int64_t col_tiles, int c, int64_t r) { return sh.begin(c) / col_tiles == r ? 2 * c : 2 * c + 1; }
+
+// Two fp32 values in one register pair: added and multiplied in one instruction.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 template <int PL>
 __device__ __forceinline__ uint32_t pack_hi(float x, float y) {
@@ -368,19 +394,25 @@ __device__ __forceinline__ uint32_t pack_lo(float x, float y, uint32_t hi) {
   return *reinterpret_cast<const uint32_t*>(&l);
 }
 
-// MODE; PL planes per operand (2: fp32 rows); NH groups of 128 rows of A; NT rows of T per tile.
-template <int MODE, int PL, int NH, int NT>
-__global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
+// MODE; PL planes per operand (2: fp32 rows); NH groups of 128 rows of A; NT rows of T per tile in shared memory; U columns of S at a time, two
+// buffers of them per group.
+//
+// Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), four more per group form weights,
+// a row per thread, while the other buffer's products run.  P takes the place of the S that it was made of.
+// 256 x 128 logits of rows of 128 take the tensor cores 2048 cycles and the exponentials 2048 (16 a cycle).
+template <int MODE, int PL, int NH, int NT, int U>
+__global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
   extern __shared__ unsigned char smem_raw[];
-  __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[2], s_pfull[2], s_pv[2];
+  __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[NH][2], s_pfull[NH][2], s_pv[NH][2];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
-  constexpr int R = 128 * NH;
+  constexpr int R = 128 * NH, PER = NT / U;            // units per tile
   constexpr int COL_BYTES = (MODE == BACKWARD ? 16 : 4) * NT;
-  constexpr float SHIFT = PL == 2 ? 7.f : 0.f;         // weights up to 2^(8 + 7): what fp16 holds, with 2^-32 of the largest above its smallest
+  constexpr float SHIFT = PL == 2 ? 7.f : 0.f;         // fp16: weights about 2^7, with 2^-32 of that above its smallest numbers
+  constexpr float MOST = PL == 2 ? 32768.f : 1.1529215e18f;      // a unit's sum that no weight's type minds (bf16: 2^60)
+  constexpr uint32_t a_chunk = R * 128, t_chunk = NT * 128;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-  const uint32_t a_chunk = R * 128, t_chunk = NT * 128;
   const uint32_t a_bytes = PL * g.chunks * a_chunk, t_bytes = PL * g.chunks * t_chunk;
   const uint32_t a_base = smem_u32(smem), t_base = a_base + a_bytes;
   unsigned char* col_base = smem + a_bytes + g.stages * t_bytes;
@@ -388,15 +420,16 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&s_full[i]), 1);
-      mbar_init(smem_u32(&s_empty[i]), 1);
+      mbar_init(smem_u32(&s_empty[i]), MODE == LOSS ? 4 * NH : NH);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&s_sfull[i]), 1);
-      mbar_init(smem_u32(&s_pfull[i]), 4);
-      mbar_init(smem_u32(&s_pv[i]), 1);
-    }
+    for (int h = 0; h < NH; ++h)
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&s_sfull[h][i]), 1);
+        mbar_init(smem_u32(&s_pfull[h][i]), 4);
+        mbar_init(smem_u32(&s_pv[h][i]), 1);
+      }
     mbar_init(smem_u32(&s_afull), 1);
-    mbar_init(smem_u32(&s_aempty), 1);
+    mbar_init(smem_u32(&s_aempty), NH);
     s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -418,7 +451,9 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
   const Share sh((a_rows + R - 1) / R * col_tiles, gridDim.x);
   const bool idle = (int)blockIdx.x >= sh.blocks;
   const int64_t x0 = idle ? 0 : sh.begin(blockIdx.x), x1 = idle ? 0 : sh.begin(blockIdx.x + 1);
-  const uint32_t o_base = tmem + 2 * NT;
+  const int64_t r0 = idle ? 0 : x0 / col_tiles, j0 = idle ? 0 : x0 - r0 * col_tiles;       // the first tile: group of rows, and tile of columns
+  const uint32_t tiles = (uint32_t)(x1 - x0);
+  const uint32_t o_base = tmem + 2 * NH * U;
 
   if (idle) {
     // fewer tiles than blocks
@@ -426,24 +461,30 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
     // ---------------------------------------------------------------- copies
     if (lane == 0) {
       bool ok = true;
-      uint32_t tile = 0, seg = 0;
-      for (int64_t x = x0; x < x1 && ok; ++x, ++tile) {
-        const int64_t r = x / col_tiles, j = x - r * col_tiles;
-        if (x == x0 || j == 0) {
+      uint32_t seg = 0, st = 0, ph = 1;
+      int64_t r = r0, j = j0;
+      for (uint32_t tile = 0; tile < tiles && ok; ++tile) {
+        if (tile == 0 || j == 0) {
           ok = mbar_wait(smem_u32(&s_aempty), (seg & 1) ^ 1, abort_flag);
           if (!ok) break;
           mbar_expect(smem_u32(&s_afull), a_bytes);
-          for (int c = 0; c < PL * g.chunks; ++c)
-            tma_2d(a_base + c * a_chunk, &g.a_map, 64 * c, (int)(r * R), smem_u32(&s_afull));
+          for (int c = 0; c < PL * g.chunks; ++c) tma_2d(a_base + c * a_chunk, &g.a_map, 64 * c, (int)(r * R), smem_u32(&s_afull));
           ++seg;
         }
-        const uint32_t st = tile % (uint32_t)g.stages;
-        ok = mbar_wait(smem_u32(&s_empty[st]), ((tile / (uint32_t)g.stages) & 1) ^ 1, abort_flag);
+        ok = mbar_wait(smem_u32(&s_empty[st]), ph, abort_flag);
         if (!ok) break;
         const uint32_t bar = smem_u32(&s_full[st]);
         mbar_expect(bar, t_bytes + COL_BYTES);
         for (int c = 0; c < PL * g.chunks; ++c) tma_2d(t_base + st * t_bytes + c * t_chunk, &g.t_map, 64 * c, (int)(j * NT), bar);
         bulk(smem_u32(col_base + st * COL_BYTES), reinterpret_cast<const char*>(g.cols) + j * COL_BYTES, COL_BYTES, bar);
+        if (++st == (uint32_t)g.stages) {
+          st = 0;
+          ph ^= 1;
+        }
+        if (++j == col_tiles) {
+          j = 0;
+          ++r;
+        }
       }
       if (!ok) {
         s_abort = 1;
@@ -451,76 +492,82 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
       }
     }
     __syncwarp();
-  } else if (warp == 1) {
-    // ---------------------------------------------------------------- matrix instructions
+  } else if (warp <= NH) {
+    // ---------------------------------------------------------------- matrix instructions of group h
     if (lane == 0) {
       bool ok = true;
+      const int h = warp - 1;
       const uint32_t fmt = PL == 2 ? 0u : 1u;            // fp16 or bf16, both operands
-      const uint32_t id_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(NT >> 3) << 17) | (8u << 24);
+      const uint32_t id_s = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(U >> 3) << 17) | (8u << 24);
       const uint32_t id_o = (1u << 4) | (fmt << 7) | (fmt << 10) | (1u << 16) | ((uint32_t)(g.s.od >> 3) << 17) | (8u << 24);
-      const int64_t units = (x1 - x0) * NH;
-      uint32_t seg = 0;
-      const int64_t first_j = x0 % col_tiles;
-      auto product_s = [&](int64_t v) {                  // S of unit v
-        const int64_t tile = v / NH;
-        const int h = (int)(v % NH);
-        const uint32_t buf = (uint32_t)(v & 1);
-        const int64_t j = (first_j + tile) % col_tiles;
-        if (h == 0 && (tile == 0 || j == 0)) {
-          if (!mbar_wait(smem_u32(&s_afull), seg & 1, abort_flag)) return false;
-          ++seg;
+      // Descriptors of the operands' first bytes; all others lie a constant further, in units of 16 bytes.
+      const uint64_t da = make_desc(a_base + h * 128 * 128, 16, 1024);             // A and, as S's second operand, T: dim side by side
+      const uint64_t dt = make_desc(t_base, 16, 1024), dv = make_desc(t_base, t_chunk, 1024);   // T as O's second operand: rows are its sum
+      const uint64_t a_plane = g.chunks * (a_chunk >> 4), t_plane = g.chunks * (t_chunk >> 4), t_stage = t_bytes >> 4;
+      const uint32_t s_cols = tmem + 2 * h * U, o = o_base + h * 128;
+      const uint32_t units = tiles * PER;
+      uint32_t s_unit = 0, s_seg = 0, s_st = 0, s_ph = 0, p_st = 0;
+      int64_t s_j = j0, p_j = j0;
+      auto product_s = [&]() {                           // S of the next unit
+        const uint32_t buf = s_unit & 1, use = s_unit >> 1, sub = s_unit % PER;
+        if (sub == 0) {
+          if (s_unit == 0 || s_j == 0) {
+            if (!mbar_wait(smem_u32(&s_afull), s_seg & 1, abort_flag)) return false;
+            ++s_seg;
+          }
+          if (!mbar_wait(smem_u32(&s_full[s_st]), s_ph, abort_flag)) return false;
         }
-        const uint32_t st = (uint32_t)(tile % g.stages);
-        if (h == 0 && !mbar_wait(smem_u32(&s_full[st]), (uint32_t)(tile / g.stages) & 1, abort_flag)) return false;
-        if (v >= 2 && !mbar_wait(MODE == LOSS ? smem_u32(&s_pfull[buf]) : smem_u32(&s_pv[buf]), (uint32_t)((v - 2) >> 1) & 1, abort_flag)) return false;
+        // the weights that lie in these columns have been used (without a backward pass: S has been read)
+        if (use > 0 && !mbar_wait(MODE == LOSS ? smem_u32(&s_pfull[h][buf]) : smem_u32(&s_pv[h][buf]), (use - 1) & 1, abort_flag)) return false;
         fence_after();
-        const uint32_t a0 = a_base + h * 128 * 128, t0 = t_base + st * t_bytes;
-        uint32_t acc = 0;
+        const uint32_t d = s_cols + buf * U;
+        const uint64_t t0 = dt + s_st * t_stage + sub * (U * 128 >> 4);
 #pragma unroll
         for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) { // hi hi, hi lo, lo hi
-          const uint32_t ap = a0 + (pr == 2 ? g.chunks * a_chunk : 0), tp = t0 + (pr == 1 ? g.chunks * t_chunk : 0);
-          for (int ks = 0; ks < g.ksteps; ++ks) {
-            mma(tmem + buf * NT, make_desc(ap + (ks >> 2) * a_chunk + (ks & 3) * 32, 16, 1024),
-                make_desc(tp + (ks >> 2) * t_chunk + (ks & 3) * 32, 16, 1024), id_s, acc);
-            acc = 1;
+          const uint64_t ap = da + (pr == 2 ? a_plane : 0), tp = t0 + (pr == 1 ? t_plane : 0);
+#pragma unroll
+          for (int ks = 0; ks < 16; ++ks) {
+            if (ks >= g.ksteps) break;
+            mma(d, ap + (ks >> 2) * (a_chunk >> 4) + (ks & 3) * 2, tp + (ks >> 2) * (t_chunk >> 4) + (ks & 3) * 2, id_s, pr > 0 || ks > 0);
           }
         }
-        commit(smem_u32(&s_sfull[buf]));
-        if (h == NH - 1 && (j == col_tiles - 1 || tile == x1 - x0 - 1)) commit(smem_u32(&s_aempty));
+        commit(smem_u32(&s_sfull[h][buf]));
+        ++s_unit;
+        if (sub == PER - 1) {
+          if (++s_st == (uint32_t)g.stages) {
+            s_st = 0;
+            s_ph ^= 1;
+          }
+          if (++s_j == col_tiles) s_j = 0;
+          if (s_j == 0 || s_unit == units) commit(smem_u32(&s_aempty));
+        }
         return true;
       };
-      for (int64_t v = 0; v < g.ahead && v < units && ok; ++v) ok = product_s(v);
-      for (int64_t u = 0; u < units && ok; ++u) {
-        const int64_t tile = u / NH;
-        const int h = (int)(u % NH);
-        const uint32_t buf = (uint32_t)(u & 1), st = (uint32_t)(tile % g.stages);
-        if (MODE == LOSS) {
-          if (h == NH - 1) {                             // every group has read its S of this tile, and its columns
-            ok = mbar_wait(smem_u32(&s_pfull[buf]), (uint32_t)(u >> 1) & 1, abort_flag);
-            if (ok && NH == 2) ok = mbar_wait(smem_u32(&s_pfull[buf ^ 1]), (uint32_t)(u >> 1) & 1, abort_flag);
-            if (!ok) break;
-            mbar_arrive(smem_u32(&s_empty[st]));
-          }
-        } else {
-          ok = mbar_wait(smem_u32(&s_pfull[buf]), (uint32_t)(u >> 1) & 1, abort_flag);
+      const uint32_t ahead = g.ahead;
+      for (uint32_t v = 0; v < ahead && v < units && ok; ++v) ok = product_s();
+      for (uint32_t u = 0; u < units && ok; ++u) {
+        if (MODE != LOSS) {
+          const uint32_t buf = u & 1, sub = u % PER;
+          ok = mbar_wait(smem_u32(&s_pfull[h][buf]), (u >> 1) & 1, abort_flag);
           if (!ok) break;
           fence_after();
-          const int64_t j = (first_j + tile) % col_tiles;
-          uint32_t acc = tile == 0 || j == 0 ? 0u : 1u;
-          const uint32_t o = o_base + h * 128, p0 = tmem + buf * NT, t0 = t_base + st * t_bytes;
+          const bool fresh = sub == 0 && (u == 0 || p_j == 0);
+          const uint64_t t0 = dv + p_st * t_stage + sub * (U * 128 >> 4);
 #pragma unroll
           for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) {
-            const uint32_t p = p0 + (pr == 2 ? NT / 2 : 0), tp = t0 + (pr == 1 ? g.chunks * t_chunk : 0);
+            const uint32_t p0 = s_cols + buf * U + (pr == 2 ? U / 2 : 0);
+            const uint64_t tp = t0 + (pr == 1 ? t_plane : 0);
 #pragma unroll
-            for (int ks = 0; ks < NT / 16; ++ks) {
-              mma_ta(o, p + 8 * ks, make_desc(tp + 2048 * ks, t_chunk, 1024), id_o, acc);
-              acc = 1;
-            }
+            for (int ks = 0; ks < U / 16; ++ks) mma_ta(o, p0 + 8 * ks, tp + 128 * ks, id_o, pr > 0 || ks > 0 || !fresh);
           }
-          commit(smem_u32(&s_pv[buf]));
-          if (h == NH - 1) commit(smem_u32(&s_empty[st]));
+          commit(smem_u32(&s_pv[h][buf]));
+          if (sub == PER - 1) {
+            commit(smem_u32(&s_empty[p_st]));
+            if (++p_st == (uint32_t)g.stages) p_st = 0;
+            if (++p_j == col_tiles) p_j = 0;
+          }
         }
-        if (u + g.ahead < units) ok = product_s(u + g.ahead);
+        if (u + ahead < units) ok = product_s();
       }
       if (!ok) {
         s_abort = 1;
@@ -528,10 +575,10 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp >= 4) {
     // ---------------------------------------------------------------- weights: a thread has a row of A
-    const int grp = (warp - 2) >> 2, quarter = warp & 3;
-    const int row_in = 128 * grp + 32 * quarter + lane;  // within the block's group of rows
+    const int grp = (warp - 4) >> 2, quarter = warp & 3;
+    const int row_in = 128 * grp + 32 * quarter + lane;
     const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
     const uint32_t o_addr = o_base + grp * 128 + lane_base;
     const int pitch = pitch_of(g.s);
@@ -540,27 +587,28 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
       float top[3] = {0.f, 0.f, 0.f};
       for (int k = 0; k < (MODE == BACKWARD ? 3 : 2); ++k) {
         for (int i = lane; i < kMaxParts; i += 32) top[k] = fmaxf(top[k], g.parts[k * kMaxParts + i]);
-        for (int o = 16; o; o >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], o));
+        for (int x = 16; x; x >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], x));
       }
       uq = unit_of(top[0]);
       ut = unit_of(top[1]);
       if (MODE == BACKWARD) ug = 2.f * unit_of(top[2]);
     }
     const float factor = g.scale * kLog2e / uq / ut;
+    const f32x2 factor2 = pack2(factor, factor);
     bool ok = true;
-    float m = -INFINITY, l = 0.f, zt = -INFINITY, rb = 0.f, sum = 0.f;
-    int64_t row = 0;
-    int64_t tgt = -1;
+    float m = -INFINITY, l = 0.f, zt = -INFINITY, rb = 0.f;      // backward: l is the row's sum of weights
+    int64_t tgt = -1, r = r0, j = j0;
     bool valid = false;
-    uint32_t tile = 0;
-    for (int64_t x = x0; x < x1 && ok; ++x, ++tile) {
-      const int64_t r = x / col_tiles, j = x - r * col_tiles;
-      const bool start = x == x0 || j == 0, end = j == col_tiles - 1 || x == x1 - 1;
+    uint32_t st = 0;
+    const uint32_t units = tiles * PER;
+    for (uint32_t u = 0; u < units && ok; ++u) {
+      const uint32_t sub = u % PER, buf = u & 1;
+      const bool start = sub == 0 && (u == 0 || j == 0), end = sub == PER - 1 && (j == col_tiles - 1 || u == units - 1);
       if (start) {
-        row = r * R + row_in;
+        const int64_t row = r * R + row_in;
         valid = row < a_rows;
         m = -INFINITY;
-        l = sum = 0.f;
+        l = 0.f;
         zt = -INFINITY;
         rb = 0.f;
         tgt = -1;
@@ -571,222 +619,274 @@ __global__ void __launch_bounds__(64 + 128 * NH, 1) destination_kernel(const __g
           tgt = g.index_bits == 64 ? static_cast<const int64_t*>(g.target)[i] : static_cast<const int32_t*>(g.target)[i];
         }
       }
-      const uint32_t u = NH == 2 ? 2 * tile + grp : tile;
-      const uint32_t buf = u & 1, st = tile % (uint32_t)g.stages;
-      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_sfull[buf]), (u >> 1) & 1, abort_flag));
+      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_sfull[grp][buf]), (u >> 1) & 1, abort_flag));
       if (!ok) break;
       fence_after();
-      const uint32_t s_addr = tmem + buf * NT + lane_base;
-      const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES);
-      float s[NT];
-#pragma unroll
-      for (int c = 0; c < NT; c += 32) TMEM_LD32(s, c, s_addr + c);
-      // the columns came with the tile, and S is complete only after it
-      wait_ld();
+      const uint32_t s_addr = tmem + (2 * grp + buf) * U + lane_base;
+      const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES) + sub * U;   // came with the tile, which S is complete after
+      float z[2][32];
+      uint32_t hi[U / 2];
+      uint32_t lo[PL == 2 ? U / 2 : 1];
       if (MODE != BACKWARD) {
+        const int64_t first_col = j * NT + sub * U, in_unit = tgt - first_col;
+        const int hit = in_unit >= 0 && in_unit < U ? (int)in_unit : -1;
+        const bool any_hit = __any_sync(FULL, hit >= 0);
+        const bool plain = !g.bias && first_col + U <= t_rows;   // the columns' values are zeros
+        // logits of 32 columns less ref in place of S, the target left out
+        auto logits = [&](float(&v)[32], int c, float ref) {
+          const f32x2 ref2 = pack2(-ref, -ref);
+          if (plain) {
 #pragma unroll
-        for (int k = 0; k < NT; k += 4) {
-          const float4 b = *reinterpret_cast<const float4*>(col + k);
-          s[k] = fmaf(s[k], factor, b.x);
-          s[k + 1] = fmaf(s[k + 1], factor, b.y);
-          s[k + 2] = fmaf(s[k + 2], factor, b.z);
-          s[k + 3] = fmaf(s[k + 3], factor, b.w);
-        }
-        const int64_t ahead = tgt - j * NT;
-        const int hit = ahead >= 0 && ahead < NT ? (int)ahead : -1;
-        if (__any_sync(FULL, hit >= 0)) {    // the target is left out
+            for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, ref2), v[k], v[k + 1]);
+          } else {
 #pragma unroll
-          for (int k = 0; k < NT; ++k)
-            if (hit == k) {
-              zt = s[k];
-              s[k] = -INFINITY;
+            for (int k = 0; k < 32; k += 4) {
+              const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(col + c + k);
+              unpack2(add2(fma2(pack2(v[k], v[k + 1]), factor2, b.x), ref2), v[k], v[k + 1]);
+              unpack2(add2(fma2(pack2(v[k + 2], v[k + 3]), factor2, b.y), ref2), v[k + 2], v[k + 3]);
             }
-        }
-        float t0 = s[0], t1 = s[1], t2 = s[2], t3 = s[3];
+          }
+          if (any_hit) {
 #pragma unroll
-        for (int k = 4; k < NT; k += 4) {
-          t0 = fmaxf(t0, s[k]);
-          t1 = fmaxf(t1, s[k + 1]);
-          t2 = fmaxf(t2, s[k + 2]);
-          t3 = fmaxf(t3, s[k + 3]);
+            for (int k = 0; k < 32; ++k)
+              if (hit == c + k) {
+                zt = v[k] + ref;
+                v[k] = -INFINITY;
+              }
+          }
+        };
+        auto maximum = [&]() {                           // of the unit's logits
+          float top = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < U; c += 32) {
+            TMEM_LD32(z[0], 0, s_addr + c);
+            WAIT_LD32(z[0]);
+            logits(z[0], c, 0.f);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) top = fmaxf(top, z[0][k]);
+          }
+          return top;
+        };
+        // A row's reference is the maximum of the first unit in which it sees anything.
+        if (__any_sync(FULL, m == -INFINITY)) {
+          const float top = maximum();
+          if (m == -INFINITY) m = top;
         }
-        const float top = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
-        // The reference is moved only when a weight would pass 2^8: O has then to be multiplied, which is rare after a row's first tiles.
-        if (__any_sync(FULL, top > m + 8.f)) {
-          const float now = fmaxf(m, top), f = now == -INFINITY ? 1.f : exp2f(m - now);
+        float sum;
+        for (int again = 0;; ++again) {
+          const float ref = m == -INFINITY ? 0.f : m;
+          const f32x2 shift2 = pack2(SHIFT, SHIFT);
+          f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+          TMEM_LD32(z[0], 0, s_addr);
+#pragma unroll
+          for (int c = 0; c < U / 32; ++c) {
+            float(&v)[32] = z[c & 1];
+            WAIT_LD32(v);
+            if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
+            logits(v, 32 * c, ref);
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              if (PL == 2) {                             // (added to the difference: beside a mask's lowest value it would be lost)
+                unpack2(add2(pack2(v[k], v[k + 1]), shift2), v[k], v[k + 1]);
+                unpack2(add2(pack2(v[k + 2], v[k + 3]), shift2), v[k + 2], v[k + 3]);
+              }
+              const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
+              const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
+              sum2 = add2(sum2, pack2(p0, p1));
+              sum3 = add2(sum3, pack2(p2, p3));
+              if (MODE == FORWARD) {
+                const int at = 16 * c + k / 2;
+                hi[at] = pack_hi<PL>(p0, p1);
+                hi[at + 1] = pack_hi<PL>(p2, p3);
+                if (PL == 2) {
+                  lo[at] = pack_lo(p0, p1, hi[at]);
+                  lo[at + 1] = pack_lo(p2, p3, hi[at + 1]);
+                }
+              }
+            }
+          }
+          float a, b;
+          unpack2(add2(sum2, sum3), a, b);
+          sum = a + b;
+          // The reference is moved only when the unit's sum says that a weight may have passed what its type holds: O has then to be multiplied and the
+          // weights are formed again.  (Once: what is too large, or no number, then stays so.)
+          if (again || !__any_sync(FULL, !(sum <= MOST))) break;
+          const float now = fmaxf(m, maximum()), f = now == -INFINITY ? 1.f : exp2f(m - now);
           l *= f;
           m = now;
-          if (MODE == FORWARD && !start) {
-            if (NH == 1) {                               // O of this group is at rest once the unit before has been added
-              const uint32_t w = u - 1;
-              ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[w & 1]), (w >> 1) & 1, abort_flag));
-              if (!ok) break;
-              fence_after();
-            }
+          if (MODE == FORWARD && !start) {               // O is at rest once the unit before has been added
+            ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[grp][buf ^ 1]), ((u - 1) >> 1) & 1, abort_flag));
+            if (!ok) break;
+            fence_after();
             for (int c = 0; c < g.s.od; c += 32) {       // od in steps of 16: the last step may pass it, inside the group's columns
-              float o[32];
-              TMEM_LD32(o, 0, o_addr + c);
-              wait_ld();
+              TMEM_LD32(z[0], 0, o_addr + c);
+              WAIT_LD32(z[0]);
 #pragma unroll
-              for (int k = 0; k < 32; ++k) o[k] *= f;
-              TMEM_ST32F(o_addr + c, o, 0);
+              for (int k = 0; k < 32; ++k) z[0][k] *= f;
+              TMEM_ST32F(o_addr + c, z[0], 0);
             }
             wait_st();
           }
         }
-        const float ref = m == -INFINITY ? 0.f : m;
-        // (the shift is added to the difference: beside a mask's lowest value it would be lost)
-        auto weight = [](float x) { return tgnn_history::exp2_fast(PL == 2 ? x + SHIFT : x); };
-        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
-#pragma unroll
-        for (int c = 0; c < NT; c += 64) {
-          uint32_t hi[32];
-#pragma unroll
-          for (int k = 0; k < 64; k += 4) {
-            float* p = s + c + k;
-            p[0] = weight(p[0] - ref);
-            p[1] = weight(p[1] - ref);
-            p[2] = weight(p[2] - ref);
-            p[3] = weight(p[3] - ref);
-            l0 += p[0];
-            l1 += p[1];
-            l2 += p[2];
-            l3 += p[3];
-            if (MODE == FORWARD) {
-              hi[k / 2] = pack_hi<PL>(p[0], p[1]);
-              hi[k / 2 + 1] = pack_hi<PL>(p[2], p[3]);
-            }
-          }
-          if (MODE == FORWARD) {
-            TMEM_ST32(s_addr + c / 2, hi, 0);
-            if (PL == 2) {
-#pragma unroll
-              for (int k = 0; k < 32; ++k) hi[k] = pack_lo(s[c + 2 * k], s[c + 2 * k + 1], hi[k]);
-              TMEM_ST32(s_addr + NT / 2 + c / 2, hi, 0);
-            }
-          }
-        }
-        l += (l0 + l1) + (l2 + l3);
+        if (!ok) break;
+        l += sum;
       } else {
-        const int32_t* ct = reinterpret_cast<const int32_t*>(col + 3 * NT);
-#pragma unroll
-        for (int k = 0; k < NT; k += 4) {
-          const float4 cm = *reinterpret_cast<const float4*>(col + k), cw = *reinterpret_cast<const float4*>(col + NT + k);
-          s[k] = tgnn_history::exp2_fast(fmaf(s[k], factor, rb) - cm.x) * cw.x;
-          s[k + 1] = tgnn_history::exp2_fast(fmaf(s[k + 1], factor, rb) - cm.y) * cw.y;
-          s[k + 2] = tgnn_history::exp2_fast(fmaf(s[k + 2], factor, rb) - cm.z) * cw.z;
-          s[k + 3] = tgnn_history::exp2_fast(fmaf(s[k + 3], factor, rb) - cm.w) * cw.w;
-        }
         // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight
+        const int32_t* ct = reinterpret_cast<const int32_t*>(col + 3 * NT);
         const int64_t row0 = r * R + 128 * grp + 32 * quarter;
+        const f32x2 rb2 = pack2(rb, rb);
+        f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+        TMEM_LD32(z[0], 0, s_addr);
 #pragma unroll
-        for (int c = 0; c < NT / 32; ++c) {
-          const int64_t v = (int64_t)ct[32 * c + lane] - row0;
-          unsigned hits = __ballot_sync(FULL, v >= 0 && v < 32);
-          while (hits) {
-            const int k = __ffs(hits) - 1;
-            hits &= hits - 1;
-            const int who = __shfl_sync(FULL, (int)v, k);
-            const float fix = col[2 * NT + 32 * c + k];
+        for (int c = 0; c < U / 32; ++c) {
+          float(&v)[32] = z[c & 1];
+          const int64_t in_rows = (int64_t)ct[32 * c + lane] - row0;
+          const int who = (int)in_rows;
+          const unsigned hits = __ballot_sync(FULL, in_rows >= 0 && in_rows < 32);
+          WAIT_LD32(v);
+          if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
+          const float* cc = col + 32 * c;
+          if (g.bias) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i == k && who == lane) s[32 * c + i] = fix;
-          }
-        }
-        float l0 = 0.f, l1 = 0.f, l2 = 0.f, l3 = 0.f;
+            for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, rb2), v[k], v[k + 1]);
 #pragma unroll
-        for (int c = 0; c < NT; c += 64) {
-          uint32_t hi[32];
-#pragma unroll
-          for (int k = 0; k < 64; k += 4) {
-            const float* p = s + c + k;
-            l0 += p[0];
-            l1 += p[1];
-            l2 += p[2];
-            l3 += p[3];
-            hi[k / 2] = pack_hi<PL>(p[0], p[1]);
-            hi[k / 2 + 1] = pack_hi<PL>(p[2], p[3]);
-          }
-          TMEM_ST32(s_addr + c / 2, hi, 0);
-          if (PL == 2) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) hi[k] = pack_lo(s[c + 2 * k], s[c + 2 * k + 1], hi[k]);
-            TMEM_ST32(s_addr + NT / 2 + c / 2, hi, 0);
-          }
-        }
-        sum += (l0 + l1) + (l2 + l3);
-      }
-      wait_st();
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_pfull[buf]));
-      if (!end) continue;
-
-      // the group's rows are done as far as this block goes
-      const bool alone = sh.begin(blockIdx.x) <= r * col_tiles && x1 >= (r + 1) * col_tiles;
-      float* part = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
-      if (MODE != BACKWARD && valid) {
-        float* to = alone ? g.full + 3 * row : part + g.s.od;
-        to[0] = m;
-        to[1] = l;
-        to[2] = zt;
-      }
-      if (MODE == LOSS) continue;
-      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[buf]), (u >> 1) & 1, abort_flag));
-      if (!ok) break;
-      fence_after();
-      if (MODE == BACKWARD && valid) {
-        if (alone) {
-          if (g.dbias) g.dbias[row] = sum / ug;
-        } else {
-          part[g.s.od] = sum;
-        }
-      }
-      const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
-      const int dim = g.s.dim;
-      float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
-      for (int c = 0; c < g.s.od; c += 32) {
-        float o[32];
-        __syncwarp();                                    // lanes without a row have gone ahead
-        TMEM_LD32(o, 0, o_addr + c);
-        wait_ld();
-        if (!valid) {
-        } else if (!alone) {
-#pragma unroll
-          for (int k = 0; k < 32; k += 4)
-            if (c + k < g.s.od) *reinterpret_cast<float4*>(part + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-        } else if (MODE == FORWARD) {
-#pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if (c + k < dim) home[c + k] = o[k];
-        } else if (g.dtable) {
-          if (g.dtype == TGNN_F32) {
-            float* to = static_cast<float*>(g.dtable) + row * dim + c;
-            if (dim % 4 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
-#pragma unroll
-              for (int k = 0; k < 32; k += 4)
-                if (c + k < dim) *reinterpret_cast<float4*>(to + k) = make_float4(o[k] * out, o[k + 1] * out, o[k + 2] * out, o[k + 3] * out);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (c + k < dim) to[k] = o[k] * out;
+            for (int k = 0; k < 32; k += 4) {
+              const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);              // -m
+              unpack2(add2(pack2(v[k], v[k + 1]), cm.x), v[k], v[k + 1]);
+              unpack2(add2(pack2(v[k + 2], v[k + 3]), cm.y), v[k + 2], v[k + 3]);
             }
           } else {
-            __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
-            if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 4)
-                if (c + k < dim) *reinterpret_cast<uint2*>(to + k) = make_uint2(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out));
-            } else {
+            for (int k = 0; k < 32; k += 4) {
+              const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);
+              unpack2(fma2(pack2(v[k], v[k + 1]), factor2, cm.x), v[k], v[k + 1]);
+              unpack2(fma2(pack2(v[k + 2], v[k + 3]), factor2, cm.y), v[k + 2], v[k + 3]);
+            }
+          }
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (c + k < dim) to[k] = __float2bfloat16_rn(o[k] * out);
+          for (int k = 0; k < 32; k += 4) {
+            const ulonglong2 cw = *reinterpret_cast<const ulonglong2*>(cc + NT + k);
+            const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
+            const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
+            unpack2(mul2(pack2(p0, p1), cw.x), v[k], v[k + 1]);
+            unpack2(mul2(pack2(p2, p3), cw.y), v[k + 2], v[k + 3]);
+          }
+          for (unsigned left = hits; left; left &= left - 1) {
+            const int k = __ffs(left) - 1;
+            const int mine = __shfl_sync(FULL, who, k);
+            const float fix = cc[2 * NT + k];
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (i == k && mine == lane) v[i] = fix;
+          }
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const int at = 16 * c + k / 2;
+            if (g.dbias) {
+              sum2 = add2(sum2, pack2(v[k], v[k + 1]));
+              sum3 = add2(sum3, pack2(v[k + 2], v[k + 3]));
+            }
+            hi[at] = pack_hi<PL>(v[k], v[k + 1]);
+            hi[at + 1] = pack_hi<PL>(v[k + 2], v[k + 3]);
+            if (PL == 2) {
+              lo[at] = pack_lo(v[k], v[k + 1], hi[at]);
+              lo[at + 1] = pack_lo(v[k + 2], v[k + 3], hi[at + 1]);
             }
           }
         }
+        float a, b;
+        unpack2(add2(sum2, sum3), a, b);
+        l += a + b;
       }
-      __syncwarp();
+      if (MODE != LOSS) {
+#pragma unroll
+        for (int c = 0; c < U / 2; c += 32) {
+          TMEM_ST32(s_addr + c, hi, c);
+          if (PL == 2) TMEM_ST32(s_addr + U / 2 + c, lo, c);
+        }
+        wait_st();
+      }
       fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&s_pfull[grp][buf]));
+        if (MODE == LOSS && sub == PER - 1) mbar_arrive(smem_u32(&s_empty[st]));
+      }
+      if (end) {
+        // the group's rows are done as far as this block goes
+        const int64_t row = r * R + row_in;
+        const bool alone = sh.begin(blockIdx.x) <= r * col_tiles && x1 >= (r + 1) * col_tiles;
+        float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
+        if (valid) {
+          if (MODE == BACKWARD) {
+            if (!alone) slot[g.s.od] = l;
+            else if (g.dbias) g.dbias[row] = l / ug;
+          } else {
+            float* to = alone ? g.full + 3 * row : slot + g.s.od;
+            to[0] = m;
+            to[1] = l;
+            to[2] = zt;
+          }
+        }
+        if (MODE != LOSS) {
+          ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[grp][buf]), (u >> 1) & 1, abort_flag));
+          if (!ok) break;
+          fence_after();
+          const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
+          const int dim = g.s.dim;
+          float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
+          float(&o)[32] = z[0];
+          for (int c = 0; c < g.s.od; c += 32) {
+            __syncwarp();                                // lanes without a row have gone ahead
+            TMEM_LD32(o, 0, o_addr + c);
+            WAIT_LD32(o);
+            if (!valid) {
+            } else if (!alone) {
+#pragma unroll
+              for (int k = 0; k < 32; k += 4)
+                if (c + k < g.s.od) *reinterpret_cast<float4*>(slot + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            } else if (MODE == FORWARD) {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (c + k < dim) home[c + k] = o[k];
+            } else if (g.dtable) {
+              if (g.dtype == TGNN_F32) {
+                float* to = static_cast<float*>(g.dtable) + row * dim + c;
+                if (dim % 4 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
+#pragma unroll
+                  for (int k = 0; k < 32; k += 4)
+                    if (c + k < dim) *reinterpret_cast<float4*>(to + k) = make_float4(o[k] * out, o[k + 1] * out, o[k + 2] * out, o[k + 3] * out);
+                } else {
+#pragma unroll
+                  for (int k = 0; k < 32; ++k)
+                    if (c + k < dim) to[k] = o[k] * out;
+                }
+              } else {
+                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
+                if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
+#pragma unroll
+                  for (int k = 0; k < 32; k += 4)
+                    if (c + k < dim)
+                      *reinterpret_cast<uint2*>(to + k) = make_uint2(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out));
+                } else {
+#pragma unroll
+                  for (int k = 0; k < 32; ++k)
+                    if (c + k < dim) to[k] = __float2bfloat16_rn(o[k] * out);
+                }
+              }
+            }
+          }
+          __syncwarp();
+          fence_before();
+        }
+      }
+      if (sub == PER - 1) {
+        if (++st == (uint32_t)g.stages) st = 0;
+        if (++j == col_tiles) {
+          j = 0;
+          ++r;
+        }
+      }
     }
     if (!ok && lane == 0) {
       s_abort = 1;
@@ -822,70 +922,105 @@ struct Join {
   float* dbias;
 };
 
-// A block per live root: eight warps take the parts in turn, then loss, m, 1 / l, 1 - p and the direction of dq.
+// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn, four columns per lane; then loss, m, 1 / l, 1 - p and the
+// direction of dq.
+template <int W>
 __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
   chain_wait();
   chain_release();
-  __shared__ float s_m[8], s_l[8], s_o[8][256];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  __shared__ float s_m[W], s_l[W];
+  __shared__ float4 s_o[W == 1 ? 1 : W][64];
+  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t live = a.count[0];
   const int64_t col_tiles = (a.s.rows + a.tile - 1) / a.tile;
   const Share sh((live + a.group - 1) / a.group * col_tiles, a.blocks);
-  const int pitch = pitch_of(a.s), dim = a.s.dim;
-  for (int64_t row = blockIdx.x; row < live; row += gridDim.x) {
+  const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
+  const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
+  float ut = 1.f;
+  if (a.s.planes == 2 && a.kept) {
+    float top = 0.f;
+    for (int k = lane; k < kMaxParts; k += 32) top = fmaxf(top, a.parts[kMaxParts + k]);
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+    ut = unit_of(top);
+  }
+  for (int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; row < live; row += step) {
     const int64_t r = row / a.group, in = row - r * a.group;
     const int i = a.act[row];
     const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
     float* dir = a.kept ? a.kept + 3 * a.s.n + (int64_t)i * dim : nullptr;
     float M, L, zt;
+    float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
     if (c0 == c1) {
       M = a.full[3 * row];
       L = a.full[3 * row + 1];
       zt = a.full[3 * row + 2];
-      if (dir)
-        for (int c = threadIdx.x; c < dim; c += 256) s_o[0][c] = dir[c];
-      __syncthreads();
-    } else {
-      auto part = [&](int c) { return a.slots + ((int64_t)slot_of(sh, col_tiles, c, r) * a.group + in) * pitch; };
-      float m = -INFINITY;
-      for (int c = c0 + (int)threadIdx.x; c <= c1; c += 256) m = fmaxf(m, part(c)[a.s.od]);
-      for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, o));
-      if (lane == 0) s_m[warp] = m;
-      __syncthreads();
-      M = s_m[0];
-      for (int w = 1; w < 8; ++w) M = fmaxf(M, s_m[w]);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float l = 0.f, o[8];
+      if (dir && warp == 0) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = 0.f;
-      for (int c = c0 + warp; c <= c1; c += 8) {
-        const float* p = part(c);
-        const float f = exp2f(p[a.s.od] - ref);
-        l = fmaf(p[a.s.od + 1], f, l);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (128 * h + 4 * lane + k < dim) (&o[h].x)[k] = dir[128 * h + 4 * lane + k];
+      }
+    } else {
+      // parts lie two places apart, but for the first, which may be its block's last
+      const float* first = a.slots + ((int64_t)slot_of(sh, col_tiles, c0, r) * a.group + in) * pitch;
+      const float* rest = a.slots + ((int64_t)2 * c0 * a.group + in) * pitch;
+      const int64_t apart = 2ll * a.group * pitch;
+      auto part = [&](int k) { return k == 0 ? first : rest + k * apart; };
+      const int parts = c1 - c0 + 1;
+      float m = -INFINITY;
+      for (int k = W == 1 ? lane : (int)threadIdx.x; k < parts; k += 32 * W) m = fmaxf(m, part(k)[od]);
+      for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, x));
+      if (W > 1) {
+        if (lane == 0) s_m[warp] = m;
+        __syncthreads();
+        for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w]);
+      }
+      M = m;
+      const float ref = M == -INFINITY ? 0.f : M;
+      zt = part(sh.owner(r * col_tiles + y / a.tile) - c0)[od + 2];
+      float l = 0.f;
+#pragma unroll 4
+      for (int k = warp; k < parts; k += W) {
+        const float* p = part(k);
+        const float4 tail = *reinterpret_cast<const float4*>(p + od);
+        const float f = exp2f(tail.x - ref);
+        l = fmaf(tail.y, f, l);
         if (dir) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (lane + 32 * k < dim) o[k] = fmaf(p[lane + 32 * k], f, o[k]);
+          for (int h = 0; h < 2; ++h)
+            if (128 * h + 4 * lane < od) {
+              const float4 v = *reinterpret_cast<const float4*>(p + 128 * h + 4 * lane);
+              o[h].x = fmaf(v.x, f, o[h].x);
+              o[h].y = fmaf(v.y, f, o[h].y);
+              o[h].z = fmaf(v.z, f, o[h].z);
+              o[h].w = fmaf(v.w, f, o[h].w);
+            }
         }
       }
-      if (lane == 0) s_l[warp] = l;
-      if (dir)
+      L = l;
+      if (W > 1) {
+        if (lane == 0) s_l[warp] = l;
+        s_o[warp][lane] = o[0];
+        s_o[warp][32 + lane] = o[1];
+        __syncthreads();
+        L = 0.f;
+        for (int w = 0; w < W; ++w) L += s_l[w];
+        if (warp == 0)
+          for (int w = 1; w < W; ++w)
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (lane + 32 * k < dim) s_o[warp][lane + 32 * k] = o[k];
-      __syncthreads();
-      L = s_l[0];
-      for (int w = 1; w < 8; ++w) L += s_l[w];
-      zt = part(sh.owner(r * col_tiles + y / a.tile))[a.s.od + 2];
-      if (dir)
-        for (int c = threadIdx.x; c < dim; c += 256) {
-          float x = s_o[0][c];
-          for (int w = 1; w < 8; ++w) x += s_o[w][c];
-          s_o[0][c] = x;
-        }
-      __syncthreads();
+            for (int h = 0; h < 2; ++h) {
+              const float4 v = s_o[w][32 * h + lane];
+              o[h].x += v.x;
+              o[h].y += v.y;
+              o[h].z += v.z;
+              o[h].w += v.w;
+            }
+        __syncthreads();
+      }
     }
+    if (warp != 0) continue;                              // (the next row's first barrier waits for warp 0)
     // L counts in units of 2^shift, O in units of 2^shift and of the table's unit
     const float shift = a.s.planes == 2 ? 7.f : 0.f;
     const float d = (M - zt) + (log2f(L) - shift);        // log2 of the others' weight over the target's
@@ -909,7 +1044,7 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       inv = 1.f / (exp2f(zt - mm) + L * exp2f((M - mm) - shift));
     }
     if (d != d && !none && !lost) loss = miss = mm = d;   // NaN stays
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
       a.loss[i] = loss;
       if (a.kept) {
         a.kept[i] = mm;
@@ -918,20 +1053,15 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       }
     }
     if (dir) {
-      float ut = 1.f;
-      if (a.s.planes == 2) {
-        float top = 0.f;
-        for (int k = lane; k < kMaxParts; k += 32) top = fmaxf(top, a.parts[kMaxParts + k]);
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-        ut = unit_of(top);
-      }
       const float per = none ? 0.f : 1.f / L;
-      for (int c = threadIdx.x; c < dim; c += 256) {
-        const float ty = value_of(a.table, a.dtype, y * dim + c);
-        dir[c] = none ? 0.f : (s_o[0][c] * per / ut - ty) * miss;
-      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int c = 128 * h + 4 * lane + k;
+          if (c < dim) dir[c] = none ? 0.f : ((&o[h].x)[k] * per / ut - value_of(a.table, a.dtype, y * dim + c)) * miss;
+        }
     }
-    __syncthreads();
   }
 }
 
@@ -969,16 +1099,30 @@ __global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
     ug = 2.f * unit_of(largest(a.parts + 2 * kMaxParts, s_red));
   }
   const float out = a.scale / ug / uq;
-  const int rows = a.group / (int)gridDim.y;
-  const int cols = dim + (a.dbias ? 1 : 0);
-  for (int e = threadIdx.x; e < rows * cols; e += 256) {
-    const int in = blockIdx.y * rows + e / cols, c = e % cols;
+  const int rows = a.group / (int)gridDim.y, lane = threadIdx.x & 31, od = a.s.od;
+  const int first_slot = slot_of(sh, col_tiles, c0, r);   // the others are their blocks' first
+  for (int k = threadIdx.x >> 5; k < rows; k += 8) {      // a warp per row, four columns per lane
+    const int in = blockIdx.y * rows + k;
     const int64_t row = r * a.group + in;
     if (row >= a.s.rows) break;
-    float v = 0.f;
-    for (int k = c0; k <= c1; ++k) v += a.slots[((int64_t)slot_of(sh, col_tiles, k, r) * a.group + in) * pitch + (c < dim ? c : a.s.od)];
-    if (c == dim) a.dbias[row] = v / ug;
-    else if (a.dtable) put(row * dim + c, v * out);
+    for (int c = 4 * lane; c < od + 4; c += 128) {
+      float4 v = *reinterpret_cast<const float4*>(a.slots + ((int64_t)first_slot * a.group + in) * pitch + c);
+#pragma unroll 4
+      for (int b2 = c0 + 1; b2 <= c1; ++b2) {
+        const float4 w = *reinterpret_cast<const float4*>(a.slots + ((int64_t)2 * b2 * a.group + in) * pitch + c);
+        v.x += w.x;
+        v.y += w.y;
+        v.z += w.z;
+        v.w += w.w;
+      }
+      if (c == od) {
+        if (a.dbias) a.dbias[row] = v.x / ug;
+      } else if (a.dtable) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < dim) put(row * dim + c + e, (&v.x)[e] * out);
+      }
+    }
   }
 }
 
@@ -1039,11 +1183,11 @@ void launch_main(Chain& c, const Main& m, int blocks, size_t smem) {
     c(kernel, dim3(blocks), dim3(threads), smem, m);
   };
   if (m.s.planes == 2) {
-    if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128>, 192);
-    else go(destination_kernel<MODE, 2, 1, 64>, 192);
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128, 128>, 256);
+    else go(destination_kernel<MODE, 2, 1, 64, 64>, 256);
   } else {
-    if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128>, 320);
-    else go(destination_kernel<MODE, 1, 1, 128>, 192);
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128, 64>, 384);
+    else go(destination_kernel<MODE, 1, 1, 128, 128>, 256);
   }
 }
 
@@ -1192,7 +1336,10 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   Join j;
   const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, &j);
   if (rc) return rc;
-  c(join_roots_kernel, dim3((unsigned)(n < 8 * num_sms() ? n : 8 * num_sms())), dim3(256), 0, j);
+  // 16 parts of a root and more: a block each (600 roots with 50 parts: see the table of cases), else a warp
+  const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
+  if (j.blocks >= 16 * groups) c(join_roots_kernel<8>, dim3((unsigned)(n < most ? n : most)), dim3(256), 0, j);
+  else c(join_roots_kernel<1>, dim3((unsigned)((n + 7) / 8 < most ? (n + 7) / 8 : most)), dim3(256), 0, j);
   return c.end(a.who, err, err_size);
 }
 
@@ -1233,7 +1380,7 @@ extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void
   if (dtable || dbias) {
     Join j;
     if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dtable, dbias, &j)) return rc;
-    c(join_table_kernel, dim3((unsigned)j.blocks, 8), dim3(256), 0, j);
+    c(join_table_kernel, dim3((unsigned)j.blocks, j.blocks < 64 ? 16 : 8), dim3(256), 0, j);
   }
   return c.end(a.who, err, err_size);
 }

@@ -271,6 +271,22 @@ def test_many_roots_and_few_nodes():
         check(x, call(x))
 
 
+@pytest.mark.parametrize("dtype,dim", [(BF16, 100), (BF16, 172), (F32, 100), (F32, 172)])
+def test_long_walks_without_a_backward_pass(dtype, dim):
+    """Groups of rows run ahead of one another; the loss alone is the loss beside the gradients, and always the same."""
+    from paper_2608_16305_b200 import binding as B
+    x = make(3000, 40_000, dim, dtype, masked=0.0)
+    out = call(x, ())
+    assert float((out["alone"] - out["loss"]).abs().max()) <= 2.0 ** -21 * float(out["loss"].abs().max())
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(B.destination_loss_scratch(3000, 40_000, dim, dtype), dtype=torch.uint8, device="cuda")
+    again = torch.empty(3000, device="cuda")
+    for _ in range(30):
+        B.destination_loss(x["q"], x["table"], x["target"], again, scratch, status, bias=x["bias"], scale=x["scale"])
+        assert torch.equal(again, out["alone"])
+    assert int(status.item()) == 0
+
+
 def test_the_same_bits_from_a_graph_and_beside_another_call():
     from paper_2608_16305_b200 import binding as B
     x, other = make(700, 5000, 100, BF16), make(500, 3000, 64, F32)
