@@ -294,6 +294,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   }
   return false;
 }
+// Whether a phase has ended, without waiting for it.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(map),
                "r"(x), "r"(y), "r"(bar)
@@ -580,7 +590,8 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     const int grp = (warp - 4) >> 2, quarter = warp & 3;
     const int row_in = 128 * grp + 32 * quarter + lane;
     const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
-    const uint32_t o_addr = o_base + grp * 128 + lane_base;
+    const uint32_t o_addr = o_base + grp * 128 + lane_base, s_base = tmem + 2 * grp * U + lane_base;
+    const uint32_t bar_s = smem_u32(&s_sfull[grp][0]), bar_p = smem_u32(&s_pfull[grp][0]), bar_pv = smem_u32(&s_pv[grp][0]);
     const int pitch = pitch_of(g.s);
     float uq = 1.f, ut = 1.f, ug = 1.f;
     if (PL == 2) {
@@ -595,299 +606,311 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     }
     const float factor = g.scale * kLog2e / uq / ut;
     const f32x2 factor2 = pack2(factor, factor);
-    bool ok = true;
-    float m = -INFINITY, l = 0.f, zt = -INFINITY, rb = 0.f;      // backward: l is the row's sum of weights
-    int64_t tgt = -1, r = r0, j = j0;
-    bool valid = false;
-    uint32_t st = 0;
-    const uint32_t units = tiles * PER;
-    for (uint32_t u = 0; u < units && ok; ++u) {
-      const uint32_t sub = u % PER, buf = u & 1;
-      const bool start = sub == 0 && (u == 0 || j == 0), end = sub == PER - 1 && (j == col_tiles - 1 || u == units - 1);
-      if (start) {
-        const int64_t row = r * R + row_in;
-        valid = row < a_rows;
-        m = -INFINITY;
-        l = 0.f;
-        zt = -INFINITY;
-        rb = 0.f;
-        tgt = -1;
-        if (MODE == BACKWARD) {
-          if (valid && g.bias) rb = bias2(g.bias[row]);
-        } else if (valid) {
-          const int i = g.act[row];
-          tgt = g.index_bits == 64 ? static_cast<const int64_t*>(g.target)[i] : static_cast<const int32_t*>(g.target)[i];
-        }
+    const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
+    const uint32_t all_cols = (uint32_t)col_tiles, full_tiles = (uint32_t)(t_rows / NT), all_units = tiles * PER;
+    uint32_t r = (uint32_t)r0, j = (uint32_t)j0, left = tiles, st = 0, u = 0;
+    bool ok = true, have = false;                        // have: the next unit's first columns are in z[0], or on their way
+    float z[2][32];
+    while (left > 0 && ok) {
+      // ---- the tiles of one group of rows
+      const int64_t row = (int64_t)r * R + row_in;
+      const bool valid = row < a_rows;
+      const uint32_t count = min(left, all_cols - j);
+      float m = -INFINITY, l = 0.f, zt = -INFINITY, rb = 0.f;    // backward: l is the row's sum of weights
+      int32_t tgt = -1;
+      if (MODE == BACKWARD) {
+        if (valid && biased) rb = bias2(g.bias[row]);
+      } else if (valid) {
+        const int i = g.act[row];
+        tgt = g.index_bits == 64 ? (int32_t) static_cast<const int64_t*>(g.target)[i] : static_cast<const int32_t*>(g.target)[i];
       }
-      ok = __all_sync(FULL, mbar_wait(smem_u32(&s_sfull[grp][buf]), (u >> 1) & 1, abort_flag));
-      if (!ok) break;
-      fence_after();
-      const uint32_t s_addr = tmem + (2 * grp + buf) * U + lane_base;
-      const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES) + sub * U;   // came with the tile, which S is complete after
-      float z[2][32];
-      uint32_t hi[U / 2];
-      uint32_t lo[PL == 2 ? U / 2 : 1];
-      if (MODE != BACKWARD) {
-        const int64_t first_col = j * NT + sub * U, in_unit = tgt - first_col;
-        const int hit = in_unit >= 0 && in_unit < U ? (int)in_unit : -1;
-        const bool any_hit = __any_sync(FULL, hit >= 0);
-        const bool plain = !g.bias && first_col + U <= t_rows;   // the columns' values are zeros
-        // logits of 32 columns less ref in place of S, the target left out
-        auto logits = [&](float(&v)[32], int c, float ref) {
-          const f32x2 ref2 = pack2(-ref, -ref);
-          if (plain) {
+      for (uint32_t t = 0; t < count && ok; ++t, ++j) {
 #pragma unroll
-            for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, ref2), v[k], v[k + 1]);
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(col + c + k);
-              unpack2(add2(fma2(pack2(v[k], v[k + 1]), factor2, b.x), ref2), v[k], v[k + 1]);
-              unpack2(add2(fma2(pack2(v[k + 2], v[k + 3]), factor2, b.y), ref2), v[k + 2], v[k + 3]);
-            }
-          }
-          if (any_hit) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (hit == c + k) {
-                zt = v[k] + ref;
-                v[k] = -INFINITY;
-              }
-          }
-        };
-        auto maximum = [&]() {                           // of the unit's logits
-          float top = -INFINITY;
-#pragma unroll
-          for (int c = 0; c < U; c += 32) {
-            TMEM_LD32(z[0], 0, s_addr + c);
-            WAIT_LD32(z[0]);
-            logits(z[0], c, 0.f);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) top = fmaxf(top, z[0][k]);
-          }
-          return top;
-        };
-        // A row's reference is the maximum of the first unit in which it sees anything.
-        if (__any_sync(FULL, m == -INFINITY)) {
-          const float top = maximum();
-          if (m == -INFINITY) m = top;
-        }
-        float sum;
-        for (int again = 0;; ++again) {
-          const float ref = m == -INFINITY ? 0.f : m;
-          const f32x2 shift2 = pack2(SHIFT, SHIFT);
-          f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
-          TMEM_LD32(z[0], 0, s_addr);
-#pragma unroll
-          for (int c = 0; c < U / 32; ++c) {
-            float(&v)[32] = z[c & 1];
-            WAIT_LD32(v);
-            if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
-            logits(v, 32 * c, ref);
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              if (PL == 2) {                             // (added to the difference: beside a mask's lowest value it would be lost)
-                unpack2(add2(pack2(v[k], v[k + 1]), shift2), v[k], v[k + 1]);
-                unpack2(add2(pack2(v[k + 2], v[k + 3]), shift2), v[k + 2], v[k + 3]);
-              }
-              const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
-              const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
-              sum2 = add2(sum2, pack2(p0, p1));
-              sum3 = add2(sum3, pack2(p2, p3));
-              if (MODE == FORWARD) {
-                const int at = 16 * c + k / 2;
-                hi[at] = pack_hi<PL>(p0, p1);
-                hi[at + 1] = pack_hi<PL>(p2, p3);
-                if (PL == 2) {
-                  lo[at] = pack_lo(p0, p1, hi[at]);
-                  lo[at + 1] = pack_lo(p2, p3, hi[at + 1]);
-                }
-              }
-            }
-          }
-          float a, b;
-          unpack2(add2(sum2, sum3), a, b);
-          sum = a + b;
-          // The reference is moved only when the unit's sum says that a weight may have passed what its type holds: O has then to be multiplied and the
-          // weights are formed again.  (Once: what is too large, or no number, then stays so.)
-          if (again || !__any_sync(FULL, !(sum <= MOST))) break;
-          const float now = fmaxf(m, maximum()), f = now == -INFINITY ? 1.f : exp2f(m - now);
-          l *= f;
-          m = now;
-          if (MODE == FORWARD && !start) {               // O is at rest once the unit before has been added
-            ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[grp][buf ^ 1]), ((u - 1) >> 1) & 1, abort_flag));
+        for (int sub = 0; sub < PER; ++sub, ++u) {
+          const uint32_t buf = PER == 2 ? sub : u & 1, use = u >> 1;
+          const uint32_t s_addr = s_base + buf * U;
+          if (!have) {
+            ok = __all_sync(FULL, mbar_wait(bar_s + 8 * buf, use & 1, abort_flag));
             if (!ok) break;
             fence_after();
-            for (int c = 0; c < g.s.od; c += 32) {       // od in steps of 16: the last step may pass it, inside the group's columns
-              TMEM_LD32(z[0], 0, o_addr + c);
-              WAIT_LD32(z[0]);
+            TMEM_LD32(z[0], 0, s_addr);
+          }
+          have = false;
+          // the columns' values came with the tile, which S is complete after
+          const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES) + sub * U;
+          // While the last columns are worked on, the next unit's first ones are asked for, if they are there.
+          auto ask = [&]() {
+            const uint32_t next = buf ^ 1, parity = ((u + 1) >> 1) & 1;
+            have = u + 1 < all_units && __all_sync(FULL, mbar_test(bar_s + 8 * next, parity));
+            if (have) {
+              fence_after();
+              TMEM_LD32(z[0], 0, s_base + next * U);
+            }
+          };
+          uint32_t hi[U / 2];
+          uint32_t lo[PL == 2 ? U / 2 : 1];
+          if (MODE != BACKWARD) {
+            const int hit = tgt - (int32_t)(j * NT + sub * U);                     // outside [0, U): not here
+            const bool any_hit = __any_sync(FULL, (uint32_t)hit < (uint32_t)U);
+            const bool plain = !biased && j < full_tiles;   // the columns' values are zeros
+            // logits of 32 columns less ref in place of S, the target left out
+            auto logits = [&](float(&v)[32], int c, float ref) {
+              const f32x2 ref2 = pack2(-ref, -ref);
+              if (plain) {
 #pragma unroll
-              for (int k = 0; k < 32; ++k) z[0][k] *= f;
-              TMEM_ST32F(o_addr + c, z[0], 0);
+                for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, ref2), v[k], v[k + 1]);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(col + c + k);
+                  unpack2(add2(fma2(pack2(v[k], v[k + 1]), factor2, b.x), ref2), v[k], v[k + 1]);
+                  unpack2(add2(fma2(pack2(v[k + 2], v[k + 3]), factor2, b.y), ref2), v[k + 2], v[k + 3]);
+                }
+              }
+              if (__builtin_expect(any_hit, 0)) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (hit == c + k) {
+                    zt = v[k] + ref;
+                    v[k] = -INFINITY;
+                  }
+              }
+            };
+            auto maximum = [&]() {                       // of the unit's logits; what was asked for is lost
+              have = false;
+              float top = -INFINITY;
+              for (int c = 0; c < U; c += 32) {
+                TMEM_LD32(z[0], 0, s_addr + c);
+                WAIT_LD32(z[0]);
+                logits(z[0], c, 0.f);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) top = fmaxf(top, z[0][k]);
+              }
+              return top;
+            };
+            // A row's reference is the maximum of the first unit in which it sees anything.
+            if (__builtin_expect(__any_sync(FULL, m == -INFINITY), 0)) {
+              WAIT_LD32(z[0]);
+              const float top = maximum();
+              if (m == -INFINITY) m = top;
+              TMEM_LD32(z[0], 0, s_addr);
+            }
+            float sum;
+            for (int again = 0;; ++again) {
+              const float ref = m == -INFINITY ? 0.f : m;
+              const f32x2 shift2 = pack2(SHIFT, SHIFT);
+              f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+#pragma unroll
+              for (int c = 0; c < U / 32; ++c) {
+                float(&v)[32] = z[c & 1];
+                WAIT_LD32(v);
+                if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
+                else ask();
+                logits(v, 32 * c, ref);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  if (PL == 2) {                         // (added to the difference: beside a mask's lowest value it would be lost)
+                    unpack2(add2(pack2(v[k], v[k + 1]), shift2), v[k], v[k + 1]);
+                    unpack2(add2(pack2(v[k + 2], v[k + 3]), shift2), v[k + 2], v[k + 3]);
+                  }
+                  const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
+                  const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
+                  sum2 = add2(sum2, pack2(p0, p1));
+                  sum3 = add2(sum3, pack2(p2, p3));
+                  if (MODE == FORWARD) {
+                    const int at = 16 * c + k / 2;
+                    hi[at] = pack_hi<PL>(p0, p1);
+                    hi[at + 1] = pack_hi<PL>(p2, p3);
+                    if (PL == 2) {
+                      lo[at] = pack_lo(p0, p1, hi[at]);
+                      lo[at + 1] = pack_lo(p2, p3, hi[at + 1]);
+                    }
+                  }
+                }
+              }
+              float a, b;
+              unpack2(add2(sum2, sum3), a, b);
+              sum = a + b;
+              // The reference is moved only when the unit's sum says that a weight may have passed what its type holds: O has then to be multiplied and
+              // the weights are formed again.  (Once: what is too large, or no number, then stays so.)
+              if (__builtin_expect(again || !__any_sync(FULL, !(sum <= MOST)), 1)) break;
+              if (have) WAIT_LD32(z[0]);
+              const float now = fmaxf(m, maximum()), f = now == -INFINITY ? 1.f : exp2f(m - now);
+              l *= f;
+              m = now;
+              if (MODE == FORWARD && (t > 0 || sub > 0)) {  // O is at rest once the unit before has been added
+                ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * (buf ^ 1), ((u - 1) >> 1) & 1, abort_flag));
+                if (!ok) break;
+                fence_after();
+                for (int c = 0; c < g.s.od; c += 32) {   // od in steps of 16: the last step may pass it, inside the group's columns
+                  TMEM_LD32(z[0], 0, o_addr + c);
+                  WAIT_LD32(z[0]);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) z[0][k] *= f;
+                  TMEM_ST32F(o_addr + c, z[0], 0);
+                }
+                wait_st();
+              }
+              TMEM_LD32(z[0], 0, s_addr);
+            }
+            if (!ok) break;
+            l += sum;
+          } else {
+            // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight
+            const int32_t* ct = reinterpret_cast<const int32_t*>(col + 3 * NT);
+            const int32_t row0 = (int32_t)(r * R) + 128 * grp + 32 * quarter;
+            const f32x2 rb2 = pack2(rb, rb);
+            f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+#pragma unroll
+            for (int c = 0; c < U / 32; ++c) {
+              float(&v)[32] = z[c & 1];
+              const int who = ct[32 * c + lane] - row0;
+              const unsigned hits = __ballot_sync(FULL, (uint32_t)who < 32u);
+              const float* cc = col + 32 * c;
+              WAIT_LD32(v);
+              if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
+              else ask();
+              if (biased) {
+#pragma unroll
+                for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, rb2), v[k], v[k + 1]);
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);          // -m
+                  unpack2(add2(pack2(v[k], v[k + 1]), cm.x), v[k], v[k + 1]);
+                  unpack2(add2(pack2(v[k + 2], v[k + 3]), cm.y), v[k + 2], v[k + 3]);
+                }
+              } else {
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);
+                  unpack2(fma2(pack2(v[k], v[k + 1]), factor2, cm.x), v[k], v[k + 1]);
+                  unpack2(fma2(pack2(v[k + 2], v[k + 3]), factor2, cm.y), v[k + 2], v[k + 3]);
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < 32; k += 4) {
+                const ulonglong2 cw = *reinterpret_cast<const ulonglong2*>(cc + NT + k);
+                const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
+                const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
+                unpack2(mul2(pack2(p0, p1), cw.x), v[k], v[k + 1]);
+                unpack2(mul2(pack2(p2, p3), cw.y), v[k + 2], v[k + 3]);
+              }
+              if (__builtin_expect(hits != 0, 0)) {
+                for (unsigned more = hits; more; more &= more - 1) {
+                  const int k = __ffs(more) - 1;
+                  const int mine = __shfl_sync(FULL, who, k);
+                  const float fix = cc[2 * NT + k];
+#pragma unroll
+                  for (int i = 0; i < 32; ++i)
+                    if (i == k && mine == lane) v[i] = fix;
+                }
+              }
+              if (summed) {
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) {
+                  sum2 = add2(sum2, pack2(v[k], v[k + 1]));
+                  sum3 = add2(sum3, pack2(v[k + 2], v[k + 3]));
+                }
+              }
+#pragma unroll
+              for (int k = 0; k < 32; k += 2) {
+                const int at = 16 * c + k / 2;
+                hi[at] = pack_hi<PL>(v[k], v[k + 1]);
+                if (PL == 2) lo[at] = pack_lo(v[k], v[k + 1], hi[at]);
+              }
+            }
+            float a, b;
+            unpack2(add2(sum2, sum3), a, b);
+            l += a + b;
+          }
+          if (MODE != LOSS) {
+#pragma unroll
+            for (int c = 0; c < U / 2; c += 32) {
+              TMEM_ST32(s_addr + c, hi, c);
+              if (PL == 2) TMEM_ST32(s_addr + U / 2 + c, lo, c);
             }
             wait_st();
           }
-        }
-        if (!ok) break;
-        l += sum;
-      } else {
-        // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight
-        const int32_t* ct = reinterpret_cast<const int32_t*>(col + 3 * NT);
-        const int64_t row0 = r * R + 128 * grp + 32 * quarter;
-        const f32x2 rb2 = pack2(rb, rb);
-        f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
-        TMEM_LD32(z[0], 0, s_addr);
-#pragma unroll
-        for (int c = 0; c < U / 32; ++c) {
-          float(&v)[32] = z[c & 1];
-          const int64_t in_rows = (int64_t)ct[32 * c + lane] - row0;
-          const int who = (int)in_rows;
-          const unsigned hits = __ballot_sync(FULL, in_rows >= 0 && in_rows < 32);
-          WAIT_LD32(v);
-          if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
-          const float* cc = col + 32 * c;
-          if (g.bias) {
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, rb2), v[k], v[k + 1]);
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);              // -m
-              unpack2(add2(pack2(v[k], v[k + 1]), cm.x), v[k], v[k + 1]);
-              unpack2(add2(pack2(v[k + 2], v[k + 3]), cm.y), v[k + 2], v[k + 3]);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              const ulonglong2 cm = *reinterpret_cast<const ulonglong2*>(cc + k);
-              unpack2(fma2(pack2(v[k], v[k + 1]), factor2, cm.x), v[k], v[k + 1]);
-              unpack2(fma2(pack2(v[k + 2], v[k + 3]), factor2, cm.y), v[k + 2], v[k + 3]);
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const ulonglong2 cw = *reinterpret_cast<const ulonglong2*>(cc + NT + k);
-            const float p0 = tgnn_history::exp2_fast(v[k]), p1 = tgnn_history::exp2_fast(v[k + 1]);
-            const float p2 = tgnn_history::exp2_fast(v[k + 2]), p3 = tgnn_history::exp2_fast(v[k + 3]);
-            unpack2(mul2(pack2(p0, p1), cw.x), v[k], v[k + 1]);
-            unpack2(mul2(pack2(p2, p3), cw.y), v[k + 2], v[k + 3]);
-          }
-          for (unsigned left = hits; left; left &= left - 1) {
-            const int k = __ffs(left) - 1;
-            const int mine = __shfl_sync(FULL, who, k);
-            const float fix = cc[2 * NT + k];
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (i == k && mine == lane) v[i] = fix;
-          }
-#pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const int at = 16 * c + k / 2;
-            if (g.dbias) {
-              sum2 = add2(sum2, pack2(v[k], v[k + 1]));
-              sum3 = add2(sum3, pack2(v[k + 2], v[k + 3]));
-            }
-            hi[at] = pack_hi<PL>(v[k], v[k + 1]);
-            hi[at + 1] = pack_hi<PL>(v[k + 2], v[k + 3]);
-            if (PL == 2) {
-              lo[at] = pack_lo(v[k], v[k + 1], hi[at]);
-              lo[at + 1] = pack_lo(v[k + 2], v[k + 3], hi[at + 1]);
-            }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar_p + 8 * buf);
+            if (MODE == LOSS && sub == PER - 1) mbar_arrive(smem_u32(&s_empty[st]));
           }
         }
-        float a, b;
-        unpack2(add2(sum2, sum3), a, b);
-        l += a + b;
+        if (++st == (uint32_t)g.stages) st = 0;
+      }
+      if (!ok) break;
+      left -= count;
+      // the group's rows are done as far as this block goes
+      const bool alone = count == all_cols;
+      float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
+      if (valid) {
+        if (MODE == BACKWARD) {
+          if (!alone) slot[g.s.od] = l;
+          else if (summed) g.dbias[row] = l / ug;
+        } else {
+          float* to = alone ? g.full + 3 * row : slot + g.s.od;
+          to[0] = m;
+          to[1] = l;
+          to[2] = zt;
+        }
       }
       if (MODE != LOSS) {
+        ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, abort_flag));
+        if (!ok) break;
+        fence_after();
+        const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
+        const int dim = g.s.dim;
+        float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
+        float(&o)[32] = z[1];                            // z[0] may hold what was asked for
+        for (int c = 0; c < g.s.od; c += 32) {
+          __syncwarp();                                  // lanes without a row have gone ahead
+          TMEM_LD32(o, 0, o_addr + c);
+          WAIT_LD32(o);
+          if (!valid) {
+          } else if (!alone) {
 #pragma unroll
-        for (int c = 0; c < U / 2; c += 32) {
-          TMEM_ST32(s_addr + c, hi, c);
-          if (PL == 2) TMEM_ST32(s_addr + U / 2 + c, lo, c);
-        }
-        wait_st();
-      }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(&s_pfull[grp][buf]));
-        if (MODE == LOSS && sub == PER - 1) mbar_arrive(smem_u32(&s_empty[st]));
-      }
-      if (end) {
-        // the group's rows are done as far as this block goes
-        const int64_t row = r * R + row_in;
-        const bool alone = sh.begin(blockIdx.x) <= r * col_tiles && x1 >= (r + 1) * col_tiles;
-        float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
-        if (valid) {
-          if (MODE == BACKWARD) {
-            if (!alone) slot[g.s.od] = l;
-            else if (g.dbias) g.dbias[row] = l / ug;
-          } else {
-            float* to = alone ? g.full + 3 * row : slot + g.s.od;
-            to[0] = m;
-            to[1] = l;
-            to[2] = zt;
-          }
-        }
-        if (MODE != LOSS) {
-          ok = __all_sync(FULL, mbar_wait(smem_u32(&s_pv[grp][buf]), (u >> 1) & 1, abort_flag));
-          if (!ok) break;
-          fence_after();
-          const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
-          const int dim = g.s.dim;
-          float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
-          float(&o)[32] = z[0];
-          for (int c = 0; c < g.s.od; c += 32) {
-            __syncwarp();                                // lanes without a row have gone ahead
-            TMEM_LD32(o, 0, o_addr + c);
-            WAIT_LD32(o);
-            if (!valid) {
-            } else if (!alone) {
+            for (int k = 0; k < 32; k += 4)
+              if (c + k < g.s.od) *reinterpret_cast<float4*>(slot + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          } else if (MODE == FORWARD) {
 #pragma unroll
-              for (int k = 0; k < 32; k += 4)
-                if (c + k < g.s.od) *reinterpret_cast<float4*>(slot + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
-            } else if (MODE == FORWARD) {
+            for (int k = 0; k < 32; ++k)
+              if (c + k < dim) home[c + k] = o[k];
+          } else if (g.dtable) {
+            if (g.dtype == TGNN_F32) {
+              float* to = static_cast<float*>(g.dtable) + row * dim + c;
+              if (dim % 4 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
 #pragma unroll
-              for (int k = 0; k < 32; ++k)
-                if (c + k < dim) home[c + k] = o[k];
-            } else if (g.dtable) {
-              if (g.dtype == TGNN_F32) {
-                float* to = static_cast<float*>(g.dtable) + row * dim + c;
-                if (dim % 4 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
-#pragma unroll
-                  for (int k = 0; k < 32; k += 4)
-                    if (c + k < dim) *reinterpret_cast<float4*>(to + k) = make_float4(o[k] * out, o[k + 1] * out, o[k + 2] * out, o[k + 3] * out);
-                } else {
-#pragma unroll
-                  for (int k = 0; k < 32; ++k)
-                    if (c + k < dim) to[k] = o[k] * out;
-                }
+                for (int k = 0; k < 32; k += 4)
+                  if (c + k < dim) *reinterpret_cast<float4*>(to + k) = make_float4(o[k] * out, o[k + 1] * out, o[k + 2] * out, o[k + 3] * out);
               } else {
-                __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
-                if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
 #pragma unroll
-                  for (int k = 0; k < 32; k += 4)
-                    if (c + k < dim)
-                      *reinterpret_cast<uint2*>(to + k) = make_uint2(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out));
-                } else {
+                for (int k = 0; k < 32; ++k)
+                  if (c + k < dim) to[k] = o[k] * out;
+              }
+            } else {
+              __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
+              if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
 #pragma unroll
-                  for (int k = 0; k < 32; ++k)
-                    if (c + k < dim) to[k] = __float2bfloat16_rn(o[k] * out);
-                }
+                for (int k = 0; k < 32; k += 4)
+                  if (c + k < dim)
+                    *reinterpret_cast<uint2*>(to + k) = make_uint2(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out));
+              } else {
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                  if (c + k < dim) to[k] = __float2bfloat16_rn(o[k] * out);
               }
             }
           }
-          __syncwarp();
-          fence_before();
         }
+        __syncwarp();
+        fence_before();
       }
-      if (sub == PER - 1) {
-        if (++st == (uint32_t)g.stages) st = 0;
-        if (++j == col_tiles) {
-          j = 0;
-          ++r;
-        }
-      }
+      j = 0;
+      ++r;
     }
+    if (have) WAIT_LD32(z[0]);
     if (!ok && lane == 0) {
       s_abort = 1;
       atomicCAS(g.status, 0, TGNN_ETIMEOUT);
