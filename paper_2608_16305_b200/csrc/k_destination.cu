@@ -35,7 +35,7 @@ namespace {
 constexpr unsigned kSpin = 1u << 22;
 constexpr int kMaxBlocks = 160;             // thread blocks of the main kernel, one per multiprocessor
 constexpr int kSmem = 226 * 1024;           // dynamic shared memory; the static part is below 1 KB
-constexpr int kMaxParts = 592;              // partial maxima of the fp32 rows
+constexpr int kMaxParts = 592;              // partial maxima: of fp32 rows, of the bias
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.40282347e38f;
@@ -67,7 +67,7 @@ struct Prep {
   int backward, tile;
   int32_t* count;                            // [0]: roots that take part
   int32_t* act;                              // their indices
-  float* parts;                              // [q, table, dloss][kMaxParts]
+  float* parts;                              // largest magnitudes of [q, table, dloss] and the largest bias, [4][kMaxParts]
   uint16_t* qp;
   uint16_t* tp;
   float* cols;                               // what a tile's columns need, tile by tile
@@ -104,7 +104,7 @@ __device__ __forceinline__ float largest(const float* parts, float* s_red) {  //
   return x;
 }
 
-// Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows.
+// Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows and the largest bias.
 __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
   chain_wait();
   chain_release();
@@ -113,27 +113,30 @@ __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   if (blockIdx.x > 0) {
     const int b = blockIdx.x - 1, nb = gridDim.x - 1;
-    float top[3] = {0.f, 0.f, 0.f};
-    const int64_t values = a.s.rows * a.s.dim;
+    float top[4] = {0.f, 0.f, 0.f, -INFINITY};
+    const int64_t values = a.s.planes == 2 ? a.s.rows * a.s.dim : 0;
+    if (!a.backward && a.bias)
+      for (int64_t i = (int64_t)b * 1024 + t; i < a.s.rows; i += (int64_t)nb * 1024) top[3] = fmaxf(top[3], a.bias[i]);
     for (int64_t i = (int64_t)b * 1024 + t; i < values; i += (int64_t)nb * 1024)
       top[1] = fmaxf(top[1], fabsf(static_cast<const float*>(a.table)[i]));
-    for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n; r += (int64_t)nb * 32) {
+    for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n && a.s.planes == 2; r += (int64_t)nb * 32) {
       const int64_t y = target_of(a, r);
       if (y < 0 || y >= a.s.rows) continue;
       for (int c = lane; c < a.s.dim; c += 32) top[0] = fmaxf(top[0], fabsf(static_cast<const float*>(a.q)[r * a.s.dim + c]));
       if (a.backward) top[2] = fmaxf(top[2], fabsf(a.dloss[r]));
     }
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
       float x = top[k];
       for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
       __syncthreads();
       if (lane == 0) s_red[warp] = x;
       __syncthreads();
-      if (t == 0) {
-        for (int w = 1; w < 32; ++w) x = fmaxf(x, s_red[w]);
-        a.parts[k * kMaxParts + b] = x;
-        for (int i = b + nb; i < kMaxParts; i += nb) a.parts[k * kMaxParts + i] = 0.f;
+      if (warp == 0) {
+        x = s_red[lane];
+        for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
+        if (lane == 0) a.parts[k * kMaxParts + b] = x;
       }
+      for (int i = b + nb * (1 + t); i < kMaxParts; i += nb * 1024) a.parts[k * kMaxParts + i] = k == 3 ? -INFINITY : 0.f;
     }
     return;
   }
@@ -317,10 +320,17 @@ __device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo, uint
   return (uint64_t)((saddr >> 4) & 0x3FFF) | (uint64_t)((lbo >> 4) & 0x3FFF) << 16 | (uint64_t)((sbo >> 4) & 0x3FFF) << 32 | (uint64_t)1 << 46 |
          (uint64_t)2 << 61;                  // the architecture's version, 128-byte swizzle
 }
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// One lane of a converged warp.  (The compiler knows of it that one lane runs what it guards, and keeps descriptors in uniform registers there:
+// 5 % of the kernel's time against lane == 0.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
+}
+__device__ __forceinline__ void mma(bool on, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"((uint32_t)on)
       : "memory");
 }
 __device__ __forceinline__ void mma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {  // A in tensor memory
@@ -417,9 +427,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   constexpr int R = 128 * NH, PER = NT / U;            // units per tile
+  constexpr int KS = NH == 2 || (PL == 2 && NT == 128) ? 8 : 16;   // steps of 16 in dim, at most
+  constexpr bool MOVING = MODE == FORWARD && PL == 2;  // the reference of a row's weights can move
   constexpr int COL_BYTES = (MODE == BACKWARD ? 16 : 4) * NT;
   constexpr float SHIFT = PL == 2 ? 7.f : 0.f;         // fp16: weights about 2^7, with 2^-32 of that above its smallest numbers
-  constexpr float MOST = PL == 2 ? 32768.f : 1.1529215e18f;      // a unit's sum that no weight's type minds (bf16: 2^60)
+  constexpr float MOST = 32768.f;                      // a unit's sum that no weight minds
   constexpr uint32_t a_chunk = R * 128, t_chunk = NT * 128;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* smem = reinterpret_cast<unsigned char*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -504,7 +516,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     __syncwarp();
   } else if (warp <= NH) {
     // ---------------------------------------------------------------- matrix instructions of group h
-    if (lane == 0) {
+    if (elect_one()) {
       bool ok = true;
       const int h = warp - 1;
       const uint32_t fmt = PL == 2 ? 0u : 1u;            // fp16 or bf16, both operands
@@ -536,9 +548,8 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
         for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) { // hi hi, hi lo, lo hi
           const uint64_t ap = da + (pr == 2 ? a_plane : 0), tp = t0 + (pr == 1 ? t_plane : 0);
 #pragma unroll
-          for (int ks = 0; ks < 16; ++ks) {
-            if (ks >= g.ksteps) break;
-            mma(d, ap + (ks >> 2) * (a_chunk >> 4) + (ks & 3) * 2, tp + (ks >> 2) * (t_chunk >> 4) + (ks & 3) * 2, id_s, pr > 0 || ks > 0);
+          for (int ks = 0; ks < KS; ++ks) {
+            mma(ks < g.ksteps, d, ap + (ks >> 2) * (a_chunk >> 4) + (ks & 3) * 2, tp + (ks >> 2) * (t_chunk >> 4) + (ks & 3) * 2, id_s, pr > 0 || ks > 0);
           }
         }
         commit(smem_u32(&s_sfull[h][buf]));
@@ -604,6 +615,13 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
       ut = unit_of(top[1]);
       if (MODE == BACKWARD) ug = 2.f * unit_of(top[2]);
     }
+    float most_bias = 0.f;
+    if (MODE != BACKWARD && !MOVING && g.bias) {
+      float top = -INFINITY;
+      for (int i = lane; i < kMaxParts; i += 32) top = fmaxf(top, g.parts[3 * kMaxParts + i]);
+      for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, x));
+      most_bias = bias2(top);
+    }
     const float factor = g.scale * kLog2e / uq / ut;
     const f32x2 factor2 = pack2(factor, factor);
     const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
@@ -667,7 +685,8 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
                   unpack2(add2(fma2(pack2(v[k + 2], v[k + 3]), factor2, b.y), ref2), v[k + 2], v[k + 3]);
                 }
               }
-              if (__builtin_expect(any_hit, 0)) {
+              if (any_hit) {
+                __syncwarp();                            // keeps this a branch: as predicated instructions it costs 50 a unit
 #pragma unroll
                 for (int k = 0; k < 32; ++k)
                   if (hit == c + k) {
@@ -688,16 +707,30 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
               }
               return top;
             };
-            // A row's reference is the maximum of the first unit in which it sees anything.
-            if (__builtin_expect(__any_sync(FULL, m == -INFINITY), 0)) {
+            // The reference of a row's weights.  Where it can move: the maximum of the first unit in which the row sees anything.  Else the
+            // largest product of the first unit (the target's apart) plus the largest bias of all, for good: below the row's maximum by no more than the products' spread, whatever the
+            // biases hide, and fp32 and bf16 hold weights that pass it by 2^127 (88 in natural units).  A row that goes beyond is done again by the last kernel.
+            if (MOVING ? (bool)__any_sync(FULL, m == -INFINITY) : t == 0 && sub == 0) {
               WAIT_LD32(z[0]);
-              const float top = maximum();
-              if (m == -INFINITY) m = top;
+              if (MOVING) {
+                const float top = maximum();
+                if (m == -INFINITY) m = top;
+              } else {
+                have = false;
+                float top = -INFINITY;
+                for (int c = 0; c < U; c += 32) {
+                  TMEM_LD32(z[0], 0, s_addr + c);
+                  WAIT_LD32(z[0]);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) top = hit == c + k ? top : fmaxf(top, z[0][k] * factor);
+                }
+                m = most_bias == -INFINITY ? 0.f : top + most_bias;
+              }
               TMEM_LD32(z[0], 0, s_addr);
             }
             float sum;
-            for (int again = 0;; ++again) {
-              const float ref = m == -INFINITY ? 0.f : m;
+            auto weights = [&]() {
+              const float ref = MOVING && m == -INFINITY ? 0.f : m;
               const f32x2 shift2 = pack2(SHIFT, SHIFT);
               f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
 #pragma unroll
@@ -709,7 +742,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
                 logits(v, 32 * c, ref);
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) {
-                  if (PL == 2) {                         // (added to the difference: beside a mask's lowest value it would be lost)
+                  if (MOVING) {                          // (added to the difference: beside a mask's lowest value it would be lost)
                     unpack2(add2(pack2(v[k], v[k + 1]), shift2), v[k], v[k + 1]);
                     unpack2(add2(pack2(v[k + 2], v[k + 3]), shift2), v[k + 2], v[k + 3]);
                   }
@@ -731,14 +764,16 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
               float a, b;
               unpack2(add2(sum2, sum3), a, b);
               sum = a + b;
-              // The reference is moved only when the unit's sum says that a weight may have passed what its type holds: O has then to be multiplied and
-              // the weights are formed again.  (Once: what is too large, or no number, then stays so.)
-              if (__builtin_expect(again || !__any_sync(FULL, !(sum <= MOST)), 1)) break;
+            };
+            weights();
+            // fp16: the reference is moved when the unit's sum says that a weight may have passed what the type holds.  O has then to be multiplied and the
+            // weights are formed again.  (Once: what is too large, or no number, then stays so.)
+            if (MOVING && __builtin_expect(__any_sync(FULL, !(sum <= MOST)), 0)) {
               if (have) WAIT_LD32(z[0]);
               const float now = fmaxf(m, maximum()), f = now == -INFINITY ? 1.f : exp2f(m - now);
               l *= f;
               m = now;
-              if (MODE == FORWARD && (t > 0 || sub > 0)) {  // O is at rest once the unit before has been added
+              if (t > 0 || sub > 0) {                    // O is at rest once the unit before has been added
                 ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * (buf ^ 1), ((u - 1) >> 1) & 1, abort_flag));
                 if (!ok) break;
                 fence_after();
@@ -752,8 +787,8 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
                 wait_st();
               }
               TMEM_LD32(z[0], 0, s_addr);
+              weights();
             }
-            if (!ok) break;
             l += sum;
           } else {
             // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight
@@ -761,11 +796,13 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
             const int32_t row0 = (int32_t)(r * R) + 128 * grp + 32 * quarter;
             const f32x2 rb2 = pack2(rb, rb);
             f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
+            bool here = false;
+#pragma unroll
+            for (int c = 0; c < U / 32; ++c) here |= (uint32_t)(ct[32 * c + lane] - row0) < 32u;
+            const bool any_hit = __any_sync(FULL, here);
 #pragma unroll
             for (int c = 0; c < U / 32; ++c) {
               float(&v)[32] = z[c & 1];
-              const int who = ct[32 * c + lane] - row0;
-              const unsigned hits = __ballot_sync(FULL, (uint32_t)who < 32u);
               const float* cc = col + 32 * c;
               WAIT_LD32(v);
               if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
@@ -795,8 +832,9 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
                 unpack2(mul2(pack2(p0, p1), cw.x), v[k], v[k + 1]);
                 unpack2(mul2(pack2(p2, p3), cw.y), v[k + 2], v[k + 3]);
               }
-              if (__builtin_expect(hits != 0, 0)) {
-                for (unsigned more = hits; more; more &= more - 1) {
+              if (any_hit) {
+                const int who = ct[32 * c + lane] - row0;
+                for (unsigned more = __ballot_sync(FULL, (uint32_t)who < 32u); more; more &= more - 1) {
                   const int k = __ffs(more) - 1;
                   const int mine = __shfl_sync(FULL, who, k);
                   const float fix = cc[2 * NT + k];
@@ -935,7 +973,9 @@ struct Join {
   const float* parts;
   const float* slots;
   const float* full;
+  const void* q;
   const void* table;
+  const float* bias;
   const void* target;
   int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles
   float scale;
@@ -951,7 +991,7 @@ template <int W>
 __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
   chain_wait();
   chain_release();
-  __shared__ float s_m[W], s_l[W];
+  __shared__ float s_m[W], s_l[W], s_z[W];
   __shared__ float4 s_o[W == 1 ? 1 : W][64];
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t live = a.count[0];
@@ -972,6 +1012,7 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
     const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
     float* dir = a.kept ? a.kept + 3 * a.s.n + (int64_t)i * dim : nullptr;
+    bool again = false;
     float M, L, zt;
     float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
     if (c0 == c1) {
@@ -1043,9 +1084,79 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
         __syncthreads();
       }
     }
+    if (!(L < INFINITY)) {
+      // A weight has passed what fp32 holds (or a value is no number): the row again, product by product, 32 nodes at a time per warp.  Parts are in
+      // units of their own maximum.
+      M = -INFINITY;
+      float l = 0.f;
+      zt = 0.f;
+      for (int k = 0; k < 8; ++k) (&o[0].x)[k] = 0.f;
+      const float factor = a.scale * kLog2e;
+      for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
+        const int64_t j = j0 + lane;
+        float x = -INFINITY;
+        if (j < a.s.rows) {
+          float dot = 0.f;
+          for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c), value_of(a.table, a.dtype, j * dim + c), dot);
+          x = fmaf(dot, factor, a.bias ? bias2(a.bias[j]) : 0.f);
+          if (j == y) {
+            zt = x;
+            x = -INFINITY;
+          }
+        }
+        float top = x;
+        for (int e = 16; e; e >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, e));
+        const float now = fmaxf(M, top), ref = now == -INFINITY ? 0.f : now, f = exp2f(M - ref);
+        M = now;
+        const float p = exp2f(x - ref);
+        l = l * f + p;
+        for (int k = 0; k < 8; ++k) (&o[0].x)[k] *= f;
+        for (int e = 0; e < 32 && j0 + e < a.s.rows; ++e) {
+          const float pe = __shfl_sync(FULL, p, e);
+          for (int h = 0; h < 2; ++h)
+            for (int k = 0; k < 4; ++k) {
+              const int c = 128 * h + 4 * lane + k;
+              if (c < dim) (&o[h].x)[k] = fmaf(pe, value_of(a.table, a.dtype, (j0 + e) * dim + c), (&o[h].x)[k]);
+            }
+        }
+      }
+      for (int e = 16; e; e >>= 1) {
+        l += __shfl_xor_sync(FULL, l, e);
+        zt += __shfl_xor_sync(FULL, zt, e);              // 0 but in one lane
+      }
+      if (W > 1) {
+        __syncthreads();
+        if (lane == 0) {
+          s_m[warp] = M;
+          s_z[warp] = zt;
+        }
+        __syncthreads();
+        const float mine = M;
+        zt = 0.f;
+        for (int w = 0; w < W; ++w) {
+          M = fmaxf(M, s_m[w]);
+          zt += s_z[w];
+        }
+        const float f = exp2f(mine - (M == -INFINITY ? 0.f : M));
+        if (lane == 0) s_l[warp] = l * f;
+        for (int k = 0; k < 8; ++k) (&s_o[warp][lane + 32 * (k >> 2)].x)[k & 3] = (&o[0].x)[k] * f;
+        __syncthreads();
+        l = 0.f;
+        for (int w = 0; w < W; ++w) l += s_l[w];
+        if (warp == 0)
+          for (int k = 0; k < 8; ++k) {
+            float v = 0.f;
+            for (int w = 0; w < W; ++w) v += (&s_o[w][lane + 32 * (k >> 2)].x)[k & 3];
+            (&o[0].x)[k] = v;
+          }
+        __syncthreads();
+      }
+      L = l;
+      again = true;
+    }
     if (warp != 0) continue;                              // (the next row's first barrier waits for warp 0)
     // L counts in units of 2^shift, O in units of 2^shift and of the table's unit
-    const float shift = a.s.planes == 2 ? 7.f : 0.f;
+    const float shift = a.s.planes == 2 && a.kept && !again ? 7.f : 0.f;
     const float d = (M - zt) + (log2f(L) - shift);        // log2 of the others' weight over the target's
     const bool none = L == 0.f, lost = zt == -INFINITY;
     float loss, miss, mm, inv;
@@ -1076,13 +1187,12 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       }
     }
     if (dir) {
-      const float per = none ? 0.f : 1.f / L;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int c = 128 * h + 4 * lane + k;
-          if (c < dim) dir[c] = none ? 0.f : ((&o[h].x)[k] * per / ut - value_of(a.table, a.dtype, y * dim + c)) * miss;
+          if (c < dim) dir[c] = none ? 0.f : ((&o[h].x)[k] / L / (again ? 1.f : ut) - value_of(a.table, a.dtype, y * dim + c)) * miss;
         }
     }
   }
@@ -1178,7 +1288,7 @@ Layout layout(const Shape& s, int dtype) {
   };
   l.count = take(4);
   l.act = take(4 * s.n);
-  l.parts = take(4ll * 3 * kMaxParts);
+  l.parts = take(4ll * 4 * kMaxParts);
   l.qp = take(2ll * up(s.n, 128) * s.planes * s.dp);
   l.tp = take(2ll * s.rows * s.planes * s.dp);
   const int64_t forward = 4ll * up(s.rows, f.tile), backward = 16ll * up(s.n, f.tile);
@@ -1310,7 +1420,8 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   if (m.stages > 4) m.stages = 4;
   m.ahead = m.stages > 1 ? 2 : 1;
   const size_t smem = 1024 + a_bytes + (size_t)m.stages * t_bytes;
-  const int blocks_of_parts = s.planes == 2 ? (int)(a.rows * a.dim >> 14 >= 4 * 148 - 1 ? 4 * 148 - 1 : (a.rows * a.dim >> 14) + 1) : 0;
+  const int64_t maxima = s.planes == 2 ? a.rows * a.dim : MODE != BACKWARD && a.bias ? a.rows : 0;
+  const int blocks_of_parts = maxima == 0 ? 0 : (int)(maxima >> 12 >= kMaxParts - 1 ? kMaxParts - 1 : (maxima >> 12) + 1);
   c(begin_kernel, dim3(1 + blocks_of_parts), dim3(1024), 0, p);
   const int64_t work = (direct ? 0 : a.rows) + a.n + (MODE == BACKWARD ? a.n : a.rows) / 32;
   c(prep_kernel, dim3((unsigned)(work / 16 >= 8 * sms ? 8 * sms : work / 16 + 1)), dim3(256), 0, p);
@@ -1324,7 +1435,9 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->parts = p.parts;
   j->slots = m.slots;
   j->full = m.full;
+  j->q = a.q;
   j->table = a.table;
+  j->bias = a.bias;
   j->target = a.target;
   j->index_bits = a.index_bits;
   j->dtype = a.dtype;

@@ -145,6 +145,32 @@ def test_logits_that_rise_along_the_table(dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [5, 400])
+def test_products_that_rise_along_the_table(n, dtype):
+    """The same by the rows themselves: logits of 0 to 600."""
+    x = make(n, 2000, 64, dtype, bias=True, masked=0.0, spread=0.2)
+    x["table"] = (x["table"].float() * 0.02 + torch.linspace(0, 1, 2000, device="cuda")[:, None]).to(dtype)
+    x["q"] = (x["q"].float() * 0.02 + 75.0).to(dtype)
+    out = call(x)
+    check(x, out)
+    assert float(out["loss"].max()) > 300
+    x["table"] = x["table"].flip(0).contiguous()
+    check(x, call(x))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("low", [-1e4, -1e9, torch.finfo(F32).min, -math.inf])
+def test_masks_over_the_first_nodes(low, dtype):
+    x = make(100, 1500, 32, dtype, masked=0.1)
+    x["bias"][:700] = low
+    x["target"] = torch.where(x["target"] >= 0, 700 + x["target"] % 800, x["target"])
+    out = call(x)
+    assert bool(torch.isfinite(out["loss"]).all()) and bool((out["dtable"][:700] == 0).all()) and bool((out["dbias"][:700] == 0).all())
+    check(x | dict(table=x["table"][700:].contiguous(), bias=x["bias"][700:].contiguous(), target=torch.where(x["target"] >= 0, x["target"] - 700, x["target"])),
+          {k: v[700:] if k in ("dtable", "dbias") else v for k, v in out.items()})
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_hidden_nodes(dtype):
     x = make(200, 700, 40, dtype, masked=0.1)
     hidden = torch.rand(700, device="cuda") < 0.5
