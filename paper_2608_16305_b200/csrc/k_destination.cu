@@ -364,16 +364,30 @@ __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers from 0; a division of 64 bits takes five times as long
+  return (((uint64_t)a | (uint64_t)b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // The blocks' shares of the tiles: block c has tiles [begin(c), begin(c + 1)), and tile x belongs to block owner(x).
 struct Share {
-  int64_t total;
-  int blocks;                                // with a tile at least
-  __device__ __forceinline__ Share(int64_t t, int launched) : total(t), blocks((int)min(t, (int64_t)launched)) {}
-  __device__ __forceinline__ int64_t begin(int c) const { return total * c / blocks; }
-  __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * blocks - 1) / total); }
+  int64_t total, per;
+  int blocks, more;                          // blocks with a tile at least; the first `more` have per + 1, the others per
+  __device__ __forceinline__ Share(int64_t t, int launched) : total(t), per(0), blocks((int)min(t, (int64_t)launched)), more(0) {
+    if (blocks > 0) {
+      per = quotient(t, blocks);
+      more = (int)(t - per * blocks);
+    }
+  }
+  __device__ __forceinline__ int64_t begin(int c) const { return per * c + min(c, more); }
+  __device__ __forceinline__ int owner(int64_t x) const {
+    const int64_t edge = more * (per + 1);
+    return x < edge ? (int)quotient(x, per + 1) : more + (int)quotient(x - edge, per);
+  }
 };
 // Where block c puts its part of row group r: its first group's place or its last one's.
-__device__ __forceinline__ int slot_of(const Share& sh, int64_t col_tiles, int c, int64_t r) { return sh.begin(c) / col_tiles == r ? 2 * c : 2 * c + 1; }
+__device__ __forceinline__ int slot_of(const Share& sh, int64_t col_tiles, int c, int64_t r) {
+  const int64_t x = sh.begin(c) - r * col_tiles;           // its first tile is of this group, or of an earlier one
+  return x >= 0 ? 2 * c : 2 * c + 1;
+}
 
 // Two fp32 values in one register pair: added and multiplied in one instruction.
 typedef unsigned long long f32x2;
@@ -473,7 +487,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
   const Share sh((a_rows + R - 1) / R * col_tiles, gridDim.x);
   const bool idle = (int)blockIdx.x >= sh.blocks;
   const int64_t x0 = idle ? 0 : sh.begin(blockIdx.x), x1 = idle ? 0 : sh.begin(blockIdx.x + 1);
-  const int64_t r0 = idle ? 0 : x0 / col_tiles, j0 = idle ? 0 : x0 - r0 * col_tiles;       // the first tile: group of rows, and tile of columns
+  const int64_t r0 = idle ? 0 : quotient(x0, col_tiles), j0 = idle ? 0 : x0 - r0 * col_tiles;       // the first tile: group of rows, and tile of columns
   const uint32_t tiles = (uint32_t)(x1 - x0);
   const uint32_t o_base = tmem + 2 * NH * U;
 
@@ -977,13 +991,59 @@ struct Join {
   const void* table;
   const float* bias;
   const void* target;
-  int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles
+  int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles (powers of two)
+  int group_bits, tile_bits;
   float scale;
   float* loss;
   float* kept;
   void* dtable;
   float* dbias;
 };
+
+// Four values of a row from column c on (zeros behind dim), of fp32 or bf16.
+__device__ __forceinline__ float4 four_of(const void* base, int dtype, int64_t row, int dim, int c) {
+  const int64_t at = row * dim + c;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (dtype == TGNN_F32) {
+    const float* p = static_cast<const float*>(base) + at;
+    if (c + 4 <= dim && ((uintptr_t)p & 15) == 0) return *reinterpret_cast<const float4*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c + k < dim) (&v.x)[k] = p[k];
+  } else {
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(base) + at;
+    if (c + 4 <= dim && ((uintptr_t)p & 7) == 0) {
+      reinterpret_cast<const Group<__nv_bfloat16, 4>*>(p)->get(&v.x);
+      return v;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (c + k < dim) (&v.x)[k] = __bfloat162float(p[k]);
+  }
+  return v;
+}
+__device__ __forceinline__ void put_four(void* base, int dtype, int64_t row, int dim, int c, float4 v) {
+  const int64_t at = row * dim + c;
+  if (dtype == TGNN_F32) {
+    float* p = static_cast<float*>(base) + at;
+    if (c + 4 <= dim && ((uintptr_t)p & 15) == 0) *reinterpret_cast<float4*>(p) = v;
+    else
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < dim) p[k] = (&v.x)[k];
+  } else {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(base) + at;
+    if (c + 4 <= dim && ((uintptr_t)p & 7) == 0) {
+      Group<__nv_bfloat16, 4> g;
+      g.set(&v.x);
+      *reinterpret_cast<Group<__nv_bfloat16, 4>*>(p) = g;
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (c + k < dim) p[k] = __float2bfloat16_rn((&v.x)[k]);
+    }
+  }
+}
 
 // W warps per live root (8: a block, where the parts of a root are many) take its parts in turn, four columns per lane; then loss, m, 1 / l, 1 - p and the
 // direction of dq.
@@ -1007,11 +1067,16 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
     ut = unit_of(top);
   }
   for (int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; row < live; row += step) {
-    const int64_t r = row / a.group, in = row - r * a.group;
+    const int64_t r = row >> a.group_bits, in = row - (r << a.group_bits);
     const int i = a.act[row];
     const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
-    float* dir = a.kept ? a.kept + 3 * a.s.n + (int64_t)i * dim : nullptr;
+    const bool dir = a.kept != nullptr;
+    float4 own[2];                                        // the target's row
+    if (dir && warp == 0)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
     bool again = false;
     float M, L, zt;
     float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
@@ -1022,9 +1087,7 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       if (dir && warp == 0) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (128 * h + 4 * lane + k < dim) (&o[h].x)[k] = dir[128 * h + 4 * lane + k];
+          if (128 * h + 4 * lane < dim) o[h] = four_of(a.kept + 3 * a.s.n, TGNN_F32, i, dim, 128 * h + 4 * lane);
       }
     } else {
       // parts lie two places apart, but for the first, which may be its block's last
@@ -1043,7 +1106,7 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       }
       M = m;
       const float ref = M == -INFINITY ? 0.f : M;
-      zt = part(sh.owner(r * col_tiles + y / a.tile) - c0)[od + 2];
+      zt = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[od + 2];
       float l = 0.f;
 #pragma unroll 4
       for (int k = warp; k < parts; k += W) {
@@ -1187,13 +1250,21 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       }
     }
     if (dir) {
+      const float unit = again ? 1.f : ut;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int c = 128 * h + 4 * lane + k;
-          if (c < dim) dir[c] = none ? 0.f : ((&o[h].x)[k] / L / (again ? 1.f : ut) - value_of(a.table, a.dtype, y * dim + c)) * miss;
+      for (int h = 0; h < 2; ++h) {
+        const int c = 128 * h + 4 * lane;
+        if (c >= dim) break;
+        const float4 ty = own[h];
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (!none) {
+          v.x = (o[h].x / L / unit - ty.x) * miss;
+          v.y = (o[h].y / L / unit - ty.y) * miss;
+          v.z = (o[h].z / L / unit - ty.z) * miss;
+          v.w = (o[h].w / L / unit - ty.w) * miss;
         }
+        put_four(a.kept + 3 * a.s.n, TGNN_F32, i, dim, c, v);
+      }
     }
   }
 }
@@ -1221,8 +1292,8 @@ __global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
   const Share sh((a.s.rows + a.group - 1) / a.group * col_tiles, a.blocks);
   const int b = blockIdx.x + 1;
   if (b >= sh.blocks) return;
-  const int64_t x = sh.begin(b), r = x / col_tiles;
-  if (x % col_tiles == 0) return;
+  const int64_t x = sh.begin(b), r = quotient(x, col_tiles);
+  if (x == r * col_tiles) return;
   const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
   if (b != c0 + 1) return;
   float uq = 1.f, ug = 1.f;
@@ -1251,9 +1322,11 @@ __global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
       if (c == od) {
         if (a.dbias) a.dbias[row] = v.x / ug;
       } else if (a.dtable) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (c + e < dim) put(row * dim + c + e, (&v.x)[e] * out);
+        v.x *= out;
+        v.y *= out;
+        v.z *= out;
+        v.w *= out;
+        put_four(a.dtable, a.dtype, row, dim, c, v);
       }
     }
   }
@@ -1444,6 +1517,8 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->blocks = blocks;
   j->group = f.group;
   j->tile = f.tile;
+  j->group_bits = f.group == 256 ? 8 : 7;
+  j->tile_bits = f.tile == 128 ? 7 : 6;
   j->scale = a.scale;
   j->loss = loss;
   j->kept = kept;
