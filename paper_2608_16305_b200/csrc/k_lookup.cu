@@ -3,17 +3,16 @@
 // out[i] = scale * table[ids[i]] is a gather: bytes of the distinct rows and of the output bound it.  The gradient,
 // dtable[r] = scale * sum of dout[i] over ids[i] = r, is summed in a fixed order instead of by atomics: ids are sorted with their places
 // (least digit first, 8 bits at most at a time, stable), and runs of equal ids in the sorted order are summed.  Chunks of that order go to groups of
-// lanes; a run inside one chunk is written at once, a run across chunks leaves one partial sum per chunk, which a last kernel adds in
-// order.  Rows that no id names are zeros: the blocks beside the sorting ones write them while the sort, which waits on latency, runs.
+// lanes; what runs have in neighboring chunks is added up within a thread block, in order, and a run across blocks leaves one partial sum per block, which a
+// last kernel adds in order.  Rows that no id names are zeros: the blocks beside the sorting ones write them while the sort, which waits on latency, runs.
+// Few ids over few rows are not sorted: the blocks, each with some rows of the table, look through all of them.
 #include "tgnn_table.cuh"
 
 using namespace tgnn_table;
 
 namespace {
 
-constexpr int kOneBlock = 12288;    // ids that one block sorts in its shared memory (180 KB)
 constexpr int kSortThreads = 1024;
-constexpr int kTile = 8 * kSortThreads;
 constexpr int kMaxSortBlocks = 148;
 constexpr int kDigits = 256;
 
@@ -95,7 +94,6 @@ struct SortArgs {
   int32_t* status;        // checked on the first look at the ids; nullptr afterwards
   uint32_t* counter;      // zeroed by the first kernel
   int shift, width;       // the digit
-  int passes;             // one-block sort: how many digits, `width` bits each
   int sort_blocks;
   uint32_t per_block;
   char* zero;             // dtable: blocks behind the sorting ones fill their share of it with zeros
@@ -187,71 +185,7 @@ __device__ __forceinline__ void scan_digits(const uint32_t* total, uint32_t* bas
   __syncthreads();
 }
 
-// Up to 12288 ids: one block takes all digits in its shared memory, the others fill zeros.
-struct OneBlock {
-  uint32_t key[2][kOneBlock];
-  uint16_t place[2][kOneBlock];
-  uint32_t counts[32][kDigits];
-};
-__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const SortArgs a) {
-  extern __shared__ unsigned char raw[];
-  OneBlock& s = *reinterpret_cast<OneBlock*>(raw);
-  __shared__ uint32_t part[4][kDigits], total[kDigits], base[kDigits], warp_sum[8];
-  chain_release();
-  if (blockIdx.x > 0) {
-    fill_zero(a, blockIdx.x - 1, gridDim.x - 1);
-    return;
-  }
-  constexpr int K = kOneBlock / kSortThreads;
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const uint32_t span = (uint32_t)up(a.n, kSortThreads) / 32;                 // places per warp, a multiple of 32
-  if (t == 0) *a.counter = 0;
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const uint32_t i = warp * span + 32 * k + lane;
-    if (32u * k < span && i < a.n) {
-      s.key[0][i] = key_of(a, i);
-      s.place[0][i] = (uint16_t)i;
-    }
-  }
-  for (int p = 0; p < a.passes; ++p) {
-    for (int i = t; i < 32 * kDigits; i += kSortThreads) (&s.counts[0][0])[i] = 0;
-    __syncthreads();
-    const uint32_t *key = s.key[p & 1];
-    const uint16_t* place = s.place[p & 1];
-    const int shift = p * a.width;
-    const uint32_t mask = (1u << a.width) - 1;
-    uint32_t digit[K], rank[K];
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const uint32_t i = warp * span + 32 * k + lane;
-      digit[k] = 32u * k < span && i < a.n ? (key[i] >> shift) & mask : kDigits;
-    }
-    if (span == K * 32) rank_keys<K>(digit, rank, s.counts[warp], lane);
-    else
-#pragma unroll
-      for (int k = 0; k < K; ++k)
-        if (32u * k < span) rank_keys<1>(reinterpret_cast<uint32_t(&)[1]>(digit[k]), reinterpret_cast<uint32_t(&)[1]>(rank[k]), s.counts[warp], lane);
-    __syncthreads();
-    scan_warps(s.counts, part, total);
-    scan_digits(total, base, warp_sum);
-    const bool last = p == a.passes - 1;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (digit[k] >= kDigits) continue;
-      const uint32_t i = warp * span + 32 * k + lane;
-      const uint32_t to = base[digit[k]] + s.counts[warp][digit[k]] + rank[k];
-      if (last) a.out[to] = make_uint2(key[i], place[i]);
-      else {
-        s.key[(p + 1) & 1][to] = key[i];
-        s.place[(p + 1) & 1][to] = place[i];
-      }
-    }
-    __syncthreads();
-  }
-}
-
-// Many ids: per digit, a kernel that counts the digits of every block's share and one that moves the keys.
+// Per digit, a kernel that counts the digits of every block's share and one that moves the keys.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
   __shared__ uint32_t count[kDigits];
   chain_wait();
@@ -265,15 +199,25 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
   if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.counter = 0;
   __syncthreads();
-  for (uint32_t i = lo + threadIdx.x; i < hi; i += kSortThreads) {
-    const uint32_t d = ((a.in ? a.in[i].x : key_of(a, i)) >> a.shift) & mask;
-    const unsigned same = __match_any_sync(__activemask(), d);                // hubs: one addition per warp and digit
-    if ((threadIdx.x & 31) == __ffs(same) - 1) atomicAdd(count + d, __popc(same));
+  constexpr int K = 4;
+  for (uint32_t tile = lo; tile < hi; tile += K * kSortThreads) {
+    uint32_t d[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t i = tile + k * kSortThreads + threadIdx.x;
+      d[k] = i < hi ? ((a.in ? a.in[i].x : key_of(a, i)) >> a.shift) & mask : kDigits;
+    }
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const unsigned same = __match_any_sync(FULL, d[k]);                     // hubs: one addition per warp and digit
+      if ((threadIdx.x & 31) == __ffs(same) - 1 && d[k] < kDigits) atomicAdd(count + d[k], __popc(same));
+    }
   }
   __syncthreads();
   if (threadIdx.x < kDigits) a.hist[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
 }
 
+template <int K>
 __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs a) {
   __shared__ uint32_t counts[32][kDigits];
   __shared__ uint32_t part[4][kDigits], total[kDigits], base[kDigits], warp_sum[8];
@@ -305,8 +249,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
   }
   const uint32_t lo = blockIdx.x * a.per_block, hi = min(a.n, lo + a.per_block);
   const uint32_t mask = (1u << a.width) - 1;
-  constexpr int K = kTile / kSortThreads;
-  for (uint32_t tile = lo; tile < hi; tile += kTile) {
+  for (uint32_t tile = lo; tile < hi; tile += K * kSortThreads) {
     for (int i = t; i < 32 * kDigits; i += kSortThreads) (&counts[0][0])[i] = 0;
     __syncthreads();
     uint2 kp[K];
@@ -338,12 +281,12 @@ struct SumArgs {
   const void* dout;
   void* dtable;
   int dtype;              // of dtable
-  float* partial;         // [chunk][head, tail][dim]
-  uint8_t* through;       // [chunk]: the run at its start goes on behind its end
-  uint32_t* list;         // chunks at whose end a run that begins in them goes on
+  float* partial;         // [block][head, tail][dim]
+  uint8_t* through;       // [block]: the run at its start goes on behind its end
+  uint32_t* list;         // blocks at whose end a run that begins in them goes on
   uint32_t* counter;
   uint32_t n, rows;
-  int dim, groups, chunk;
+  int dim, groups, chunk, span;   // span: ids of a thread block
   float scale;
 };
 
@@ -384,44 +327,49 @@ __device__ __forceinline__ void store_values(void* base, int dtype, int64_t at, 
 }
 
 // G lanes take a chunk of the sorted order and V values each of a slice of G * V columns (grid.y slices).  Eight rows are asked for before
-// the first is added.
+// the first is added, and the ids of the next eight.
 template <typename T, int V, int G>
 __global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
+  constexpr int NG = 256 / G;
+  __shared__ float s_head[NG][G * V];
+  __shared__ uint8_t s_through[NG];
   chain_wait();
   chain_release();
-  const int lane = threadIdx.x & (G - 1);
-  const uint32_t chunk = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const int lane = threadIdx.x & (G - 1), grp = threadIdx.x / G;
   const int col = blockIdx.y * G + lane;
-  const int64_t t0 = (int64_t)chunk * a.chunk;
-  if (t0 >= a.n) return;
+  const int64_t t0 = min((int64_t)a.n, ((int64_t)blockIdx.x * NG + grp) * a.chunk);
   const uint32_t end = (uint32_t)min((int64_t)a.n, t0 + a.chunk);
   const bool active = col < a.groups;
   const T* dout = static_cast<const T*>(a.dout) + col * V;
-  uint32_t cur = a.sorted[t0].x;
-  bool head = t0 > 0 && cur < a.rows && a.sorted[t0 - 1].x == cur;            // the first run began in an earlier chunk
+  uint32_t cur = t0 < end ? a.sorted[t0].x : 0xffffffffu;
+  const bool head = t0 > 0 && cur < a.rows && a.sorted[t0 - 1].x == cur;      // the first run began in an earlier chunk
+  bool whole = true;                                                          // no run has ended yet
   float acc[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.f;
   constexpr int U = 8;
-  auto write = [&](bool to_partial, int slot) {
+  auto write = [&]() {
     if (!active) return;
-    if (to_partial) {
-      float* p = a.partial + ((int64_t)2 * chunk + slot) * a.dim + col * V;
+    float x[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = acc[i];
-    } else {
-      float x[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = acc[i] * a.scale;
-      store_values<V>(a.dtable, a.dtype, (int64_t)cur * a.dim + col * V, x);
-    }
+    for (int i = 0; i < V; ++i) x[i] = acc[i] * a.scale;
+    store_values<V>(a.dtable, a.dtype, (int64_t)cur * a.dim + col * V, x);
   };
-  bool whole = true;                                                          // no run has ended yet
+  auto keep = [&]() {                                                         // what the first run has here
+#pragma unroll
+    for (int i = 0; i < V; ++i) s_head[grp][lane * V + i] = acc[i];
+  };
+  uint2 next[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = t0 + u < end ? a.sorted[t0 + u] : make_uint2(0xffffffffu, 0);
   for (uint32_t t = (uint32_t)t0; t < end && cur < a.rows; t += U) {
     uint2 kp[U];
     Group<T, V> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) kp[u] = t + u < end ? a.sorted[t + u] : make_uint2(0xffffffffu, 0);
+    for (int u = 0; u < U; ++u) {
+      kp[u] = next[u];
+      next[u] = t + U + u < end ? a.sorted[t + U + u] : make_uint2(0xffffffffu, 0);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (active && kp[u].x < a.rows) v[u] = *reinterpret_cast<const Group<T, V>*>(dout + (int64_t)kp[u].y * a.dim);
@@ -429,8 +377,9 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
     for (int u = 0; u < U; ++u) {
       if (t + u >= end) break;
       if (kp[u].x != cur) {
-        write(head, 0);
-        head = whole = false;
+        if (head && whole) keep();
+        else write();
+        whole = false;
         cur = kp[u].x;
         if (cur >= a.rows) break;
 #pragma unroll
@@ -442,31 +391,197 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
       for (int i = 0; i < V; ++i) acc[i] += f[i];
     }
   }
-  bool goes_on = false;
-  if (cur < a.rows) {
-    goes_on = end < a.n && a.sorted[end].x == cur;
-    if (head) write(true, 0);
-    else write(goes_on, 1);
+  const bool goes_on = cur < a.rows && end < a.n && a.sorted[end].x == cur, begun = head && whole && cur < a.rows;
+  if (begun) keep();
+  else if (cur < a.rows && !goes_on) write();
+  if (lane == 0) s_through[grp] = begun && goes_on;
+  __syncthreads();
+  // Runs across the block's chunks: the group that a run begins in adds what the next ones have of it; the first group does so for the run that the
+  // block before began.
+  auto follow = [&](int g) {                                                  // from group g on; whether the run goes on behind the block
+    for (; g < NG; ++g) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] += s_head[g][lane * V + i];
+      if (!s_through[g]) return false;
+    }
+    return true;
+  };
+  auto part = [&](int slot) {
+    if (!active) return;
+    float* p = a.partial + ((int64_t)2 * blockIdx.x + slot) * a.dim + col * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = acc[i];
+  };
+  if (goes_on && !begun) {
+    if (follow(grp + 1)) {
+      part(1);
+      if (lane == 0 && blockIdx.y == 0) a.list[atomicAdd(a.counter, 1u)] = blockIdx.x;
+    } else {
+      write();
+    }
   }
-  if (lane == 0 && blockIdx.y == 0) {
-    a.through[chunk] = head && whole && goes_on;
-    if (goes_on && !head) a.list[atomicAdd(a.counter, 1u)] = chunk;
+  if (grp == 0) {
+    bool on = false;
+    if (head) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) acc[i] = 0.f;
+      on = follow(0);
+      part(0);
+    }
+    if (lane == 0 && blockIdx.y == 0) a.through[blockIdx.x] = on;
   }
 }
 
-// Runs across chunks: tail of the chunk that they begin in, then the heads of the next ones.  A block per run and 32 columns, eight warps that take every
-// eighth part; the list's order does not matter.
-__global__ void __launch_bounds__(256) run_join_kernel(const SumArgs a, uint32_t chunks) {
+// Few ids and few rows: a thread block per `kRows` rows of the table and slice of 32 * V columns looks through all ids, every warp an equal part of them, adds
+// up what it finds of its rows in shared memory, in order, and the parts of the warps are added in order.  One kernel in place of a sort's five.
+struct FewArgs {
+  const void* ids;
+  const void* dout;
+  void* dtable;
+  int32_t* status;
+  int64_t rows;
+  int index_bits, n, dim, dtype;
+  float scale;
+};
+constexpr int kFewWarps = 16;
+template <typename T, int V>
+__global__ void __launch_bounds__(32 * kFewWarps) few_sum_kernel(const FewArgs a) {
+  constexpr int kRows = 32 / V, kHeld = 128;
+  extern __shared__ float s_sum[];                                            // [warp][row][32 * V]
+  __shared__ uint16_t s_place[kFewWarps][kHeld];
+  __shared__ uint8_t s_row[kFewWarps][kHeld];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int col = (blockIdx.y * 32 + lane) * V;
+  const bool active = col < a.dim;
+  const T* dout = static_cast<const T*>(a.dout) + col;
+  float* mine = s_sum + warp * kRows * 32 * V + lane * V;
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+#pragma unroll
+    for (int k = 0; k < V; ++k) mine[r * 32 * V + k] = 0.f;
+  const int64_t row0 = (int64_t)blockIdx.x * kRows;
+  const int per = (a.n + kFewWarps - 1) / kFewWarps, lo = min(a.n, warp * per), hi = min(a.n, lo + per);
+  int held = 0;
+  auto flush = [&]() {
+    __syncwarp();
+    for (int u0 = 0; u0 < held; u0 += 8) {
+      Group<T, V> v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (u0 + u < held && active) v[u] = *reinterpret_cast<const Group<T, V>*>(dout + (int64_t)s_place[warp][u0 + u] * a.dim);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (u0 + u < held) {
+          float f[V], *x = mine + s_row[warp][u0 + u] * 32 * V;
+          v[u].get(f);
+#pragma unroll
+          for (int k = 0; k < V; ++k) x[k] += f[k];
+        }
+    }
+    held = 0;
+    __syncwarp();
+  };
+  bool beyond = false;
+  for (int j0 = lo; j0 < hi; j0 += 128) {
+    int64_t id[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int j = j0 + 32 * k + lane;
+      id[k] = -1;
+      if (j < hi) id[k] = a.index_bits == 64 ? static_cast<const int64_t*>(a.ids)[j] : (int64_t) static_cast<const int32_t*>(a.ids)[j];
+      beyond |= id[k] >= a.rows;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const bool here = id[k] >= row0 && id[k] < row0 + kRows && id[k] < a.rows;
+      const unsigned hits = __ballot_sync(FULL, here);
+      if (hits == 0) continue;
+      if (held + __popc(hits) > kHeld) flush();
+      if (here) {
+        const int at = held + __popc(hits & ((1u << lane) - 1));
+        s_place[warp][at] = (uint16_t)(j0 + 32 * k + lane);
+        s_row[warp][at] = (uint8_t)(id[k] - row0);
+      }
+      held += __popc(hits);
+    }
+  }
+  flush();
+  if (beyond) *a.status = 4;
+  __syncthreads();
+  for (int r = warp; r < kRows; r += kFewWarps) {
+    if (row0 + r >= a.rows) break;
+    float x[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) x[k] = 0.f;
+    for (int w = 0; w < kFewWarps; ++w)
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[k] += s_sum[((w * kRows + r) * 32 + lane) * V + k];
+#pragma unroll
+    for (int k = 0; k < V; ++k) x[k] *= a.scale;
+    if (active) store_values<V>(a.dtable, a.dtype, (row0 + r) * a.dim + col, x);
+  }
+}
+
+// Runs across blocks: tail of the block that they begin in, then the heads of the next ones.  A warp per run of up to 16 heads; longer ones (hubs) are put
+// aside and taken by the whole block, every warp its part of the heads.  The list's order does not matter.
+constexpr int kJoinWarps = 16, kAside = 256;
+template <int V>
+__device__ __forceinline__ void add_part(const float* p, float* x) {
+  float f[V];
+  reinterpret_cast<const Group<float, V>*>(p)->get(f);
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] += f[i];
+}
+template <int V>
+__global__ void __launch_bounds__(32 * kJoinWarps) run_join_kernel(const SumArgs a, uint32_t chunks) {
   chain_wait();
   chain_release();
-  __shared__ float sum[8][32];
-  __shared__ uint32_t s_last;
+  __shared__ float sum[kJoinWarps][32 * V];
+  __shared__ uint32_t aside[kAside], s_count, s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t runs = *a.counter;
-  for (uint32_t r = blockIdx.x; r < runs; r += gridDim.x) {
-    const uint32_t c0 = a.list[r];
-    uint32_t last = c0 + 1;                                                   // the last chunk that the run reaches
-    for (;; last += 256) {
+  const int col = (blockIdx.y * 32 + lane) * V;
+  const bool active = col < a.dim;
+  if (threadIdx.x == 0) s_count = 0;
+  __syncthreads();
+  auto finish = [&](uint32_t c0, float* x) {
+    if (!active) return;
+    const uint32_t id = a.sorted[(int64_t)(c0 + 1) * a.span].x;
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] *= a.scale;
+    store_values<V>(a.dtable, a.dtype, (int64_t)id * a.dim + col, x);
+  };
+  for (uint32_t r = blockIdx.x * kJoinWarps + warp; r < runs; r += gridDim.x * kJoinWarps) {
+    const uint32_t c0 = a.list[r], c = c0 + 1 + lane;
+    const unsigned ends = __ballot_sync(FULL, c >= chunks || !a.through[c]) & 0xffffu;
+    if (ends == 0) {                                                           // more than 16 heads
+      uint32_t at = 0;
+      if (lane == 0) at = atomicAdd(&s_count, 1u);
+      at = __shfl_sync(FULL, at, 0);
+      if (at < kAside) {
+        if (lane == 0) aside[at] = c0;
+        continue;
+      }
+    }
+    uint32_t heads = __ffs(ends);
+    if (ends == 0)                                                             // there was no room to put it aside
+      for (heads = 17; c0 + heads < chunks && a.through[c0 + heads]; ++heads) {}
+    float x[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = 0.f;
+    if (active) {
+      add_part<V>(a.partial + ((int64_t)2 * c0 + 1) * a.dim + col, x);
+#pragma unroll 8
+      for (uint32_t h = 1; h <= heads; ++h) add_part<V>(a.partial + (int64_t)2 * (c0 + h) * a.dim + col, x);
+    }
+    finish(c0, x);
+  }
+  __syncthreads();
+  const uint32_t long_runs = min(s_count, (uint32_t)kAside);
+  for (uint32_t r = 0; r < long_runs; ++r) {
+    const uint32_t c0 = aside[r];
+    uint32_t last = c0 + 1;                                                    // the last chunk that the run reaches
+    for (;; last += 32 * kJoinWarps) {
       if (threadIdx.x == 0) s_last = 0xffffffffu;
       __syncthreads();
       const uint32_t c = last + threadIdx.x;
@@ -479,24 +594,24 @@ __global__ void __launch_bounds__(256) run_join_kernel(const SumArgs a, uint32_t
         break;
       }
     }
-    const uint32_t id = a.sorted[(int64_t)(c0 + 1) * a.chunk].x;
-    for (int col = blockIdx.y * 32 + lane; col - lane < a.dim; col += gridDim.y * 32) {
-      float x = 0.f;
-      if (col < a.dim) {
-        if (warp == 0) x = a.partial[((int64_t)2 * c0 + 1) * a.dim + col];
-#pragma unroll 4
-        for (uint32_t c = c0 + 1 + warp; c <= last; c += 8) x += a.partial[(int64_t)2 * c * a.dim + col];
-      }
-      sum[warp][lane] = x;
-      __syncthreads();
-      if (warp == 0 && col < a.dim) {
-        float y = sum[0][lane];
+    float x[V];
 #pragma unroll
-        for (int w = 1; w < 8; ++w) y += sum[w][lane];
-        store_row(a.dtable, a.dtype, (int64_t)id * a.dim + col, y * a.scale);
-      }
-      __syncthreads();
+    for (int i = 0; i < V; ++i) x[i] = 0.f;
+    if (active) {
+      if (warp == 0) add_part<V>(a.partial + ((int64_t)2 * c0 + 1) * a.dim + col, x);
+#pragma unroll 8
+      for (uint32_t c = c0 + 1 + warp; c <= last; c += kJoinWarps) add_part<V>(a.partial + (int64_t)2 * c * a.dim + col, x);
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[warp][lane * V + i] = x[i];
+    __syncthreads();
+    if (warp == 0) {
+      for (int w = 1; w < kJoinWarps; ++w)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] += sum[w][lane * V + i];
+      finish(c0, x);
+    }
+    __syncthreads();
   }
 }
 
@@ -533,31 +648,57 @@ void gather_out(Chain& c, const GatherArgs& a, int out_dtype, int bits) {
 }
 
 template <typename T, int V>
-void sum_lanes(Chain& c, const SumArgs& a, uint32_t chunks) {
-  auto go = [&](auto kernel, int g) { c(kernel, dim3((chunks + 256 / g - 1) / (256 / g), (a.groups + g - 1) / g), dim3(256), 0, a); };
+uint32_t sum_lanes(Chain& c, SumArgs& a) {
+  uint32_t blocks = 0;
+  auto go = [&](auto kernel, int g) {
+    a.span = 256 / g * a.chunk;
+    blocks = (uint32_t)(((int64_t)a.n + a.span - 1) / a.span);
+    c(kernel, dim3(blocks, (a.groups + g - 1) / g), dim3(256), 0, a);
+  };
   if (a.groups <= 8) go(run_sum_kernel<T, V, 8>, 8);
   else if (a.groups <= 16) go(run_sum_kernel<T, V, 16>, 16);
   else go(run_sum_kernel<T, V, 32>, 32);
+  return blocks;
+}
+// The widest group of values that divides a row and that the gradient's address allows.
+template <typename T>
+int width_of(const void* dout, int dim) {
+  constexpr int W = 16 / (int)sizeof(T);
+  auto fits = [&](int v) { return dim % v == 0 && ((uintptr_t)dout & (v * sizeof(T) - 1)) == 0; };
+  return fits(W) ? W : fits(2) ? 2 : 1;
 }
 template <typename T>
-void sum_type(Chain& c, SumArgs a, uint32_t chunks) {
+uint32_t sum_type(Chain& c, SumArgs& a) {
   constexpr int W = 16 / (int)sizeof(T);
-  auto fits = [&](int v) { return a.dim % v == 0 && ((uintptr_t)a.dout & (v * sizeof(T) - 1)) == 0; };
-  const int v = fits(W) ? W : fits(2) ? 2 : 1;
+  const int v = width_of<T>(a.dout, a.dim);
   a.groups = a.dim / v;
-  if (v == W) sum_lanes<T, W>(c, a, chunks);
-  else if (v == 2) sum_lanes<T, 2>(c, a, chunks);
-  else sum_lanes<T, 1>(c, a, chunks);
+  return v == W ? sum_lanes<T, W>(c, a) : v == 2 ? sum_lanes<T, 2>(c, a) : sum_lanes<T, 1>(c, a);
+}
+template <typename T>
+void few_type(Chain& c, const FewArgs& a) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const int v = width_of<T>(a.dout, a.dim);
+  constexpr int kSmem = kFewWarps * 32 * 32 * 4;                               // 32 / v rows of 32 v columns per warp
+  auto go = [&](auto kernel) {
+    c.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    c(kernel, dim3((unsigned)((a.rows * v + 31) / 32), (a.dim + 32 * v - 1) / (32 * v)), dim3(32 * kFewWarps), kSmem, a);
+  };
+  if (v == W) go(few_sum_kernel<T, W>);
+  else if (v == 2) go(few_sum_kernel<T, 2>);
+  else go(few_sum_kernel<T, 1>);
 }
 
-// Ids per chunk: few enough that the chunks fill the device, and so many that a hub's run has few parts.
+// Ids per group of lanes: few enough that the groups fill the device.
 int chunk_of(int64_t n) { return n <= 1 << 16 ? 16 : n <= 1 << 18 ? 32 : n <= 1 << 19 ? 64 : 128; }
+
+// Whether every block of rows looks through all ids, or the ids are sorted: WHICH
+bool few(int64_t n, int64_t rows) { return n <= 8192 && rows > 0 && rows <= 16384; }
 
 struct Scratch {
   int64_t sorted[2], hist, through, list, counter, partial, bytes;
 };
 Scratch layout(int64_t n, int dim) {
-  const int64_t chunks = (n + chunk_of(n) - 1) / chunk_of(n);
+  const int64_t span = 8 * chunk_of(n), blocks = (n + span - 1) / span;       // of a thread block, at least (8 to 32 groups)
   Scratch s;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -566,12 +707,12 @@ Scratch layout(int64_t n, int dim) {
     return p;
   };
   s.sorted[0] = take(8 * n);
-  s.sorted[1] = n > kOneBlock ? take(8 * n) : s.sorted[0];
+  s.sorted[1] = take(8 * n);
   s.hist = take(4ll * kMaxSortBlocks * kDigits);
-  s.through = take(chunks);
-  s.list = take(4 * chunks);
+  s.through = take(blocks);
+  s.list = take(4 * blocks);
   s.counter = take(4);
-  s.partial = take(8ll * chunks * dim);
+  s.partial = take(8ll * blocks * dim);
   s.bytes = at;
   return s;
 }
@@ -613,7 +754,7 @@ extern "C" TGNN_API int tgnn_lookup(const void* table, int dtype, int64_t rows, 
 
 extern "C" TGNN_API int64_t tgnn_lookup_scratch(int64_t n, int64_t rows, int dim) {
   if (n < 0 || rows < 0 || n >= 0x7fffffff || rows >= 0x7fffffff || dim < 1 || dim > 8192) return -1;
-  return layout(n, dim).bytes;
+  return few(n, rows) ? 0 : layout(n, dim).bytes;
 }
 
 extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, int64_t n, const void* dout, int out_dtype, int64_t rows, int dim,
@@ -621,7 +762,7 @@ extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, in
                                              int64_t err_size) {
   const char* who = "tgnn_lookup_backward";
   if (int rc = check(who, rows, dim, index_bits, n, dtype, out_dtype, err, err_size)) return rc;
-  if ((rows > 0 && !dtable) || (n > 0 && (!ids || !dout || !scratch || !status))) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", who);
+  if ((rows > 0 && !dtable) || (n > 0 && (!ids || !dout || !status || (!scratch && !few(n, rows))))) return fail(err, err_size, TGNN_EINVAL, "%s: null pointer", who);
   if (((uintptr_t)dtable & (elem_bytes(dtype) - 1)) || ((uintptr_t)dout & (elem_bytes(out_dtype) - 1)) ||
       ((uintptr_t)ids & (index_bits / 8 - 1)) || ((uintptr_t)scratch & 255) || ((uintptr_t)status & 3))
     return fail(err, err_size, TGNN_EINVAL, "%s: a pointer is not aligned (scratch to 256 bytes, the others to their elements)", who);
@@ -631,47 +772,61 @@ extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, in
       return fail(err, err_size, TGNN_ECUDA, "%s: %s", who, cudaGetErrorString(cudaGetLastError()));
     return TGNN_OK;
   }
-  const Scratch l = layout(n, dim);
-  char* base = static_cast<char*>(scratch);
-  int key_bits = 1;
-  while ((rows >> key_bits) != 0) ++key_bits;
   SortArgs s = {};
   s.ids = ids;
   s.index_bits = index_bits;
   s.rows = rows;
   s.n = (uint32_t)n;
-  s.hist = reinterpret_cast<uint32_t*>(base + l.hist);
-  s.status = status;
-  s.counter = reinterpret_cast<uint32_t*>(base + l.counter);
   s.zero = static_cast<char*>(dtable);
   s.zero_bytes = bytes;
-  s.passes = (key_bits + 7) / 8;
-  s.width = (key_bits + s.passes - 1) / s.passes;
   const int sms = num_sms();
   const int fillers = (int)(bytes >> 14 >= 4 * sms ? 4 * sms : (bytes >> 14) + 1);
   Chain c(stream);
+  if (few(n, rows)) {
+    FewArgs f = {};
+    f.ids = ids;
+    f.dout = dout;
+    f.dtable = dtable;
+    f.status = status;
+    f.rows = rows;
+    f.index_bits = index_bits;
+    f.n = (int)n;
+    f.dim = dim;
+    f.dtype = dtype;
+    f.scale = scale;
+    if (out_dtype == TGNN_F32) few_type<float>(c, f);
+    else if (out_dtype == TGNN_BF16) few_type<__nv_bfloat16>(c, f);
+    else few_type<__half>(c, f);
+    return c.end(who, err, err_size);
+  }
+  const Scratch l = layout(n, dim);
+  char* base = static_cast<char*>(scratch);
+  int key_bits = 1;
+  while ((rows >> key_bits) != 0) ++key_bits;
+  s.hist = reinterpret_cast<uint32_t*>(base + l.hist);
+  s.status = status;
+  s.counter = reinterpret_cast<uint32_t*>(base + l.counter);
+  const int passes = (key_bits + 7) / 8;
+  s.width = (key_bits + passes - 1) / passes;
+  const int64_t tiles = (n + kSortThreads - 1) / kSortThreads;                 // few ids: a key per thread, so that a block's work is short
+  s.sort_blocks = (int)(tiles < kMaxSortBlocks ? tiles : kMaxSortBlocks);
+  s.per_block = (uint32_t)((n + s.sort_blocks - 1) / s.sort_blocks);
+  s.shares = 2 * passes;
   int sorted = 0;
-  if (n <= kOneBlock) {
-    c.e = cudaFuncSetAttribute(sort_one_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(OneBlock));
-    s.out = reinterpret_cast<uint2*>(base + l.sorted[0]);
-    s.shares = 1;
-    c(sort_one_kernel, dim3(1 + fillers), dim3(kSortThreads), sizeof(OneBlock), s);
-  } else {
-    const int64_t tiles = (n + kTile - 1) / kTile;
-    s.sort_blocks = (int)(tiles < kMaxSortBlocks ? tiles : kMaxSortBlocks);
-    s.per_block = (uint32_t)((n + s.sort_blocks - 1) / s.sort_blocks);
-    s.shares = 2 * s.passes;
-    for (int p = 0; p < s.passes; ++p) {
-      s.shift = p * s.width;
-      s.in = p ? reinterpret_cast<uint2*>(base + l.sorted[sorted]) : nullptr;
-      sorted = p & 1;
-      s.out = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
-      s.share = 2 * p;
-      c(sort_count_kernel, dim3(s.sort_blocks + fillers), dim3(kSortThreads), 0, s);
-      s.share = 2 * p + 1;
-      s.status = nullptr;
-      c(sort_move_kernel, dim3(s.sort_blocks + fillers), dim3(kSortThreads), 0, s);
-    }
+  for (int p = 0; p < passes; ++p) {
+    s.shift = p * s.width;
+    s.in = p ? reinterpret_cast<uint2*>(base + l.sorted[sorted]) : nullptr;
+    sorted = p & 1;
+    s.out = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
+    s.share = 2 * p;
+    const dim3 grid(s.sort_blocks + fillers), block(kSortThreads);
+    c(sort_count_kernel, grid, block, 0, s);
+    s.share = 2 * p + 1;
+    s.status = nullptr;
+    if (s.per_block <= 1024) c(sort_move_kernel<1>, grid, block, 0, s);
+    else if (s.per_block <= 2048) c(sort_move_kernel<2>, grid, block, 0, s);
+    else if (s.per_block <= 4096) c(sort_move_kernel<4>, grid, block, 0, s);
+    else c(sort_move_kernel<8>, grid, block, 0, s);
   }
   SumArgs a = {};
   a.sorted = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
@@ -687,13 +842,15 @@ extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, in
   a.dim = dim;
   a.chunk = chunk_of(n);
   a.scale = scale;
-  const uint32_t chunks = (uint32_t)((n + a.chunk - 1) / a.chunk);
-  if (out_dtype == TGNN_F32) sum_type<float>(c, a, chunks);
-  else if (out_dtype == TGNN_BF16) sum_type<__nv_bfloat16>(c, a, chunks);
-  else sum_type<__half>(c, a, chunks);
-  if (chunks > 1) {
-    const unsigned y = (unsigned)(dim + 31) / 32, x = (unsigned)(8 * sms) / (y < 8 ? y : 8);
-    c(run_join_kernel, dim3(chunks < x ? chunks : x, y), dim3(256), 0, a, chunks);
+  const uint32_t blocks = out_dtype == TGNN_F32 ? sum_type<float>(c, a) : out_dtype == TGNN_BF16 ? sum_type<__nv_bfloat16>(c, a) : sum_type<__half>(c, a);
+  if (blocks > 1) {
+    // four columns per lane where rows allow it; a run per warp at most while the device has room, so that no block is left with many hubs
+    const int v = dim % 4 == 0 ? 4 : dim % 2 == 0 ? 2 : 1;
+    const unsigned y = (unsigned)(dim + 32 * v - 1) / (32 * v), most = (unsigned)(4 * sms), want = (blocks + kJoinWarps - 1) / kJoinWarps;
+    const dim3 grid(want < most ? want : most, y), block(32 * kJoinWarps);
+    if (v == 4) c(run_join_kernel<4>, grid, block, 0, a, blocks);
+    else if (v == 2) c(run_join_kernel<2>, grid, block, 0, a, blocks);
+    else c(run_join_kernel<1>, grid, block, 0, a, blocks);
   }
   return c.end(who, err, err_size);
 }

@@ -70,7 +70,7 @@ def test_against_64_bits(dtype, out_dtype, rows, dim, n):
     assert int(status.item()) == 0
 
 
-@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 1023, 1024, 1025, 12_287, 12_288, 12_289, 65_537, 300_001, 1_200_000])
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 31, 1023, 1024, 1025, 8191, 8192, 8193, 65_537, 300_001, 1_200_000])
 @pytest.mark.parametrize("kind", ["one", "ascending", "random", "unused"])
 def test_lengths_and_orders(n, kind):
     rows, dim = 513, 8
