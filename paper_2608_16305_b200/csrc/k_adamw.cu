@@ -12,6 +12,8 @@
 // A warp takes 256 values at a time, eight per lane as two groups of four, which are 16-byte words of fp32 and 4-byte words of codes.
 // Tensors are described in the kernel's parameters: nothing is copied to the device ahead of the launch, and a captured graph
 // keeps them.  Bound by bytes: 28 per value with fp32 gradients and moments, 16 with moments in 8 bits.
+#include <type_traits>
+
 #include "tgnn_table.cuh"
 
 using namespace tgnn_table;
@@ -62,9 +64,10 @@ __device__ __forceinline__ double one_minus_power(double b, int64_t t) {
   return 1.0 - r;
 }
 
+// Four values (codes) from place `at` of a thread block's n on: words where `whole` says that all of them are there and aligned.
 template <typename T>
-__device__ __forceinline__ void load4(const T* p, int64_t at, int64_t n, bool wide, float* x) {
-  if (wide && at + 4 <= n) {
+__device__ __forceinline__ void load4(const T* p, int at, int n, bool whole, float* x) {
+  if (whole) {
     reinterpret_cast<const Group<T, 4>*>(p + at)->get(x);
   } else {
 #pragma unroll
@@ -72,8 +75,8 @@ __device__ __forceinline__ void load4(const T* p, int64_t at, int64_t n, bool wi
   }
 }
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int64_t at, int64_t n, bool wide, const float* x) {
-  if (wide && at + 4 <= n) {
+__device__ __forceinline__ void store4(T* p, int at, int n, bool whole, const float* x) {
+  if (whole) {
     Group<T, 4> g;
     g.set(x);
     *reinterpret_cast<Group<T, 4>*>(p + at) = g;
@@ -83,28 +86,36 @@ __device__ __forceinline__ void store4(T* p, int64_t at, int64_t n, bool wide, c
       if (at + i < n) p[at + i] = tgnn_history::from_float<T>(x[i]);
   }
 }
-__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int64_t at, int64_t n, bool wide) {
-  if (wide && at + 4 <= n) return *reinterpret_cast<const uint32_t*>(p + at);
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int at, int n, bool whole) {
+  if (whole) return *reinterpret_cast<const uint32_t*>(p + at);
   uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (at + i < n) w |= (uint32_t)p[at + i] << (8 * i);
   return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, int64_t at, int64_t n, bool wide, uint32_t w) {
-  if (wide && at + 4 <= n) *reinterpret_cast<uint32_t*>(p + at) = w;
+__device__ __forceinline__ void store_codes(uint8_t* p, int at, int n, bool whole, uint32_t w) {
+  if (whole) *reinterpret_cast<uint32_t*>(p + at) = w;
   else
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (at + i < n) p[at + i] = (uint8_t)(w >> (8 * i));
 }
-__device__ __forceinline__ float signed_square(uint32_t byte, float scale) {
-  const float c = (float)(int8_t)byte;
+// Conversions by bits: a byte under the exponent of 2^23 is a number behind it, and a sum with 2^23 (1.5 * 2^23 for signs) has its integer in the low
+// bits.  The conversion instructions share the 16 lanes a cycle of the special functions: 8 of them per value would take longer than the memory.
+__device__ __forceinline__ float byte_of(uint32_t w, int i) { return __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440u | i)); }   // + 2^23
+__device__ __forceinline__ float signed_square(uint32_t codes_plus_128, int i, float scale) {
+  const float c = byte_of(codes_plus_128, i) - 8388736.f;
   return __fmul_rn(c * fabsf(c), scale);      // squares up to 16129 are exact
 }
-__device__ __forceinline__ float square(uint32_t byte, float scale) {
-  const float c = (float)(byte & 255u);
+__device__ __forceinline__ float square(uint32_t codes, int i, float scale) {
+  const float c = byte_of(codes, i) - 8388608.f;
   return __fmul_rn(c * c, scale);
+}
+// Low bytes of four numbers.
+__device__ __forceinline__ uint32_t low_bytes(const float* x) {
+  const uint32_t a = __byte_perm(__float_as_uint(x[0]), __float_as_uint(x[1]), 0x0040), b = __byte_perm(__float_as_uint(x[2]), __float_as_uint(x[3]), 0x0040);
+  return __byte_perm(a, b, 0x5410);
 }
 
 // Scale of a block whose largest magnitude (as bits, so that NaN stays on top) is `top`, and its reciprocal.
@@ -122,15 +133,15 @@ __device__ __forceinline__ float code_of(float x, float back, float a, float mos
   const float y = __fmul_rn(fabsf(x), back);
   float r;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(y));
-  float c = floorf(r);                        // within one of the root's floor; made exact here (squares are exact)
-  if (c * c > y) c -= 1.f;
-  if ((c + 1.f) * (c + 1.f) <= y) c += 1.f;
-  c = fminf(c, most);
-  if (y - c * c > __fmul_rn(a, 2.f * c + 1.f) && c < most) c += 1.f;          // the difference is exact too
-  return c;
+  float c = (r + 8388608.f) - 8388608.f;      // the nearest integer: the root's floor or one more (the root is off by 2^-23 of it at most)
+  if (c * c > y) c -= 1.f;                    // squares are exact
+  if (y - c * c > __fmul_rn(a, 2.f * c + 1.f)) c += 1.f;                       // the difference is exact too
+  return fminf(c, most);
 }
 __device__ __forceinline__ uint32_t warp_max(uint32_t x) { return __reduce_max_sync(FULL, x); }
-__device__ __forceinline__ float chance(uint32_t bits16) { return __fmul_rn((float)bits16 + 0.5f, 1.f / 65536.f); }
+// (h + 0.5) / 65536 of the low or the high 16 bits: 1 + h / 65536 by bits, less 1 - 2^-17; exact.
+__device__ __forceinline__ float chance_low(uint32_t w) { return __uint_as_float(0x3f800000u | ((w << 7) & 0x7fff80u)) - 0.99999237060546875f; }
+__device__ __forceinline__ float chance_high(uint32_t w) { return __uint_as_float(0x3f800000u | ((w >> 9) & 0x7fff80u)) - 0.99999237060546875f; }
 
 template <int BITS, int MAX>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ Many<MAX> a) {
@@ -158,42 +169,48 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
   }
   const One& o = a.t[lo];
   const int64_t begin = (int64_t)(blockIdx.x - (lo ? a.end[lo - 1] : 0)) * a.per_chunk;
-  const int64_t n = o.n, stop = min(n, begin + a.per_chunk);
+  const int n = (int)min(o.n - begin, (int64_t)a.per_chunk);        // of this block, from `begin` on
   const bool wide = o.wide;
+  float* const op = o.p + begin;
+  const int g_size = o.g_dtype == TGNN_F32 ? 4 : 2, state_size = BITS / 8;
+  const char* const og = static_cast<const char*>(o.g) + begin * g_size;
+  char *const om = static_cast<char*>(o.m) + begin * state_size, *const ov = static_cast<char*>(o.v) + begin * state_size;
+  char* const oc = o.copy ? static_cast<char*>(o.copy) + begin * 2 : nullptr;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   __syncthreads();
   const float c1 = s_c1, c2 = s_c2, eps = (float)a.eps;
   const uint64_t salt = s_salt;
-  for (int64_t at0 = begin + warp * kBlock; at0 < stop; at0 += (kThreads / 32) * kBlock) {
+  auto values = [&](const int at0, auto whole_) {
+    constexpr bool whole = decltype(whole_)::value;
     float p[8], g[8], m[8], v[8];
-    const int64_t at[2] = {at0 + 4 * lane, at0 + 128 + 4 * lane};
+    const int at[2] = {at0 + 4 * lane, at0 + 128 + 4 * lane};
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      load4(o.p, at[h], n, wide, p + 4 * h);
-      if (o.g_dtype == TGNN_F32) load4(static_cast<const float*>(o.g), at[h], n, wide, g + 4 * h);
-      else if (o.g_dtype == TGNN_BF16) load4(static_cast<const __nv_bfloat16*>(o.g), at[h], n, wide, g + 4 * h);
-      else load4(static_cast<const __half*>(o.g), at[h], n, wide, g + 4 * h);
+      load4(op, at[h], n, whole, p + 4 * h);
+      if (o.g_dtype == TGNN_F32) load4(reinterpret_cast<const float*>(og), at[h], n, whole, g + 4 * h);
+      else if (o.g_dtype == TGNN_BF16) load4(reinterpret_cast<const __nv_bfloat16*>(og), at[h], n, whole, g + 4 * h);
+      else load4(reinterpret_cast<const __half*>(og), at[h], n, whole, g + 4 * h);
     }
-    const int64_t block = at0 / kBlock;
+    const int64_t block = (begin + at0) / kBlock;
     if (BITS == 8) {
       uint32_t wm[2], wv[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        wm[h] = load_codes(static_cast<const uint8_t*>(o.m), at[h], n, wide);
-        wv[h] = load_codes(static_cast<const uint8_t*>(o.v), at[h], n, wide);
+        wm[h] = load_codes(reinterpret_cast<const uint8_t*>(om), at[h], n, whole);
+        wv[h] = load_codes(reinterpret_cast<const uint8_t*>(ov), at[h], n, whole);
       }
       const float sm = o.m_scale[block], sv = o.v_scale[block];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        m[i] = signed_square(wm[i >> 2] >> (8 * (i & 3)), sm);
-        const float u = square(wv[i >> 2] >> (8 * (i & 3)), sv);
+        m[i] = signed_square(wm[i >> 2] ^ 0x80808080u, i & 3, sm);
+        const float u = square(wv[i >> 2], i & 3, sv);
         v[i] = __fmul_rn(u, u);
       }
     } else {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        load4(static_cast<const float*>(o.m), at[h], n, wide, m + 4 * h);
-        load4(static_cast<const float*>(o.v), at[h], n, wide, v + 4 * h);
+        load4(reinterpret_cast<const float*>(om), at[h], n, whole, m + 4 * h);
+        load4(reinterpret_cast<const float*>(ov), at[h], n, whole, v + 4 * h);
       }
     }
     float u[8];
@@ -204,14 +221,14 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
       v[i] = __fadd_rn(__fmul_rn(v[i], a.b2f), __fmul_rn(__fmul_rn(x, a.n2), x));
       u[i] = __fsqrt_rn(v[i]);
       // 1 - lr decay would round to fp32: the change is formed and taken off instead
-      p[i] -= a.lr * fmaf(o.decay, p[i], __fdividef(m[i] * c1, fmaf(u[i], c2, eps)));
+      p[i] -= a.lr * fmaf(o.decay, p[i], m[i] * c1 * tgnn_history::rcp_fast(fmaf(u[i], c2, eps)));
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      store4(o.p, at[h], n, wide, p + 4 * h);
-      if (o.copy) {
-        if (o.copy_dtype == TGNN_BF16) store4(static_cast<__nv_bfloat16*>(o.copy), at[h], n, wide, p + 4 * h);
-        else store4(static_cast<__half*>(o.copy), at[h], n, wide, p + 4 * h);
+      store4(op, at[h], n, whole, p + 4 * h);
+      if (oc) {
+        if (o.copy_dtype == TGNN_BF16) store4(reinterpret_cast<__nv_bfloat16*>(oc), at[h], n, whole, p + 4 * h);
+        else store4(reinterpret_cast<__half*>(oc), at[h], n, whole, p + 4 * h);
       }
     }
     if (BITS == 8) {
@@ -227,34 +244,39 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
         o.m_scale[block] = sm;
         o.v_scale[block] = su;
       }
+      constexpr uint64_t kPair = 0xC2B2AE3D27D4EB4Full;
+      const uint64_t pair = (((uint64_t)(a.first + lo) << 40) + (uint64_t)((begin + at[0]) >> 1)) * kPair;     // those that follow are sums
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint32_t wm = 0, wv = 0;
+        float cm[4], cu[4];
 #pragma unroll
         for (int j = 0; j < 4; j += 2) {
-          const uint64_t pair = ((uint64_t)(a.first + lo) << 40) + (uint64_t)((at[h] + j) >> 1);
-          const uint64_t r = mix(salt ^ (pair * 0xC2B2AE3D27D4EB4Full));
+          const uint64_t r = mix(salt ^ (pair + (uint64_t)(64 * h + j / 2) * kPair));
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int i = 4 * h + j + e;
             const uint32_t w = (uint32_t)(r >> (32 * e));
-            const float cm = code_of(m[i], bm, chance(w & 0xffffu), 127.f);
-            float cu = code_of(u[i], bu, chance(w >> 16), 255.f);
-            if (cu == 0.f && u[i] > 0.f && bu > 0.f) cu = 1.f;
-            wm |= ((uint32_t)(int)copysignf(cm, m[i]) & 255u) << (8 * (j + e));
-            wv |= (uint32_t)cu << (8 * (j + e));
+            cm[j + e] = copysignf(code_of(m[i], bm, chance_low(w), 127.f), m[i]) + 12582912.f;
+            float c = code_of(u[i], bu, chance_high(w), 255.f);
+            if (c == 0.f && u[i] > 0.f && bu > 0.f) c = 1.f;
+            cu[j + e] = c + 8388608.f;
           }
         }
-        store_codes(static_cast<uint8_t*>(o.m), at[h], n, wide, wm);
-        store_codes(static_cast<uint8_t*>(o.v), at[h], n, wide, wv);
+        const uint32_t wm = low_bytes(cm), wv = low_bytes(cu);
+        store_codes(reinterpret_cast<uint8_t*>(om), at[h], n, whole, wm);
+        store_codes(reinterpret_cast<uint8_t*>(ov), at[h], n, whole, wv);
       }
     } else {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        store4(static_cast<float*>(o.m), at[h], n, wide, m + 4 * h);
-        store4(static_cast<float*>(o.v), at[h], n, wide, v + 4 * h);
+        store4(reinterpret_cast<float*>(om), at[h], n, whole, m + 4 * h);
+        store4(reinterpret_cast<float*>(ov), at[h], n, whole, v + 4 * h);
       }
     }
+  };
+  for (int at0 = warp * kBlock; at0 < n; at0 += (kThreads / 32) * kBlock) {
+    if (wide && at0 + kBlock <= n) values(at0, std::true_type());
+    else values(at0, std::false_type());
   }
 }
 
@@ -269,20 +291,22 @@ __global__ void __launch_bounds__(kThreads) moments_kernel(const __grid_constant
   }
   const One& o = a.t[lo];
   const int64_t begin = (int64_t)(blockIdx.x - (lo ? a.end[lo - 1] : 0)) * a.per_chunk;
-  const int64_t n = o.n, stop = min(n, begin + a.per_chunk);
-  const bool wide = o.wide;
-  for (int64_t at = begin + 4 * threadIdx.x; at < stop; at += 4 * kThreads) {
-    const uint32_t wm = load_codes(static_cast<const uint8_t*>(o.m), at, n, wide), wv = load_codes(static_cast<const uint8_t*>(o.v), at, n, wide);
-    const float sm = o.m_scale[at / kBlock], sv = o.v_scale[at / kBlock];
+  const int n = (int)min(o.n - begin, (int64_t)a.per_chunk);
+  const uint8_t *om = static_cast<const uint8_t*>(o.m) + begin, *ov = static_cast<const uint8_t*>(o.v) + begin;
+  for (int at = 4 * threadIdx.x; at < n; at += 4 * kThreads) {
+    const bool whole = o.wide && at + 4 <= n;
+    const uint32_t wm = load_codes(om, at, n, whole), wv = load_codes(ov, at, n, whole);
+    const int64_t block = (begin + at) / kBlock;
+    const float sm = o.m_scale[block], sv = o.v_scale[block];
     float m[4], v[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      m[i] = signed_square(wm >> (8 * i), sm);
-      const float u = square(wv >> (8 * i), sv);
+      m[i] = signed_square(wm ^ 0x80808080u, i, sm);
+      const float u = square(wv, i, sv);
       v[i] = __fmul_rn(u, u);
     }
-    store4(o.p, at, n, wide, m);
-    store4(static_cast<float*>(o.copy), at, n, wide, v);
+    store4(o.p + begin, at, n, whole, m);
+    store4(static_cast<float*>(o.copy) + begin, at, n, whole, v);
   }
 }
 

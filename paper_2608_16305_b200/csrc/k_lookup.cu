@@ -6,6 +6,8 @@
 // lanes; what runs have in neighboring chunks is added up within a thread block, in order, and a run across blocks leaves one partial sum per block, which a
 // last kernel adds in order.  Rows that no id names are zeros: the blocks beside the sorting ones write them while the sort, which waits on latency, runs.
 // Few ids over few rows are not sorted: the blocks, each with some rows of the table, look through all of them.
+#include <type_traits>
+
 #include "tgnn_table.cuh"
 
 using namespace tgnn_table;
@@ -34,44 +36,40 @@ __global__ void __launch_bounds__(256) lookup_kernel(const GatherArgs a) {
   const int64_t r0 = (int64_t)blockIdx.x * a.rows_per_block;
   const int count = (int)min((int64_t)a.rows_per_block, a.n - r0) * a.groups;
   const I* ids = static_cast<const I*>(a.ids) + r0;
-  const TT* table = static_cast<const TT*>(a.table);
   TO* out = static_cast<TO*>(a.out) + r0 * a.dim;
+  const char* const base = static_cast<const char*>(a.table);
+  const uint32_t row_bytes = (uint32_t)a.dim * (uint32_t)sizeof(TT);
+  typedef typename std::make_unsigned<I>::type Unsigned;
   constexpr int U = 4;
   for (int x0 = threadIdx.x; x0 < count; x0 += 256 * U) {
-    int row[U];
-    int64_t id[U];
+    uint32_t at[U];                                                            // byte in the row
+    I id[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int x = x0 + 256 * u;
-      row[u] = a.magic ? (int)__umulhi((uint32_t)x, a.magic) : x;
-      id[u] = x < count ? (int64_t)ids[row[u]] : -1;
+      const uint32_t x = x0 + 256 * u, row = a.magic ? __umulhi(x, a.magic) : x;
+      at[u] = (x - row * a.groups) * (V * (uint32_t)sizeof(TT));
+      id[u] = x < (uint32_t)count ? ids[row] : (I)-1;
     }
     Group<TT, V> v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int x = x0 + 256 * u;
-      if (id[u] >= 0 && id[u] < a.rows)
-        v[u] = *reinterpret_cast<const Group<TT, V>*>(table + id[u] * a.dim + (x - row[u] * a.groups) * V);
-      else if (id[u] >= a.rows) {
-        *a.status = 4;
-        id[u] = -1;
-      }
-    }
+    for (int u = 0; u < U; ++u)
+      if ((Unsigned)id[u] < (Unsigned)a.rows) v[u] = *reinterpret_cast<const Group<TT, V>*>(base + (uint64_t)id[u] * row_bytes + at[u]);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int x = x0 + 256 * u;
       if (x >= count) break;
       float f[V];
-      if (id[u] >= 0) {
+      if ((Unsigned)id[u] < (Unsigned)a.rows) {
         v[u].get(f);
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] *= a.scale;
       } else {
+        if (id[u] >= 0) *a.status = 4;
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = 0.f;
       }
-      TO* p = out + (int64_t)x * V;
-      constexpr int W = V * sizeof(TO) > 16 ? 16 / (int)sizeof(TO) : V;      // values per store
+      TO* p = out + (uint32_t)x * V;
+      constexpr int W = V * sizeof(TO) > 16 ? 16 / (int)sizeof(TO) : V;        // values per store
 #pragma unroll
       for (int i = 0; i < V; i += W) {
         Group<TO, W> g;
@@ -689,7 +687,7 @@ void few_type(Chain& c, const FewArgs& a) {
 }
 
 // Ids per group of lanes: few enough that the groups fill the device.
-int chunk_of(int64_t n) { return n <= 1 << 16 ? 16 : n <= 1 << 18 ? 32 : n <= 1 << 19 ? 64 : 128; }
+int chunk_of(int64_t n) { return n <= 1 << 16 ? 16 : n <= 1 << 18 ? 32 : n <= 1 << 21 ? 64 : 128; }
 
 // Whether every block of rows looks through all ids, or the ids are sorted: WHICH
 bool few(int64_t n, int64_t rows) { return n <= 8192 && rows > 0 && rows <= 16384; }
