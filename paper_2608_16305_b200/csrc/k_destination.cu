@@ -68,6 +68,7 @@ struct Prep {
   int32_t* count;                            // [0]: roots that take part
   int32_t* act;                              // their indices
   float* parts;                              // largest magnitudes of [q, table, dloss] and the largest bias, [4][kMaxParts]
+  int parts_used;
   uint16_t* qp;
   uint16_t* tp;
   float* cols;                               // what a tile's columns need, tile by tile
@@ -93,23 +94,21 @@ __device__ __forceinline__ float unit_of(float top) {
   frexpf(fminf(top, 3e38f), &e);
   return ldexpf(1.f, max(-110, min(110, 14 - e)));
 }
-__device__ __forceinline__ float largest(const float* parts, float* s_red) {  // of kMaxParts values, by the whole block
-  float x = 0.f;
-  for (int i = threadIdx.x; i < kMaxParts; i += blockDim.x) x = fmaxf(x, parts[i]);
+// The largest of the partial maxima `which`, by a warp.
+__device__ __forceinline__ float largest(const float* parts, int used, int which) {
+  float x = -INFINITY;
+  for (int i = threadIdx.x & 31; i < used; i += 32) x = fmaxf(x, parts[which * kMaxParts + i]);
+#pragma unroll
   for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) s_red[threadIdx.x >> 5] = x;
-  __syncthreads();
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) x = fmaxf(x, s_red[w]);
   return x;
 }
 
-// Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows and the largest bias.
+// Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows and the largest bias, and form dq.
 __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
   chain_wait();
   chain_release();
   __shared__ int s_sum[32];
-  __shared__ float s_red[32];
+  __shared__ float s_red[4][32];
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   if (blockIdx.x > 0) {
     const int b = blockIdx.x - 1, nb = gridDim.x - 1;
@@ -125,21 +124,34 @@ __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
       for (int c = lane; c < a.s.dim; c += 32) top[0] = fmaxf(top[0], fabsf(static_cast<const float*>(a.q)[r * a.s.dim + c]));
       if (a.backward) top[2] = fmaxf(top[2], fabsf(a.dloss[r]));
     }
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
-      float x = top[k];
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], o));
+      if (lane == 0) s_red[k][warp] = top[k];
+    }
+    __syncthreads();
+    if (warp < 4) {
+      float x = s_red[warp][lane];
       for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
-      __syncthreads();
-      if (lane == 0) s_red[warp] = x;
-      __syncthreads();
-      if (warp == 0) {
-        x = s_red[lane];
-        for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
-        if (lane == 0) a.parts[k * kMaxParts + b] = x;
+      if (lane == 0) a.parts[warp * kMaxParts + b] = x;
+    }
+    if (a.dq) {                                          // dq_i = g_i scale (what the forward pass kept)
+      for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n; r += (int64_t)nb * 32) {
+        const int64_t y = target_of(a, r);
+        const bool in = y >= 0 && y < a.s.rows;
+        const float g = in ? a.dloss[r] * a.scale : 0.f;
+        for (int c = lane; c < a.s.dim; c += 32) {
+          const int64_t x = r * a.s.dim + c;
+          const float v = in ? g * a.kept[3 * a.s.n + x] : 0.f;
+          if (a.dtype == TGNN_F32) static_cast<float*>(a.dq)[x] = v;
+          else static_cast<__nv_bfloat16*>(a.dq)[x] = __float2bfloat16_rn(v);
+        }
       }
-      for (int i = b + nb * (1 + t); i < kMaxParts; i += nb * 1024) a.parts[k * kMaxParts + i] = k == 3 ? -INFINITY : 0.f;
     }
     return;
   }
+  if (!a.count) return;                                  // dq alone is wanted
   int done = 0;
   constexpr int K = 4;
   for (int64_t base = 0; base < a.s.n; base += 1024 * K) {
@@ -185,16 +197,15 @@ __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
 __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
   chain_wait();
   chain_release();
-  __shared__ float s_red[8];
   const int t = threadIdx.x, lane = t & 31;
   const int64_t worker = (int64_t)blockIdx.x * 8 + (t >> 5), workers = (int64_t)gridDim.x * 8;
   const int64_t live = a.count[0], padded = up(live, 128);
   const bool split = a.s.planes == 2;
   float uq = 1.f, ut = 1.f, ug = 1.f;
   if (split) {
-    uq = unit_of(largest(a.parts, s_red));
-    ut = unit_of(largest(a.parts + kMaxParts, s_red));
-    if (a.backward) ug = 2.f * unit_of(largest(a.parts + 2 * kMaxParts, s_red));   // |g| up to 2^15
+    uq = unit_of(largest(a.parts, a.parts_used, 0));
+    ut = unit_of(largest(a.parts, a.parts_used, 1));
+    if (a.backward) ug = 2.f * unit_of(largest(a.parts, a.parts_used, 2));         // |g| up to 2^15
   }
   const int dp = a.s.dp, dim = a.s.dim;
   auto operand = [&](const void* src, int64_t row, uint16_t* to, float unit) {     // a row, 2 values at a time
@@ -238,19 +249,6 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
   }
 }
 
-// dq_i = g_i scale (what the forward pass kept).
-__global__ void __launch_bounds__(256) dq_kernel(const Prep a) {
-  chain_wait();
-  chain_release();
-  const int64_t values = a.s.n * a.s.dim;
-  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < values; x += (int64_t)gridDim.x * 256) {
-    const int64_t i = x / a.s.dim, y = target_of(a, i);
-    const float v = y >= 0 && y < a.s.rows ? a.dloss[i] * a.scale * a.kept[3 * a.s.n + x] : 0.f;
-    if (a.dtype == TGNN_F32) static_cast<float*>(a.dq)[x] = v;
-    else static_cast<__nv_bfloat16*>(a.dq)[x] = __float2bfloat16_rn(v);
-  }
-}
-
 // -------------------------------------------------------------------------------------------------- the main kernel --
 struct Main {
   CUtensorMap a_map, t_map;
@@ -258,6 +256,7 @@ struct Main {
   const int32_t* count;
   const int32_t* act;
   const float* parts;
+  int parts_used;
   const float* cols;
   const void* target;
   int index_bits;
@@ -620,22 +619,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     const int pitch = pitch_of(g.s);
     float uq = 1.f, ut = 1.f, ug = 1.f;
     if (PL == 2) {
-      float top[3] = {0.f, 0.f, 0.f};
-      for (int k = 0; k < (MODE == BACKWARD ? 3 : 2); ++k) {
-        for (int i = lane; i < kMaxParts; i += 32) top[k] = fmaxf(top[k], g.parts[k * kMaxParts + i]);
-        for (int x = 16; x; x >>= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], x));
-      }
-      uq = unit_of(top[0]);
-      ut = unit_of(top[1]);
-      if (MODE == BACKWARD) ug = 2.f * unit_of(top[2]);
+      uq = unit_of(largest(g.parts, g.parts_used, 0));
+      ut = unit_of(largest(g.parts, g.parts_used, 1));
+      if (MODE == BACKWARD) ug = 2.f * unit_of(largest(g.parts, g.parts_used, 2));
     }
-    float most_bias = 0.f;
-    if (MODE != BACKWARD && !MOVING && g.bias) {
-      float top = -INFINITY;
-      for (int i = lane; i < kMaxParts; i += 32) top = fmaxf(top, g.parts[3 * kMaxParts + i]);
-      for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, x));
-      most_bias = bias2(top);
-    }
+    const float most_bias = MODE != BACKWARD && !MOVING && g.bias ? bias2(largest(g.parts, g.parts_used, 3)) : 0.f;
     const float factor = g.scale * kLog2e / uq / ut;
     const f32x2 factor2 = pack2(factor, factor);
     const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
@@ -985,6 +973,7 @@ struct Join {
   const int32_t* count;
   const int32_t* act;
   const float* parts;
+  int parts_used;
   const float* slots;
   const float* full;
   const void* q;
@@ -1045,41 +1034,158 @@ __device__ __forceinline__ void put_four(void* base, int dtype, int64_t row, int
   }
 }
 
-// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn, four columns per lane; then loss, m, 1 / l, 1 - p and the
-// direction of dq.
+// What a root's sums make: loss, m, 1 / l, 1 - p and the direction of dq.  L counts in units of 2^shift beside M, o in units of 2^shift and `unit`; own: the
+// target's row.  By a warp, four columns per lane and half.
+__device__ __forceinline__ void finish_root(const Join& a, int i, float M, float L, float zt, float shift, float unit, const float4 (&o)[2],
+                                            const float4 (&own)[2]) {
+  const int lane = threadIdx.x & 31, dim = a.s.dim;
+  const float d = (M - zt) + (log2f(L) - shift);          // log2 of the others' weight over the target's
+  const bool none = L == 0.f, lost = zt == -INFINITY;
+  float loss, miss, mm, inv;
+  if (none) {                                             // no other node in sight
+    loss = lost ? INFINITY : zt - zt;
+    miss = 0.f;
+    mm = lost ? INFINITY : zt;                            // weights of 0 where nothing is in sight
+    inv = lost ? 0.f : 1.f;
+  } else if (lost) {
+    loss = INFINITY;
+    miss = 1.f;
+    mm = M;
+    inv = exp2f(shift) / L;
+  } else {
+    const float small = exp2f(-fabsf(d));                 // the smaller side over the larger
+    loss = kLn2 * fmaxf(d, 0.f) + log1pf(small);
+    miss = (d > 0.f ? 1.f : small) / (1.f + small);
+    mm = fmaxf(M, zt);
+    inv = 1.f / (exp2f(zt - mm) + L * exp2f((M - mm) - shift));
+  }
+  if (d != d && !none && !lost) loss = miss = mm = d;     // NaN stays
+  if (lane == 0) {
+    a.loss[i] = loss;
+    if (a.kept) {
+      a.kept[i] = mm;
+      a.kept[a.s.n + i] = inv;
+      a.kept[2 * a.s.n + i] = miss;
+    }
+  }
+  if (!a.kept) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int c = 128 * h + 4 * lane;
+    if (c >= dim) break;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!none) {
+      v.x = (o[h].x / L / unit - own[h].x) * miss;
+      v.y = (o[h].y / L / unit - own[h].y) * miss;
+      v.z = (o[h].z / L / unit - own[h].z) * miss;
+      v.w = (o[h].w / L / unit - own[h].w) * miss;
+    }
+    put_four(a.kept + 3 * a.s.n, TGNN_F32, i, dim, c, v);
+  }
+}
+
 template <int W>
-__global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
+struct RootParts {                                        // of the warps that share a root
+  float m[W], l[W], z[W];
+  float4 o[W][64];
+};
+
+// A root with a weight that has passed what fp32 holds (or a value that is no number): again, product by product, 32 nodes at a time per warp.
+template <int W>
+__device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, int64_t y) {
+  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, dim = a.s.dim;
+  float M = -INFINITY, l = 0.f, zt = 0.f;
+  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}, own[2];
+  const float factor = a.scale * kLog2e;
+  for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
+    const int64_t j = j0 + lane;
+    float x = -INFINITY;
+    if (j < a.s.rows) {
+      float dot = 0.f;
+      for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c), value_of(a.table, a.dtype, j * dim + c), dot);
+      x = fmaf(dot, factor, a.bias ? bias2(a.bias[j]) : 0.f);
+      if (j == y) {
+        zt = x;
+        x = -INFINITY;
+      }
+    }
+    float top = x;
+    for (int e = 16; e; e >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, e));
+    const float now = fmaxf(M, top), ref = now == -INFINITY ? 0.f : now, f = exp2f(M - ref), p = exp2f(x - ref);
+    M = now;
+    l = l * f + p;
+    for (int k = 0; k < 8; ++k) (&o[0].x)[k] *= f;
+    for (int e = 0; e < 32 && j0 + e < a.s.rows && a.kept; ++e) {
+      const float pe = __shfl_sync(FULL, p, e);
+      for (int h = 0; h < 2; ++h)
+        if (128 * h + 4 * lane < dim) {
+          const float4 t = four_of(a.table, a.dtype, j0 + e, dim, 128 * h + 4 * lane);
+          for (int k = 0; k < 4; ++k) (&o[h].x)[k] = fmaf(pe, (&t.x)[k], (&o[h].x)[k]);
+        }
+    }
+  }
+  for (int e = 16; e; e >>= 1) {
+    l += __shfl_xor_sync(FULL, l, e);
+    zt += __shfl_xor_sync(FULL, zt, e);                   // 0 but in one lane
+  }
+  if (W > 1) {
+    __syncthreads();
+    if (lane == 0) {
+      s->m[warp] = M;
+      s->z[warp] = zt;
+    }
+    __syncthreads();
+    const float mine = M;
+    zt = 0.f;
+    for (int w = 0; w < W; ++w) {
+      M = fmaxf(M, s->m[w]);
+      zt += s->z[w];
+    }
+    const float f = exp2f(mine - (M == -INFINITY ? 0.f : M));
+    if (lane == 0) s->l[warp] = l * f;
+    for (int k = 0; k < 8; ++k) (&s->o[warp][lane + 32 * (k >> 2)].x)[k & 3] = (&o[0].x)[k] * f;
+    __syncthreads();
+    l = 0.f;
+    for (int w = 0; w < W; ++w) l += s->l[w];
+    for (int k = 0; k < 8; ++k) {
+      float v = 0.f;
+      for (int w = 0; w < W; ++w) v += (&s->o[w][lane + 32 * (k >> 2)].x)[k & 3];
+      (&o[0].x)[k] = v;
+    }
+    __syncthreads();
+  }
+  if (warp != 0) return;
+  for (int h = 0; h < 2; ++h)
+    if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
+  finish_root(a, i, M, l, zt, 0.f, 1.f, o, own);
+}
+
+// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn.
+template <int W>
+__global__ void __launch_bounds__(256, 3) join_roots_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
-  __shared__ float s_m[W], s_l[W], s_z[W];
-  __shared__ float4 s_o[W == 1 ? 1 : W][64];
+  __shared__ RootParts<W> s_parts;
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t live = a.count[0];
-  const int64_t col_tiles = (a.s.rows + a.tile - 1) / a.tile;
-  const Share sh((live + a.group - 1) / a.group * col_tiles, a.blocks);
+  const int64_t col_tiles = (a.s.rows + a.tile - 1) >> a.tile_bits;
+  const Share sh(((live + a.group - 1) >> a.group_bits) * col_tiles, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
-  float ut = 1.f;
-  if (a.s.planes == 2 && a.kept) {
-    float top = 0.f;
-    for (int k = lane; k < kMaxParts; k += 32) top = fmaxf(top, a.parts[kMaxParts + k]);
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
-    ut = unit_of(top);
-  }
+  const float unit = a.s.planes == 2 && a.kept ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
+  const float shift = a.s.planes == 2 && a.kept ? 7.f : 0.f;
   for (int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; row < live; row += step) {
     const int64_t r = row >> a.group_bits, in = row - (r << a.group_bits);
     const int i = a.act[row];
-    const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
+    const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     const bool dir = a.kept != nullptr;
-    float4 own[2];                                        // the target's row
+    float4 own[2], o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
     if (dir && warp == 0)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
-    bool again = false;
     float M, L, zt;
-    float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
     if (c0 == c1) {
       M = a.full[3 * row];
       L = a.full[3 * row + 1];
@@ -1098,47 +1204,51 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
       const int parts = c1 - c0 + 1;
       float m = -INFINITY;
       for (int k = W == 1 ? lane : (int)threadIdx.x; k < parts; k += 32 * W) m = fmaxf(m, part(k)[od]);
+      const float mine = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[od + 2];
+#pragma unroll
       for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, x));
       if (W > 1) {
-        if (lane == 0) s_m[warp] = m;
+        if (lane == 0) s_parts.m[warp] = m;
         __syncthreads();
-        for (int w = 0; w < W; ++w) m = fmaxf(m, s_m[w]);
+        for (int w = 0; w < W; ++w) m = fmaxf(m, s_parts.m[w]);
       }
       M = m;
+      zt = mine;
       const float ref = M == -INFINITY ? 0.f : M;
-      zt = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[od + 2];
       float l = 0.f;
 #pragma unroll 4
       for (int k = warp; k < parts; k += W) {
         const float* p = part(k);
         const float4 tail = *reinterpret_cast<const float4*>(p + od);
+        float4 v[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (dir && 128 * h + 4 * lane < od) v[h] = *reinterpret_cast<const float4*>(p + 128 * h + 4 * lane);
         const float f = exp2f(tail.x - ref);
         l = fmaf(tail.y, f, l);
-        if (dir) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-            if (128 * h + 4 * lane < od) {
-              const float4 v = *reinterpret_cast<const float4*>(p + 128 * h + 4 * lane);
-              o[h].x = fmaf(v.x, f, o[h].x);
-              o[h].y = fmaf(v.y, f, o[h].y);
-              o[h].z = fmaf(v.z, f, o[h].z);
-              o[h].w = fmaf(v.w, f, o[h].w);
-            }
-        }
+        for (int h = 0; h < 2; ++h)
+          if (dir && 128 * h + 4 * lane < od) {
+            o[h].x = fmaf(v[h].x, f, o[h].x);
+            o[h].y = fmaf(v[h].y, f, o[h].y);
+            o[h].z = fmaf(v[h].z, f, o[h].z);
+            o[h].w = fmaf(v[h].w, f, o[h].w);
+          }
       }
       L = l;
       if (W > 1) {
-        if (lane == 0) s_l[warp] = l;
-        s_o[warp][lane] = o[0];
-        s_o[warp][32 + lane] = o[1];
+        if (lane == 0) s_parts.l[warp] = l;
+        s_parts.o[warp][lane] = o[0];
+        s_parts.o[warp][32 + lane] = o[1];
         __syncthreads();
         L = 0.f;
-        for (int w = 0; w < W; ++w) L += s_l[w];
+        for (int w = 0; w < W; ++w) L += s_parts.l[w];
         if (warp == 0)
+#pragma unroll
           for (int w = 1; w < W; ++w)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const float4 v = s_o[w][32 * h + lane];
+              const float4 v = s_parts.o[w][32 * h + lane];
               o[h].x += v.x;
               o[h].y += v.y;
               o[h].z += v.z;
@@ -1147,131 +1257,14 @@ __global__ void __launch_bounds__(256) join_roots_kernel(const Join a) {
         __syncthreads();
       }
     }
-    if (!(L < INFINITY)) {
-      // A weight has passed what fp32 holds (or a value is no number): the row again, product by product, 32 nodes at a time per warp.  Parts are in
-      // units of their own maximum.
-      M = -INFINITY;
-      float l = 0.f;
-      zt = 0.f;
-      for (int k = 0; k < 8; ++k) (&o[0].x)[k] = 0.f;
-      const float factor = a.scale * kLog2e;
-      for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
-        const int64_t j = j0 + lane;
-        float x = -INFINITY;
-        if (j < a.s.rows) {
-          float dot = 0.f;
-          for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c), value_of(a.table, a.dtype, j * dim + c), dot);
-          x = fmaf(dot, factor, a.bias ? bias2(a.bias[j]) : 0.f);
-          if (j == y) {
-            zt = x;
-            x = -INFINITY;
-          }
-        }
-        float top = x;
-        for (int e = 16; e; e >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, e));
-        const float now = fmaxf(M, top), ref = now == -INFINITY ? 0.f : now, f = exp2f(M - ref);
-        M = now;
-        const float p = exp2f(x - ref);
-        l = l * f + p;
-        for (int k = 0; k < 8; ++k) (&o[0].x)[k] *= f;
-        for (int e = 0; e < 32 && j0 + e < a.s.rows; ++e) {
-          const float pe = __shfl_sync(FULL, p, e);
-          for (int h = 0; h < 2; ++h)
-            for (int k = 0; k < 4; ++k) {
-              const int c = 128 * h + 4 * lane + k;
-              if (c < dim) (&o[h].x)[k] = fmaf(pe, value_of(a.table, a.dtype, (j0 + e) * dim + c), (&o[h].x)[k]);
-            }
-        }
-      }
-      for (int e = 16; e; e >>= 1) {
-        l += __shfl_xor_sync(FULL, l, e);
-        zt += __shfl_xor_sync(FULL, zt, e);              // 0 but in one lane
-      }
-      if (W > 1) {
-        __syncthreads();
-        if (lane == 0) {
-          s_m[warp] = M;
-          s_z[warp] = zt;
-        }
-        __syncthreads();
-        const float mine = M;
-        zt = 0.f;
-        for (int w = 0; w < W; ++w) {
-          M = fmaxf(M, s_m[w]);
-          zt += s_z[w];
-        }
-        const float f = exp2f(mine - (M == -INFINITY ? 0.f : M));
-        if (lane == 0) s_l[warp] = l * f;
-        for (int k = 0; k < 8; ++k) (&s_o[warp][lane + 32 * (k >> 2)].x)[k & 3] = (&o[0].x)[k] * f;
-        __syncthreads();
-        l = 0.f;
-        for (int w = 0; w < W; ++w) l += s_l[w];
-        if (warp == 0)
-          for (int k = 0; k < 8; ++k) {
-            float v = 0.f;
-            for (int w = 0; w < W; ++w) v += (&s_o[w][lane + 32 * (k >> 2)].x)[k & 3];
-            (&o[0].x)[k] = v;
-          }
-        __syncthreads();
-      }
-      L = l;
-      again = true;
-    }
-    if (warp != 0) continue;                              // (the next row's first barrier waits for warp 0)
-    // L counts in units of 2^shift, O in units of 2^shift and of the table's unit
-    const float shift = a.s.planes == 2 && a.kept && !again ? 7.f : 0.f;
-    const float d = (M - zt) + (log2f(L) - shift);        // log2 of the others' weight over the target's
-    const bool none = L == 0.f, lost = zt == -INFINITY;
-    float loss, miss, mm, inv;
-    if (none) {                                           // no other node in sight
-      loss = lost ? INFINITY : zt - zt;
-      miss = 0.f;
-      mm = lost ? INFINITY : zt;                          // weights of 0 where nothing is in sight
-      inv = lost ? 0.f : 1.f;
-    } else if (lost) {
-      loss = INFINITY;
-      miss = 1.f;
-      mm = M;
-      inv = exp2f(shift) / L;
-    } else {
-      const float small = exp2f(-fabsf(d));               // the smaller side over the larger
-      loss = kLn2 * fmaxf(d, 0.f) + log1pf(small);
-      miss = (d > 0.f ? 1.f : small) / (1.f + small);
-      mm = fmaxf(M, zt);
-      inv = 1.f / (exp2f(zt - mm) + L * exp2f((M - mm) - shift));
-    }
-    if (d != d && !none && !lost) loss = miss = mm = d;   // NaN stays
-    if (lane == 0) {
-      a.loss[i] = loss;
-      if (a.kept) {
-        a.kept[i] = mm;
-        a.kept[a.s.n + i] = inv;
-        a.kept[2 * a.s.n + i] = miss;
-      }
-    }
-    if (dir) {
-      const float unit = again ? 1.f : ut;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = 128 * h + 4 * lane;
-        if (c >= dim) break;
-        const float4 ty = own[h];
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (!none) {
-          v.x = (o[h].x / L / unit - ty.x) * miss;
-          v.y = (o[h].y / L / unit - ty.y) * miss;
-          v.z = (o[h].z / L / unit - ty.z) * miss;
-          v.w = (o[h].w / L / unit - ty.w) * miss;
-        }
-        put_four(a.kept + 3 * a.s.n, TGNN_F32, i, dim, c, v);
-      }
-    }
+    if (__builtin_expect(!(L < INFINITY), 0)) redo_root<W>(a, &s_parts, i, y);
+    else if (warp == 0) finish_root(a, i, M, L, zt, shift, unit, o, own);   // (the next row's first barrier waits for warp 0)
   }
 }
 
 // Groups of table rows that several blocks share: block b takes the group that begins before the boundary between blocks b - 1 and b, if that is the
 // group's first one; grid.y parts of its rows.  Without any live root, zeros everywhere.
-__global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
+__global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
   const int64_t live = a.count[0];
@@ -1298,9 +1291,8 @@ __global__ void __launch_bounds__(256) join_table_kernel(const Join a) {
   if (b != c0 + 1) return;
   float uq = 1.f, ug = 1.f;
   if (a.s.planes == 2) {
-    __shared__ float s_red[8];
-    uq = unit_of(largest(a.parts, s_red));
-    ug = 2.f * unit_of(largest(a.parts + 2 * kMaxParts, s_red));
+    uq = unit_of(largest(a.parts, a.parts_used, 0));
+    ug = 2.f * unit_of(largest(a.parts, a.parts_used, 2));
   }
   const float out = a.scale / ug / uq;
   const int rows = a.group / (int)gridDim.y, lane = threadIdx.x & 31, od = a.s.od;
@@ -1433,7 +1425,7 @@ int check(const Call& a) {
 
 // begin, prep and main kernels of one direction
 template <int MODE>
-int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, void* dtable, float* dbias, Join* j) {
+int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, void* dq, void* dtable, float* dbias, Join* j) {
   const Shape s = shape_of(a.n, a.rows, a.dim, a.dtype);
   const Form f = form_of(a.dim, a.dtype);
   const Layout l = layout(s, a.dtype);
@@ -1462,6 +1454,7 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   p.tp = reinterpret_cast<uint16_t*>(base + l.tp);
   p.cols = reinterpret_cast<float*>(base + l.cols);
   p.status = a.status;
+  p.dq = dq;
   Main m = {};
   m.s = s;
   m.count = p.count;
@@ -1493,8 +1486,10 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   if (m.stages > 4) m.stages = 4;
   m.ahead = m.stages > 1 ? 2 : 1;
   const size_t smem = 1024 + a_bytes + (size_t)m.stages * t_bytes;
-  const int64_t maxima = s.planes == 2 ? a.rows * a.dim : MODE != BACKWARD && a.bias ? a.rows : 0;
-  const int blocks_of_parts = maxima == 0 ? 0 : (int)(maxima >> 12 >= kMaxParts - 1 ? kMaxParts - 1 : (maxima >> 12) + 1);
+  // blocks beside the first one: some 4096 values each
+  const int64_t beside = s.planes == 2 ? a.rows * a.dim + (dq ? a.n * a.dim : 0) : dq ? a.n * a.dim : MODE != BACKWARD && a.bias ? a.rows : 0;
+  const int blocks_of_parts = beside == 0 ? 0 : (int)(beside >> 12 >= kMaxParts - 1 ? kMaxParts - 1 : (beside >> 12) + 1);
+  p.parts_used = m.parts_used = blocks_of_parts;
   c(begin_kernel, dim3(1 + blocks_of_parts), dim3(1024), 0, p);
   const int64_t work = (direct ? 0 : a.rows) + a.n + (MODE == BACKWARD ? a.n : a.rows) / 32;
   c(prep_kernel, dim3((unsigned)(work / 16 >= 8 * sms ? 8 * sms : work / 16 + 1)), dim3(256), 0, p);
@@ -1506,6 +1501,7 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->count = p.count;
   j->act = p.act;
   j->parts = p.parts;
+  j->parts_used = p.parts_used;
   j->slots = m.slots;
   j->full = m.full;
   j->q = a.q;
@@ -1545,7 +1541,7 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   if (!loss || (((uintptr_t)loss | (uintptr_t)kept) & 3)) return fail(err, err_size, TGNN_EINVAL, "%s: loss is null, or loss or kept not aligned", a.who);
   Chain c(stream);
   Join j;
-  const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, &j);
+  const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j);
   if (rc) return rc;
   // 16 parts of a root and more: a block each (600 roots with 50 parts: see the table of cases), else a warp
   const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
@@ -1575,9 +1571,13 @@ extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void
     return TGNN_OK;
   }
   Chain c(stream);
-  if (dq) {
+  if (dtable || dbias) {
+    Join j;
+    if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dq, dtable, dbias, &j)) return rc;
+    c(join_table_kernel, dim3((unsigned)j.blocks, j.blocks < 64 ? 16 : 8), dim3(256), 0, j);
+  } else if (dq) {
     Prep p = {};
-    p.s = shape_of(n, rows, dim, dtype);
+    p.s = shape_of(n, rows, dim, TGNN_BF16);              // no maxima of rows
     p.target = target;
     p.index_bits = index_bits;
     p.dtype = dtype;
@@ -1585,13 +1585,11 @@ extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void
     p.kept = kept;
     p.dq = dq;
     p.scale = scale;
-    const int64_t blocks = (n * dim + 1023) / 1024;
-    c(dq_kernel, dim3((unsigned)(blocks < 8 * num_sms() ? blocks : 8 * num_sms())), dim3(256), 0, p);
-  }
-  if (dtable || dbias) {
-    Join j;
-    if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dtable, dbias, &j)) return rc;
-    c(join_table_kernel, dim3((unsigned)j.blocks, j.blocks < 64 ? 16 : 8), dim3(256), 0, j);
+    p.backward = 1;
+    const Layout l = layout(shape_of(n, rows, dim, dtype), dtype);
+    p.parts = reinterpret_cast<float*>(static_cast<char*>(scratch) + l.parts);
+    const int64_t blocks = n * dim >> 12;
+    c(begin_kernel, dim3((unsigned)(2 + (blocks < kMaxParts - 1 ? blocks : kMaxParts - 2))), dim3(1024), 0, p);
   }
   return c.end(a.who, err, err_size);
 }
