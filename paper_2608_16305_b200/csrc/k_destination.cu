@@ -34,7 +34,7 @@ namespace {
 
 constexpr unsigned kSpin = 1u << 22;
 constexpr int kMaxBlocks = 160;             // thread blocks of the main kernel, one per multiprocessor
-constexpr int kSmem = 226 * 1024;           // dynamic shared memory; the static part is below 1 KB
+constexpr int kSmem = 222 * 1024;           // dynamic shared memory; the static part is up to 5 KB
 constexpr int kMaxParts = 592;              // partial maxima: of fp32 rows, of the bias
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -350,12 +350,19 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 #define AS_BOTH(x) "+f"(x)
 #define AS_IN(x) "r"(x)
 #define AS_INF(x) "f"(x)
+#define REGS16(M, r, o)                                                                                                                  \
+  M(r[o + 0]), M(r[o + 1]), M(r[o + 2]), M(r[o + 3]), M(r[o + 4]), M(r[o + 5]), M(r[o + 6]), M(r[o + 7]), M(r[o + 8]), M(r[o + 9]),       \
+      M(r[o + 10]), M(r[o + 11]), M(r[o + 12]), M(r[o + 13]), M(r[o + 14]), M(r[o + 15])
 #define LIST32                                                                                                                           \
   "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}"
 #define LIST32_1                                                                                                                         \
   "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32}"
 #define TMEM_LD32(r, o, addr) asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 " LIST32 ", [%32];" : REGS32(AS_OUT, r, o) : "r"(addr))
 #define TMEM_ST32(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_IN, r, o) : "memory")
+#define TMEM_ST16(addr, r, o)                                                                                                             \
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),      \
+               REGS16(AS_IN, r, o)                                                                                                        \
+               : "memory")
 #define TMEM_ST32F(addr, r, o) asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], " LIST32_1 ";" ::"r"(addr), REGS32(AS_INF, r, o) : "memory")
 // the wait, with the loaded registers as its results: nothing that reads them is moved ahead of it
 #define WAIT_LD32(r) asm volatile("tcgen05.wait::ld.sync.aligned;" : REGS32(AS_BOTH, r, 0)::"memory")
@@ -427,19 +434,30 @@ __device__ __forceinline__ uint32_t pack_lo(float x, float y, uint32_t hi) {
   return *reinterpret_cast<const uint32_t*>(&l);
 }
 
+// The meeting of the two warps that share 32 rows, each with half of a unit's columns; false when a role has given up.  A warp that gives up arrives
+// once more (pair_leave), behind the flag: its partner is held by no meeting, and leaves at the first that it comes to.
+__device__ __forceinline__ bool pair_sync(int id, volatile int* abort_flag) {
+  asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory");
+  return !__any_sync(FULL, *abort_flag);
+}
+__device__ __forceinline__ void pair_leave(int id) { asm volatile("bar.arrive %0, 64;" ::"r"(id) : "memory"); }
+
 // MODE; PL planes per operand (2: fp32 rows); NH groups of 128 rows of A; NT rows of T per tile in shared memory; U columns of S at a time, two
 // buffers of them per group.
 //
-// Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), four more per group form weights,
-// a row per thread, while the other buffer's products run.  P takes the place of the S that it was made of.
-// 256 x 128 logits of rows of 128 take the tensor cores 2048 cycles and the exponentials 2048 (16 a cycle).
+// Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), the others form weights, a row per
+// thread, while the other buffer's products run.  With two groups eight warps each do, and a thread has half of a unit's columns (four warps per
+// scheduler hide what two wait for: SPLIT_TIMES); with one group the products take longer than four warps.  P takes the place of the S that it was made of.
+// 256 x 128 logits of rows of 128 take the tensor cores 2560 cycles (S is bound by shared memory: 48 cycles for 128 x 64 x 16) and the exponentials 2048.
 template <int MODE, int PL, int NH, int NT, int U>
-__global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
+__global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(const __grid_constant__ Main g) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[NH][2], s_pfull[NH][2], s_pv[NH][2];
+  __shared__ float s_m[2][NH][128], s_l[NH][128], s_zt[NH][128];   // from one half of a row to the other
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   constexpr int R = 128 * NH, PER = NT / U;            // units per tile
+  constexpr int SPLIT = NH == 2 ? 2 : 1, NC = U / SPLIT, CH = NC / 32;   // threads per row, their columns, in steps of 32
   constexpr int KS = NH == 2 || (PL == 2 && NT == 128) ? 8 : 16;   // steps of 16 in dim, at most
   constexpr bool MOVING = MODE == FORWARD && PL == 2;  // the reference of a row's weights can move
   constexpr int COL_BYTES = (MODE == BACKWARD ? 16 : 4) * NT;
@@ -455,12 +473,12 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
   if (tid == 0) {
     for (int i = 0; i < 4; ++i) {
       mbar_init(smem_u32(&s_full[i]), 1);
-      mbar_init(smem_u32(&s_empty[i]), MODE == LOSS ? 4 * NH : NH);
+      mbar_init(smem_u32(&s_empty[i]), MODE == LOSS ? 4 * SPLIT * NH : NH);
     }
     for (int h = 0; h < NH; ++h)
       for (int i = 0; i < 2; ++i) {
         mbar_init(smem_u32(&s_sfull[h][i]), 1);
-        mbar_init(smem_u32(&s_pfull[h][i]), 4);
+        mbar_init(smem_u32(&s_pfull[h][i]), 4 * SPLIT);
         mbar_init(smem_u32(&s_pv[h][i]), 1);
       }
     mbar_init(smem_u32(&s_afull), 1);
@@ -589,10 +607,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
           const uint64_t t0 = dv + p_st * t_stage + sub * (U * 128 >> 4);
 #pragma unroll
           for (int pr = 0; pr < (PL == 2 ? 3 : 1); ++pr) {
-            const uint32_t p0 = s_cols + buf * U + (pr == 2 ? U / 2 : 0);
+            const uint32_t p0 = s_cols + buf * U + (pr == 2 ? NC / 2 : 0);
             const uint64_t tp = t0 + (pr == 1 ? t_plane : 0);
 #pragma unroll
-            for (int ks = 0; ks < U / 16; ++ks) mma_ta(o, p0 + 8 * ks, tp + 128 * ks, id_o, pr > 0 || ks > 0 || !fresh);
+            for (int ks = 0; ks < U / 16; ++ks)
+              mma_ta(o, p0 + ks / (NC / 16) * NC + ks % (NC / 16) * 8, tp + 128 * ks, id_o, pr > 0 || ks > 0 || !fresh);
           }
           commit(smem_u32(&s_pv[h][buf]));
           if (sub == PER - 1) {
@@ -611,10 +630,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     __syncwarp();
   } else if (warp >= 4) {
     // ---------------------------------------------------------------- weights: a thread has a row of A
-    const int grp = (warp - 4) >> 2, quarter = warp & 3;
-    const int row_in = 128 * grp + 32 * quarter + lane;
+    const int grp = (warp - 4) / (4 * SPLIT), part = (warp - 4) / 4 % SPLIT, quarter = warp & 3;
+    const int pair = 1 + 4 * grp + quarter;              // the named barrier of the two warps with these rows
+    const int lane_row = 32 * quarter + lane, row_in = 128 * grp + lane_row;
     const uint32_t lane_base = (uint32_t)(32 * quarter) << 16;
-    const uint32_t o_addr = o_base + grp * 128 + lane_base, s_base = tmem + 2 * grp * U + lane_base;
+    const uint32_t o_addr = o_base + grp * 128 + lane_base, s_base = tmem + 2 * grp * U + part * NC + lane_base;
     const uint32_t bar_s = smem_u32(&s_sfull[grp][0]), bar_p = smem_u32(&s_pfull[grp][0]), bar_pv = smem_u32(&s_pv[grp][0]);
     const int pitch = pitch_of(g.s);
     float uq = 1.f, ut = 1.f, ug = 1.f;
@@ -630,7 +650,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
     const uint32_t all_cols = (uint32_t)col_tiles, full_tiles = (uint32_t)(t_rows / NT), all_units = tiles * PER;
     uint32_t r = (uint32_t)r0, j = (uint32_t)j0, left = tiles, st = 0, u = 0;
     bool ok = true, have = false;                        // have: the next unit's first columns are in z[0], or on their way
-    float z[2][32];
+    float z[CH > 1 ? 2 : 1][32];
     while (left > 0 && ok) {
       // ---- the tiles of one group of rows
       const int64_t row = (int64_t)r * R + row_in;
@@ -657,7 +677,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
           }
           have = false;
           // the columns' values came with the tile, which S is complete after
-          const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES) + sub * U;
+          const float* col = reinterpret_cast<const float*>(col_base + st * COL_BYTES) + sub * U + part * NC;
           // While the last columns are worked on, the next unit's first ones are asked for, if they are there.
           auto ask = [&]() {
             const uint32_t next = buf ^ 1, parity = ((u + 1) >> 1) & 1;
@@ -667,11 +687,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
               TMEM_LD32(z[0], 0, s_base + next * U);
             }
           };
-          uint32_t hi[U / 2];
-          uint32_t lo[PL == 2 ? U / 2 : 1];
+          uint32_t hi[NC / 2];
+          uint32_t lo[PL == 2 ? NC / 2 : 1];
           if (MODE != BACKWARD) {
-            const int hit = tgt - (int32_t)(j * NT + sub * U);                     // outside [0, U): not here
-            const bool any_hit = __any_sync(FULL, (uint32_t)hit < (uint32_t)U);
+            const int hit = tgt - (int32_t)(j * NT + sub * U + part * NC);         // outside [0, NC): not here
+            const bool any_hit = __any_sync(FULL, (uint32_t)hit < (uint32_t)NC);
             const bool plain = !biased && j < full_tiles;   // the columns' values are zeros
             // logits of 32 columns less ref in place of S, the target left out
             auto logits = [&](float(&v)[32], int c, float ref) {
@@ -700,7 +720,7 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
             auto maximum = [&]() {                       // of the unit's logits; what was asked for is lost
               have = false;
               float top = -INFINITY;
-              for (int c = 0; c < U; c += 32) {
+              for (int c = 0; c < NC; c += 32) {
                 TMEM_LD32(z[0], 0, s_addr + c);
                 WAIT_LD32(z[0]);
                 logits(z[0], c, 0.f);
@@ -720,11 +740,17 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
               } else {
                 have = false;
                 float top = -INFINITY;
-                for (int c = 0; c < U; c += 32) {
+                for (int c = 0; c < NC; c += 32) {
                   TMEM_LD32(z[0], 0, s_addr + c);
                   WAIT_LD32(z[0]);
 #pragma unroll
                   for (int k = 0; k < 32; ++k) top = hit == c + k ? top : fmaxf(top, z[0][k] * factor);
+                }
+                if (SPLIT == 2) {                        // one reference for both halves of the row
+                  s_m[part][grp][lane_row] = top;
+                  ok = pair_sync(pair, abort_flag);
+                  if (!ok) break;
+                  top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
                 }
                 m = most_bias == -INFINITY ? 0.f : top + most_bias;
               }
@@ -736,11 +762,11 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
               const f32x2 shift2 = pack2(SHIFT, SHIFT);
               f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
 #pragma unroll
-              for (int c = 0; c < U / 32; ++c) {
-                float(&v)[32] = z[c & 1];
+              for (int c = 0; c < CH; ++c) {
+                float(&v)[32] = z[CH > 1 ? c & 1 : 0];
                 WAIT_LD32(v);
-                if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
-                else ask();
+                if (c + 1 < CH) TMEM_LD32(z[CH > 1 ? (c + 1) & 1 : 0], 0, s_addr + 32 * (c + 1));
+                else if (CH > 1) ask();
                 logits(v, 32 * c, ref);
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) {
@@ -800,15 +826,15 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
             f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
             bool here = false;
 #pragma unroll
-            for (int c = 0; c < U / 32; ++c) here |= (uint32_t)(ct[32 * c + lane] - row0) < 32u;
+            for (int c = 0; c < CH; ++c) here |= (uint32_t)(ct[32 * c + lane] - row0) < 32u;
             const bool any_hit = __any_sync(FULL, here);
 #pragma unroll
-            for (int c = 0; c < U / 32; ++c) {
-              float(&v)[32] = z[c & 1];
+            for (int c = 0; c < CH; ++c) {
+              float(&v)[32] = z[CH > 1 ? c & 1 : 0];
               const float* cc = col + 32 * c;
               WAIT_LD32(v);
-              if (c + 1 < U / 32) TMEM_LD32(z[(c + 1) & 1], 0, s_addr + 32 * (c + 1));
-              else ask();
+              if (c + 1 < CH) TMEM_LD32(z[CH > 1 ? (c + 1) & 1 : 0], 0, s_addr + 32 * (c + 1));
+              else if (CH > 1) ask();
               if (biased) {
 #pragma unroll
                 for (int k = 0; k < 32; k += 2) unpack2(fma2(pack2(v[k], v[k + 1]), factor2, rb2), v[k], v[k + 1]);
@@ -864,10 +890,14 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
             l += a + b;
           }
           if (MODE != LOSS) {
+            if (NC == 32) {
+              TMEM_ST16(s_addr, hi, 0);
+            } else {
 #pragma unroll
-            for (int c = 0; c < U / 2; c += 32) {
-              TMEM_ST32(s_addr + c, hi, c);
-              if (PL == 2) TMEM_ST32(s_addr + U / 2 + c, lo, c);
+              for (int c = 0; c < NC / 2; c += 32) {
+                TMEM_ST32(s_addr + c, hi, c);
+                if (PL == 2) TMEM_ST32(s_addr + NC / 2 + c, lo, c);
+              }
             }
             wait_st();
           }
@@ -885,7 +915,22 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
       // the group's rows are done as far as this block goes
       const bool alone = count == all_cols;
       float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
-      if (valid) {
+      if (SPLIT == 2) {                                  // what the two halves of a row have is put together
+        if (part == 1) {
+          s_l[grp][lane_row] = l;
+          s_zt[grp][lane_row] = zt;
+        }
+        ok = pair_sync(pair, abort_flag);
+        if (!ok) break;
+        if (part == 0) {
+          const float other = s_zt[grp][lane_row];
+          l += s_l[grp][lane_row];
+          if (other != -INFINITY) zt = other;
+        }
+        ok = pair_sync(pair, abort_flag);                // (the next group's values go to the same places)
+        if (!ok) break;
+      }
+      if (valid && part == 0) {
         if (MODE == BACKWARD) {
           if (!alone) slot[g.s.od] = l;
           else if (summed) g.dbias[row] = l / ug;
@@ -903,8 +948,8 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
         const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
         const int dim = g.s.dim;
         float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
-        float(&o)[32] = z[1];                            // z[0] may hold what was asked for
-        for (int c = 0; c < g.s.od; c += 32) {
+        float(&o)[32] = z[CH > 1 ? 1 : 0];               // z[0] may hold what was asked for
+        for (int c = 32 * part; c < g.s.od; c += 32 * SPLIT) {
           __syncwarp();                                  // lanes without a row have gone ahead
           TMEM_LD32(o, 0, o_addr + c);
           WAIT_LD32(o);
@@ -951,9 +996,14 @@ __global__ void __launch_bounds__(128 + 128 * NH, 1) destination_kernel(const __
       ++r;
     }
     if (have) WAIT_LD32(z[0]);
-    if (!ok && lane == 0) {
-      s_abort = 1;
-      atomicCAS(g.status, 0, TGNN_ETIMEOUT);
+    if (!ok) {
+      if (lane == 0) {
+        s_abort = 1;
+        atomicCAS(g.status, 0, TGNN_ETIMEOUT);
+        __threadfence_block();
+      }
+      __syncwarp();
+      if (SPLIT == 2) pair_leave(pair);
     }
   }
   fence_before();
@@ -1384,7 +1434,7 @@ void launch_main(Chain& c, const Main& m, int blocks, size_t smem) {
     if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128, 128>, 256);
     else go(destination_kernel<MODE, 2, 1, 64, 64>, 256);
   } else {
-    if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128, 64>, 384);
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128, 64>, 640);
     else go(destination_kernel<MODE, 1, 1, 128, 128>, 256);
   }
 }
