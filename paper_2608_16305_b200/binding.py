@@ -494,11 +494,15 @@ def adamw_step(tensors, bits: int, device: int, steps, params, grads, lr: float,
                seed: int = 0) -> int:
     """tgnn_adamw_step: `tensors` is an array of TgnnAdamwTensor whose moments, sizes, decays and copies are set; parameters and gradients (lists; a
     gradient may be None: that tensor stays as it is) are filled in for the call."""
+    if len(tensors) != len(params):
+        raise TypeError(f"expected as many parameters as descriptions, got {len(params)} for {len(tensors)}")
     return _call("adamw_step", C.addressof(tensors), bits, device, steps, lr, beta1, beta2, eps, grad_scale, seed, params, grads)
 
 
 def adamw_moments(tensors, device: int, m_out, v_out) -> int:
     """tgnn_adamw_moments: values of 8-bit moments; m_out, v_out: arrays of c_void_p, one fp32 tensor's address each."""
+    if len(m_out) < len(tensors) or len(v_out) < len(tensors):
+        raise TypeError("expected an address of each moment per tensor")
     return _call("adamw_moments", C.addressof(tensors), len(tensors), C.addressof(m_out), C.addressof(v_out), device)
 
 

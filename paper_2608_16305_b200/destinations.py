@@ -6,8 +6,9 @@ learned, and the same table gives the rows of neighbor slots.  All under autogra
     lookup(table, ids)                 tgnn_lookup, its gradient by tgnn_lookup_backward
     destination_loss(q, table, target) tgnn_destination_loss, its gradients by tgnn_destination_loss_backward
     AdamW(params, ...)                 tgnn_adamw_step: all tensors in one launch, moments in 32 or 8 bits
+    DestinationModel(workload, ...)    all three over a workload's batches, with the attention over sampled slots between them
 
-All arithmetic happens inside the library.
+All arithmetic happens inside the library, but the sum of a root's own row and what it attends to.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ from typing import List, Optional, Sequence, Tuple, Union
 import torch
 
 from . import binding as B
+from .history import Slots, TimeBias, slot_attention
 
 
 class _Lookup(torch.autograd.Function):
@@ -144,3 +146,68 @@ class AdamW:
         m, v, pm, pv = self._values
         B.adamw_moments(self._t, self.device.index, pm, pv)
         return m, v
+
+
+class DestinationModel:
+    """Which node a source meets next, from a learned table alone: a root's row plus attention from it over the rows of its last neighbors
+    (with a learned bias by age) is scored against every node's row.
+
+    workload    a DeviceWorkload (its events, T-CSR and batches); a batch's target events are roots at their sources and times
+    dtype       of the rows that are looked up and scored: fp32, or bf16 beside fp32 weights
+    heads, dim  of the attention; a row has heads * dim values, 256 at most (default: the workload's d over its heads)
+    window      the last entries of its source that a root sees
+    bits        of the optimizer's moments, 32 or 8"""
+
+    def __init__(self, workload, heads: Optional[int] = None, dim: Optional[int] = None, window: Optional[int] = None, buckets: int = 16,
+                 dtype: torch.dtype = torch.float32, lr: float = 1e-3, weight_decay: float = 0.0, bits: int = 32, seed: int = 0):
+        cfg, dev = workload.cfg, workload.device
+        self.workload = workload
+        self.heads = cfg.heads if heads is None else int(heads)
+        self.dim = cfg.d // self.heads if dim is None else int(dim)
+        self.window = cfg.k if window is None else int(window)
+        if dtype not in (torch.float32, torch.bfloat16) or not 1 <= self.heads * self.dim <= 256:
+            raise B.TgnnError(B.TGNN_EINVAL, f"DestinationModel: rows of {self.heads * self.dim} values of {dtype} (fp32 or bf16, 1 to 256)")
+        wide = self.heads * self.dim
+        gen = torch.Generator(device=dev).manual_seed(seed)
+        self.weights = torch.randn((cfg.num_nodes, wide), generator=gen, device=dev) * wide ** -0.25
+        self.table = self.weights if dtype == torch.float32 else self.weights.to(dtype)
+        self.bias = torch.zeros(cfg.num_nodes, device=dev)
+        self.age = TimeBias.logarithmic(self.heads, buckets, 1.0, 1e6, device=dev)
+        self.leaves = [x.requires_grad_() for x in (self.table, self.bias, self.age.table)]
+        self.optimizer = AdamW([self.weights.detach(), self.bias.detach(), self.age.table.detach()], lr=lr, weight_decay=[weight_decay, 0.0, 0.0],
+                               bits=bits, seed=seed, copies=None if dtype == torch.float32 else [self.table.detach(), None, None])
+        self._status = torch.zeros(1, dtype=torch.int32, device=dev)
+
+    def status(self) -> int:
+        """0, or the first error that a call met on the device (4: an index outside its table); reads the device."""
+        return int(self._status.item())
+
+    def slots(self, nodes: torch.Tensor, times: torch.Tensor) -> Slots:
+        w, n, dev = self.workload, nodes.numel(), nodes.device
+        out = Slots(*(torch.empty((n, self.window), dtype=t, device=dev) for t in (torch.int32, torch.int32, torch.float64)),
+                    torch.empty(n, dtype=torch.int32, device=dev))
+        B.sample_window(w.indptr, w.nbr, w.eid, w.ts, nodes, times, self.window, 0, *out, None, None, self._status)
+        return out
+
+    def loss(self, nodes: torch.Tensor, times: torch.Tensor, destinations: torch.Tensor) -> torch.Tensor:
+        """Cross entropy [n] of each root's destination among all nodes (below 0: a root that takes no part); differentiable in `leaves`, and with
+        nothing kept under torch.no_grad()."""
+        s = self.slots(nodes, times)
+        shape = (self.heads, self.dim)
+        own = lookup(self.table, nodes, status=self._status)
+        rows = lookup(self.table, s.nbr, status=self._status).view(*s.nbr.shape, *shape)
+        seen = slot_attention(own.view(nodes.numel(), *shape), rows, rows, s.cnt, bias=self.age, times=times, ts=s.ts)
+        return destination_loss(own + seen.view_as(own), self.table, destinations, bias=self.bias, status=self._status)
+
+    def targets(self, b: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+        """Sources, times and destinations of batch b; destinations of events that only come along (a workload with embed_aux) are -1."""
+        src, dst, _, t = self.workload.targets(b)
+        mask = self.workload.loss_mask(b)
+        return src, t, dst if mask is None else torch.where(mask != 0, dst, -1)
+
+    def step(self, b: int) -> torch.Tensor:
+        """One training step on batch b; its losses, one per event."""
+        loss = self.loss(*self.targets(b))
+        grads = torch.autograd.grad(loss, self.leaves, grad_outputs=torch.ones_like(loss))
+        self.optimizer.step(list(grads), grad_scale=1.0 / max(1, loss.numel()))
+        return loss.detach()
