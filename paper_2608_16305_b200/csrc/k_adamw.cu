@@ -310,12 +310,10 @@ __global__ void __launch_bounds__(kThreads) moments_kernel(const __grid_constant
   }
 }
 
-// Values per thread block: 2048 while that leaves no multiprocessor idle, more where there is more, so that a block's set-up (the powers of b1
-// and b2, 0.3 us) is a small part of it.
-int per_chunk_of(int64_t values) {
-  const int64_t per_block = values / (16 * num_sms());
-  return per_block >= 8192 ? 8192 : per_block >= 4096 ? 4096 : 2048;
-}
+// Values per thread block: 2048, so that few values have many blocks.  With moments in 8 bits, where a block's set-up (the powers of b1 and b2) is felt
+// beside its arithmetic, 8192 where enough blocks remain (us with 2048 / 8192 / 16384: 4M values 21 / 22 / 24, 10M 49 / 47 / 52, 20M 93 / 92 / 89,
+// 60M 269 / 248 / 233, 26M in 18 tensors - / 173 / 184; with moments in 32 bits 2048 is best throughout: 10M 44 / 48 / 52, 60M 244 / 251 / 258).
+int per_chunk_of(int64_t values, int bits) { return bits == 8 && values / (8 * num_sms()) >= 8192 ? 8192 : 2048; }
 
 template <int MAX, typename K>
 void launch(K kernel, Chain& c, const tgnn_adamw_tensor* t, float* const* m_out, float* const* v_out, int from, int count, int bits, Many<MAX>& a,
@@ -388,7 +386,7 @@ extern "C" TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, i
     return fail(err, err_size, TGNN_EINVAL, "%s: lr >= 0, 0 <= beta < 1, eps >= 0 and a finite grad_scale are needed", who);
   if (!steps || ((uintptr_t)steps & 7)) return fail(err, err_size, TGNN_EINVAL, "%s: steps is null or not 8-byte aligned", who);
   if (values == 0) return TGNN_OK;
-  const int per = per_chunk_of(values);
+  const int per = per_chunk_of(values, state_bits);
   Chain c(stream);
   auto fill = [&](auto& a) {
     a.steps = steps;
@@ -434,7 +432,7 @@ extern "C" TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host
   for (int i = 0; i < used; ++i)
     if (tensors_host[i].numel > 0 && (!m_out_host[i] || !v_out_host[i] || (((uintptr_t)m_out_host[i] | (uintptr_t)v_out_host[i]) & 3)))
       return fail(err, err_size, TGNN_EINVAL, "%s: tensor %d: an output is null or not aligned", who, i);
-  const int per = per_chunk_of(values);
+  const int per = per_chunk_of(values, 8);
   Chain c(stream);
   for (int from = 0; from < used;) {
     c.first = true;

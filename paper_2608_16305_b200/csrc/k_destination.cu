@@ -1599,9 +1599,10 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   Join j;
   const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j);
   if (rc) return rc;
-  // 16 parts of a root and more: a block each (600 roots with 50 parts: see the table of cases), else a warp
+  // 24 parts of a root and more: a block each, else a warp.  Us of a loss with what the backward pass needs, a warp and a block per root, rows of 100: 49 parts
+  // (600 roots, 9000 nodes, bf16) 58 and 40, 29 (the same in fp32) 50 and 45, 18 (2000 roots, bf16) 45 and 57, (1024 roots, 100 000 nodes, fp32) 176 and 182
   const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
-  if (j.blocks >= 16 * groups) c(join_roots_kernel<8>, dim3((unsigned)(n < most ? n : most)), dim3(256), 0, j);
+  if (j.blocks >= 24 * groups) c(join_roots_kernel<8>, dim3((unsigned)(n < most ? n : most)), dim3(256), 0, j);
   else c(join_roots_kernel<1>, dim3((unsigned)((n + 7) / 8 < most ? (n + 7) / 8 : most)), dim3(256), 0, j);
   return c.end(a.who, err, err_size);
 }
@@ -1630,7 +1631,7 @@ extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void
   if (dtable || dbias) {
     Join j;
     if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dq, dtable, dbias, &j)) return rc;
-    c(join_table_kernel, dim3((unsigned)j.blocks, j.blocks < 64 ? 16 : 8), dim3(256), 0, j);
+    c(join_table_kernel, dim3((unsigned)j.blocks, 8), dim3(256), 0, j);
   } else if (dq) {
     Prep p = {};
     p.s = shape_of(n, rows, dim, TGNN_BF16);              // no maxima of rows

@@ -431,7 +431,8 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
 }
 
 // Few ids and few rows: a thread block per `kRows` rows of the table and slice of 32 * V columns looks through all ids, every warp an equal part of them, adds
-// up what it finds of its rows in shared memory, in order, and the parts of the warps are added in order.  One kernel in place of a sort's five.
+// up what it finds of its rows in shared memory, in order, and the parts of the warps are added in order.  One kernel in place of a sort's five.  The rows of
+// a block are as far apart as there are blocks: hubs often have neighboring numbers.
 struct FewArgs {
   const void* ids;
   const void* dout;
@@ -439,25 +440,25 @@ struct FewArgs {
   int32_t* status;
   int64_t rows;
   int index_bits, n, dim, dtype;
+  uint32_t magic;         // ceil(2^32 / blocks of rows), 0 for one block: x * magic >> 32 = x / blocks for x * blocks < 2^32
   float scale;
 };
 constexpr int kFewWarps = 16;
 template <typename T, int V>
 __global__ void __launch_bounds__(32 * kFewWarps) few_sum_kernel(const FewArgs a) {
   constexpr int kRows = 32 / V, kHeld = 128;
-  extern __shared__ float s_sum[];                                            // [warp][row][32 * V]
+  extern __shared__ float s_sum[];                                            // [warp][row][V][32]
   __shared__ uint16_t s_place[kFewWarps][kHeld];
   __shared__ uint8_t s_row[kFewWarps][kHeld];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int col = (blockIdx.y * 32 + lane) * V;
   const bool active = col < a.dim;
   const T* dout = static_cast<const T*>(a.dout) + col;
-  float* mine = s_sum + warp * kRows * 32 * V + lane * V;
+  float* mine = s_sum + warp * kRows * 32 * V + lane;
 #pragma unroll
   for (int r = 0; r < kRows; ++r)
 #pragma unroll
-    for (int k = 0; k < V; ++k) mine[r * 32 * V + k] = 0.f;
-  const int64_t row0 = (int64_t)blockIdx.x * kRows;
+    for (int k = 0; k < V; ++k) mine[(r * V + k) * 32] = 0.f;
   const int per = (a.n + kFewWarps - 1) / kFewWarps, lo = min(a.n, warp * per), hi = min(a.n, lo + per);
   int held = 0;
   auto flush = [&]() {
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_sum_kernel(const FewArgs a
           float f[V], *x = mine + s_row[warp][u0 + u] * 32 * V;
           v[u].get(f);
 #pragma unroll
-          for (int k = 0; k < V; ++k) x[k] += f[k];
+          for (int k = 0; k < V; ++k) x[32 * k] += f[k];
         }
     }
     held = 0;
@@ -491,14 +492,15 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_sum_kernel(const FewArgs a
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const bool here = id[k] >= row0 && id[k] < row0 + kRows && id[k] < a.rows;
+      const uint32_t row = a.magic ? __umulhi((uint32_t)id[k], a.magic) : (uint32_t)id[k];
+      const bool here = id[k] >= 0 && id[k] < a.rows && (uint32_t)id[k] - row * gridDim.x == blockIdx.x;
       const unsigned hits = __ballot_sync(FULL, here);
       if (hits == 0) continue;
       if (held + __popc(hits) > kHeld) flush();
       if (here) {
         const int at = held + __popc(hits & ((1u << lane) - 1));
         s_place[warp][at] = (uint16_t)(j0 + 32 * k + lane);
-        s_row[warp][at] = (uint8_t)(id[k] - row0);
+        s_row[warp][at] = (uint8_t)row;
       }
       held += __popc(hits);
     }
@@ -507,16 +509,17 @@ __global__ void __launch_bounds__(32 * kFewWarps) few_sum_kernel(const FewArgs a
   if (beyond) *a.status = 4;
   __syncthreads();
   for (int r = warp; r < kRows; r += kFewWarps) {
-    if (row0 + r >= a.rows) break;
+    const int64_t row = (int64_t)r * gridDim.x + blockIdx.x;
+    if (row >= a.rows) break;
     float x[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) x[k] = 0.f;
     for (int w = 0; w < kFewWarps; ++w)
 #pragma unroll
-      for (int k = 0; k < V; ++k) x[k] += s_sum[((w * kRows + r) * 32 + lane) * V + k];
+      for (int k = 0; k < V; ++k) x[k] += s_sum[((w * kRows + r) * V + k) * 32 + lane];
 #pragma unroll
     for (int k = 0; k < V; ++k) x[k] *= a.scale;
-    if (active) store_values<V>(a.dtable, a.dtype, (row0 + r) * a.dim + col, x);
+    if (active) store_values<V>(a.dtable, a.dtype, row * a.dim + col, x);
   }
 }
 
@@ -645,10 +648,17 @@ void gather_out(Chain& c, const GatherArgs& a, int out_dtype, int bits) {
   else gather_type<TT, __half>(c, a, bits);
 }
 
+// Ids per group of lanes, with `groups` of them in a thread block: few enough that the groups fill the device, and 1024 or more in a block where there are
+// many, so that hubs leave few parts (rows of 100 fp32, 8 groups, chunks of 16 / 32 / 64 / 128 in us, ids of 17 000 nodes drawn with weights 1 / i^1.2:
+// 2^16 ids 37 / 38 / 39 / 48, 2^17 61 / 46 / 49 / 56, 2^18 114 / 87 / 73 / 74, 2^20 326 / 249 / 210 / 186, 2^22 1133 / 824 / 670 / 597; drawn evenly
+// 2^16 32 / 32 / 34 / 41, 2^20 175 / 171 / 169 / 174).
+int chunk_of(int64_t n, int groups) { return n <= 1 << 16 ? 16 : n <= 1 << 17 ? 32 : n <= 1 << 19 || groups > 8 ? 64 : 128; }
+
 template <typename T, int V>
 uint32_t sum_lanes(Chain& c, SumArgs& a) {
   uint32_t blocks = 0;
   auto go = [&](auto kernel, int g) {
+    a.chunk = chunk_of(a.n, 256 / g);
     a.span = 256 / g * a.chunk;
     blocks = (uint32_t)(((int64_t)a.n + a.span - 1) / a.span);
     c(kernel, dim3(blocks, (a.groups + g - 1) / g), dim3(256), 0, a);
@@ -679,24 +689,28 @@ void few_type(Chain& c, const FewArgs& a) {
   constexpr int kSmem = kFewWarps * 32 * 32 * 4;                               // 32 / v rows of 32 v columns per warp
   auto go = [&](auto kernel) {
     c.e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    c(kernel, dim3((unsigned)((a.rows * v + 31) / 32), (a.dim + 32 * v - 1) / (32 * v)), dim3(32 * kFewWarps), kSmem, a);
+    const unsigned blocks = (unsigned)((a.rows * v + 31) / 32);
+    FewArgs f = a;
+    f.magic = blocks == 1 ? 0 : (uint32_t)(((1ull << 32) + blocks - 1) / blocks);
+    c(kernel, dim3(blocks, (a.dim + 32 * v - 1) / (32 * v)), dim3(32 * kFewWarps), kSmem, f);
   };
   if (v == W) go(few_sum_kernel<T, W>);
   else if (v == 2) go(few_sum_kernel<T, 2>);
   else go(few_sum_kernel<T, 1>);
 }
 
-// Ids per group of lanes: few enough that the groups fill the device.
-int chunk_of(int64_t n) { return n <= 1 << 16 ? 16 : n <= 1 << 18 ? 32 : n <= 1 << 21 ? 64 : 128; }
-
-// Whether every block of rows looks through all ids, or the ids are sorted: WHICH
-bool few(int64_t n, int64_t rows) { return n <= 8192 && rows > 0 && rows <= 16384; }
+// Whether every block of rows looks through all ids, or the ids are sorted.  Rows of 100 fp32, us looked through and sorted:
+//   ids of nodes       600 of 1000  600 of 16 384  2048 of 9000  2048 of 16 384  6000 of 9000  6000 of 16 384  8192 of 1000  16 384 of 1000
+//   drawn evenly        3 and 17      16 and 18      11 and 22     17 and 22       17 and 22     28 and 24        6 and 19     10 and 22
+//   weights 1 / i^1.2   4 and 16      15 and 18      10 and 19     16 and 21       18 and 23     26 and 23       22 and 22     49 and 25
+//   all one node        8 and 14      14 and 18      21 and 20     23 and 21       60 and 19     62 and 19       81 and 17    161 and 22
+bool few(int64_t n, int64_t rows) { return n <= 8192 && rows > 0 && rows <= 16384 && n * rows <= 1 << 26; }
 
 struct Scratch {
   int64_t sorted[2], hist, through, list, counter, partial, bytes;
 };
 Scratch layout(int64_t n, int dim) {
-  const int64_t span = 8 * chunk_of(n), blocks = (n + span - 1) / span;       // of a thread block, at least (8 to 32 groups)
+  const int64_t span = 8 * chunk_of(n, 8), blocks = (n + span - 1) / span;    // of a thread block, at least (8 to 32 groups)
   Scratch s;
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -838,7 +852,6 @@ extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, in
   a.n = (uint32_t)n;
   a.rows = (uint32_t)rows;
   a.dim = dim;
-  a.chunk = chunk_of(n);
   a.scale = scale;
   const uint32_t blocks = out_dtype == TGNN_F32 ? sum_type<float>(c, a) : out_dtype == TGNN_BF16 ? sum_type<__nv_bfloat16>(c, a) : sum_type<__half>(c, a);
   if (blocks > 1) {

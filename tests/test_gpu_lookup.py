@@ -205,3 +205,18 @@ def test_gradients_under_autograd():
     assert wide.grad.shape == (12, 30) and bool((wide.grad[1::2] == 0).all())
     counts = torch.bincount(ids[ids >= 0].long(), minlength=30).float()
     assert torch.equal(wide.grad[0], counts)
+
+
+@pytest.mark.parametrize("n,rows", [(50, 1), (50, 3), (50, 4), (50, 9), (1000, 33), (8192, 8191), (8192, 8192), (8192, 8193), (8193, 8191), (4096, 16_384), (4096, 16_383),
+                                    (4097, 16_384), (64, 16_384), (64, 16_385)])
+@pytest.mark.parametrize("dim,dtype", [(36, F32), (34, F32), (33, BF16), (72, BF16)])
+def test_few_ids_over_few_rows(n, rows, dim, dtype):
+    g = torch.Generator(device="cuda").manual_seed(n + rows)
+    ids = torch.randint(-1, rows, (n,), generator=g, device="cuda")
+    ids[::5] = rows - 1
+    ids[n // 2], ids[0] = (1 << 33) + 1, -(1 << 33)
+    table, dout = make(rows, dim, ids, dtype, dtype)
+    out, dtable, status = both(table, ids, dout, 1.0)
+    check(table, ids, dout, 1.0, out, dtable)
+    assert int(status.item()) == 4
+    assert torch.equal(both(table, ids, dout, 1.0)[1], dtable)
