@@ -19,7 +19,7 @@
 // while weights are formed.  All tiles, in order of A's rows, are split evenly over the blocks: a block's first and last group of rows may be
 // shared with others and go to scratch as parts, which a last kernel joins.
 //
-// bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes: 128 * 17 000 rows of 100 take 3 us).  fp32 rows are split into
+// bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes, or below 64 values).  fp32 rows are split into
 // two fp16 numbers each, hi + lo, after a multiplication by a power of two that puts the matrix's largest magnitude below 2^14: 22 bits for what
 // is within 2^-17 of the largest, and a product takes three passes (hi hi, hi lo, lo hi).  Weights are split the same way, in units that put the
 // largest near 2^15.
@@ -447,7 +447,7 @@ __device__ __forceinline__ void pair_leave(int id) { asm volatile("bar.arrive %0
 //
 // Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), the others form weights, a row per
 // thread, while the other buffer's products run.  With two groups eight warps each do, and a thread has half of a unit's columns (four warps per
-// scheduler hide what two wait for: SPLIT_TIMES); with one group the products take longer than four warps.  P takes the place of the S that it was made of.
+// scheduler hide what two wait for: 4800 roots over 200 000 nodes, rows of 128: forward 430 to 379 us, backward 530 to 457); with one group the products take longer than four warps.  P takes the place of the S that it was made of.
 // 256 x 128 logits of rows of 128 take the tensor cores 2560 cycles (S is bound by shared memory: 48 cycles for 128 x 64 x 16) and the exponentials 2048.
 template <int MODE, int PL, int NH, int NT, int U>
 __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(const __grid_constant__ Main g) {
@@ -1086,8 +1086,9 @@ __device__ __forceinline__ void put_four(void* base, int dtype, int64_t row, int
 
 // What a root's sums make: loss, m, 1 / l, 1 - p and the direction of dq.  L counts in units of 2^shift beside M, o in units of 2^shift and `unit`; own: the
 // target's row.  By a warp, four columns per lane and half.
-__device__ __forceinline__ void finish_root(const Join& a, int i, float M, float L, float zt, float shift, float unit, const float4 (&o)[2],
-                                            const float4 (&own)[2]) {
+template <int H>
+__device__ __forceinline__ void finish_root(const Join& a, int i, float M, float L, float zt, float shift, float unit, const float4 (&o)[H],
+                                            const float4 (&own)[H]) {
   const int lane = threadIdx.x & 31, dim = a.s.dim;
   const float d = (M - zt) + (log2f(L) - shift);          // log2 of the others' weight over the target's
   const bool none = L == 0.f, lost = zt == -INFINITY;
@@ -1120,7 +1121,7 @@ __device__ __forceinline__ void finish_root(const Join& a, int i, float M, float
   }
   if (!a.kept) return;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < H; ++h) {
     const int c = 128 * h + 4 * lane;
     if (c >= dim) break;
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1210,39 +1211,48 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
   finish_root(a, i, M, l, zt, 0.f, 1.f, o, own);
 }
 
-// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn.
-template <int W>
+// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn, 32 at a time: maxima and sums by lane, and the first rows of
+// sums asked for before those are there.  H: halves of 128 columns.
+template <int W, int H>
 __global__ void __launch_bounds__(256, 3) join_roots_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
   __shared__ RootParts<W> s_parts;
+  constexpr int AHEAD = 4 / H;
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t live = a.count[0];
   const int64_t col_tiles = (a.s.rows + a.tile - 1) >> a.tile_bits;
   const Share sh(((live + a.group - 1) >> a.group_bits) * col_tiles, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
-  const float unit = a.s.planes == 2 && a.kept ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
-  const float shift = a.s.planes == 2 && a.kept ? 7.f : 0.f;
+  const bool dir = a.kept != nullptr;
+  const float unit = a.s.planes == 2 && dir ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
+  const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
   for (int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; row < live; row += step) {
     const int64_t r = row >> a.group_bits, in = row - (r << a.group_bits);
     const int i = a.act[row];
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
-    const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
-    const bool dir = a.kept != nullptr;
-    float4 own[2], o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};       // columns 4 lane, 128 + 4 lane
-    if (dir && warp == 0)
+    float4 own[H], o[H];
+    float M = -INFINITY, L = 0.f, zt;
+    auto target = [&]() {
+      const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
+      if (dir && warp == 0)
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
-    float M, L, zt;
+        for (int h = 0; h < H; ++h)
+          if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
+      return y;
+    };
+    int64_t y;
+#pragma unroll
+    for (int h = 0; h < H; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c0 == c1) {
+      y = target();
       M = a.full[3 * row];
       L = a.full[3 * row + 1];
       zt = a.full[3 * row + 2];
       if (dir && warp == 0) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < H; ++h)
           if (128 * h + 4 * lane < dim) o[h] = four_of(a.kept + 3 * a.s.n, TGNN_F32, i, dim, 128 * h + 4 * lane);
       }
     } else {
@@ -1250,65 +1260,95 @@ __global__ void __launch_bounds__(256, 3) join_roots_kernel(const __grid_constan
       const float* first = a.slots + ((int64_t)slot_of(sh, col_tiles, c0, r) * a.group + in) * pitch;
       const float* rest = a.slots + ((int64_t)2 * c0 * a.group + in) * pitch;
       const int64_t apart = 2ll * a.group * pitch;
-      auto part = [&](int k) { return k == 0 ? first : rest + k * apart; };
-      const int parts = c1 - c0 + 1;
-      float m = -INFINITY;
-      for (int k = W == 1 ? lane : (int)threadIdx.x; k < parts; k += 32 * W) m = fmaxf(m, part(k)[od]);
-      const float mine = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[od + 2];
+      const int parts = c1 - c0 + 1, mine = (parts - warp + W - 1) / W;               // this warp's: warp, warp + W, ...
+      auto part = [&](int j) {
+        const int k = warp + j * W;
+        return k == 0 ? first : rest + k * apart;
+      };
+      auto sums = [&](int j, float4 (&v)[H]) {
 #pragma unroll
-      for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, x));
-      if (W > 1) {
-        if (lane == 0) s_parts.m[warp] = m;
-        __syncthreads();
-        for (int w = 0; w < W; ++w) m = fmaxf(m, s_parts.m[w]);
-      }
-      M = m;
-      zt = mine;
-      const float ref = M == -INFINITY ? 0.f : M;
-      float l = 0.f;
-#pragma unroll 4
-      for (int k = warp; k < parts; k += W) {
-        const float* p = part(k);
-        const float4 tail = *reinterpret_cast<const float4*>(p + od);
-        float4 v[2];
+        for (int h = 0; h < H; ++h)
+          if (dir && 128 * h + 4 * lane < od) v[h] = *reinterpret_cast<const float4*>(part(j) + 128 * h + 4 * lane);
+      };
+      for (int j0 = 0; j0 < mine; j0 += 32) {
+        const int here = min(32, mine - j0);
+        float4 tail = make_float4(-INFINITY, 0.f, 0.f, 0.f), v[AHEAD][H];
+        if (lane < here) tail = *reinterpret_cast<const float4*>(part(j0 + lane) + od);
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (dir && 128 * h + 4 * lane < od) v[h] = *reinterpret_cast<const float4*>(p + 128 * h + 4 * lane);
-        const float f = exp2f(tail.x - ref);
-        l = fmaf(tail.y, f, l);
+        for (int j = 0; j < AHEAD; ++j)
+          if (j < here) sums(j0 + j, v[j]);
+        if (j0 == 0) {
+          y = target();
+          const int k = sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0;
+          zt = (k == 0 ? first : rest + k * apart)[od + 2];
+        }
+        float top = tail.x;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          if (dir && 128 * h + 4 * lane < od) {
-            o[h].x = fmaf(v[h].x, f, o[h].x);
-            o[h].y = fmaf(v[h].y, f, o[h].y);
-            o[h].z = fmaf(v[h].z, f, o[h].z);
-            o[h].w = fmaf(v[h].w, f, o[h].w);
+        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, x));
+        top = fmaxf(top, M);
+        const float ref = top == -INFINITY ? 0.f : top, f = exp2f(tail.x - ref), before = exp2f(M - ref);
+        float l = tail.y * f;
+#pragma unroll
+        for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(FULL, l, x);
+        L = j0 == 0 ? l : fmaf(L, before, l);
+        M = top;
+        if (!dir) continue;
+        if (j0 > 0)
+#pragma unroll
+          for (int h = 0; h < H; ++h) o[h] = make_float4(o[h].x * before, o[h].y * before, o[h].z * before, o[h].w * before);
+        for (int j = 0; j < here; j += AHEAD) {
+#pragma unroll
+          for (int u = 0; u < AHEAD; ++u) {
+            const float fu = __shfl_sync(FULL, f, j + u);
+            if (j + u >= here) continue;
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+              if (128 * h + 4 * lane < od) {
+                o[h].x = fmaf(v[u][h].x, fu, o[h].x);
+                o[h].y = fmaf(v[u][h].y, fu, o[h].y);
+                o[h].z = fmaf(v[u][h].z, fu, o[h].z);
+                o[h].w = fmaf(v[u][h].w, fu, o[h].w);
+              }
+            if (j + AHEAD + u < here) sums(j0 + j + AHEAD + u, v[u]);
           }
+        }
       }
-      L = l;
+      if (mine <= 0) {                                    // (fewer parts than warps)
+        y = target();
+        const int k = sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0;
+        zt = (k == 0 ? first : rest + k * apart)[od + 2];
+      }
       if (W > 1) {
-        if (lane == 0) s_parts.l[warp] = l;
-        s_parts.o[warp][lane] = o[0];
-        s_parts.o[warp][32 + lane] = o[1];
+        if (lane == 0) {
+          s_parts.m[warp] = M;
+          s_parts.l[warp] = L;
+        }
+#pragma unroll
+        for (int h = 0; h < H; ++h) s_parts.o[warp][32 * h + lane] = o[h];
         __syncthreads();
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_parts.m[w]);
+        const float ref = M == -INFINITY ? 0.f : M;
         L = 0.f;
-        for (int w = 0; w < W; ++w) L += s_parts.l[w];
-        if (warp == 0)
 #pragma unroll
-          for (int w = 1; w < W; ++w)
+        for (int h = 0; h < H; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < W; ++w) {
+          const float f = exp2f(s_parts.m[w] - ref);
+          L = fmaf(s_parts.l[w], f, L);
+          if (warp == 0)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float4 v = s_parts.o[w][32 * h + lane];
-              o[h].x += v.x;
-              o[h].y += v.y;
-              o[h].z += v.z;
-              o[h].w += v.w;
+            for (int h = 0; h < H; ++h) {
+              const float4 x = s_parts.o[w][32 * h + lane];
+              o[h].x = fmaf(x.x, f, o[h].x);
+              o[h].y = fmaf(x.y, f, o[h].y);
+              o[h].z = fmaf(x.z, f, o[h].z);
+              o[h].w = fmaf(x.w, f, o[h].w);
             }
+        }
         __syncthreads();
       }
     }
     if (__builtin_expect(!(L < INFINITY), 0)) redo_root<W>(a, &s_parts, i, y);
-    else if (warp == 0) finish_root(a, i, M, L, zt, shift, unit, o, own);   // (the next row's first barrier waits for warp 0)
+    else if (warp == 0) finish_root(a, i, M, L, zt, shift, unit, o, own);
   }
 }
 
@@ -1602,8 +1642,11 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   // 24 parts of a root and more: a block each, else a warp.  Us of a loss with what the backward pass needs, a warp and a block per root, rows of 100: 49 parts
   // (600 roots, 9000 nodes, bf16) 58 and 40, 29 (the same in fp32) 50 and 45, 18 (2000 roots, bf16) 45 and 57, (1024 roots, 100 000 nodes, fp32) 176 and 182
   const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
-  if (j.blocks >= 24 * groups) c(join_roots_kernel<8>, dim3((unsigned)(n < most ? n : most)), dim3(256), 0, j);
-  else c(join_roots_kernel<1>, dim3((unsigned)((n + 7) / 8 < most ? (n + 7) / 8 : most)), dim3(256), 0, j);
+  const bool many = j.blocks >= 24 * groups;
+  const int64_t blocks = many ? n : (n + 7) / 8;
+  auto go = [&](auto kernel) { c(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, j); };
+  if (dim <= 128) many ? go(join_roots_kernel<8, 1>) : go(join_roots_kernel<1, 1>);
+  else many ? go(join_roots_kernel<8, 2>) : go(join_roots_kernel<1, 2>);
   return c.end(a.who, err, err_size);
 }
 
