@@ -450,14 +450,16 @@ __device__ __forceinline__ void pair_leave(int id) { asm volatile("bar.arrive %0
 // scheduler hide what two wait for: 4800 roots over 200 000 nodes, rows of 128: forward 430 to 379 us, backward 530 to 457); with one group the products take longer than four warps.  P takes the place of the S that it was made of.
 // 256 x 128 logits of rows of 128 take the tensor cores 2560 cycles (S is bound by shared memory: 48 cycles for 128 x 64 x 16) and the exponentials 2048.
 template <int MODE, int PL, int NH, int NT, int U>
-__global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(const __grid_constant__ Main g) {
+__global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[NH][2], s_pfull[NH][2], s_pv[NH][2];
   __shared__ float s_m[2][NH][128], s_l[NH][128], s_zt[NH][128];   // from one half of a row to the other
+  __shared__ float s_now[2][MODE == FORWARD && PL == 2 ? 128 : 1];
+  __shared__ int s_over[2][2][4];                                  // by unit (even, odd), half and quarter of the rows: a weight has passed what the type holds
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   constexpr int R = 128 * NH, PER = NT / U;            // units per tile
-  constexpr int SPLIT = NH == 2 ? 2 : 1, NC = U / SPLIT, CH = NC / 32;   // threads per row, their columns, in steps of 32
+  constexpr int SPLIT = 2, NC = U / SPLIT, CH = NC / 32;   // threads per row, their columns, in steps of 32
   constexpr int KS = NH == 2 || (PL == 2 && NT == 128) ? 8 : 16;   // steps of 16 in dim, at most
   constexpr bool MOVING = MODE == FORWARD && PL == 2;  // the reference of a row's weights can move
   constexpr int COL_BYTES = (MODE == BACKWARD ? 16 : 4) * NT;
@@ -735,7 +737,11 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
             if (MOVING ? (bool)__any_sync(FULL, m == -INFINITY) : t == 0 && sub == 0) {
               WAIT_LD32(z[0]);
               if (MOVING) {
-                const float top = maximum();
+                float top = maximum();
+                s_m[part][grp][lane_row] = top;          // one reference for both halves of the row
+                ok = pair_sync(pair, abort_flag);
+                if (!ok) break;
+                top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
                 if (m == -INFINITY) m = top;
               } else {
                 have = false;
@@ -746,12 +752,10 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
 #pragma unroll
                   for (int k = 0; k < 32; ++k) top = hit == c + k ? top : fmaxf(top, z[0][k] * factor);
                 }
-                if (SPLIT == 2) {                        // one reference for both halves of the row
-                  s_m[part][grp][lane_row] = top;
-                  ok = pair_sync(pair, abort_flag);
-                  if (!ok) break;
-                  top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
-                }
+                s_m[part][grp][lane_row] = top;
+                ok = pair_sync(pair, abort_flag);
+                if (!ok) break;
+                top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
                 m = most_bias == -INFINITY ? 0.f : top + most_bias;
               }
               TMEM_LD32(z[0], 0, s_addr);
@@ -796,16 +800,30 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
             weights();
             // fp16: the reference is moved when the unit's sum says that a weight may have passed what the type holds.  O has then to be multiplied and the
             // weights are formed again.  (Once: what is too large, or no number, then stays so.)
-            if (MOVING && __builtin_expect(__any_sync(FULL, !(sum <= MOST)), 0)) {
+            // Both halves do it if one has to: O is theirs in common.
+            bool over = false;
+            if (MOVING) {
+              over = __any_sync(FULL, !(sum <= MOST));
+              if (lane == 0) s_over[u & 1][part][quarter] = over;
+              ok = pair_sync(pair, abort_flag);          // (between two writes to one place lies the meeting of the other parity)
+              if (!ok) break;
+              over |= s_over[u & 1][part ^ 1][quarter] != 0;
+            }
+            if (MOVING && __builtin_expect(over, 0)) {
               if (have) WAIT_LD32(z[0]);
-              const float now = fmaxf(m, maximum()), f = now == -INFINITY ? 1.f : exp2f(m - now);
+              float now = fmaxf(m, maximum());
+              s_now[part][lane_row] = now;
+              ok = pair_sync(pair, abort_flag);
+              if (!ok) break;
+              now = fmaxf(now, s_now[part ^ 1][lane_row]);
+              const float f = now == -INFINITY ? 1.f : exp2f(m - now);
               l *= f;
               m = now;
               if (t > 0 || sub > 0) {                    // O is at rest once the unit before has been added
                 ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * (buf ^ 1), ((u - 1) >> 1) & 1, abort_flag));
                 if (!ok) break;
                 fence_after();
-                for (int c = 0; c < g.s.od; c += 32) {   // od in steps of 16: the last step may pass it, inside the group's columns
+                for (int c = 32 * part; c < g.s.od; c += 32 * SPLIT) {   // od in steps of 16: the last step may pass it, inside the group's columns
                   TMEM_LD32(z[0], 0, o_addr + c);
                   WAIT_LD32(z[0]);
 #pragma unroll
@@ -892,11 +910,12 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
           if (MODE != LOSS) {
             if (NC == 32) {
               TMEM_ST16(s_addr, hi, 0);
+              if constexpr (PL == 2) TMEM_ST16(s_addr + NC / 2, lo, 0);
             } else {
 #pragma unroll
               for (int c = 0; c < NC / 2; c += 32) {
                 TMEM_ST32(s_addr + c, hi, c);
-                if (PL == 2) TMEM_ST32(s_addr + NC / 2 + c, lo, c);
+                if constexpr (PL == 2) TMEM_ST32(s_addr + NC / 2 + c, lo, c);
               }
             }
             wait_st();
@@ -915,21 +934,19 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
       // the group's rows are done as far as this block goes
       const bool alone = count == all_cols;
       float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
-      if (SPLIT == 2) {                                  // what the two halves of a row have is put together
-        if (part == 1) {
-          s_l[grp][lane_row] = l;
-          s_zt[grp][lane_row] = zt;
-        }
-        ok = pair_sync(pair, abort_flag);
-        if (!ok) break;
-        if (part == 0) {
-          const float other = s_zt[grp][lane_row];
-          l += s_l[grp][lane_row];
-          if (other != -INFINITY) zt = other;
-        }
-        ok = pair_sync(pair, abort_flag);                // (the next group's values go to the same places)
-        if (!ok) break;
+      if (part == 1) {                                   // what the two halves of a row have is put together
+        s_l[grp][lane_row] = l;
+        s_zt[grp][lane_row] = zt;
       }
+      ok = pair_sync(pair, abort_flag);
+      if (!ok) break;
+      if (part == 0) {
+        const float other = s_zt[grp][lane_row];
+        l += s_l[grp][lane_row];
+        if (other != -INFINITY) zt = other;
+      }
+      ok = pair_sync(pair, abort_flag);                  // (the next group's values go to the same places)
+      if (!ok) break;
       if (valid && part == 0) {
         if (MODE == BACKWARD) {
           if (!alone) slot[g.s.od] = l;
@@ -1003,7 +1020,7 @@ __global__ void __launch_bounds__(NH == 2 ? 640 : 256, 1) destination_kernel(con
         __threadfence_block();
       }
       __syncwarp();
-      if (SPLIT == 2) pair_leave(pair);
+      pair_leave(pair);
     }
   }
   fence_before();
@@ -1477,11 +1494,11 @@ void launch_main(Chain& c, const Main& m, int blocks, size_t smem) {
     c(kernel, dim3(blocks), dim3(threads), smem, m);
   };
   if (m.s.planes == 2) {
-    if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128, 128>, 256);
-    else go(destination_kernel<MODE, 2, 1, 64, 64>, 256);
+    if (m.s.dim <= 128) go(destination_kernel<MODE, 2, 1, 128, 128>, 384);
+    else go(destination_kernel<MODE, 2, 1, 64, 64>, 384);
   } else {
     if (m.s.dim <= 128) go(destination_kernel<MODE, 1, 2, 128, 64>, 640);
-    else go(destination_kernel<MODE, 1, 1, 128, 128>, 256);
+    else go(destination_kernel<MODE, 1, 1, 128, 128>, 384);
   }
 }
 
