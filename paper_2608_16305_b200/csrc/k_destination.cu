@@ -97,7 +97,13 @@ __device__ __forceinline__ float unit_of(float top) {
 // The largest of the partial maxima `which`, by a warp.
 __device__ __forceinline__ float largest(const float* parts, int used, int which) {
   float x = -INFINITY;
-  for (int i = threadIdx.x & 31; i < used; i += 32) x = fmaxf(x, parts[which * kMaxParts + i]);
+  for (int i0 = threadIdx.x & 31; i0 < used; i0 += 256) {
+    float v[8];                                            // (asked for together)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = i0 + 32 * k < used ? parts[which * kMaxParts + i0 + 32 * k] : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x = fmaxf(x, v[k]);
+  }
 #pragma unroll
   for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
   return x;
@@ -261,7 +267,7 @@ struct Main {
   const void* target;
   int index_bits;
   const float* bias;
-  float* slots;              // parts: two per block, [rows of a group][pitch]
+  float* slots;              // parts: two per block, [rows of a group / 4][pitch / 4][4 rows][4 columns]: 64 bytes of neighboring rows side by side
   float* full;               // forward, groups of rows that one block has to itself: {m, l, target's z} of every live root
   float* kept;
   void* dtable;
@@ -933,7 +939,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
       left -= count;
       // the group's rows are done as far as this block goes
       const bool alone = count == all_cols;
-      float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + row_in) * pitch;
+      float* slot = g.slots + ((int64_t)slot_of(sh, col_tiles, blockIdx.x, r) * R + (row_in & ~3)) * pitch + 4 * (row_in & 3);
       if (part == 1) {                                   // what the two halves of a row have is put together
         s_l[grp][lane_row] = l;
         s_zt[grp][lane_row] = zt;
@@ -949,10 +955,10 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
       if (!ok) break;
       if (valid && part == 0) {
         if (MODE == BACKWARD) {
-          if (!alone) slot[g.s.od] = l;
+          if (!alone) slot[4 * g.s.od] = l;
           else if (summed) g.dbias[row] = l / ug;
         } else {
-          float* to = alone ? g.full + 3 * row : slot + g.s.od;
+          float* to = alone ? g.full + 3 * row : slot + 4 * g.s.od;
           to[0] = m;
           to[1] = l;
           to[2] = zt;
@@ -974,11 +980,17 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
           } else if (!alone) {
 #pragma unroll
             for (int k = 0; k < 32; k += 4)
-              if (c + k < g.s.od) *reinterpret_cast<float4*>(slot + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+              if (c + k < g.s.od) *reinterpret_cast<float4*>(slot + 4 * (c + k)) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
           } else if (MODE == FORWARD) {
+            if (((uintptr_t)home & 15) == 0 && dim % 4 == 0) {
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-              if (c + k < dim) home[c + k] = o[k];
+              for (int k = 0; k < 32; k += 4)
+                if (c + k < dim) *reinterpret_cast<float4*>(home + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 32; ++k)
+                if (c + k < dim) home[c + k] = o[k];
+            }
           } else if (g.dtable) {
             if (g.dtype == TGNN_F32) {
               float* to = static_cast<float*>(g.dtable) + row * dim + c;
@@ -993,7 +1005,13 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               }
             } else {
               __nv_bfloat16* to = static_cast<__nv_bfloat16*>(g.dtable) + row * dim + c;
-              if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
+              if (dim % 8 == 0 && ((uintptr_t)g.dtable & 15) == 0) {
+#pragma unroll
+                for (int k = 0; k < 32; k += 8)
+                  if (c + k < dim)
+                    *reinterpret_cast<uint4*>(to + k) = make_uint4(pack_hi<1>(o[k] * out, o[k + 1] * out), pack_hi<1>(o[k + 2] * out, o[k + 3] * out),
+                                                                   pack_hi<1>(o[k + 4] * out, o[k + 5] * out), pack_hi<1>(o[k + 6] * out, o[k + 7] * out));
+              } else if (dim % 4 == 0 && ((uintptr_t)g.dtable & 7) == 0) {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4)
                   if (c + k < dim)
@@ -1101,55 +1119,53 @@ __device__ __forceinline__ void put_four(void* base, int dtype, int64_t row, int
   }
 }
 
-// What a root's sums make: loss, m, 1 / l, 1 - p and the direction of dq.  L counts in units of 2^shift beside M, o in units of 2^shift and `unit`; own: the
-// target's row.  By a warp, four columns per lane and half.
-template <int H>
-__device__ __forceinline__ void finish_root(const Join& a, int i, float M, float L, float zt, float shift, float unit, const float4 (&o)[H],
-                                            const float4 (&own)[H]) {
-  const int lane = threadIdx.x & 31, dim = a.s.dim;
+// What a root's sums make: loss, m, 1 / l, 1 - p.  L counts in units of 2^shift beside M.
+struct Verdict {
+  float loss, miss, m, inv;
+  bool none;
+};
+__device__ __forceinline__ Verdict judge(float M, float L, float zt, float shift) {
+  Verdict v;
   const float d = (M - zt) + (log2f(L) - shift);          // log2 of the others' weight over the target's
-  const bool none = L == 0.f, lost = zt == -INFINITY;
-  float loss, miss, mm, inv;
-  if (none) {                                             // no other node in sight
-    loss = lost ? INFINITY : zt - zt;
-    miss = 0.f;
-    mm = lost ? INFINITY : zt;                            // weights of 0 where nothing is in sight
-    inv = lost ? 0.f : 1.f;
+  const bool lost = zt == -INFINITY;
+  v.none = L == 0.f;
+  if (v.none) {                                           // no other node in sight
+    v.loss = lost ? INFINITY : zt - zt;
+    v.miss = 0.f;
+    v.m = lost ? INFINITY : zt;                           // weights of 0 where nothing is in sight
+    v.inv = lost ? 0.f : 1.f;
   } else if (lost) {
-    loss = INFINITY;
-    miss = 1.f;
-    mm = M;
-    inv = exp2f(shift) / L;
+    v.loss = INFINITY;
+    v.miss = 1.f;
+    v.m = M;
+    v.inv = exp2f(shift) / L;
   } else {
     const float small = exp2f(-fabsf(d));                 // the smaller side over the larger
-    loss = kLn2 * fmaxf(d, 0.f) + log1pf(small);
-    miss = (d > 0.f ? 1.f : small) / (1.f + small);
-    mm = fmaxf(M, zt);
-    inv = 1.f / (exp2f(zt - mm) + L * exp2f((M - mm) - shift));
+    v.loss = kLn2 * fmaxf(d, 0.f) + log1pf(small);
+    v.miss = (d > 0.f ? 1.f : small) / (1.f + small);
+    v.m = fmaxf(M, zt);
+    v.inv = 1.f / (exp2f(zt - v.m) + L * exp2f((M - v.m) - shift));
   }
-  if (d != d && !none && !lost) loss = miss = mm = d;     // NaN stays
-  if (lane == 0) {
-    a.loss[i] = loss;
-    if (a.kept) {
-      a.kept[i] = mm;
-      a.kept[a.s.n + i] = inv;
-      a.kept[2 * a.s.n + i] = miss;
-    }
-  }
+  if (d != d && !v.none && !lost) v.loss = v.miss = v.m = d;   // NaN stays
+  return v;
+}
+__device__ __forceinline__ void put_verdict(const Join& a, int i, const Verdict& v) {
+  a.loss[i] = v.loss;
   if (!a.kept) return;
-#pragma unroll
-  for (int h = 0; h < H; ++h) {
-    const int c = 128 * h + 4 * lane;
-    if (c >= dim) break;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!none) {
-      v.x = (o[h].x / L / unit - own[h].x) * miss;
-      v.y = (o[h].y / L / unit - own[h].y) * miss;
-      v.z = (o[h].z / L / unit - own[h].z) * miss;
-      v.w = (o[h].w / L / unit - own[h].w) * miss;
-    }
-    put_four(a.kept + 3 * a.s.n, TGNN_F32, i, dim, c, v);
+  a.kept[i] = v.m;
+  a.kept[a.s.n + i] = v.inv;
+  a.kept[2 * a.s.n + i] = v.miss;
+}
+// Four columns of the direction of dq; o counts in units of those of L and `unit`, own: the target's row.
+__device__ __forceinline__ void put_direction(const Join& a, int i, int c, const Verdict& v, float4 o, float L, float unit, float4 own) {
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!v.none) {
+    x.x = (o.x / L / unit - own.x) * v.miss;
+    x.y = (o.y / L / unit - own.y) * v.miss;
+    x.z = (o.z / L / unit - own.z) * v.miss;
+    x.w = (o.w / L / unit - own.w) * v.miss;
   }
+  put_four(a.kept + 3 * a.s.n, TGNN_F32, i, a.s.dim, c, x);
 }
 
 template <int W>
@@ -1163,7 +1179,7 @@ template <int W>
 __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, int64_t y) {
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, dim = a.s.dim;
   float M = -INFINITY, l = 0.f, zt = 0.f;
-  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}, own[2];
+  float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
   const float factor = a.scale * kLog2e;
   for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
     const int64_t j = j0 + lane;
@@ -1223,20 +1239,26 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
     __syncthreads();
   }
   if (warp != 0) return;
-  for (int h = 0; h < 2; ++h)
-    if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
-  finish_root(a, i, M, l, zt, 0.f, 1.f, o, own);
+  const Verdict v = judge(M, l, zt, 0.f);
+  if (lane == 0) put_verdict(a, i, v);
+  if (!a.kept) return;
+  for (int h = 0; h < 2; ++h) {
+    const int c = 128 * h + 4 * lane;
+    if (c < dim) put_direction(a, i, c, v, o[h], l, 1.f, four_of(a.table, a.dtype, y, dim, c));
+  }
 }
 
-// W warps per live root (8: a block, where the parts of a root are many) take its parts in turn, 32 at a time: maxima and sums by lane, and the first rows of
-// sums asked for before those are there.  H: halves of 128 columns.
+// W warps (8: a block, where the parts of a root are many) take the parts of four neighboring roots in turn, a few at a time: a lane has one of the roots
+// and every eighth four of its columns.  H: halves of 128 columns.
 template <int W, int H>
-__global__ void __launch_bounds__(256, 3) join_roots_kernel(const __grid_constant__ Join a) {
+__global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
-  __shared__ RootParts<W> s_parts;
-  constexpr int AHEAD = 4 / H;
-  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  constexpr int AHEAD = 4 / H, K = 4 * H;
+  __shared__ RootParts<W> s_root;
+  __shared__ float s_m[W][4], s_l[W][4];
+  __shared__ float4 s_o[W > 1 ? W : 1][W > 1 ? K : 1][32];
+  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, which = lane & 3, c_first = lane >> 2 << 2;
   const int64_t live = a.count[0];
   const int64_t col_tiles = (a.s.rows + a.tile - 1) >> a.tile_bits;
   const Share sh(((live + a.group - 1) >> a.group_bits) * col_tiles, a.blocks);
@@ -1245,127 +1267,126 @@ __global__ void __launch_bounds__(256, 3) join_roots_kernel(const __grid_constan
   const bool dir = a.kept != nullptr;
   const float unit = a.s.planes == 2 && dir ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
   const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
-  for (int64_t row = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; row < live; row += step) {
-    const int64_t r = row >> a.group_bits, in = row - (r << a.group_bits);
-    const int i = a.act[row];
+  for (int64_t four = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; 4 * four < live; four += step) {
+    const int64_t row = 4 * four + which, r = 4 * four >> a.group_bits, in = 4 * four - (r << a.group_bits);
+    const bool valid = row < live;
+    const int i = valid ? a.act[row] : 0;
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
-    float4 own[H], o[H];
-    float M = -INFINITY, L = 0.f, zt;
-    auto target = [&]() {
-      const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
+    float M = -INFINITY, L = 0.f, zt = 0.f;
+    float4 o[K], own[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) o[k] = own[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    int64_t y = 0;
+    if (valid) y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
+    auto targets_row = [&]() {
       if (dir && warp == 0)
 #pragma unroll
-        for (int h = 0; h < H; ++h)
-          if (128 * h + 4 * lane < dim) own[h] = four_of(a.table, a.dtype, y, dim, 128 * h + 4 * lane);
-      return y;
+        for (int k = 0; k < K; ++k)
+          if (c_first + 32 * k < dim) own[k] = four_of(a.table, a.dtype, y, dim, c_first + 32 * k);
     };
-    int64_t y;
-#pragma unroll
-    for (int h = 0; h < H; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c0 == c1) {
-      y = target();
-      M = a.full[3 * row];
-      L = a.full[3 * row + 1];
-      zt = a.full[3 * row + 2];
-      if (dir && warp == 0) {
+      targets_row();
+      if (valid) {
+        M = a.full[3 * row];
+        L = a.full[3 * row + 1];
+        zt = a.full[3 * row + 2];
+        if (dir && warp == 0)
 #pragma unroll
-        for (int h = 0; h < H; ++h)
-          if (128 * h + 4 * lane < dim) o[h] = four_of(a.kept + 3 * a.s.n, TGNN_F32, i, dim, 128 * h + 4 * lane);
+          for (int k = 0; k < K; ++k)
+            if (c_first + 32 * k < dim) o[k] = four_of(a.kept + 3 * a.s.n, TGNN_F32, i, dim, c_first + 32 * k);
       }
     } else {
       // parts lie two places apart, but for the first, which may be its block's last
-      const float* first = a.slots + ((int64_t)slot_of(sh, col_tiles, c0, r) * a.group + in) * pitch;
-      const float* rest = a.slots + ((int64_t)2 * c0 * a.group + in) * pitch;
+      const float* first = a.slots + ((int64_t)slot_of(sh, col_tiles, c0, r) * a.group + in) * pitch + 4 * which;
+      const float* rest = a.slots + ((int64_t)2 * c0 * a.group + in) * pitch + 4 * which;
       const int64_t apart = 2ll * a.group * pitch;
-      const int parts = c1 - c0 + 1, mine = (parts - warp + W - 1) / W;               // this warp's: warp, warp + W, ...
-      auto part = [&](int j) {
-        const int k = warp + j * W;
-        return k == 0 ? first : rest + k * apart;
-      };
-      auto sums = [&](int j, float4 (&v)[H]) {
+      const int parts = c1 - c0 + 1;
+      auto part = [&](int k) { return k == 0 ? first : rest + k * apart; };
+      for (int j0 = warp; j0 < parts; j0 += W * AHEAD) {
+        float4 tail[AHEAD], v[AHEAD][K];
 #pragma unroll
-        for (int h = 0; h < H; ++h)
-          if (dir && 128 * h + 4 * lane < od) v[h] = *reinterpret_cast<const float4*>(part(j) + 128 * h + 4 * lane);
-      };
-      for (int j0 = 0; j0 < mine; j0 += 32) {
-        const int here = min(32, mine - j0);
-        float4 tail = make_float4(-INFINITY, 0.f, 0.f, 0.f), v[AHEAD][H];
-        if (lane < here) tail = *reinterpret_cast<const float4*>(part(j0 + lane) + od);
+        for (int u = 0; u < AHEAD; ++u) {
+          const int j = j0 + u * W;
+          tail[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+          if (j >= parts) continue;
+          const float* p = part(j);
+          tail[u] = *reinterpret_cast<const float4*>(p + 4 * od);
+          if (dir)
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j)
-          if (j < here) sums(j0 + j, v[j]);
-        if (j0 == 0) {
-          y = target();
-          const int k = sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0;
-          zt = (k == 0 ? first : rest + k * apart)[od + 2];
+            for (int k = 0; k < K; ++k)
+              if (c_first + 32 * k < od) v[u][k] = *reinterpret_cast<const float4*>(p + 4 * (c_first + 32 * k));
         }
-        float top = tail.x;
+        if (j0 == warp) {                                 // (asked for behind the first parts)
+          targets_row();
+          zt = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[4 * od + 2];
+        }
+        float top = M;
 #pragma unroll
-        for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, x));
-        top = fmaxf(top, M);
-        const float ref = top == -INFINITY ? 0.f : top, f = exp2f(tail.x - ref), before = exp2f(M - ref);
-        float l = tail.y * f;
-#pragma unroll
-        for (int x = 16; x; x >>= 1) l += __shfl_xor_sync(FULL, l, x);
-        L = j0 == 0 ? l : fmaf(L, before, l);
+        for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, tail[u].x);
+        const float ref = top == -INFINITY ? 0.f : top, before = exp2f(M - ref);
         M = top;
-        if (!dir) continue;
-        if (j0 > 0)
+        L *= before;
 #pragma unroll
-          for (int h = 0; h < H; ++h) o[h] = make_float4(o[h].x * before, o[h].y * before, o[h].z * before, o[h].w * before);
-        for (int j = 0; j < here; j += AHEAD) {
+        for (int k = 0; k < K; ++k) o[k] = make_float4(o[k].x * before, o[k].y * before, o[k].z * before, o[k].w * before);
 #pragma unroll
-          for (int u = 0; u < AHEAD; ++u) {
-            const float fu = __shfl_sync(FULL, f, j + u);
-            if (j + u >= here) continue;
+        for (int u = 0; u < AHEAD; ++u) {
+          if (j0 + u * W >= parts) break;
+          const float f = exp2f(tail[u].x - ref);
+          L = fmaf(tail[u].y, f, L);
+          if (dir)
 #pragma unroll
-            for (int h = 0; h < H; ++h)
-              if (128 * h + 4 * lane < od) {
-                o[h].x = fmaf(v[u][h].x, fu, o[h].x);
-                o[h].y = fmaf(v[u][h].y, fu, o[h].y);
-                o[h].z = fmaf(v[u][h].z, fu, o[h].z);
-                o[h].w = fmaf(v[u][h].w, fu, o[h].w);
+            for (int k = 0; k < K; ++k)
+              if (c_first + 32 * k < od) {
+                o[k].x = fmaf(v[u][k].x, f, o[k].x);
+                o[k].y = fmaf(v[u][k].y, f, o[k].y);
+                o[k].z = fmaf(v[u][k].z, f, o[k].z);
+                o[k].w = fmaf(v[u][k].w, f, o[k].w);
               }
-            if (j + AHEAD + u < here) sums(j0 + j + AHEAD + u, v[u]);
-          }
         }
-      }
-      if (mine <= 0) {                                    // (fewer parts than warps)
-        y = target();
-        const int k = sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0;
-        zt = (k == 0 ? first : rest + k * apart)[od + 2];
       }
       if (W > 1) {
-        if (lane == 0) {
-          s_parts.m[warp] = M;
-          s_parts.l[warp] = L;
+        if (lane < 4) {
+          s_m[warp][lane] = M;
+          s_l[warp][lane] = L;
         }
 #pragma unroll
-        for (int h = 0; h < H; ++h) s_parts.o[warp][32 * h + lane] = o[h];
+        for (int k = 0; k < K; ++k) s_o[warp][k][lane] = o[k];
         __syncthreads();
-        for (int w = 0; w < W; ++w) M = fmaxf(M, s_parts.m[w]);
+        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][which]);
         const float ref = M == -INFINITY ? 0.f : M;
         L = 0.f;
 #pragma unroll
-        for (int h = 0; h < H; ++h) o[h] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < K; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int w = 0; w < W; ++w) {
-          const float f = exp2f(s_parts.m[w] - ref);
-          L = fmaf(s_parts.l[w], f, L);
+          const float f = exp2f(s_m[w][which] - ref);
+          L = fmaf(s_l[w][which], f, L);
           if (warp == 0)
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-              const float4 x = s_parts.o[w][32 * h + lane];
-              o[h].x = fmaf(x.x, f, o[h].x);
-              o[h].y = fmaf(x.y, f, o[h].y);
-              o[h].z = fmaf(x.z, f, o[h].z);
-              o[h].w = fmaf(x.w, f, o[h].w);
+            for (int k = 0; k < K; ++k) {
+              const float4 x = s_o[w][k][lane];
+              o[k].x = fmaf(x.x, f, o[k].x);
+              o[k].y = fmaf(x.y, f, o[k].y);
+              o[k].z = fmaf(x.z, f, o[k].z);
+              o[k].w = fmaf(x.w, f, o[k].w);
             }
         }
         __syncthreads();
       }
     }
-    if (__builtin_expect(!(L < INFINITY), 0)) redo_root<W>(a, &s_parts, i, y);
-    else if (warp == 0) finish_root(a, i, M, L, zt, shift, unit, o, own);
+    const bool lost = valid && !(L < INFINITY);
+    if (warp == 0 && valid && !lost) {
+      const Verdict v = judge(M, L, zt, shift);
+      if (lane < 4) put_verdict(a, i, v);
+      if (dir)
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (c_first + 32 * k < dim) put_direction(a, i, c_first + 32 * k, v, o[k], L, unit, own[k]);
+    }
+    __syncwarp();
+    for (unsigned again = __ballot_sync(FULL, lost && lane < 4); again; again &= again - 1) {
+      const int x = __ffs(again) - 1;
+      redo_root<W>(a, &s_root, __shfl_sync(FULL, i, x), __shfl_sync(FULL, y, x));
+    }
   }
 }
 
@@ -1402,31 +1423,28 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
     ug = 2.f * unit_of(largest(a.parts, a.parts_used, 2));
   }
   const float out = a.scale / ug / uq;
-  const int rows = a.group / (int)gridDim.y, lane = threadIdx.x & 31, od = a.s.od;
-  const int first_slot = slot_of(sh, col_tiles, c0, r);   // the others are their blocks' first
-  for (int k = threadIdx.x >> 5; k < rows; k += 8) {      // a warp per row, four columns per lane
-    const int in = blockIdx.y * rows + k;
-    const int64_t row = r * a.group + in;
-    if (row >= a.s.rows) break;
-    for (int c = 4 * lane; c < od + 4; c += 128) {
-      float4 v = *reinterpret_cast<const float4*>(a.slots + ((int64_t)first_slot * a.group + in) * pitch + c);
+  const int od = a.s.od, chunks = pitch / 4, all = a.group * chunks;
+  // the others than the first part are their blocks' first; all in the order in which they lie
+  const float4* first = reinterpret_cast<const float4*>(a.slots + (int64_t)slot_of(sh, col_tiles, c0, r) * a.group * pitch);
+  const float4* rest = reinterpret_cast<const float4*>(a.slots + (int64_t)2 * c0 * a.group * pitch);
+  const int64_t apart = (int64_t)a.group * pitch / 2;
+  for (int e = blockIdx.y * 256 + threadIdx.x; e < all; e += gridDim.y * 256) {
+    const int fours = e / 4 / chunks, c = 4 * (e / 4 - fours * chunks);
+    const int64_t row = r * a.group + 4 * fours + (e & 3);
+    if (row >= a.s.rows) continue;
+    float4 v = first[e];
 #pragma unroll 4
-      for (int b2 = c0 + 1; b2 <= c1; ++b2) {
-        const float4 w = *reinterpret_cast<const float4*>(a.slots + ((int64_t)2 * b2 * a.group + in) * pitch + c);
-        v.x += w.x;
-        v.y += w.y;
-        v.z += w.z;
-        v.w += w.w;
-      }
-      if (c == od) {
-        if (a.dbias) a.dbias[row] = v.x / ug;
-      } else if (a.dtable) {
-        v.x *= out;
-        v.y *= out;
-        v.z *= out;
-        v.w *= out;
-        put_four(a.dtable, a.dtype, row, dim, c, v);
-      }
+    for (int k = 1; k <= c1 - c0; ++k) {
+      const float4 w = rest[k * apart + e];
+      v.x += w.x;
+      v.y += w.y;
+      v.z += w.z;
+      v.w += w.w;
+    }
+    if (c == od) {
+      if (a.dbias) a.dbias[row] = v.x / ug;
+    } else if (a.dtable) {
+      put_four(a.dtable, a.dtype, row, dim, c, make_float4(v.x * out, v.y * out, v.z * out, v.w * out));
     }
   }
 }
@@ -1660,7 +1678,7 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   // (600 roots, 9000 nodes, bf16) 58 and 40, 29 (the same in fp32) 50 and 45, 18 (2000 roots, bf16) 45 and 57, (1024 roots, 100 000 nodes, fp32) 176 and 182
   const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
   const bool many = j.blocks >= 24 * groups;
-  const int64_t blocks = many ? n : (n + 7) / 8;
+  const int64_t blocks = many ? (n + 3) / 4 : (n + 31) / 32;
   auto go = [&](auto kernel) { c(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, j); };
   if (dim <= 128) many ? go(join_roots_kernel<8, 1>) : go(join_roots_kernel<1, 1>);
   else many ? go(join_roots_kernel<8, 2>) : go(join_roots_kernel<1, 2>);
