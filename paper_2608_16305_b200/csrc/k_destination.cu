@@ -1249,22 +1249,22 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
 }
 
 // W warps (8: a block, where the parts of a root are many) take the parts of four neighboring roots in turn, a few at a time: a lane has one of the roots
-// and every eighth four of its columns.  H: halves of 128 columns.
+// and every eighth four of its columns.  H: halves of 128 columns, 0 where the loss alone is wanted.
 template <int W, int H>
 __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
-  constexpr int AHEAD = 4 / H, K = 4 * H;
+  constexpr int AHEAD = H == 0 ? 4 : 2 / H, K = 4 * H;     // (four parts ahead leave no room in registers: 600 roots 38 us in place of 36)
+  constexpr bool dir = H > 0;
   __shared__ RootParts<W> s_root;
   __shared__ float s_m[W][4], s_l[W][4];
-  __shared__ float4 s_o[W > 1 ? W : 1][W > 1 ? K : 1][32];
+  __shared__ float4 s_o[W > 1 ? W : 1][W > 1 && H > 0 ? K : 1][32];
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, which = lane & 3, c_first = lane >> 2 << 2;
   const int64_t live = a.count[0];
   const int64_t col_tiles = (a.s.rows + a.tile - 1) >> a.tile_bits;
   const Share sh(((live + a.group - 1) >> a.group_bits) * col_tiles, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
-  const bool dir = a.kept != nullptr;
   const float unit = a.s.planes == 2 && dir ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
   const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
   for (int64_t four = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; 4 * four < live; four += step) {
@@ -1273,12 +1273,12 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
     const int i = valid ? a.act[row] : 0;
     const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
     float M = -INFINITY, L = 0.f, zt = 0.f;
-    float4 o[K], own[K];
+    float4 o[dir ? K : 1], own[dir ? K : 1];
 #pragma unroll
     for (int k = 0; k < K; ++k) o[k] = own[k] = make_float4(0.f, 0.f, 0.f, 0.f);
     int64_t y = 0;
-    if (valid) y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
     auto targets_row = [&]() {
+      if (valid) y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
       if (dir && warp == 0)
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -1302,8 +1302,9 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
       const int64_t apart = 2ll * a.group * pitch;
       const int parts = c1 - c0 + 1;
       auto part = [&](int k) { return k == 0 ? first : rest + k * apart; };
+      if (warp >= parts) targets_row();
       for (int j0 = warp; j0 < parts; j0 += W * AHEAD) {
-        float4 tail[AHEAD], v[AHEAD][K];
+        float4 tail[AHEAD], v[AHEAD][dir ? K : 1];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
           const int j = j0 + u * W;
@@ -1674,13 +1675,15 @@ extern "C" TGNN_API int tgnn_destination_loss(const void* q, const void* table, 
   Join j;
   const int rc = kept ? run<FORWARD>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j) : run<LOSS>(a, c, loss, kept, nullptr, nullptr, nullptr, nullptr, &j);
   if (rc) return rc;
-  // 24 parts of a root and more: a block each, else a warp.  Us of a loss with what the backward pass needs, a warp and a block per root, rows of 100: 49 parts
-  // (600 roots, 9000 nodes, bf16) 58 and 40, 29 (the same in fp32) 50 and 45, 18 (2000 roots, bf16) 45 and 57, (1024 roots, 100 000 nodes, fp32) 176 and 182
+  // 16 parts of a root and more: a block for four roots, else a warp.  Us of a loss with what the backward pass needs, a warp and a block, rows of 100: 49 parts
+  // (600 roots, 9000 nodes, bf16) 50 and 31, 29 (the same in fp32) 46 and 36, 18 (2000 roots, bf16) 39 and 40, (1024 roots, 100 000 nodes, fp32) 181 and 174,
+  // 9 (2000 roots, 9000 nodes, fp32) 52 and 55, 8 (4800 roots, 17 000 nodes, bf16) 61 and 81
   const int64_t groups = (n + j.group - 1) / j.group, most = 8 * num_sms();
-  const bool many = j.blocks >= 24 * groups;
+  const bool many = j.blocks >= 16 * groups;
   const int64_t blocks = many ? (n + 3) / 4 : (n + 31) / 32;
   auto go = [&](auto kernel) { c(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, j); };
-  if (dim <= 128) many ? go(join_roots_kernel<8, 1>) : go(join_roots_kernel<1, 1>);
+  if (!kept) many ? go(join_roots_kernel<8, 0>) : go(join_roots_kernel<1, 0>);
+  else if (dim <= 128) many ? go(join_roots_kernel<8, 1>) : go(join_roots_kernel<1, 1>);
   else many ? go(join_roots_kernel<8, 2>) : go(join_roots_kernel<1, 2>);
   return c.end(a.who, err, err_size);
 }
