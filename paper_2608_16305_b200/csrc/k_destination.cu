@@ -1429,23 +1429,33 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
   const float4* first = reinterpret_cast<const float4*>(a.slots + (int64_t)slot_of(sh, col_tiles, c0, r) * a.group * pitch);
   const float4* rest = reinterpret_cast<const float4*>(a.slots + (int64_t)2 * c0 * a.group * pitch);
   const int64_t apart = (int64_t)a.group * pitch / 2;
-  for (int e = blockIdx.y * 256 + threadIdx.x; e < all; e += gridDim.y * 256) {
-    const int fours = e / 4 / chunks, c = 4 * (e / 4 - fours * chunks);
-    const int64_t row = r * a.group + 4 * fours + (e & 3);
-    if (row >= a.s.rows) continue;
-    float4 v = first[e];
-#pragma unroll 4
+  const int stride = gridDim.y * 256;
+  for (int e0 = blockIdx.y * 256 + threadIdx.x; e0 < all; e0 += 4 * stride) {               // four at a time
+    float4 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = e0 + q * stride < all ? first[e0 + q * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
     for (int k = 1; k <= c1 - c0; ++k) {
-      const float4 w = rest[k * apart + e];
-      v.x += w.x;
-      v.y += w.y;
-      v.z += w.z;
-      v.w += w.w;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (e0 + q * stride >= all) continue;
+        const float4 w = rest[k * apart + e0 + q * stride];
+        v[q].x += w.x;
+        v[q].y += w.y;
+        v[q].z += w.z;
+        v[q].w += w.w;
+      }
     }
-    if (c == od) {
-      if (a.dbias) a.dbias[row] = v.x / ug;
-    } else if (a.dtable) {
-      put_four(a.dtable, a.dtype, row, dim, c, make_float4(v.x * out, v.y * out, v.z * out, v.w * out));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int e = e0 + q * stride, fours = e / 4 / chunks, c = 4 * (e / 4 - fours * chunks);
+      const int64_t row = r * a.group + 4 * fours + (e & 3);
+      if (e >= all || row >= a.s.rows) continue;
+      if (c == od) {
+        if (a.dbias) a.dbias[row] = v[q].x / ug;
+      } else if (a.dtable) {
+        put_four(a.dtable, a.dtype, row, dim, c, make_float4(v[q].x * out, v[q].y * out, v[q].z * out, v[q].w * out));
+      }
     }
   }
 }
