@@ -274,7 +274,7 @@ struct Main {
   float* dbias;
   int dtype;
   float scale;
-  int chunks, ksteps, stages, ahead;   // chunks of 64 columns in shared memory, steps of 16 of a product over dim
+  int chunks, ksteps, stages, ahead, extra;   // chunks of 64 columns in shared memory, steps of 16 of a product over dim
   int32_t* status;
 };
 
@@ -379,19 +379,25 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers from 0; a division of 64 bits takes five times as long
   return (((uint64_t)a | (uint64_t)b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// The blocks' shares of the tiles: block c has tiles [begin(c), begin(c + 1)), and tile x belongs to block owner(x).
+// The blocks' shares of the tiles: block c has tiles [begin(c), begin(c + 1)), and tile o of group r belongs to block owner(r, o).  Shares are even with
+// `extra` tiles more in front of each group's: what its block needs to write one group and begin the next.
 struct Share {
-  int64_t total, per;
-  int blocks, more;                          // blocks with a tile at least; the first `more` have per + 1, the others per
-  __device__ __forceinline__ Share(int64_t t, int launched) : total(t), per(0), blocks((int)min(t, (int64_t)launched)), more(0) {
+  int64_t tiles, wide, per;                  // of a group, without and with the extra ones; of a block
+  int blocks, more;                          // blocks that have a share; the first `more` have per + 1, the others per
+  int extra;
+  __device__ __forceinline__ Share(int64_t groups, int64_t col_tiles, int extra_tiles, int launched)
+      : tiles(col_tiles), wide(col_tiles + extra_tiles), per(0), blocks((int)min(groups * col_tiles, (int64_t)launched)), more(0), extra(extra_tiles) {
     if (blocks > 0) {
-      per = quotient(t, blocks);
-      more = (int)(t - per * blocks);
+      per = quotient(groups * wide, blocks);
+      more = (int)(groups * wide - per * blocks);
     }
   }
-  __device__ __forceinline__ int64_t begin(int c) const { return per * c + min(c, more); }
-  __device__ __forceinline__ int owner(int64_t x) const {
-    const int64_t edge = more * (per + 1);
+  __device__ __forceinline__ int64_t begin(int c) const {
+    const int64_t x = per * c + min(c, more), r = quotient(x, wide), o = x - r * wide - extra;
+    return r * tiles + (o < 0 ? 0 : o);
+  }
+  __device__ __forceinline__ int owner(int64_t r, int64_t o) const {
+    const int64_t x = r * wide + extra + o, edge = more * (per + 1);
     return x < edge ? (int)quotient(x, per + 1) : more + (int)quotient(x - edge, per);
   }
 };
@@ -509,15 +515,15 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
   const int64_t live = g.count[0];
   const int64_t a_rows = MODE == BACKWARD ? g.s.rows : live, t_rows = MODE == BACKWARD ? live : g.s.rows;
   const int64_t col_tiles = (t_rows + NT - 1) / NT;
-  const Share sh((a_rows + R - 1) / R * col_tiles, gridDim.x);
-  const bool idle = (int)blockIdx.x >= sh.blocks;
-  const int64_t x0 = idle ? 0 : sh.begin(blockIdx.x), x1 = idle ? 0 : sh.begin(blockIdx.x + 1);
+  const Share sh((a_rows + R - 1) / R, col_tiles, g.extra, gridDim.x);
+  const int64_t x0 = (int)blockIdx.x >= sh.blocks ? 0 : sh.begin(blockIdx.x), x1 = (int)blockIdx.x >= sh.blocks ? 0 : sh.begin(blockIdx.x + 1);
+  const bool idle = x0 == x1;
   const int64_t r0 = idle ? 0 : quotient(x0, col_tiles), j0 = idle ? 0 : x0 - r0 * col_tiles;       // the first tile: group of rows, and tile of columns
   const uint32_t tiles = (uint32_t)(x1 - x0);
   const uint32_t o_base = tmem + 2 * NH * U;
 
   if (idle) {
-    // fewer tiles than blocks
+    // fewer tiles than blocks (or a share of extra ones)
   } else if (warp == 0) {
     // ---------------------------------------------------------------- copies
     if (lane == 0) {
@@ -1066,7 +1072,7 @@ struct Join {
   const float* bias;
   const void* target;
   int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles (powers of two)
-  int group_bits, tile_bits;
+  int group_bits, tile_bits, extra;
   float scale;
   float* loss;
   float* kept;
@@ -1262,7 +1268,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, which = lane & 3, c_first = lane >> 2 << 2;
   const int64_t live = a.count[0];
   const int64_t col_tiles = (a.s.rows + a.tile - 1) >> a.tile_bits;
-  const Share sh(((live + a.group - 1) >> a.group_bits) * col_tiles, a.blocks);
+  const Share sh((live + a.group - 1) >> a.group_bits, col_tiles, a.extra, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
   const float unit = a.s.planes == 2 && dir ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
@@ -1271,7 +1277,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
     const int64_t row = 4 * four + which, r = 4 * four >> a.group_bits, in = 4 * four - (r << a.group_bits);
     const bool valid = row < live;
     const int i = valid ? a.act[row] : 0;
-    const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
+    const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
     float M = -INFINITY, L = 0.f, zt = 0.f;
     float4 o[dir ? K : 1], own[dir ? K : 1];
 #pragma unroll
@@ -1319,7 +1325,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         }
         if (j0 == warp) {                                 // (asked for behind the first parts)
           targets_row();
-          zt = part(sh.owner(r * col_tiles + (y >> a.tile_bits)) - c0)[4 * od + 2];
+          zt = part(sh.owner(r, y >> a.tile_bits) - c0)[4 * od + 2];
         }
         float top = M;
 #pragma unroll
@@ -1411,12 +1417,12 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
     return;
   }
   const int64_t col_tiles = (live + a.tile - 1) / a.tile;
-  const Share sh((a.s.rows + a.group - 1) / a.group * col_tiles, a.blocks);
+  const Share sh((a.s.rows + a.group - 1) / a.group, col_tiles, a.extra, a.blocks);
   const int b = blockIdx.x + 1;
   if (b >= sh.blocks) return;
   const int64_t x = sh.begin(b), r = quotient(x, col_tiles);
   if (x == r * col_tiles) return;
-  const int c0 = sh.owner(r * col_tiles), c1 = sh.owner((r + 1) * col_tiles - 1);
+  const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
   if (b != c0 + 1) return;
   float uq = 1.f, ug = 1.f;
   if (a.s.planes == 2) {
@@ -1637,6 +1643,10 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   c(prep_kernel, dim3((unsigned)(work / 16 >= 8 * sms ? 8 * sms : work / 16 + 1)), dim3(256), 0, p);
   const int64_t r_tiles = ((MODE == BACKWARD ? a.rows : a.n) + f.group - 1) / f.group, c_tiles = ((MODE == BACKWARD ? a.n : a.rows) + f.tile - 1) / f.tile;
   const int blocks = (int)(r_tiles * c_tiles < sms ? r_tiles * c_tiles : sms);
+  // Extra tiles of a group, where a block has several tiles.  Us of the forward pass with 0 / 1 / 2 / 3 / 4 of them, rows of 100 in bf16: 4000 roots over 17 000
+  // nodes 58.1 / 56.0 / 54.0 / 54.3 / 54.2, 12 000 roots 124 / 117 / 116 / 112 / 112, 30 000 roots over 2000 nodes 93 / 92 / 93 / 92 / 102; fp32, 2000 roots over
+  // 50 000 nodes, both passes 312 / 309 / 309 / 312 / 315.
+  m.extra = r_tiles * c_tiles < 8 * blocks ? 0 : s.planes == 2 ? 2 : 3;
   launch_main<MODE>(c, m, blocks, smem);
   *j = Join{};
   j->s = s;
@@ -1657,6 +1667,7 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->tile = f.tile;
   j->group_bits = f.group == 256 ? 8 : 7;
   j->tile_bits = f.tile == 128 ? 7 : 6;
+  j->extra = m.extra;
   j->scale = a.scale;
   j->loss = loss;
   j->kept = kept;
