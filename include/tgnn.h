@@ -614,7 +614,8 @@ TGNN_API int tgnn_slot_attend_backward(const void* q, const void* k, const void*
  * What trains a table with one row per node: its rows are looked up by id (neighbor slots, roots), every root is scored against all
  * rows (which node comes next, instead of one sampled negative), and all tensors are stepped at once.
  * Stateless, device pointers (except *_host), work enqueued on `stream` of the current device, nothing allocated; errors as above.
- * status: device int32, NOT zeroed by these calls; 4 is recorded for an index beyond its table.  A scratch buffer (256-byte aligned) belongs to
+ * status: device int32, NOT zeroed by these calls; 4 is recorded for an index beyond its table (and TGNN_ETIMEOUT by the destination loss where a
+ * bounded wait on the device expired: its results are then worthless).  A scratch buffer (256-byte aligned) belongs to
  * the call until the call's work has ended (calls that may overlap, two captured graphs among them, need one each); contents undefined after.
  *
  * tgnn_lookup: out[i] = scale * table[ids[i]], i < n.  table: [rows, dim] of `dtype`, out: [n, dim] of `out_dtype` (TGNN_F32, TGNN_BF16,
@@ -643,7 +644,7 @@ TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, int64_t n, co
  *   0xC2B2AE3D27D4EB4F: bits 0-15 for m and 16-31 for u of even elements, 32-47 and 48-63 of odd ones.  So a value's mean is itself.
  *   A block below 2^-60 is held as zeros, one with an infinity or a NaN reads back as NaN, all of it.
  * tgnn_adamw_moments: m and v of states in 8 bits as fp32 values (m_out_host, v_out_host: a device pointer per tensor; param, grad, copy unused).
- * Tensors of no elements are passed over.  Up to 2^20 tensors. */
+ * Tensors of no elements are passed over; a call with nothing else is no step.  Up to 2^20 tensors, none overlapping another. */
 typedef struct tgnn_adamw_tensor {
   float* param;
   const void* grad;
