@@ -565,12 +565,21 @@ __global__ void __launch_bounds__(32 * kJoinWarps) run_join_kernel(const SumArgs
       }
     }
     uint32_t heads = __ffs(ends);
-    if (ends == 0)                                                             // there was no room to put it aside
-      for (heads = 17; c0 + heads < chunks && a.through[c0 + heads]; ++heads) {}
     float x[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = 0.f;
-    if (active) {
+    if (ends == 0) {                                                           // there was no room to put it aside: the same sums in the same order
+      for (heads = 17; c0 + heads < chunks && a.through[c0 + heads]; ++heads) {}
+      for (int w = 0; w < kJoinWarps && active; ++w) {
+        float y[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = 0.f;
+        if (w == 0) add_part<V>(a.partial + ((int64_t)2 * c0 + 1) * a.dim + col, y);
+        for (uint32_t h = 1 + w; h <= heads && c0 + h < chunks; h += kJoinWarps) add_part<V>(a.partial + (int64_t)2 * (c0 + h) * a.dim + col, y);
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = w ? x[i] + y[i] : y[i];
+      }
+    } else if (active) {
       add_part<V>(a.partial + ((int64_t)2 * c0 + 1) * a.dim + col, x);
 #pragma unroll 8
       for (uint32_t h = 1; h <= heads; ++h) add_part<V>(a.partial + (int64_t)2 * (c0 + h) * a.dim + col, x);
