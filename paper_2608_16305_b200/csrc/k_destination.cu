@@ -14,9 +14,9 @@
 // accuracy (a loss of 1e-9 is one; a weight rounded to bf16 would leave 2^-8 of it where 1 - p belongs).
 //
 // One kernel does both directions.  A thread block holds 128 or 256 rows of one matrix (A) in shared memory and walks tiles of 128 (64) rows of the
-// other (T): S = A T' on the tensor cores into tensor memory, weights P from S in registers (a thread has a row), P back to
+// other (T): S = A T' on the tensor cores into tensor memory, weights P from S in registers (two threads have a row), P back to
 // tensor memory, O += P T with the same tile as the second operand.  Two groups of 128 rows (or two buffers of S) keep the tensor cores busy
-// while weights are formed.  All tiles, in order of A's rows, are split evenly over the blocks: a block's first and last group of rows may be
+// while weights are formed.  All tiles, in order of A's rows, are split over the blocks: a block's first and last group of rows may be
 // shared with others and go to scratch as parts, which a last kernel joins.
 //
 // bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes, or below 64 values).  fp32 rows are split into
@@ -457,10 +457,11 @@ __device__ __forceinline__ void pair_leave(int id) { asm volatile("bar.arrive %0
 // MODE; PL planes per operand (2: fp32 rows); NH groups of 128 rows of A; NT rows of T per tile in shared memory; U columns of S at a time, two
 // buffers of them per group.
 //
-// Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), the others form weights, a row per
-// thread, while the other buffer's products run.  With two groups eight warps each do, and a thread has half of a unit's columns (four warps per
-// scheduler hide what two wait for: 4800 roots over 200 000 nodes, rows of 128: forward 430 to 379 us, backward 530 to 457); with one group the products take longer than four warps.  P takes the place of the S that it was made of.
-// 256 x 128 logits of rows of 128 take the tensor cores 2560 cycles (S is bound by shared memory: 48 cycles for 128 x 64 x 16) and the exponentials 2048.
+// Warps: 0 copies, 1 and 2 issue matrix instructions (one per group of rows, so that neither group waits for the other), the others form weights while the
+// other buffer's products run: eight warps per group of rows, two threads per row, each with half of a unit's columns (one thread per row: 4800 roots over
+// 200 000 nodes, rows of 128 in bf16, forward 430 us and backward 530; two: 379 and 457, and 365 and 430 with what came after).  P takes the place of the S
+// that it was made of.  256 x 128 logits of rows of 128 take the tensor cores 2560 cycles (S is bound by shared memory: 48 cycles for 128 x 64 x 16) and the
+// exponentials 2048: the tensor pipe is 72 % active forward and 60 % backward, where groups change five times as often and a weight takes a factor more.
 template <int MODE, int PL, int NH, int NT, int U>
 __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __grid_constant__ Main g) {
   extern __shared__ unsigned char smem_raw[];
@@ -643,7 +644,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
     }
     __syncwarp();
   } else if (warp >= 4) {
-    // ---------------------------------------------------------------- weights: a thread has a row of A
+    // ---------------------------------------------------------------- weights: two threads have a row of A
     const int grp = (warp - 4) / (4 * SPLIT), part = (warp - 4) / 4 % SPLIT, quarter = warp & 3;
     const int pair = 1 + 4 * grp + quarter;              // the named barrier of the two warps with these rows
     const int lane_row = 32 * quarter + lane, row_in = 128 * grp + lane_row;

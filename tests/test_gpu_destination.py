@@ -378,3 +378,11 @@ def test_only_some_leaves_and_an_eager_step_beside_a_captured_one():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(g, captured) and torch.equal(g, warm)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,rows,masked", [(61_000, 600, 0.999), (61_000, 600, 0.5), (1300, 40_000, 0.2), (1300, 40_000, 0.99)])
+def test_uneven_shares(n, rows, masked, dtype):
+    """Walks long enough that a change of groups counts in the blocks' shares, and so few roots that some shares are nothing else."""
+    x = make(n, rows, 40, dtype, masked=masked)
+    check(x, call(x))
