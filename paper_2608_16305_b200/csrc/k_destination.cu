@@ -94,19 +94,39 @@ __device__ __forceinline__ float unit_of(float top) {
   frexpf(fminf(top, 3e38f), &e);
   return ldexpf(1.f, max(-110, min(110, 14 - e)));
 }
-// The largest of the partial maxima `which`, by a warp.
-__device__ __forceinline__ float largest(const float* parts, int used, int which) {
-  float x = -INFINITY;
+// The largest of the partial maxima first, first + 1, ..., by a warp; all asked for together.
+template <int N>
+__device__ __forceinline__ void largest(const float* parts, int used, int first, float (&x)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) x[n] = -INFINITY;
   for (int i0 = threadIdx.x & 31; i0 < used; i0 += 256) {
-    float v[8];                                            // (asked for together)
+    float v[N][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = i0 + 32 * k < used ? parts[which * kMaxParts + i0 + 32 * k] : -INFINITY;
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x = fmaxf(x, v[k]);
+      for (int k = 0; k < 8; ++k) v[n][k] = i0 + 32 * k < used ? parts[(first + n) * kMaxParts + i0 + 32 * k] : -INFINITY;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[n] = fmaxf(x[n], v[n][k]);
   }
 #pragma unroll
-  for (int o = 16; o; o >>= 1) x = fmaxf(x, __shfl_xor_sync(FULL, x, o));
-  return x;
+  for (int o = 16; o; o >>= 1)
+#pragma unroll
+    for (int n = 0; n < N; ++n) x[n] = fmaxf(x[n], __shfl_xor_sync(FULL, x[n], o));
+}
+__device__ __forceinline__ float largest(const float* parts, int used, int which) {
+  float x[1];
+  largest(parts, used, which, x);
+  return x[0];
+}
+// What fp32 rows (and the gradients of losses) are multiplied by.
+__device__ __forceinline__ void units(const float* parts, int used, bool backward, float& q, float& table, float& g) {
+  float x[3];
+  largest(parts, used, 0, x);
+  q = unit_of(x[0]);
+  table = unit_of(x[1]);
+  g = backward ? 2.f * unit_of(x[2]) : 1.f;              // |g| up to 2^15
 }
 
 // Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows and the largest bias, and form dq.
@@ -208,11 +228,7 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
   const int64_t live = a.count[0], padded = up(live, 128);
   const bool split = a.s.planes == 2;
   float uq = 1.f, ut = 1.f, ug = 1.f;
-  if (split) {
-    uq = unit_of(largest(a.parts, a.parts_used, 0));
-    ut = unit_of(largest(a.parts, a.parts_used, 1));
-    if (a.backward) ug = 2.f * unit_of(largest(a.parts, a.parts_used, 2));         // |g| up to 2^15
-  }
+  if (split) units(a.parts, a.parts_used, a.backward, uq, ut, ug);
   const int dp = a.s.dp, dim = a.s.dim;
   auto operand = [&](const void* src, int64_t row, uint16_t* to, float unit) {     // a row, 2 values at a time
     for (int c = 2 * lane; c < dp; c += 64) {
@@ -653,11 +669,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
     const uint32_t bar_s = smem_u32(&s_sfull[grp][0]), bar_p = smem_u32(&s_pfull[grp][0]), bar_pv = smem_u32(&s_pv[grp][0]);
     const int pitch = pitch_of(g.s);
     float uq = 1.f, ut = 1.f, ug = 1.f;
-    if (PL == 2) {
-      uq = unit_of(largest(g.parts, g.parts_used, 0));
-      ut = unit_of(largest(g.parts, g.parts_used, 1));
-      if (MODE == BACKWARD) ug = 2.f * unit_of(largest(g.parts, g.parts_used, 2));
-    }
+    if (PL == 2) units(g.parts, g.parts_used, MODE == BACKWARD, uq, ut, ug);
     const float most_bias = MODE != BACKWARD && !MOVING && g.bias ? bias2(largest(g.parts, g.parts_used, 3)) : 0.f;
     const float factor = g.scale * kLog2e / uq / ut;
     const f32x2 factor2 = pack2(factor, factor);
@@ -745,8 +757,8 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               return top;
             };
             // The reference of a row's weights.  Where it can move: the maximum of the first unit in which the row sees anything.  Else the
-            // largest product of the first unit (the target's apart) plus the largest bias of all, for good: below the row's maximum by no more than the products' spread, whatever the
-            // biases hide, and fp32 and bf16 hold weights that pass it by 2^127 (88 in natural units).  A row that goes beyond is done again by the last kernel.
+            // largest product of the first unit (the target's apart) plus the largest bias of all, for good: below the row's maximum by no more than the
+            // products' spread, whatever the biases hide, and fp32 and bf16 hold weights that pass it by 2^127 (88 in natural units).  A row that goes beyond is done again by the last kernel.
             if (MOVING ? (bool)__any_sync(FULL, m == -INFINITY) : t == 0 && sub == 0) {
               WAIT_LD32(z[0]);
               if (MOVING) {
@@ -1127,12 +1139,12 @@ __device__ __forceinline__ void put_four(void* base, int dtype, int64_t row, int
 }
 
 // What a root's sums make: loss, m, 1 / l, 1 - p.  L counts in units of 2^shift beside M.
-struct Verdict {
+struct Outcome {
   float loss, miss, m, inv;
   bool none;
 };
-__device__ __forceinline__ Verdict judge(float M, float L, float zt, float shift) {
-  Verdict v;
+__device__ __forceinline__ Outcome outcome_of(float M, float L, float zt, float shift) {
+  Outcome v;
   const float d = (M - zt) + (log2f(L) - shift);          // log2 of the others' weight over the target's
   const bool lost = zt == -INFINITY;
   v.none = L == 0.f;
@@ -1156,7 +1168,7 @@ __device__ __forceinline__ Verdict judge(float M, float L, float zt, float shift
   if (d != d && !v.none && !lost) v.loss = v.miss = v.m = d;   // NaN stays
   return v;
 }
-__device__ __forceinline__ void put_verdict(const Join& a, int i, const Verdict& v) {
+__device__ __forceinline__ void put_outcome(const Join& a, int i, const Outcome& v) {
   a.loss[i] = v.loss;
   if (!a.kept) return;
   a.kept[i] = v.m;
@@ -1164,7 +1176,7 @@ __device__ __forceinline__ void put_verdict(const Join& a, int i, const Verdict&
   a.kept[2 * a.s.n + i] = v.miss;
 }
 // Four columns of the direction of dq; o counts in units of those of L and `unit`, own: the target's row.
-__device__ __forceinline__ void put_direction(const Join& a, int i, int c, const Verdict& v, float4 o, float L, float unit, float4 own) {
+__device__ __forceinline__ void put_direction(const Join& a, int i, int c, const Outcome& v, float4 o, float L, float unit, float4 own) {
   float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
   if (!v.none) {
     x.x = (o.x / L / unit - own.x) * v.miss;
@@ -1246,8 +1258,8 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
     __syncthreads();
   }
   if (warp != 0) return;
-  const Verdict v = judge(M, l, zt, 0.f);
-  if (lane == 0) put_verdict(a, i, v);
+  const Outcome v = outcome_of(M, l, zt, 0.f);
+  if (lane == 0) put_outcome(a, i, v);
   if (!a.kept) return;
   for (int h = 0; h < 2; ++h) {
     const int c = 128 * h + 4 * lane;
@@ -1272,7 +1284,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   const Share sh((live + a.group - 1) >> a.group_bits, col_tiles, a.extra, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
-  const float unit = a.s.planes == 2 && dir ? unit_of(largest(a.parts, a.parts_used, 1)) : 1.f;
+  float unit = a.s.planes == 2 && dir ? 0.f : 1.f;        // 0: not looked for so far
   const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
   for (int64_t four = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; 4 * four < live; four += step) {
     const int64_t row = 4 * four + which, r = 4 * four >> a.group_bits, in = 4 * four - (r << a.group_bits);
@@ -1381,10 +1393,11 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         __syncthreads();
       }
     }
+    if (unit == 0.f) unit = unit_of(largest(a.parts, a.parts_used, 1));
     const bool lost = valid && !(L < INFINITY);
     if (warp == 0 && valid && !lost) {
-      const Verdict v = judge(M, L, zt, shift);
-      if (lane < 4) put_verdict(a, i, v);
+      const Outcome v = outcome_of(M, L, zt, shift);
+      if (lane < 4) put_outcome(a, i, v);
       if (dir)
 #pragma unroll
         for (int k = 0; k < K; ++k)
@@ -1425,11 +1438,8 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
   if (x == r * col_tiles) return;
   const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
   if (b != c0 + 1) return;
-  float uq = 1.f, ug = 1.f;
-  if (a.s.planes == 2) {
-    uq = unit_of(largest(a.parts, a.parts_used, 0));
-    ug = 2.f * unit_of(largest(a.parts, a.parts_used, 2));
-  }
+  float uq = 1.f, ut = 1.f, ug = 1.f;
+  if (a.s.planes == 2) units(a.parts, a.parts_used, true, uq, ut, ug);
   const float out = a.scale / ug / uq;
   const int od = a.s.od, chunks = pitch / 4, all = a.group * chunks;
   // the others than the first part are their blocks' first; all in the order in which they lie
