@@ -67,7 +67,7 @@ struct Prep {
   int backward, tile;
   int32_t* count;                            // [0]: roots that take part
   int32_t* act;                              // their indices
-  float* parts;                              // largest magnitudes of [q, table, dloss] and the largest bias, [4][kMaxParts]
+  float* parts;                              // largest magnitudes of [q, table, dloss] and the largest bias, [4][kMaxParts], and what the later kernels make of them
   int parts_used;
   uint16_t* qp;
   uint16_t* tp;
@@ -94,39 +94,25 @@ __device__ __forceinline__ float unit_of(float top) {
   frexpf(fminf(top, 3e38f), &e);
   return ldexpf(1.f, max(-110, min(110, 14 - e)));
 }
-// The largest of the partial maxima first, first + 1, ..., by a warp; all asked for together.
-template <int N>
-__device__ __forceinline__ void largest(const float* parts, int used, int first, float (&x)[N]) {
+// The largest of the partial maxima of each kind, by a warp; all asked for together.
+__device__ __forceinline__ void largest(const float* parts, int used, float (&x)[4]) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) x[n] = -INFINITY;
+  for (int n = 0; n < 4; ++n) x[n] = -INFINITY;
   for (int i0 = threadIdx.x & 31; i0 < used; i0 += 256) {
-    float v[N][8];
+    float v[4][8];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[n][k] = i0 + 32 * k < used ? parts[(first + n) * kMaxParts + i0 + 32 * k] : -INFINITY;
+      for (int k = 0; k < 8; ++k) v[n][k] = i0 + 32 * k < used ? parts[n * kMaxParts + i0 + 32 * k] : -INFINITY;
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[n] = fmaxf(x[n], v[n][k]);
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1)
 #pragma unroll
-    for (int n = 0; n < N; ++n) x[n] = fmaxf(x[n], __shfl_xor_sync(FULL, x[n], o));
-}
-__device__ __forceinline__ float largest(const float* parts, int used, int which) {
-  float x[1];
-  largest(parts, used, which, x);
-  return x[0];
-}
-// What fp32 rows (and the gradients of losses) are multiplied by.
-__device__ __forceinline__ void units(const float* parts, int used, bool backward, float& q, float& table, float& g) {
-  float x[3];
-  largest(parts, used, 0, x);
-  q = unit_of(x[0]);
-  table = unit_of(x[1]);
-  g = backward ? 2.f * unit_of(x[2]) : 1.f;              // |g| up to 2^15
+    for (int n = 0; n < 4; ++n) x[n] = fmaxf(x[n], __shfl_xor_sync(FULL, x[n], o));
 }
 
 // Roots that take part, in order, by the first block; the others find the largest magnitudes of fp32 rows and the largest bias, and form dq.
@@ -228,7 +214,14 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
   const int64_t live = a.count[0], padded = up(live, 128);
   const bool split = a.s.planes == 2;
   float uq = 1.f, ut = 1.f, ug = 1.f;
-  if (split) units(a.parts, a.parts_used, a.backward, uq, ut, ug);
+  float x[4];
+  if (split || blockIdx.x == 0) largest(a.parts, a.parts_used, x);
+  if (split) {
+    uq = unit_of(x[0]);
+    ut = unit_of(x[1]);
+    if (a.backward) ug = 2.f * unit_of(x[2]);            // |g| up to 2^15
+  }
+  if (blockIdx.x == 0 && t == 0) *reinterpret_cast<float4*>(a.parts + 4 * kMaxParts) = make_float4(uq, ut, ug, bias2(x[3]));
   const int dp = a.s.dp, dim = a.s.dim;
   auto operand = [&](const void* src, int64_t row, uint16_t* to, float unit) {     // a row, 2 values at a time
     for (int c = 2 * lane; c < dp; c += 64) {
@@ -278,7 +271,6 @@ struct Main {
   const int32_t* count;
   const int32_t* act;
   const float* parts;
-  int parts_used;
   const float* cols;
   const void* target;
   int index_bits;
@@ -668,9 +660,14 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
     const uint32_t o_addr = o_base + grp * 128 + lane_base, s_base = tmem + 2 * grp * U + part * NC + lane_base;
     const uint32_t bar_s = smem_u32(&s_sfull[grp][0]), bar_p = smem_u32(&s_pfull[grp][0]), bar_pv = smem_u32(&s_pv[grp][0]);
     const int pitch = pitch_of(g.s);
-    float uq = 1.f, ut = 1.f, ug = 1.f;
-    if (PL == 2) units(g.parts, g.parts_used, MODE == BACKWARD, uq, ut, ug);
-    const float most_bias = MODE != BACKWARD && !MOVING && g.bias ? bias2(largest(g.parts, g.parts_used, 3)) : 0.f;
+    float uq = 1.f, ut = 1.f, ug = 1.f, most_bias = 0.f;
+    if (PL == 2 || MODE != BACKWARD) {
+      const float4 x = *reinterpret_cast<const float4*>(g.parts + 4 * kMaxParts);
+      uq = x.x;
+      ut = x.y;
+      ug = x.z;
+      if (MODE != BACKWARD && !MOVING && g.bias) most_bias = x.w;
+    }
     const float factor = g.scale * kLog2e / uq / ut;
     const f32x2 factor2 = pack2(factor, factor);
     const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
@@ -1077,7 +1074,6 @@ struct Join {
   const int32_t* count;
   const int32_t* act;
   const float* parts;
-  int parts_used;
   const float* slots;
   const float* full;
   const void* q;
@@ -1284,7 +1280,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   const Share sh((live + a.group - 1) >> a.group_bits, col_tiles, a.extra, a.blocks);
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
-  float unit = a.s.planes == 2 && dir ? 0.f : 1.f;        // 0: not looked for so far
+  const float unit = a.parts[4 * kMaxParts + 1];
   const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
   for (int64_t four = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; 4 * four < live; four += step) {
     const int64_t row = 4 * four + which, r = 4 * four >> a.group_bits, in = 4 * four - (r << a.group_bits);
@@ -1393,7 +1389,6 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         __syncthreads();
       }
     }
-    if (unit == 0.f) unit = unit_of(largest(a.parts, a.parts_used, 1));
     const bool lost = valid && !(L < INFINITY);
     if (warp == 0 && valid && !lost) {
       const Outcome v = outcome_of(M, L, zt, shift);
@@ -1438,9 +1433,8 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
   if (x == r * col_tiles) return;
   const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
   if (b != c0 + 1) return;
-  float uq = 1.f, ut = 1.f, ug = 1.f;
-  if (a.s.planes == 2) units(a.parts, a.parts_used, true, uq, ut, ug);
-  const float out = a.scale / ug / uq;
+  const float4 units = *reinterpret_cast<const float4*>(a.parts + 4 * kMaxParts);
+  const float uq = units.x, ug = units.z, out = a.scale / ug / uq;
   const int od = a.s.od, chunks = pitch / 4, all = a.group * chunks;
   // the others than the first part are their blocks' first; all in the order in which they lie
   const float4* first = reinterpret_cast<const float4*>(a.slots + (int64_t)slot_of(sh, col_tiles, c0, r) * a.group * pitch);
@@ -1506,7 +1500,7 @@ Layout layout(const Shape& s, int dtype) {
   };
   l.count = take(4);
   l.act = take(4 * s.n);
-  l.parts = take(4ll * 4 * kMaxParts);
+  l.parts = take(4ll * (4 * kMaxParts + 4));
   l.qp = take(2ll * up(s.n, 128) * s.planes * s.dp);
   l.tp = take(2ll * s.rows * s.planes * s.dp);
   const int64_t forward = 4ll * up(s.rows, f.tile), backward = 16ll * up(s.n, f.tile);
@@ -1648,7 +1642,7 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   // blocks beside the first one: some 4096 values each
   const int64_t beside = s.planes == 2 ? a.rows * a.dim + (dq ? a.n * a.dim : 0) : dq ? a.n * a.dim : MODE != BACKWARD && a.bias ? a.rows : 0;
   const int blocks_of_parts = beside == 0 ? 0 : (int)(beside >> 12 >= kMaxParts - 1 ? kMaxParts - 1 : (beside >> 12) + 1);
-  p.parts_used = m.parts_used = blocks_of_parts;
+  p.parts_used = blocks_of_parts;
   c(begin_kernel, dim3(1 + blocks_of_parts), dim3(1024), 0, p);
   const int64_t work = (direct ? 0 : a.rows) + a.n + (MODE == BACKWARD ? a.n : a.rows) / 32;
   c(prep_kernel, dim3((unsigned)(work / 16 >= 8 * sms ? 8 * sms : work / 16 + 1)), dim3(256), 0, p);
@@ -1664,7 +1658,6 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->count = p.count;
   j->act = p.act;
   j->parts = p.parts;
-  j->parts_used = p.parts_used;
   j->slots = m.slots;
   j->full = m.full;
   j->q = a.q;
