@@ -162,3 +162,8 @@ def test_captured_and_replayed(bits):
     assert opt.steps.tolist() == twin.steps.tolist() == [4, 0]
     for a, b in zip(params + opt.m + opt.v, twin_p + twin.m + twin.v):
         assert torch.equal(a, b)
+
+
+def test_many_values_in_8_bits():
+    """So many values that a thread block takes more of them."""
+    test_steps_against_the_definition([9_800_001, 300, 4097], torch.bfloat16, 8)

@@ -220,3 +220,14 @@ def test_few_ids_over_few_rows(n, rows, dim, dtype):
     check(table, ids, dout, 1.0, out, dtable)
     assert int(status.item()) == 4
     assert torch.equal(both(table, ids, dout, 1.0)[1], dtable)
+
+
+@pytest.mark.parametrize("n,dim", [(70_001, 100), (140_001, 100), (530_001, 100), (530_001, 128), (530_001, 33)])
+@pytest.mark.parametrize("kind", ["hubs", "even"])
+def test_chunks_of_every_size(n, dim, kind):
+    g = torch.Generator(device="cuda").manual_seed(n + dim)
+    at = torch.rand(n, generator=g, device="cuda")
+    ids = ((at ** 6 if kind == "hubs" else at) * 700).long().clamp(max=699)
+    table, dout = make(700, dim, ids, F32, F32)
+    out, dtable, _ = both(table, ids, dout, 1.0)
+    check(table, ids, dout, 1.0, out, dtable)
