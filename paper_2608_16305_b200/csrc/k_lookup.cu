@@ -17,6 +17,7 @@ namespace {
 constexpr int kSortThreads = 1024;
 constexpr int kMaxSortBlocks = 148;
 constexpr int kDigits = 256;
+constexpr int kMaxPasses = 4;
 
 // ------------------------------------------------------------------------------------------------------------ forward --
 struct GatherArgs {
@@ -88,7 +89,9 @@ struct SortArgs {
   uint32_t n;
   const uint2* in;        // (id, place) of the pass before; nullptr: the ids themselves
   uint2* out;
-  uint32_t* hist;         // [sort blocks][kDigits]
+  uint32_t* hist;         // [sort blocks][kDigits]: of this pass
+  uint32_t* next_hist;    // of the next one, counted as keys are moved; nullptr: there is none
+  int later_words;        // words of those of all later passes, which lie one behind the other: zeroed by the first kernel
   int32_t* status;        // checked on the first look at the ids; nullptr afterwards
   uint32_t* counter;      // zeroed by the first kernel
   int shift, width;       // the digit
@@ -183,7 +186,7 @@ __device__ __forceinline__ void scan_digits(const uint32_t* total, uint32_t* bas
   __syncthreads();
 }
 
-// Per digit, a kernel that counts the digits of every block's share and one that moves the keys.
+// A kernel counts the first digits of every block's share, and one per digit moves the keys and counts the next digits where they come to lie.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs a) {
   __shared__ uint32_t count[kDigits];
   chain_wait();
@@ -196,6 +199,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
   const uint32_t mask = (1u << a.width) - 1;
   if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.counter = 0;
+  for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < a.later_words; i += a.sort_blocks * kSortThreads) a.next_hist[i] = 0;
   __syncthreads();
   constexpr int K = 4;
   for (uint32_t tile = lo; tile < hi; tile += K * kSortThreads) {
@@ -203,7 +207,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const SortArgs
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const uint32_t i = tile + k * kSortThreads + threadIdx.x;
-      d[k] = i < hi ? ((a.in ? a.in[i].x : key_of(a, i)) >> a.shift) & mask : kDigits;
+      d[k] = i < hi ? key_of(a, i) & mask : kDigits;
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -265,8 +269,18 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(const SortArgs 
     __syncthreads();
     scan_warps(counts, part, total);
 #pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (digit[k] < kDigits) a.out[base[digit[k]] + counts[warp][digit[k]] + rank[k]] = kp[k];
+    for (int k = 0; k < K; ++k) {
+      uint32_t counted = 0xffffffffu;
+      if (digit[k] < kDigits) {
+        const uint32_t to = base[digit[k]] + counts[warp][digit[k]] + rank[k];
+        a.out[to] = kp[k];
+        if (a.next_hist) counted = to / a.per_block * kDigits + ((kp[k].x >> (a.shift + a.width)) & mask);
+      }
+      if (a.next_hist) {                                                       // whole numbers: the order of additions does not matter
+        const unsigned same = __match_any_sync(FULL, counted);
+        if (lane == __ffs(same) - 1 && counted != 0xffffffffu) atomicAdd(a.next_hist + counted, __popc(same));
+      }
+    }
     __syncthreads();
     if (t < kDigits) base[t] += total[t];
     __syncthreads();
@@ -729,7 +743,7 @@ Scratch layout(int64_t n, int dim) {
   };
   s.sorted[0] = take(8 * n);
   s.sorted[1] = take(8 * n);
-  s.hist = take(4ll * kMaxSortBlocks * kDigits);
+  s.hist = take(4ll * kMaxPasses * kMaxSortBlocks * kDigits);
   s.through = take(blocks);
   s.list = take(4 * blocks);
   s.counter = take(4);
@@ -832,18 +846,26 @@ extern "C" TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, in
   const int64_t tiles = (n + kSortThreads - 1) / kSortThreads;                 // few ids: a key per thread, so that a block's work is short
   s.sort_blocks = (int)(tiles < kMaxSortBlocks ? tiles : kMaxSortBlocks);
   s.per_block = (uint32_t)((n + s.sort_blocks - 1) / s.sort_blocks);
-  s.shares = 2 * passes;
+  s.shares = passes + 1;
+  const int words = s.sort_blocks * kDigits;
+  s.later_words = (passes - 1) * words;
   int sorted = 0;
   for (int p = 0; p < passes; ++p) {
     s.shift = p * s.width;
     s.in = p ? reinterpret_cast<uint2*>(base + l.sorted[sorted]) : nullptr;
     sorted = p & 1;
     s.out = reinterpret_cast<uint2*>(base + l.sorted[sorted]);
-    s.share = 2 * p;
     const dim3 grid(s.sort_blocks + fillers), block(kSortThreads);
-    c(sort_count_kernel, grid, block, 0, s);
-    s.share = 2 * p + 1;
-    s.status = nullptr;
+    if (p == 0) {
+      s.share = 0;
+      s.next_hist = s.hist + words;
+      c(sort_count_kernel, grid, block, 0, s);
+      s.status = nullptr;
+    } else {
+      s.hist += words;
+    }
+    s.next_hist = p + 1 < passes ? s.hist + words : nullptr;
+    s.share = p + 1;
     if (s.per_block <= 1024) c(sort_move_kernel<1>, grid, block, 0, s);
     else if (s.per_block <= 2048) c(sort_move_kernel<2>, grid, block, 0, s);
     else if (s.per_block <= 4096) c(sort_move_kernel<4>, grid, block, 0, s);
