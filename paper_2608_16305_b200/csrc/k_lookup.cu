@@ -2,7 +2,7 @@
 //
 // out[i] = scale * table[ids[i]] is a gather: bytes of the distinct rows and of the output bound it.  The gradient,
 // dtable[r] = scale * sum of dout[i] over ids[i] = r, is summed in a fixed order instead of by atomics: ids are sorted with their places
-// (least digit first, 8 bits at most at a time, stable), and runs of equal ids in the sorted order are summed.  Chunks of that order go to groups of
+// (least digit first, 8 bits at most at a time, stable, a kernel per digit), and runs of equal ids in the sorted order are summed.  Chunks of that order go to groups of
 // lanes; what runs have in neighboring chunks is added up within a thread block, in order, and a run across blocks leaves one partial sum per block, which a
 // last kernel adds in order.  Rows that no id names are zeros: the blocks beside the sorting ones write them while the sort, which waits on latency, runs.
 // Few ids over few rows are not sorted: the blocks, each with some rows of the table, look through all of them.
@@ -445,7 +445,7 @@ __global__ void __launch_bounds__(256) run_sum_kernel(const SumArgs a) {
 }
 
 // Few ids and few rows: a thread block per `kRows` rows of the table and slice of 32 * V columns looks through all ids, every warp an equal part of them, adds
-// up what it finds of its rows in shared memory, in order, and the parts of the warps are added in order.  One kernel in place of a sort's five.  The rows of
+// up what it finds of its rows in shared memory, in order, and the parts of the warps are added in order.  One kernel in place of a sort's three or four and the sums' two.  The rows of
 // a block are as far apart as there are blocks: hubs often have neighboring numbers.
 struct FewArgs {
   const void* ids;
@@ -673,8 +673,8 @@ void gather_out(Chain& c, const GatherArgs& a, int out_dtype, int bits) {
 
 // Ids per group of lanes, with `groups` of them in a thread block: few enough that the groups fill the device, and 1024 or more in a block where there are
 // many, so that hubs leave few parts (rows of 100 fp32, 8 groups, chunks of 16 / 32 / 64 / 128 in us, ids of 17 000 nodes drawn with weights 1 / i^1.2:
-// 2^16 ids 37 / 38 / 39 / 48, 2^17 61 / 46 / 49 / 56, 2^18 114 / 87 / 73 / 74, 2^20 326 / 249 / 210 / 186, 2^22 1133 / 824 / 670 / 597; drawn evenly
-// 2^16 32 / 32 / 34 / 41, 2^20 175 / 171 / 169 / 174).
+// 2^16 ids 34 / 36 / 38 / 46, 2^17 58 / 44 / 47 / 59, 2^18 110 / 84 / 70 / 69, 2^20 326 / 249 / 209 / 186, 2^22 1144 / 830 / 676 / 605; drawn evenly
+// 2^16 33 / 33 / 38 / 45, 2^20 174 / 170 / 167 / 172).
 int chunk_of(int64_t n, int groups) { return n <= 1 << 16 ? 16 : n <= 1 << 17 ? 32 : n <= 1 << 19 || groups > 8 ? 64 : 128; }
 
 template <typename T, int V>
@@ -724,9 +724,9 @@ void few_type(Chain& c, const FewArgs& a) {
 
 // Whether every block of rows looks through all ids, or the ids are sorted.  Rows of 100 fp32, us looked through and sorted:
 //   ids of nodes       600 of 1000  600 of 16 384  2048 of 9000  2048 of 16 384  6000 of 9000  6000 of 16 384  8192 of 1000  16 384 of 1000
-//   drawn evenly        3 and 17      16 and 18      11 and 22     17 and 22       17 and 22     28 and 24        6 and 19     10 and 22
-//   weights 1 / i^1.2   4 and 16      15 and 18      10 and 19     16 and 21       18 and 23     26 and 23       22 and 22     49 and 25
-//   all one node        8 and 14      14 and 18      21 and 20     23 and 21       60 and 19     62 and 19       81 and 17    161 and 22
+//   drawn evenly        3 and 17      16 and 17      11 and 21     18 and 21       17 and 22     28 and 22        6 and 20     10 and 22
+//   weights 1 / i^1.2   4 and 16      15 and 17      10 and 18     16 and 18       18 and 21     26 and 20       23 and 21     49 and 24
+//   all one node        8 and 15      14 and 16      21 and 18     23 and 19       60 and 17     62 and 18       81 and 18    161 and 21
 bool few(int64_t n, int64_t rows) { return n <= 8192 && rows > 0 && rows <= 16384 && n * rows <= 1 << 26; }
 
 struct Scratch {
