@@ -34,11 +34,13 @@ namespace {
 
 constexpr unsigned kSpin = 1u << 22;
 constexpr int kMaxBlocks = 160;             // thread blocks of the main kernel, one per multiprocessor
-constexpr int kSmem = 222 * 1024;           // dynamic shared memory; the static part is up to 5 KB
+constexpr int kSmem = 220 * 1024;           // dynamic shared memory; the static part is up to 7 KB
 constexpr int kMaxParts = 592;              // partial maxima: of fp32 rows, of the bias
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.40282347e38f;
+constexpr float kRoom = 60.f;               // a row's sum of weights is trusted within 2^-60 and 2^60 of its reference
+constexpr float kLeast = 8.6736174e-19f;    // 2^-60
 
 enum Mode { LOSS = 0, FORWARD = 1, BACKWARD = 2 };
 
@@ -475,6 +477,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t s_full[4], s_empty[4], s_afull, s_aempty, s_sfull[NH][2], s_pfull[NH][2], s_pv[NH][2];
   __shared__ float s_m[2][NH][128], s_l[NH][128], s_zt[NH][128];   // from one half of a row to the other
+  __shared__ float s_product[MODE == BACKWARD || (MODE == FORWARD && PL == 2) ? 1 : 2][NH][128];
   __shared__ float s_now[2][MODE == FORWARD && PL == 2 ? 128 : 1];
   __shared__ int s_over[2][2][4];                                  // by unit (even, odd), half and quarter of the rows: a weight has passed what the type holds
   __shared__ uint32_t s_tmem;
@@ -753,9 +756,10 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               }
               return top;
             };
-            // The reference of a row's weights.  Where it can move: the maximum of the first unit in which the row sees anything.  Else the
-            // largest product of the first unit (the target's apart) plus the largest bias of all, for good: below the row's maximum by no more than the
-            // products' spread, whatever the biases hide, and fp32 and bf16 hold weights that pass it by 2^127 (88 in natural units).  A row that goes beyond is done again by the last kernel.
+            // The reference of a row's weights.  Where it can move: the maximum of the first unit in which the row sees anything.  Else, for good, the maximum
+            // of the first unit (the target's apart); where biases hide most of that unit it would lie far below the others, and the largest product plus the
+            // largest bias of all is taken: right within the products' spread, whatever the biases hide.  A row for which neither is right is seen by the
+            // last kernel, in its sums, and done again there.
             if (MOVING ? (bool)__any_sync(FULL, m == -INFINITY) : t == 0 && sub == 0) {
               WAIT_LD32(z[0]);
               if (MOVING) {
@@ -766,25 +770,37 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
                 top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
                 if (m == -INFINITY) m = top;
               } else {
+                const int there = (int32_t)t_rows - (int32_t)(j * NT + sub * U + part * NC);   // columns that are nodes
                 have = false;
-                float top = -INFINITY;
+                float seen = -INFINITY, product = -INFINITY;
                 for (int c = 0; c < NC; c += 32) {
                   TMEM_LD32(z[0], 0, s_addr + c);
                   WAIT_LD32(z[0]);
+                  if (biased && (any_hit || j >= full_tiles)) {
+                    __syncwarp();                        // (a branch)
 #pragma unroll
-                  for (int k = 0; k < 32; ++k) top = hit == c + k ? top : fmaxf(top, z[0][k] * factor);
+                    for (int k = 0; k < 32; ++k) product = hit == c + k || c + k >= there ? product : fmaxf(product, z[0][k] * factor);
+                  } else if (biased) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) product = fmaxf(product, z[0][k] * factor);
+                  }
+                  logits(z[0], c, 0.f);
+#pragma unroll
+                  for (int k = 0; k < 32; ++k) seen = fmaxf(seen, z[0][k]);
                 }
-                s_m[part][grp][lane_row] = top;
+                s_m[part][grp][lane_row] = seen;
+                s_product[part][grp][lane_row] = product;
                 ok = pair_sync(pair, abort_flag);
                 if (!ok) break;
-                top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
-                m = most_bias == -INFINITY ? 0.f : top + most_bias;
+                seen = fmaxf(seen, s_m[part ^ 1][grp][lane_row]);
+                product = fmaxf(product, s_product[part ^ 1][grp][lane_row]) + most_bias;
+                m = !biased || !(seen < product - kRoom / 2) ? seen : product;    // -infinity: the target alone, or nothing at all
               }
               TMEM_LD32(z[0], 0, s_addr);
             }
             float sum;
             auto weights = [&]() {
-              const float ref = MOVING && m == -INFINITY ? 0.f : m;
+              const float ref = m == -INFINITY ? 0.f : m;
               const f32x2 shift2 = pack2(SHIFT, SHIFT);
               f32x2 sum2 = pack2(0.f, 0.f), sum3 = sum2;
 #pragma unroll
@@ -1189,7 +1205,7 @@ struct RootParts {                                        // of the warps that s
   float4 o[W][64];
 };
 
-// A root with a weight that has passed what fp32 holds (or a value that is no number): again, product by product, 32 nodes at a time per warp.
+// A root whose weights do not fit beside their references (or a value that is no number): again, product by product, 32 nodes at a time per warp.
 template <int W>
 __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, int64_t y) {
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, dim = a.s.dim;
@@ -1272,7 +1288,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   constexpr int AHEAD = H == 0 ? 4 : 2 / H, K = 4 * H;     // (four parts ahead leave no room in registers: 600 roots 38 us in place of 36)
   constexpr bool dir = H > 0;
   __shared__ RootParts<W> s_root;
-  __shared__ float s_m[W][4], s_l[W][4];
+  __shared__ float s_m[W][4], s_l[W][4], s_high[W][4];
   __shared__ float4 s_o[W > 1 ? W : 1][W > 1 && H > 0 ? K : 1][32];
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, which = lane & 3, c_first = lane >> 2 << 2;
   const int64_t live = a.count[0];
@@ -1288,6 +1304,15 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
     const int i = valid ? a.act[row] : 0;
     const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
     float M = -INFINITY, L = 0.f, zt = 0.f;
+    float high = -INFINITY;                               // the highest reference beside which there is nothing; +infinity: a sum too small to be trusted
+    auto look = [&](float& m, float l) {                  // a part of no weight does not count with its reference
+      if (l == 0.f) {
+        high = fmaxf(high, m);
+        m = -INFINITY;
+      } else if (l < kLeast) {
+        high = INFINITY;
+      }
+    };
     float4 o[dir ? K : 1], own[dir ? K : 1];
 #pragma unroll
     for (int k = 0; k < K; ++k) o[k] = own[k] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1305,6 +1330,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         M = a.full[3 * row];
         L = a.full[3 * row + 1];
         zt = a.full[3 * row + 2];
+        look(M, L);
         if (dir && warp == 0)
 #pragma unroll
           for (int k = 0; k < K; ++k)
@@ -1338,7 +1364,10 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         }
         float top = M;
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, tail[u].x);
+        for (int u = 0; u < AHEAD; ++u) {
+          look(tail[u].x, tail[u].y);
+          top = fmaxf(top, tail[u].x);
+        }
         const float ref = top == -INFINITY ? 0.f : top, before = exp2f(M - ref);
         M = top;
         L *= before;
@@ -1364,11 +1393,15 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         if (lane < 4) {
           s_m[warp][lane] = M;
           s_l[warp][lane] = L;
+          s_high[warp][lane] = high;
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) s_o[warp][k][lane] = o[k];
         __syncthreads();
-        for (int w = 0; w < W; ++w) M = fmaxf(M, s_m[w][which]);
+        for (int w = 0; w < W; ++w) {
+          M = fmaxf(M, s_m[w][which]);
+          high = fmaxf(high, s_high[w][which]);
+        }
         const float ref = M == -INFINITY ? 0.f : M;
         L = 0.f;
 #pragma unroll
@@ -1389,7 +1422,8 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         __syncthreads();
       }
     }
-    const bool lost = valid && !(L < INFINITY);
+    // Weights below 2^-126 of a reference were left out: where it lies so far above the root's sum that they may count, they are missing.
+    const bool lost = valid && (!(L < INFINITY) || high > M + log2f(L) + kRoom);
     if (warp == 0 && valid && !lost) {
       const Outcome v = outcome_of(M, L, zt, shift);
       if (lane < 4) put_outcome(a, i, v);
