@@ -39,8 +39,10 @@ constexpr int kMaxParts = 592;              // partial maxima: of fp32 rows, of 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLowest = -3.40282347e38f;
-constexpr float kRoom = 60.f;               // a row's sum of weights is trusted within 2^-60 and 2^60 of its reference
+constexpr float kRoom = 60.f;               // a row's sum of weights is trusted within 2^-60 and 2^60 of its reference: sums of rows up to 2^67 fit beside
+                                            // it, and gradients down to 2^-66 times its inverse
 constexpr float kLeast = 8.6736174e-19f;    // 2^-60
+constexpr float kMost = 1.1529215e18f;      // 2^60
 
 enum Mode { LOSS = 0, FORWARD = 1, BACKWARD = 2 };
 
@@ -1289,6 +1291,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   constexpr bool dir = H > 0;
   __shared__ RootParts<W> s_root;
   __shared__ float s_m[W][4], s_l[W][4], s_high[W][4];
+  __shared__ unsigned s_again;
   __shared__ float4 s_o[W > 1 ? W : 1][W > 1 && H > 0 ? K : 1][32];
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, which = lane & 3, c_first = lane >> 2 << 2;
   const int64_t live = a.count[0];
@@ -1304,12 +1307,12 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
     const int i = valid ? a.act[row] : 0;
     const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
     float M = -INFINITY, L = 0.f, zt = 0.f;
-    float high = -INFINITY;                               // the highest reference beside which there is nothing; +infinity: a sum too small to be trusted
+    float high = -INFINITY;                               // the highest reference beside which there is nothing; +infinity: a sum that is not trusted
     auto look = [&](float& m, float l) {                  // a part of no weight does not count with its reference
       if (l == 0.f) {
         high = fmaxf(high, m);
         m = -INFINITY;
-      } else if (l < kLeast) {
+      } else if (l < kLeast || l > kMost) {
         high = INFINITY;
       }
     };
@@ -1422,9 +1425,26 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
         __syncthreads();
       }
     }
-    // Weights below 2^-126 of a reference were left out: where it lies so far above the root's sum that they may count, they are missing.
-    const bool lost = valid && (!(L < INFINITY) || high > M + log2f(L) + kRoom);
-    if (warp == 0 && valid && !lost) {
+    // Done again: where weights below 2^-126 of a reference, which were left out, lie so near the root's sum that they may count; where sums are not trusted,
+    // those of the table's rows among them, which can pass fp32 before the weights' do.  (What is no number stays so.)
+    bool lost = high == INFINITY || high > M + log2f(L) + kRoom;
+    if (dir && warp == 0 && L == L) {
+      float size = 0.f;
+#pragma unroll
+      for (int k = 0; k < K; ++k) size += fabsf(o[k].x) + fabsf(o[k].y) + fabsf(o[k].z) + fabsf(o[k].w);
+      lost |= !(size < INFINITY);
+    }
+    unsigned again = __ballot_sync(FULL, valid && lost);
+    again |= again >> 16;
+    again |= again >> 8;
+    again = (again | again >> 4) & 15u;                   // of the four roots
+    if (W > 1) {
+      if (threadIdx.x == 0) s_again = again;
+      __syncthreads();
+      again = s_again;
+      __syncthreads();
+    }
+    if (warp == 0 && valid && !(again >> which & 1)) {
       const Outcome v = outcome_of(M, L, zt, shift);
       if (lane < 4) put_outcome(a, i, v);
       if (dir)
@@ -1433,7 +1453,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
           if (c_first + 32 * k < dim) put_direction(a, i, c_first + 32 * k, v, o[k], L, unit, own[k]);
     }
     __syncwarp();
-    for (unsigned again = __ballot_sync(FULL, lost && lane < 4); again; again &= again - 1) {
+    for (; again; again &= again - 1) {
       const int x = __ffs(again) - 1;
       redo_root<W>(a, &s_root, __shfl_sync(FULL, i, x), __shfl_sync(FULL, y, x));
     }
