@@ -20,9 +20,11 @@
 // shared with others and go to scratch as parts, which a last kernel joins.
 //
 // bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes, or below 64 values).  fp32 rows are split into
-// two fp16 numbers each, hi + lo, after a multiplication by a power of two that puts the matrix's largest magnitude below 2^14: 22 bits for what
-// is within 2^-17 of the largest, and a product takes three passes (hi hi, hi lo, lo hi).  Weights are split the same way, in units that put the
-// largest near 2^15.
+// two fp16 numbers each, hi + lo, after a multiplication by a power of two that puts the matrix's largest magnitude (of roots that take part and nodes in
+// sight) below 2^14: 22 bits for what is within 2^-16 of the largest, 2^-38 of the largest for what is smaller, and a product takes three passes (hi hi,
+// hi lo, lo hi).  So a logit is off by 2^-37 scale dim times both largest at most; where that could pass 2^-20 (logits beyond 10^5, which a row or a
+// root far larger than all others gives) every product is formed in fp32 instead, by the last kernels, which is slow.  Weights are split the same way, in
+// units that put the largest near 2^15.
 #include <cuda.h>
 
 #include "tgnn_table.cuh"
@@ -85,19 +87,24 @@ __device__ __forceinline__ int64_t target_of(const Prep& a, int64_t i) {
 __device__ __forceinline__ float value_of(const void* p, int dtype, int64_t i) {
   return dtype == TGNN_F32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
 }
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers from 0; a division of 64 bits takes five times as long
+  return (((uint64_t)a | (uint64_t)b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // A bias in units of log 2; finite ones stay finite.
 __device__ __forceinline__ float bias2(float b) {
   const float x = b * kLog2e;
   return b > -INFINITY ? fmaxf(x, kLowest) : x;
 }
 
-// 2^e such that a magnitude up to `top` times it is at most 2^14.
+// 2^e such that a magnitude up to `top` times it is at most 2^14 (e to 110: of matrices below 2^-97 fewer bits are kept).
 __device__ __forceinline__ float unit_of(float top) {
   if (!(top > 0.f)) return 1.f;
   int e;
-  frexpf(fminf(top, 3e38f), &e);
-  return ldexpf(1.f, max(-110, min(110, 14 - e)));
+  frexpf(fminf(top, 3.4e38f), &e);
+  return ldexpf(1.f, min(110, 14 - e));
 }
+// What a product of rows in their units is multiplied by to be a logit in units of log 2 (in fp64: a scale beside large rows may be subnormal).
+__device__ __forceinline__ float factor_of(float scale, float uq, float ut) { return (float)((double)scale * 1.4426950408889634 / uq / ut); }
 // The largest of the partial maxima of each kind, by a warp; all asked for together.
 __device__ __forceinline__ void largest(const float* parts, int used, float (&x)[4]) {
 #pragma unroll
@@ -129,11 +136,32 @@ __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
   if (blockIdx.x > 0) {
     const int b = blockIdx.x - 1, nb = gridDim.x - 1;
     float top[4] = {0.f, 0.f, 0.f, -INFINITY};
-    const int64_t values = a.s.planes == 2 ? a.s.rows * a.s.dim : 0;
+    const int64_t values = a.s.planes == 2 ? a.s.rows * a.s.dim : 0, stride = (int64_t)nb * 1024;
     if (!a.backward && a.bias)
       for (int64_t i = (int64_t)b * 1024 + t; i < a.s.rows; i += (int64_t)nb * 1024) top[3] = fmaxf(top[3], a.bias[i]);
-    for (int64_t i = (int64_t)b * 1024 + t; i < values; i += (int64_t)nb * 1024)
-      top[1] = fmaxf(top[1], fabsf(static_cast<const float*>(a.table)[i]));
+    if (values > 0) {                                    // (nodes in sight: what a hidden one's row holds is not to cost the others bits)
+      const int64_t rows_on = quotient(stride, a.s.dim);
+      const int columns_on = (int)(stride - rows_on * a.s.dim);
+      int64_t i = (int64_t)b * 1024 + t, row = quotient(i, a.s.dim);
+      int column = (int)(i - row * a.s.dim);
+      while (i < values) {                               // four at a time, asked for together
+        float x[4], hide[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = i < values ? static_cast<const float*>(a.table)[i] : 0.f;
+          hide[k] = a.bias && i < values ? a.bias[row] : 0.f;
+          i += stride;
+          row += rows_on;
+          column += columns_on;
+          if (column >= a.s.dim) {
+            column -= a.s.dim;
+            ++row;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[1] = fmaxf(top[1], hide[k] != -INFINITY ? fabsf(x[k]) : 0.f);
+      }
+    }
     for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n && a.s.planes == 2; r += (int64_t)nb * 32) {
       const int64_t y = target_of(a, r);
       if (y < 0 || y >= a.s.rows) continue;
@@ -156,10 +184,10 @@ __global__ void __launch_bounds__(1024) begin_kernel(const Prep a) {
       for (int64_t r = (int64_t)b * 32 + warp; r < a.s.n; r += (int64_t)nb * 32) {
         const int64_t y = target_of(a, r);
         const bool in = y >= 0 && y < a.s.rows;
-        const float g = in ? a.dloss[r] * a.scale : 0.f;
+        const double g = in ? (double)a.dloss[r] * a.scale : 0.0;
         for (int c = lane; c < a.s.dim; c += 32) {
           const int64_t x = r * a.s.dim + c;
-          const float v = in ? g * a.kept[3 * a.s.n + x] : 0.f;
+          const float v = in ? (float)(g * a.kept[3 * a.s.n + x]) : 0.f;
           if (a.dtype == TGNN_F32) static_cast<float*>(a.dq)[x] = v;
           else static_cast<__nv_bfloat16*>(a.dq)[x] = __float2bfloat16_rn(v);
         }
@@ -225,8 +253,11 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
     ut = unit_of(x[1]);
     if (a.backward) ug = 2.f * unit_of(x[2]);            // |g| up to 2^15
   }
-  if (blockIdx.x == 0 && t == 0) *reinterpret_cast<float4*>(a.parts + 4 * kMaxParts) = make_float4(uq, ut, ug, bias2(x[3]));
   const int dp = a.s.dp, dim = a.s.dim;
+  if (blockIdx.x == 0 && t == 0) {
+    const float mark = split && fabsf(a.scale) * x[0] * x[1] * (float)dim > 131072.f ? -1.f : 1.f;      // both below 0: products are to be formed in fp32
+    *reinterpret_cast<float4*>(a.parts + 4 * kMaxParts) = make_float4(mark * uq, mark * ut, ug, bias2(x[3]));
+  }
   auto operand = [&](const void* src, int64_t row, uint16_t* to, float unit) {     // a row, 2 values at a time
     for (int c = 2 * lane; c < dp; c += 64) {
       float x = 0.f, y = 0.f;
@@ -249,7 +280,7 @@ __global__ void __launch_bounds__(256) prep_kernel(const Prep a) {
   const int64_t wide = (int64_t)a.s.planes * dp;
   for (int64_t i = worker; i < padded; i += workers) operand(a.q, i < live ? a.act[i] : -1, a.qp + i * wide, uq);
   if (a.copy_table)
-    for (int64_t i = worker; i < a.s.rows; i += workers) operand(a.table, i, a.tp + i * wide, ut);
+    for (int64_t i = worker; i < a.s.rows; i += workers) operand(a.table, i, a.tp + i * wide, split && a.bias && a.bias[i] == -INFINITY ? 0.f : ut);
   const int64_t thread = (int64_t)blockIdx.x * 256 + t, threads = (int64_t)gridDim.x * 256;
   if (!a.backward) {
     const int64_t cols = up(a.s.rows, a.tile);
@@ -388,9 +419,6 @@ __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers from 0; a division of 64 bits takes five times as long
-  return (((uint64_t)a | (uint64_t)b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
-}
 // The blocks' shares of the tiles: block c has tiles [begin(c), begin(c + 1)), and tile o of group r belongs to block owner(r, o).  Shares are even with
 // `extra` tiles more in front of each group's: what its block needs to write one group and begin the next.
 struct Share {
@@ -673,7 +701,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
       ug = x.z;
       if (MODE != BACKWARD && !MOVING && g.bias) most_bias = x.w;
     }
-    const float factor = g.scale * kLog2e / uq / ut;
+    const float factor = factor_of(g.scale, uq, ut);
     const f32x2 factor2 = pack2(factor, factor);
     const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
     const uint32_t all_cols = (uint32_t)col_tiles, full_tiles = (uint32_t)(t_rows / NT), all_units = tiles * PER;
@@ -1002,7 +1030,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
         ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, abort_flag));
         if (!ok) break;
         fence_after();
-        const float out = MODE == BACKWARD ? g.scale / ug / uq : 1.f;
+        const float out = MODE == BACKWARD ? (float)((double)g.scale / ug / uq) : 1.f;
         const int dim = g.s.dim;
         float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
         float(&o)[32] = z[CH > 1 ? 1 : 0];               // z[0] may hold what was asked for
@@ -1097,6 +1125,7 @@ struct Join {
   const void* q;
   const void* table;
   const float* bias;
+  const float* dloss;
   const void* target;
   int index_bits, dtype, blocks, group, tile;   // blocks of the main kernel, rows of its groups, columns of its tiles (powers of two)
   int group_bits, tile_bits, extra;
@@ -1207,20 +1236,22 @@ struct RootParts {                                        // of the warps that s
   float4 o[W][64];
 };
 
-// A root whose weights do not fit beside their references (or a value that is no number): again, product by product, 32 nodes at a time per warp.
+// A root whose weights do not fit beside their references, or whose products want more bits: again, product by product, 32 nodes at a time per warp.
 template <int W>
 __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, int64_t y) {
   const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31, dim = a.s.dim;
   float M = -INFINITY, l = 0.f, zt = 0.f;
   float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-  const float factor = a.scale * kLog2e;
+  const float2 units = *reinterpret_cast<const float2*>(a.parts + 4 * kMaxParts);      // of equal signs
+  const float uq = units.x, ut = units.y, factor = factor_of(a.scale, uq, ut);
   for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
     const int64_t j = j0 + lane;
     float x = -INFINITY;
     if (j < a.s.rows) {
       float dot = 0.f;
-      for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c), value_of(a.table, a.dtype, j * dim + c), dot);
-      x = fmaf(dot, factor, a.bias ? bias2(a.bias[j]) : 0.f);
+      for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c) * uq, value_of(a.table, a.dtype, j * dim + c) * ut, dot);
+      const float b = a.bias ? bias2(a.bias[j]) : 0.f;
+      x = b == -INFINITY ? b : fmaf(dot, factor, b);
       if (j == y) {
         zt = x;
         x = -INFINITY;
@@ -1300,6 +1331,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   const int pitch = pitch_of(a.s), dim = a.s.dim, od = a.s.od;
   const int64_t step = W == 1 ? (int64_t)gridDim.x * 8 : gridDim.x;
   const float unit = a.parts[4 * kMaxParts + 1];
+  const bool plain = unit < 0.f;
   const float shift = a.s.planes == 2 && dir ? 7.f : 0.f;
   for (int64_t four = W == 1 ? (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5) : blockIdx.x; 4 * four < live; four += step) {
     const int64_t row = 4 * four + which, r = 4 * four >> a.group_bits, in = 4 * four - (r << a.group_bits);
@@ -1427,7 +1459,7 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
     }
     // Done again: where weights below 2^-126 of a reference, which were left out, lie so near the root's sum that they may count; where sums are not trusted,
     // those of the table's rows among them, which can pass fp32 before the weights' do.  (What is no number stays so.)
-    bool lost = high == INFINITY || high > M + log2f(L) + kRoom;
+    bool lost = plain || high == INFINITY || high > M + log2f(L) + kRoom;
     if (dir && warp == 0 && L == L) {
       float size = 0.f;
 #pragma unroll
@@ -1460,9 +1492,49 @@ __global__ void __launch_bounds__(256, 2) join_roots_kernel(const __grid_constan
   }
 }
 
+// Gradients of table rows whose products want more bits than the operands have: product by product, a warp per row, 32 roots at a time.
+__device__ __noinline__ void plain_table(const Join& a, int64_t live, float uq, float ut) {
+  const int lane = threadIdx.x & 31, dim = a.s.dim;
+  const int64_t warps = (int64_t)gridDim.x * gridDim.y * 8, first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const float* table = static_cast<const float*>(a.table);
+  const float factor = factor_of(a.scale, uq, ut);
+  for (int64_t j = first; j < a.s.rows; j += warps) {
+    const float b = a.bias ? bias2(a.bias[j]) : 0.f;
+    float t[8], sum[8], all = 0.f;
+    for (int k = 0; k < 8; ++k) {
+      t[k] = lane + 32 * k < dim && b != -INFINITY ? table[j * dim + lane + 32 * k] * ut : 0.f;
+      sum[k] = 0.f;
+    }
+    for (int64_t x0 = 0; x0 < live; x0 += 32) {
+      float part[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, part_all = 0.f;
+      for (int64_t x = x0; x < min(live, x0 + 32); ++x) {
+        const int64_t i = a.act[x];
+        float q[8], dot = 0.f;
+        for (int k = 0; k < 8; ++k) {
+          q[k] = lane + 32 * k < dim ? static_cast<const float*>(a.q)[i * dim + lane + 32 * k] * uq : 0.f;
+          dot = fmaf(q[k], t[k], dot);
+        }
+        for (int e = 16; e; e >>= 1) dot += __shfl_xor_sync(FULL, dot, e);
+        const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
+        const float g = a.dloss[i];
+        const float w = y == j ? -g * a.kept[2 * a.s.n + i] : g * (exp2f(fmaf(dot, factor, b) - a.kept[i]) * a.kept[a.s.n + i]);
+        part_all += w;
+        for (int k = 0; k < 8; ++k) part[k] = fmaf(w, q[k], part[k]);
+      }
+      all += part_all;
+      for (int k = 0; k < 8; ++k) sum[k] += part[k];
+    }
+    if (a.dtable)
+      for (int k = 0; k < 8; ++k)
+        if (lane + 32 * k < dim) static_cast<float*>(a.dtable)[j * dim + lane + 32 * k] = (float)((double)sum[k] * a.scale / uq);
+    if (a.dbias && lane == 0) a.dbias[j] = all;
+  }
+}
+
 // Groups of table rows that several blocks share: block b takes the group that begins before the boundary between blocks b - 1 and b, if that is the
 // group's first one; grid.y parts of its rows.  Without any live root, zeros everywhere.
-__global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__ Join a) {
+template <bool FP32>
+__global__ void __launch_bounds__(256, 4) join_table_kernel(const __grid_constant__ Join a) {
   chain_wait();
   chain_release();
   const int64_t live = a.count[0];
@@ -1479,6 +1551,12 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
       for (int64_t x = t; x < a.s.rows; x += all) a.dbias[x] = 0.f;
     return;
   }
+  const float4 units = *reinterpret_cast<const float4*>(a.parts + 4 * kMaxParts);
+  const float uq = units.x, ug = units.z, out = (float)((double)a.scale / ug / uq);
+  if (FP32 && uq < 0.f) {
+    plain_table(a, live, uq, units.y);
+    return;
+  }
   const int64_t col_tiles = (live + a.tile - 1) / a.tile;
   const Share sh((a.s.rows + a.group - 1) / a.group, col_tiles, a.extra, a.blocks);
   const int b = blockIdx.x + 1;
@@ -1487,8 +1565,6 @@ __global__ void __launch_bounds__(256) join_table_kernel(const __grid_constant__
   if (x == r * col_tiles) return;
   const int c0 = sh.owner(r, 0), c1 = sh.owner(r, col_tiles - 1);
   if (b != c0 + 1) return;
-  const float4 units = *reinterpret_cast<const float4*>(a.parts + 4 * kMaxParts);
-  const float uq = units.x, ug = units.z, out = a.scale / ug / uq;
   const int od = a.s.od, chunks = pitch / 4, all = a.group * chunks;
   // the others than the first part are their blocks' first; all in the order in which they lie
   const float4* first = reinterpret_cast<const float4*>(a.slots + (int64_t)slot_of(sh, col_tiles, c0, r) * a.group * pitch);
@@ -1717,6 +1793,7 @@ int run(const Call& a, Chain& c, float* loss, float* kept, const float* dloss, v
   j->q = a.q;
   j->table = a.table;
   j->bias = a.bias;
+  j->dloss = dloss;
   j->target = a.target;
   j->index_bits = a.index_bits;
   j->dtype = a.dtype;
@@ -1791,7 +1868,7 @@ extern "C" TGNN_API int tgnn_destination_loss_backward(const void* q, const void
   if (dtable || dbias) {
     Join j;
     if (int rc = run<BACKWARD>(a, c, nullptr, const_cast<float*>(kept), dloss, dq, dtable, dbias, &j)) return rc;
-    c(join_table_kernel, dim3((unsigned)j.blocks, 8), dim3(256), 0, j);
+    c(dtype == TGNN_F32 ? join_table_kernel<true> : join_table_kernel<false>, dim3((unsigned)j.blocks, 8), dim3(256), 0, j);
   } else if (dq) {
     Prep p = {};
     p.s = shape_of(n, rows, dim, TGNN_BF16);              // no maxima of rows
