@@ -52,17 +52,17 @@ def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: Op
 
 class _DestinationLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, table, bias, target, scale, status):
+    def forward(ctx, q, table, bias, target, scale, status, wanted):
         q, table, target = q.contiguous(), table.contiguous(), target.contiguous()
         bias = None if bias is None else bias.contiguous()
         (n, dim), rows, dev = q.shape, table.shape[0], q.device
         loss = torch.empty(n, device=dev)
-        wanted = any(ctx.needs_input_grad[:3])
         kept = torch.empty(B.destination_loss_kept(n, dim), device=dev) if wanted else None
         scratch = torch.empty(B.destination_loss_scratch(n, rows, dim, q.dtype), dtype=torch.uint8, device=dev)
         status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
         B.destination_loss(q, table, target, loss, scratch, status, bias=bias, kept=kept, scale=scale)
-        ctx.save_for_backward(q, table, bias, target, kept)
+        if wanted:
+            ctx.save_for_backward(q, table, bias, target, kept)
         ctx.scale, ctx.status = scale, status
         return loss
 
@@ -75,15 +75,18 @@ class _DestinationLoss(torch.autograd.Function):
         scratch = torch.empty(B.destination_loss_scratch(q.shape[0], table.shape[0], q.shape[1], q.dtype), dtype=torch.uint8, device=q.device)
         B.destination_loss_backward(q, table, target, kept, dloss.contiguous(), dq, dtable, scratch, ctx.status, bias=bias, dbias=dbias,
                                     scale=ctx.scale)
-        return dq, dtable, dbias, None, None, None
+        return dq, dtable, dbias, None, None, None, None
 
 
 def destination_loss(q: torch.Tensor, table: torch.Tensor, target: torch.Tensor, bias: Optional[torch.Tensor] = None,
                      scale: Optional[float] = None, status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Cross entropy [n] (fp32) of target [n] among all rows of table [rows, dim] for q [n, dim]: logits scale * q . row + bias, scale 1 / sqrt(dim) by
-    default.  A target below 0 takes no part: loss 0, no gradient.  Differentiable in q, table and bias; fp32 or bf16 rows, bias fp32.
+    default.  A target below 0 takes no part: loss 0, no gradient.  Differentiable in q, table and bias; fp32 or bf16 rows, bias fp32.  Where no gradient
+    can be asked for (torch.no_grad(), no leaf that wants one) the loss alone is computed, and nothing kept.
     status: int32 [1], set to 4 where a target is beyond the table (which takes no part either)."""
-    return _DestinationLoss.apply(q, table, bias, target, scale, status)
+    # asked here: inside a Function the grad mode is off, and needs_input_grad does not go by it
+    wanted = torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, table, bias))
+    return _DestinationLoss.apply(q, table, bias, target, scale, status, wanted)
 
 
 class AdamW:
