@@ -56,6 +56,7 @@ def hold(x: np.ndarray, L: int, a: np.ndarray):
 def step(s: State, p: np.ndarray, grad: np.ndarray, t: int, tensor: int, lr, b1, b2, eps, decay, grad_scale, seed):
     """The new parameters in fp64 from p (fp64), and the largest step that the parts of m and the decay could add up to; s is advanced."""
     g = grad.astype(f32) * f32(grad_scale)
+    b1, b2 = float(f32(b1)), float(f32(b2))                          # one number throughout: 1 - b belongs to the powers of b
     n1, n2 = f32(1) - f32(b1), f32(1) - f32(b2)
     m = s.m * f32(b1) + g * n1
     v = s.v * f32(b2) + (g * n2) * g

@@ -382,8 +382,9 @@ extern "C" TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, i
   int64_t values;
   int used;
   if (int rc = check(who, tensors_host, count, state_bits, false, &values, &used, err, err_size)) return rc;
-  if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(grad_scale - grad_scale == 0))
-    return fail(err, err_size, TGNN_EINVAL, "%s: lr >= 0, 0 <= beta < 1, eps >= 0 and a finite grad_scale are needed", who);
+  const float b1 = (float)beta1, b2 = (float)beta2;
+  if (!(lr >= 0) || !(beta1 >= 0 && b1 < 1.f) || !(beta2 >= 0 && b2 < 1.f) || !(eps >= 0) || !(grad_scale - grad_scale == 0))
+    return fail(err, err_size, TGNN_EINVAL, "%s: lr >= 0, 0 <= beta < 1 (in fp32, too), eps >= 0 and a finite grad_scale are needed", who);
   if (!steps || ((uintptr_t)steps & 7)) return fail(err, err_size, TGNN_EINVAL, "%s: steps is null or not 8-byte aligned", who);
   if (values == 0) return TGNN_OK;
   const int per = per_chunk_of(values, state_bits);
@@ -391,15 +392,15 @@ extern "C" TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, i
   auto fill = [&](auto& a) {
     a.steps = steps;
     a.seed = seed;
-    a.b1 = beta1;
-    a.b2 = beta2;
+    a.b1 = b1;                                 // one number in the moments and in their corrections: with 0.9999 in fp64 there, 1 - beta would be 1.7e-4 off
+    a.b2 = b2;
     a.eps = eps;
     a.lr = (float)lr;
     a.grad_scale = (float)grad_scale;
-    a.b1f = (float)beta1;
-    a.b2f = (float)beta2;
-    a.n1 = 1.f - a.b1f;
-    a.n2 = 1.f - a.b2f;
+    a.b1f = b1;
+    a.b2f = b2;
+    a.n1 = 1.f - b1;                           // exact from 0.5 on
+    a.n2 = 1.f - b2;
   };
   for (int from = 0; from < used;) {
     c.first = true;                            // launches of one step touch different tensors, and the counter in stream order
