@@ -137,6 +137,8 @@ class AdamW:
         grads = [p.grad for p in self.params] if grads is None else grads if type(grads) is list else list(grads)
         B.adamw_step(self._t, self.bits, self.device.index, self.steps, self.params, grads, self.lr, self.betas[0], self.betas[1], self.eps,
                      grad_scale, self.seed)
+        # written by address: autograd is told, so that a backward pass over a graph from before the step is an error and not one over the new values
+        torch.autograd.graph.increment_version([x for p, c, g in zip(self.params, self.copies, grads) if g is not None for x in (p, c) if x is not None])
 
     def moments(self) -> Tuple[List[torch.Tensor], List[torch.Tensor]]:
         """First and second moments as fp32 values: the state itself in 32 bits, else tensors that the next call overwrites."""
