@@ -148,18 +148,23 @@ __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__
   __shared__ float s_c1, s_c2;
   __shared__ uint64_t s_salt;
   if (threadIdx.x == 0) {
-    const int64_t t = *reinterpret_cast<volatile int64_t*>(a.steps) + 1;
-    if (a.blocks > 0) {
-      // the last block to have read the counter advances it: the others do not look at it again
-      const unsigned long long before = atomicAdd(reinterpret_cast<unsigned long long*>(a.steps + 1), 1ull);
-      if (before == a.blocks - 1) {
-        a.steps[0] = t;
-        a.steps[1] = 0;
-      }
-    }
+    volatile int64_t* const steps = a.steps;
+    const int64_t t = steps[0] + 1;
+    // The last block to have read the counter advances it: the others do not look at it again.  What a block announces is made of what it read (1 for any
+    // number of steps), and what the last one writes of what it was told: a value cannot be its own cause, so no block reads the new one.
+    unsigned long long before = 0;
+    if (a.blocks > 0)
+      asm volatile("{\n\t.reg .u64 one;\n\tshr.u64 one, %2, 63;\n\tadd.u64 one, one, 1;\n\tatom.add.gpu.global.u64 %0, [%1], one;\n\t}"
+                   : "=l"(before)
+                   : "l"(a.steps + 1), "l"(t)
+                   : "memory");
     s_c1 = (float)(1.0 / one_minus_power(a.b1, t));
     s_c2 = (float)rsqrt(one_minus_power(a.b2, t));
     s_salt = a.seed ^ ((uint64_t)t * 0x9E3779B97F4A7C15ull);
+    if (a.blocks > 0 && before == a.blocks - 1) {
+      steps[0] = t;
+      steps[1] = 0;
+    }
   }
   int lo = 0, hi = a.count - 1;               // the tensor of this chunk: the first whose chunks end behind it
   while (lo < hi) {
