@@ -3,6 +3,7 @@
 The link head scores an event against one sampled negative; here a root answers with a distribution over all nodes, whose rows are
 learned, and the same table gives the rows of neighbor slots.  All under autograd, without a row of logits in memory.
 
+    status()                           what calls of the two below without a status tensor have met on the device
     lookup(table, ids)                 tgnn_lookup, its gradient by tgnn_lookup_backward
     destination_loss(q, table, target) tgnn_destination_loss, its gradients by tgnn_destination_loss_backward
     AdamW(params, ...)                 tgnn_adamw_step: all tensors in one launch, moments in 32 or 8 bits
@@ -13,7 +14,7 @@ All arithmetic happens inside the library, but the sum of a root's own row and w
 from __future__ import annotations
 
 import ctypes as C
-from typing import List, Optional, Sequence, Tuple, Union
+from typing import Dict, List, Optional, Sequence, Tuple, Union
 
 import torch
 
@@ -21,12 +22,39 @@ from . import binding as B
 from .history import Slots, TimeBias, slot_attention
 
 
+_flags: Dict[int, torch.Tensor] = {}
+
+
+def _flag(device: torch.device) -> torch.Tensor:
+    """Where calls without a status of their own record what goes wrong on the device.  (A call that is captured before any other has come is given one that
+    lives in its graph, and that nobody reads.)"""
+    flag = _flags.get(device.index)
+    if flag is None:
+        with torch.inference_mode(False):
+            flag = torch.zeros(1, dtype=torch.int32, device=device)
+        if device.type == "cuda" and not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream(device).synchronize()      # it is zero before a call on any stream gets it
+            _flags[device.index] = flag
+    return flag
+
+
+def status(device: Union[torch.device, int, None] = None, clear: bool = False) -> int:
+    """0, or what lookups and destination losses without a status of their own have met on the device (the current one by default) since it was last cleared: 4
+    for an id or a target beyond its table (which counts as none), TGNN_ETIMEOUT where results are worthless.  Reads the device."""
+    index = torch.cuda.current_device() if device is None else device if isinstance(device, int) else torch.device(device).index
+    flag = _flags.get(torch.cuda.current_device() if index is None else index)
+    code = 0 if flag is None else int(flag.item())
+    if clear and code:
+        flag.zero_()
+    return code
+
+
 class _Lookup(torch.autograd.Function):
     @staticmethod
     def forward(ctx, table, ids, scale, dtype, status):
         table, ids = table.contiguous(), ids.contiguous()
         out = torch.empty((*ids.shape, table.shape[1]), dtype=dtype, device=table.device)
-        status = torch.zeros(1, dtype=torch.int32, device=table.device) if status is None else status
+        status = _flag(table.device) if status is None else status
         B.lookup(table, ids, out, status, scale=scale)
         ctx.save_for_backward(ids)
         ctx.like, ctx.scale, ctx.status = (table.shape, table.dtype), scale, status
@@ -46,7 +74,7 @@ class _Lookup(torch.autograd.Function):
 def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: Optional[torch.dtype] = None,
            status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """scale * table[ids] as [*ids.shape, dim] of `dtype` (the table's own by default), zeros where an id is below 0; differentiable in the table.
-    status: int32 [1], set to 4 where an id is beyond the table (such a row is zeros, too)."""
+    status: int32 [1], set to 4 where an id is beyond the table (such a row is zeros, too); without one, status() tells."""
     return _Lookup.apply(table, ids, float(scale), table.dtype if dtype is None else dtype, status)
 
 
@@ -59,7 +87,7 @@ class _DestinationLoss(torch.autograd.Function):
         loss = torch.empty(n, device=dev)
         kept = torch.empty(B.destination_loss_kept(n, dim), device=dev) if wanted else None
         scratch = torch.empty(B.destination_loss_scratch(n, rows, dim, q.dtype), dtype=torch.uint8, device=dev)
-        status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
+        status = _flag(dev) if status is None else status
         B.destination_loss(q, table, target, loss, scratch, status, bias=bias, kept=kept, scale=scale)
         if wanted:
             ctx.save_for_backward(q, table, bias, target, kept)
@@ -83,7 +111,7 @@ def destination_loss(q: torch.Tensor, table: torch.Tensor, target: torch.Tensor,
     """Cross entropy [n] (fp32) of target [n] among all rows of table [rows, dim] for q [n, dim]: logits scale * q . row + bias, scale 1 / sqrt(dim) by
     default.  A target below 0 takes no part: loss 0, no gradient.  Differentiable in q, table and bias; fp32 or bf16 rows, bias fp32.  Where no gradient
     can be asked for (torch.no_grad(), no leaf that wants one) the loss alone is computed, and nothing kept.
-    status: int32 [1], set to 4 where a target is beyond the table (which takes no part either)."""
+    status: int32 [1], set to 4 where a target is beyond the table (which takes no part either); without one, status() tells."""
     # asked here: inside a Function the grad mode is off, and needs_input_grad does not go by it
     wanted = torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in (q, table, bias))
     return _DestinationLoss.apply(q, table, bias, target, scale, status, wanted)
