@@ -633,7 +633,8 @@ TGNN_API int tgnn_lookup_backward(const void* ids, int index_bits, int64_t n, co
 /* tgnn_adamw_step: one AdamW step of all tensors, t = steps[0] + 1:
  *   g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + ((1 - beta2) g) g
  *   param -= lr * (weight_decay * param + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
- * beta1 and beta2 are rounded to fp32 first, and have to be below 1 as such; the powers are formed in fp64.
+ * beta1 and beta2 are rounded to fp32 first, and have to be below 1 as such; the powers are formed in fp64.  eps: 0 (a value without any gradient is then
+ * 0 / 0, no number), or 2^-126 at least.
  * param: fp32; grad: fp32, bf16 or fp16; copy: bf16 or fp16, the new parameters rounded, or NULL.  tensors_host is read during the call only
  * (it travels as kernel parameters; a captured call keeps its addresses, and lr and the other numbers as they were).
  * steps: device int64[2], zeros at first: steps taken, and a word of the library's; advanced by the call.  Calls on one `steps` do not overlap.

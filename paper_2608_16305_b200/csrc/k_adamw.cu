@@ -390,6 +390,8 @@ extern "C" TGNN_API int tgnn_adamw_step(const tgnn_adamw_tensor* tensors_host, i
   const float b1 = (float)beta1, b2 = (float)beta2;
   if (!(lr >= 0) || !(beta1 >= 0 && b1 < 1.f) || !(beta2 >= 0 && b2 < 1.f) || !(eps >= 0) || !(grad_scale - grad_scale == 0))
     return fail(err, err_size, TGNN_EINVAL, "%s: lr >= 0, 0 <= beta < 1 (in fp32, too), eps >= 0 and a finite grad_scale are needed", who);
+  if (eps > 0 && !((float)eps >= 1.17549435e-38f))         // the quotient's reciprocal takes what is smaller for 0: a value without gradients would be 0 / 0
+    return fail(err, err_size, TGNN_EINVAL, "%s: eps is below the smallest normal number of fp32 and not 0", who);
   if (!steps || ((uintptr_t)steps & 7)) return fail(err, err_size, TGNN_EINVAL, "%s: steps is null or not 8-byte aligned", who);
   if (values == 0) return TGNN_OK;
   const int per = per_chunk_of(values, state_bits);
