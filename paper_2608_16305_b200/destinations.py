@@ -157,6 +157,10 @@ class AdamW:
                                            self.m_scale[i].data_ptr() if bits == 8 else None, self.v_scale[i].data_ptr() if bits == 8 else None,
                                            None if c is None else c.data_ptr(), p.numel(), decay[i], 0,
                                            B.TGNN_F16 if c is not None and c.dtype == torch.float16 else B.TGNN_BF16, 0)
+        # a thread block may be at any place of any tensor when another one writes
+        spans = sorted((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()) for x in self.params + self.copies if x is not None and x.numel() > 0)
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("AdamW: a tensor is given twice, or parameters or copies overlap")
         self._values = None
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, grad_scale: float = 1.0) -> None:
