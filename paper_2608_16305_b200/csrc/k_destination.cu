@@ -103,8 +103,9 @@ __device__ __forceinline__ float unit_of(float top) {
   frexpf(fminf(top, 3.4e38f), &e);
   return ldexpf(1.f, min(110, 14 - e));
 }
-// What a product of rows in their units is multiplied by to be a logit in units of log 2 (in fp64: a scale beside large rows may be subnormal).
-__device__ __forceinline__ float factor_of(float scale, float uq, float ut) { return (float)((double)scale * 1.4426950408889634 / uq / ut); }
+// What a product of rows in their units (powers of two, whose reciprocals are exact) is multiplied by to be a logit in units of log 2.  In fp64: a scale beside
+// large rows may be subnormal.
+__device__ __forceinline__ float factor_of(float scale, float uq, float ut) { return (float)((double)scale * 1.4426950408889634 * __frcp_rn(uq) * __frcp_rn(ut)); }
 // The largest of the partial maxima of each kind, by a warp; all asked for together.
 __device__ __forceinline__ void largest(const float* parts, int used, float (&x)[4]) {
 #pragma unroll
@@ -787,7 +788,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               return top;
             };
             // The reference of a row's weights.  Where it can move: the maximum of the first unit in which the row sees anything.  Else, for good, the maximum
-            // of the first unit (the target's apart); where biases hide most of that unit it would lie far below the others, and the largest product plus the
+            // of the first unit (the target's apart); where biases hide most of that unit it would lie far below the others, and the largest product there plus the
             // largest bias of all is taken: right within the products' spread, whatever the biases hide.  A row for which neither is right is seen by the
             // last kernel, in its sums, and done again there.
             if (MOVING ? (bool)__any_sync(FULL, m == -INFINITY) : t == 0 && sub == 0) {
@@ -800,19 +801,14 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
                 top = fmaxf(top, s_m[part ^ 1][grp][lane_row]);
                 if (m == -INFINITY) m = top;
               } else {
-                const int there = (int32_t)t_rows - (int32_t)(j * NT + sub * U + part * NC);   // columns that are nodes
                 have = false;
                 float seen = -INFINITY, product = -INFINITY;
                 for (int c = 0; c < NC; c += 32) {
                   TMEM_LD32(z[0], 0, s_addr + c);
                   WAIT_LD32(z[0]);
-                  if (biased && (any_hit || j >= full_tiles)) {
-                    __syncwarp();                        // (a branch)
+                  if (biased) {                          // (the zeros behind the table's end among them)
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) product = hit == c + k || c + k >= there ? product : fmaxf(product, z[0][k] * factor);
-                  } else if (biased) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) product = fmaxf(product, z[0][k] * factor);
+                    for (int k = 0; k < 32; ++k) product = hit == c + k ? product : fmaxf(product, z[0][k] * factor);
                   }
                   logits(z[0], c, 0.f);
 #pragma unroll
@@ -1030,7 +1026,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
         ok = __all_sync(FULL, mbar_wait(bar_pv + 8 * ((u - 1) & 1), ((u - 1) >> 1) & 1, abort_flag));
         if (!ok) break;
         fence_after();
-        const float out = MODE == BACKWARD ? (float)((double)g.scale / ug / uq) : 1.f;
+        const float out = MODE == BACKWARD ? (float)((double)g.scale * __frcp_rn(ug) * __frcp_rn(uq)) : 1.f;
         const int dim = g.s.dim;
         float* home = MODE == FORWARD && alone && valid ? g.kept + 3 * g.s.n + (int64_t)g.act[row] * dim : nullptr;
         float(&o)[32] = z[CH > 1 ? 1 : 0];               // z[0] may hold what was asked for
@@ -1526,7 +1522,7 @@ __device__ __noinline__ void plain_table(const Join& a, int64_t live, float uq, 
     }
     if (a.dtable)
       for (int k = 0; k < 8; ++k)
-        if (lane + 32 * k < dim) static_cast<float*>(a.dtable)[j * dim + lane + 32 * k] = (float)((double)sum[k] * a.scale / uq);
+        if (lane + 32 * k < dim) static_cast<float*>(a.dtable)[j * dim + lane + 32 * k] = (float)((double)sum[k] * a.scale * __frcp_rn(uq));
     if (a.dbias && lane == 0) a.dbias[j] = all;
   }
 }
@@ -1552,7 +1548,7 @@ __global__ void __launch_bounds__(256, 4) join_table_kernel(const __grid_constan
     return;
   }
   const float4 units = *reinterpret_cast<const float4*>(a.parts + 4 * kMaxParts);
-  const float uq = units.x, ug = units.z, out = (float)((double)a.scale / ug / uq);
+  const float uq = units.x, ug = units.z, out = (float)((double)a.scale * __frcp_rn(ug) * __frcp_rn(uq));
   if (FP32 && uq < 0.f) {
     plain_table(a, live, uq, units.y);
     return;
