@@ -105,7 +105,7 @@ __device__ __forceinline__ float unit_of(float top) {
 }
 // What a product of rows in their units (powers of two, whose reciprocals are exact) is multiplied by to be a logit in units of log 2.  In fp64: a scale beside
 // large rows may be subnormal.
-__device__ __forceinline__ float factor_of(float scale, float uq, float ut) { return (float)((double)scale * 1.4426950408889634 * __frcp_rn(uq) * __frcp_rn(ut)); }
+__device__ __forceinline__ double factor_of(float scale, float uq, float ut) { return (double)scale * 1.4426950408889634 * __frcp_rn(uq) * __frcp_rn(ut); }
 // The largest of the partial maxima of each kind, by a warp; all asked for together.
 __device__ __forceinline__ void largest(const float* parts, int used, float (&x)[4]) {
 #pragma unroll
@@ -702,7 +702,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
       ug = x.z;
       if (MODE != BACKWARD && !MOVING && g.bias) most_bias = x.w;
     }
-    const float factor = factor_of(g.scale, uq, ut);
+    const float factor = (float)factor_of(g.scale, uq, ut);
     const f32x2 factor2 = pack2(factor, factor);
     const bool biased = g.bias != nullptr, summed = g.dbias != nullptr;
     const uint32_t all_cols = (uint32_t)col_tiles, full_tiles = (uint32_t)(t_rows / NT), all_units = tiles * PER;
@@ -1239,7 +1239,8 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
   float M = -INFINITY, l = 0.f, zt = 0.f;
   float4 o[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
   const float2 units = *reinterpret_cast<const float2*>(a.parts + 4 * kMaxParts);      // of equal signs
-  const float uq = units.x, ut = units.y, factor = factor_of(a.scale, uq, ut);
+  const float uq = units.x, ut = units.y;
+  const double factor = factor_of(a.scale, uq, ut);     // (beyond fp32 where the largest logits are: others need not be)
   for (int64_t j0 = 32ll * warp; j0 < a.s.rows; j0 += 32 * W) {
     const int64_t j = j0 + lane;
     float x = -INFINITY;
@@ -1247,7 +1248,7 @@ __device__ __noinline__ void redo_root(const Join& a, RootParts<W>* s, int i, in
       float dot = 0.f;
       for (int c = 0; c < dim; ++c) dot = fmaf(value_of(a.q, a.dtype, (int64_t)i * dim + c) * uq, value_of(a.table, a.dtype, j * dim + c) * ut, dot);
       const float b = a.bias ? bias2(a.bias[j]) : 0.f;
-      x = b == -INFINITY ? b : fmaf(dot, factor, b);
+      x = b == -INFINITY ? b : (float)(dot * factor + b);
       if (j == y) {
         zt = x;
         x = -INFINITY;
@@ -1493,7 +1494,7 @@ __device__ __noinline__ void plain_table(const Join& a, int64_t live, float uq, 
   const int lane = threadIdx.x & 31, dim = a.s.dim;
   const int64_t warps = (int64_t)gridDim.x * gridDim.y * 8, first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 8 + (threadIdx.x >> 5);
   const float* table = static_cast<const float*>(a.table);
-  const float factor = factor_of(a.scale, uq, ut);
+  const double factor = factor_of(a.scale, uq, ut);
   for (int64_t j = first; j < a.s.rows; j += warps) {
     const float b = a.bias ? bias2(a.bias[j]) : 0.f;
     float t[8], sum[8], all = 0.f;
@@ -1513,7 +1514,7 @@ __device__ __noinline__ void plain_table(const Join& a, int64_t live, float uq, 
         for (int e = 16; e; e >>= 1) dot += __shfl_xor_sync(FULL, dot, e);
         const int64_t y = a.index_bits == 64 ? static_cast<const int64_t*>(a.target)[i] : static_cast<const int32_t*>(a.target)[i];
         const float g = a.dloss[i];
-        const float w = y == j ? -g * a.kept[2 * a.s.n + i] : g * (exp2f(fmaf(dot, factor, b) - a.kept[i]) * a.kept[a.s.n + i]);
+        const float w = y == j ? -g * a.kept[2 * a.s.n + i] : g * (exp2f((float)(dot * factor + b) - a.kept[i]) * a.kept[a.s.n + i]);
         part_all += w;
         for (int k = 0; k < 8; ++k) part[k] = fmaf(w, q[k], part[k]);
       }

@@ -83,3 +83,15 @@ def test_a_root_without_numbers_is_alone_with_them():
         assert not any(bool(torch.isfinite(out[k][7])) for k in ("loss", "alone"))     # infinite where the target's product alone is -infinity
         check(x | dict(q=x["q"][some], target=x["target"][some], g=x["g"][some]), {k: out[k][some] for k in ("loss", "alone", "dq")})
     assert bool(torch.isfinite(clean["loss"]).all())
+
+
+def test_logits_beyond_fp32_beside_others():
+    """A root whose logits are infinite has no numbers; one of zeros, beside it, has all nodes alike."""
+    x = make(20, 100, 16, F32, bias=False, masked=0.0)
+    x["q"] *= 2.0 ** 120
+    x["table"] *= 2.0 ** 110
+    x["q"][4:] = 0.0
+    x["scale"] = 1.0
+    out = call(x, ())
+    for k in ("loss", "alone"):
+        assert not bool(torch.isfinite(out[k][:4]).any()) and float((out[k][4:] - math.log(100)).abs().max()) < 1e-5
