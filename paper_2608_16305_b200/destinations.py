@@ -9,7 +9,8 @@ learned, and the same table gives the rows of neighbor slots.  All under autogra
     AdamW(params, ...)                 tgnn_adamw_step: all tensors in one launch, moments in 32 or 8 bits
     DestinationModel(workload, ...)    all three over a workload's batches, with the attention over sampled slots between them
 
-All arithmetic happens inside the library, but the sum of a root's own row and what it attends to.
+All arithmetic happens inside the library, but the sum of a root's own row and what it attends to, and autograd's sums of the table's three gradients (roots, slots,
+answers; in the table's type, so that a bf16 table's are rounded twice more).
 """
 from __future__ import annotations
 
@@ -120,10 +121,11 @@ def destination_loss(q: torch.Tensor, table: torch.Tensor, target: torch.Tensor,
 class AdamW:
     """AdamW over all of `params` (fp32 CUDA tensors, contiguous, on one device) in one launch, moments in 32 or 8 bits.
 
-    m, v        the moments, a list each: fp32, or int8 / uint8 codes with m_scale, v_scale (one fp32 per 256 values)
+    m, v        the moments, a list each: fp32, or int8 / uint8 codes with m_scale, v_scale (one fp32 per 256 values); saved moments are copied into them
     steps       int64 [2]; the first is the number of steps taken (set it when moments are loaded)
     copies      16-bit tensors (or None) that the new parameters are written to as well, e.g. the table that a bf16 loss reads
     weight_decay  one number, or one per tensor
+    Betas are rounded to fp32; eps is 0 or a normal number of fp32; no two of parameters and copies may overlap.
     A step captured into a graph keeps lr and the addresses of parameters and gradients."""
 
     def __init__(self, params: Sequence[torch.Tensor], lr: float = 1e-3, betas: Tuple[float, float] = (0.9, 0.999), eps: float = 1e-8,
@@ -161,7 +163,11 @@ class AdamW:
         spans = sorted((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()) for x in self.params + self.copies if x is not None and x.numel() > 0)
         if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
             raise ValueError("AdamW: a tensor is given twice, or parameters or copies overlap")
+        self._all = self._written(self.params)
         self._values = None
+
+    def _written(self, grads) -> List[torch.Tensor]:
+        return [x for p, c, g in zip(self.params, self.copies, grads) if g is not None for x in (p, c) if x is not None]
 
     def step(self, grads: Optional[Sequence[Optional[torch.Tensor]]] = None, grad_scale: float = 1.0) -> None:
         """One step on the gradients given, or on the parameters' own (.grad); a tensor without one stays as it is.  Gradients are multiplied
@@ -170,7 +176,7 @@ class AdamW:
         B.adamw_step(self._t, self.bits, self.device.index, self.steps, self.params, grads, self.lr, self.betas[0], self.betas[1], self.eps,
                      grad_scale, self.seed)
         # written by address: autograd is told, so that a backward pass over a graph from before the step is an error and not one over the new values
-        torch.autograd.graph.increment_version([x for p, c, g in zip(self.params, self.copies, grads) if g is not None for x in (p, c) if x is not None])
+        torch.autograd.graph.increment_version(self._written(grads) if type(None) in map(type, grads) else self._all)
 
     def moments(self) -> Tuple[List[torch.Tensor], List[torch.Tensor]]:
         """First and second moments as fp32 values: the state itself in 32 bits, else tensors that the next call overwrites."""
