@@ -671,6 +671,7 @@ TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count
  *   z[i, j] = scale * q[i] . table[j] + bias[j];   loss[i] = log(sum_j exp z[i, j]) - z[i, target[i]]
  *   q: [n, dim], table: [rows, dim] of `dtype` (TGNN_F32, TGNN_BF16), dense; target of index_bits bits; bias: fp32[rows] or NULL; loss: fp32[n].
  *   target[i] < 0: the root takes no part (a masked event): loss 0, and whatever its row holds touches nothing.  Beyond the table: the same, status 4.
+ *   A row of logits may lie anywhere and span any range: a root whose weights do not fit fp32 is computed again, one product after the other, which is slow.
  *   A bias of -infinity hides a node (its row has to be finite all the same); one of the type's lowest value works as any finite one.  Where the target
  *   is hidden the loss is +infinity; where all nodes are, too, and the root has no gradient.
  *   kept: fp32[tgnn_destination_loss_kept(n, dim)], what the backward pass needs, or NULL where there will be none.
@@ -678,6 +679,7 @@ TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count
  *   dq[i] = scale * sum_j dz[i, j] table[j], dtable[j] = scale * sum_i dz[i, j] q[i] (of `dtype`), dbias[j] = sum_i dz[i, j] (fp32);
  *   each may be NULL where it is not wanted.  Everything asked for is overwritten, in an order fixed by the sizes and the device.  kept as the
  *   forward pass left it, for the same inputs.
+ * bf16 rows are multiplied as they are, sums are fp32; the weights that rows are summed with (p in dq, dz in dtable) are rounded to bf16 first (2^-8 of each).
  * fp32 rows are held in 22 bits (2^-22 of a value, and 2^-38 of the largest one of q's rows that take part or of the table's that are not hidden); where that could
  *   put a logit 2^-20 off or more (scale dim max|q| max|table| > 2^17) every product is formed in fp32 instead, which is slow.  dtable's weights are exact
  *   to 2^-22 of themselves and 2^-40 of the largest |dloss|: what a root with a gradient far below the largest adds has fewer bits.

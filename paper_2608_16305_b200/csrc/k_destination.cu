@@ -19,7 +19,8 @@
 // while weights are formed.  All tiles, in order of A's rows, are split over the blocks: a block's first and last group of rows may be
 // shared with others and go to scratch as parts, which a last kernel joins.
 //
-// bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes, or below 64 values).  fp32 rows are split into
+// bf16 rows are operands as they are (copied where a row is no multiple of 16 bytes, or below 64 values), and weights are rounded to bf16 beside them, once (a
+// product's operands are of one type; 2^-8 of each, as much as the result's own rounding).  fp32 rows are split into
 // two fp16 numbers each, hi + lo, after a multiplication by a power of two that puts the matrix's largest magnitude (of roots that take part and nodes in
 // sight) below 2^14: 22 bits for what is within 2^-16 of the largest, 2^-38 of the largest for what is smaller, and a product takes three passes (hi hi,
 // hi lo, lo hi).  So a logit is off by 2^-37 scale dim times both largest at most; where that could pass 2^-20 (logits beyond 10^5, which a row or a
