@@ -862,6 +862,21 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               unpack2(add2(sum2, sum3), a, b);
               sum = a + b;
             };
+            // The target's own logit apart from a large reference: where a unit's other nodes are hidden that is a mask's value, in which the logit would be lost.
+            // (A fixed reference is none, unless all nodes are hidden.)
+            float own = 0.f;
+            const bool apart = MOVING && any_hit && __any_sync(FULL, fabsf(m) > 64.f);
+            if (apart) {
+              WAIT_LD32(z[0]);
+              for (int c = 0; c < NC; c += 32) {
+                TMEM_LD32(z[0], 0, s_addr + c);
+                WAIT_LD32(z[0]);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) own = hit == c + k ? z[0][k] : own;
+              }
+              if ((uint32_t)hit < (uint32_t)NC) own = fmaf(own, factor, plain ? 0.f : col[hit]);
+              TMEM_LD32(z[0], 0, s_addr);
+            }
             weights();
             // fp16: the reference is moved when the unit's sum says that a weight may have passed what the type holds.  O has then to be multiplied and the
             // weights are formed again.  (Once: what is too large, or no number, then stays so.)
@@ -900,6 +915,7 @@ __global__ void __launch_bounds__(128 + 256 * NH, 1) destination_kernel(const __
               TMEM_LD32(z[0], 0, s_addr);
               weights();
             }
+            if (apart && (uint32_t)hit < (uint32_t)NC) zt = own;
             l += sum;
           } else {
             // roots whose target is one of this warp's rows: -g (1 - p) in place of their weight

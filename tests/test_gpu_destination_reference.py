@@ -82,3 +82,20 @@ def test_a_single_node_in_sight(n, rows, dim, low, dtype):
         x["target"][:] = 70
         out = call(x)
         assert all(bool((v == 0).all()) for v in out.values()), above
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("low", [-math.inf, -1e4, -1e9, torch.finfo(F32).min])
+@pytest.mark.parametrize("n,rows,dim", [(20, 131, 40), (300, 900, 100), (90, 1000, 200)])
+def test_a_target_among_hidden_nodes(n, rows, dim, low, dtype):
+    """The only node in sight of its tile, beside masks of any size: its logit is not lost in theirs."""
+    x = make(n, rows, dim, dtype, masked=0.0)
+    seen = torch.arange(rows, device="cuda") % 128 >= 64
+    seen[rows - 2] = True
+    seen[256:384] = False
+    seen[300:301] = True
+    x["bias"][~seen] = low
+    x["target"][:] = rows - 2
+    if rows > 300:
+        x["target"][::2] = 300
+    check_seen(x, call(x), seen)
