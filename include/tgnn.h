@@ -683,6 +683,7 @@ TGNN_API int tgnn_adamw_moments(const tgnn_adamw_tensor* tensors_host, int count
  * fp32 rows are held in 22 bits (2^-22 of a value, and 2^-38 of the largest one of q's rows that take part or of the table's that are not hidden); where that could
  *   put a logit 2^-20 off or more (scale dim max|q| max|table| > 2^17) every product is formed in fp32 instead, which is slow.  dtable's weights are exact
  *   to 2^-22 of themselves and 2^-40 of the largest |dloss|: what a root with a gradient far below the largest adds has fewer bits.
+ * A weight below 2^-60 of its root's sum, and with fp32 rows in dq one below 2^-32 of the largest one, may count as none.
  * scratch: tgnn_destination_loss_scratch(n, rows, dim, dtype) bytes, in both directions.
  * dim 1 to 256; rows 1 to 2^31 - 2^16, n below 2^31 - 2^16.  No output may alias an input. */
 TGNN_API int64_t tgnn_destination_loss_kept(int64_t n, int dim);
